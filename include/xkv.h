@@ -18,6 +18,8 @@
  *                         rows into a ragged paged cache                             (Alg. 2 steps 5-7)
  *   4. xkv_decode_attn    per generation step: attention over the ragged compacted caches,
  *                         new K/V appended first                                     (Eq. 1; Sec. IV-A, generation phase)
+ *      xkv_plan_append    serving: block tables, slot maps and new lengths of a step, pages taken from a free list
+ *      xkv_store_rows     serving: any number of new K/V rows per sequence stored at their slots
  *
  * Conventions that hold for every entry point
  *   - Plain C types only. "dev" = pointer to device memory of the current CUDA device,
@@ -70,11 +72,16 @@ typedef int32_t xkv_status;
 
 #define XKV_KV_BF16 0
 #define XKV_KV_INT8 1
+#define XKV_KV_E4M3 2
+
+#define XKV_SCALE_BLOCK 16 /* XKV_KV_E4M3: consecutive cache slots that share a scale */
 
 #define XKV_OP_SCORE          0
 #define XKV_OP_SELECT_COMPACT 1
 #define XKV_OP_DECODE_ATTN    2
 #define XKV_OP_PREFILL_ATTN   3
+#define XKV_OP_PLAN_APPEND    4
+#define XKV_OP_STORE_ROWS     5
 
 /* Problem shape shared by the device entry points. */
 typedef struct xkv_dims {
@@ -110,6 +117,20 @@ typedef struct xkv_dims {
  * in (K: on the logits, V: on the weights) and computes in fp16 x fp16 -> fp32: query magnitudes must stay below
  * 65504, and so must 256 * max|v| / 127 of a row. head_dim 64 and 128.
  *
+ * With kv_format = XKV_KV_E4M3 the pages hold 8-bit floats (1 sign, 4 exponent, 3 mantissa bits; no infinities) and one
+ * scale per block of XKV_SCALE_BLOCK slots and KV head,
+ *   k_pages / v_pages : dev uint8 [n_pages][Hkv][page_size][d]
+ *   k_scales / v_scales : dev fp32 [n_pages][Hkv][page_size / 16], powers of two
+ * and a cached value stands for code * scale. The writers (xkv_select_compact, xkv_store_rows, the append of
+ * xkv_decode_attn) choose a block's scale as the smallest power of two s, exponent within [-100, 120], with
+ * max|x| <= 448 s over the finite values of its rows, and a code as x / s rounded to nearest, ties to even; values beyond
+ * 448 s (only infinities are) saturate, a NaN stays a NaN. Rows added to a block that already holds some never shrink its scale; where they
+ * raise it, the earlier rows' codes are re-expressed in the new scale, which is exact except for codes that fall below
+ * 2^-6 (their step is 2^-9). The slots of a block are filled in ascending order: a row stored at the block's first slot
+ * starts the block anew, whatever its scale was. xkv_decode_attn multiplies codes on the tensor cores as they are, with
+ * fp32 accumulation: the query as a sum of two codes (exact for bf16 values within 2^-14 of the row's largest), the
+ * weights as a sum of two codes (2^-8 of a weight, as if rounded to bf16). head_dim 64 and 128.
+ *
  * Head-level budgets (XKV_BUDGET_PER_HEAD) give every KV head of a sequence a cache of its own length. The same
  * structure then describes B*Hkv caches of one KV head each per layer:
  *   k_pages / v_pages : dev bf16 [n_pages][1][page_size][d]
@@ -128,9 +149,9 @@ typedef struct xkv_cache {
   int32_t  page_size;
   int32_t  max_pages_per_seq;
   int32_t  n_pages;
-  float*   k_scales;   /* XKV_KV_INT8 only: dev fp32 [n_pages][Hkv][page_size], one scale per cached row */
+  float*   k_scales;   /* XKV_KV_INT8: dev fp32 [n_pages][Hkv][page_size]; XKV_KV_E4M3: [n_pages][Hkv][page_size / 16] */
   float*   v_scales;
-  int32_t  kv_format;  /* XKV_KV_BF16 (0) or XKV_KV_INT8 */
+  int32_t  kv_format;  /* XKV_KV_BF16 (0), XKV_KV_INT8 or XKV_KV_E4M3 */
   int32_t  reserved;   /* 0 */
 } xkv_cache;
 
@@ -331,6 +352,55 @@ xkv_status xkv_build_block_table(const int32_t* first_page, const int32_t* n_pag
                                  int32_t batch, void* stream);
 
 /*
+ * xkv_plan_append -- the page bookkeeping of a step, on the device (no counterpart in the paper: bookkeeping of the
+ * reduced caches whose sizes differ per layer, Sec. IV-A).
+ *
+ * For every layer l and sequence b, with n = lens_before[l][b] rows cached and a = n_new[l][b] rows to come:
+ *   have = ceil(n / page_size), need = ceil((n + a) / page_size)
+ *   block_table[l][b][have .. need-1] = the next need - have pages of the free list, in the order of (l, b)
+ *   seq_lens[l][b] = n + a
+ *   slots[l][sum of n_new[l][0..b-1] + i] = page * page_size + offset of row n + i, for i < a
+ * It serves a whole batch of prompts (lens_before NULL: block tables from nothing) and a decode step (a = 1) alike.
+ *
+ * cache         block_table, seq_lens, n_layers, page_size, max_pages_per_seq and n_pages are used. Table entries other
+ *               than the new ones stay as they are
+ * n_new         dev int32, row l at n_new + l * n_new_stride; n_new_stride 0: the same counts for every layer, else >= batch
+ * lens_before   dev int32 [n_layers][batch], may be cache->seq_lens itself; NULL: all caches empty
+ * free_pages    dev int32 [n_free], the pages that may be handed out, in the order they are; NULL: pages 0 .. n_free-1
+ * pages_used_before  dev int32 [1], entries of the list handed out so far; NULL: none. pages_used_after: dev out int32
+ *               [1], may be NULL or the same pointer
+ * slots         dev out int64, row l at slots + l * slots_stride; NULL: not wanted. Entries behind a layer's last token
+ *               stay as they are
+ * workspace     dev, at least xkv_workspace_bytes(XKV_OP_PLAN_APPEND, dims.batch = batch, n_layers) bytes, 256-byte aligned
+ * A cache that cannot grow (more rows than max_pages_per_seq pages hold, or the free list ends) keeps its length, gets no
+ * page and its tokens get slot -1; device status XKV_ERR_CAPACITY, also when a layer has more new tokens than
+ * slots_stride. Negative counts are taken as 0 and page ids outside [0, n_pages) give slot -1; device status
+ * XKV_ERR_INVALID_ARG. At most 16384 sequences a layer.
+ */
+xkv_status xkv_plan_append(const xkv_cache* cache, int32_t batch, const int32_t* n_new, int32_t n_new_stride,
+                           const int32_t* lens_before, const int32_t* free_pages, int32_t n_free,
+                           const int32_t* pages_used_before, int32_t* pages_used_after, int64_t* slots,
+                           int64_t slots_stride, void* workspace, size_t workspace_bytes, void* stream);
+
+/*
+ * xkv_store_rows -- stores K and V rows at given slots of the page pool (Sec. IV-A, generation phase, for any number of
+ * new tokens per sequence: newly generated or newly read tokens are stored and never evicted).
+ *
+ * dims          n_kv_heads, head_dim and kv_stride_* are used; cache: the pages, scales, page_size, n_pages, kv_format
+ *               (any); block_table and seq_lens are not touched
+ * k, v          dev bf16, head g of token i at element offset i * kv_stride_token + g * kv_stride_head
+ * slots         dev int64 [n_tokens] as xkv_plan_append writes them; a negative slot skips its token (padding)
+ * A slot occurs at most once in a call. With XKV_KV_E4M3 the tokens of one block follow each other in slot order and
+ * the block's rows before them are in place (what xkv_plan_append's order gives); a token whose slot does not follow its
+ * predecessor's inside a block is not stored, nor is the rest of its run: device status XKV_ERR_INVALID_ARG. A slot
+ * beyond the pool is not stored: device status XKV_ERR_CAPACITY. No slot but the given ones is written, except
+ * that the earlier rows of a block whose scale grows are re-expressed.
+ * workspace     dev, at least xkv_workspace_bytes(XKV_OP_STORE_ROWS, ...) bytes (the status word), 256-byte aligned
+ */
+xkv_status xkv_store_rows(const xkv_dims* dims, const xkv_cache* cache, const void* k, const void* v,
+                          const int64_t* slots, int64_t n_tokens, void* workspace, size_t workspace_bytes, void* stream);
+
+/*
  * xkv_decode_attn -- one generation step of attention over the reduced caches of layers
  * [layer_begin, layer_end) (Eq. 1 with one query row per head; Sec. IV-A generation phase).
  *
@@ -398,7 +468,8 @@ xkv_status xkv_decode_attn_static(const xkv_dims* dims, const xkv_cache* cache, 
 /*
  * Workspace size in bytes for one call of `op` (XKV_OP_*). Unused arguments may be 0.
  *   XKV_OP_SCORE, XKV_OP_SELECT_COMPACT: dims, max_seqlen, total_tokens
- *   XKV_OP_PREFILL_ATTN: dims
+ *   XKV_OP_PREFILL_ATTN, XKV_OP_STORE_ROWS: dims
+ *   XKV_OP_PLAN_APPEND: dims (its batch), n_layers
  *   XKV_OP_DECODE_ATTN: dims, n_layers (layers per call), max_cache_len (upper bound of any
  *                       seq_lens entry, e.g. max_pages_per_seq*page_size), chunk_rows as passed
  * Returns 0 for invalid arguments.

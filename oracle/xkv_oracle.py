@@ -460,3 +460,97 @@ def near_tie(w: np.ndarray, n: int, rel: float = 1e-5) -> bool:
     thr = sort_descending(w)[n - 1]
     band = np.abs(w - thr) <= rel * abs(thr)
     return bool(np.any(band & (w != thr)))
+
+
+# ----------------------------------------------------------------------------------------------
+# Caches of 8-bit floats (1-4-3) with one power-of-two scale per block of 16 slots, and the page bookkeeping of a step
+# (formats and bookkeeping of the library; the paper only says that quantisation is compatible with eviction)
+# ----------------------------------------------------------------------------------------------
+E4M3_MAX = 448.0
+SCALE_BLOCK = 16
+
+
+def e4m3_grid(Y: np.ndarray) -> np.ndarray:
+    """Y on the grid of 1-4-3 floats (float64): nearest, ties to even, saturating at +-448; NaN stays NaN."""
+    Y = np.clip(np.asarray(Y, dtype=np.float64), -E4M3_MAX, E4M3_MAX)
+    _, e = np.frexp(Y)
+    step = np.ldexp(1.0, np.maximum(e - 1, -6) - 3)
+    return np.rint(Y / step) * step
+
+
+def e4m3_values(codes: np.ndarray) -> np.ndarray:
+    """What stored bytes stand for (float64); 0x7f and 0xff are NaN."""
+    c = np.asarray(codes).astype(np.int64)
+    s, e, m = c >> 7, (c >> 3) & 15, c & 7
+    mag = np.where(e == 0, np.ldexp(m.astype(np.float64), -9), np.ldexp(8.0 + m, e - 10))
+    mag = np.where((e == 15) & (m == 7), np.nan, mag)
+    return np.where(s == 1, -mag, mag)
+
+
+def e4m3_block_scale(X: np.ndarray) -> float:
+    """Smallest power of two s, exponent within [-100, 120], with |x| <= 448 s over the finite values of X."""
+    X = np.abs(np.asarray(X, dtype=np.float64))
+    X = X[np.isfinite(X)]
+    top = float(X.max()) if X.size else 0.0
+    e = -100
+    while e < 120 and top > math.ldexp(E4M3_MAX, e):
+        e += 1
+    return math.ldexp(1.0, e)
+
+
+class BlockCache:
+    """One KV head's cached rows of K or of V: appended rows are encoded block by block (16 slots)."""
+
+    def __init__(self, d: int):
+        self.d, self.n = d, 0
+        self.codes = np.zeros((0, d))                 # code values, float64
+        self.scales: list[float] = []
+
+    def append(self, rows: np.ndarray) -> None:
+        rows = np.asarray(rows, dtype=np.float64)
+        while rows.shape[0]:
+            first = self.n % SCALE_BLOCK
+            part, rows = rows[: SCALE_BLOCK - first], rows[SCALE_BLOCK - first:]
+            s = e4m3_block_scale(part)
+            lo = self.n - first
+            if first:
+                was = self.scales[-1]
+                s = max(s, was)
+                self.codes[lo:] = e4m3_grid(self.codes[lo:] * (was / s))
+                self.scales[-1] = s
+            else:
+                self.scales.append(s)
+            self.codes = np.concatenate([self.codes, e4m3_grid(part / s)], 0)
+            self.n += part.shape[0]
+
+    def values(self) -> np.ndarray:
+        return self.codes * np.repeat(np.asarray(self.scales), SCALE_BLOCK)[: self.n, None]
+
+
+def plan_append(n_new, lens_before, table, page_size: int, free_pages, used: int):
+    """The page bookkeeping of a step.  n_new, lens_before [L, B]; table [L, B, max_pages].  Returns (table, lens, slots
+    per layer, used, ok): pages are handed out in the order of (layer, sequence); a cache that cannot grow keeps its
+    length, and once the free list has run short no later cache that asks for pages gets any."""
+    n_new, lens, table = np.asarray(n_new), np.asarray(lens_before).copy(), np.asarray(table).copy()
+    L, B, cols = table.shape
+    asked, ok, slots, end = used, True, [], used
+    for l in range(L):
+        row = []
+        for b in range(B):
+            n, a = int(lens[l, b]), int(n_new[l, b])
+            have, need = -(-n // page_size), -(-(n + a) // page_size)
+            fits = need <= cols
+            if fits and need > have:
+                start, asked = asked, asked + need - have
+                fits = asked <= len(free_pages)
+                if fits:
+                    table[l, b, have:need] = free_pages[start:asked]
+                    end = asked
+            if fits:
+                lens[l, b] = n + a
+                row += [int(table[l, b, i // page_size]) * page_size + i % page_size for i in range(n, n + a)]
+            else:
+                ok = False
+                row += [-1] * a
+        slots.append(row)
+    return table, lens, slots, end, ok

@@ -9,8 +9,9 @@ import sys
 HERE = os.path.dirname(os.path.abspath(__file__))
 CSRC = os.path.join(HERE, "csrc")
 LIB = os.path.join(HERE, "libxkv.so")
-SOURCES = ["xkv_api.cu", "xkv_score.cu", "xkv_score_tc.cu", "xkv_score_fused.cu", "xkv_select.cu", "xkv_decode.cu", "xkv_prefill.cu"]
-HEADERS = ["common.cuh", "ops.h", "score_params.h", "tc_common.cuh", os.path.join("..", "..", "include", "xkv.h")]
+SOURCES = ["xkv_api.cu", "xkv_score.cu", "xkv_score_tc.cu", "xkv_score_fused.cu", "xkv_select.cu", "xkv_decode.cu", "xkv_prefill.cu",
+           "xkv_serve.cu", "xkv_decode_e4m3.cu"]
+HEADERS = ["common.cuh", "ops.h", "score_params.h", "tc_common.cuh", "e4m3.cuh", os.path.join("..", "..", "include", "xkv.h")]
 
 
 def _nvcc() -> str:

@@ -22,7 +22,9 @@ struct WorkspaceHeader {
   int32_t n_multi;       // decode: (layer, sequence) units cut into more than one chunk
   int32_t merge_counter; // decode: next split-K merge job to hand to a warp
   int32_t grid_arrivals; // decode: CTAs of the self-planning launch that have finished all their work
-  int32_t reserved[56];
+  int32_t plan_ticket;   // step plan: CTAs that have finished (zero between calls)
+  int32_t plan_used;     // step plan: free-list position behind the last page handed out (zero between calls)
+  int32_t reserved[54];
 };
 static_assert(sizeof(WorkspaceHeader) == 256, "header is 256 bytes");
 

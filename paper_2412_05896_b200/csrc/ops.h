@@ -42,6 +42,32 @@ xkv_status decode_attn(const xkv_dims* d, const xkv_cache* c, int layer_begin, i
 xkv_status decode_attn_static(const xkv_dims* d, const xkv_cache* c, int layer_begin, int layer_end,
                               const void* q, const void* k_new, const void* v_new, void* out, float* lse,
                               int chunk_rows, int32_t* status_out, cudaStream_t st);
+// Where decode_attn's workspace holds what the decode kernels need.
+struct DecodeScratch {
+  void* header;
+  int32_t* tickets;    // [n_layers * batch * n_kv_heads], zero at the start of the call like the rest of the header
+  int4* items;         // [max_items]
+  float* part_o;       // [max_items][G][d]
+  float* part_ml;      // [max_items][G][2]
+  int64_t max_items;
+};
+xkv_status decode_attn_e4m3(const xkv_dims* d, const xkv_cache* c, int layer_begin, int n_layers, const void* q,
+                            const void* k_new, const void* v_new, void* out, float* lse, int chunk_rows,
+                            const DecodeScratch& ws, cudaStream_t st);
+// One new row per (layer, sequence) and KV head stored in a cache of 8-bit floats, lengths advanced.
+xkv_status append_e4m3(const xkv_dims* d, const xkv_cache* c, int layer_begin, int n_units, const void* k_new,
+                       const void* v_new, void* workspace, cudaStream_t st);
+
+size_t store_workspace_bytes();
+xkv_status store_rows(const xkv_dims* d, const xkv_cache* c, const void* k, const void* v, const int64_t* slots,
+                      int64_t n_tokens, void* workspace, cudaStream_t st);
+
+size_t plan_workspace_bytes(int n_layers, int batch);
+int plan_max_batch();
+xkv_status plan_append(const xkv_cache* c, int batch, const int32_t* n_new, int n_new_stride, const int32_t* lens_before,
+                       const int32_t* free_pages, int n_free, const int32_t* pages_used_before, int32_t* pages_used_after,
+                       int64_t* slots, int64_t slots_stride, void* workspace, cudaStream_t st);
+
 void set_profile_events(cudaEvent_t start, cudaEvent_t stop);
 
 }  // namespace xkv

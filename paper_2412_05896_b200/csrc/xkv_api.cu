@@ -1,6 +1,5 @@
 // C ABI of libxkv: host-side argument validation, workspace sizing, status plumbing, and the
-// host-only budget solver (Algorithm 1).  Device work is in xkv_score.cu, xkv_select.cu and
-// xkv_decode.cu.
+// host-only budget solver (Algorithm 1).  Device work is in the other .cu files beside this one.
 #include <atomic>
 #include <cmath>
 #include <queue>
@@ -64,19 +63,31 @@ xkv_status check_prefill_dims(const xkv_dims* d) {
   return XKV_OK;
 }
 
+xkv_status check_format(const xkv_cache* c) {
+  if (c->kv_format != XKV_KV_BF16 && c->kv_format != XKV_KV_INT8 && c->kv_format != XKV_KV_E4M3)
+    return XKV_ERR_INVALID_ARG;
+  if (c->kv_format != XKV_KV_BF16 &&
+      (c->k_scales == nullptr || c->v_scales == nullptr || !aligned16(c->k_scales) || !aligned16(c->v_scales)))
+    return XKV_ERR_INVALID_ARG;
+  return XKV_OK;
+}
+
+xkv_status check_page_size(int32_t page_size) {
+  return page_size <= 0 || page_size % 16 != 0 || page_size > 256 ? XKV_ERR_INVALID_ARG : XKV_OK;
+}
+
 xkv_status check_cache(const xkv_cache* c, const xkv_dims* d) {
   if (c == nullptr) return XKV_ERR_INVALID_ARG;
+  xkv_status s;
   if (c->k_pages == nullptr || c->v_pages == nullptr || c->block_table == nullptr || c->seq_lens == nullptr)
     return XKV_ERR_INVALID_ARG;
   if (!aligned16(c->k_pages) || !aligned16(c->v_pages) || !aligned16(c->block_table) || !aligned16(c->seq_lens))
     return XKV_ERR_INVALID_ARG;
   if (c->n_layers <= 0 || c->max_pages_per_seq <= 0 || c->n_pages <= 0) return XKV_ERR_INVALID_ARG;
-  if (c->page_size <= 0 || c->page_size % 16 != 0 || c->page_size > 256) return XKV_ERR_INVALID_ARG;
+  if ((s = check_page_size(c->page_size)) != XKV_OK) return s;
   if ((int64_t)c->max_pages_per_seq * c->page_size > (1 << 30)) return XKV_ERR_INVALID_ARG;
-  if (c->kv_format != XKV_KV_BF16 && c->kv_format != XKV_KV_INT8) return XKV_ERR_INVALID_ARG;
-  if (c->kv_format == XKV_KV_INT8 &&
-      (c->k_scales == nullptr || c->v_scales == nullptr || !aligned16(c->k_scales) || !aligned16(c->v_scales)))
-    return XKV_ERR_INVALID_ARG;
+  s = check_format(c);
+  if (s != XKV_OK) return s;
   (void)d;
   return XKV_OK;
 }
@@ -221,6 +232,52 @@ xkv_status xkv_build_block_table(const int32_t* first_page, const int32_t* n_pag
                            cache->max_pages_per_seq, static_cast<cudaStream_t>(stream));
 }
 
+xkv_status xkv_plan_append(const xkv_cache* cache, int32_t batch, const int32_t* n_new, int32_t n_new_stride,
+                           const int32_t* lens_before, const int32_t* free_pages, int32_t n_free,
+                           const int32_t* pages_used_before, int32_t* pages_used_after, int64_t* slots,
+                           int64_t slots_stride, void* workspace, size_t workspace_bytes, void* stream) {
+  if (cache == nullptr || cache->block_table == nullptr || cache->seq_lens == nullptr || n_new == nullptr ||
+      workspace == nullptr)
+    return XKV_ERR_INVALID_ARG;
+  if (!aligned16(cache->block_table) || !aligned16(cache->seq_lens) || !aligned16(n_new) || !aligned16(lens_before) ||
+      !aligned16(free_pages) || !aligned16(pages_used_before) || !aligned16(pages_used_after) || !aligned16(slots) ||
+      (reinterpret_cast<uintptr_t>(workspace) & 255u) != 0)
+    return XKV_ERR_INVALID_ARG;
+  if (batch <= 0 || cache->n_layers <= 0 || cache->max_pages_per_seq <= 0 || cache->n_pages <= 0 || n_free < 0)
+    return XKV_ERR_INVALID_ARG;
+  xkv_status s = check_page_size(cache->page_size);
+  if (s != XKV_OK) return s;
+  if ((int64_t)cache->max_pages_per_seq * cache->page_size > (1 << 30)) return XKV_ERR_INVALID_ARG;
+  if (n_new_stride != 0 && n_new_stride < batch) return XKV_ERR_INVALID_ARG;
+  if (slots != nullptr && (slots_stride <= 0 || slots_stride >= (1ll << 31))) return XKV_ERR_INVALID_ARG;
+  if (batch > plan_max_batch() || cache->n_layers > 65535 || (int64_t)batch * cache->n_layers >= (1ll << 31))
+    return XKV_ERR_UNSUPPORTED;
+  if (workspace_bytes < plan_workspace_bytes(cache->n_layers, batch)) return XKV_ERR_WORKSPACE;
+  return plan_append(cache, batch, n_new, n_new_stride, lens_before, free_pages, n_free, pages_used_before,
+                     pages_used_after, slots, slots_stride, workspace, static_cast<cudaStream_t>(stream));
+}
+
+xkv_status xkv_store_rows(const xkv_dims* dims, const xkv_cache* cache, const void* k, const void* v,
+                          const int64_t* slots, int64_t n_tokens, void* workspace, size_t workspace_bytes,
+                          void* stream) {
+  xkv_status s = check_dims(dims);
+  if (s != XKV_OK) return s;
+  if (cache == nullptr || cache->k_pages == nullptr || cache->v_pages == nullptr || k == nullptr || v == nullptr ||
+      slots == nullptr || workspace == nullptr)
+    return XKV_ERR_INVALID_ARG;
+  if (!aligned16(cache->k_pages) || !aligned16(cache->v_pages) || !aligned16(k) || !aligned16(v) || !aligned16(slots) ||
+      (reinterpret_cast<uintptr_t>(workspace) & 255u) != 0)
+    return XKV_ERR_INVALID_ARG;
+  if ((s = check_page_size(cache->page_size)) != XKV_OK || (s = check_format(cache)) != XKV_OK) return s;
+  if (cache->n_pages <= 0 || n_tokens < 0 || n_tokens >= (1ll << 31)) return XKV_ERR_INVALID_ARG;
+  if (dims->kv_stride_head < dims->head_dim || dims->kv_stride_head % 8 != 0 ||
+      dims->kv_stride_token < (int64_t)dims->n_kv_heads * dims->head_dim || dims->kv_stride_token % 8 != 0)
+    return XKV_ERR_INVALID_ARG;
+  if (workspace_bytes < store_workspace_bytes()) return XKV_ERR_WORKSPACE;
+  if (n_tokens == 0) return XKV_OK;
+  return store_rows(dims, cache, k, v, slots, n_tokens, workspace, static_cast<cudaStream_t>(stream));
+}
+
 xkv_status xkv_decode_attn(const xkv_dims* dims, const xkv_cache* cache, int32_t layer_begin, int32_t layer_end,
                            const void* q, const void* k_new, const void* v_new, void* out, float* lse,
                            int32_t chunk_rows, void* workspace, size_t workspace_bytes, void* stream) {
@@ -278,6 +335,12 @@ size_t xkv_workspace_bytes(int32_t op, const xkv_dims* dims, int32_t max_seqlen,
           chunk_rows % 64 != 0)
         return 0;
       return decode_workspace_bytes(dims, n_layers, max_cache_len, chunk_rows);
+    case XKV_OP_PLAN_APPEND:
+      if (dims->batch <= 0 || n_layers <= 0) return 0;
+      return plan_workspace_bytes(n_layers, dims->batch);
+    case XKV_OP_STORE_ROWS:
+      if (check_dims(dims) != XKV_OK) return 0;
+      return store_workspace_bytes();
     default:
       return 0;
   }

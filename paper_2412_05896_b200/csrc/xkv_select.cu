@@ -13,6 +13,7 @@
 //   gather_kernel  16-byte vectorised copy of the kept K and V rows (256-byte rows for d = 128) into
 //                  the layer's cache pages; pure data movement, HBM-bound.
 #include "common.cuh"
+#include "e4m3.cuh"
 #include "ops.h"
 
 namespace xkv {
@@ -307,6 +308,35 @@ __global__ void __launch_bounds__(kGatherThreads) gather_kernel(SelectParams p) 
   }
 }
 
+// The kept rows as 8-bit floats with one scale per block of 16 cache slots: a warp per (block, K or V) reads the block's
+// rows, finds their largest magnitude and stores the codes.  Same grid as gather_kernel.
+template <int D>
+__global__ void __launch_bounds__(kGatherThreads) gather_e4m3_kernel(SelectParams p) {
+  const int unit = blockIdx.x;
+  const int b = unit / p.n_kv_heads, g = unit % p.n_kv_heads;
+  int cu, t, P, kb;
+  unit_shape(p, b, g, &cu, &t, &P, &kb);
+  const int n_keep = kb + (t - P);
+  if (n_keep > p.max_pages_per_seq * p.page_size) return;
+  const int32_t* sel = p.sel + (size_t)unit * p.sel_stride;
+  const int32_t* bt = p.block_table_layer + (size_t)cache_index(p, b, g) * p.max_pages_per_seq;
+  const int page_heads = p.head_level ? 1 : p.n_kv_heads, page_head = p.head_level ? 0 : g;
+  for (int job = threadIdx.x >> 5; job < 2 * (kGatherRows / kScaleBlock); job += kGatherThreads / 32) {
+    const int r0 = blockIdx.y * kGatherRows + (job >> 1) * kScaleBlock, is_v = job & 1;
+    if (r0 >= n_keep) break;
+    const int page = bt[r0 / p.page_size];                    // a block lies within one page
+    if (page < 0 || page >= p.n_pages) {
+      if ((threadIdx.x & 31) == 0) record_status(p.hdr, XKV_ERR_CAPACITY);
+      continue;
+    }
+    const size_t slot = ((size_t)page * page_heads + page_head) * p.page_size + r0 % p.page_size;
+    const __nv_bfloat16* src = (is_v ? p.v : p.k) + (size_t)g * p.stride_head;
+    e4m3_store_block<D>(reinterpret_cast<uint8_t*>(is_v ? p.v_pages : p.k_pages) + slot * D,
+                        (is_v ? p.v_scales : p.k_scales) + slot / kScaleBlock, 0, min(kScaleBlock, n_keep - r0),
+                        [&](int i) { return src + (size_t)(cu + sel[r0 + i]) * p.stride_token; });
+  }
+}
+
 // block_table[l][b][i] = first_page[l][b] + i for i < n_pages_lb[l][b], else 0.  grid = (L*B), any block size.
 __global__ void block_table_kernel(const int32_t* first_page, const int32_t* n_pages_lb, int32_t* block_table,
                                    int max_pages_per_seq) {
@@ -477,7 +507,12 @@ xkv_status select_compact(const xkv_dims* d, int layer, const int32_t* budget, i
   if (s != XKV_OK) return s;
   if (max_keep > 0) {
     dim3 grid(n_units, (max_keep + kGatherRows - 1) / kGatherRows);
-    gather_kernel<<<grid, kGatherThreads, 0, st>>>(p);
+    if (c->kv_format == XKV_KV_E4M3) {
+      if (d->head_dim == 128) gather_e4m3_kernel<128><<<grid, kGatherThreads, 0, st>>>(p);
+      else                    gather_e4m3_kernel<64><<<grid, kGatherThreads, 0, st>>>(p);
+    } else {
+      gather_kernel<<<grid, kGatherThreads, 0, st>>>(p);
+    }
     count_launch();
     s = check_launch();
   }

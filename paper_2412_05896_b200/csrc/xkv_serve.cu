@@ -1,0 +1,467 @@
+// Serving on a reduced cache: the plan of a step (xkv_plan_append) and rows stored by slot (xkv_store_rows).
+//
+//   plan_kernel         block tables, slot maps and new lengths of every (layer, sequence) from the lengths before the
+//                       step and the new tokens.  grid = (slices, layers); no CTA waits for another one: each forms
+//                       the pages asked for by the layers before its own and the scan over its layer's sequences by
+//                       itself (integers out of L2), and the last CTA to leave writes the lengths, so that they may
+//                       be advanced in place.
+//   store_block_kernel  caches of 8-bit floats: one warp per (run of tokens within a block of 16 slots, KV head, K or V)
+//   store_row_kernel    caches of bf16 or of 8-bit integers: D/8 lanes per (token, KV head)
+//   append_block_kernel one new row per (layer, sequence) and KV head of a cache of 8-bit floats, lengths advanced
+#include "common.cuh"
+#include "e4m3.cuh"
+#include "ops.h"
+
+namespace xkv {
+namespace {
+
+// ---------------------------------------------------------------------------------------------
+// Plan of a step
+// ---------------------------------------------------------------------------------------------
+constexpr int kPlanThreads = 512;
+constexpr int kPlanMaxBatch = 16384;          // sequences of a layer: two 4-byte table entries each in shared memory
+
+struct PlanParams {
+  const int32_t* n_new;
+  int64_t n_new_stride;
+  const int32_t* lens_before;   // null: all zero
+  int32_t* lens_after;
+  const int32_t* free_pages;    // null: page id = position
+  int32_t n_free;
+  const int32_t* used_before;   // null: 0
+  int32_t* used_after;
+  int32_t* block_table;
+  int64_t* slots;
+  int64_t slots_stride;
+  int32_t n_layers, batch, page_size, max_pages_per_seq, n_pages;
+  WorkspaceHeader* hdr;
+  int32_t* new_lens;            // [n_layers][batch] in the workspace, until the last CTA copies them out
+};
+
+struct Ask {
+  int32_t len, add;             // rows before, rows to add (both clamped at 0)
+  int32_t pages;                // pages to take; -1: the cache cannot hold that many rows
+  bool bad;                     // a negative count was found
+};
+
+__device__ __forceinline__ Ask plan_ask(const PlanParams& p, int l, int b) {
+  Ask a;
+  const int len = p.lens_before != nullptr ? __ldg(&p.lens_before[(size_t)l * p.batch + b]) : 0;
+  const int add = __ldg(&p.n_new[l * p.n_new_stride + b]);
+  a.bad = len < 0 || add < 0;
+  a.len = max(len, 0);
+  a.add = max(add, 0);
+  const int64_t total = (int64_t)a.len + a.add;
+  if (total > (int64_t)p.max_pages_per_seq * p.page_size) {
+    a.pages = -1;
+  } else {
+    const int ps = p.page_size;
+    a.pages = ((int)total + ps - 1) / ps - (a.len + ps - 1) / ps;
+  }
+  return a;
+}
+
+__device__ __forceinline__ long long warp_sum(long long v) {
+#pragma unroll
+  for (int o = 16; o > 0; o >>= 1) v += __shfl_xor_sync(0xffffffffu, v, o);
+  return v;
+}
+
+__global__ void __launch_bounds__(kPlanThreads) plan_kernel(const PlanParams p) {
+  extern __shared__ int32_t s_plan[];
+  int32_t* s_tok = s_plan;                    // [batch + 1] tokens of the layer before each sequence
+  int32_t* s_start = s_plan + p.batch + 1;    // [batch] position in the free list, -1: the pages do not fit
+  __shared__ long long s_red[32], s_red2[32];
+  __shared__ int s_last;
+  const int tid = threadIdx.x, lane = tid & 31, warp = tid >> 5;
+  constexpr int kWarps = kPlanThreads / 32;
+  const int layer = blockIdx.y, slice = blockIdx.x, n_slices = gridDim.x;
+  int used = p.used_before != nullptr ? __ldg(p.used_before) : 0;
+  if (used < 0 || used > p.n_free) {
+    if (tid == 0) record_status(p.hdr, XKV_ERR_INVALID_ARG);
+    used = p.n_free;                          // nothing can be handed out
+  }
+
+  // ---- pages asked for by the layers before this one
+  long long before = 0;
+  for (int e = tid; e < layer * p.batch; e += kPlanThreads) {
+    const Ask a = plan_ask(p, e / p.batch, e % p.batch);
+    before += max(a.pages, 0);
+  }
+  before = warp_sum(before);
+  if (lane == 0) s_red[warp] = before;
+  __syncthreads();
+  before = used;
+#pragma unroll
+  for (int w = 0; w < kWarps; ++w) before += s_red[w];
+
+  // ---- scan over the layer's sequences
+  long long carry = before, tok_carry = 0;
+  int end_max = 0;
+  for (int b0 = 0; b0 < p.batch; b0 += kPlanThreads) {
+    const int b = b0 + tid;
+    Ask a = {0, 0, 0, false};
+    if (b < p.batch) a = plan_ask(p, layer, b);
+    const long long ask = max(a.pages, 0), add = a.add;
+    long long incl = ask, tincl = add;
+#pragma unroll
+    for (int o = 1; o < 32; o <<= 1) {
+      const long long x = __shfl_up_sync(0xffffffffu, incl, o), y = __shfl_up_sync(0xffffffffu, tincl, o);
+      if (lane >= o) {
+        incl += x;
+        tincl += y;
+      }
+    }
+    __syncthreads();
+    if (lane == 31) {
+      s_red[warp] = incl;
+      s_red2[warp] = tincl;
+    }
+    __syncthreads();
+    long long base = carry, tbase = tok_carry, all = 0, tall = 0;
+#pragma unroll
+    for (int w = 0; w < kWarps; ++w) {
+      if (w < warp) {
+        base += s_red[w];
+        tbase += s_red2[w];
+      }
+      all += s_red[w];
+      tall += s_red2[w];
+    }
+    if (b < p.batch) {
+      const long long start = base + incl - ask;
+      const bool fits = a.pages >= 0 && (ask == 0 || start + ask <= p.n_free);
+      s_start[b] = fits ? (int)min(start, (long long)p.n_free) : -1;
+      s_tok[b] = (int)min(tbase + tincl - add, 0x7fffffffll);
+      if (fits && ask > 0) end_max = max(end_max, (int)(start + ask));
+      if (slice == 0) {
+        p.new_lens[(size_t)layer * p.batch + b] = fits ? a.len + a.add : a.len;
+        if (a.bad) record_status(p.hdr, XKV_ERR_INVALID_ARG);
+        else if (!fits) record_status(p.hdr, XKV_ERR_CAPACITY);
+      }
+    }
+    carry += all;
+    tok_carry += tall;
+  }
+  if (tid == 0) s_tok[p.batch] = (int)min(tok_carry, 0x7fffffffll);
+  if (slice == 0) {
+    end_max = __reduce_max_sync(0xffffffffu, end_max);
+    if (lane == 0 && end_max > 0) atomicMax(&p.hdr->plan_used, end_max);
+  }
+  __syncthreads();
+
+  // ---- the new entries of the block tables: a warp per sequence
+  int32_t* table = p.block_table + (size_t)layer * p.batch * p.max_pages_per_seq;
+  for (int b = slice * kWarps + warp; b < p.batch; b += n_slices * kWarps) {
+    const int start = s_start[b];
+    if (start < 0) continue;
+    const Ask a = plan_ask(p, layer, b);
+    const int have = (a.len + p.page_size - 1) / p.page_size;
+    for (int i = lane; i < a.pages; i += 32) {
+      const int page = p.free_pages != nullptr ? __ldg(&p.free_pages[start + i]) : start + i;
+      if (page < 0 || page >= p.n_pages) record_status(p.hdr, XKV_ERR_INVALID_ARG);
+      table[(size_t)b * p.max_pages_per_seq + have + i] = page;
+    }
+  }
+
+  // ---- slots of the layer's new tokens
+  if (p.slots != nullptr) {
+    const int64_t total = min((int64_t)s_tok[p.batch], p.slots_stride);
+    if (slice == 0 && tid == 0 && s_tok[p.batch] > p.slots_stride) record_status(p.hdr, XKV_ERR_CAPACITY);
+    int64_t* out = p.slots + layer * p.slots_stride;
+    for (int64_t t = (int64_t)slice * kPlanThreads + tid; t < total; t += (int64_t)n_slices * kPlanThreads) {
+      int lo = 0, hi = p.batch;                // s_tok[lo] <= t < s_tok[hi]
+      while (hi - lo > 1) {
+        const int mid = (lo + hi) >> 1;
+        if (s_tok[mid] <= t) lo = mid;
+        else hi = mid;
+      }
+      const int start = s_start[lo];
+      int64_t slot = -1;
+      if (start >= 0) {
+        const int len = p.lens_before != nullptr ? max(__ldg(&p.lens_before[(size_t)layer * p.batch + lo]), 0) : 0;
+        const int pos = len + ((int)t - s_tok[lo]);
+        const int have = (len + p.page_size - 1) / p.page_size;
+        const int i = pos / p.page_size;
+        int page;
+        if (i < have) page = table[(size_t)lo * p.max_pages_per_seq + i];
+        else page = p.free_pages != nullptr ? __ldg(&p.free_pages[start + i - have]) : start + i - have;
+        if (page >= 0 && page < p.n_pages) slot = (int64_t)page * p.page_size + (pos - i * p.page_size);
+        else record_status(p.hdr, XKV_ERR_INVALID_ARG);
+      }
+      out[t] = slot;
+    }
+  }
+
+  // ---- the last CTA to get here writes the lengths (every other one has read them) and the list position
+  __threadfence();
+  __syncthreads();
+  const int n_ctas = gridDim.x * gridDim.y;
+  if (tid == 0) s_last = (atomicAdd(&p.hdr->plan_ticket, 1) == n_ctas - 1) ? 1 : 0;
+  __syncthreads();
+  if (!s_last) return;
+  __threadfence();
+  for (int64_t e = tid; e < (int64_t)p.n_layers * p.batch; e += kPlanThreads) p.lens_after[e] = __ldcg(&p.new_lens[e]);
+  if (tid == 0) {
+    const int end = atomicExch(&p.hdr->plan_used, 0);
+    if (p.used_after != nullptr) *p.used_after = max(end, used);
+    p.hdr->plan_ticket = 0;
+  }
+}
+
+// ---------------------------------------------------------------------------------------------
+// Rows stored by slot
+// ---------------------------------------------------------------------------------------------
+constexpr int kStoreThreads = 256;
+
+struct StoreParams {
+  const __nv_bfloat16* k;
+  const __nv_bfloat16* v;
+  const int64_t* slots;
+  int64_t n_tokens, n_slots;
+  int64_t stride_token, stride_head;
+  uint8_t* k_pages;
+  uint8_t* v_pages;
+  float* k_scales;
+  float* v_scales;
+  int32_t n_kv_heads, page_size, tokens_per_warp;
+  WorkspaceHeader* hdr;
+};
+
+// One warp: the runs that begin among tokens_per_warp consecutive tokens, of one KV head of K or of V.  A run is the
+// longest stretch of tokens whose slots follow each other inside one block; rows of the block before the run are there
+// already, rows behind it are not in use.
+template <int D>
+__global__ void __launch_bounds__(kStoreThreads) store_block_kernel(const StoreParams p) {
+  const int lane = threadIdx.x & 31;
+  const int64_t w = (int64_t)blockIdx.x * (kStoreThreads / 32) + (threadIdx.x >> 5);
+  const int n_jobs = 2 * p.n_kv_heads;                        // (head, K or V) of a token
+  const int64_t t0 = w / n_jobs * p.tokens_per_warp;
+  const int job = (int)(w % n_jobs);
+  const int h = job >> 1, is_v = job & 1;
+  if (t0 >= p.n_tokens) return;
+  // lane i: the slots of token t0 + i and of the one before it
+  const int64_t ti = t0 + lane;
+  int64_t s = -1, prev = -1;
+  if (lane < p.tokens_per_warp && ti < p.n_tokens) {
+    s = __ldg(&p.slots[ti]);
+    if (ti > 0) prev = __ldg(&p.slots[ti - 1]);
+    if (s >= p.n_slots) {
+      if (job == 0) record_status(p.hdr, XKV_ERR_CAPACITY);
+      s = -1;
+    }
+    if (s >= 0 && prev >= 0 && prev / kScaleBlock == s / kScaleBlock && prev + 1 != s) {
+      if (job == 0) record_status(p.hdr, XKV_ERR_INVALID_ARG);   // a block's tokens are not in slot order
+      s = -1;
+    }
+  }
+  unsigned heads = __ballot_sync(0xffffffffu, s >= 0 && (s % kScaleBlock == 0 || prev + 1 != s));
+  const __nv_bfloat16* src = is_v ? p.v : p.k;
+  while (heads != 0) {
+    const int first = __ffs(heads) - 1;
+    heads &= heads - 1;
+    const int64_t t = t0 + first;
+    const int64_t slot = __shfl_sync(0xffffffffu, s, first);
+    const int n_old = (int)(slot % kScaleBlock);
+    // tokens of the run
+    bool follows = false;
+    if (lane < kScaleBlock - n_old && t + lane < p.n_tokens) follows = __ldg(&p.slots[t + lane]) == slot + lane;
+    const int n_new = __ffs(~__ballot_sync(0xffffffffu, follows)) - 1;
+    const int64_t page = slot / p.page_size, in_page = slot % p.page_size - n_old;
+    const int64_t row = (page * p.n_kv_heads + h) * p.page_size + in_page;
+    const __nv_bfloat16* rows = src + t * p.stride_token + h * p.stride_head;
+    e4m3_store_block<D>((is_v ? p.v_pages : p.k_pages) + row * D, (is_v ? p.v_scales : p.k_scales) + row / kScaleBlock,
+                        n_old, n_new, [&](int i) { return rows + i * p.stride_token; });
+    __syncwarp();
+  }
+}
+
+template <int D, bool Q8>
+__global__ void __launch_bounds__(kStoreThreads) store_row_kernel(const StoreParams p) {
+  constexpr int kPieces = D / 8;
+  const int64_t idx = (int64_t)blockIdx.x * kStoreThreads + threadIdx.x;
+  const int c = (int)(idx % kPieces);
+  const int64_t r = idx / kPieces;
+  const int h = (int)(r % p.n_kv_heads);
+  const int64_t t = r / p.n_kv_heads;
+  if (t >= p.n_tokens) return;                                // whole rows: a row's lanes leave together
+  const int64_t slot = __ldg(&p.slots[t]);
+  if (slot < 0) return;
+  if (slot >= p.n_slots) {
+    if (c == 0) record_status(p.hdr, XKV_ERR_CAPACITY);
+    return;
+  }
+  const size_t src = (size_t)t * p.stride_token + (size_t)h * p.stride_head + c * 8;
+  const uint4 kv = __ldg(reinterpret_cast<const uint4*>(p.k + src));
+  const uint4 vv = __ldg(reinterpret_cast<const uint4*>(p.v + src));
+  const size_t row = ((size_t)(slot / p.page_size) * p.n_kv_heads + h) * p.page_size + slot % p.page_size;
+  if constexpr (Q8) {
+    float x[8], ks, vs;
+    bf16x8_to_f32(kv, x);
+    const uint2 kc = quantize_row_piece(x, kPieces, &ks);
+    bf16x8_to_f32(vv, x);
+    const uint2 vc = quantize_row_piece(x, kPieces, &vs);
+    *reinterpret_cast<uint2*>(p.k_pages + row * D + c * 8) = kc;
+    *reinterpret_cast<uint2*>(p.v_pages + row * D + c * 8) = vc;
+    if (c == 0) {
+      p.k_scales[row] = ks;
+      p.v_scales[row] = vs;
+    }
+  } else {
+    *reinterpret_cast<uint4*>(p.k_pages + (row * D + c * 8) * 2) = kv;
+    *reinterpret_cast<uint4*>(p.v_pages + (row * D + c * 8) * 2) = vv;
+  }
+}
+
+// ---------------------------------------------------------------------------------------------
+// One new row per (layer, sequence): grid = units, a warp per (KV head, K or V)
+// ---------------------------------------------------------------------------------------------
+struct AppendParams {
+  const __nv_bfloat16* k_new;
+  const __nv_bfloat16* v_new;
+  uint8_t* k_pages;
+  uint8_t* v_pages;
+  float* k_scales;
+  float* v_scales;
+  const int32_t* block_table;
+  int32_t* seq_lens;
+  int32_t layer_begin, batch, n_kv_heads, page_size, max_pages_per_seq, n_pages;
+  WorkspaceHeader* hdr;
+};
+
+template <int D>
+__global__ void __launch_bounds__(kStoreThreads) append_block_kernel(const AppendParams p) {
+  const int e = blockIdx.x;
+  const size_t le = (size_t)p.layer_begin * p.batch + e;
+  const int n = p.seq_lens[le];
+  int page = -1;
+  if (n >= 0 && n < p.max_pages_per_seq * p.page_size) page = p.block_table[le * p.max_pages_per_seq + n / p.page_size];
+  if (page < 0 || page >= p.n_pages) {
+    if (threadIdx.x == 0) record_status(p.hdr, XKV_ERR_CAPACITY);
+    return;
+  }
+  const int n_old = n % kScaleBlock;
+  for (int job = threadIdx.x >> 5; job < 2 * p.n_kv_heads; job += kStoreThreads / 32) {
+    const int h = job >> 1, is_v = job & 1;
+    const int64_t row = ((int64_t)page * p.n_kv_heads + h) * p.page_size + (n % p.page_size - n_old);
+    const __nv_bfloat16* src = (is_v ? p.v_new : p.k_new) + ((size_t)e * p.n_kv_heads + h) * D;
+    e4m3_store_block<D>((is_v ? p.v_pages : p.k_pages) + row * D, (is_v ? p.v_scales : p.k_scales) + row / kScaleBlock,
+                        n_old, 1, [&](int) { return src; });
+  }
+  __syncthreads();                                           // every warp has read the length
+  if (threadIdx.x == 0) p.seq_lens[le] = n + 1;
+}
+
+}  // namespace
+
+size_t plan_workspace_bytes(int n_layers, int batch) { return kHeaderBytes + align_up((size_t)n_layers * batch * 4, 256); }
+
+int plan_max_batch() { return kPlanMaxBatch; }
+
+xkv_status plan_append(const xkv_cache* c, int batch, const int32_t* n_new, int n_new_stride, const int32_t* lens_before,
+                       const int32_t* free_pages, int n_free, const int32_t* pages_used_before, int32_t* pages_used_after,
+                       int64_t* slots, int64_t slots_stride, void* workspace, cudaStream_t st) {
+  PlanParams p;
+  p.n_new = n_new;
+  p.n_new_stride = n_new_stride;
+  p.lens_before = lens_before;
+  p.lens_after = c->seq_lens;
+  p.free_pages = free_pages;
+  p.n_free = n_free;
+  p.used_before = pages_used_before;
+  p.used_after = pages_used_after;
+  p.block_table = c->block_table;
+  p.slots = slots;
+  p.slots_stride = slots_stride;
+  p.n_layers = c->n_layers;
+  p.batch = batch;
+  p.page_size = c->page_size;
+  p.max_pages_per_seq = c->max_pages_per_seq;
+  p.n_pages = c->n_pages;
+  p.hdr = static_cast<WorkspaceHeader*>(workspace);
+  p.new_lens = reinterpret_cast<int32_t*>(static_cast<uint8_t*>(workspace) + kHeaderBytes);
+  const size_t smem = (size_t)(2 * batch + 1) * 4;
+  if (smem > 40 * 1024 &&
+      cudaFuncSetAttribute(plan_kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)smem) != cudaSuccess)
+    return XKV_ERR_CUDA;
+  const int64_t tokens = slots != nullptr ? slots_stride : 0;
+  int64_t slices = (tokens + 4 * kPlanThreads - 1) / (4 * kPlanThreads);
+  const int64_t most = (4 * (int64_t)sm_count() + c->n_layers - 1) / c->n_layers;
+  slices = slices < 1 ? 1 : (slices > most ? most : slices);
+  plan_kernel<<<dim3((unsigned)slices, (unsigned)c->n_layers), kPlanThreads, smem, st>>>(p);
+  count_launch();
+  return check_launch();
+}
+
+size_t store_workspace_bytes() { return kHeaderBytes; }
+
+xkv_status store_rows(const xkv_dims* d, const xkv_cache* c, const void* k, const void* v, const int64_t* slots,
+                      int64_t n_tokens, void* workspace, cudaStream_t st) {
+  StoreParams p;
+  p.k = static_cast<const __nv_bfloat16*>(k);
+  p.v = static_cast<const __nv_bfloat16*>(v);
+  p.slots = slots;
+  p.n_tokens = n_tokens;
+  p.n_slots = (int64_t)c->n_pages * c->page_size;
+  p.stride_token = d->kv_stride_token;
+  p.stride_head = d->kv_stride_head;
+  p.k_pages = static_cast<uint8_t*>(c->k_pages);
+  p.v_pages = static_cast<uint8_t*>(c->v_pages);
+  p.k_scales = c->k_scales;
+  p.v_scales = c->v_scales;
+  p.n_kv_heads = d->n_kv_heads;
+  p.page_size = c->page_size;
+  p.hdr = static_cast<WorkspaceHeader*>(workspace);
+  if (c->kv_format == XKV_KV_E4M3) {
+    // One warp per token while that leaves every SM a few dozen warps (a decode step: every token is a run of its
+    // own), else one per 16 tokens (a prompt: one run or two), so that few warps start only to find no run.
+    const int64_t jobs = n_tokens * 2 * d->n_kv_heads;
+    p.tokens_per_warp = jobs <= 64 * (int64_t)sm_count() ? 1 : kScaleBlock;
+    const int64_t warps = (n_tokens + p.tokens_per_warp - 1) / p.tokens_per_warp * 2 * d->n_kv_heads;
+    const int64_t grid = (warps + kStoreThreads / 32 - 1) / (kStoreThreads / 32);
+    if (grid > 0x7fffffffll) return XKV_ERR_UNSUPPORTED;
+    if (d->head_dim == 128) store_block_kernel<128><<<(unsigned)grid, kStoreThreads, 0, st>>>(p);
+    else                    store_block_kernel<64><<<(unsigned)grid, kStoreThreads, 0, st>>>(p);
+  } else {
+    p.tokens_per_warp = 0;
+    const int64_t threads = n_tokens * d->n_kv_heads * (d->head_dim / 8);
+    const int64_t grid = (threads + kStoreThreads - 1) / kStoreThreads;
+    if (grid > 0x7fffffffll) return XKV_ERR_UNSUPPORTED;
+    const bool q8 = c->kv_format == XKV_KV_INT8;
+    if (d->head_dim == 128) {
+      if (q8) store_row_kernel<128, true><<<(unsigned)grid, kStoreThreads, 0, st>>>(p);
+      else    store_row_kernel<128, false><<<(unsigned)grid, kStoreThreads, 0, st>>>(p);
+    } else {
+      if (q8) store_row_kernel<64, true><<<(unsigned)grid, kStoreThreads, 0, st>>>(p);
+      else    store_row_kernel<64, false><<<(unsigned)grid, kStoreThreads, 0, st>>>(p);
+    }
+  }
+  count_launch();
+  return check_launch();
+}
+
+xkv_status append_e4m3(const xkv_dims* d, const xkv_cache* c, int layer_begin, int n_units, const void* k_new,
+                       const void* v_new, void* workspace, cudaStream_t st) {
+  AppendParams p;
+  p.k_new = static_cast<const __nv_bfloat16*>(k_new);
+  p.v_new = static_cast<const __nv_bfloat16*>(v_new);
+  p.k_pages = static_cast<uint8_t*>(c->k_pages);
+  p.v_pages = static_cast<uint8_t*>(c->v_pages);
+  p.k_scales = c->k_scales;
+  p.v_scales = c->v_scales;
+  p.block_table = c->block_table;
+  p.seq_lens = c->seq_lens;
+  p.layer_begin = layer_begin;
+  p.batch = d->batch;
+  p.n_kv_heads = d->n_kv_heads;
+  p.page_size = c->page_size;
+  p.max_pages_per_seq = c->max_pages_per_seq;
+  p.n_pages = c->n_pages;
+  p.hdr = static_cast<WorkspaceHeader*>(workspace);
+  if (d->head_dim == 128) append_block_kernel<128><<<n_units, kStoreThreads, 0, st>>>(p);
+  else                    append_block_kernel<64><<<n_units, kStoreThreads, 0, st>>>(p);
+  count_launch();
+  return check_launch();
+}
+
+}  // namespace xkv

@@ -23,13 +23,17 @@ class XkvSession:
                  max_new_tokens: int = 0, max_budget: int | None = None, total_budget: int | None = None,
                  curve_len: int | None = None, device="cuda:0", scale: float = 0.0,
                  decode_chunk_rows: int = 0, n_lanes: int = 6, head_level: bool = False,
-                 kv_format: int = xkv.KV_BF16):
+                 kv_format: int = xkv.KV_BF16, pages_on_demand: bool = False):
         """head_level: budgets, cache lengths and page lists per (layer, sequence, KV head) instead of per (layer,
         sequence); total_budget and the solver's total then count prefix tokens over all heads of all layers, and
-        max_budget bounds one head."""
+        max_budget bounds one head.
+        pages_on_demand: caches take pages from the pool as they grow (planned on the device, `append`); otherwise the
+        pages of all max_new_tokens are set aside when the budgets are known."""
         self.L, self.Hq, self.Hkv, self.d, self.W = n_layers, n_q_heads, n_kv_heads, head_dim, window
         self.head_level = bool(head_level)
-        self.kv_format = kv_format                 # xkv.KV_INT8: the reduced caches hold 8-bit codes and row scales
+        # xkv.KV_INT8: the reduced caches hold 8-bit codes and row scales; xkv.KV_E4M3: 8-bit floats and block scales
+        self.kv_format = kv_format
+        self.pages_on_demand = bool(pages_on_demand)
         self.G = n_q_heads // n_kv_heads
         self.B = len(lengths)
         self.lengths = list(lengths)
@@ -98,13 +102,14 @@ class XkvSession:
             n_pages += math.ceil(rows / page_size)
         self.n_pages = max(n_pages, 1)
         bf16 = dict(dtype=torch.bfloat16, device=self.device)
-        page_dtype = torch.uint8 if kv_format == xkv.KV_INT8 else torch.bfloat16
+        page_dtype = torch.bfloat16 if kv_format == xkv.KV_BF16 else torch.uint8
         self.k_pages = torch.zeros(self.n_pages, page_heads, page_size, head_dim, dtype=page_dtype, device=self.device)
         self.v_pages = torch.zeros(self.n_pages, page_heads, page_size, head_dim, dtype=page_dtype, device=self.device)
         self.k_scales = self.v_scales = None
-        if kv_format == xkv.KV_INT8:
-            self.k_scales = torch.zeros(self.n_pages, page_heads, page_size, **f32)
-            self.v_scales = torch.zeros(self.n_pages, page_heads, page_size, **f32)
+        if kv_format != xkv.KV_BF16:
+            n_scales = page_size if kv_format == xkv.KV_INT8 else page_size // xkv.SCALE_BLOCK
+            self.k_scales = torch.zeros(self.n_pages, page_heads, n_scales, **f32)
+            self.v_scales = torch.zeros(self.n_pages, page_heads, n_scales, **f32)
         self.block_table = torch.zeros(n_layers, self.n_caches, self.max_pages_per_seq, dtype=torch.int32,
                                        device=self.device)
         # page runs of every (layer, cache): [0] first page, [1] number of pages; expanded on the device
@@ -120,6 +125,11 @@ class XkvSession:
         # decode sees the head-level caches as B*Hkv sequences of one KV head with G query heads each
         self.dec_dims = self.dims if not self.head_level else xkv.Dims(
             self.n_caches, self.G, 1, head_dim, window, pool_kernel, pool_mode, scale, head_dim, head_dim)
+        self.ws_plan = self.ws_store = None
+        if self.pages_on_demand:
+            self.pages_used = torch.zeros(1, dtype=torch.int32, device=self.device)
+            self.ws_plan = self._ws(xkv.workspace_bytes(xkv.OP_PLAN_APPEND, self.dec_dims, n_layers=n_layers))
+            self.ws_store = self._ws(xkv.workspace_bytes(xkv.OP_STORE_ROWS, self.dec_dims))
         self.chunk_rows = decode_chunk_rows
         self.ws_decode = self._ws(xkv.workspace_bytes(xkv.OP_DECODE_ATTN, self.dec_dims, n_layers=n_layers,
                                                       max_cache_len=self.max_pages_per_seq * page_size,
@@ -313,10 +323,17 @@ class XkvSession:
         window = np.minimum(self.W, np.asarray(self.lengths))[None, :]
         if self.head_level:                                  # budgets [L, Hkv] -> one cache per (layer, b, g)
             k_lb = np.broadcast_to(budgets.reshape(self.L, 1, self.Hkv), (self.L, self.B, self.Hkv))
-            rows = (np.minimum(k_lb, prefix[:, :, None]) + window[:, :, None] + self.max_new).reshape(self.L, -1)
+            rows = (np.minimum(k_lb, prefix[:, :, None]) + window[:, :, None]).reshape(self.L, -1)
         else:
             k_lb = budgets.T if budgets.ndim == 2 else np.broadcast_to(budgets[:, None], (self.L, self.B))   # [L, B]
-            rows = np.minimum(k_lb, prefix) + window + self.max_new
+            rows = np.minimum(k_lb, prefix) + window
+        if self.pages_on_demand:                             # the kept rows only: tables and lengths from nothing
+            self.page_runs_host[0].numpy()[:] = rows
+            self.page_runs[0].copy_(self.page_runs_host[0], non_blocking=True)
+            xkv.plan_append(self.cache, self.n_caches, self.page_runs[0], self.n_caches, None, None, self.n_pages, None,
+                            self.pages_used, None, 0, self.ws_plan)
+            return
+        rows = rows + self.max_new
         n = np.minimum(-(-rows // self.page_size), self.max_pages_per_seq).astype(np.int64)               # pages
         start = np.concatenate([[0], np.cumsum(n.ravel())[:-1]]).reshape(self.L, self.n_caches)
         if int(start.ravel()[-1] + n.ravel()[-1]) > self.n_pages:
@@ -350,12 +367,48 @@ class XkvSession:
         return budgets
 
     # ------------------------------------------------------------------ generation
+    def append(self, k: torch.Tensor, v: torch.Tensor, n_new) -> torch.Tensor:
+        """Stores n_new[b] more rows of every sequence in every layer (a further turn of a conversation, a generated
+        token): k, v bf16 [L, T, Hkv, d], the sequences' tokens one after the other, T = sum(n_new) (host integers).
+        Needs pages_on_demand.  Returns the slots, int64 [L, T] ([L, T*Hkv] in a head-level session)."""
+        if not self.pages_on_demand:
+            raise ValueError("append needs a session with pages_on_demand=True")
+        self.join()
+        n_new = np.asarray(n_new, dtype=np.int32)
+        T = int(n_new.sum())
+        if n_new.shape != (self.B,) or int(n_new.min()) < 0 or tuple(k.shape) != (self.L, T, self.Hkv, self.d) \
+                or k.shape != v.shape:
+            raise ValueError("append: k and v are [L, sum(n_new), Hkv, d], n_new one count per sequence")
+        counts = n_new
+        if self.head_level:                                  # caches (b, g): a sequence's tokens head by head
+            counts = np.repeat(n_new, self.Hkv)
+            if T:
+                first = np.concatenate([[0], np.cumsum(n_new)[:-1]])
+                order = np.concatenate([((first[b] + np.arange(n_new[b]))[None, :] * self.Hkv +
+                                         np.arange(self.Hkv)[:, None]).ravel() for b in range(self.B)])
+                order = torch.from_numpy(order.astype(np.int64)).to(self.device)
+                k, v = (x.reshape(self.L, T * self.Hkv, self.d)[:, order] for x in (k, v))
+        n_tokens = int(counts.sum())
+        slots = torch.empty(self.L, n_tokens, dtype=torch.int64, device=self.device)
+        xkv.plan_append(self.cache, self.n_caches, torch.from_numpy(counts).to(self.device), 0, self.seq_lens, None,
+                        self.n_pages, self.pages_used, self.pages_used, slots if n_tokens else None, n_tokens, self.ws_plan)
+        # the layers' tokens are one list: their rows lie one after the other and so do their slots
+        if n_tokens:
+            xkv.store_rows(self.dec_dims, self.cache, k.contiguous(), v.contiguous(), slots, self.L * n_tokens,
+                           self.ws_store)
+        return slots
+
     def decode(self, q: torch.Tensor, k_new: torch.Tensor | None, v_new: torch.Tensor | None,
                out: torch.Tensor | None = None, lse: torch.Tensor | None = None, layer_begin: int = 0,
                layer_end: int | None = None, chunk_rows: int | None = None) -> torch.Tensor:
         self.join()
         out = self.out if out is None else out
         layer_end = self.L if layer_end is None else layer_end
+        if self.pages_on_demand and k_new is not None:
+            if (layer_begin, layer_end) != (0, self.L):
+                raise ValueError("with pages_on_demand a step plans all layers: append first, then decode layer by layer")
+            self.append(k_new, v_new, np.ones(self.B, dtype=np.int32))
+            k_new = v_new = None
         xkv.decode_attn(self.dec_dims, self.cache, layer_begin, layer_end, q, k_new, v_new, out,
                         self.lse if lse is None else lse,
                         self.chunk_rows if chunk_rows is None else chunk_rows, self.ws_decode)
@@ -366,7 +419,8 @@ class XkvSession:
         reading resets them), XKV_OK otherwise."""
         self.join()
         ws = {"decode": [self.ws_decode], "score": self.ws_score, "select": self.ws_select,
-              "prefill": [] if self.ws_prefill is None else [self.ws_prefill]}[which]
+              "prefill": [] if self.ws_prefill is None else [self.ws_prefill],
+              "append": [] if self.ws_plan is None else [self.ws_plan, self.ws_store]}[which]
         first = xkv.OK
         for w in ws:
             st = xkv.read_device_status(w)

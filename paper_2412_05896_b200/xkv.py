@@ -18,13 +18,15 @@ OK = 0
 ERR_INVALID_ARG, ERR_UNSUPPORTED, ERR_WORKSPACE, ERR_BUDGET = -1, -2, -3, -4
 ERR_CUDA, ERR_TIMEOUT, ERR_CAPACITY = -5, -6, -7
 POOL_MAX, POOL_AVG = 0, 1
-OP_SCORE, OP_SELECT_COMPACT, OP_DECODE_ATTN, OP_PREFILL_ATTN = 0, 1, 2, 3
+OP_SCORE, OP_SELECT_COMPACT, OP_DECODE_ATTN, OP_PREFILL_ATTN, OP_PLAN_APPEND, OP_STORE_ROWS = 0, 1, 2, 3, 4, 5
 BUDGET_PER_LAYER, BUDGET_PER_SEQUENCE, BUDGET_PER_HEAD = 0, 1, 2
-KV_BF16, KV_INT8 = 0, 1
+KV_BF16, KV_INT8, KV_E4M3 = 0, 1, 2
+SCALE_BLOCK = 16                 # KV_E4M3: consecutive cache slots that share a scale
 
 STATIC_SCRATCH_BYTES = 16 << 20
 
 EXPORTS = ("xkv_score", "xkv_score_lse", "xkv_prefill_attn", "xkv_batch_curves", "xkv_head_curves", "xkv_build_block_table", "xkv_alloc_budgets", "xkv_average_budgets", "xkv_select_compact", "xkv_decode_attn", "xkv_decode_attn_static",
+           "xkv_plan_append", "xkv_store_rows",
            "xkv_workspace_bytes",
            "xkv_read_device_status", "xkv_profile_events", "xkv_test_hooks", "xkv_launch_count", "xkv_status_string",
            "xkv_version")
@@ -90,6 +92,10 @@ def lib() -> ctypes.CDLL:
     L.xkv_decode_attn_static.restype = i32
     L.xkv_decode_attn_static.argtypes = [ctypes.POINTER(Dims), ctypes.POINTER(Cache), i32, i32, vp, vp, vp, vp,
                                          vp, i32, vp, vp]
+    L.xkv_plan_append.restype = i32
+    L.xkv_plan_append.argtypes = [ctypes.POINTER(Cache), i32, vp, i32, vp, vp, i32, vp, vp, vp, i64, vp, sz, vp]
+    L.xkv_store_rows.restype = i32
+    L.xkv_store_rows.argtypes = [ctypes.POINTER(Dims), ctypes.POINTER(Cache), vp, vp, vp, i64, vp, sz, vp]
     L.xkv_workspace_bytes.restype = sz
     L.xkv_workspace_bytes.argtypes = [i32, ctypes.POINTER(Dims), i32, i64, i32, i32, i32]
     L.xkv_read_device_status.restype = i32
@@ -233,6 +239,21 @@ def select_compact(dims: Dims, layer: int, budget, per_sequence, scores, sorted_
                                     _ptr(scores), _ptr(sorted_scores), _ptr(k), _ptr(v), _ptr(cu_seqlens),
                                     total_tokens, max_seqlen, ctypes.byref(cache), _ptr(sel), sel_stride,
                                     _ptr(workspace), _nbytes(workspace), _stream(stream)), "xkv_select_compact")
+
+
+def plan_append(cache: Cache, batch: int, n_new, n_new_stride: int, lens_before, free_pages, n_free: int,
+                pages_used_before, pages_used_after, slots, slots_stride: int, workspace, stream=None) -> None:
+    """Block tables, slot maps (dev int64 [L, slots_stride]) and new lengths of a step; n_new dev int32 [B] (stride 0)
+    or [L, n_new_stride]."""
+    _check(lib().xkv_plan_append(ctypes.byref(cache), batch, _ptr(n_new), n_new_stride, _ptr(lens_before),
+                                 _ptr(free_pages), n_free, _ptr(pages_used_before), _ptr(pages_used_after), _ptr(slots),
+                                 slots_stride, _ptr(workspace), _nbytes(workspace), _stream(stream)), "xkv_plan_append")
+
+
+def store_rows(dims: Dims, cache: Cache, k, v, slots, n_tokens: int, workspace, stream=None) -> None:
+    """k, v dev bf16 rows (strides of dims) stored at slots dev int64 [n_tokens]; negative slots are skipped."""
+    _check(lib().xkv_store_rows(ctypes.byref(dims), ctypes.byref(cache), _ptr(k), _ptr(v), _ptr(slots), n_tokens,
+                                _ptr(workspace), _nbytes(workspace), _stream(stream)), "xkv_store_rows")
 
 
 def decode_attn(dims: Dims, cache: Cache, layer_begin: int, layer_end: int, q, k_new, v_new, out, lse,
