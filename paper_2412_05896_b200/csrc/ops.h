@@ -46,14 +46,13 @@ xkv_status decode_attn_static(const xkv_dims* d, const xkv_cache* c, int layer_b
 struct DecodeScratch {
   void* header;
   int32_t* tickets;    // [n_layers * batch * n_kv_heads], zero at the start of the call like the rest of the header
-  int4* items;         // [max_items]
   float* part_o;       // [max_items][G][d]
   float* part_ml;      // [max_items][G][2]
   int64_t max_items;
 };
 xkv_status decode_attn_e4m3(const xkv_dims* d, const xkv_cache* c, int layer_begin, int n_layers, const void* q,
-                            const void* k_new, const void* v_new, void* out, float* lse, int chunk_rows,
-                            const DecodeScratch& ws, cudaStream_t st);
+                            const void* k_new, const void* v_new, void* out, float* lse, const DecodeScratch& ws,
+                            cudaStream_t st);
 // One new row per (layer, sequence) and KV head stored in a cache of 8-bit floats, lengths advanced.
 xkv_status append_e4m3(const xkv_dims* d, const xkv_cache* c, int layer_begin, int n_units, const void* k_new,
                        const void* v_new, void* workspace, cudaStream_t st);

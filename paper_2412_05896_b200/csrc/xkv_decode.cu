@@ -1121,9 +1121,9 @@ xkv_status decode_attn(const xkv_dims* d, const xkv_cache* c, int layer_begin, i
     const size_t keep = clear_status ? 0 : sizeof(int32_t);   // see below
     if (cudaMemsetAsync(base + keep, 0, L.unit_info - keep, st) != cudaSuccess) return XKV_ERR_CUDA;
     const DecodeScratch scratch = {base, reinterpret_cast<int32_t*>(base + L.tickets),
-                                   reinterpret_cast<int4*>(base + L.items), reinterpret_cast<float*>(base + L.part_o),
-                                   reinterpret_cast<float*>(base + L.part_ml), L.max_items};
-    return decode_attn_e4m3(d, c, layer_begin, Lr, q, k_new, v_new, out, lse, chunk_rows, scratch, st);
+                                   reinterpret_cast<float*>(base + L.part_o), reinterpret_cast<float*>(base + L.part_ml),
+                                   L.max_items};
+    return decode_attn_e4m3(d, c, layer_begin, Lr, q, k_new, v_new, out, lse, scratch, st);
   }
 
   const bool q8 = c->kv_format == XKV_KV_INT8;

@@ -1,122 +1,776 @@
-// Decode attention over caches of 8-bit floats with one scale per block of 16 slots and KV head (Eq. 1).
+// Decode attention over caches of 8-bit floats with one scale per block of 16 slots and KV head (Eq. 1, one query row
+// per head), on the 5th-generation tensor cores without converting a cached byte.
 //
-// One CTA per (layer, sequence, KV head); a warp takes every fourth cached row, its lanes share the row's columns, and
-// the four warps' softmax states are joined at the end.  All arithmetic in fp32.
+// Mathematics.  With stored codes k, v (e4m3), block scales s_k, s_v and the G query heads of a KV head:
+//   logits  S[c, h] = (codes k_c . q_h) s_k[c] scale          M = 128 cache rows, N = heads, K = d
+//   output  O[j, h] = sum_c v[c, j] (s_v[c] P[c, h])          M = d, N = heads, K = 128 cache rows
+// Both products are tcgen05.mma kind::f8f6f4 with the cache tile as the A operand exactly as it lies in the page (K rows
+// are K-major, V rows are M-major), fp32 accumulators in tensor memory.  The small operand has more bits than one code
+// holds, so it enters as two codes side by side on the N axis: q = a1 + a2 / 32 and p = b1 + b2 / 32, each part rounded to
+// nearest.  The query is scaled so that its largest element lies in [128, 256): a bf16 value (8 significant bits) is
+// exactly such a sum down to 2^-15, 2^-22 of the largest.  The weights of a tile are scaled so that its largest possible
+// one is 256: the sum keeps 2^-8 of a weight (the rounding of bf16) down to 2^-15, 2^-23 of the tile's largest.  Because that
+// range is per tile, every tile's product goes to fresh accumulators and is added in fp32 registers with the tile's
+// own factor; nothing in tensor memory is ever rescaled.
+//
+// Shape of the launch: two CTAs of seven warps per SM, no CTA waits for another one.  All tiles of all (layer, sequence,
+// KV head) caches, in that order, are dealt out evenly: CTA c takes tiles [c T / C, (c + 1) T / C), found by every CTA
+// for itself from the lengths.  A cache cut by a boundary leaves partial results (m, l, O), at most two pieces a CTA, and
+// the CTA that finishes its last piece joins them in the order of the pieces.
+//   warp 4     walks the CTA's tiles: descriptors of the cache pieces ("items"), TMA boxes of K and V, block scales
+//   warp 5     one thread issues the MMAs: logits up to two tiles ahead of the outputs
+//   warp 6     the items' queries as two codes per element
+//   warps 0-3  one thread per cache row: logits out of tensor memory, the tile's maximum (one exchange among the four
+//              warps), weights back as codes; then, as one thread per output column, O of the tile before
+#include <cuda.h>
+
+#include <atomic>
 #include <cmath>
 
 #include "common.cuh"
 #include "e4m3.cuh"
 #include "ops.h"
+#include "tc_common.cuh"
 
 namespace xkv {
 namespace {
 
-constexpr int kMaxGroup = 8;
-constexpr int kWarps = 4;
+using tc::tc_fence_after_sync;
+using tc::tc_fence_before_sync;
+using tc::tmem_alloc;
+using tc::tmem_dealloc;
+using tc::tmem_relinquish;
+using tc::tmem_wait_ld;
+using tc::umma_commit;
+using tc::ws_wait;
+
+constexpr int kTile = 128;            // cache rows per tile
+constexpr int kN = 16;                // N of both MMAs: two codes x up to eight heads, the rest zero rows
+constexpr int kThreads = 224;
+constexpr int kSoftThreads = 128;
+constexpr int kFifo = 3;              // items between the walk and the last reader
+constexpr int kTmemCols = 64;         // two logit buffers and two output buffers of 16 columns
+constexpr int kCtasPerSm = 2;
+constexpr float kPart = 32.f;         // weight of the second code
+constexpr int kBarSoft = 1;           // named barrier of warps 0-3
+
+template <int D>
+struct Cfg {
+  static constexpr int kStages = D == 128 ? 3 : 6;              // K and V tiles of 16 KB (8 KB): 96 KB a CTA
+  static constexpr int kTileBytes = kTile * D;
+  static constexpr int kQBytes = kN * D;
+  static constexpr int kPBytes = kN * kTile;
+  static constexpr int kOffV = kStages * kTileBytes;
+  static constexpr int kOffQ = 2 * kStages * kTileBytes;
+  static constexpr int kOffP = kOffQ + kFifo * kQBytes;
+  static constexpr int kOffScales = kOffP + 2 * kPBytes;         // [kStages][16]: 8 of K, 8 of V
+  static constexpr int kSmemBytes = 1024 + kOffScales + kStages * 64;
+};
 
 struct Params {
   const __nv_bfloat16* q;
   __nv_bfloat16* out;
   float* lse;
-  const uint8_t* k_pages;
-  const uint8_t* v_pages;
   const float* k_scales;
   const float* v_scales;
   const int32_t* block_table;
   const int32_t* seq_lens;
-  int32_t layer_begin, batch, n_q_heads, n_kv_heads, group, page_size, max_pages_per_seq, n_pages;
+  int32_t layer_begin, batch, n_units, n_q_heads, n_kv_heads, group, page_size, max_pages_per_seq, n_pages;
+  int32_t box_rows;                   // rows of a TMA box: the largest power of two up to 128 that divides page_size
+  int32_t max_ctas;                   // CTAs that the partial results have room for
   float scale_log2;
+  uint64_t wait_ns;
+  WorkspaceHeader* hdr;
+  int32_t* tickets;                   // [units * n_kv_heads] pieces of a cache that are done
+  float* part_o;                      // [2 * CTAs][G][D]
+  float* part_ml;                     // [2 * CTAs][G][2]
 };
 
-template <int D>
-__global__ void __launch_bounds__(32 * kWarps) decode_rows_kernel(const Params p) {
-  constexpr int kCols = D / 32;
-  __shared__ float s_o[kWarps][kMaxGroup][D];
-  __shared__ float s_ml[kWarps][kMaxGroup][2];
-  const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5;
-  const int e = blockIdx.x / p.n_kv_heads, h = blockIdx.x % p.n_kv_heads;
-  const size_t le = (size_t)p.layer_begin * p.batch + e;
-  const int n = min(max(p.seq_lens[le], 0), p.max_pages_per_seq * p.page_size);
-  const size_t row0 = (size_t)e * p.n_q_heads + (size_t)h * p.group;
-  float q[kMaxGroup][kCols], o[kMaxGroup][kCols], m[kMaxGroup], l[kMaxGroup], lost[kMaxGroup];
+struct Item {                         // one CTA's piece of one cache
+  int32_t e, h, row0, rows;           // unit, KV head, first row, rows; e < 0: no more
+  int32_t first_cta, n_pieces;        // the CTAs that share the cache
+};
+
+// D[tmem] (+)= A[smem] B[smem]^T, e4m3 x e4m3 -> fp32; issued by one thread.
+__device__ __forceinline__ void umma_e4m3(uint32_t tmem_d, uint64_t adesc, uint64_t bdesc, uint32_t idesc,
+                                          uint32_t accumulate) {
+  asm volatile(
+      "{\n\t"
+      ".reg .pred p;\n\t"
+      "setp.ne.b32 p, %4, 0;\n\t"
+      "tcgen05.mma.cta_group::1.kind::f8f6f4 [%0], %1, %2, %3, {%5, %5, %5, %5}, p;\n\t"
+      "}\n" ::"r"(tmem_d),
+      "l"(adesc), "l"(bdesc), "r"(idesc), "r"(accumulate), "r"(0u)
+      : "memory");
+}
+
+// Shared-memory matrix descriptor: rows of kRowBytes (128: 128-byte swizzle, 64: 64-byte swizzle), groups of eight rows
+// 8 * kRowBytes apart.  The same for a K-major operand (rows = M or N) and an M-major one (rows = K) whose M extent is
+// the row.
+template <int kRowBytes>
+__device__ __forceinline__ uint64_t smem_desc(uint32_t addr) {
+  uint64_t d = (uint64_t)((addr & 0x3ffffu) >> 4);
+  d |= (uint64_t)1 << 16;
+  d |= (uint64_t)((8 * kRowBytes) >> 4) << 32;
+  d |= (uint64_t)1 << 46;
+  d |= (uint64_t)(kRowBytes == 128 ? 2 : 4) << 61;
+  return d;
+}
+// e4m3 x e4m3 -> fp32, M x N; a_mn: the A operand is M-major
+__host__ __device__ constexpr uint32_t idesc_e4m3(int M, int N, bool a_mn) {
+  return (1u << 4) | (a_mn ? 1u << 15 : 0u) | ((uint32_t)(N >> 3) << 17) | ((uint32_t)(M >> 4) << 24);
+}
+// byte offset of (row, column byte) in a swizzled operand
+template <int kRowBytes>
+__device__ __forceinline__ uint32_t swizzled(int row, int col) {
+  const int x = kRowBytes == 128 ? (row & 7) : ((row >> 1) & 3);
+  return (uint32_t)(row * kRowBytes + (((col >> 4) ^ x) << 4) + (col & 15));
+}
+
+template <int N>
+__device__ __forceinline__ void tmem_ld(uint32_t taddr, float (&v)[N]) {
+  uint32_t r[N];
+  if constexpr (N == 2) {
+    asm volatile("tcgen05.ld.sync.aligned.32x32b.x2.b32 {%0, %1}, [%2];" : "=r"(r[0]), "=r"(r[1]) : "r"(taddr) : "memory");
+  } else if constexpr (N == 4) {
+    asm volatile("tcgen05.ld.sync.aligned.32x32b.x4.b32 {%0, %1, %2, %3}, [%4];"
+                 : "=r"(r[0]), "=r"(r[1]), "=r"(r[2]), "=r"(r[3])
+                 : "r"(taddr)
+                 : "memory");
+  } else if constexpr (N == 8) {
+    asm volatile("tcgen05.ld.sync.aligned.32x32b.x8.b32 {%0, %1, %2, %3, %4, %5, %6, %7}, [%8];"
+                 : "=r"(r[0]), "=r"(r[1]), "=r"(r[2]), "=r"(r[3]), "=r"(r[4]), "=r"(r[5]), "=r"(r[6]), "=r"(r[7])
+                 : "r"(taddr)
+                 : "memory");
+  } else {
+    static_assert(N == 16, "2, 4, 8 or 16 columns");
+    asm volatile(
+        "tcgen05.ld.sync.aligned.32x32b.x16.b32 {%0, %1, %2, %3, %4, %5, %6, %7, %8, %9, %10, %11, %12, %13, %14, %15}, "
+        "[%16];"
+        : "=r"(r[0]), "=r"(r[1]), "=r"(r[2]), "=r"(r[3]), "=r"(r[4]), "=r"(r[5]), "=r"(r[6]), "=r"(r[7]), "=r"(r[8]),
+          "=r"(r[9]), "=r"(r[10]), "=r"(r[11]), "=r"(r[12]), "=r"(r[13]), "=r"(r[14]), "=r"(r[15])
+        : "r"(taddr)
+        : "memory");
+  }
+  tmem_wait_ld();
 #pragma unroll
-  for (int g = 0; g < kMaxGroup; ++g) {
-    m[g] = -INFINITY;
-    l[g] = 0.f;
-    lost[g] = 0.f;                              // what the running sum l has rounded off (thousands of rows per warp)
+  for (int i = 0; i < N; ++i) v[i] = __uint_as_float(r[i]);
+}
+
+__device__ __forceinline__ float warp_max(float x) {
+  float r;
+  asm volatile("redux.sync.max.f32 %0, %1, 0xffffffff;" : "=f"(r) : "f"(x));
+  return r;
+}
+// Barrier of the four softmax warps that also tells whether any of its threads passed a true predicate.
+__device__ __forceinline__ bool soft_any(bool x) {
+  uint32_t r;
+  asm volatile(
+      "{\n\t.reg .pred p, q;\n\t"
+      "setp.ne.b32 p, %1, 0;\n\t"
+      "barrier.cta.red.or.pred q, %2, %3, p;\n\t"
+      "selp.u32 %0, 1, 0, q;\n\t}"
+      : "=r"(r)
+      : "r"((uint32_t)x), "n"(kBarSoft), "n"(kSoftThreads)
+      : "memory");
+  return r != 0;
+}
+// 4-byte asynchronous copy global -> shared, zero when !valid
+__device__ __forceinline__ void cp_async_4(void* dst, const void* src, bool valid) {
+  asm volatile("cp.async.ca.shared.global [%0], [%1], 4, %2;" ::"r"(smem_u32(dst)), "l"(src), "r"(valid ? 4 : 0) : "memory");
+}
+// the barrier gets one arrival once this thread's copies so far have landed
+__device__ __forceinline__ void cp_async_arrive(uint64_t* bar) {
+  asm volatile("cp.async.mbarrier.arrive.noinc.shared::cta.b64 [%0];" ::"r"(smem_u32(bar)) : "memory");
+}
+
+__device__ __forceinline__ int unit_rows(const Params& p, int e) {
+  const int n = __ldg(&p.seq_lens[(size_t)p.layer_begin * p.batch + e]);
+  return min(max(n, 0), p.max_pages_per_seq * p.page_size);
+}
+__device__ __forceinline__ int tiles_of(int rows) { return (rows + kTile - 1) / kTile; }
+
+template <int D, int GP>              // GP: query heads per KV head, rounded up to a power of two
+__global__ void __launch_bounds__(kThreads, kCtasPerSm)
+decode_e4m3_kernel(const __grid_constant__ CUtensorMap tmap_k, const __grid_constant__ CUtensorMap tmap_v, const Params p) {
+  using C = Cfg<D>;
+  extern __shared__ uint8_t smem_raw[];
+  uint8_t* smem = reinterpret_cast<uint8_t*>((reinterpret_cast<uintptr_t>(smem_raw) + 1023) & ~uintptr_t(1023));
+  __shared__ uint64_t s_k_full[C::kStages], s_k_empty[C::kStages], s_v_full[C::kStages], s_v_empty[C::kStages],
+      s_scale_full[C::kStages], s_s_full[2], s_p_full[2], s_d_full[2], s_fifo_full[kFifo], s_fifo_empty[kFifo],
+      s_q_full[kFifo];
+  __shared__ Item s_item[kFifo];
+  __shared__ float s_qscale[kFifo][8];
+  __shared__ float s_max[2][4][8];
+  __shared__ float s_sum[4][8];
+  __shared__ long long s_scan[8];
+  __shared__ long long s_first[2];                // tile index of the CTA's first unit, that unit
+  __shared__ uint32_t s_tmem;
+  __shared__ int s_abort_store, s_last;
+  volatile int* s_abort = &s_abort_store;
+  const int tid = threadIdx.x, lane = tid & 31, warp = tid >> 5;
+  const int Hkv = p.n_kv_heads, G = p.group;
+
+  if (tid == 0) {
+    for (int i = 0; i < C::kStages; ++i) {
+      mbar_init(&s_k_full[i], 1);
+      mbar_init(&s_k_empty[i], 1);
+      mbar_init(&s_v_full[i], 1);
+      mbar_init(&s_v_empty[i], 1);
+      mbar_init(&s_scale_full[i], 32);
+    }
+    for (int i = 0; i < 2; ++i) {
+      mbar_init(&s_s_full[i], 1);
+      mbar_init(&s_p_full[i], 4);
+      mbar_init(&s_d_full[i], 1);
+    }
+    for (int i = 0; i < kFifo; ++i) {
+      mbar_init(&s_fifo_full[i], 1);
+      mbar_init(&s_fifo_empty[i], 5);             // the logit MMAs of the item, four softmax warps
+      mbar_init(&s_q_full[i], 1);
+    }
+    s_abort_store = 0;
+    fence_mbar_init();
+    prefetch_tmap(&tmap_k);
+    prefetch_tmap(&tmap_v);
+  }
+  if (warp == 5) {
+    tmem_alloc(&s_tmem, kTmemCols);
+    tmem_relinquish();
+  }
+  // operand rows that no head fills stay zero
+  for (int i = tid; i < (kFifo * C::kQBytes + 2 * C::kPBytes) / 16; i += kThreads)
+    reinterpret_cast<uint4*>(smem + C::kOffQ)[i] = make_uint4(0u, 0u, 0u, 0u);
+  fence_proxy_async_smem();
+
+  // ---- the CTA's share: tiles before each thread's run of units, then the unit that holds the first tile
+  const int per = (p.n_units + kThreads - 1) / kThreads;
+  long long mine = 0;
+  for (int i = 0; i < per; ++i) {
+    const int e = tid * per + i;
+    if (e < p.n_units) mine += tiles_of(unit_rows(p, e));
+  }
+  long long incl = mine;
 #pragma unroll
-    for (int j = 0; j < kCols; ++j) {
-      o[g][j] = 0.f;
-      q[g][j] = g < p.group ? __bfloat162float(p.q[(row0 + g) * D + lane * kCols + j]) * p.scale_log2 : 0.f;
+  for (int o = 1; o < 32; o <<= 1) {
+    const long long x = __shfl_up_sync(0xffffffffu, incl, o);
+    if (lane >= o) incl += x;
+  }
+  if (lane == 31) s_scan[warp] = incl;
+  tc_fence_before_sync();
+  __syncthreads();
+  tc_fence_after_sync();
+  long long T = 0, before = incl - mine;
+#pragma unroll
+  for (int w = 0; w < kThreads / 32; ++w) {
+    if (w < warp) before += s_scan[w];
+    T += s_scan[w];
+  }
+  T *= Hkv;
+  const long long n_ctas = min(min((long long)gridDim.x, (long long)p.max_ctas), max(T, 1ll));
+  const long long t_begin = blockIdx.x < n_ctas ? blockIdx.x * T / n_ctas : T;
+  const long long t_end = blockIdx.x < n_ctas ? (blockIdx.x + 1) * T / n_ctas : T;
+  if (t_begin < t_end && before * Hkv <= t_begin && t_begin < (before + mine) * Hkv) {
+    long long at = before * Hkv;
+    for (int i = 0; i < per; ++i) {
+      const int e = tid * per + i;
+      const int nt = e < p.n_units ? tiles_of(unit_rows(p, e)) : 0;
+      if (t_begin < at + (long long)nt * Hkv) {
+        s_first[0] = at;
+        s_first[1] = e;
+        break;
+      }
+      at += (long long)nt * Hkv;
     }
   }
-  for (int r = warp; r < n; r += kWarps) {
-    int page = p.block_table[le * p.max_pages_per_seq + r / p.page_size];
-    page = min(max(page, 0), p.n_pages - 1);
-    const size_t row = ((size_t)page * p.n_kv_heads + h) * p.page_size + r % p.page_size;
-    const float ks = p.k_scales[row / kScaleBlock], vs = p.v_scales[row / kScaleBlock];
-    float k[kCols], v[kCols];
-#pragma unroll
-    for (int j = 0; j < kCols; j += 2) {
-      const float2 a = f32_from_e4m3x2(*reinterpret_cast<const uint16_t*>(p.k_pages + row * D + lane * kCols + j));
-      const float2 b = f32_from_e4m3x2(*reinterpret_cast<const uint16_t*>(p.v_pages + row * D + lane * kCols + j));
-      k[j] = a.x; k[j + 1] = a.y;
-      v[j] = b.x; v[j + 1] = b.y;
-    }
-#pragma unroll
-    for (int g = 0; g < kMaxGroup; ++g) {
-      if (g >= p.group) break;
-      float s = 0.f;
-#pragma unroll
-      for (int j = 0; j < kCols; ++j) s += q[g][j] * k[j];
-#pragma unroll
-      for (int x = 16; x > 0; x >>= 1) s += __shfl_xor_sync(0xffffffffu, s, x);
-      s *= ks;
-      const float mn = fmaxf(m[g], s);
-      const float al = m[g] == mn ? 1.f : exp2f(m[g] - mn), w = exp2f(s - mn);
-      m[g] = mn;
-      l[g] *= al;
-      const float y = w - lost[g] * al, t = l[g] + y;
-      lost[g] = (t - l[g]) - y;
-      l[g] = t;
-#pragma unroll
-      for (int j = 0; j < kCols; ++j) o[g][j] = o[g][j] * al + w * vs * v[j];
-    }
+  // rows of empty caches
+  for (int e = blockIdx.x; e < p.n_units; e += gridDim.x) {
+    if (unit_rows(p, e) != 0) continue;
+    const size_t row0 = (size_t)e * p.n_q_heads;
+    for (int i = tid; i < p.n_q_heads * D / 8; i += kThreads)
+      reinterpret_cast<uint4*>(p.out + row0 * D)[i] = make_uint4(0u, 0u, 0u, 0u);
+    if (p.lse != nullptr)
+      for (int i = tid; i < p.n_q_heads; i += kThreads) p.lse[row0 + i] = -INFINITY;
   }
-#pragma unroll
-  for (int g = 0; g < kMaxGroup; ++g) {
-    if (g >= p.group) break;
-#pragma unroll
-    for (int j = 0; j < kCols; ++j) s_o[warp][g][lane * kCols + j] = o[g][j];
+  __syncthreads();
+  const uint32_t tmem = s_tmem;
+
+  if (warp == 4) {
+    // ================================================================ the walk and the copies
+    const int R = p.box_rows, boxes_per_tile = kTile / R;
+    long long at = t_begin;                       // next tile of the CTA
+    int e = 0, h = 0, rows = 0, nt = 0;
+    long long unit_at = 0;                        // tile index of (e, head 0)
+    if (t_begin < t_end) {
+      unit_at = s_first[0];
+      e = (int)s_first[1];
+      rows = unit_rows(p, e);
+      nt = tiles_of(rows);
+      h = (int)((t_begin - unit_at) / nt);
+    }
+    // the CTA that works on tile x
+    auto cta_of = [&](long long x) -> int {
+      long long c = x * n_ctas / T;
+      while ((c + 1) * T / n_ctas <= x) ++c;
+      while (c * T / n_ctas > x) --c;
+      return (int)c;
+    };
+    auto next_item = [&]() -> Item {
+      Item it = {-1, 0, 0, 0, 0, 0};
+      if (at >= t_end) return it;
+      while (h == Hkv || nt == 0) {               // on to the next cache that holds rows
+        unit_at += (long long)nt * Hkv;
+        ++e;
+        h = 0;
+        if (e >= p.n_units) return it;
+        rows = unit_rows(p, e);
+        nt = tiles_of(rows);
+      }
+      const long long g0 = unit_at + (long long)h * nt, g1 = g0 + nt;      // tiles of this (cache, KV head)
+      const long long stop = min(g1, t_end);
+      it.e = e;
+      it.h = h;
+      it.row0 = (int)(at - g0) * kTile;
+      it.rows = min(rows, (int)(stop - g0) * kTile) - it.row0;
+      if (g0 >= t_begin && g1 <= t_end) {
+        it.first_cta = blockIdx.x;
+        it.n_pieces = 1;
+      } else {
+        it.first_cta = cta_of(g0);
+        it.n_pieces = cta_of(g1 - 1) - it.first_cta + 1;
+      }
+      at = stop;
+      ++h;
+      return it;
+    };
+    // page of box `lane` of a batch of 32 boxes of an item
+    auto load_pages = [&](const Item& it, int box0) -> int {
+      const int r = it.row0 + (box0 + lane) * R;
+      int page = 0;
+      if (it.e >= 0 && r < it.row0 + it.rows)
+        page = __ldg(&p.block_table[((size_t)p.layer_begin * p.batch + it.e) * p.max_pages_per_seq + r / p.page_size]);
+      return page;
+    };
+    Item cur = next_item();
+    int pages = load_pages(cur, 0);
+    uint32_t j = 0, n_item = 0;                   // tiles issued, items published
+    bool ok = true;
+    while (ok) {
+      const int slot = n_item % kFifo;
+      if (n_item >= kFifo) ok = ws_wait(&s_fifo_empty[slot], ((n_item / kFifo) - 1) & 1, s_abort, p.wait_ns);
+      ok = __all_sync(0xffffffffu, ok);
+      if (!ok) break;
+      if (lane == 0) {
+        s_item[slot] = cur;
+        mbar_arrive(&s_fifo_full[slot]);
+      }
+      ++n_item;
+      if (cur.e < 0) break;
+      const Item nxt = next_item();
+      int ahead = 0;
+      const int n_tiles = tiles_of(cur.rows);
+      for (int t = 0; t < n_tiles; ++t, ++j) {
+        const int box0 = t * boxes_per_tile;
+        if ((box0 & 31) == 0) {                   // a new batch of page ids; the next one is on its way meanwhile
+          if (t > 0) pages = ahead;
+          ahead = (box0 + 32) * R < cur.rows ? load_pages(cur, box0 + 32) : load_pages(nxt, 0);
+        }
+        const int stage = j % C::kStages;
+        const uint32_t ph = ((j / C::kStages) - 1) & 1;
+        const int left = min(kTile, cur.rows - t * kTile);
+        const int n_box = (left + R - 1) / R, n_blk = (left + kScaleBlock - 1) / kScaleBlock;
+        // first row of this lane's box in the page pool (lanes past the last box: not used)
+        const int row_of_box = cur.row0 + t * kTile + lane * R;
+        int page = __shfl_sync(0xffffffffu, pages, (box0 + lane) & 31);
+        page = min(max(page, 0), p.n_pages - 1);
+        const int grow = (page * Hkv + cur.h) * p.page_size + row_of_box % p.page_size;
+        if (j >= C::kStages) ok = ws_wait(&s_k_empty[stage], ph, s_abort, p.wait_ns);
+        ok = __all_sync(0xffffffffu, ok);
+        if (!ok) break;
+        if (lane == 0) mbar_arrive_expect_tx(&s_k_full[stage], (uint32_t)(n_box * R * D));
+        __syncwarp();
+        if (lane < n_box)
+          tma_load_2d(smem + stage * C::kTileBytes + lane * R * D, &tmap_k, 0, grow, &s_k_full[stage]);
+        if (j >= C::kStages) ok = ws_wait(&s_v_empty[stage], ph, s_abort, p.wait_ns);
+        ok = __all_sync(0xffffffffu, ok);
+        if (!ok) break;
+        if (lane == 0) mbar_arrive_expect_tx(&s_v_full[stage], (uint32_t)(n_box * R * D));
+        __syncwarp();
+        if (lane < n_box)
+          tma_load_2d(smem + C::kOffV + stage * C::kTileBytes + lane * R * D, &tmap_v, 0, grow, &s_v_full[stage]);
+        {
+          // lanes 0-7: scales of the tile's eight blocks of K rows, lanes 8-15: of V rows
+          const int blk = lane & 7;
+          int bg = __shfl_sync(0xffffffffu, grow, (blk * kScaleBlock) / R);
+          bg = bg / kScaleBlock + blk - (blk * kScaleBlock) / R * (R / kScaleBlock);
+          if (lane < 16) {
+            const bool live = blk < n_blk;
+            float* dst = reinterpret_cast<float*>(smem + C::kOffScales) + stage * 16 + lane;
+            cp_async_4(dst, (lane < 8 ? p.k_scales : p.v_scales) + (live ? bg : 0), live);
+          }
+          cp_async_arrive(&s_scale_full[stage]);
+        }
+      }
+      if (!ok) break;
+      if (n_tiles > 0) pages = ahead;
+      cur = nxt;
+    }
+  } else if (warp == 5) {
+    // ================================================================ the MMAs
     if (lane == 0) {
-      s_ml[warp][g][0] = m[g];
-      s_ml[warp][g][1] = l[g];
+      constexpr uint32_t kIdescS = idesc_e4m3(kTile, kN, false), kIdescO = idesc_e4m3(D, kN, true);
+      uint32_t js = 0, jo = 0, n_item = 0;        // logit tiles issued, output tiles issued, items begun
+      int slot = 0, t = 0, n_tiles = 0;           // of the logits
+      uint32_t tail_rows[2] = {kTile, kTile};     // rows of the tiles between the two products
+      bool more = true, ok = true;
+      while (ok) {
+        if (more && js - jo < 2) {
+          if (t == n_tiles) {                     // next item
+            slot = n_item % kFifo;
+            ok = ws_wait(&s_fifo_full[slot], (n_item / kFifo) & 1, s_abort, p.wait_ns);
+            if (!ok) break;
+            const Item it = s_item[slot];
+            if (it.e < 0) {
+              more = false;
+              continue;
+            }
+            ok = ws_wait(&s_q_full[slot], (n_item / kFifo) & 1, s_abort, p.wait_ns);
+            if (!ok) break;
+            ++n_item;
+            t = 0;
+            n_tiles = tiles_of(it.rows);
+            tail_rows[0] = it.rows - (n_tiles - 1) * kTile;
+          }
+          const int stage = js % C::kStages;
+          ok = ws_wait(&s_k_full[stage], (js / C::kStages) & 1, s_abort, p.wait_ns);
+          if (!ok) break;
+          tc_fence_after_sync();
+          const uint32_t a = smem_u32(smem + stage * C::kTileBytes), b = smem_u32(smem + C::kOffQ + slot * C::kQBytes);
+#pragma unroll
+          for (int k = 0; k < D / 32; ++k)
+            umma_e4m3(tmem + (js & 1) * kN, smem_desc<D>(a + 32 * k), smem_desc<D>(b + 32 * k), kIdescS, k > 0);
+          umma_commit(&s_k_empty[stage]);
+          umma_commit(&s_s_full[js & 1]);
+          ++t;
+          if (t == n_tiles) umma_commit(&s_fifo_empty[slot]);
+          // rows of this tile, for its output product (bit 8: parity slot)
+          if ((js & 1) == 0) tail_rows[1] = (tail_rows[1] & 0xffff0000u) | (t == n_tiles ? tail_rows[0] : kTile);
+          else               tail_rows[1] = (tail_rows[1] & 0x0000ffffu) | ((t == n_tiles ? tail_rows[0] : kTile) << 16);
+          ++js;
+        } else if (jo < js) {
+          const int stage = jo % C::kStages;
+          ok = ws_wait(&s_v_full[stage], (jo / C::kStages) & 1, s_abort, p.wait_ns) &&
+               ws_wait(&s_p_full[jo & 1], (jo / 2) & 1, s_abort, p.wait_ns);
+          if (!ok) break;
+          tc_fence_after_sync();
+          const int rows = (jo & 1) ? tail_rows[1] >> 16 : tail_rows[1] & 0xffffu;
+          const int steps = (rows + 31) / 32;
+          const uint32_t a = smem_u32(smem + C::kOffV + stage * C::kTileBytes);
+          const uint32_t b = smem_u32(smem + C::kOffP + (jo & 1) * C::kPBytes);
+          for (int k = 0; k < steps; ++k)
+            umma_e4m3(tmem + 2 * kN + (jo & 1) * kN, smem_desc<D>(a + 32 * D * k), smem_desc<128>(b + 32 * k), kIdescO, k > 0);
+          umma_commit(&s_v_empty[stage]);
+          umma_commit(&s_d_full[jo & 1]);
+          ++jo;
+        } else {
+          break;                                  // no more logits, every output issued
+        }
+      }
+    }
+    __syncwarp();
+  } else if (warp == 6) {
+    // ================================================================ the queries as two codes per element
+    constexpr int kCols = D / 32;
+    for (uint32_t n_item = 0;; ++n_item) {
+      const int slot = n_item % kFifo;
+      const bool ok = ws_wait(&s_fifo_full[slot], (n_item / kFifo) & 1, s_abort, p.wait_ns);
+      if (!__all_sync(0xffffffffu, ok)) break;
+      const Item it = s_item[slot];
+      if (it.e < 0) break;
+      const __nv_bfloat16* q = p.q + ((size_t)it.e * p.n_q_heads + (size_t)it.h * G) * D + lane * kCols;
+      uint32_t w[GP][kCols / 2];
+#pragma unroll
+      for (int g = 0; g < GP; ++g)
+#pragma unroll
+        for (int i = 0; i < kCols / 2; ++i) w[g][i] = g < G ? __ldg(reinterpret_cast<const uint32_t*>(q + (size_t)g * D) + i) : 0u;
+      uint8_t* dst = smem + C::kOffQ + slot * C::kQBytes;
+#pragma unroll
+      for (int g = 0; g < GP; ++g) {
+        if (g >= G) break;
+        uint32_t top = 0;
+#pragma unroll
+        for (int i = 0; i < kCols / 2; ++i) top = __vmaxu2(top, w[g][i] & 0x7fff7fffu);
+        top = __reduce_max_sync(0xffffffffu, max(top & 0xffffu, top >> 16));
+        const bool bad = top >= 0x7f80u;                       // an infinity or NaN in the row: every code a NaN
+        const int ex = min(max((int)(top >> 7), 20), 254);     // exponent field; largest element in [128, 256) after scaling
+        const float inv = __uint_as_float((uint32_t)(261 - ex) << 23);
+        uint32_t c1[kCols / 2], c2[kCols / 2];
+#pragma unroll
+        for (int i = 0; i < kCols / 2; ++i) {
+          const float x = bf16_lo(w[g][i]) * inv, y = bf16_hi(w[g][i]) * inv;
+          c1[i] = e4m3x2_from_f32(x, y);
+          const float2 f = f32_from_e4m3x2(c1[i]);
+          c2[i] = e4m3x2_from_f32((x - f.x) * kPart, (y - f.y) * kPart);
+          if (bad) c1[i] = c2[i] = 0x7f7fu;
+        }
+        const int col = lane * kCols;
+        if constexpr (kCols == 4) {
+          *reinterpret_cast<uint32_t*>(dst + swizzled<D>(g, col)) = c1[0] | (c1[1] << 16);
+          *reinterpret_cast<uint32_t*>(dst + swizzled<D>(GP + g, col)) = c2[0] | (c2[1] << 16);
+        } else {
+          *reinterpret_cast<uint16_t*>(dst + swizzled<D>(g, col)) = (uint16_t)c1[0];
+          *reinterpret_cast<uint16_t*>(dst + swizzled<D>(GP + g, col)) = (uint16_t)c2[0];
+        }
+        if (lane == 0) s_qscale[slot][g] = __uint_as_float((uint32_t)(ex - 7) << 23) * p.scale_log2;
+      }
+      fence_proxy_async_smem();
+      __syncwarp();
+      if (lane == 0) mbar_arrive(&s_q_full[slot]);
+    }
+  } else {
+    // ================================================================ softmax and output
+    const uint32_t lane_base = (uint32_t)warp << 21;            // tensor-memory lanes 32 * warp ..
+    const bool holds_col = D == 128 || lane < 16;               // M = 64 accumulators lie in lanes 0-15 of each quarter
+    const int col = D == 128 ? warp * 32 + lane : warp * 16 + lane;
+    const int blk = tid / kScaleBlock;
+    uint32_t j = 0;                                              // tiles begun
+    for (uint32_t n_item = 0;; ++n_item) {
+      const int slot = n_item % kFifo;
+      bool bad = !ws_wait(&s_fifo_full[slot], (n_item / kFifo) & 1, s_abort, p.wait_ns);
+      if (!bad) bad = *s_abort != 0;
+      if (soft_any(bad)) break;
+      const Item it = s_item[slot];
+      if (it.e < 0) break;
+      // From here to the end of the item every thread takes every barrier, also when a wait has expired.
+      ws_wait(&s_q_full[slot], (n_item / kFifo) & 1, s_abort, p.wait_ns);
+      float qs[GP], m[GP], l[GP], acc[GP], f[GP];
+#pragma unroll
+      for (int g = 0; g < GP; ++g) {
+        qs[g] = g < G ? s_qscale[slot][g] : 0.f;
+        m[g] = -INFINITY;
+        l[g] = acc[g] = f[g] = 0.f;
+      }
+      auto add_output = [&](uint32_t jd) {                       // O of tile jd
+        ws_wait(&s_d_full[jd & 1], (jd / 2) & 1, s_abort, p.wait_ns);
+        tc_fence_after_sync();
+        float d[2 * GP];
+        tmem_ld<2 * GP>(tmem + 2 * kN + (jd & 1) * kN + lane_base, d);
+#pragma unroll
+        for (int g = 0; g < GP; ++g) acc[g] = fmaf(fmaf(d[GP + g], 1.f / kPart, d[g]), f[g], acc[g]);
+      };
+      const int n_tiles = tiles_of(it.rows);
+      for (int t = 0; t < n_tiles; ++t, ++j) {
+        const int stage = j % C::kStages;
+        const int left = it.rows - t * kTile;
+        const bool live = tid < left;
+        ws_wait(&s_scale_full[stage], (j / C::kStages) & 1, s_abort, p.wait_ns);
+        const float* sc = reinterpret_cast<const float*>(smem + C::kOffScales) + stage * 16;
+        const float ks = sc[blk], vs = sc[8 + blk];
+        const float4 va = *reinterpret_cast<const float4*>(sc + 8), vb = *reinterpret_cast<const float4*>(sc + 12);
+        const float vmax = fmaxf(fmaxf(fmaxf(fmaxf(va.x, va.y), fmaxf(va.z, va.w)),
+                                       fmaxf(fmaxf(vb.x, vb.y), fmaxf(vb.z, vb.w))), 0x1p-110f);
+        const float vr = vs * __fdiv_rn(256.f, vmax);
+        ws_wait(&s_s_full[j & 1], (j / 2) & 1, s_abort, p.wait_ns);
+        tc_fence_after_sync();
+        float s[GP], mt[GP];
+        {
+          float r[2 * GP];
+          tmem_ld<2 * GP>(tmem + (j & 1) * kN + lane_base, r);
+#pragma unroll
+          for (int g = 0; g < GP; ++g) {
+            s[g] = fmaf(r[GP + g], 1.f / kPart, r[g]) * (ks * qs[g]);
+            if (!live) s[g] = -INFINITY;
+          }
+        }
+#pragma unroll
+        for (int g = 0; g < GP; ++g) mt[g] = warp_max(s[g]);
+        if (lane == 0) {
+#pragma unroll
+          for (int g = 0; g < GP; ++g) s_max[j & 1][warp][g] = mt[g];
+        }
+        named_bar_sync(kBarSoft, kSoftThreads);
+#pragma unroll
+        for (int g = 0; g < GP; ++g)
+          mt[g] = fmaxf(fmaxf(s_max[j & 1][0][g], s_max[j & 1][1][g]), fmaxf(s_max[j & 1][2][g], s_max[j & 1][3][g]));
+        // weights relative to the tile's maximum; the codes also carry the V scale relative to the tile's largest
+        uint8_t* pb = smem + C::kOffP + (j & 1) * C::kPBytes;
+        float w[GP];
+#pragma unroll
+        for (int g = 0; g < GP; ++g) w[g] = fast_exp2(s[g] - mt[g]);
+#pragma unroll
+        for (int g = 0; g < GP; g += 2) {
+          const float x = w[g] * vr, y = GP > 1 ? w[g + (GP > 1)] * vr : 0.f;
+          const uint32_t c1 = e4m3x2_from_f32(x, y);
+          const float2 b = f32_from_e4m3x2(c1);
+          const uint32_t c2 = e4m3x2_from_f32((x - b.x) * kPart, (y - b.y) * kPart);
+          pb[swizzled<128>(g, tid)] = (uint8_t)c1;
+          pb[swizzled<128>(GP + g, tid)] = (uint8_t)c2;
+          if (GP > 1) {
+            pb[swizzled<128>(g + 1, tid)] = (uint8_t)(c1 >> 8);
+            pb[swizzled<128>(GP + g + 1, tid)] = (uint8_t)(c2 >> 8);
+          }
+        }
+        if (left < kTile) {
+          // rows behind the last one hold whatever the page or the stage held before; the product runs over whole
+          // groups of 32 rows, so clear V there (0 * NaN)
+          ws_wait(&s_v_full[stage], (j / C::kStages) & 1, s_abort, p.wait_ns);
+          uint4* z = reinterpret_cast<uint4*>(smem + C::kOffV + stage * C::kTileBytes);
+          for (int i = left * (D / 16) + tid; i < (left + 31) / 32 * 32 * (D / 16); i += kSoftThreads)
+            z[i] = make_uint4(0u, 0u, 0u, 0u);
+        }
+        fence_proxy_async_smem();
+        tc_fence_before_sync();
+        __syncwarp();
+        if (lane == 0) mbar_arrive(&s_p_full[j & 1]);
+        if (t > 0) add_output(j - 1);
+        // on to the new reference maximum
+#pragma unroll
+        for (int g = 0; g < GP; ++g) {
+          const float mn = fmaxf(m[g], mt[g]);
+          const float al = fast_exp2(m[g] - mn), fw = fast_exp2(mt[g] - mn);
+          l[g] = fmaf(l[g], al, w[g] * fw);
+          acc[g] *= al;
+          f[g] = fw * (vmax * (1.f / 256.f));
+          m[g] = mn;
+        }
+      }
+      add_output(j - 1);
+      // ---- denominators over the 128 rows' threads
+#pragma unroll
+      for (int g = 0; g < GP; ++g) {
+#pragma unroll
+        for (int o = 16; o > 0; o >>= 1) l[g] += __shfl_xor_sync(0xffffffffu, l[g], o);
+        if (lane == 0) s_sum[warp][g] = l[g];
+      }
+      named_bar_sync(kBarSoft, kSoftThreads);
+#pragma unroll
+      for (int g = 0; g < GP; ++g) l[g] = (s_sum[0][g] + s_sum[1][g]) + (s_sum[2][g] + s_sum[3][g]);
+      tc_fence_before_sync();
+      __syncwarp();
+      if (lane == 0) mbar_arrive(&s_fifo_empty[slot]);
+      const size_t row0 = (size_t)it.e * p.n_q_heads + (size_t)it.h * G;
+      if (it.n_pieces == 1) {
+        if (!*s_abort) {
+#pragma unroll
+          for (int g = 0; g < GP; ++g) {
+            if (g < G && holds_col) p.out[(row0 + g) * D + col] = __float2bfloat16(acc[g] / l[g]);
+            if (g < G && tid == g && p.lse != nullptr) p.lse[row0 + g] = (m[g] + log2f(l[g])) * 0.6931471805599453f;
+          }
+        }
+        named_bar_sync(kBarSoft, kSoftThreads);                  // s_sum is free again
+      } else {
+        // ---- one piece of a cache that several CTAs share
+        const int cta = blockIdx.x;
+        const size_t piece = 2 * (size_t)cta + (cta == it.first_cta ? 1 : 0);
+#pragma unroll
+        for (int g = 0; g < GP; ++g) {
+          if (g < G && holds_col) __stcg(&p.part_o[(piece * G + g) * D + col], acc[g]);
+          if (g < G && tid == g) __stcg(reinterpret_cast<float2*>(p.part_ml) + piece * G + g, make_float2(m[g], l[g]));
+        }
+        __threadfence();
+        named_bar_sync(kBarSoft, kSoftThreads);
+        if (tid == 0) s_last = !*s_abort && atomicAdd(&p.tickets[(size_t)it.e * Hkv + it.h], 1) == it.n_pieces - 1;
+        named_bar_sync(kBarSoft, kSoftThreads);
+        if (s_last) {
+          __threadfence();
+          // a warp joins every fourth query head; its lanes share the columns
+          constexpr int kCols = D / 32;
+          for (int g = warp; g < G; g += 4) {
+            auto piece_of = [&](int i) -> size_t { return 2 * (size_t)(it.first_cta + i) + (i == 0 ? 1 : 0); };
+            float mx = -INFINITY;
+            for (int i = lane; i < it.n_pieces; i += 32)
+              mx = fmaxf(mx, __ldcg(reinterpret_cast<const float2*>(p.part_ml) + piece_of(i) * G + g).x);
+#pragma unroll
+            for (int o = 16; o > 0; o >>= 1) mx = fmaxf(mx, __shfl_xor_sync(0xffffffffu, mx, o));
+            float den = 0.f, o4[kCols];
+#pragma unroll
+            for (int c = 0; c < kCols; ++c) o4[c] = 0.f;
+            for (int i0 = 0; i0 < it.n_pieces; i0 += 32) {
+              const int i = i0 + lane;
+              float wgt = 0.f, ds = 0.f;
+              if (i < it.n_pieces) {
+                const float2 ml = __ldcg(reinterpret_cast<const float2*>(p.part_ml) + piece_of(i) * G + g);
+                wgt = fast_exp2(ml.x - mx);
+                ds = wgt * ml.y;
+              }
+#pragma unroll
+              for (int o = 16; o > 0; o >>= 1) ds += __shfl_xor_sync(0xffffffffu, ds, o);
+              den += ds;
+              const int nb = min(32, it.n_pieces - i0);
+              for (int k0 = 0; k0 < nb; k0 += 8) {
+                float v[8][kCols];
+#pragma unroll
+                for (int k = 0; k < 8; ++k)
+#pragma unroll
+                  for (int c = 0; c < kCols; ++c)
+                    v[k][c] = k0 + k < nb ? __ldcg(&p.part_o[(piece_of(i0 + k0 + k) * G + g) * D + c * 32 + lane]) : 0.f;
+#pragma unroll
+                for (int k = 0; k < 8; ++k) {
+                  const float wk = __shfl_sync(0xffffffffu, wgt, k0 + k);
+#pragma unroll
+                  for (int c = 0; c < kCols; ++c) o4[c] = fmaf(wk, v[k][c], o4[c]);
+                }
+              }
+            }
+#pragma unroll
+            for (int c = 0; c < kCols; ++c) p.out[(row0 + g) * D + c * 32 + lane] = __float2bfloat16(o4[c] / den);
+            if (lane == 0 && p.lse != nullptr) p.lse[row0 + g] = (mx + log2f(den)) * 0.6931471805599453f;
+          }
+        }
+        named_bar_sync(kBarSoft, kSoftThreads);                  // s_last and s_sum are free again
+      }
     }
   }
   __syncthreads();
-  for (int i = threadIdx.x; i < p.group * D; i += 32 * kWarps) {
-    const int g = i / D, c = i % D;
-    float mx = -INFINITY;
-    for (int w = 0; w < kWarps; ++w) mx = fmaxf(mx, s_ml[w][g][0]);
-    float den = 0.f, acc = 0.f;
-    for (int w = 0; w < kWarps; ++w) {
-      if (s_ml[w][g][1] == 0.f) continue;                    // this warp saw no row
-      const float f = exp2f(s_ml[w][g][0] - mx);
-      den += f * s_ml[w][g][1];
-      acc += f * s_o[w][g][c];
-    }
-    p.out[(row0 + g) * D + c] = __float2bfloat16(n > 0 ? acc / den : 0.f);
-    if (c == 0 && p.lse != nullptr) p.lse[row0 + g] = n > 0 ? (mx + log2f(den)) * 0.6931471805599453f : -INFINITY;
+  if (*s_abort) {
+    if (tid == 0) record_status(p.hdr, XKV_ERR_TIMEOUT);
+    // let copies already issued land before this CTA's shared memory can be handed on
+    for (int i = 0; i < 1000; ++i) __nanosleep(1000);
   }
+  tc_fence_after_sync();
+  if (warp == 5) tmem_dealloc(tmem, kTmemCols);
+}
+
+bool make_tmap(CUtensorMap* tmap, void* base, int D, uint64_t rows, int box_rows) {
+  tc::EncodeTiledFn enc = tc::tc_encode_fn();
+  if (enc == nullptr) return false;
+  const cuuint64_t dims[2] = {(cuuint64_t)D, (cuuint64_t)rows};
+  const cuuint64_t strides[1] = {(cuuint64_t)D};
+  const cuuint32_t box[2] = {(cuuint32_t)D, (cuuint32_t)box_rows};
+  const cuuint32_t estr[2] = {1u, 1u};
+  return enc(tmap, CU_TENSOR_MAP_DATA_TYPE_UINT8, 2, base, dims, strides, box, estr, CU_TENSOR_MAP_INTERLEAVE_NONE,
+             D == 128 ? CU_TENSOR_MAP_SWIZZLE_128B : CU_TENSOR_MAP_SWIZZLE_64B, CU_TENSOR_MAP_L2_PROMOTION_L2_256B,
+             CU_TENSOR_MAP_FLOAT_OOB_FILL_NONE) == CUDA_SUCCESS;
+}
+
+template <int D, int GP>
+xkv_status launch(const CUtensorMap& tk, const CUtensorMap& tv, const Params& p, int grid, cudaStream_t st) {
+  int dev = 0;
+  if (cudaGetDevice(&dev) != cudaSuccess || dev < 0 || dev >= 64) return XKV_ERR_CUDA;
+  static std::atomic<bool> done[64];   // idempotent set-up: two threads doing it twice is harmless
+  if (!done[dev].load(std::memory_order_acquire)) {
+    if (cudaFuncSetAttribute(decode_e4m3_kernel<D, GP>, cudaFuncAttributeMaxDynamicSharedMemorySize,
+                             Cfg<D>::kSmemBytes) != cudaSuccess)
+      return XKV_ERR_CUDA;
+    done[dev].store(true, std::memory_order_release);
+  }
+  decode_e4m3_kernel<D, GP><<<grid, kThreads, Cfg<D>::kSmemBytes, st>>>(tk, tv, p);
+  count_launch();
+  return check_launch();
 }
 
 }  // namespace
 
 xkv_status decode_attn_e4m3(const xkv_dims* d, const xkv_cache* c, int layer_begin, int n_layers, const void* q,
-                            const void* k_new, const void* v_new, void* out, float* lse, int chunk_rows,
-                            const DecodeScratch& ws, cudaStream_t st) {
-  (void)chunk_rows;
+                            const void* k_new, const void* v_new, void* out, float* lse, const DecodeScratch& ws,
+                            cudaStream_t st) {
   const int n_units = n_layers * d->batch;
+  int box = 16;
+  while (box < kTile && c->page_size % (2 * box) == 0) box *= 2;
+  const uint64_t page_rows = (uint64_t)c->n_pages * d->n_kv_heads * c->page_size;
+  CUtensorMap tk, tv;
+  if (!make_tmap(&tk, c->k_pages, d->head_dim, page_rows, box) || !make_tmap(&tv, c->v_pages, d->head_dim, page_rows, box))
+    return XKV_ERR_CUDA;
   if (k_new != nullptr) {
     const xkv_status s = append_e4m3(d, c, layer_begin, n_units, k_new, v_new, ws.header, st);
     if (s != XKV_OK) return s;
@@ -125,26 +779,42 @@ xkv_status decode_attn_e4m3(const xkv_dims* d, const xkv_cache* c, int layer_beg
   p.q = static_cast<const __nv_bfloat16*>(q);
   p.out = static_cast<__nv_bfloat16*>(out);
   p.lse = lse;
-  p.k_pages = static_cast<const uint8_t*>(c->k_pages);
-  p.v_pages = static_cast<const uint8_t*>(c->v_pages);
   p.k_scales = c->k_scales;
   p.v_scales = c->v_scales;
   p.block_table = c->block_table;
   p.seq_lens = c->seq_lens;
   p.layer_begin = layer_begin;
   p.batch = d->batch;
+  p.n_units = n_units;
   p.n_q_heads = d->n_q_heads;
   p.n_kv_heads = d->n_kv_heads;
   p.group = d->n_q_heads / d->n_kv_heads;
   p.page_size = c->page_size;
   p.max_pages_per_seq = c->max_pages_per_seq;
   p.n_pages = c->n_pages;
+  p.box_rows = box;
+  p.max_ctas = (int32_t)(ws.max_items / 2 > 1 ? (ws.max_items / 2 < (1 << 20) ? ws.max_items / 2 : 1 << 20) : 1);
   p.scale_log2 = (d->scale != 0.f ? d->scale : 1.0f / sqrtf((float)d->head_dim)) * 1.4426950408889634f;
-  const int grid = n_units * d->n_kv_heads;
-  if (d->head_dim == 128) decode_rows_kernel<128><<<grid, 32 * kWarps, 0, st>>>(p);
-  else                    decode_rows_kernel<64><<<grid, 32 * kWarps, 0, st>>>(p);
-  count_launch();
-  return check_launch();
+  p.wait_ns = wait_limit_ns();
+  p.hdr = static_cast<WorkspaceHeader*>(ws.header);
+  p.tickets = ws.tickets;
+  p.part_o = ws.part_o;
+  p.part_ml = ws.part_ml;
+  // no more CTAs than tiles there can be
+  const int64_t most = (int64_t)n_units * d->n_kv_heads * (((int64_t)c->max_pages_per_seq * c->page_size + kTile - 1) / kTile);
+  const int64_t full = (int64_t)kCtasPerSm * sm_count();
+  const int grid = (int)(most < full ? most : full);
+  const int G = p.group;
+  if (d->head_dim == 128) {
+    if (G == 1) return launch<128, 1>(tk, tv, p, grid, st);
+    if (G == 2) return launch<128, 2>(tk, tv, p, grid, st);
+    if (G <= 4) return launch<128, 4>(tk, tv, p, grid, st);
+    return launch<128, 8>(tk, tv, p, grid, st);
+  }
+  if (G == 1) return launch<64, 1>(tk, tv, p, grid, st);
+  if (G == 2) return launch<64, 2>(tk, tv, p, grid, st);
+  if (G <= 4) return launch<64, 4>(tk, tv, p, grid, st);
+  return launch<64, 8>(tk, tv, p, grid, st);
 }
 
 }  // namespace xkv
