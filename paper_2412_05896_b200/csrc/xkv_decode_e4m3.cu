@@ -104,6 +104,13 @@ __device__ __forceinline__ void umma_e4m3(uint32_t tmem_d, uint64_t adesc, uint6
       : "memory");
 }
 
+// One lane of a converged warp.
+__device__ __forceinline__ bool elect_one() {
+  uint32_t r;
+  asm volatile("{\n\t.reg .pred q;\n\telect.sync _|q, 0xffffffff;\n\tselp.u32 %0, 1, 0, q;\n\t}" : "=r"(r));
+  return r != 0;
+}
+
 // Shared-memory matrix descriptor: rows of kRowBytes (128: 128-byte swizzle, 64: 64-byte swizzle), groups of eight rows
 // 8 * kRowBytes apart.  The same for a K-major operand (rows = M or N) and an M-major one (rows = K) whose M extent is
 // the row.
@@ -417,67 +424,71 @@ decode_e4m3_kernel(const __grid_constant__ CUtensorMap tmap_k, const __grid_cons
     }
   } else if (warp == 5) {
     // ================================================================ the MMAs
-    if (lane == 0) {
-      constexpr uint32_t kIdescS = idesc_e4m3(kTile, kN, false), kIdescO = idesc_e4m3(D, kN, true);
-      uint32_t js = 0, jo = 0, n_item = 0;        // logit tiles issued, output tiles issued, items begun
-      int slot = 0, t = 0, n_tiles = 0;           // of the logits
-      uint32_t tail_rows[2] = {kTile, kTile};     // rows of the tiles between the two products
-      bool more = true, ok = true;
-      while (ok) {
-        if (more && js - jo < 2) {
-          if (t == n_tiles) {                     // next item
-            slot = n_item % kFifo;
-            ok = ws_wait(&s_fifo_full[slot], (n_item / kFifo) & 1, s_abort, p.wait_ns);
-            if (!ok) break;
-            const Item it = s_item[slot];
-            if (it.e < 0) {
-              more = false;
-              continue;
-            }
-            ok = ws_wait(&s_q_full[slot], (n_item / kFifo) & 1, s_abort, p.wait_ns);
-            if (!ok) break;
-            ++n_item;
-            t = 0;
-            n_tiles = tiles_of(it.rows);
-            tail_rows[0] = it.rows - (n_tiles - 1) * kTile;
+    // The whole warp walks, one elected lane issues: a branch on elect.sync costs 49 clocks an MMA, one on the lane
+    // index 78 (measured, whatever the shape; the 128 x 16 x 32 product itself takes 42).
+    constexpr uint32_t kIdescS = idesc_e4m3(kTile, kN, false), kIdescO = idesc_e4m3(D, kN, true);
+    uint32_t js = 0, jo = 0, n_item = 0;          // logit tiles issued, output tiles issued, items begun
+    int slot = 0, t = 0, n_tiles = 0, last_rows = 0;   // of the logits
+    int rows0 = kTile, rows1 = kTile;             // rows of the even and the odd tile between the two products
+    bool more = true;
+    while (true) {
+      if (more && js - jo < 2) {
+        if (t == n_tiles) {                       // next item
+          slot = n_item % kFifo;
+          if (!__all_sync(0xffffffffu, ws_wait(&s_fifo_full[slot], (n_item / kFifo) & 1, s_abort, p.wait_ns))) break;
+          const int e = s_item[slot].e, rows = s_item[slot].rows;
+          if (e < 0) {
+            more = false;
+            continue;
           }
-          const int stage = js % C::kStages;
-          ok = ws_wait(&s_k_full[stage], (js / C::kStages) & 1, s_abort, p.wait_ns);
-          if (!ok) break;
-          tc_fence_after_sync();
-          const uint32_t a = smem_u32(smem + stage * C::kTileBytes), b = smem_u32(smem + C::kOffQ + slot * C::kQBytes);
-#pragma unroll
-          for (int k = 0; k < D / 32; ++k)
-            umma_e4m3(tmem + (js & 1) * kN, smem_desc<D>(a + 32 * k), smem_desc<D>(b + 32 * k), kIdescS, k > 0);
-          umma_commit(&s_k_empty[stage]);
-          umma_commit(&s_s_full[js & 1]);
-          ++t;
-          if (t == n_tiles) umma_commit(&s_fifo_empty[slot]);
-          // rows of this tile, for its output product (bit 8: parity slot)
-          if ((js & 1) == 0) tail_rows[1] = (tail_rows[1] & 0xffff0000u) | (t == n_tiles ? tail_rows[0] : kTile);
-          else               tail_rows[1] = (tail_rows[1] & 0x0000ffffu) | ((t == n_tiles ? tail_rows[0] : kTile) << 16);
-          ++js;
-        } else if (jo < js) {
-          const int stage = jo % C::kStages;
-          ok = ws_wait(&s_v_full[stage], (jo / C::kStages) & 1, s_abort, p.wait_ns) &&
-               ws_wait(&s_p_full[jo & 1], (jo / 2) & 1, s_abort, p.wait_ns);
-          if (!ok) break;
-          tc_fence_after_sync();
-          const int rows = (jo & 1) ? tail_rows[1] >> 16 : tail_rows[1] & 0xffffu;
-          const int steps = (rows + 31) / 32;
-          const uint32_t a = smem_u32(smem + C::kOffV + stage * C::kTileBytes);
-          const uint32_t b = smem_u32(smem + C::kOffP + (jo & 1) * C::kPBytes);
-          for (int k = 0; k < steps; ++k)
-            umma_e4m3(tmem + 2 * kN + (jo & 1) * kN, smem_desc<D>(a + 32 * D * k), smem_desc<128>(b + 32 * k), kIdescO, k > 0);
-          umma_commit(&s_v_empty[stage]);
-          umma_commit(&s_d_full[jo & 1]);
-          ++jo;
-        } else {
-          break;                                  // no more logits, every output issued
+          if (!__all_sync(0xffffffffu, ws_wait(&s_q_full[slot], (n_item / kFifo) & 1, s_abort, p.wait_ns))) break;
+          ++n_item;
+          t = 0;
+          n_tiles = tiles_of(rows);
+          last_rows = rows - (n_tiles - 1) * kTile;
         }
+        const int stage = js % C::kStages;
+        if (!__all_sync(0xffffffffu, ws_wait(&s_k_full[stage], (js / C::kStages) & 1, s_abort, p.wait_ns))) break;
+        tc_fence_after_sync();
+        ++t;
+        const bool last = t == n_tiles;
+        if (elect_one()) {
+          const uint64_t a = smem_desc<D>(smem_u32(smem + stage * C::kTileBytes));
+          const uint64_t b = smem_desc<D>(smem_u32(smem + C::kOffQ + slot * C::kQBytes));
+          const uint32_t d = tmem + (js & 1) * kN;
+#pragma unroll
+          for (int k = 0; k < D / 32; ++k) umma_e4m3(d, a + 2 * k, b + 2 * k, kIdescS, k > 0);
+          umma_commit(&s_s_full[js & 1]);
+          umma_commit(&s_k_empty[stage]);
+          if (last) umma_commit(&s_fifo_empty[slot]);
+        }
+        __syncwarp();
+        if (js & 1) rows1 = last ? last_rows : kTile;
+        else        rows0 = last ? last_rows : kTile;
+        ++js;
+      } else if (jo < js) {
+        const int stage = jo % C::kStages;
+        if (!__all_sync(0xffffffffu, ws_wait(&s_v_full[stage], (jo / C::kStages) & 1, s_abort, p.wait_ns) &&
+                                         ws_wait(&s_p_full[jo & 1], (jo / 2) & 1, s_abort, p.wait_ns)))
+          break;
+        tc_fence_after_sync();
+        const int rows = (jo & 1) ? rows1 : rows0;
+        if (elect_one()) {
+          const uint64_t a = smem_desc<D>(smem_u32(smem + C::kOffV + stage * C::kTileBytes));
+          const uint64_t b = smem_desc<128>(smem_u32(smem + C::kOffP + (jo & 1) * C::kPBytes));
+          const uint32_t d = tmem + 2 * kN + (jo & 1) * kN;
+#pragma unroll
+          for (int k = 0; k < kTile / 32; ++k)    // whole groups of 32 rows; those behind the last row stay out
+            if (32 * k < rows) umma_e4m3(d, a + 2 * D * k, b + 2 * k, kIdescO, k > 0);
+          umma_commit(&s_d_full[jo & 1]);
+          umma_commit(&s_v_empty[stage]);
+        }
+        __syncwarp();
+        ++jo;
+      } else {
+        break;                                    // no more logits, every output issued
       }
     }
-    __syncwarp();
   } else if (warp == 6) {
     // ================================================================ the queries as two codes per element
     constexpr int kCols = D / 32;
