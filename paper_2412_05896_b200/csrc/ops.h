@@ -45,7 +45,9 @@ xkv_status decode_attn_static(const xkv_dims* d, const xkv_cache* c, int layer_b
 // Where decode_attn's workspace holds what the decode kernels need.
 struct DecodeScratch {
   void* header;
-  int32_t* tickets;    // [n_layers * batch * n_kv_heads], zero at the start of the call like the rest of the header
+  int32_t* clear;      // n_clear words that start a call at zero: the header's counters (the status word, where it is to
+  int32_t n_clear;     // stay, is left out) and the tickets
+  int32_t* tickets;    // [n_layers * batch * n_kv_heads]
   float* part_o;       // [max_items][G][d]
   float* part_ml;      // [max_items][G][2]
   int64_t max_items;
@@ -53,9 +55,10 @@ struct DecodeScratch {
 xkv_status decode_attn_e4m3(const xkv_dims* d, const xkv_cache* c, int layer_begin, int n_layers, const void* q,
                             const void* k_new, const void* v_new, void* out, float* lse, const DecodeScratch& ws,
                             cudaStream_t st);
-// One new row per (layer, sequence) and KV head stored in a cache of 8-bit floats, lengths advanced.
+// One new row per (layer, sequence) and KV head stored in a cache of 8-bit floats, lengths advanced; n_clear words are
+// cleared on the way.
 xkv_status append_e4m3(const xkv_dims* d, const xkv_cache* c, int layer_begin, int n_units, const void* k_new,
-                       const void* v_new, void* workspace, cudaStream_t st);
+                       const void* v_new, void* workspace, int32_t* clear, int n_clear, cudaStream_t st);
 
 size_t store_workspace_bytes();
 xkv_status store_rows(const xkv_dims* d, const xkv_cache* c, const void* k, const void* v, const int64_t* slots,
@@ -68,5 +71,6 @@ xkv_status plan_append(const xkv_cache* c, int batch, const int32_t* n_new, int 
                        int64_t* slots, int64_t slots_stride, void* workspace, cudaStream_t st);
 
 void set_profile_events(cudaEvent_t start, cudaEvent_t stop);
+void get_profile_events(cudaEvent_t* start, cudaEvent_t* stop);
 
 }  // namespace xkv

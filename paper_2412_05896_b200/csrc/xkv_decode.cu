@@ -1097,6 +1097,11 @@ void set_profile_events(cudaEvent_t start, cudaEvent_t stop) {
   g_ev_stop = stop;
 }
 
+void get_profile_events(cudaEvent_t* start, cudaEvent_t* stop) {
+  *start = g_ev_start;
+  *stop = g_ev_stop;
+}
+
 size_t decode_workspace_bytes(const xkv_dims* d, int n_layers, int max_cache_len, int chunk_rows) {
   DecodeLayout L;
   if (!decode_layout(d, n_layers, max_cache_len, chunk_rows, &L)) return 0;
@@ -1119,8 +1124,8 @@ xkv_status decode_attn(const xkv_dims* d, const xkv_cache* c, int layer_begin, i
   if (c->kv_format == XKV_KV_E4M3) {
     uint8_t* base = static_cast<uint8_t*>(workspace);
     const size_t keep = clear_status ? 0 : sizeof(int32_t);   // see below
-    if (cudaMemsetAsync(base + keep, 0, L.unit_info - keep, st) != cudaSuccess) return XKV_ERR_CUDA;
-    const DecodeScratch scratch = {base, reinterpret_cast<int32_t*>(base + L.tickets),
+    const DecodeScratch scratch = {base, reinterpret_cast<int32_t*>(base + keep), (int32_t)((L.unit_info - keep) / 4),
+                                   reinterpret_cast<int32_t*>(base + L.tickets),
                                    reinterpret_cast<float*>(base + L.part_o), reinterpret_cast<float*>(base + L.part_ml),
                                    L.max_items};
     return decode_attn_e4m3(d, c, layer_begin, Lr, q, k_new, v_new, out, lse, scratch, st);

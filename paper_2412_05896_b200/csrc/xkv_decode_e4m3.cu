@@ -13,15 +13,20 @@
 // range is per tile, every tile's product goes to fresh accumulators and is added in fp32 registers with the tile's
 // own factor; nothing in tensor memory is ever rescaled.
 //
-// Shape of the launch: two CTAs of seven warps per SM, no CTA waits for another one.  All tiles of all (layer, sequence,
-// KV head) caches, in that order, are dealt out evenly: CTA c takes tiles [c T / C, (c + 1) T / C), found by every CTA
-// for itself from the lengths.  A cache cut by a boundary leaves partial results (m, l, O), at most two pieces a CTA, and
-// the CTA that finishes its last piece joins them in the order of the pieces.
-//   warp 4     walks the CTA's tiles: descriptors of the cache pieces ("items"), TMA boxes of K and V, block scales
-//   warp 5     one thread issues the MMAs: logits up to two tiles ahead of the outputs
-//   warp 6     the items' queries as two codes per element
+// Shape of the launch: two CTAs of eight warps per SM, no CTA waits for another one.  All (layer, sequence, KV head) caches
+// lie on one line, a cache as long as its blocks of 16 rows plus a constant for what a cache costs besides its bytes, and the
+// line is cut into equal segments, one per CTA, that every CTA derives for itself from the lengths.  A tile belongs to
+// the segment in which it starts.  A cache cut by a boundary leaves partial results (m, l, O), at most two pieces a CTA, and
+// the CTA that finishes the last piece joins them in the order of the pieces, so the result does not depend on who
+// was when.  (Small segments at the ends of the shares that go to whoever is done first level the finishing times, but
+// what they add in pieces and joins costs more: 74.6 against 70.2 us for 363 MB, 150.8 against 140.2 us for 814 MB.)
+//   warp 6     finds the CTA's pieces of caches ("items") and lays out their queries as two codes per element
+//   warp 4     copies: TMA boxes of K and V, block scales
+//   warp 5     issues the MMAs: logits up to two tiles ahead of the outputs
 //   warps 0-3  one thread per cache row: logits out of tensor memory, the tile's maximum (one exchange among the four
 //              warps), weights back as codes; then, as one thread per output column, O of the tile before
+//   warp 7     counts finished pieces of cut caches and joins those that are complete, one query head at a time; warps that
+//              have run out of tiles help
 #include <cuda.h>
 
 #include <atomic>
@@ -42,17 +47,22 @@ using tc::tmem_dealloc;
 using tc::tmem_relinquish;
 using tc::tmem_wait_ld;
 using tc::umma_commit;
-using tc::ws_wait;
 
 constexpr int kTile = 128;            // cache rows per tile
 constexpr int kN = 16;                // N of both MMAs: two codes x up to eight heads, the rest zero rows
-constexpr int kThreads = 224;
+constexpr int kThreads = 256;
 constexpr int kSoftThreads = 128;
 constexpr int kFifo = 3;              // items between the walk and the last reader
 constexpr int kTmemCols = 64;         // two logit buffers and two output buffers of 16 columns
 constexpr int kCtasPerSm = 2;
 constexpr float kPart = 32.f;         // weight of the second code
 constexpr int kBarSoft = 1;           // named barrier of warps 0-3
+constexpr int kTileBlocks = kTile / kScaleBlock;
+constexpr int kCacheCost = 8;         // what a cache costs besides its bytes, in blocks of 16 rows (4: 70.3 us, 8: 68.8 us, 16:
+                                      // 70.5 us for 2048 caches of 203 to 1101 rows)
+constexpr int kMinSegment = 8;        // shortest segment, in blocks: a tile, so that a cache has a tile in every segment
+                                      // between its first and its last one
+constexpr int kJobs = 32;             // joins a CTA may have open
 
 template <int D>
 struct Cfg {
@@ -78,12 +88,22 @@ struct Params {
   int32_t layer_begin, batch, n_units, n_q_heads, n_kv_heads, group, page_size, max_pages_per_seq, n_pages;
   int32_t box_rows;                   // rows of a TMA box: the largest power of two up to 128 that divides page_size
   int32_t max_ctas;                   // CTAs that the partial results have room for
+  int32_t withhold_cta;               // test hook: this CTA's pieces are never counted (-1: none)
+  int32_t wait_first;                 // the launch before this one appends rows: wait for it before reading a length
   float scale_log2;
   uint64_t wait_ns;
   WorkspaceHeader* hdr;
   int32_t* tickets;                   // [units * n_kv_heads] pieces of a cache that are done
   float* part_o;                      // [2 * CTAs][G][D]
   float* part_ml;                     // [2 * CTAs][G][2]
+};
+
+// [0, n) cut into `parts` runs that differ by at most one.
+struct Cut {
+  int32_t q, r;
+  __device__ __forceinline__ Cut(int n, int parts) : q(n / parts), r(n % parts) {}
+  __device__ __forceinline__ int begin(int i) const { return i * q + min(i, r); }
+  __device__ __forceinline__ int part_of(int x) const { return x < r * (q + 1) ? x / (q + 1) : r + (x - r * (q + 1)) / q; }
 };
 
 struct Item {                         // one CTA's piece of one cache
@@ -182,6 +202,38 @@ __device__ __forceinline__ bool soft_any(bool x) {
       : "memory");
   return r != 0;
 }
+// Bounded wait for the phase with the given parity; gives up when another role has raised the abort flag.  A short rolled
+// loop: the kernel waits in two dozen places, and its roles share the instruction cache.
+__device__ __forceinline__ bool wait_bar(uint64_t* bar, uint32_t parity, volatile int* abort_flag, uint64_t limit_ns) {
+  if (mbar_try_wait(bar, parity)) return true;
+  const uint64_t t0 = global_timer_ns();
+#pragma unroll 1
+  while (!mbar_try_wait(bar, parity)) {
+    if (*abort_flag) return false;
+    if (global_timer_ns() - t0 > limit_ns) {
+      *abort_flag = 1;
+      return false;
+    }
+  }
+  return true;
+}
+__device__ __forceinline__ int add_acq_rel(int32_t* at, int v) {
+  int was;
+  asm volatile("atom.add.acq_rel.gpu.global.s32 %0, [%1], %2;" : "=r"(was) : "l"(at), "r"(v) : "memory");
+  return was;
+}
+// Whether the phase with the given parity is over, without waiting.
+__device__ __forceinline__ bool mbar_test(uint64_t* bar, uint32_t parity) {
+  uint32_t ok;
+  asm volatile(
+      "{\n\t.reg .pred p;\n\t"
+      "mbarrier.test_wait.parity.shared::cta.b64 p, [%1], %2;\n\t"
+      "selp.u32 %0, 1, 0, p;\n\t}"
+      : "=r"(ok)
+      : "r"(smem_u32(bar)), "r"(parity)
+      : "memory");
+  return ok != 0;
+}
 // 4-byte asynchronous copy global -> shared, zero when !valid
 __device__ __forceinline__ void cp_async_4(void* dst, const void* src, bool valid) {
   asm volatile("cp.async.ca.shared.global [%0], [%1], 4, %2;" ::"r"(smem_u32(dst)), "l"(src), "r"(valid ? 4 : 0) : "memory");
@@ -191,29 +243,142 @@ __device__ __forceinline__ void cp_async_arrive(uint64_t* bar) {
   asm volatile("cp.async.mbarrier.arrive.noinc.shared::cta.b64 [%0];" ::"r"(smem_u32(bar)) : "memory");
 }
 
+// Programmatic dependent launch: returns once the launch before this one has completed and its writes are visible.
+__device__ __forceinline__ void grid_dependency_wait() { asm volatile("griddepcontrol.wait;" ::: "memory"); }
+
 __device__ __forceinline__ int unit_rows(const Params& p, int e) {
   const int n = __ldg(&p.seq_lens[(size_t)p.layer_begin * p.batch + e]);
   return min(max(n, 0), p.max_pages_per_seq * p.page_size);
 }
 __device__ __forceinline__ int tiles_of(int rows) { return (rows + kTile - 1) / kTile; }
+// length of a cache on the line
+__device__ __forceinline__ int cost_of(int rows) { return rows > 0 ? (rows + kScaleBlock - 1) / kScaleBlock + kCacheCost : 0; }
+
+// Caches that this CTA has found complete and is to join, one query head at a time.
+struct Joins {
+  int4 job[kJobs];                    // {unit, KV head, first CTA, pieces}
+  int n_jobs, claimed, joined;        // jobs so far, heads claimed and heads joined
+  int all;                            // no more jobs to come
+};
+
+// Joins kHeads query heads from g on (those behind the last one are left out) of a cut cache, kPieces pieces at a time,
+// all loads of a batch in flight together; the lanes share the columns.
+template <int D, int kHeads, int kPieces>
+__device__ __forceinline__ void join_heads(const Params& p, const int4 job, int g) {
+  constexpr int kCols = D / 32;
+  const int lane = threadIdx.x & 31, G = p.group;
+  const float2* ml_at = reinterpret_cast<const float2*>(p.part_ml);
+  const float* o_at = p.part_o + lane;
+  float mx[kHeads], den[kHeads], o[kHeads][kCols];
+#pragma unroll
+  for (int x = 0; x < kHeads; ++x) {
+    mx[x] = -INFINITY;
+    den[x] = 0.f;
+#pragma unroll
+    for (int c = 0; c < kCols; ++c) o[x][c] = 0.f;
+  }
+#pragma unroll 1
+  for (int i0 = 0; i0 < job.w; i0 += kPieces) {
+    const int nb = min(kPieces, job.w - i0);
+    // Row of (piece i of the batch, head g + x).  Rounds past the last piece or head read that one: loads under a
+    // condition would be taken one after the other.
+    auto row_of = [&](int i, int x) -> int {
+      i = i0 + min(i, nb - 1);
+      return (2 * (job.z + i) + (i == 0 ? 1 : 0)) * G + min(g + x, G - 1);
+    };
+    float2 ml[kHeads];
+    float v[kHeads][kPieces][kCols];
+#pragma unroll
+    for (int x = 0; x < kHeads; ++x) ml[x] = __ldcg(ml_at + row_of(lane, x));
+#pragma unroll
+    for (int x = 0; x < kHeads; ++x)
+#pragma unroll
+      for (int k = 0; k < kPieces; ++k) {
+        const float* src = o_at + (size_t)row_of(k, x) * D;
+#pragma unroll
+        for (int c = 0; c < kCols; ++c) v[x][k][c] = __ldcg(src + c * 32);
+      }
+#pragma unroll
+    for (int x = 0; x < kHeads; ++x) {
+      const float mn = fmaxf(mx[x], warp_max(ml[x].x));
+      const float al = fast_exp2(mx[x] - mn), wgt = lane < nb ? fast_exp2(ml[x].x - mn) : 0.f;
+      float ds = wgt * ml[x].y;
+#pragma unroll
+      for (int y = 16; y > 0; y >>= 1) ds += __shfl_xor_sync(0xffffffffu, ds, y);
+      den[x] = fmaf(den[x], al, ds);
+      mx[x] = mn;
+#pragma unroll
+      for (int c = 0; c < kCols; ++c) o[x][c] *= al;
+#pragma unroll
+      for (int k = 0; k < kPieces; ++k) {
+        const float wk = __shfl_sync(0xffffffffu, wgt, k);
+#pragma unroll
+        for (int c = 0; c < kCols; ++c) o[x][c] = k < nb ? fmaf(wk, v[x][k][c], o[x][c]) : o[x][c];
+      }
+    }
+  }
+#pragma unroll
+  for (int x = 0; x < kHeads; ++x) {
+    if (g + x >= G) break;
+    const size_t row = (size_t)job.x * p.n_q_heads + (size_t)job.y * G + g + x;
+#pragma unroll
+    for (int c = 0; c < kCols; ++c) p.out[row * D + c * 32 + lane] = __float2bfloat16(o[x][c] / den[x]);
+    if (lane == 0 && p.lse != nullptr) p.lse[row] = (mx[x] + log2f(den[x])) * 0.6931471805599453f;
+  }
+}
+
+// Takes query heads of open jobs, up to four of one job at a time, until none is left (a whole warp).
+template <int D>
+__device__ __noinline__ void join_open(const Params& p, Joins* joins) {
+  const int lane = threadIdx.x & 31, G = p.group;
+#pragma unroll 1
+  while (true) {
+    int claim = -1, n = 0;
+    if (lane == 0) {
+      int at = *(volatile int*)&joins->claimed;
+      const int open = *(volatile int*)&joins->n_jobs * G;
+      __threadfence_block();                      // n_jobs before the jobs and, behind them, the pieces
+      while (at < open) {
+        // few pieces: four heads in one go; many: one head a warp, so that several warps share the job
+        n = joins->job[at / G % kJobs].w <= 4 ? min(4, G - at % G) : 1;
+        const int was = atomicCAS(&joins->claimed, at, at + n);
+        if (was == at) {
+          claim = at;
+          break;
+        }
+        at = was;
+      }
+    }
+    claim = __shfl_sync(0xffffffffu, claim, 0);
+    if (claim < 0) return;
+    n = __shfl_sync(0xffffffffu, n, 0);
+    const int4 job = joins->job[claim / G % kJobs];
+    if (job.w <= 4) join_heads<D, 4, 4>(p, job, claim % G);
+    else            join_heads<D, 1, 16>(p, job, claim % G);
+    __syncwarp();
+    if (lane == 0) atomicAdd(&joins->joined, n);
+  }
+}
 
 template <int D, int GP>              // GP: query heads per KV head, rounded up to a power of two
 __global__ void __launch_bounds__(kThreads, kCtasPerSm)
-decode_e4m3_kernel(const __grid_constant__ CUtensorMap tmap_k, const __grid_constant__ CUtensorMap tmap_v, const Params p) {
+decode_e4m3_kernel(const __grid_constant__ CUtensorMap tmap_k, const __grid_constant__ CUtensorMap tmap_v,
+                   const __grid_constant__ Params p) {
   using C = Cfg<D>;
   extern __shared__ uint8_t smem_raw[];
   uint8_t* smem = reinterpret_cast<uint8_t*>((reinterpret_cast<uintptr_t>(smem_raw) + 1023) & ~uintptr_t(1023));
   __shared__ uint64_t s_k_full[C::kStages], s_k_empty[C::kStages], s_v_full[C::kStages], s_v_empty[C::kStages],
       s_scale_full[C::kStages], s_s_full[2], s_p_full[2], s_d_full[2], s_fifo_full[kFifo], s_fifo_empty[kFifo],
-      s_q_full[kFifo];
+      s_q_full[kFifo], s_done_full[kFifo];
   __shared__ Item s_item[kFifo];
   __shared__ float s_qscale[kFifo][8];
   __shared__ float s_max[2][4][8];
-  __shared__ float s_sum[4][8];
-  __shared__ long long s_scan[8];
-  __shared__ long long s_first[2];                // tile index of the CTA's first unit, that unit
+  __shared__ float s_sum[2][4][8];
+  __shared__ int s_scan[kThreads / 32];
+  __shared__ int s_before[kThreads];              // line (of one KV head) before each thread's run of units
   __shared__ uint32_t s_tmem;
-  __shared__ int s_abort_store, s_last;
+  __shared__ int s_abort_store;
+  __shared__ Joins s_joins;
   volatile int* s_abort = &s_abort_store;
   const int tid = threadIdx.x, lane = tid & 31, warp = tid >> 5;
   const int Hkv = p.n_kv_heads, G = p.group;
@@ -233,10 +398,12 @@ decode_e4m3_kernel(const __grid_constant__ CUtensorMap tmap_k, const __grid_cons
     }
     for (int i = 0; i < kFifo; ++i) {
       mbar_init(&s_fifo_full[i], 1);
-      mbar_init(&s_fifo_empty[i], 5);             // the logit MMAs of the item, four softmax warps
+      mbar_init(&s_fifo_empty[i], 7);             // copies, logit MMAs, four softmax warps, warp 7
       mbar_init(&s_q_full[i], 1);
+      mbar_init(&s_done_full[i], 4);
     }
     s_abort_store = 0;
+    s_joins.n_jobs = s_joins.claimed = s_joins.joined = s_joins.all = 0;
     fence_mbar_init();
     prefetch_tmap(&tmap_k);
     prefetch_tmap(&tmap_v);
@@ -250,46 +417,36 @@ decode_e4m3_kernel(const __grid_constant__ CUtensorMap tmap_k, const __grid_cons
     reinterpret_cast<uint4*>(smem + C::kOffQ)[i] = make_uint4(0u, 0u, 0u, 0u);
   fence_proxy_async_smem();
 
-  // ---- the CTA's share: tiles before each thread's run of units, then the unit that holds the first tile
+  if (p.wait_first) grid_dependency_wait();
+  // ---- the plan: the line before each thread's run of units
   const int per = (p.n_units + kThreads - 1) / kThreads;
-  long long mine = 0;
+  int mine = 0;
+#pragma unroll 8
   for (int i = 0; i < per; ++i) {
     const int e = tid * per + i;
-    if (e < p.n_units) mine += tiles_of(unit_rows(p, e));
+    if (e < p.n_units) mine += cost_of(unit_rows(p, e));
   }
-  long long incl = mine;
+  int incl = mine;
 #pragma unroll
   for (int o = 1; o < 32; o <<= 1) {
-    const long long x = __shfl_up_sync(0xffffffffu, incl, o);
+    const int x = __shfl_up_sync(0xffffffffu, incl, o);
     if (lane >= o) incl += x;
   }
   if (lane == 31) s_scan[warp] = incl;
   tc_fence_before_sync();
   __syncthreads();
   tc_fence_after_sync();
-  long long T = 0, before = incl - mine;
+  int line = 0, before = incl - mine;
 #pragma unroll
   for (int w = 0; w < kThreads / 32; ++w) {
     if (w < warp) before += s_scan[w];
-    T += s_scan[w];
+    line += s_scan[w];
   }
-  T *= Hkv;
-  const long long n_ctas = min(min((long long)gridDim.x, (long long)p.max_ctas), max(T, 1ll));
-  const long long t_begin = blockIdx.x < n_ctas ? blockIdx.x * T / n_ctas : T;
-  const long long t_end = blockIdx.x < n_ctas ? (blockIdx.x + 1) * T / n_ctas : T;
-  if (t_begin < t_end && before * Hkv <= t_begin && t_begin < (before + mine) * Hkv) {
-    long long at = before * Hkv;
-    for (int i = 0; i < per; ++i) {
-      const int e = tid * per + i;
-      const int nt = e < p.n_units ? tiles_of(unit_rows(p, e)) : 0;
-      if (t_begin < at + (long long)nt * Hkv) {
-        s_first[0] = at;
-        s_first[1] = e;
-        break;
-      }
-      at += (long long)nt * Hkv;
-    }
-  }
+  s_before[tid] = before;
+  line *= Hkv;
+  const int n_ctas = min(min((int)gridDim.x, p.max_ctas), max(line / kMinSegment, 1));
+  const Cut share(line, n_ctas);
+  if (!p.wait_first) grid_dependency_wait();      // the counters below are cleared by the launch before this one
   // rows of empty caches
   for (int e = blockIdx.x; e < p.n_units; e += gridDim.x) {
     if (unit_rows(p, e) != 0) continue;
@@ -303,53 +460,8 @@ decode_e4m3_kernel(const __grid_constant__ CUtensorMap tmap_k, const __grid_cons
   const uint32_t tmem = s_tmem;
 
   if (warp == 4) {
-    // ================================================================ the walk and the copies
+    // ================================================================ the copies
     const int R = p.box_rows, boxes_per_tile = kTile / R;
-    long long at = t_begin;                       // next tile of the CTA
-    int e = 0, h = 0, rows = 0, nt = 0;
-    long long unit_at = 0;                        // tile index of (e, head 0)
-    if (t_begin < t_end) {
-      unit_at = s_first[0];
-      e = (int)s_first[1];
-      rows = unit_rows(p, e);
-      nt = tiles_of(rows);
-      h = (int)((t_begin - unit_at) / nt);
-    }
-    // the CTA that works on tile x
-    auto cta_of = [&](long long x) -> int {
-      long long c = x * n_ctas / T;
-      while ((c + 1) * T / n_ctas <= x) ++c;
-      while (c * T / n_ctas > x) --c;
-      return (int)c;
-    };
-    auto next_item = [&]() -> Item {
-      Item it = {-1, 0, 0, 0, 0, 0};
-      if (at >= t_end) return it;
-      while (h == Hkv || nt == 0) {               // on to the next cache that holds rows
-        unit_at += (long long)nt * Hkv;
-        ++e;
-        h = 0;
-        if (e >= p.n_units) return it;
-        rows = unit_rows(p, e);
-        nt = tiles_of(rows);
-      }
-      const long long g0 = unit_at + (long long)h * nt, g1 = g0 + nt;      // tiles of this (cache, KV head)
-      const long long stop = min(g1, t_end);
-      it.e = e;
-      it.h = h;
-      it.row0 = (int)(at - g0) * kTile;
-      it.rows = min(rows, (int)(stop - g0) * kTile) - it.row0;
-      if (g0 >= t_begin && g1 <= t_end) {
-        it.first_cta = blockIdx.x;
-        it.n_pieces = 1;
-      } else {
-        it.first_cta = cta_of(g0);
-        it.n_pieces = cta_of(g1 - 1) - it.first_cta + 1;
-      }
-      at = stop;
-      ++h;
-      return it;
-    };
     // page of box `lane` of a batch of 32 boxes of an item
     auto load_pages = [&](const Item& it, int box0) -> int {
       const int r = it.row0 + (box0 + lane) * R;
@@ -358,29 +470,28 @@ decode_e4m3_kernel(const __grid_constant__ CUtensorMap tmap_k, const __grid_cons
         page = __ldg(&p.block_table[((size_t)p.layer_begin * p.batch + it.e) * p.max_pages_per_seq + r / p.page_size]);
       return page;
     };
-    Item cur = next_item();
-    int pages = load_pages(cur, 0);
-    uint32_t j = 0, n_item = 0;                   // tiles issued, items published
-    bool ok = true;
-    while (ok) {
+    uint32_t j = 0;                               // tiles issued
+    Item nxt = {-1, 0, 0, 0, 0, 0};
+    int nxt_pages = 0;
+    bool have_next = false, ok = true;
+    for (uint32_t n_item = 0; ok; ++n_item) {
       const int slot = n_item % kFifo;
-      if (n_item >= kFifo) ok = ws_wait(&s_fifo_empty[slot], ((n_item / kFifo) - 1) & 1, s_abort, p.wait_ns);
-      ok = __all_sync(0xffffffffu, ok);
-      if (!ok) break;
-      if (lane == 0) {
-        s_item[slot] = cur;
-        mbar_arrive(&s_fifo_full[slot]);
+      if (!have_next) {
+        ok = __all_sync(0xffffffffu, wait_bar(&s_fifo_full[slot], (n_item / kFifo) & 1, s_abort, p.wait_ns));
+        if (!ok) break;
+        nxt = s_item[slot];
+        nxt_pages = load_pages(nxt, 0);
       }
-      ++n_item;
+      const Item cur = nxt;
       if (cur.e < 0) break;
-      const Item nxt = next_item();
-      int ahead = 0;
+      int pages = nxt_pages, ahead = 0;
+      have_next = false;
       const int n_tiles = tiles_of(cur.rows);
       for (int t = 0; t < n_tiles; ++t, ++j) {
         const int box0 = t * boxes_per_tile;
         if ((box0 & 31) == 0) {                   // a new batch of page ids; the next one is on its way meanwhile
           if (t > 0) pages = ahead;
-          ahead = (box0 + 32) * R < cur.rows ? load_pages(cur, box0 + 32) : load_pages(nxt, 0);
+          ahead = load_pages(cur, box0 + 32);
         }
         const int stage = j % C::kStages;
         const uint32_t ph = ((j / C::kStages) - 1) & 1;
@@ -391,14 +502,14 @@ decode_e4m3_kernel(const __grid_constant__ CUtensorMap tmap_k, const __grid_cons
         int page = __shfl_sync(0xffffffffu, pages, (box0 + lane) & 31);
         page = min(max(page, 0), p.n_pages - 1);
         const int grow = (page * Hkv + cur.h) * p.page_size + row_of_box % p.page_size;
-        if (j >= C::kStages) ok = ws_wait(&s_k_empty[stage], ph, s_abort, p.wait_ns);
+        if (j >= C::kStages) ok = wait_bar(&s_k_empty[stage], ph, s_abort, p.wait_ns);
         ok = __all_sync(0xffffffffu, ok);
         if (!ok) break;
         if (lane == 0) mbar_arrive_expect_tx(&s_k_full[stage], (uint32_t)(n_box * R * D));
         __syncwarp();
         if (lane < n_box)
           tma_load_2d(smem + stage * C::kTileBytes + lane * R * D, &tmap_k, 0, grow, &s_k_full[stage]);
-        if (j >= C::kStages) ok = ws_wait(&s_v_empty[stage], ph, s_abort, p.wait_ns);
+        if (j >= C::kStages) ok = wait_bar(&s_v_empty[stage], ph, s_abort, p.wait_ns);
         ok = __all_sync(0xffffffffu, ok);
         if (!ok) break;
         if (lane == 0) mbar_arrive_expect_tx(&s_v_full[stage], (uint32_t)(n_box * R * D));
@@ -417,10 +528,18 @@ decode_e4m3_kernel(const __grid_constant__ CUtensorMap tmap_k, const __grid_cons
           }
           cp_async_arrive(&s_scale_full[stage]);
         }
+        if (!have_next) {                         // the next item's first page ids, if that item is known already
+          const int ns = (n_item + 1) % kFifo;
+          if (__all_sync(0xffffffffu, mbar_test(&s_fifo_full[ns], ((n_item + 1) / kFifo) & 1))) {
+            nxt = s_item[ns];
+            nxt_pages = load_pages(nxt, 0);
+            have_next = true;
+          }
+        }
       }
       if (!ok) break;
-      if (n_tiles > 0) pages = ahead;
-      cur = nxt;
+      __syncwarp();
+      if (lane == 0) mbar_arrive(&s_fifo_empty[slot]);
     }
   } else if (warp == 5) {
     // ================================================================ the MMAs
@@ -435,20 +554,20 @@ decode_e4m3_kernel(const __grid_constant__ CUtensorMap tmap_k, const __grid_cons
       if (more && js - jo < 2) {
         if (t == n_tiles) {                       // next item
           slot = n_item % kFifo;
-          if (!__all_sync(0xffffffffu, ws_wait(&s_fifo_full[slot], (n_item / kFifo) & 1, s_abort, p.wait_ns))) break;
+          if (!__all_sync(0xffffffffu, wait_bar(&s_fifo_full[slot], (n_item / kFifo) & 1, s_abort, p.wait_ns))) break;
           const int e = s_item[slot].e, rows = s_item[slot].rows;
           if (e < 0) {
             more = false;
             continue;
           }
-          if (!__all_sync(0xffffffffu, ws_wait(&s_q_full[slot], (n_item / kFifo) & 1, s_abort, p.wait_ns))) break;
+          if (!__all_sync(0xffffffffu, wait_bar(&s_q_full[slot], (n_item / kFifo) & 1, s_abort, p.wait_ns))) break;
           ++n_item;
           t = 0;
           n_tiles = tiles_of(rows);
           last_rows = rows - (n_tiles - 1) * kTile;
         }
         const int stage = js % C::kStages;
-        if (!__all_sync(0xffffffffu, ws_wait(&s_k_full[stage], (js / C::kStages) & 1, s_abort, p.wait_ns))) break;
+        if (!__all_sync(0xffffffffu, wait_bar(&s_k_full[stage], (js / C::kStages) & 1, s_abort, p.wait_ns))) break;
         tc_fence_after_sync();
         ++t;
         const bool last = t == n_tiles;
@@ -468,8 +587,8 @@ decode_e4m3_kernel(const __grid_constant__ CUtensorMap tmap_k, const __grid_cons
         ++js;
       } else if (jo < js) {
         const int stage = jo % C::kStages;
-        if (!__all_sync(0xffffffffu, ws_wait(&s_v_full[stage], (jo / C::kStages) & 1, s_abort, p.wait_ns) &&
-                                         ws_wait(&s_p_full[jo & 1], (jo / 2) & 1, s_abort, p.wait_ns)))
+        if (!__all_sync(0xffffffffu, wait_bar(&s_v_full[stage], (jo / C::kStages) & 1, s_abort, p.wait_ns) &&
+                                         wait_bar(&s_p_full[jo & 1], (jo / 2) & 1, s_abort, p.wait_ns)))
           break;
         tc_fence_after_sync();
         const int rows = (jo & 1) ? rows1 : rows0;
@@ -490,13 +609,83 @@ decode_e4m3_kernel(const __grid_constant__ CUtensorMap tmap_k, const __grid_cons
       }
     }
   } else if (warp == 6) {
-    // ================================================================ the queries as two codes per element
+    // ================================================================ the walk, and the queries as two codes per element
+    const bool works = (int)blockIdx.x < n_ctas && line > 0;
+    int at = works ? share.begin(blockIdx.x) : 0;      // next position, the end of the segment
+    const int stop_at = works ? share.begin(blockIdx.x + 1) : 0;
+    int e = -1, h = 0, rows = 0, cost = 0;
+    int unit_at = 0;                              // where (e, head 0) begins
+    // Stands on position x: the run of units that holds it, then the unit (all lanes).
+    auto find_unit = [&](int x) {
+      int n = 0;
+      for (int i = lane; i < kThreads; i += 32) n += (long long)s_before[i] * Hkv <= x ? 1 : 0;
+      const int run = (int)__reduce_add_sync(0xffffffffu, (unsigned)n) - 1;
+      int base = s_before[run];
+      for (int i0 = 0; i0 < per; i0 += 32) {
+        const int u = run * per + i0 + lane;
+        const int ur = i0 + lane < per && u < p.n_units ? unit_rows(p, u) : 0;
+        const int uc = cost_of(ur);
+        int sum = uc;
+#pragma unroll
+        for (int o = 1; o < 32; o <<= 1) {
+          const int y = __shfl_up_sync(0xffffffffu, sum, o);
+          if (lane >= o) sum += y;
+        }
+        const unsigned hit = __ballot_sync(0xffffffffu, (long long)(base + sum) * Hkv > x);
+        if (hit != 0) {
+          const int w = __ffs(hit) - 1;
+          e = run * per + i0 + w;
+          rows = __shfl_sync(0xffffffffu, ur, w);
+          cost = __shfl_sync(0xffffffffu, uc, w);
+          unit_at = (base + __shfl_sync(0xffffffffu, sum - uc, w)) * Hkv;
+          h = (x - unit_at) / cost;
+          return;
+        }
+        base += __shfl_sync(0xffffffffu, sum, 31);
+      }
+    };
+    if (works) find_unit(at);
+    // The next piece: the tiles of (e, h) that start in [at, stop_at).
+    auto next_item = [&]() -> Item {
+      Item it = {-1, 0, 0, 0, 0, 0};
+      while (at < stop_at) {
+        while (h == Hkv || rows == 0) {           // on to the next cache that holds rows
+          unit_at += cost * Hkv;
+          ++e;
+          h = 0;
+          if (e >= p.n_units) return it;
+          rows = unit_rows(p, e);
+          cost = cost_of(rows);
+        }
+        const int g0 = unit_at + h * cost, nt = tiles_of(rows);
+        const int t0 = (at - g0 + kTileBlocks - 1) / kTileBlocks;                       // first tile that starts at or behind `at`
+        const int t1 = min(nt, (min(stop_at, g0 + cost) - g0 + kTileBlocks - 1) / kTileBlocks);   // first one behind the piece
+        const int this_h = h;
+        at = min(stop_at, g0 + cost);
+        if (at == g0 + cost) ++h;
+        if (t0 >= t1) continue;                   // no tile starts here
+        it.e = e;
+        it.h = this_h;
+        it.row0 = t0 * kTile;
+        it.rows = min(rows, t1 * kTile) - it.row0;
+        const bool whole = t0 == 0 && t1 == nt;
+        it.first_cta = whole ? (int)blockIdx.x : share.part_of(g0);
+        it.n_pieces = whole ? 1 : share.part_of(g0 + (nt - 1) * kTileBlocks) - it.first_cta + 1;
+        return it;
+      }
+      return it;
+    };
     constexpr int kCols = D / 32;
     for (uint32_t n_item = 0;; ++n_item) {
       const int slot = n_item % kFifo;
-      const bool ok = ws_wait(&s_fifo_full[slot], (n_item / kFifo) & 1, s_abort, p.wait_ns);
-      if (!__all_sync(0xffffffffu, ok)) break;
-      const Item it = s_item[slot];
+      const Item it = next_item();
+      if (n_item >= kFifo &&
+          !__all_sync(0xffffffffu, wait_bar(&s_fifo_empty[slot], ((n_item / kFifo) - 1) & 1, s_abort, p.wait_ns)))
+        break;
+      if (lane == 0) {
+        s_item[slot] = it;
+        mbar_arrive(&s_fifo_full[slot]);
+      }
       if (it.e < 0) break;
       const __nv_bfloat16* q = p.q + ((size_t)it.e * p.n_q_heads + (size_t)it.h * G) * D + lane * kCols;
       uint32_t w[GP][kCols / 2];
@@ -538,6 +727,38 @@ decode_e4m3_kernel(const __grid_constant__ CUtensorMap tmap_k, const __grid_cons
       __syncwarp();
       if (lane == 0) mbar_arrive(&s_q_full[slot]);
     }
+  } else if (warp == 7) {
+    // ================================================================ finished pieces of cut caches
+    for (uint32_t n_item = 0;; ++n_item) {
+      const int slot = n_item % kFifo;
+      if (!__all_sync(0xffffffffu, wait_bar(&s_fifo_full[slot], (n_item / kFifo) & 1, s_abort, p.wait_ns))) break;
+      const Item it = s_item[slot];
+      if (it.e < 0) break;
+      if (!__all_sync(0xffffffffu, wait_bar(&s_done_full[slot], (n_item / kFifo) & 1, s_abort, p.wait_ns))) break;
+      __syncwarp();
+      if (lane == 0) mbar_arrive(&s_fifo_empty[slot]);
+      if (it.n_pieces == 1) continue;
+      int last = 0;
+      if (lane == 0 && (int)blockIdx.x != p.withhold_cta) {
+        // counted once it is visible; whoever counts the last one sees all
+        last = add_acq_rel(&p.tickets[(size_t)it.e * Hkv + it.h], 1) == it.n_pieces - 1;
+      }
+      if (__shfl_sync(0xffffffffu, last, 0)) {
+        const int n = *(volatile int*)&s_joins.n_jobs;
+        if (n > 0 && n % kJobs == 0) {            // the job table comes round: let it run empty first
+          join_open<D>(p, &s_joins);
+          while (*(volatile int*)&s_joins.joined < n * G) __nanosleep(100);
+        }
+        if (lane == 0) {
+          s_joins.job[n % kJobs] = make_int4(it.e, it.h, it.first_cta, it.n_pieces);
+          __threadfence_block();
+          *(volatile int*)&s_joins.n_jobs = n + 1;
+        }
+        __syncwarp();
+        join_open<D>(p, &s_joins);
+      }
+    }
+    if (lane == 0) *(volatile int*)&s_joins.all = 1;
   } else {
     // ================================================================ softmax and output
     const uint32_t lane_base = (uint32_t)warp << 21;            // tensor-memory lanes 32 * warp ..
@@ -547,13 +768,13 @@ decode_e4m3_kernel(const __grid_constant__ CUtensorMap tmap_k, const __grid_cons
     uint32_t j = 0;                                              // tiles begun
     for (uint32_t n_item = 0;; ++n_item) {
       const int slot = n_item % kFifo;
-      bool bad = !ws_wait(&s_fifo_full[slot], (n_item / kFifo) & 1, s_abort, p.wait_ns);
+      bool bad = !wait_bar(&s_fifo_full[slot], (n_item / kFifo) & 1, s_abort, p.wait_ns);
       if (!bad) bad = *s_abort != 0;
       if (soft_any(bad)) break;
       const Item it = s_item[slot];
       if (it.e < 0) break;
       // From here to the end of the item every thread takes every barrier, also when a wait has expired.
-      ws_wait(&s_q_full[slot], (n_item / kFifo) & 1, s_abort, p.wait_ns);
+      wait_bar(&s_q_full[slot], (n_item / kFifo) & 1, s_abort, p.wait_ns);
       float qs[GP], m[GP], l[GP], acc[GP], f[GP];
 #pragma unroll
       for (int g = 0; g < GP; ++g) {
@@ -562,7 +783,7 @@ decode_e4m3_kernel(const __grid_constant__ CUtensorMap tmap_k, const __grid_cons
         l[g] = acc[g] = f[g] = 0.f;
       }
       auto add_output = [&](uint32_t jd) {                       // O of tile jd
-        ws_wait(&s_d_full[jd & 1], (jd / 2) & 1, s_abort, p.wait_ns);
+        wait_bar(&s_d_full[jd & 1], (jd / 2) & 1, s_abort, p.wait_ns);
         tc_fence_after_sync();
         float d[2 * GP];
         tmem_ld<2 * GP>(tmem + 2 * kN + (jd & 1) * kN + lane_base, d);
@@ -574,14 +795,14 @@ decode_e4m3_kernel(const __grid_constant__ CUtensorMap tmap_k, const __grid_cons
         const int stage = j % C::kStages;
         const int left = it.rows - t * kTile;
         const bool live = tid < left;
-        ws_wait(&s_scale_full[stage], (j / C::kStages) & 1, s_abort, p.wait_ns);
+        wait_bar(&s_scale_full[stage], (j / C::kStages) & 1, s_abort, p.wait_ns);
         const float* sc = reinterpret_cast<const float*>(smem + C::kOffScales) + stage * 16;
         const float ks = sc[blk], vs = sc[8 + blk];
         const float4 va = *reinterpret_cast<const float4*>(sc + 8), vb = *reinterpret_cast<const float4*>(sc + 12);
         const float vmax = fmaxf(fmaxf(fmaxf(fmaxf(va.x, va.y), fmaxf(va.z, va.w)),
                                        fmaxf(fmaxf(vb.x, vb.y), fmaxf(vb.z, vb.w))), 0x1p-110f);
         const float vr = vs * __fdiv_rn(256.f, vmax);
-        ws_wait(&s_s_full[j & 1], (j / 2) & 1, s_abort, p.wait_ns);
+        wait_bar(&s_s_full[j & 1], (j / 2) & 1, s_abort, p.wait_ns);
         tc_fence_after_sync();
         float s[GP], mt[GP];
         {
@@ -624,7 +845,7 @@ decode_e4m3_kernel(const __grid_constant__ CUtensorMap tmap_k, const __grid_cons
         if (left < kTile) {
           // rows behind the last one hold whatever the page or the stage held before; the product runs over whole
           // groups of 32 rows, so clear V there (0 * NaN)
-          ws_wait(&s_v_full[stage], (j / C::kStages) & 1, s_abort, p.wait_ns);
+          wait_bar(&s_v_full[stage], (j / C::kStages) & 1, s_abort, p.wait_ns);
           uint4* z = reinterpret_cast<uint4*>(smem + C::kOffV + stage * C::kTileBytes);
           for (int i = left * (D / 16) + tid; i < (left + 31) / 32 * 32 * (D / 16); i += kSoftThreads)
             z[i] = make_uint4(0u, 0u, 0u, 0u);
@@ -651,11 +872,11 @@ decode_e4m3_kernel(const __grid_constant__ CUtensorMap tmap_k, const __grid_cons
       for (int g = 0; g < GP; ++g) {
 #pragma unroll
         for (int o = 16; o > 0; o >>= 1) l[g] += __shfl_xor_sync(0xffffffffu, l[g], o);
-        if (lane == 0) s_sum[warp][g] = l[g];
+        if (lane == 0) s_sum[n_item & 1][warp][g] = l[g];
       }
       named_bar_sync(kBarSoft, kSoftThreads);
 #pragma unroll
-      for (int g = 0; g < GP; ++g) l[g] = (s_sum[0][g] + s_sum[1][g]) + (s_sum[2][g] + s_sum[3][g]);
+      for (int g = 0; g < GP; ++g) l[g] = (s_sum[n_item & 1][0][g] + s_sum[n_item & 1][1][g]) + (s_sum[n_item & 1][2][g] + s_sum[n_item & 1][3][g]);
       tc_fence_before_sync();
       __syncwarp();
       if (lane == 0) mbar_arrive(&s_fifo_empty[slot]);
@@ -668,69 +889,24 @@ decode_e4m3_kernel(const __grid_constant__ CUtensorMap tmap_k, const __grid_cons
             if (g < G && tid == g && p.lse != nullptr) p.lse[row0 + g] = (m[g] + log2f(l[g])) * 0.6931471805599453f;
           }
         }
-        named_bar_sync(kBarSoft, kSoftThreads);                  // s_sum is free again
-      } else {
-        // ---- one piece of a cache that several CTAs share
-        const int cta = blockIdx.x;
-        const size_t piece = 2 * (size_t)cta + (cta == it.first_cta ? 1 : 0);
+      } else {                                                    // a piece; warp 7 counts it
+        const size_t piece = 2 * (size_t)blockIdx.x + ((int)blockIdx.x == it.first_cta ? 1 : 0);
 #pragma unroll
         for (int g = 0; g < GP; ++g) {
           if (g < G && holds_col) __stcg(&p.part_o[(piece * G + g) * D + col], acc[g]);
           if (g < G && tid == g) __stcg(reinterpret_cast<float2*>(p.part_ml) + piece * G + g, make_float2(m[g], l[g]));
         }
-        __threadfence();
-        named_bar_sync(kBarSoft, kSoftThreads);
-        if (tid == 0) s_last = !*s_abort && atomicAdd(&p.tickets[(size_t)it.e * Hkv + it.h], 1) == it.n_pieces - 1;
-        named_bar_sync(kBarSoft, kSoftThreads);
-        if (s_last) {
-          __threadfence();
-          // a warp joins every fourth query head; its lanes share the columns
-          constexpr int kCols = D / 32;
-          for (int g = warp; g < G; g += 4) {
-            auto piece_of = [&](int i) -> size_t { return 2 * (size_t)(it.first_cta + i) + (i == 0 ? 1 : 0); };
-            float mx = -INFINITY;
-            for (int i = lane; i < it.n_pieces; i += 32)
-              mx = fmaxf(mx, __ldcg(reinterpret_cast<const float2*>(p.part_ml) + piece_of(i) * G + g).x);
-#pragma unroll
-            for (int o = 16; o > 0; o >>= 1) mx = fmaxf(mx, __shfl_xor_sync(0xffffffffu, mx, o));
-            float den = 0.f, o4[kCols];
-#pragma unroll
-            for (int c = 0; c < kCols; ++c) o4[c] = 0.f;
-            for (int i0 = 0; i0 < it.n_pieces; i0 += 32) {
-              const int i = i0 + lane;
-              float wgt = 0.f, ds = 0.f;
-              if (i < it.n_pieces) {
-                const float2 ml = __ldcg(reinterpret_cast<const float2*>(p.part_ml) + piece_of(i) * G + g);
-                wgt = fast_exp2(ml.x - mx);
-                ds = wgt * ml.y;
-              }
-#pragma unroll
-              for (int o = 16; o > 0; o >>= 1) ds += __shfl_xor_sync(0xffffffffu, ds, o);
-              den += ds;
-              const int nb = min(32, it.n_pieces - i0);
-              for (int k0 = 0; k0 < nb; k0 += 8) {
-                float v[8][kCols];
-#pragma unroll
-                for (int k = 0; k < 8; ++k)
-#pragma unroll
-                  for (int c = 0; c < kCols; ++c)
-                    v[k][c] = k0 + k < nb ? __ldcg(&p.part_o[(piece_of(i0 + k0 + k) * G + g) * D + c * 32 + lane]) : 0.f;
-#pragma unroll
-                for (int k = 0; k < 8; ++k) {
-                  const float wk = __shfl_sync(0xffffffffu, wgt, k0 + k);
-#pragma unroll
-                  for (int c = 0; c < kCols; ++c) o4[c] = fmaf(wk, v[k][c], o4[c]);
-                }
-              }
-            }
-#pragma unroll
-            for (int c = 0; c < kCols; ++c) p.out[(row0 + g) * D + c * 32 + lane] = __float2bfloat16(o4[c] / den);
-            if (lane == 0 && p.lse != nullptr) p.lse[row0 + g] = (mx + log2f(den)) * 0.6931471805599453f;
-          }
-        }
-        named_bar_sync(kBarSoft, kSoftThreads);                  // s_last and s_sum are free again
       }
+      __syncwarp();
+      if (lane == 0) mbar_arrive(&s_done_full[slot]);
     }
+  }
+  // ---- out of tiles: help with the joins until warp 7 has counted its last piece
+  while (warp != 7) {
+    const bool over = __any_sync(0xffffffffu, *(volatile int*)&s_joins.all != 0);   // set on every way out of warp 7's loop
+    join_open<D>(p, &s_joins);
+    if (over) break;
+    __nanosleep(100);
   }
   __syncthreads();
   if (*s_abort) {
@@ -765,9 +941,35 @@ xkv_status launch(const CUtensorMap& tk, const CUtensorMap& tv, const Params& p,
       return XKV_ERR_CUDA;
     done[dev].store(true, std::memory_order_release);
   }
-  decode_e4m3_kernel<D, GP><<<grid, kThreads, Cfg<D>::kSmemBytes, st>>>(tk, tv, p);
+  cudaEvent_t start, stop;
+  get_profile_events(&start, &stop);
+  const bool timed = start != nullptr && stop != nullptr;
+  if (timed) cudaEventRecord(start, st);
+  cudaLaunchConfig_t cfg = {};
+  cfg.gridDim = dim3((unsigned)grid);
+  cfg.blockDim = dim3(kThreads);
+  cfg.dynamicSmemBytes = Cfg<D>::kSmemBytes;
+  cfg.stream = st;
+  // its CTAs may start while the launch before (counters cleared, rows appended) is still running
+  cudaLaunchAttribute attr;
+  attr.id = cudaLaunchAttributeProgrammaticStreamSerialization;
+  attr.val.programmaticStreamSerializationAllowed = 1;
+  cfg.attrs = &attr;
+  cfg.numAttrs = timed ? 0 : 1;
+  const cudaError_t err = cudaLaunchKernelEx(&cfg, decode_e4m3_kernel<D, GP>, tk, tv, p);
+  if (timed) cudaEventRecord(stop, st);
   count_launch();
+  if (err != cudaSuccess) {
+    (void)cudaGetLastError();
+    return XKV_ERR_CUDA;
+  }
   return check_launch();
+}
+
+// Clears the call's counters and tickets.
+__global__ void clear_kernel(int32_t* words, int n) {
+  asm volatile("griddepcontrol.launch_dependents;");
+  for (int i = blockIdx.x * blockDim.x + threadIdx.x; i < n; i += gridDim.x * blockDim.x) words[i] = 0;
 }
 
 }  // namespace
@@ -782,10 +984,19 @@ xkv_status decode_attn_e4m3(const xkv_dims* d, const xkv_cache* c, int layer_beg
   CUtensorMap tk, tv;
   if (!make_tmap(&tk, c->k_pages, d->head_dim, page_rows, box) || !make_tmap(&tv, c->v_pages, d->head_dim, page_rows, box))
     return XKV_ERR_CUDA;
+  const int64_t max_rows = (int64_t)c->max_pages_per_seq * c->page_size;
+  const int64_t caches = (int64_t)n_units * d->n_kv_heads, most = caches * ((max_rows + kTile - 1) / kTile);
+  if (caches * (max_rows / kScaleBlock + kCacheCost) >= (1ll << 31)) return XKV_ERR_UNSUPPORTED;
+  xkv_status s;
   if (k_new != nullptr) {
-    const xkv_status s = append_e4m3(d, c, layer_begin, n_units, k_new, v_new, ws.header, st);
-    if (s != XKV_OK) return s;
+    s = append_e4m3(d, c, layer_begin, n_units, k_new, v_new, ws.header, ws.clear, ws.n_clear, st);
+  } else {
+    const int blocks = (ws.n_clear + 1023) / 1024;
+    clear_kernel<<<blocks < 64 ? blocks : 64, 256, 0, st>>>(ws.clear, ws.n_clear);
+    count_launch();
+    s = check_launch();
   }
+  if (s != XKV_OK) return s;
   Params p;
   p.q = static_cast<const __nv_bfloat16*>(q);
   p.out = static_cast<__nv_bfloat16*>(out);
@@ -804,15 +1015,17 @@ xkv_status decode_attn_e4m3(const xkv_dims* d, const xkv_cache* c, int layer_beg
   p.max_pages_per_seq = c->max_pages_per_seq;
   p.n_pages = c->n_pages;
   p.box_rows = box;
-  p.max_ctas = (int32_t)(ws.max_items / 2 > 1 ? (ws.max_items / 2 < (1 << 20) ? ws.max_items / 2 : 1 << 20) : 1);
+  const int64_t room = ws.max_items / 2;
+  p.max_ctas = (int32_t)(room < 1 ? 1 : (room < (1 << 20) ? room : 1 << 20));
+  p.wait_first = k_new != nullptr ? 1 : 0;
   p.scale_log2 = (d->scale != 0.f ? d->scale : 1.0f / sqrtf((float)d->head_dim)) * 1.4426950408889634f;
+  p.withhold_cta = debug_withhold_item();
   p.wait_ns = wait_limit_ns();
   p.hdr = static_cast<WorkspaceHeader*>(ws.header);
   p.tickets = ws.tickets;
   p.part_o = ws.part_o;
   p.part_ml = ws.part_ml;
   // no more CTAs than tiles there can be
-  const int64_t most = (int64_t)n_units * d->n_kv_heads * (((int64_t)c->max_pages_per_seq * c->page_size + kTile - 1) / kTile);
   const int64_t full = (int64_t)kCtasPerSm * sm_count();
   const int grid = (int)(most < full ? most : full);
   const int G = p.group;

@@ -327,10 +327,14 @@ struct AppendParams {
   int32_t* seq_lens;
   int32_t layer_begin, batch, n_kv_heads, page_size, max_pages_per_seq, n_pages;
   WorkspaceHeader* hdr;
+  int32_t* clear;              // words that the attention launch behind this one wants at zero
+  int32_t n_clear;
 };
 
 template <int D>
 __global__ void __launch_bounds__(kStoreThreads) append_block_kernel(const AppendParams p) {
+  asm volatile("griddepcontrol.launch_dependents;");          // that launch waits for this one before it reads a length
+  for (int i = blockIdx.x * kStoreThreads + threadIdx.x; i < p.n_clear; i += gridDim.x * kStoreThreads) p.clear[i] = 0;
   const int e = blockIdx.x;
   const size_t le = (size_t)p.layer_begin * p.batch + e;
   const int n = p.seq_lens[le];
@@ -441,8 +445,10 @@ xkv_status store_rows(const xkv_dims* d, const xkv_cache* c, const void* k, cons
 }
 
 xkv_status append_e4m3(const xkv_dims* d, const xkv_cache* c, int layer_begin, int n_units, const void* k_new,
-                       const void* v_new, void* workspace, cudaStream_t st) {
+                       const void* v_new, void* workspace, int32_t* clear, int n_clear, cudaStream_t st) {
   AppendParams p;
+  p.clear = clear;
+  p.n_clear = n_clear;
   p.k_new = static_cast<const __nv_bfloat16*>(k_new);
   p.v_new = static_cast<const __nv_bfloat16*>(v_new);
   p.k_pages = static_cast<uint8_t*>(c->k_pages);
