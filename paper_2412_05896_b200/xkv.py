@@ -115,25 +115,34 @@ def lib() -> ctypes.CDLL:
 
 
 def _ptr(x):
-    if x is None:
-        return None
-    if isinstance(x, int):
+    try:
+        return x.data_ptr()   # torch tensor
+    except AttributeError:
+        pass
+    if x is None or isinstance(x, int):
         return x
-    if isinstance(x, np.ndarray):
-        return x.ctypes.data
-    return x.data_ptr()       # torch tensor
+    return x.ctypes.data      # numpy array
 
 
 def _nbytes(x) -> int:
-    if isinstance(x, np.ndarray):
-        return x.nbytes
-    return x.numel() * x.element_size()
+    return x.nbytes           # torch tensor or numpy array
+
+
+_current_raw_stream = None    # torch's own short way to the current stream's handle, where this torch has it
 
 
 def _stream(stream):
     if stream is None:
-        import torch
-        return torch.cuda.current_stream().cuda_stream
+        global _current_raw_stream
+        if _current_raw_stream is None:
+            import torch
+            get, dev = (getattr(torch._C, n, None) for n in ("_cuda_getCurrentRawStream", "_cuda_getDevice"))
+            if get is not None and dev is not None and torch.cuda.is_available():
+                torch.cuda.current_stream()                  # initialises CUDA the ordinary way
+                _current_raw_stream = lambda: get(dev())     # noqa: E731
+            else:
+                _current_raw_stream = lambda: torch.cuda.current_stream().cuda_stream     # noqa: E731
+        return _current_raw_stream()
     if isinstance(stream, int):
         return stream
     return stream.cuda_stream
