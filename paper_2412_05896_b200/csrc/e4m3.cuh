@@ -39,14 +39,21 @@ __device__ __forceinline__ float2 f32_from_e4m3x2(uint32_t w) {
       : "r"(h));
   return f;
 }
-// Sixteen bf16 (two 16-byte pieces) times inv_scale -> sixteen codes.
+// Two bf16 times a power of two (exact, or below every code's reach), in one instruction.
+__device__ __forceinline__ uint32_t bf16x2_scale(uint32_t v, __nv_bfloat162 f) {
+  const __nv_bfloat162 r = __hmul2(*reinterpret_cast<const __nv_bfloat162*>(&v), f);
+  return *reinterpret_cast<const uint32_t*>(&r);
+}
+// Sixteen bf16 (two 16-byte pieces) times inv, a power of two, -> sixteen codes.
 __device__ __forceinline__ uint4 e4m3x16_from_bf16(const uint4& a, const uint4& b, float inv) {
   const uint32_t w[8] = {a.x, a.y, a.z, a.w, b.x, b.y, b.z, b.w};
+  const __nv_bfloat162 f = __float2bfloat162_rn(inv);
   uint32_t r[4];
 #pragma unroll
-  for (int i = 0; i < 4; ++i)
-    r[i] = e4m3x2_from_f32(bf16_lo(w[2 * i]) * inv, bf16_hi(w[2 * i]) * inv) |
-           (e4m3x2_from_f32(bf16_lo(w[2 * i + 1]) * inv, bf16_hi(w[2 * i + 1]) * inv) << 16);
+  for (int i = 0; i < 4; ++i) {
+    const uint32_t x = bf16x2_scale(w[2 * i], f), y = bf16x2_scale(w[2 * i + 1], f);
+    r[i] = __byte_perm(e4m3x2_from_f32(bf16_lo(x), bf16_hi(x)), e4m3x2_from_f32(bf16_lo(y), bf16_hi(y)), 0x5410);
+  }
   return make_uint4(r[0], r[1], r[2], r[3]);
 }
 // Sixteen codes times a power of two <= 1, rounded back to codes.
@@ -73,7 +80,6 @@ __device__ __forceinline__ void e4m3_store_block(uint8_t* codes, float* scale, i
   const int lane = threadIdx.x & 31;
   const int lr = lane / kLanesPerRow, lc = lane % kLanesPerRow;
   uint4 x[kPasses][2];
-  uint32_t top = 0;
 #pragma unroll
   for (int p = 0; p < kPasses; ++p) {
     const int i = p * kRowsPerPass + lr - n_old;
@@ -84,17 +90,21 @@ __device__ __forceinline__ void e4m3_store_block(uint8_t* codes, float* scale, i
       x[p][1] = __ldg(src + 1);
     }
   }
+  auto largest = [&](auto magnitude) -> uint32_t {           // over the block's new rows, as bf16 bits
+    uint32_t m = 0;
 #pragma unroll
-  for (int p = 0; p < kPasses; ++p)
+    for (int p = 0; p < kPasses; ++p)
 #pragma unroll
-    for (int h = 0; h < 2; ++h) {
-      top = __vmaxu2(top, finite_abs_bf16x2(x[p][h].x));
-      top = __vmaxu2(top, finite_abs_bf16x2(x[p][h].y));
-      top = __vmaxu2(top, finite_abs_bf16x2(x[p][h].z));
-      top = __vmaxu2(top, finite_abs_bf16x2(x[p][h].w));
-    }
-  top = max(top & 0xffffu, top >> 16);
-  top = __reduce_max_sync(0xffffffffu, top);
+      for (int h = 0; h < 2; ++h) {
+        m = __vmaxu2(m, magnitude(x[p][h].x));
+        m = __vmaxu2(m, magnitude(x[p][h].y));
+        m = __vmaxu2(m, magnitude(x[p][h].z));
+        m = __vmaxu2(m, magnitude(x[p][h].w));
+      }
+    return __reduce_max_sync(0xffffffffu, max(m & 0xffffu, m >> 16));
+  };
+  uint32_t top = largest([](uint32_t v) { return v & 0x7fff7fffu; });
+  if (top >= 0x7f80u) top = largest([](uint32_t v) { return finite_abs_bf16x2(v); });   // infinities or NaN: leave them out
   float s = e4m3_block_scale(__uint_as_float(top << 16));
   if (n_old > 0) {
     const float was = *scale;

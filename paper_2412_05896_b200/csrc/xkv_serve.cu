@@ -424,7 +424,7 @@ struct StoreParams {
 // longest stretch of tokens whose slots follow each other inside one block; rows of the block before the run are there
 // already, rows behind it are not in use.
 template <int D>
-__global__ void __launch_bounds__(kStoreThreads) store_block_kernel(const StoreParams p) {
+__global__ void __launch_bounds__(kStoreThreads, 4) store_block_kernel(const StoreParams p) {
   const int lane = threadIdx.x & 31;
   const int64_t w = (int64_t)blockIdx.x * (kStoreThreads / 32) + (threadIdx.x >> 5);
   const int n_jobs = 2 * p.n_kv_heads;                        // (head, K or V) of a token
