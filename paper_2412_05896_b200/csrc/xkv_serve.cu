@@ -21,9 +21,9 @@ namespace {
 // Plan of a step
 // ---------------------------------------------------------------------------------------------
 constexpr int kPlanThreads = 256;
-constexpr int kSlotRun = 256;                 // consecutive tokens of a warp
 constexpr int kSmallThreads = 1024;           // one CTA plans up to kSmallUnits sequences of all layers
 constexpr int kSmallUnits = 4096;
+constexpr int kSlotRun = 64;                  // ... and hands its tokens to its warps in runs of so many
 constexpr int64_t kSmallTokens = 32768;
 constexpr int kPlanMaxBatch = 16384;          // sequences of a layer: two 4-byte table entries each in shared memory
 
@@ -42,13 +42,10 @@ struct PlanParams {
   int32_t n_layers, batch, page_size, max_pages_per_seq, n_pages;
   WorkspaceHeader* hdr;
   int32_t* new_lens;            // [n_layers][batch] in the workspace, until the last CTA copies them out
-  // row -> page: page_size is 16 d with d <= 16, and n / d = (n * ceil(2^32 / d)) >> 32 for n < 2^26 (exact, since
-  // n * (d - 1) < 2^32)
-  uint32_t page_mul;            // ceil(2^32 / d), 0 for d = 1
-  __device__ __forceinline__ int page_of(int row) const {
-    const uint32_t n = (uint32_t)row >> 4;
-    return (int)(page_mul != 0 ? __umulhi(n, page_mul) : n);
-  }
+  // row -> page: page_size is 8 D with D even, 2 <= D <= 32, and n / D = (n * ceil(2^32 / D)) >> 32 for n <= 2^27 + 32
+  // (exact: n times what the ceiling adds, at most 29 where D is no power of two and else nothing, stays below 2^32)
+  uint32_t page_mul;            // ceil(2^32 / D)
+  __device__ __forceinline__ int page_of(int row) const { return (int)__umulhi((uint32_t)row >> 3, page_mul); }
 };
 
 struct Ask {
@@ -57,9 +54,10 @@ struct Ask {
   bool bad;                     // a negative count was found
 };
 
-__device__ __forceinline__ Ask plan_ask(const PlanParams& p, int l, int b) {
+// e = l * batch + b
+__device__ __forceinline__ Ask plan_ask(const PlanParams& p, int l, int e, int b) {
   Ask a;
-  const int len = p.lens_before != nullptr ? __ldg(&p.lens_before[(size_t)l * p.batch + b]) : 0;
+  const int len = p.lens_before != nullptr ? __ldg(&p.lens_before[e]) : 0;
   const int add = __ldg(&p.n_new[l * p.n_new_stride + b]);
   a.bad = len < 0 || add < 0;
   a.len = max(len, 0);
@@ -84,67 +82,103 @@ __device__ __forceinline__ int free_page(const PlanParams& p, int at) {
   return p.free_pages != nullptr ? __ldg(&p.free_pages[at]) : at;
 }
 
-// kSlotRun consecutive new tokens of a layer, from t0 on (a whole warp): their slots, and the table entries of the pages
-// that begin with one of them (every new page begins with a new token).  tok(b): tokens of the layer before sequence b
-// (b <= batch), start(b): where its new pages begin in the free list (-1: it cannot grow), len(b): its rows before the
-// step.  total: tokens of the layer; the first n_slots of them have a place in `out`.
-template <class Tok, class Start, class Len>
-__device__ __forceinline__ void write_run(const PlanParams& p, int32_t* table, int64_t* out, int t0, int total, int n_slots,
-                                          Tok tok, Start start, Len len) {
+constexpr int kRounds = 8;                    // tokens a lane takes at a time
+
+// The tokens [t, end) of one sequence, all in new pages.  Row `x + shift` of the sequence is token x; id(i): its page i.
+template <class Id>
+__device__ __forceinline__ void write_stretch(const PlanParams& p, int32_t* row, int64_t* out, int t, int end, int shift,
+                                              Id id) {
   const int lane = threadIdx.x & 31;
-  int lo = 0, hi = p.batch;                    // tok(lo) <= t0 < tok(hi)
-  while (hi - lo > 1) {
-    const int mid = (lo + hi) >> 1;
-    if (tok(mid) <= t0) lo = mid;
-    else hi = mid;
-  }
-  constexpr int kRounds = kSlotRun / 32;
-  const int st0 = start(lo), n0 = len(lo), shift = n0 - (int)tok(lo), have0 = p.page_of(n0 + p.page_size - 1);
-  if (st0 >= 0 && t0 + kSlotRun <= n_slots && tok(lo + 1) >= t0 + kSlotRun && t0 + shift >= have0 * p.page_size &&
-      p.free_pages != nullptr) {
-    // the whole run lies in new pages of one sequence (prompts): page ids first, all loads in flight together
-    int32_t* row = table + (size_t)lo * p.max_pages_per_seq;
-    const int32_t* ids = p.free_pages + (st0 - have0);
-    int64_t* dst = out + t0 + lane;
+#pragma unroll 1
+  for (; t < end; t += 32 * kRounds) {
+    const int pos0 = t + lane + shift, n = end - t - lane;        // rounds 32 k < n of this lane hold a token
+    int64_t* dst = out + t + lane;
     int page[kRounds];
+    uint32_t top = 0;
 #pragma unroll
-    for (int k = 0; k < kRounds; ++k) page[k] = __ldg(&ids[p.page_of(t0 + 32 * k + lane + shift)]);
-    bool bad = false;
+    for (int k = 0; k < kRounds; ++k) page[k] = id(p.page_of(32 * k < n ? pos0 + 32 * k : end - 1 + shift));
 #pragma unroll
     for (int k = 0; k < kRounds; ++k) {
-      const int pos = t0 + 32 * k + lane + shift, i = p.page_of(pos), in_page = pos - i * p.page_size;
-      const bool ok = (unsigned)page[k] < (unsigned)p.n_pages;
-      bad |= !ok;
-      dst[32 * k] = ok ? (int64_t)page[k] * p.page_size + in_page : -1;
-      if (in_page == 0) row[i] = page[k];
-    }
-    if (bad) record_status(p.hdr, XKV_ERR_INVALID_ARG);
-    return;
-  }
-#pragma unroll 1
-  for (int k = 0; k < kRounds; ++k) {
-    const int t = t0 + 32 * k + lane;
-    if (t >= total) break;
-    if (tok(lo + 1) <= t) {                    // every lane its own search: a step has one token per sequence
-      hi = p.batch;
-      while (hi - lo > 1) {
-        const int mid = (lo + hi) >> 1;
-        if (tok(mid) <= t) lo = mid;
-        else hi = mid;
+      const int i = p.page_of(pos0 + 32 * k), in_page = pos0 + 32 * k - i * p.page_size;
+      top = max(top, (uint32_t)page[k]);
+      if (32 * k < n) {
+        dst[32 * k] = (int64_t)page[k] * p.page_size + in_page;
+        if (in_page == 0) row[i] = page[k];
       }
     }
-    int64_t slot = -1;
-    const int st = start(lo);
-    if (st >= 0) {
-      const int n = len(lo), pos = n + (int)(t - tok(lo));
-      const int have = p.page_of(n + p.page_size - 1), i = p.page_of(pos), in_page = pos - i * p.page_size;
-      int32_t* at = table + (size_t)lo * p.max_pages_per_seq + i;
-      const int page = i < have ? *at : free_page(p, st + i - have);
-      if (in_page == 0) *at = page;            // i >= have: the page is new
-      if ((unsigned)page < (unsigned)p.n_pages) slot = (int64_t)page * p.page_size + in_page;
-      else record_status(p.hdr, XKV_ERR_INVALID_ARG);
+    if (top >= (uint32_t)p.n_pages) {                       // an id outside the pool: no slot
+      record_status(p.hdr, XKV_ERR_INVALID_ARG);
+      for (int k = 0; k < kRounds && 32 * k < n; ++k)
+        if ((uint32_t)id(p.page_of(pos0 + 32 * k)) >= (uint32_t)p.n_pages) dst[32 * k] = -1;
     }
-    if (t < n_slots) out[t] = slot;
+  }
+}
+
+// The new tokens [t, t_end) of a layer (a whole warp): their slots, and the table entries of the pages that begin with one
+// of them (every new page begins with a new token).  tok(b): tokens of the layer before sequence b (b <= batch),
+// start(b): where its new pages begin in the free list (-1: it cannot grow), len(b): its rows before the step.  The
+// layer's first n_slots tokens have a place in `out`.
+template <class Tok, class Start, class Len>
+__device__ __forceinline__ void write_range(const PlanParams& p, int32_t* table, int64_t* out, int t, int t_end, int n_slots,
+                                            Tok tok, Start start, Len len) {
+  const int lane = threadIdx.x & 31;
+  constexpr int kMix = 2;
+  auto search = [&](int lo, int x) -> int {    // the sequence that holds token x; lo: one at or before it
+    int hi = p.batch;                          // tok(lo) <= x < tok(hi)
+    while (hi - lo > 1) {
+      const int mid = (lo + hi) >> 1;
+      if (tok(mid) <= x) lo = mid;
+      else hi = mid;
+    }
+    return lo;
+  };
+  int lo = t < t_end ? search(0, t) : 0;
+#pragma unroll 1
+  while (t < t_end) {
+    const int seq_end = (int)min((long long)tok(lo + 1), (long long)t_end);
+    if (seq_end - t >= 32 * kMix && seq_end <= n_slots && start(lo) >= 0) {
+      // a stretch of one sequence (prompts), in new pages: the page ids of eight rounds in flight together
+      const int n = len(lo), shift = n - (int)tok(lo), have = p.page_of(n + p.page_size - 1), first = start(lo) - have;
+      if (t + shift >= have * p.page_size) {
+        int32_t* row = table + (size_t)lo * p.max_pages_per_seq;
+        if (p.free_pages != nullptr) write_stretch(p, row, out, t, seq_end, shift, [&](int i) { return __ldg(p.free_pages + first + i); });
+        else                         write_stretch(p, row, out, t, seq_end, shift, [&](int i) { return first + i; });
+        t = seq_end;
+        if (t < t_end) lo = search(lo, t);
+        continue;
+      }
+    }
+    // any mixture: every lane its own search (a decode step has one token per sequence)
+    int seq[kMix], page[kMix];
+#pragma unroll
+    for (int k = 0; k < kMix; ++k) {
+      const int at = t + 32 * k + lane;
+      seq[k] = -1;
+      page[k] = -1;
+      if (at < t_end) {
+        if (tok(lo + 1) <= at) lo = search(lo, at);
+        const int st = start(lo);
+        if (st >= 0) {
+          const int n = len(lo), i = p.page_of(n + (int)(at - tok(lo))), have = p.page_of(n + p.page_size - 1);
+          seq[k] = lo;
+          page[k] = i < have ? table[(size_t)lo * p.max_pages_per_seq + i] : free_page(p, st + i - have);
+        }
+      }
+    }
+#pragma unroll
+    for (int k = 0; k < kMix; ++k) {
+      const int at = t + 32 * k + lane, b = seq[k];
+      int64_t slot = -1;
+      if (b >= 0) {
+        const int pos = len(b) + (int)(at - tok(b)), i = p.page_of(pos), in_page = pos - i * p.page_size;
+        if (in_page == 0) table[(size_t)b * p.max_pages_per_seq + i] = page[k];
+        if ((unsigned)page[k] < (unsigned)p.n_pages) slot = (int64_t)page[k] * p.page_size + in_page;
+        else record_status(p.hdr, XKV_ERR_INVALID_ARG);
+      }
+      if (at < min(t_end, n_slots)) out[at] = slot;
+    }
+    t += 32 * kMix;
+    if (t < t_end) lo = search(__shfl_sync(0xffffffffu, lo, 0), t);
   }
 }
 
@@ -174,9 +208,9 @@ __global__ void __launch_bounds__(kPlanThreads) plan_kernel(const PlanParams p) 
 
   // ---- pages asked for by the layers before this one
   long long before = 0;
-#pragma unroll 4
+#pragma unroll 8
   for (int e = tid; e < layer * p.batch; e += kPlanThreads) {
-    const Ask a = plan_ask(p, e / p.batch, e % p.batch);
+    const Ask a = plan_ask(p, e / p.batch, e, e % p.batch);
     before += max(a.pages, 0);
   }
   before = warp_sum(before);
@@ -192,7 +226,7 @@ __global__ void __launch_bounds__(kPlanThreads) plan_kernel(const PlanParams p) 
   for (int b0 = 0; b0 < p.batch; b0 += kPlanThreads) {
     const int b = b0 + tid;
     Ask a = {0, 0, 0, false};
-    if (b < p.batch) a = plan_ask(p, layer, b);
+    if (b < p.batch) a = plan_ask(p, layer, layer * p.batch + b, b);
     const long long ask = max(a.pages, 0), add = a.add;
     long long incl = ask, tincl = add;
 #pragma unroll
@@ -238,6 +272,7 @@ __global__ void __launch_bounds__(kPlanThreads) plan_kernel(const PlanParams p) 
   if (slice == 0) {
     end_max = __reduce_max_sync(0xffffffffu, end_max);
     if (lane == 0 && end_max > 0) atomicMax(&p.hdr->plan_used, end_max);
+    __threadfence();                          // the new lengths, for the last CTA; what follows is not waited for
   }
   __syncthreads();
 
@@ -248,28 +283,31 @@ __global__ void __launch_bounds__(kPlanThreads) plan_kernel(const PlanParams p) 
     if (slice == 0 && tid == 0 && total > p.slots_stride) record_status(p.hdr, XKV_ERR_CAPACITY);
     int64_t* out = p.slots + layer * p.slots_stride;
     const int32_t* lens = p.lens_before != nullptr ? p.lens_before + (size_t)layer * p.batch : nullptr;
-    for (int64_t t0 = ((int64_t)slice * kWarps + warp) * kSlotRun; t0 < total; t0 += (int64_t)n_slices * kWarps * kSlotRun)
-      write_run(p, table, out, (int)t0, total, n_slots, [&](int b) { return s_tok[b]; }, [&](int b) { return s_start[b]; },
+    // every warp one stretch: it looks up a sequence once and finds its page ids in the L1 cache
+    const int64_t stretch = ((int64_t)total + n_slices * kWarps - 1) / (n_slices * kWarps);
+    const int64_t t0 = (slice * kWarps + warp) * stretch;
+    write_range(p, table, out, (int)min(t0, (int64_t)total), (int)min(t0 + stretch, (int64_t)total), n_slots,
+                [&](int b) { return s_tok[b]; }, [&](int b) { return s_start[b]; },
                 [&](int b) { return lens != nullptr ? max(__ldg(&lens[b]), 0) : 0; });
   } else {
     // ---- the new table entries: a warp per sequence
     for (int b = slice * kWarps + warp; b < p.batch; b += n_slices * kWarps) {
       const int start = s_start[b];
       if (start < 0) continue;
-      const Ask a = plan_ask(p, layer, b);
+      const Ask a = plan_ask(p, layer, layer * p.batch + b, b);
       write_pages(p, table + (size_t)b * p.max_pages_per_seq + p.page_of(a.len + p.page_size - 1), a.pages, start);
     }
   }
 
   // ---- the last CTA to get here writes the lengths (every other one has read them) and the list position
-  __threadfence();
   __syncthreads();
   const int n_ctas = gridDim.x * gridDim.y;
   if (tid == 0) s_last = (atomicAdd(&p.hdr->plan_ticket, 1) == n_ctas - 1) ? 1 : 0;
   __syncthreads();
   if (!s_last) return;
   __threadfence();
-  for (int64_t e = tid; e < (int64_t)p.n_layers * p.batch; e += kPlanThreads) p.lens_after[e] = __ldcg(&p.new_lens[e]);
+#pragma unroll 8
+  for (int e = tid; e < p.n_layers * p.batch; e += kPlanThreads) p.lens_after[e] = __ldcg(&p.new_lens[e]);
   if (tid == 0) {
     const int end = atomicExch(&p.hdr->plan_used, 0);
     if (p.used_after != nullptr) *p.used_after = max(end, used);
@@ -296,7 +334,7 @@ __global__ void __launch_bounds__(kSmallThreads) plan_small_kernel(const PlanPar
   for (int i = 0; i < kPer; ++i) {
     const int e = tid * per + i;
     a[i] = {0, 0, 0, false};
-    if (i < per && e < n_units) a[i] = plan_ask(p, e / p.batch, e % p.batch);
+    if (i < per && e < n_units) a[i] = plan_ask(p, e / p.batch, e, e % p.batch);
     ask += max(a[i].pages, 0);
     add += a[i].add;
   }
@@ -388,9 +426,9 @@ __global__ void __launch_bounds__(kSmallThreads) plan_small_kernel(const PlanPar
     const int total = (int)min(s_tok64[e0 + p.batch] - first, 0x7fffffffll);
     if (r == 0 && lane == 0 && total > p.slots_stride) record_status(p.hdr, XKV_ERR_CAPACITY);
     if ((long long)r * kSlotRun >= total) return false;
-    write_run(p, p.block_table + (size_t)e0 * p.max_pages_per_seq, p.slots + l * p.slots_stride, r * kSlotRun, total,
-              (int)min((int64_t)total, p.slots_stride), [&](int b) { return s_tok64[e0 + b] - first; },
-              [&](int b) { return s_start[e0 + b]; }, [&](int b) { return s_len[e0 + b]; });
+    write_range(p, p.block_table + (size_t)e0 * p.max_pages_per_seq, p.slots + l * p.slots_stride, r * kSlotRun,
+                min((r + 1) * kSlotRun, total), (int)min((int64_t)total, p.slots_stride), [&](int b) { return s_tok64[e0 + b] - first; },
+                [&](int b) { return s_start[e0 + b]; }, [&](int b) { return s_len[e0 + b]; });
     return true;
   };
 #pragma unroll 1
@@ -574,8 +612,8 @@ xkv_status plan_append(const xkv_cache* c, int batch, const int32_t* n_new, int 
   p.page_size = c->page_size;
   p.max_pages_per_seq = c->max_pages_per_seq;
   p.n_pages = c->n_pages;
-  const uint32_t d16 = (uint32_t)c->page_size / 16;
-  p.page_mul = d16 == 1 ? 0u : (uint32_t)(((1ull << 32) + d16 - 1) / d16);
+  const uint32_t d8 = (uint32_t)c->page_size / 8;
+  p.page_mul = (uint32_t)(((1ull << 32) + d8 - 1) / d8);
   p.hdr = static_cast<WorkspaceHeader*>(workspace);
   p.new_lens = reinterpret_cast<int32_t*>(static_cast<uint8_t*>(workspace) + kHeaderBytes);
   // One CTA where that is little work for it: 3.x us against y us for the step of a batch of 64 in 32 layers.
