@@ -423,7 +423,9 @@ xkv_status xkv_store_rows(const xkv_dims* dims, const xkv_cache* cache, const vo
  * plan their work themselves from the lengths before the call; the block that handles the end of a
  * cache takes the new row from k_new / v_new and stores it, and seq_lens is advanced when the last
  * block leaves. No block waits for another one to start, so the launch needs no particular
- * residency. Larger problems run a separate append-and-plan kernel first.
+ * residency. Larger problems run a separate append-and-plan kernel first. Over an XKV_KV_E4M3 cache the call is one small
+ * kernel (appends the new rows, advances seq_lens, clears counters) and one attention kernel whatever the number of
+ * units; the rows are cut into equal shares, chunk_rows only sizes the workspace (fewer partial results, fewer shares).
  */
 xkv_status xkv_decode_attn(const xkv_dims* dims, const xkv_cache* cache, int32_t layer_begin,
                            int32_t layer_end, const void* q, const void* k_new, const void* v_new,
@@ -497,7 +499,8 @@ void xkv_profile_events(void* start, void* stop);
  * Test hook (no counterpart in the paper), process-wide: the limit of every bounded wait inside the kernels
  * (nanoseconds; <= 0 restores the default of two seconds), and the index of one decode work item whose
  * split-K merge ticket is never published (-1: none), so that a test can watch a wait run out: the kernel
- * returns, the device status reads XKV_ERR_TIMEOUT and the workspace stays usable.
+ * returns, the device status reads XKV_ERR_TIMEOUT and the workspace stays usable. (Decode over XKV_KV_E4M3 caches has no
+ * wait for a ticket: there the second argument is the index of a CTA whose copies are never issued.)
  */
 void xkv_test_hooks(int64_t wait_limit_ns, int32_t withhold_decode_item);
 

@@ -88,7 +88,7 @@ struct Params {
   int32_t layer_begin, batch, n_units, n_q_heads, n_kv_heads, group, page_size, max_pages_per_seq, n_pages;
   int32_t box_rows;                   // rows of a TMA box: the largest power of two up to 128 that divides page_size
   int32_t max_ctas;                   // CTAs that the partial results have room for
-  int32_t withhold_cta;               // test hook: this CTA's pieces are never counted (-1: none)
+  int32_t withhold_cta;               // test hook: this CTA's copies are never issued, so that waits expire (-1: none)
   int32_t wait_first;                 // the launch before this one appends rows: wait for it before reading a length
   float scale_log2;
   uint64_t wait_ns;
@@ -268,7 +268,7 @@ __device__ __forceinline__ void join_heads(const Params& p, const int4 job, int 
   constexpr int kCols = D / 32;
   const int lane = threadIdx.x & 31, G = p.group;
   const float2* ml_at = reinterpret_cast<const float2*>(p.part_ml);
-  const float* o_at = p.part_o + lane;
+  const float* o_at = p.part_o + lane * kCols;
   float mx[kHeads], den[kHeads], o[kHeads][kCols];
 #pragma unroll
   for (int x = 0; x < kHeads; ++x) {
@@ -295,8 +295,13 @@ __device__ __forceinline__ void join_heads(const Params& p, const int4 job, int 
 #pragma unroll
       for (int k = 0; k < kPieces; ++k) {
         const float* src = o_at + (size_t)row_of(k, x) * D;
-#pragma unroll
-        for (int c = 0; c < kCols; ++c) v[x][k][c] = __ldcg(src + c * 32);
+        if constexpr (kCols == 4) {
+          const float4 q = __ldcg(reinterpret_cast<const float4*>(src));
+          v[x][k][0] = q.x, v[x][k][1] = q.y, v[x][k][2] = q.z, v[x][k][3] = q.w;
+        } else {
+          const float2 q = __ldcg(reinterpret_cast<const float2*>(src));
+          v[x][k][0] = q.x, v[x][k][1] = q.y;
+        }
       }
 #pragma unroll
     for (int x = 0; x < kHeads; ++x) {
@@ -322,7 +327,8 @@ __device__ __forceinline__ void join_heads(const Params& p, const int4 job, int 
     if (g + x >= G) break;
     const size_t row = (size_t)job.x * p.n_q_heads + (size_t)job.y * G + g + x;
 #pragma unroll
-    for (int c = 0; c < kCols; ++c) p.out[row * D + c * 32 + lane] = __float2bfloat16(o[x][c] / den[x]);
+    for (int c = 0; c < kCols; c += 2)
+      *reinterpret_cast<uint32_t*>(p.out + row * D + lane * kCols + c) = pack_bf16(o[x][c] / den[x], o[x][c + 1] / den[x]);
     if (lane == 0 && p.lse != nullptr) p.lse[row] = (mx[x] + log2f(den[x])) * 0.6931471805599453f;
   }
 }
@@ -483,7 +489,7 @@ decode_e4m3_kernel(const __grid_constant__ CUtensorMap tmap_k, const __grid_cons
         nxt_pages = load_pages(nxt, 0);
       }
       const Item cur = nxt;
-      if (cur.e < 0) break;
+      if (cur.e < 0 || (int)blockIdx.x == p.withhold_cta) break;
       int pages = nxt_pages, ahead = 0;
       have_next = false;
       const int n_tiles = tiles_of(cur.rows);
@@ -739,7 +745,7 @@ decode_e4m3_kernel(const __grid_constant__ CUtensorMap tmap_k, const __grid_cons
       if (lane == 0) mbar_arrive(&s_fifo_empty[slot]);
       if (it.n_pieces == 1) continue;
       int last = 0;
-      if (lane == 0 && (int)blockIdx.x != p.withhold_cta) {
+      if (lane == 0) {
         // counted once it is visible; whoever counts the last one sees all
         last = add_acq_rel(&p.tickets[(size_t)it.e * Hkv + it.h], 1) == it.n_pieces - 1;
       }
@@ -906,7 +912,7 @@ decode_e4m3_kernel(const __grid_constant__ CUtensorMap tmap_k, const __grid_cons
     const bool over = __any_sync(0xffffffffu, *(volatile int*)&s_joins.all != 0);   // set on every way out of warp 7's loop
     join_open<D>(p, &s_joins);
     if (over) break;
-    __nanosleep(100);
+    __nanosleep(40);
   }
   __syncthreads();
   if (*s_abort) {

@@ -310,6 +310,52 @@ def test_decode_append_beyond_the_page_table():
     check_all(pool, 1, q, out, lse, [[32, 32, 6]], what="full")
 
 
+def test_decode_waits_that_expire():
+    """One CTA's copies are never issued: its waits run out after a millisecond, the launch returns and says so, and
+    workspace and cache stay usable."""
+    pool = Pool([[3000, 40], [17, 5000]], 2, 128, 16, seed=12)
+    q = queries(2, 2, 8, 128, 12)
+    want, want_lse, st = run_decode(pool, 8, q)
+    assert st == xkv.OK
+    dims = xkv.Dims(2, 8, 2, 128, 1, 1, 0, 0.0, 256, 128)
+    ws = torch.zeros(xkv.workspace_bytes(xkv.OP_DECODE_ATTN, dims, n_layers=2, max_cache_len=pool.cols * 16),
+                     dtype=torch.uint8, device=DEV)
+    try:
+        xkv.test_hooks(wait_limit_ns=1_000_000, withhold_decode_item=1)
+        _, _, st = run_decode(pool, 8, q, ws=ws)
+    finally:
+        xkv.test_hooks()
+    assert st == xkv.ERR_TIMEOUT
+    got, got_lse, st = run_decode(pool, 8, q, ws=ws)
+    assert st == xkv.OK and torch.equal(got, want) and torch.equal(got_lse, want_lse)
+
+
+def test_decode_profile_events():
+    pool = Pool([[500, 40]], 2, 64, 16, seed=13)
+    q = queries(1, 2, 4, 64, 13)
+    start, stop = (torch.cuda.Event(enable_timing=True) for _ in range(2))
+    start.record()
+    stop.record()
+    try:
+        xkv.profile_events(start, stop)
+        out, lse, st = run_decode(pool, 4, q)
+    finally:
+        xkv.profile_events(None, None)
+    assert st == xkv.OK and 0.0 < start.elapsed_time(stop) < 100.0
+    check_all(pool, 4, q, out, lse, pool.lens, what="timed")
+
+
+def test_decode_repeats_bit_for_bit():
+    lens = np.random.default_rng(2).integers(1, 3000, (3, 9))
+    pool = Pool(lens, 2, 128, 32, seed=14)
+    q = queries(3, 9, 10, 128, 14)
+    want, want_lse, st = run_decode(pool, 10, q)
+    assert st == xkv.OK
+    for _ in range(30):
+        got, got_lse, _ = run_decode(pool, 10, q)
+        assert torch.equal(got, want) and torch.equal(got_lse, want_lse)
+
+
 # ------------------------------------------------------------------ rows stored by slot
 def store(pool, k, v, slots, dims=None):
     dims = dims or xkv.Dims(1, pool.H, pool.H, pool.d, 1, 1, 0, 0.0, pool.H * pool.d, pool.d)
