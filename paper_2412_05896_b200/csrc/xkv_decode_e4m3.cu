@@ -381,7 +381,7 @@ decode_e4m3_kernel(const __grid_constant__ CUtensorMap tmap_k, const __grid_cons
   __shared__ float s_max[2][4][8];
   __shared__ float s_sum[2][4][8];
   __shared__ int s_scan[kThreads / 32];
-  __shared__ int s_before[kThreads];              // line (of one KV head) before each thread's run of units
+  __shared__ int4 s_first;                        // the unit in which the share begins: unit, rows, where it begins on the line
   __shared__ uint32_t s_tmem;
   __shared__ int s_abort_store;
   __shared__ Joins s_joins;
@@ -389,6 +389,15 @@ decode_e4m3_kernel(const __grid_constant__ CUtensorMap tmap_k, const __grid_cons
   const int tid = threadIdx.x, lane = tid & 31, warp = tid >> 5;
   const int Hkv = p.n_kv_heads, G = p.group;
 
+  if (p.wait_first) grid_dependency_wait();
+  // ---- the plan: each thread a run of units, and their length on the line
+  const int per = (p.n_units + kThreads - 1) / kThreads;
+  int mine = 0;
+#pragma unroll 8
+  for (int i = 0; i < per; ++i) {
+    const int e = tid * per + i;
+    if (e < p.n_units) mine += cost_of(unit_rows(p, e));
+  }
   if (tid == 0) {
     for (int i = 0; i < C::kStages; ++i) {
       mbar_init(&s_k_full[i], 1);
@@ -423,15 +432,6 @@ decode_e4m3_kernel(const __grid_constant__ CUtensorMap tmap_k, const __grid_cons
     reinterpret_cast<uint4*>(smem + C::kOffQ)[i] = make_uint4(0u, 0u, 0u, 0u);
   fence_proxy_async_smem();
 
-  if (p.wait_first) grid_dependency_wait();
-  // ---- the plan: the line before each thread's run of units
-  const int per = (p.n_units + kThreads - 1) / kThreads;
-  int mine = 0;
-#pragma unroll 8
-  for (int i = 0; i < per; ++i) {
-    const int e = tid * per + i;
-    if (e < p.n_units) mine += cost_of(unit_rows(p, e));
-  }
   int incl = mine;
 #pragma unroll
   for (int o = 1; o < 32; o <<= 1) {
@@ -448,19 +448,25 @@ decode_e4m3_kernel(const __grid_constant__ CUtensorMap tmap_k, const __grid_cons
     if (w < warp) before += s_scan[w];
     line += s_scan[w];
   }
-  s_before[tid] = before;
   line *= Hkv;
   const int n_ctas = min(min((int)gridDim.x, p.max_ctas), max(line / kMinSegment, 1));
   const Cut share(line, n_ctas);
-  if (!p.wait_first) grid_dependency_wait();      // the counters below are cleared by the launch before this one
-  // rows of empty caches
-  for (int e = blockIdx.x; e < p.n_units; e += gridDim.x) {
-    if (unit_rows(p, e) != 0) continue;
-    const size_t row0 = (size_t)e * p.n_q_heads;
-    for (int i = tid; i < p.n_q_heads * D / 8; i += kThreads)
-      reinterpret_cast<uint4*>(p.out + row0 * D)[i] = make_uint4(0u, 0u, 0u, 0u);
-    if (p.lse != nullptr)
-      for (int i = tid; i < p.n_q_heads; i += kThreads) p.lse[row0 + i] = -INFINITY;
+  const bool works = (int)blockIdx.x < n_ctas && line > 0;
+  const int begin = works ? share.begin(blockIdx.x) : 0, stop_at = works ? share.begin(blockIdx.x + 1) : 0;
+  if (works && before * Hkv <= begin && begin < (before + mine) * Hkv) {
+    int at = before * Hkv;                        // this thread's run of units holds the begin of the share
+    for (int i = 0; i < per; ++i) {
+      const int e = tid * per + i, rows = e < p.n_units ? unit_rows(p, e) : 0, next = at + cost_of(rows) * Hkv;
+      if (begin < next) {
+        s_first = make_int4(e, rows, at, 0);
+        // have the page id of the first tile on its way to the L1 cache
+        const int row = min((begin - at) % cost_of(rows) * kScaleBlock, rows - 1);
+        asm volatile("prefetch.global.L1 [%0];" ::"l"(p.block_table + ((size_t)p.layer_begin * p.batch + e) * p.max_pages_per_seq +
+                                                     row / p.page_size));
+        break;
+      }
+      at = next;
+    }
   }
   __syncthreads();
   const uint32_t tmem = s_tmem;
@@ -616,41 +622,9 @@ decode_e4m3_kernel(const __grid_constant__ CUtensorMap tmap_k, const __grid_cons
     }
   } else if (warp == 6) {
     // ================================================================ the walk, and the queries as two codes per element
-    const bool works = (int)blockIdx.x < n_ctas && line > 0;
-    int at = works ? share.begin(blockIdx.x) : 0;      // next position, the end of the segment
-    const int stop_at = works ? share.begin(blockIdx.x + 1) : 0;
-    int e = -1, h = 0, rows = 0, cost = 0;
-    int unit_at = 0;                              // where (e, head 0) begins
-    // Stands on position x: the run of units that holds it, then the unit (all lanes).
-    auto find_unit = [&](int x) {
-      int n = 0;
-      for (int i = lane; i < kThreads; i += 32) n += (long long)s_before[i] * Hkv <= x ? 1 : 0;
-      const int run = (int)__reduce_add_sync(0xffffffffu, (unsigned)n) - 1;
-      int base = s_before[run];
-      for (int i0 = 0; i0 < per; i0 += 32) {
-        const int u = run * per + i0 + lane;
-        const int ur = i0 + lane < per && u < p.n_units ? unit_rows(p, u) : 0;
-        const int uc = cost_of(ur);
-        int sum = uc;
-#pragma unroll
-        for (int o = 1; o < 32; o <<= 1) {
-          const int y = __shfl_up_sync(0xffffffffu, sum, o);
-          if (lane >= o) sum += y;
-        }
-        const unsigned hit = __ballot_sync(0xffffffffu, (long long)(base + sum) * Hkv > x);
-        if (hit != 0) {
-          const int w = __ffs(hit) - 1;
-          e = run * per + i0 + w;
-          rows = __shfl_sync(0xffffffffu, ur, w);
-          cost = __shfl_sync(0xffffffffu, uc, w);
-          unit_at = (base + __shfl_sync(0xffffffffu, sum - uc, w)) * Hkv;
-          h = (x - unit_at) / cost;
-          return;
-        }
-        base += __shfl_sync(0xffffffffu, sum, 31);
-      }
-    };
-    if (works) find_unit(at);
+    int at = begin;                               // next position of the share
+    int e = s_first.x, rows = s_first.y, unit_at = s_first.z;      // unit_at: where (e, head 0) begins
+    int cost = cost_of(rows), h = works ? (begin - unit_at) / cost : 0;
     // The next piece: the tiles of (e, h) that start in [at, stop_at).
     auto next_item = [&]() -> Item {
       Item it = {-1, 0, 0, 0, 0, 0};
@@ -735,6 +709,16 @@ decode_e4m3_kernel(const __grid_constant__ CUtensorMap tmap_k, const __grid_cons
     }
   } else if (warp == 7) {
     // ================================================================ finished pieces of cut caches
+    // first the rows of empty caches
+    for (int e = blockIdx.x; e < p.n_units; e += gridDim.x) {
+      if (unit_rows(p, e) != 0) continue;
+      const size_t row0 = (size_t)e * p.n_q_heads;
+      for (int i = lane; i < p.n_q_heads * D / 8; i += 32)
+        reinterpret_cast<uint4*>(p.out + row0 * D)[i] = make_uint4(0u, 0u, 0u, 0u);
+      if (p.lse != nullptr)
+        for (int i = lane; i < p.n_q_heads; i += 32) p.lse[row0 + i] = -INFINITY;
+    }
+    if (!p.wait_first) grid_dependency_wait();    // the tickets are cleared by the launch before this one
     for (uint32_t n_item = 0;; ++n_item) {
       const int slot = n_item % kFifo;
       if (!__all_sync(0xffffffffu, wait_bar(&s_fifo_full[slot], (n_item / kFifo) & 1, s_abort, p.wait_ns))) break;
