@@ -86,7 +86,11 @@ struct Params {
   const int32_t* block_table;
   const int32_t* seq_lens;
   int32_t layer_begin, batch, n_units, n_q_heads, n_kv_heads, group, page_size, max_pages_per_seq, n_pages;
+  // row -> page: page_size is 8 n with n even, 2 <= n <= 32, and x / n = (x * ceil(2^32 / n)) >> 32 for x <= 2^27 + 32
+  uint32_t page_mul;                  // ceil(2^32 / n)
+  __device__ __forceinline__ int page_of(int row) const { return (int)__umulhi((uint32_t)row >> 3, page_mul); }
   int32_t box_rows;                   // rows of a TMA box: the largest power of two up to 128 that divides page_size
+  int32_t box_shift;                  // its logarithm
   int32_t max_ctas;                   // CTAs that the partial results have room for
   int32_t withhold_cta;               // test hook: this CTA's copies are never issued, so that waits expire (-1: none)
   int32_t wait_first;                 // the launch before this one appends rows: wait for it before reading a length
@@ -98,12 +102,25 @@ struct Params {
   float* part_ml;                     // [2 * CTAs][G][2]
 };
 
+// a / b for 0 <= a < 2^31, 0 < b: two steps of a reciprocal and a correction, half the instructions of the general
+// division.  (What a CTA runs once it runs out of a cold instruction cache, at some seven clocks an instruction.)
+__device__ __forceinline__ int quotient(int a, int b) {
+  const float inv = __frcp_rn((float)b);
+  int q = (int)((float)a * inv);                  // off by at most a / b * 2^-22 + 1
+  q += (int)((float)(a - q * b) * inv);           // off by at most one
+  const int r = a - q * b;
+  return r < 0 ? q - 1 : (r >= b ? q + 1 : q);
+}
+
 // [0, n) cut into `parts` runs that differ by at most one.
 struct Cut {
   int32_t q, r;
-  __device__ __forceinline__ Cut(int n, int parts) : q(n / parts), r(n % parts) {}
+  __device__ __forceinline__ Cut(int n, int parts) : q(quotient(n, parts)), r(n - q * parts) {}
   __device__ __forceinline__ int begin(int i) const { return i * q + min(i, r); }
-  __device__ __forceinline__ int part_of(int x) const { return x < r * (q + 1) ? x / (q + 1) : r + (x - r * (q + 1)) / q; }
+  __device__ __forceinline__ int part_of(int x) const {
+    const bool longer = x < r * (q + 1);
+    return longer ? quotient(x, q + 1) : r + quotient(x - r * (q + 1), q);
+  }
 };
 
 struct Item {                         // one CTA's piece of one cache
@@ -375,7 +392,7 @@ decode_e4m3_kernel(const __grid_constant__ CUtensorMap tmap_k, const __grid_cons
   uint8_t* smem = reinterpret_cast<uint8_t*>((reinterpret_cast<uintptr_t>(smem_raw) + 1023) & ~uintptr_t(1023));
   __shared__ uint64_t s_k_full[C::kStages], s_k_empty[C::kStages], s_v_full[C::kStages], s_v_empty[C::kStages],
       s_scale_full[C::kStages], s_s_full[2], s_p_full[2], s_d_full[2], s_fifo_full[kFifo], s_fifo_empty[kFifo],
-      s_q_full[kFifo], s_done_full[kFifo];
+      s_q_full[kFifo], s_done_full[kFifo], s_wake;
   __shared__ Item s_item[kFifo];
   __shared__ float s_qscale[kFifo][8];
   __shared__ float s_max[2][4][8];
@@ -417,6 +434,7 @@ decode_e4m3_kernel(const __grid_constant__ CUtensorMap tmap_k, const __grid_cons
       mbar_init(&s_q_full[i], 1);
       mbar_init(&s_done_full[i], 4);
     }
+    mbar_init(&s_wake, 1);
     s_abort_store = 0;
     s_joins.n_jobs = s_joins.claimed = s_joins.joined = s_joins.all = 0;
     fence_mbar_init();
@@ -459,10 +477,6 @@ decode_e4m3_kernel(const __grid_constant__ CUtensorMap tmap_k, const __grid_cons
       const int e = tid * per + i, rows = e < p.n_units ? unit_rows(p, e) : 0, next = at + cost_of(rows) * Hkv;
       if (begin < next) {
         s_first = make_int4(e, rows, at, 0);
-        // have the page id of the first tile on its way to the L1 cache
-        const int row = min((begin - at) % cost_of(rows) * kScaleBlock, rows - 1);
-        asm volatile("prefetch.global.L1 [%0];" ::"l"(p.block_table + ((size_t)p.layer_begin * p.batch + e) * p.max_pages_per_seq +
-                                                     row / p.page_size));
         break;
       }
       at = next;
@@ -473,17 +487,27 @@ decode_e4m3_kernel(const __grid_constant__ CUtensorMap tmap_k, const __grid_cons
 
   if (warp == 4) {
     // ================================================================ the copies
-    const int R = p.box_rows, boxes_per_tile = kTile / R;
+    const int R = p.box_rows, boxes_per_tile = kTile >> p.box_shift;
     // page of box `lane` of a batch of 32 boxes of an item
     auto load_pages = [&](const Item& it, int box0) -> int {
       const int r = it.row0 + (box0 + lane) * R;
       int page = 0;
       if (it.e >= 0 && r < it.row0 + it.rows)
-        page = __ldg(&p.block_table[((size_t)p.layer_begin * p.batch + it.e) * p.max_pages_per_seq + r / p.page_size]);
+        page = __ldg(&p.block_table[((size_t)p.layer_begin * p.batch + it.e) * p.max_pages_per_seq + p.page_of(r)]);
       return page;
     };
     uint32_t j = 0;                               // tiles issued
     Item nxt = {-1, 0, 0, 0, 0, 0};
+    // Page ids of the share's first tile, on their way before the first item is known: it begins in this unit (unless no
+    // tile starts there any more).
+    Item guess = {-1, 0, 0, 0, 0, 0};
+    if (works) {
+      guess.e = s_first.x;
+      const int cost = cost_of(s_first.y), off = begin - s_first.z;
+      guess.row0 = (off - quotient(off, cost) * cost + kTileBlocks - 1) / kTileBlocks * kTile;
+      guess.rows = s_first.y - guess.row0;
+    }
+    const int guess_pages = load_pages(guess, 0);
     int nxt_pages = 0;
     bool have_next = false, ok = true;
     for (uint32_t n_item = 0; ok; ++n_item) {
@@ -492,7 +516,7 @@ decode_e4m3_kernel(const __grid_constant__ CUtensorMap tmap_k, const __grid_cons
         ok = __all_sync(0xffffffffu, wait_bar(&s_fifo_full[slot], (n_item / kFifo) & 1, s_abort, p.wait_ns));
         if (!ok) break;
         nxt = s_item[slot];
-        nxt_pages = load_pages(nxt, 0);
+        nxt_pages = n_item == 0 && nxt.e == guess.e && nxt.row0 == guess.row0 ? guess_pages : load_pages(nxt, 0);
       }
       const Item cur = nxt;
       if (cur.e < 0 || (int)blockIdx.x == p.withhold_cta) break;
@@ -508,12 +532,12 @@ decode_e4m3_kernel(const __grid_constant__ CUtensorMap tmap_k, const __grid_cons
         const int stage = j % C::kStages;
         const uint32_t ph = ((j / C::kStages) - 1) & 1;
         const int left = min(kTile, cur.rows - t * kTile);
-        const int n_box = (left + R - 1) / R, n_blk = (left + kScaleBlock - 1) / kScaleBlock;
+        const int n_box = (left + R - 1) >> p.box_shift, n_blk = (left + kScaleBlock - 1) / kScaleBlock;
         // first row of this lane's box in the page pool (lanes past the last box: not used)
         const int row_of_box = cur.row0 + t * kTile + lane * R;
         int page = __shfl_sync(0xffffffffu, pages, (box0 + lane) & 31);
         page = min(max(page, 0), p.n_pages - 1);
-        const int grow = (page * Hkv + cur.h) * p.page_size + row_of_box % p.page_size;
+        const int grow = (page * Hkv + cur.h - p.page_of(row_of_box)) * p.page_size + row_of_box;
         if (j >= C::kStages) ok = wait_bar(&s_k_empty[stage], ph, s_abort, p.wait_ns);
         ok = __all_sync(0xffffffffu, ok);
         if (!ok) break;
@@ -531,8 +555,9 @@ decode_e4m3_kernel(const __grid_constant__ CUtensorMap tmap_k, const __grid_cons
         {
           // lanes 0-7: scales of the tile's eight blocks of K rows, lanes 8-15: of V rows
           const int blk = lane & 7;
-          int bg = __shfl_sync(0xffffffffu, grow, (blk * kScaleBlock) / R);
-          bg = bg / kScaleBlock + blk - (blk * kScaleBlock) / R * (R / kScaleBlock);
+          const int in_box = (blk * kScaleBlock) >> p.box_shift;
+          int bg = __shfl_sync(0xffffffffu, grow, in_box);
+          bg = bg / kScaleBlock + blk - (in_box << p.box_shift) / kScaleBlock;
           if (lane < 16) {
             const bool live = blk < n_blk;
             float* dst = reinterpret_cast<float*>(smem + C::kOffScales) + stage * 16 + lane;
@@ -624,7 +649,7 @@ decode_e4m3_kernel(const __grid_constant__ CUtensorMap tmap_k, const __grid_cons
     // ================================================================ the walk, and the queries as two codes per element
     int at = begin;                               // next position of the share
     int e = s_first.x, rows = s_first.y, unit_at = s_first.z;      // unit_at: where (e, head 0) begins
-    int cost = cost_of(rows), h = works ? (begin - unit_at) / cost : 0;
+    int cost = cost_of(rows), h = works ? quotient(begin - unit_at, cost) : 0;
     // The next piece: the tiles of (e, h) that start in [at, stop_at).
     auto next_item = [&]() -> Item {
       Item it = {-1, 0, 0, 0, 0, 0};
@@ -709,6 +734,7 @@ decode_e4m3_kernel(const __grid_constant__ CUtensorMap tmap_k, const __grid_cons
     }
   } else if (warp == 7) {
     // ================================================================ finished pieces of cut caches
+    bool woken = false;                           // warps that are out of tiles wait for the first job or for the end
     // first the rows of empty caches
     for (int e = blockIdx.x; e < p.n_units; e += gridDim.x) {
       if (unit_rows(p, e) != 0) continue;
@@ -743,12 +769,17 @@ decode_e4m3_kernel(const __grid_constant__ CUtensorMap tmap_k, const __grid_cons
           s_joins.job[n % kJobs] = make_int4(it.e, it.h, it.first_cta, it.n_pieces);
           __threadfence_block();
           *(volatile int*)&s_joins.n_jobs = n + 1;
+          if (!woken) mbar_arrive(&s_wake);
         }
+        woken = true;
         __syncwarp();
         join_open<D>(p, &s_joins);
       }
     }
-    if (lane == 0) *(volatile int*)&s_joins.all = 1;
+    if (lane == 0) {
+      *(volatile int*)&s_joins.all = 1;
+      if (!woken) mbar_arrive(&s_wake);
+    }
   } else {
     // ================================================================ softmax and output
     const uint32_t lane_base = (uint32_t)warp << 21;            // tensor-memory lanes 32 * warp ..
@@ -892,6 +923,7 @@ decode_e4m3_kernel(const __grid_constant__ CUtensorMap tmap_k, const __grid_cons
     }
   }
   // ---- out of tiles: help with the joins until warp 7 has counted its last piece
+  if (warp != 7) wait_bar(&s_wake, 0, s_abort, p.wait_ns);
   while (warp != 7) {
     const bool over = __any_sync(0xffffffffu, *(volatile int*)&s_joins.all != 0);   // set on every way out of warp 7's loop
     join_open<D>(p, &s_joins);
@@ -1004,7 +1036,10 @@ xkv_status decode_attn_e4m3(const xkv_dims* d, const xkv_cache* c, int layer_beg
   p.page_size = c->page_size;
   p.max_pages_per_seq = c->max_pages_per_seq;
   p.n_pages = c->n_pages;
+  const uint32_t n8 = (uint32_t)c->page_size / 8;
+  p.page_mul = (uint32_t)(((1ull << 32) + n8 - 1) / n8);
   p.box_rows = box;
+  p.box_shift = 31 - __builtin_clz((unsigned)box);
   const int64_t room = ws.max_items / 2;
   p.max_ctas = (int32_t)(room < 1 ? 1 : (room < (1 << 20) ? room : 1 << 20));
   p.wait_first = k_new != nullptr ? 1 : 0;
