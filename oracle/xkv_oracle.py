@@ -492,7 +492,7 @@ def e4m3_block_scale(X: np.ndarray) -> float:
     X = np.abs(np.asarray(X, dtype=np.float64))
     X = X[np.isfinite(X)]
     top = float(X.max()) if X.size else 0.0
-    e = -100
+    e = max(-100, min(120, math.floor(math.log2(top / E4M3_MAX)) - 1)) if top > 0 else -100
     while e < 120 and top > math.ldexp(E4M3_MAX, e):
         e += 1
     return math.ldexp(1.0, e)

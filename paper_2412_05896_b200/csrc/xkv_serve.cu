@@ -1,11 +1,18 @@
 // Serving on a reduced cache: the plan of a step (xkv_plan_append) and rows stored by slot (xkv_store_rows).
 //
-//   plan_kernel         block tables, slot maps and new lengths of every (layer, sequence) from the lengths before the
-//                       step and the new tokens.  grid = (slices, layers); no CTA waits for another one: each forms
-//                       the pages asked for by the layers before its own and the scan over its layer's sequences by
+//   plan_small_kernel   the plan of up to 4096 (layer, sequence) caches by one CTA: pages asked for, their scan, new
+//                       lengths; for a decode step's few tokens also their slots and table entries
+//   slots_kernel        slots and table entries of many tokens, from what plan_small_kernel found (programmatic dependent
+//                       launch): a stretch of tokens per warp, the page ids of eight rounds in flight together.  Bound by
+//                       its 8 bytes written per layer and token (84 MB of 64 prompts in 32 layers: 27 us, 3.1 TB/s, of
+//                       which about 7 us are the first launch) and the dozen instructions that make one.
+//   plan_kernel         more caches than that, in one launch: grid = (slices, layers), no CTA waits for another one: each
+//                       forms the pages asked for by the layers before its own and the scan over its layer's sequences by
 //                       itself (integers out of L2), and the last CTA to leave writes the lengths, so that they may
 //                       be advanced in place.
-//   store_block_kernel  caches of 8-bit floats: one warp per (run of tokens within a block of 16 slots, KV head, K or V)
+//   store_block_kernel  caches of 8-bit floats: one warp per (run of tokens within a block of 16 slots, KV head, K or V),
+//                       which reads the run once, finds its largest magnitude and stores the codes: HBM-bound, 3 bytes a
+//                       value (K and V of 9160 tokens, 32 heads of 128: 225 MB in 38 us, 0.90 of the copy rate)
 //   store_row_kernel    caches of bf16 or of 8-bit integers: D/8 lanes per (token, KV head)
 //   append_block_kernel one new row per (layer, sequence) and KV head of a cache of 8-bit floats, lengths advanced
 #include <algorithm>
@@ -24,7 +31,7 @@ constexpr int kPlanThreads = 256;
 constexpr int kSmallThreads = 1024;           // one CTA plans up to kSmallUnits sequences of all layers
 constexpr int kSmallUnits = 4096;
 constexpr int kSlotRun = 64;                  // ... and hands its tokens to its warps in runs of so many
-constexpr int64_t kSmallTokens = 32768;
+constexpr int64_t kSmallTokens = 1024;        // ... where they are no more than this (by the slot maps' sizes)
 constexpr int kPlanMaxBatch = 16384;          // sequences of a layer: two 4-byte table entries each in shared memory
 
 struct PlanParams {
@@ -41,7 +48,12 @@ struct PlanParams {
   int64_t slots_stride;
   int32_t n_layers, batch, page_size, max_pages_per_seq, n_pages;
   WorkspaceHeader* hdr;
-  int32_t* new_lens;            // [n_layers][batch] in the workspace, until the last CTA copies them out
+  // in the workspace
+  int32_t* new_lens;            // [n_layers][batch]: one launch of many CTAs: until the last of them copies them out
+  int32_t* ws_tok;              // [n_layers][batch + 1], [n_layers][batch] twice: two launches: what the first one found
+  int32_t* ws_start;
+  int32_t* ws_len;
+  int32_t two_launches;
   // row -> page: page_size is 8 D with D even, 2 <= D <= 32, and n / D = (n * ceil(2^32 / D)) >> 32 for n <= 2^27 + 32
   // (exact: n times what the ceiling adds, at most 29 where D is no power of two and else nothing, stays below 2^32)
   uint32_t page_mul;            // ceil(2^32 / D)
@@ -316,7 +328,8 @@ __global__ void __launch_bounds__(kPlanThreads) plan_kernel(const PlanParams p) 
 }
 
 // The same by one CTA, for a decode step's sizes: all lengths are read before any is written by a barrier instead of a
-// count of CTAs, and nothing is read twice.
+// count of CTAs, and nothing is read twice.  Where the tokens are many (two_launches) it leaves their slots and table
+// entries to slots_kernel.
 __global__ void __launch_bounds__(kSmallThreads) plan_small_kernel(const PlanParams p) {
   extern __shared__ long long s_tok64[];      // [units + 1] new tokens before each (layer, sequence)
   const int n_units = p.n_layers * p.batch;
@@ -324,6 +337,7 @@ __global__ void __launch_bounds__(kSmallThreads) plan_small_kernel(const PlanPar
   int32_t* s_len = s_start + n_units;                                     // [units]
   __shared__ long long s_red[32], s_red2[32];
   __shared__ int s_end[32];
+  asm volatile("griddepcontrol.launch_dependents;");
   const int tid = threadIdx.x, lane = tid & 31, warp = tid >> 5;
   constexpr int kPer = kSmallUnits / kSmallThreads;
   const int per = (n_units + kSmallThreads - 1) / kSmallThreads;
@@ -383,6 +397,10 @@ __global__ void __launch_bounds__(kSmallThreads) plan_small_kernel(const PlanPar
     s_start[e] = fits ? (int)min(start, (long long)p.n_free) : -1;
     s_tok64[e] = tok;
     s_len[e] = a[i].len;
+    if (p.two_launches) {
+      p.ws_start[e] = s_start[e];
+      p.ws_len[e] = a[i].len;
+    }
     p.lens_after[e] = fits ? a[i].len + a[i].add : a[i].len;
     if (fits && pages > 0) end_max = max(end_max, (int)(start + pages));
     if (a[i].bad) record_status(p.hdr, XKV_ERR_INVALID_ARG);
@@ -417,6 +435,13 @@ __global__ void __launch_bounds__(kSmallThreads) plan_small_kernel(const PlanPar
     *p.used_after = end;
   }
   if (p.slots == nullptr) return;
+  if (p.two_launches) {
+    for (int i = tid; i < p.n_layers * (p.batch + 1); i += kSmallThreads) {
+      const int l = i / (p.batch + 1), b = i - l * (p.batch + 1);
+      p.ws_tok[i] = (int32_t)min(s_tok64[l * p.batch + b] - s_tok64[l * p.batch], 0x7fffffffll);
+    }
+    return;
+  }
   // The layers' runs, dealt out to the warps: first those that the slot maps have room for, then, where a layer has more
   // tokens than that (the status says so), the others: they still get their pages.
   const int runs = (int)((p.slots_stride + kSlotRun - 1) / kSlotRun);
@@ -437,6 +462,31 @@ __global__ void __launch_bounds__(kSmallThreads) plan_small_kernel(const PlanPar
   for (int l = warp; l < p.n_layers; l += kSmallThreads / 32)
     for (int r = runs; do_run(l, r); ++r) {
     }
+}
+
+// Slots and new table entries from what plan_small_kernel found.  grid = (slices, layers), a stretch of tokens per warp.
+__global__ void __launch_bounds__(kPlanThreads) slots_kernel(const PlanParams p) {
+  extern __shared__ int32_t s_plan[];
+  int32_t* s_tok = s_plan;                    // [batch + 1]
+  int32_t* s_start = s_plan + p.batch + 1;    // [batch]
+  int32_t* s_len = s_start + p.batch;         // [batch]
+  const int tid = threadIdx.x, layer = blockIdx.y, n_warps = gridDim.x * (kPlanThreads / 32);
+  asm volatile("griddepcontrol.wait;" ::: "memory");
+  for (int i = tid; i <= p.batch; i += kPlanThreads) {
+    s_tok[i] = __ldg(&p.ws_tok[(size_t)layer * (p.batch + 1) + i]);
+    if (i < p.batch) {
+      s_start[i] = __ldg(&p.ws_start[(size_t)layer * p.batch + i]);
+      s_len[i] = __ldg(&p.ws_len[(size_t)layer * p.batch + i]);
+    }
+  }
+  __syncthreads();
+  const int total = s_tok[p.batch], n_slots = (int)min((int64_t)total, p.slots_stride);
+  if (blockIdx.x == 0 && tid == 0 && total > p.slots_stride) record_status(p.hdr, XKV_ERR_CAPACITY);
+  const int64_t stretch = ((int64_t)total + n_warps - 1) / n_warps;
+  const int64_t t0 = (blockIdx.x * (kPlanThreads / 32) + (tid >> 5)) * stretch;
+  write_range(p, p.block_table + (size_t)layer * p.batch * p.max_pages_per_seq, p.slots + layer * p.slots_stride,
+              (int)min(t0, (int64_t)total), (int)min(t0 + stretch, (int64_t)total), n_slots,
+              [&](int b) { return s_tok[b]; }, [&](int b) { return s_start[b]; }, [&](int b) { return s_len[b]; });
 }
 
 // ---------------------------------------------------------------------------------------------
@@ -588,7 +638,9 @@ __global__ void __launch_bounds__(kStoreThreads) append_block_kernel(const Appen
 
 }  // namespace
 
-size_t plan_workspace_bytes(int n_layers, int batch) { return kHeaderBytes + align_up((size_t)n_layers * batch * 4, 256); }
+size_t plan_workspace_bytes(int n_layers, int batch) {
+  return kHeaderBytes + align_up(((size_t)n_layers * batch * 4 + n_layers) * 4, 256);
+}
 
 int plan_max_batch() { return kPlanMaxBatch; }
 
@@ -615,15 +667,47 @@ xkv_status plan_append(const xkv_cache* c, int batch, const int32_t* n_new, int 
   const uint32_t d8 = (uint32_t)c->page_size / 8;
   p.page_mul = (uint32_t)(((1ull << 32) + d8 - 1) / d8);
   p.hdr = static_cast<WorkspaceHeader*>(workspace);
+  p.two_launches = 0;
   p.new_lens = reinterpret_cast<int32_t*>(static_cast<uint8_t*>(workspace) + kHeaderBytes);
-  // One CTA where that is little work for it: 3.x us against y us for the step of a batch of 64 in 32 layers.
   const int64_t n_units = (int64_t)c->n_layers * batch;
-  if (n_units <= kSmallUnits && (slots == nullptr ? 0 : c->n_layers * slots_stride) <= kSmallTokens) {
+  p.ws_tok = p.new_lens + n_units;
+  p.ws_start = p.ws_tok + n_units + c->n_layers;
+  p.ws_len = p.ws_start + n_units;
+  const int64_t tokens = slots != nullptr ? slots_stride : 0;
+  int64_t slices = (tokens + 4 * kPlanThreads - 1) / (4 * kPlanThreads);
+  const int64_t most = std::max<int64_t>(1, 4 * (int64_t)sm_count() / c->n_layers);     // one wave
+  slices = slices < 1 ? 1 : (slices > most ? most : slices);
+  const dim3 grid((unsigned)slices, (unsigned)c->n_layers);
+  if (n_units <= kSmallUnits) {
+    // One CTA finds out who gets what; it also writes the slots where they are few.  One launch against two, device time
+    // of layers x sequences x new tokens: 4 x 1 x 1: 3.5 / 4.5 us, 32 x 8 x 1: 4.5 / 4.7, 32 x 64 x 1: 7.2 / 7.2, 32 x 64 x 4:
+    // 15.3 / 7.0, 32 x 64 x 128: 269 / 7.4.
+    p.two_launches = c->n_layers * tokens > kSmallTokens ? 1 : 0;
     const size_t small = (size_t)(n_units + 1) * 8 + (size_t)n_units * 8;
     if (small > 40 * 1024 &&
         cudaFuncSetAttribute(plan_small_kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)small) != cudaSuccess)
       return XKV_ERR_CUDA;
     plan_small_kernel<<<1, kSmallThreads, small, st>>>(p);
+    count_launch();
+    xkv_status s = check_launch();
+    if (s != XKV_OK || !p.two_launches) return s;
+    cudaLaunchConfig_t cfg = {};
+    cfg.gridDim = grid;
+    cfg.blockDim = dim3(kPlanThreads);
+    cfg.dynamicSmemBytes = (size_t)(3 * batch + 1) * 4;
+    cfg.stream = st;
+    cudaLaunchAttribute attr;                 // its CTAs are in place when the first launch ends
+    attr.id = cudaLaunchAttributeProgrammaticStreamSerialization;
+    attr.val.programmaticStreamSerializationAllowed = 1;
+    cfg.attrs = &attr;
+    cfg.numAttrs = 1;
+    if (cfg.dynamicSmemBytes > 40 * 1024 &&
+        cudaFuncSetAttribute(slots_kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)cfg.dynamicSmemBytes) != cudaSuccess)
+      return XKV_ERR_CUDA;
+    if (cudaLaunchKernelEx(&cfg, slots_kernel, p) != cudaSuccess) {
+      (void)cudaGetLastError();
+      return XKV_ERR_CUDA;
+    }
     count_launch();
     return check_launch();
   }
@@ -631,11 +715,7 @@ xkv_status plan_append(const xkv_cache* c, int batch, const int32_t* n_new, int 
   if (smem > 40 * 1024 &&
       cudaFuncSetAttribute(plan_kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)smem) != cudaSuccess)
     return XKV_ERR_CUDA;
-  const int64_t tokens = slots != nullptr ? slots_stride : 0;
-  int64_t slices = (tokens + 4 * kPlanThreads - 1) / (4 * kPlanThreads);
-  const int64_t most = std::max<int64_t>(1, 4 * (int64_t)sm_count() / c->n_layers);     // one wave
-  slices = slices < 1 ? 1 : (slices > most ? most : slices);
-  plan_kernel<<<dim3((unsigned)slices, (unsigned)c->n_layers), kPlanThreads, smem, st>>>(p);
+  plan_kernel<<<grid, kPlanThreads, smem, st>>>(p);
   count_launch();
   return check_launch();
 }
@@ -660,10 +740,12 @@ xkv_status store_rows(const xkv_dims* d, const xkv_cache* c, const void* k, cons
   p.page_size = c->page_size;
   p.hdr = static_cast<WorkspaceHeader*>(workspace);
   if (c->kv_format == XKV_KV_E4M3) {
-    // One warp per token while that leaves every SM a few dozen warps (a decode step: every token is a run of its
-    // own), else one per 16 tokens (a prompt: one run or two), so that few warps start only to find no run.
+    // A warp looks for runs among 1, 4 or 16 tokens and takes them one after the other.  Few tokens: one each (a decode
+    // step: every token is a run of its own); many: more, so that few warps start only to find no run (a prompt: one run
+    // in 16 tokens).  Measured with 1 / 4 / 16, 8 heads of 128: step of 64 tokens 2.9 / 6.3 / 19.6 us, of 600 7.7 / 8.4 / 20.5, of
+    // 4000 37 / 31 / 36; prompts of 1000 tokens 5.8 / 4.1 / 3.0 us, of 4 x 2048 26.0 / 12.3 / 7.4.
     const int64_t jobs = n_tokens * 2 * d->n_kv_heads;
-    p.tokens_per_warp = jobs <= 64 * (int64_t)sm_count() ? 1 : kScaleBlock;
+    p.tokens_per_warp = jobs <= 64 * (int64_t)sm_count() ? 1 : (jobs <= 448 * (int64_t)sm_count() ? 4 : kScaleBlock);
     const int64_t warps = (n_tokens + p.tokens_per_warp - 1) / p.tokens_per_warp * 2 * d->n_kv_heads;
     const int64_t grid = (warps + kStoreThreads / 32 - 1) / (kStoreThreads / 32);
     if (grid > 0x7fffffffll) return XKV_ERR_UNSUPPORTED;

@@ -310,6 +310,26 @@ def test_decode_append_beyond_the_page_table():
     check_all(pool, 1, q, out, lse, [[32, 32, 6]], what="full")
 
 
+def test_decode_two_calls_at_once():
+    """Two streams, a workspace each."""
+    pool = Pool(np.random.default_rng(3).integers(1, 2500, (2, 6)), 2, 128, 16, seed=21)
+    qs = [queries(2, 6, 8, 128, 30 + i) for i in range(2)]
+    want = [run_decode(pool, 8, q)[:2] for q in qs]
+    dims = xkv.Dims(6, 8, 2, 128, 1, 1, 0, 0.0, 256, 128)
+    nbytes = xkv.workspace_bytes(xkv.OP_DECODE_ATTN, dims, n_layers=2, max_cache_len=pool.cols * 16)
+    ws = [torch.zeros(nbytes, dtype=torch.uint8, device=DEV) for _ in qs]
+    outs = [torch.empty_like(want[0][0]) for _ in qs]
+    streams = [torch.cuda.Stream(device=DEV) for _ in qs]
+    handle = pool.handle()
+    torch.cuda.synchronize()
+    for _ in range(20):
+        for q, w, o, s in zip(qs, ws, outs, streams):
+            xkv.decode_attn(dims, handle, 0, 2, q, None, None, o, None, 0, w, stream=s)
+    torch.cuda.synchronize()
+    for o, w, (ref, _) in zip(outs, ws, want):
+        assert xkv.read_device_status(w) == xkv.OK and torch.equal(o, ref)
+
+
 def test_decode_waits_that_expire():
     """One CTA's copies are never issued: its waits run out after a millisecond, the launch returns and says so, and
     workspace and cache stay usable."""
@@ -379,16 +399,16 @@ def expect_store(pool, x, rows, slots):
         while i + n < len(slots) and slots[i + n] == s + n and (s + n) % 16:
             n += 1
         pg, sub, first = s // page, (s % page) // 16, s % 16
-        for g in range(pool.H):
-            new = rows[i:i + n, g]
-            sc = O.e4m3_block_scale(new)
-            lo = sub * 16
-            if first:
-                was = scales[pg, g, sub]
-                sc = max(sc, was)
-                codes[pg, g, lo:lo + first] = O.e4m3_grid(codes[pg, g, lo:lo + first] * (was / sc))
-            scales[pg, g, sub] = sc
-            codes[pg, g, lo + first:lo + first + n] = O.e4m3_grid(new / sc)
+        new, lo = rows[i:i + n].transpose(1, 0, 2), sub * 16                     # [H, n, d]
+        top = np.where(np.isfinite(new), np.abs(new), 0).max((1, 2))
+        m, e = np.frexp(top)                                                     # top = m 2^e, 448 = 0.875 2^9
+        sc = np.where(top > 0, np.ldexp(1.0, np.clip(np.where(m <= 0.875, e - 9, e - 8), -100, 120)), 2.0 ** -100)
+        if first:
+            was = scales[pg, :, sub]
+            sc = np.where(was >= sc, was, sc)
+            codes[pg, :, lo:lo + first] = O.e4m3_grid(codes[pg, :, lo:lo + first] * (was / sc)[:, None, None])
+        scales[pg, :, sub] = sc
+        codes[pg, :, lo + first:lo + first + n] = O.e4m3_grid(new / sc[:, None, None])
         i += n
     return codes, scales
 
@@ -403,6 +423,9 @@ def same(a, b):
     (128, 8, 64, [0, 0, 0], [700, 1, 64]),
     (64, 1, 256, [3, 260, 15], [512, 0, 2]),
     (128, 1, 112, [111], [2000]),
+    (128, 8, 16, [7, 0], [4300, 333]),                       # many tokens: a warp looks for runs among sixteen
+    (64, 8, 32, [i % 37 for i in range(720)], [1] * 720),    # a step of many sequences: among four
+    (64, 16, 16, [i % 29 for i in range(2400)], [1] * 2400),  # of more: among sixteen
 ])
 @pytest.mark.parametrize("pad", [0, 37])
 def test_store_rows(d, H, page, lens, new, pad):
@@ -530,7 +553,8 @@ def check_plan(want, bt, after, slots, used):
 
 
 @pytest.mark.parametrize("L,B,page,hi,new_hi", [(1, 1, 16, 0, 1), (4, 3, 16, 50, 1), (3, 7, 48, 200, 90), (2, 600, 32, 64, 33),
-                                                (32, 64, 16, 700, 1), (5, 2, 256, 3000, 5000)])
+                                                (32, 64, 16, 700, 1), (5, 2, 256, 3000, 5000),
+                                                (3, 1500, 16, 40, 3), (2, 2100, 48, 100, 60)])
 @pytest.mark.parametrize("per_layer", [False, True])
 def test_plan_append(L, B, page, hi, new_hi, per_layer):
     rng = np.random.default_rng(L * B + page)
