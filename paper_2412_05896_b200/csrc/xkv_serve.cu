@@ -69,7 +69,7 @@ struct Ask {
 // e = l * batch + b
 __device__ __forceinline__ Ask plan_ask(const PlanParams& p, int l, int e, int b) {
   Ask a;
-  const int len = p.lens_before != nullptr ? __ldg(&p.lens_before[e]) : 0;
+  const int len = p.lens_before != nullptr ? p.lens_before[e] : 0;      // (not through the read-only path: may be seq_lens)
   const int add = __ldg(&p.n_new[l * p.n_new_stride + b]);
   a.bad = len < 0 || add < 0;
   a.len = max(len, 0);
@@ -212,7 +212,7 @@ __global__ void __launch_bounds__(kPlanThreads) plan_kernel(const PlanParams p) 
   const int tid = threadIdx.x, lane = tid & 31, warp = tid >> 5;
   constexpr int kWarps = kPlanThreads / 32;
   const int layer = blockIdx.y, slice = blockIdx.x, n_slices = gridDim.x;
-  int used = p.used_before != nullptr ? __ldg(p.used_before) : 0;
+  int used = p.used_before != nullptr ? *p.used_before : 0;
   if (used < 0 || used > p.n_free) {
     if (tid == 0) record_status(p.hdr, XKV_ERR_INVALID_ARG);
     used = p.n_free;                          // nothing can be handed out
@@ -300,7 +300,7 @@ __global__ void __launch_bounds__(kPlanThreads) plan_kernel(const PlanParams p) 
     const int64_t t0 = (slice * kWarps + warp) * stretch;
     write_range(p, table, out, (int)min(t0, (int64_t)total), (int)min(t0 + stretch, (int64_t)total), n_slots,
                 [&](int b) { return s_tok[b]; }, [&](int b) { return s_start[b]; },
-                [&](int b) { return lens != nullptr ? max(__ldg(&lens[b]), 0) : 0; });
+                [&](int b) { return lens != nullptr ? max(lens[b], 0) : 0; });
   } else {
     // ---- the new table entries: a warp per sequence
     for (int b = slice * kWarps + warp; b < p.batch; b += n_slices * kWarps) {
@@ -341,7 +341,7 @@ __global__ void __launch_bounds__(kSmallThreads) plan_small_kernel(const PlanPar
   const int tid = threadIdx.x, lane = tid & 31, warp = tid >> 5;
   constexpr int kPer = kSmallUnits / kSmallThreads;
   const int per = (n_units + kSmallThreads - 1) / kSmallThreads;
-  int used = p.used_before != nullptr ? __ldg(p.used_before) : 0;
+  int used = p.used_before != nullptr ? *p.used_before : 0;
   Ask a[kPer];
   long long ask = 0, add = 0;
 #pragma unroll

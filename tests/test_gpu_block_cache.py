@@ -31,7 +31,7 @@ class Pool:
     """A page pool of block-scaled 8-bit floats filled by numpy (not by the library): random codes and power-of-two
     scales, pages of every (layer, sequence) in shuffled order, NaN codes and NaN scales behind the last row."""
 
-    def __init__(self, lens, H, d, page, seed=0, spare_rows=0, spread=3, big_k_row=None):
+    def __init__(self, lens, H, d, page, seed=0, spare_rows=0, spread=3, big_k_row=None, any_code=False):
         self.lens = np.asarray(lens, dtype=np.int64)
         L, B = self.lens.shape
         rng = np.random.default_rng(seed)
@@ -42,8 +42,11 @@ class Pool:
         nb = page // O.SCALE_BLOCK
         self.codes, self.scales = {}, {}
         for x in "kv":
-            c = O.e4m3_grid(rng.normal(0, 60, (self.n_pages, H, page, d)))
-            sign_mag = self._bytes(c)
+            if any_code:                                 # every finite code alike
+                sign_mag = rng.integers(0, 0x7F, (self.n_pages, H, page, d), dtype=np.uint8)
+                sign_mag |= rng.integers(0, 2, sign_mag.shape, dtype=np.uint8) << 7
+            else:
+                sign_mag = self._bytes(O.e4m3_grid(rng.normal(0, 60, (self.n_pages, H, page, d))))
             s = 2.0 ** rng.integers(-7 - spread, -6 + spread, (self.n_pages, H, nb))
             for l in range(L):
                 for b in range(B):
@@ -200,6 +203,24 @@ def test_decode_small_weights_of_many_rows_count():
     out, lse, st = run_decode(pool, 2, q)
     assert st == xkv.OK
     check_all(pool, 2, q, out, lse, pool.lens, what="sink")
+
+
+def test_decode_nothing_cached():
+    pool = Pool([[0, 0], [0, 0]], 2, 64, 16, seed=1)
+    q = queries(2, 2, 6, 64, 1)
+    out, lse, st = run_decode(pool, 6, q)
+    assert st == xkv.OK
+    check_all(pool, 6, q, out, lse, pool.lens, what="empty")
+
+
+def test_decode_bad_pages():
+    """Table entries outside the pool are read as its nearest page: no fault, and the other sequences are untouched."""
+    pool = Pool([[40, 300, 77]], 2, 128, 16, seed=17)
+    q = queries(1, 3, 8, 128, 17)
+    want, _, _ = run_decode(pool, 8, q)
+    pool.bt[0, 1, 3], pool.bt[0, 1, 5] = -7, 1 << 30
+    got, _, st = run_decode(pool, 8, q)
+    assert st == xkv.OK and torch.equal(got[0, 0], want[0, 0]) and torch.equal(got[0, 2], want[0, 2])
 
 
 def test_decode_extreme_scales_and_queries():
@@ -430,7 +451,7 @@ def same(a, b):
 @pytest.mark.parametrize("pad", [0, 37])
 def test_store_rows(d, H, page, lens, new, pad):
     lens, new = np.asarray(lens), np.asarray(new)
-    pool = Pool([lens], H, d, page, seed=len(lens) + pad, spare_rows=int(new.max()))
+    pool = Pool([lens], H, d, page, seed=len(lens) + pad, spare_rows=int(new.max()), any_code=True)
     slots = np.concatenate([pool.table[0, b, (n + np.arange(a)) // page] * page + (n + np.arange(a)) % page
                             for b, (n, a) in enumerate(zip(lens, new))] + [np.full(pad, -1)]).astype(np.int64)
     T = len(slots)
