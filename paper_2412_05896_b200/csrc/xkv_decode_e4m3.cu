@@ -399,6 +399,7 @@ decode_e4m3_kernel(const __grid_constant__ CUtensorMap tmap_k, const __grid_cons
   __shared__ float s_sum[2][4][8];
   __shared__ int s_scan[kThreads / 32];
   __shared__ int4 s_first;                        // the unit in which the share begins: unit, rows, where it begins on the line
+  __shared__ int4 s_end_cut;                      // the cache that the share's end cuts: unit, KV head, where it begins, rows
   __shared__ uint32_t s_tmem;
   __shared__ int s_abort_store;
   __shared__ Joins s_joins;
@@ -471,17 +472,22 @@ decode_e4m3_kernel(const __grid_constant__ CUtensorMap tmap_k, const __grid_cons
   const Cut share(line, n_ctas);
   const bool works = (int)blockIdx.x < n_ctas && line > 0;
   const int begin = works ? share.begin(blockIdx.x) : 0, stop_at = works ? share.begin(blockIdx.x + 1) : 0;
-  if (works && before * Hkv <= begin && begin < (before + mine) * Hkv) {
-    int at = before * Hkv;                        // this thread's run of units holds the begin of the share
+  const int my_begin = before * Hkv, my_end = (before + mine) * Hkv;
+  if (works && my_begin < my_end && ((my_begin <= begin && begin < my_end) || (my_begin <= stop_at && stop_at < my_end))) {
+    int at = my_begin;                            // this thread's run of units holds the begin or the end of the share
     for (int i = 0; i < per; ++i) {
-      const int e = tid * per + i, rows = e < p.n_units ? unit_rows(p, e) : 0, next = at + cost_of(rows) * Hkv;
-      if (begin < next) {
-        s_first = make_int4(e, rows, at, 0);
-        break;
+      const int e = tid * per + i, rows = e < p.n_units ? unit_rows(p, e) : 0, cost = cost_of(rows), next = at + cost * Hkv;
+      if (at <= begin && begin < next) s_first = make_int4(e, rows, at, 0);
+      if (at <= stop_at && stop_at < next) {
+        const int h = quotient(stop_at - at, cost), g0 = at + h * cost;
+        // cut: some of its tiles start before the end, others behind it (and none in the piece that the begin cuts)
+        const bool cut = g0 > begin && g0 < stop_at && stop_at - g0 <= (tiles_of(rows) - 1) * kTileBlocks;
+        s_end_cut = make_int4(e, h, g0, cut ? rows : 0);
       }
       at = next;
     }
   }
+  if (tid == 0 && (!works || stop_at >= line)) s_end_cut = make_int4(0, 0, 0, 0);
   __syncthreads();
   const uint32_t tmem = s_tmem;
 
@@ -506,6 +512,11 @@ decode_e4m3_kernel(const __grid_constant__ CUtensorMap tmap_k, const __grid_cons
       const int cost = cost_of(s_first.y), off = begin - s_first.z;
       guess.row0 = (off - quotient(off, cost) * cost + kTileBlocks - 1) / kTileBlocks * kTile;
       guess.rows = s_first.y - guess.row0;
+      if (s_end_cut.w > 0) {
+        guess.e = s_end_cut.x;
+        guess.row0 = 0;
+        guess.rows = s_end_cut.w;
+      }
     }
     const int guess_pages = load_pages(guess, 0);
     int nxt_pages = 0;
@@ -650,10 +661,24 @@ decode_e4m3_kernel(const __grid_constant__ CUtensorMap tmap_k, const __grid_cons
     int at = begin;                               // next position of the share
     int e = s_first.x, rows = s_first.y, unit_at = s_first.z;      // unit_at: where (e, head 0) begins
     int cost = cost_of(rows), h = works ? quotient(begin - unit_at, cost) : 0;
-    // The next piece: the tiles of (e, h) that start in [at, stop_at).
+    // The piece that the end of the share cuts comes first, then the one that its begin cuts, then the whole caches: counting
+    // and joining pieces takes microseconds, which then lie under the copies of what follows.
+    const int walk_end = s_end_cut.w > 0 ? s_end_cut.z : stop_at;
+    bool end_first = s_end_cut.w > 0;
+    // The next piece: the tiles of (e, h) that start in [at, walk_end).
     auto next_item = [&]() -> Item {
       Item it = {-1, 0, 0, 0, 0, 0};
-      while (at < stop_at) {
+      if (end_first) {
+        end_first = false;
+        const int g0 = s_end_cut.z;
+        it.e = s_end_cut.x;
+        it.h = s_end_cut.y;
+        it.rows = (stop_at - g0 + kTileBlocks - 1) / kTileBlocks * kTile;
+        it.first_cta = (int)blockIdx.x;
+        it.n_pieces = share.part_of(g0 + (tiles_of(s_end_cut.w) - 1) * kTileBlocks) - it.first_cta + 1;
+        return it;
+      }
+      while (at < walk_end) {
         while (h == Hkv || rows == 0) {           // on to the next cache that holds rows
           unit_at += cost * Hkv;
           ++e;
@@ -664,9 +689,9 @@ decode_e4m3_kernel(const __grid_constant__ CUtensorMap tmap_k, const __grid_cons
         }
         const int g0 = unit_at + h * cost, nt = tiles_of(rows);
         const int t0 = (at - g0 + kTileBlocks - 1) / kTileBlocks;                       // first tile that starts at or behind `at`
-        const int t1 = min(nt, (min(stop_at, g0 + cost) - g0 + kTileBlocks - 1) / kTileBlocks);   // first one behind the piece
+        const int t1 = min(nt, (min(walk_end, g0 + cost) - g0 + kTileBlocks - 1) / kTileBlocks);   // first one behind the piece
         const int this_h = h;
-        at = min(stop_at, g0 + cost);
+        at = min(walk_end, g0 + cost);
         if (at == g0 + cost) ++h;
         if (t0 >= t1) continue;                   // no tile starts here
         it.e = e;
