@@ -20,12 +20,18 @@
 // the CTA that finishes the last piece joins them in the order of the pieces, so the result does not depend on who
 // was when.  (Small segments at the ends of the shares that go to whoever is done first level the finishing times, but
 // what they add in pieces and joins costs more: 74.6 against 70.2 us for 363 MB, 150.8 against 140.2 us for 814 MB.)
+// Bound by HBM where caches are long, else by what a launch costs before the first and after the last byte (about 8 us: the
+// lengths, page ids and first tiles one after the other; the last tile's softmax, output, count and join).  Measured, device
+// time a call: 538 MB in two caches of 131 000 rows x 8 heads 93.3 us (0.88 of the measured copy rate; 7.4 TB/s between
+// the first tile and the last), 814 MB ragged batch 134.5 us (0.92), 363 MB of 2048 short caches 64.3 us (0.86), one request
+// of 2129 rows 12.7 us.
+//
 //   warp 6     finds the CTA's pieces of caches ("items") and lays out their queries as two codes per element
 //   warp 4     copies: TMA boxes of K and V, block scales
 //   warp 5     issues the MMAs: logits up to two tiles ahead of the outputs
 //   warps 0-3  one thread per cache row: logits out of tensor memory, the tile's maximum (one exchange among the four
 //              warps), weights back as codes; then, as one thread per output column, O of the tile before
-//   warp 7     counts finished pieces of cut caches and joins those that are complete, one query head at a time; warps that
+//   warp 7     counts finished pieces of cut caches and joins those that are complete, by query heads; warps that
 //              have run out of tiles help
 #include <cuda.h>
 
@@ -58,8 +64,8 @@ constexpr int kCtasPerSm = 2;
 constexpr float kPart = 32.f;         // weight of the second code
 constexpr int kBarSoft = 1;           // named barrier of warps 0-3
 constexpr int kTileBlocks = kTile / kScaleBlock;
-constexpr int kCacheCost = 8;         // what a cache costs besides its bytes, in blocks of 16 rows (4: 70.3 us, 8: 68.8 us, 16:
-                                      // 70.5 us for 2048 caches of 203 to 1101 rows)
+constexpr int kCacheCost = 12;        // what a cache costs besides its bytes, in blocks of 16 rows (2048 caches of 203 to 1101 rows:
+                                      // 66.6 us with 4, 64.9 with 8, 64.2 with 12, 64.9 with 16)
 constexpr int kMinSegment = 8;        // shortest segment, in blocks: a tile, so that a cache has a tile in every segment
                                       // between its first and its last one
 constexpr int kJobs = 32;             // joins a CTA may have open
@@ -271,7 +277,7 @@ __device__ __forceinline__ int tiles_of(int rows) { return (rows + kTile - 1) / 
 // length of a cache on the line
 __device__ __forceinline__ int cost_of(int rows) { return rows > 0 ? (rows + kScaleBlock - 1) / kScaleBlock + kCacheCost : 0; }
 
-// Caches that this CTA has found complete and is to join, one query head at a time.
+// Caches that this CTA has found complete and is to join.
 struct Joins {
   int4 job[kJobs];                    // {unit, KV head, first CTA, pieces}
   int n_jobs, claimed, joined;        // jobs so far, heads claimed and heads joined

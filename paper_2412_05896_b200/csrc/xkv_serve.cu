@@ -4,8 +4,8 @@
 //                       lengths; for a decode step's few tokens also their slots and table entries
 //   slots_kernel        slots and table entries of many tokens, from what plan_small_kernel found (programmatic dependent
 //                       launch): a stretch of tokens per warp, the page ids of eight rounds in flight together.  Bound by
-//                       its 8 bytes written per layer and token (84 MB of 64 prompts in 32 layers: 27 us, 3.1 TB/s, of
-//                       which about 7 us are the first launch) and the dozen instructions that make one.
+//                       its 8 bytes written per layer and token and by the instructions that make them: 64 prompts in 32
+//                       layers, 84 MB: 25.7 us, of which about 7 us are the first launch (a plain fill takes 13 us)
 //   plan_kernel         more caches than that, in one launch: grid = (slices, layers), no CTA waits for another one: each
 //                       forms the pages asked for by the layers before its own and the scan over its layer's sequences by
 //                       itself (integers out of L2), and the last CTA to leave writes the lengths, so that they may
@@ -96,34 +96,45 @@ __device__ __forceinline__ int free_page(const PlanParams& p, int at) {
 
 constexpr int kRounds = 8;                    // tokens a lane takes at a time
 
-// The tokens [t, end) of one sequence, all in new pages.  Row `x + shift` of the sequence is token x; id(i): its page i.
+// 32 * kRounds tokens from t on, or those of them before `end` (kAll: all), of one sequence and in new pages.  Row `x +
+// shift` of the sequence is token x; id(i): its page i.
+template <bool kAll, class Id>
+__device__ __forceinline__ void write_batch(const PlanParams& p, int32_t* row, int64_t* out, int t, int end, int shift, Id id) {
+  const int lane = threadIdx.x & 31;
+  const int pos0 = t + lane + shift, n = end - t - lane;          // rounds 32 k < n of this lane hold a token
+  int64_t* dst = out + t + lane;
+  int page[kRounds];
+  uint32_t top = 0;
+#pragma unroll
+  for (int k = 0; k < kRounds; ++k) page[k] = id(p.page_of(kAll || 32 * k < n ? pos0 + 32 * k : end - 1 + shift));
+#pragma unroll
+  for (int k = 0; k < kRounds; ++k) top = max(top, (uint32_t)page[k]);
+  if (top >= (uint32_t)p.n_pages) {                               // an id outside the pool: no slot
+    record_status(p.hdr, XKV_ERR_INVALID_ARG);
+#pragma unroll 1
+    for (int k = 0; k < kRounds && 32 * k < n; ++k) {
+      const int i = p.page_of(pos0 + 32 * k), in_page = pos0 + 32 * k - i * p.page_size, pg = id(i);
+      dst[32 * k] = (uint32_t)pg < (uint32_t)p.n_pages ? (int64_t)pg * p.page_size + in_page : -1;
+      if (in_page == 0) row[i] = pg;
+    }
+    return;
+  }
+#pragma unroll
+  for (int k = 0; k < kRounds; ++k) {
+    const int i = p.page_of(pos0 + 32 * k), in_page = pos0 + 32 * k - i * p.page_size;
+    if (kAll || 32 * k < n) {
+      dst[32 * k] = (int64_t)page[k] * p.page_size + in_page;
+      if (in_page == 0) row[i] = page[k];
+    }
+  }
+}
+
 template <class Id>
 __device__ __forceinline__ void write_stretch(const PlanParams& p, int32_t* row, int64_t* out, int t, int end, int shift,
                                               Id id) {
-  const int lane = threadIdx.x & 31;
 #pragma unroll 1
-  for (; t < end; t += 32 * kRounds) {
-    const int pos0 = t + lane + shift, n = end - t - lane;        // rounds 32 k < n of this lane hold a token
-    int64_t* dst = out + t + lane;
-    int page[kRounds];
-    uint32_t top = 0;
-#pragma unroll
-    for (int k = 0; k < kRounds; ++k) page[k] = id(p.page_of(32 * k < n ? pos0 + 32 * k : end - 1 + shift));
-#pragma unroll
-    for (int k = 0; k < kRounds; ++k) {
-      const int i = p.page_of(pos0 + 32 * k), in_page = pos0 + 32 * k - i * p.page_size;
-      top = max(top, (uint32_t)page[k]);
-      if (32 * k < n) {
-        dst[32 * k] = (int64_t)page[k] * p.page_size + in_page;
-        if (in_page == 0) row[i] = page[k];
-      }
-    }
-    if (top >= (uint32_t)p.n_pages) {                       // an id outside the pool: no slot
-      record_status(p.hdr, XKV_ERR_INVALID_ARG);
-      for (int k = 0; k < kRounds && 32 * k < n; ++k)
-        if ((uint32_t)id(p.page_of(pos0 + 32 * k)) >= (uint32_t)p.n_pages) dst[32 * k] = -1;
-    }
-  }
+  for (; t + 32 * kRounds <= end; t += 32 * kRounds) write_batch<true>(p, row, out, t, end, shift, id);
+  if (t < end) write_batch<false>(p, row, out, t, end, shift, id);
 }
 
 // The new tokens [t, t_end) of a layer (a whole warp): their slots, and the table entries of the pages that begin with one
