@@ -31,7 +31,8 @@ constexpr int kPlanThreads = 256;
 constexpr int kSmallThreads = 1024;           // one CTA plans up to kSmallUnits sequences of all layers
 constexpr int kSmallUnits = 4096;
 constexpr int kSlotRun = 64;                  // ... and hands its tokens to its warps in runs of so many
-constexpr int64_t kSmallTokens = 1024;        // ... where they are no more than this (by the slot maps' sizes)
+constexpr int64_t kSmallTokens = 4096;        // ... where they are no more than this (by the slot maps' sizes)
+constexpr int kStepTokens = 2;                // ... unless no cache takes more than so many: then by its threads
 constexpr int kPlanMaxBatch = 16384;          // sequences of a layer: two 4-byte table entries each in shared memory
 
 struct PlanParams {
@@ -439,13 +440,51 @@ __global__ void __launch_bounds__(kSmallThreads) plan_small_kernel(const PlanPar
       }
     }
   }
-  __syncthreads();
+  bool few = true;                            // no cache takes more than kStepTokens
+#pragma unroll
+  for (int i = 0; i < kPer; ++i) few = few && a[i].add <= kStepTokens;
+  few = __syncthreads_and(few) != 0;
   if (tid == 0 && p.used_after != nullptr) {
     int end = s_end[0];
     for (int w = 1; w < 32; ++w) end = max(end, s_end[w]);
     *p.used_after = end;
   }
   if (p.slots == nullptr) return;
+  if (few && !p.two_launches) {
+    // a decode step: every thread the tokens of its own caches, all page ids in flight together
+    int page[kPer][kStepTokens];
+#pragma unroll
+    for (int i = 0; i < kPer; ++i) {
+      const int e = tid * per + i, st = i < per && e < n_units ? s_start[e] : -1;
+      const int have = p.page_of(a[i].len + p.page_size - 1);
+#pragma unroll
+      for (int k = 0; k < kStepTokens; ++k) {
+        page[i][k] = -1;
+        if (st < 0 || k >= a[i].add) continue;
+        const int at = p.page_of(a[i].len + k);
+        page[i][k] = at < have ? p.block_table[(size_t)e * p.max_pages_per_seq + at] : free_page(p, st + at - have);
+      }
+    }
+#pragma unroll
+    for (int i = 0; i < kPer; ++i) {
+      const int e = tid * per + i;
+      if (i >= per || e >= n_units) break;
+      const int l = e / p.batch, st = s_start[e];
+      const long long first = s_tok64[e] - s_tok64[l * p.batch];
+      if (e - l * p.batch == p.batch - 1 && first + a[i].add > p.slots_stride) record_status(p.hdr, XKV_ERR_CAPACITY);
+#pragma unroll
+      for (int k = 0; k < kStepTokens; ++k) {
+        if (k >= a[i].add) break;
+        const int pos = a[i].len + k, at = p.page_of(pos), in_page = pos - at * p.page_size;
+        const bool ok = (unsigned)page[i][k] < (unsigned)p.n_pages;
+        if (st >= 0 && in_page == 0) p.block_table[(size_t)e * p.max_pages_per_seq + at] = page[i][k];   // the page is new
+        if (st >= 0 && !ok) record_status(p.hdr, XKV_ERR_INVALID_ARG);
+        if (first + k < p.slots_stride)
+          p.slots[l * p.slots_stride + first + k] = ok ? (int64_t)page[i][k] * p.page_size + in_page : -1;
+      }
+    }
+    return;
+  }
   if (p.two_launches) {
     for (int i = tid; i < p.n_layers * (p.batch + 1); i += kSmallThreads) {
       const int l = i / (p.batch + 1), b = i - l * (p.batch + 1);
@@ -691,8 +730,8 @@ xkv_status plan_append(const xkv_cache* c, int batch, const int32_t* n_new, int 
   const dim3 grid((unsigned)slices, (unsigned)c->n_layers);
   if (n_units <= kSmallUnits) {
     // One CTA finds out who gets what; it also writes the slots where they are few.  One launch against two, device time
-    // of layers x sequences x new tokens: 4 x 1 x 1: 3.5 / 4.5 us, 32 x 8 x 1: 4.5 / 4.7, 32 x 64 x 1: 7.2 / 7.2, 32 x 64 x 4:
-    // 15.3 / 7.0, 32 x 64 x 128: 269 / 7.4.
+    // of layers x sequences x new tokens: steps 4 x 1 x 1: 3.2 / 4.3 us, 32 x 8 x 1: 3.3 / 4.7, 32 x 64 x 1: 5.5 / 7.0, 32 x 120 x 1:
+    // 9.1 / 10.1; more tokens a cache 4 x 1 x 300: 4.2 / 4.5, 32 x 4 x 16: 5.0 / 4.5, 4 x 1 x 1000: 6.5 / 4.7, 32 x 64 x 4: 15.2 / 6.8.
     p.two_launches = c->n_layers * tokens > kSmallTokens ? 1 : 0;
     const size_t small = (size_t)(n_units + 1) * 8 + (size_t)n_units * 8;
     if (small > 40 * 1024 &&
