@@ -212,6 +212,33 @@ __device__ __forceinline__ float warp_max(float x) {
   asm volatile("redux.sync.max.f32 %0, %1, 0xffffffff;" : "=f"(r) : "f"(x));
   return r;
 }
+// A value per head to and from shared memory (16-byte aligned), in as few accesses as there are.
+template <int GP>
+__device__ __forceinline__ void put_heads(float* dst, const float (&v)[GP]) {
+  if constexpr (GP >= 4) {
+#pragma unroll
+    for (int g = 0; g < GP; g += 4) *reinterpret_cast<float4*>(dst + g) = make_float4(v[g], v[g + 1], v[g + 2], v[g + 3]);
+  } else if constexpr (GP == 2) {
+    *reinterpret_cast<float2*>(dst) = make_float2(v[0], v[1]);
+  } else {
+    dst[0] = v[0];
+  }
+}
+template <int GP>
+__device__ __forceinline__ void get_heads(const float* src, float (&v)[GP]) {
+  if constexpr (GP >= 4) {
+#pragma unroll
+    for (int g = 0; g < GP; g += 4) {
+      const float4 x = *reinterpret_cast<const float4*>(src + g);
+      v[g] = x.x, v[g + 1] = x.y, v[g + 2] = x.z, v[g + 3] = x.w;
+    }
+  } else if constexpr (GP == 2) {
+    const float2 x = *reinterpret_cast<const float2*>(src);
+    v[0] = x.x, v[1] = x.y;
+  } else {
+    v[0] = src[0];
+  }
+}
 // Barrier of the four softmax warps that also tells whether any of its threads passed a true predicate.
 __device__ __forceinline__ bool soft_any(bool x) {
   uint32_t r;
@@ -349,10 +376,11 @@ __device__ __forceinline__ void join_heads(const Params& p, const int4 job, int 
   for (int x = 0; x < kHeads; ++x) {
     if (g + x >= G) break;
     const size_t row = (size_t)job.x * p.n_q_heads + (size_t)job.y * G + g + x;
+    const float inv = __frcp_rn(den[x]);
 #pragma unroll
     for (int c = 0; c < kCols; c += 2)
-      *reinterpret_cast<uint32_t*>(p.out + row * D + lane * kCols + c) = pack_bf16(o[x][c] / den[x], o[x][c + 1] / den[x]);
-    if (lane == 0 && p.lse != nullptr) p.lse[row] = (mx[x] + log2f(den[x])) * 0.6931471805599453f;
+      *reinterpret_cast<uint32_t*>(p.out + row * D + lane * kCols + c) = pack_bf16(o[x][c] * inv, o[x][c + 1] * inv);
+    if (lane == 0 && p.lse != nullptr) p.lse[row] = (mx[x] + __log2f(den[x])) * 0.6931471805599453f;
   }
 }
 
@@ -401,8 +429,8 @@ decode_e4m3_kernel(const __grid_constant__ CUtensorMap tmap_k, const __grid_cons
       s_q_full[kFifo], s_done_full[kFifo], s_wake;
   __shared__ Item s_item[kFifo];
   __shared__ float s_qscale[kFifo][8];
-  __shared__ float s_max[2][4][8];
-  __shared__ float s_sum[2][4][8];
+  __shared__ __align__(16) float s_max[2][4][8];
+  __shared__ __align__(16) float s_sum[2][16];    // reciprocal denominators, or (one or two heads) the warps' sums from [8] on
   __shared__ int s_scan[kThreads / 32];
   __shared__ int4 s_first;                        // the unit in which the share begins: unit, rows, where it begins on the line
   __shared__ int4 s_end_cut;                      // the cache that the share's end cuts: unit, KV head, where it begins, rows
@@ -453,6 +481,7 @@ decode_e4m3_kernel(const __grid_constant__ CUtensorMap tmap_k, const __grid_cons
     tmem_relinquish();
   }
   // operand rows that no head fills stay zero
+#pragma unroll 1
   for (int i = tid; i < (kFifo * C::kQBytes + 2 * C::kPBytes) / 16; i += kThreads)
     reinterpret_cast<uint4*>(smem + C::kOffQ)[i] = make_uint4(0u, 0u, 0u, 0u);
   fence_proxy_async_smem();
@@ -481,6 +510,7 @@ decode_e4m3_kernel(const __grid_constant__ CUtensorMap tmap_k, const __grid_cons
   const int my_begin = before * Hkv, my_end = (before + mine) * Hkv;
   if (works && my_begin < my_end && ((my_begin <= begin && begin < my_end) || (my_begin <= stop_at && stop_at < my_end))) {
     int at = my_begin;                            // this thread's run of units holds the begin or the end of the share
+#pragma unroll 1
     for (int i = 0; i < per; ++i) {
       const int e = tid * per + i, rows = e < p.n_units ? unit_rows(p, e) : 0, cost = cost_of(rows), next = at + cost * Hkv;
       if (at <= begin && begin < next) s_first = make_int4(e, rows, at, 0);
@@ -527,6 +557,7 @@ decode_e4m3_kernel(const __grid_constant__ CUtensorMap tmap_k, const __grid_cons
     const int guess_pages = load_pages(guess, 0);
     int nxt_pages = 0;
     bool have_next = false, ok = true;
+#pragma unroll 1
     for (uint32_t n_item = 0; ok; ++n_item) {
       const int slot = n_item % kFifo;
       if (!have_next) {
@@ -540,6 +571,7 @@ decode_e4m3_kernel(const __grid_constant__ CUtensorMap tmap_k, const __grid_cons
       int pages = nxt_pages, ahead = 0;
       have_next = false;
       const int n_tiles = tiles_of(cur.rows);
+#pragma unroll 1
       for (int t = 0; t < n_tiles; ++t, ++j) {
         const int box0 = t * boxes_per_tile;
         if ((box0 & 31) == 0) {                   // a new batch of page ids; the next one is on its way meanwhile
@@ -604,6 +636,7 @@ decode_e4m3_kernel(const __grid_constant__ CUtensorMap tmap_k, const __grid_cons
     int slot = 0, t = 0, n_tiles = 0, last_rows = 0;   // of the logits
     int rows0 = kTile, rows1 = kTile;             // rows of the even and the odd tile between the two products
     bool more = true;
+#pragma unroll 1
     while (true) {
       if (more && js - jo < 2) {
         if (t == n_tiles) {                       // next item
@@ -684,7 +717,9 @@ decode_e4m3_kernel(const __grid_constant__ CUtensorMap tmap_k, const __grid_cons
         it.n_pieces = share.part_of(g0 + (tiles_of(s_end_cut.w) - 1) * kTileBlocks) - it.first_cta + 1;
         return it;
       }
+#pragma unroll 1
       while (at < walk_end) {
+#pragma unroll 1
         while (h == Hkv || rows == 0) {           // on to the next cache that holds rows
           unit_at += cost * Hkv;
           ++e;
@@ -711,7 +746,7 @@ decode_e4m3_kernel(const __grid_constant__ CUtensorMap tmap_k, const __grid_cons
       }
       return it;
     };
-    constexpr int kCols = D / 32;
+#pragma unroll 1
     for (uint32_t n_item = 0;; ++n_item) {
       const int slot = n_item % kFifo;
       const Item it = next_item();
@@ -723,41 +758,52 @@ decode_e4m3_kernel(const __grid_constant__ CUtensorMap tmap_k, const __grid_cons
         mbar_arrive(&s_fifo_full[slot]);
       }
       if (it.e < 0) break;
-      const __nv_bfloat16* q = p.q + ((size_t)it.e * p.n_q_heads + (size_t)it.h * G) * D + lane * kCols;
-      uint32_t w[GP][kCols / 2];
-#pragma unroll
-      for (int g = 0; g < GP; ++g)
-#pragma unroll
-        for (int i = 0; i < kCols / 2; ++i) w[g][i] = g < G ? __ldg(reinterpret_cast<const uint32_t*>(q + (size_t)g * D) + i) : 0u;
+      // D / 16 lanes a head, sixteen elements a lane, as many heads at a time as the warp holds
+      constexpr int kLanes = D / 16, kHeads = 32 / kLanes, kPasses = (GP + kHeads - 1) / kHeads;
+      const int c = lane % kLanes;
+      const __nv_bfloat16* q = p.q + ((size_t)it.e * p.n_q_heads + (size_t)it.h * G) * D + c * 16;
       uint8_t* dst = smem + C::kOffQ + slot * C::kQBytes;
+      uint4 raw[kPasses][2];
 #pragma unroll
-      for (int g = 0; g < GP; ++g) {
-        if (g >= G) break;
+      for (int x = 0; x < kPasses; ++x) {
+        const int g = min(x * kHeads + lane / kLanes, G - 1);
+        raw[x][0] = __ldg(reinterpret_cast<const uint4*>(q + (size_t)g * D));
+        raw[x][1] = __ldg(reinterpret_cast<const uint4*>(q + (size_t)g * D) + 1);
+      }
+#pragma unroll
+      for (int x = 0; x < kPasses; ++x) {
+        const int g = x * kHeads + lane / kLanes;
+        const uint32_t v[8] = {raw[x][0].x, raw[x][0].y, raw[x][0].z, raw[x][0].w,
+                               raw[x][1].x, raw[x][1].y, raw[x][1].z, raw[x][1].w};
         uint32_t top = 0;
 #pragma unroll
-        for (int i = 0; i < kCols / 2; ++i) top = __vmaxu2(top, w[g][i] & 0x7fff7fffu);
-        top = __reduce_max_sync(0xffffffffu, max(top & 0xffffu, top >> 16));
+        for (int i = 0; i < 8; ++i) top = __vmaxu2(top, v[i] & 0x7fff7fffu);
+        top = max(top & 0xffffu, top >> 16);
+#pragma unroll
+        for (int o = 1; o < kLanes; o <<= 1) top = max(top, __shfl_xor_sync(0xffffffffu, top, o));
         const bool bad = top >= 0x7f80u;                       // an infinity or NaN in the row: every code a NaN
         const int ex = min(max((int)(top >> 7), 20), 254);     // exponent field; largest element in [128, 256) after scaling
-        const float inv = __uint_as_float((uint32_t)(261 - ex) << 23);
-        uint32_t c1[kCols / 2], c2[kCols / 2];
+        const __nv_bfloat162 inv = __float2bfloat162_rn(__uint_as_float((uint32_t)(261 - ex) << 23));
+        uint32_t c1[4], c2[4];
 #pragma unroll
-        for (int i = 0; i < kCols / 2; ++i) {
-          const float x = bf16_lo(w[g][i]) * inv, y = bf16_hi(w[g][i]) * inv;
-          c1[i] = e4m3x2_from_f32(x, y);
-          const float2 f = f32_from_e4m3x2(c1[i]);
-          c2[i] = e4m3x2_from_f32((x - f.x) * kPart, (y - f.y) * kPart);
-          if (bad) c1[i] = c2[i] = 0x7f7fu;
+        for (int i = 0; i < 4; ++i) {
+          uint32_t a[2], b[2];
+#pragma unroll
+          for (int k = 0; k < 2; ++k) {
+            const uint32_t y = bf16x2_scale(v[2 * i + k], inv);
+            const float lo = bf16_lo(y), hi = bf16_hi(y);
+            a[k] = e4m3x2_from_f32(lo, hi);
+            const float2 f = f32_from_e4m3x2(a[k]);
+            b[k] = e4m3x2_from_f32((lo - f.x) * kPart, (hi - f.y) * kPart);
+          }
+          c1[i] = bad ? 0x7f7f7f7fu : __byte_perm(a[0], a[1], 0x5410);
+          c2[i] = bad ? 0x7f7f7f7fu : __byte_perm(b[0], b[1], 0x5410);
         }
-        const int col = lane * kCols;
-        if constexpr (kCols == 4) {
-          *reinterpret_cast<uint32_t*>(dst + swizzled<D>(g, col)) = c1[0] | (c1[1] << 16);
-          *reinterpret_cast<uint32_t*>(dst + swizzled<D>(GP + g, col)) = c2[0] | (c2[1] << 16);
-        } else {
-          *reinterpret_cast<uint16_t*>(dst + swizzled<D>(g, col)) = (uint16_t)c1[0];
-          *reinterpret_cast<uint16_t*>(dst + swizzled<D>(GP + g, col)) = (uint16_t)c2[0];
+        if (g < G) {
+          *reinterpret_cast<uint4*>(dst + swizzled<D>(g, c * 16)) = make_uint4(c1[0], c1[1], c1[2], c1[3]);
+          *reinterpret_cast<uint4*>(dst + swizzled<D>(GP + g, c * 16)) = make_uint4(c2[0], c2[1], c2[2], c2[3]);
+          if (c == 0) s_qscale[slot][g] = __uint_as_float((uint32_t)(ex - 7) << 23) * p.scale_log2;
         }
-        if (lane == 0) s_qscale[slot][g] = __uint_as_float((uint32_t)(ex - 7) << 23) * p.scale_log2;
       }
       fence_proxy_async_smem();
       __syncwarp();
@@ -767,15 +813,19 @@ decode_e4m3_kernel(const __grid_constant__ CUtensorMap tmap_k, const __grid_cons
     // ================================================================ finished pieces of cut caches
     bool woken = false;                           // warps that are out of tiles wait for the first job or for the end
     // first the rows of empty caches
+#pragma unroll 1
     for (int e = blockIdx.x; e < p.n_units; e += gridDim.x) {
       if (unit_rows(p, e) != 0) continue;
       const size_t row0 = (size_t)e * p.n_q_heads;
+#pragma unroll 1
       for (int i = lane; i < p.n_q_heads * D / 8; i += 32)
         reinterpret_cast<uint4*>(p.out + row0 * D)[i] = make_uint4(0u, 0u, 0u, 0u);
       if (p.lse != nullptr)
+#pragma unroll 1
         for (int i = lane; i < p.n_q_heads; i += 32) p.lse[row0 + i] = -INFINITY;
     }
     if (!p.wait_first) grid_dependency_wait();    // the tickets are cleared by the launch before this one
+#pragma unroll 1
     for (uint32_t n_item = 0;; ++n_item) {
       const int slot = n_item % kFifo;
       if (!__all_sync(0xffffffffu, wait_bar(&s_fifo_full[slot], (n_item / kFifo) & 1, s_abort, p.wait_ns))) break;
@@ -818,6 +868,7 @@ decode_e4m3_kernel(const __grid_constant__ CUtensorMap tmap_k, const __grid_cons
     const int col = D == 128 ? warp * 32 + lane : warp * 16 + lane;
     const int blk = tid / kScaleBlock;
     uint32_t j = 0;                                              // tiles begun
+#pragma unroll 1
     for (uint32_t n_item = 0;; ++n_item) {
       const int slot = n_item % kFifo;
       bool bad = !wait_bar(&s_fifo_full[slot], (n_item / kFifo) & 1, s_abort, p.wait_ns);
@@ -843,6 +894,7 @@ decode_e4m3_kernel(const __grid_constant__ CUtensorMap tmap_k, const __grid_cons
         for (int g = 0; g < GP; ++g) acc[g] = fmaf(fmaf(d[GP + g], 1.f / kPart, d[g]), f[g], acc[g]);
       };
       const int n_tiles = tiles_of(it.rows);
+#pragma unroll 1
       for (int t = 0; t < n_tiles; ++t, ++j) {
         const int stage = j % C::kStages;
         const int left = it.rows - t * kTile;
@@ -853,7 +905,7 @@ decode_e4m3_kernel(const __grid_constant__ CUtensorMap tmap_k, const __grid_cons
         const float4 va = *reinterpret_cast<const float4*>(sc + 8), vb = *reinterpret_cast<const float4*>(sc + 12);
         const float vmax = fmaxf(fmaxf(fmaxf(fmaxf(va.x, va.y), fmaxf(va.z, va.w)),
                                        fmaxf(fmaxf(vb.x, vb.y), fmaxf(vb.z, vb.w))), 0x1p-110f);
-        const float vr = vs * __fdiv_rn(256.f, vmax);
+        const float vr = vs * (256.f * __frcp_rn(vmax));
         wait_bar(&s_s_full[j & 1], (j / 2) & 1, s_abort, p.wait_ns);
         tc_fence_after_sync();
         float s[GP], mt[GP];
@@ -866,23 +918,28 @@ decode_e4m3_kernel(const __grid_constant__ CUtensorMap tmap_k, const __grid_cons
             if (!live) s[g] = -INFINITY;
           }
         }
+        // (heads from G on are left out by uniform branches: their columns hold nothing that is read)
 #pragma unroll
-        for (int g = 0; g < GP; ++g) mt[g] = warp_max(s[g]);
-        if (lane == 0) {
-#pragma unroll
-          for (int g = 0; g < GP; ++g) s_max[j & 1][warp][g] = mt[g];
-        }
+        for (int g = 0; g < GP; ++g) mt[g] = g < G ? warp_max(s[g]) : 0.f;
+        if (lane == 0) put_heads<GP>(s_max[j & 1][warp], mt);
         named_bar_sync(kBarSoft, kSoftThreads);
+        {
+          float a[GP], b[GP], c[GP], d[GP];
+          get_heads<GP>(s_max[j & 1][0], a);
+          get_heads<GP>(s_max[j & 1][1], b);
+          get_heads<GP>(s_max[j & 1][2], c);
+          get_heads<GP>(s_max[j & 1][3], d);
 #pragma unroll
-        for (int g = 0; g < GP; ++g)
-          mt[g] = fmaxf(fmaxf(s_max[j & 1][0][g], s_max[j & 1][1][g]), fmaxf(s_max[j & 1][2][g], s_max[j & 1][3][g]));
+          for (int g = 0; g < GP; ++g) mt[g] = fmaxf(fmaxf(a[g], b[g]), fmaxf(c[g], d[g]));
+        }
         // weights relative to the tile's maximum; the codes also carry the V scale relative to the tile's largest
         uint8_t* pb = smem + C::kOffP + (j & 1) * C::kPBytes;
         float w[GP];
 #pragma unroll
-        for (int g = 0; g < GP; ++g) w[g] = fast_exp2(s[g] - mt[g]);
+        for (int g = 0; g < GP; ++g) w[g] = g < G ? fast_exp2(s[g] - mt[g]) : 0.f;
 #pragma unroll
         for (int g = 0; g < GP; g += 2) {
+          if (g >= G) break;
           const float x = w[g] * vr, y = GP > 1 ? w[g + (GP > 1)] * vr : 0.f;
           const uint32_t c1 = e4m3x2_from_f32(x, y);
           const float2 b = f32_from_e4m3x2(c1);
@@ -899,6 +956,7 @@ decode_e4m3_kernel(const __grid_constant__ CUtensorMap tmap_k, const __grid_cons
           // groups of 32 rows, so clear V there (0 * NaN)
           wait_bar(&s_v_full[stage], (j / C::kStages) & 1, s_abort, p.wait_ns);
           uint4* z = reinterpret_cast<uint4*>(smem + C::kOffV + stage * C::kTileBytes);
+#pragma unroll 1
           for (int i = left * (D / 16) + tid; i < (left + 31) / 32 * 32 * (D / 16); i += kSoftThreads)
             z[i] = make_uint4(0u, 0u, 0u, 0u);
         }
@@ -910,43 +968,90 @@ decode_e4m3_kernel(const __grid_constant__ CUtensorMap tmap_k, const __grid_cons
         // on to the new reference maximum
 #pragma unroll
         for (int g = 0; g < GP; ++g) {
-          const float mn = fmaxf(m[g], mt[g]);
-          const float al = fast_exp2(m[g] - mn), fw = fast_exp2(mt[g] - mn);
+          if (g >= G) break;
+          const float up = mt[g] - m[g];                          // +inf at the first tile
+          const bool grows = up > 0.f;
+          const float ex = fast_exp2(grows ? -up : up);
+          const float al = grows ? ex : 1.f, fw = grows ? 1.f : ex;
           l[g] = fmaf(l[g], al, w[g] * fw);
           acc[g] *= al;
           f[g] = fw * (vmax * (1.f / 256.f));
-          m[g] = mn;
+          m[g] = grows ? mt[g] : m[g];
         }
       }
       add_output(j - 1);
-      // ---- denominators over the 128 rows' threads
+      // ---- denominators over the 128 rows' threads; the thread that has head g's also writes its statistics
+      const size_t row0 = (size_t)it.e * p.n_q_heads + (size_t)it.h * G;
+      const size_t piece = 2 * (size_t)blockIdx.x + ((int)blockIdx.x == it.first_cta ? 1 : 0);
+      const bool drop = *s_abort != 0;
+      auto write_stats = [&](int g, float mg, float lg) {
+        if (it.n_pieces > 1) __stcg(reinterpret_cast<float2*>(p.part_ml) + piece * G + g, make_float2(mg, lg));
+        else if (p.lse != nullptr && !drop) p.lse[row0 + g] = (mg + __log2f(lg)) * 0.6931471805599453f;
+      };
+      float* sum_at = s_sum[n_item & 1];
+      if constexpr (GP >= 4) {
+        // through shared memory (the weights' buffers, which no product reads any more): 128 / GP threads a head.  (What
+        // runs once an item runs out of a cold instruction cache: shuffles of every head take four times the code.)
+        constexpr int kPer = 128 / GP;
+        float* part = reinterpret_cast<float*>(smem + C::kOffP);
 #pragma unroll
-      for (int g = 0; g < GP; ++g) {
+        for (int g = 0; g < GP; ++g) part[g * 128 + tid] = l[g];
+        if (lane == 0) put_heads<GP>(s_max[j & 1][warp], m);     // the same in every warp (the buffer of the tile before last)
+        named_bar_sync(kBarSoft, kSoftThreads);
+        const int g = tid / kPer;
+        float x = 0.f;
 #pragma unroll
-        for (int o = 16; o > 0; o >>= 1) l[g] += __shfl_xor_sync(0xffffffffu, l[g], o);
-        if (lane == 0) s_sum[n_item & 1][warp][g] = l[g];
+        for (int k = 0; k < GP; k += 4) {
+          const float4 v = *reinterpret_cast<const float4*>(part + g * 128 + tid % kPer * GP + k);
+          x += (v.x + v.y) + (v.z + v.w);
+        }
+#pragma unroll
+        for (int o = kPer / 2; o > 0; o >>= 1) x += __shfl_xor_sync(0xffffffffu, x, o);
+        if (tid % kPer == 0 && g < G) {
+          sum_at[g] = __frcp_rn(x);
+          write_stats(g, s_max[j & 1][warp][g], x);
+        }
+        named_bar_sync(kBarSoft, kSoftThreads);
+      } else {
+#pragma unroll
+        for (int g = 0; g < GP; ++g) {
+#pragma unroll
+          for (int o = 16; o > 0; o >>= 1) l[g] += __shfl_xor_sync(0xffffffffu, l[g], o);
+          if (lane == 0) sum_at[8 + 4 * g + warp] = l[g];
+        }
+        named_bar_sync(kBarSoft, kSoftThreads);
+#pragma unroll
+        for (int g = 0; g < GP; ++g) {
+          const float4 v = *reinterpret_cast<const float4*>(sum_at + 8 + 4 * g);
+          l[g] = (v.x + v.y) + (v.z + v.w);
+          if (tid == g) write_stats(g, m[g], l[g]);
+        }
       }
-      named_bar_sync(kBarSoft, kSoftThreads);
-#pragma unroll
-      for (int g = 0; g < GP; ++g) l[g] = (s_sum[n_item & 1][0][g] + s_sum[n_item & 1][1][g]) + (s_sum[n_item & 1][2][g] + s_sum[n_item & 1][3][g]);
       tc_fence_before_sync();
       __syncwarp();
       if (lane == 0) mbar_arrive(&s_fifo_empty[slot]);
-      const size_t row0 = (size_t)it.e * p.n_q_heads + (size_t)it.h * G;
       if (it.n_pieces == 1) {
-        if (!*s_abort) {
+        float inv[GP];
+        if constexpr (GP >= 4) {
+          get_heads<GP>(sum_at, inv);
+        } else {
+#pragma unroll
+          for (int g = 0; g < GP; ++g) inv[g] = __frcp_rn(l[g]);
+        }
+        if (holds_col && !drop) {
+          __nv_bfloat16* o = p.out + row0 * D + col;
 #pragma unroll
           for (int g = 0; g < GP; ++g) {
-            if (g < G && holds_col) p.out[(row0 + g) * D + col] = __float2bfloat16(acc[g] / l[g]);
-            if (g < G && tid == g && p.lse != nullptr) p.lse[row0 + g] = (m[g] + log2f(l[g])) * 0.6931471805599453f;
+            if (g >= G) break;
+            o[g * D] = __float2bfloat16(acc[g] * inv[g]);
           }
         }
-      } else {                                                    // a piece; warp 7 counts it
-        const size_t piece = 2 * (size_t)blockIdx.x + ((int)blockIdx.x == it.first_cta ? 1 : 0);
+      } else if (holds_col) {                                     // a piece; warp 7 counts it
+        float* o = p.part_o + piece * G * D + col;
 #pragma unroll
         for (int g = 0; g < GP; ++g) {
-          if (g < G && holds_col) __stcg(&p.part_o[(piece * G + g) * D + col], acc[g]);
-          if (g < G && tid == g) __stcg(reinterpret_cast<float2*>(p.part_ml) + piece * G + g, make_float2(m[g], l[g]));
+          if (g >= G) break;
+          __stcg(o + g * D, acc[g]);
         }
       }
       __syncwarp();
@@ -955,6 +1060,7 @@ decode_e4m3_kernel(const __grid_constant__ CUtensorMap tmap_k, const __grid_cons
   }
   // ---- out of tiles: help with the joins until warp 7 has counted its last piece
   if (warp != 7) wait_bar(&s_wake, 0, s_abort, p.wait_ns);
+#pragma unroll 1
   while (warp != 7) {
     const bool over = __any_sync(0xffffffffu, *(volatile int*)&s_joins.all != 0);   // set on every way out of warp 7's loop
     join_open<D>(p, &s_joins);
