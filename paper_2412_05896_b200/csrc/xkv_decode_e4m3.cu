@@ -430,6 +430,7 @@ decode_e4m3_kernel(const __grid_constant__ CUtensorMap tmap_k, const __grid_cons
   __shared__ Item s_item[kFifo];
   __shared__ float s_qscale[kFifo][8];
   __shared__ __align__(16) float s_max[2][4][8];
+  __shared__ __align__(16) float s_head[4][3][8];
   __shared__ __align__(16) float s_sum[2][16];    // reciprocal denominators, or (one or two heads) the warps' sums from [8] on
   __shared__ int s_scan[kThreads / 32];
   __shared__ int4 s_first;                        // the unit in which the share begins: unit, rows, where it begins on the line
@@ -878,7 +879,8 @@ decode_e4m3_kernel(const __grid_constant__ CUtensorMap tmap_k, const __grid_cons
       if (it.e < 0) break;
       // From here to the end of the item every thread takes every barrier, also when a wait has expired.
       wait_bar(&s_q_full[slot], (n_item / kFifo) & 1, s_abort, p.wait_ns);
-      float qs[GP], m[GP], l[GP], acc[GP], f[GP];
+      float qs[GP], l[GP], acc[GP], f[GP];
+      float m[GP];                                               // four heads and more: m[0] of lane g is that of head g
 #pragma unroll
       for (int g = 0; g < GP; ++g) {
         qs[g] = g < G ? s_qscale[slot][g] : 0.f;
@@ -923,14 +925,29 @@ decode_e4m3_kernel(const __grid_constant__ CUtensorMap tmap_k, const __grid_cons
         for (int g = 0; g < GP; ++g) mt[g] = g < G ? warp_max(s[g]) : 0.f;
         if (lane == 0) put_heads<GP>(s_max[j & 1][warp], mt);
         named_bar_sync(kBarSoft, kSoftThreads);
-        {
-          float a[GP], b[GP], c[GP], d[GP];
-          get_heads<GP>(s_max[j & 1][0], a);
-          get_heads<GP>(s_max[j & 1][1], b);
-          get_heads<GP>(s_max[j & 1][2], c);
-          get_heads<GP>(s_max[j & 1][3], d);
+        // The tile's maximum of a head, and how the running sums move to the new reference maximum: for four heads and more
+        // lane g works for head g and hands the results round (the same arithmetic in every thread is six times the code).
+        bool grows_any;                                           // the reference maximum of some head has grown
+        if constexpr (GP >= 4) {
+          bool grows = false;
+          if (lane < GP) {
+            const float top = fmaxf(fmaxf(s_max[j & 1][0][lane], s_max[j & 1][1][lane]),
+                                    fmaxf(s_max[j & 1][2][lane], s_max[j & 1][3][lane]));
+            const float up = top - m[0];                          // +inf at the first tile
+            grows = up > 0.f;
+            const float ex = fast_exp2(grows ? -up : up);
+            m[0] = grows ? top : m[0];
+            s_head[warp][0][lane] = top;
+            s_head[warp][1][lane] = grows ? ex : 1.f;             // what the sums so far are multiplied by
+            s_head[warp][2][lane] = grows ? 1.f : ex;             // and the tile's
+          }
+          grows_any = __any_sync(0xffffffffu, grows);             // (orders the stores before the loads below)
+          get_heads<GP>(s_head[warp][0], mt);
+        } else {
 #pragma unroll
-          for (int g = 0; g < GP; ++g) mt[g] = fmaxf(fmaxf(a[g], b[g]), fmaxf(c[g], d[g]));
+          for (int g = 0; g < GP; ++g)
+            mt[g] = fmaxf(fmaxf(s_max[j & 1][0][g], s_max[j & 1][1][g]), fmaxf(s_max[j & 1][2][g], s_max[j & 1][3][g]));
+          grows_any = true;
         }
         // weights relative to the tile's maximum; the codes also carry the V scale relative to the tile's largest
         uint8_t* pb = smem + C::kOffP + (j & 1) * C::kPBytes;
@@ -966,17 +983,35 @@ decode_e4m3_kernel(const __grid_constant__ CUtensorMap tmap_k, const __grid_cons
         if (lane == 0) mbar_arrive(&s_p_full[j & 1]);
         if (t > 0) add_output(j - 1);
         // on to the new reference maximum
+        if constexpr (GP >= 4) {
+          float fw[GP];
+          if (grows_any) {
+            float al[GP];
+            get_heads<GP>(s_head[warp][1], al);
 #pragma unroll
-        for (int g = 0; g < GP; ++g) {
-          if (g >= G) break;
-          const float up = mt[g] - m[g];                          // +inf at the first tile
-          const bool grows = up > 0.f;
-          const float ex = fast_exp2(grows ? -up : up);
-          const float al = grows ? ex : 1.f, fw = grows ? 1.f : ex;
-          l[g] = fmaf(l[g], al, w[g] * fw);
-          acc[g] *= al;
-          f[g] = fw * (vmax * (1.f / 256.f));
-          m[g] = grows ? mt[g] : m[g];
+            for (int g = 0; g < GP; ++g) {
+              l[g] *= al[g];
+              acc[g] *= al[g];
+            }
+          }
+          get_heads<GP>(s_head[warp][2], fw);
+#pragma unroll
+          for (int g = 0; g < GP; ++g) {
+            l[g] = fmaf(w[g], fw[g], l[g]);
+            f[g] = fw[g] * (vmax * (1.f / 256.f));
+          }
+        } else {
+#pragma unroll
+          for (int g = 0; g < GP; ++g) {
+            const float up = mt[g] - m[g];                        // +inf at the first tile
+            const bool grows = up > 0.f;
+            const float ex = fast_exp2(grows ? -up : up);
+            const float al = grows ? ex : 1.f, fw = grows ? 1.f : ex;
+            l[g] = fmaf(l[g], al, w[g] * fw);
+            acc[g] *= al;
+            f[g] = fw * (vmax * (1.f / 256.f));
+            m[g] = grows ? mt[g] : m[g];
+          }
         }
       }
       add_output(j - 1);
@@ -996,7 +1031,7 @@ decode_e4m3_kernel(const __grid_constant__ CUtensorMap tmap_k, const __grid_cons
         float* part = reinterpret_cast<float*>(smem + C::kOffP);
 #pragma unroll
         for (int g = 0; g < GP; ++g) part[g * 128 + tid] = l[g];
-        if (lane == 0) put_heads<GP>(s_max[j & 1][warp], m);     // the same in every warp (the buffer of the tile before last)
+        if (lane < GP) s_head[warp][0][lane] = m[0];
         named_bar_sync(kBarSoft, kSoftThreads);
         const int g = tid / kPer;
         float x = 0.f;
@@ -1009,7 +1044,7 @@ decode_e4m3_kernel(const __grid_constant__ CUtensorMap tmap_k, const __grid_cons
         for (int o = kPer / 2; o > 0; o >>= 1) x += __shfl_xor_sync(0xffffffffu, x, o);
         if (tid % kPer == 0 && g < G) {
           sum_at[g] = __frcp_rn(x);
-          write_stats(g, s_max[j & 1][warp][g], x);
+          write_stats(g, s_head[warp][0][g], x);
         }
         named_bar_sync(kBarSoft, kSoftThreads);
       } else {
