@@ -3,7 +3,7 @@
 //
 // Mathematics.  With stored codes k, v (e4m3), block scales s_k, s_v and the G query heads of a KV head:
 //   logits  S[c, h] = (codes k_c . q_h) s_k[c] scale          M = 128 cache rows, N = heads, K = d
-//   output  O[j, h] = sum_c v[c, j] (s_v[c] P[c, h])          M = d, N = heads, K = 128 cache rows
+//   output  O[j, h] = sum_c v[c, j] (s_v[c] P[c, h])          M = d, N = heads, K = a tile's cache rows
 // Both products are tcgen05.mma kind::f8f6f4 with the cache tile as the A operand exactly as it lies in the page (K rows
 // are K-major, V rows are M-major), fp32 accumulators in tensor memory.  The small operand has more bits than one code
 // holds, so it enters as two codes side by side on the N axis: q = a1 + a2 / 32 and p = b1 + b2 / 32, each part rounded to
@@ -54,33 +54,37 @@ using tc::tmem_relinquish;
 using tc::tmem_wait_ld;
 using tc::umma_commit;
 
-constexpr int kTile = 128;            // cache rows per tile
 constexpr int kN = 16;                // N of both MMAs: two codes x up to eight heads, the rest zero rows
 constexpr int kThreads = 256;
 constexpr int kSoftThreads = 128;
 constexpr int kFifo = 3;              // items between the walk and the last reader
-constexpr int kTmemCols = 64;         // two logit buffers and two output buffers of 16 columns
 constexpr int kCtasPerSm = 2;
 constexpr float kPart = 32.f;         // weight of the second code
 constexpr int kBarSoft = 1;           // named barrier of warps 0-3
-constexpr int kTileBlocks = kTile / kScaleBlock;
 constexpr int kCacheCost = 12;        // what a cache costs besides its bytes, in blocks of 16 rows (2048 caches of 203 to 1101 rows:
                                       // 66.6 us with 4, 64.9 with 8, 64.2 with 12, 64.9 with 16)
-constexpr int kMinSegment = 8;        // shortest segment, in blocks: a tile, so that a cache has a tile in every segment
-                                      // between its first and its last one
 constexpr int kJobs = 32;             // joins a CTA may have open
 
 template <int D>
 struct Cfg {
-  static constexpr int kStages = D == 128 ? 3 : 6;              // K and V tiles of 16 KB (8 KB): 96 KB a CTA
+  // A tile is 16 KB of K and of V: 128 rows of 128 elements or 256 of 64.  What the softmax warps spend on a tile is mostly
+  // waits and exchanges that do not grow with its rows.
+  static constexpr int kTile = 128 * (128 / D);                 // cache rows per tile
+  static constexpr int kSpans = kTile / 128;                    // M = 128 products per tile of logits, rows per softmax thread
+  static constexpr int kTileBlocks = kTile / kScaleBlock;
+  static constexpr int kMinSegment = kTileBlocks;               // shortest segment, in blocks: a tile, so that a cache has a
+                                                                // tile in every segment between its first and its last one
+  static constexpr int kTmemCols = kSpans == 1 ? 64 : 128;      // two logit buffers, two output buffers; 16 columns a product
+  static constexpr int kStages = 3;                             // 96 KB a CTA
   static constexpr int kTileBytes = kTile * D;
   static constexpr int kQBytes = kN * D;
-  static constexpr int kPBytes = kN * kTile;
+  static constexpr int kPBytes = kN * kTile;                    // spans one after the other
+  static constexpr int kPSpan = kN * 128;
   static constexpr int kOffV = kStages * kTileBytes;
   static constexpr int kOffQ = 2 * kStages * kTileBytes;
   static constexpr int kOffP = kOffQ + kFifo * kQBytes;
-  static constexpr int kOffScales = kOffP + 2 * kPBytes;         // [kStages][16]: 8 of K, 8 of V
-  static constexpr int kSmemBytes = 1024 + kOffScales + kStages * 64;
+  static constexpr int kOffScales = kOffP + 2 * kPBytes;         // [kStages][2 * kTileBlocks]: of K, of V
+  static constexpr int kSmemBytes = 1024 + kOffScales + kStages * 8 * kTileBlocks;
 };
 
 struct Params {
@@ -95,7 +99,7 @@ struct Params {
   // row -> page: page_size is 8 n with n even, 2 <= n <= 32, and x / n = (x * ceil(2^32 / n)) >> 32 for x <= 2^27 + 32
   uint32_t page_mul;                  // ceil(2^32 / n)
   __device__ __forceinline__ int page_of(int row) const { return (int)__umulhi((uint32_t)row >> 3, page_mul); }
-  int32_t box_rows;                   // rows of a TMA box: the largest power of two up to 128 that divides page_size
+  int32_t box_rows;                   // rows of a TMA box: the largest power of two up to a tile's that divides page_size
   int32_t box_shift;                  // its logarithm
   int32_t max_ctas;                   // CTAs that the partial results have room for
   int32_t withhold_cta;               // test hook: this CTA's copies are never issued, so that waits expire (-1: none)
@@ -300,7 +304,11 @@ __device__ __forceinline__ int unit_rows(const Params& p, int e) {
   const int n = __ldg(&p.seq_lens[(size_t)p.layer_begin * p.batch + e]);
   return min(max(n, 0), p.max_pages_per_seq * p.page_size);
 }
-__device__ __forceinline__ int tiles_of(int rows) { return (rows + kTile - 1) / kTile; }
+template <int D>
+__device__ __forceinline__ int tiles_of(int rows) {
+  constexpr int kTile = Cfg<D>::kTile;
+  return (rows + kTile - 1) / kTile;
+}
 // length of a cache on the line
 __device__ __forceinline__ int cost_of(int rows) { return rows > 0 ? (rows + kScaleBlock - 1) / kScaleBlock + kCacheCost : 0; }
 
@@ -422,6 +430,7 @@ __global__ void __launch_bounds__(kThreads, kCtasPerSm)
 decode_e4m3_kernel(const __grid_constant__ CUtensorMap tmap_k, const __grid_constant__ CUtensorMap tmap_v,
                    const __grid_constant__ Params p) {
   using C = Cfg<D>;
+  constexpr int kTile = C::kTile, kTileBlocks = C::kTileBlocks;
   extern __shared__ uint8_t smem_raw[];
   uint8_t* smem = reinterpret_cast<uint8_t*>((reinterpret_cast<uintptr_t>(smem_raw) + 1023) & ~uintptr_t(1023));
   __shared__ uint64_t s_k_full[C::kStages], s_k_empty[C::kStages], s_v_full[C::kStages], s_v_empty[C::kStages],
@@ -478,7 +487,7 @@ decode_e4m3_kernel(const __grid_constant__ CUtensorMap tmap_k, const __grid_cons
     prefetch_tmap(&tmap_v);
   }
   if (warp == 5) {
-    tmem_alloc(&s_tmem, kTmemCols);
+    tmem_alloc(&s_tmem, C::kTmemCols);
     tmem_relinquish();
   }
   // operand rows that no head fills stay zero
@@ -504,7 +513,7 @@ decode_e4m3_kernel(const __grid_constant__ CUtensorMap tmap_k, const __grid_cons
     line += s_scan[w];
   }
   line *= Hkv;
-  const int n_ctas = min(min((int)gridDim.x, p.max_ctas), max(line / kMinSegment, 1));
+  const int n_ctas = min(min((int)gridDim.x, p.max_ctas), max(line / C::kMinSegment, 1));
   const Cut share(line, n_ctas);
   const bool works = (int)blockIdx.x < n_ctas && line > 0;
   const int begin = works ? share.begin(blockIdx.x) : 0, stop_at = works ? share.begin(blockIdx.x + 1) : 0;
@@ -518,7 +527,7 @@ decode_e4m3_kernel(const __grid_constant__ CUtensorMap tmap_k, const __grid_cons
       if (at <= stop_at && stop_at < next) {
         const int h = quotient(stop_at - at, cost), g0 = at + h * cost;
         // cut: some of its tiles start before the end, others behind it (and none in the piece that the begin cuts)
-        const bool cut = g0 > begin && g0 < stop_at && stop_at - g0 <= (tiles_of(rows) - 1) * kTileBlocks;
+        const bool cut = g0 > begin && g0 < stop_at && stop_at - g0 <= (tiles_of<D>(rows) - 1) * kTileBlocks;
         s_end_cut = make_int4(e, h, g0, cut ? rows : 0);
       }
       at = next;
@@ -571,7 +580,7 @@ decode_e4m3_kernel(const __grid_constant__ CUtensorMap tmap_k, const __grid_cons
       if (cur.e < 0 || (int)blockIdx.x == p.withhold_cta) break;
       int pages = nxt_pages, ahead = 0;
       have_next = false;
-      const int n_tiles = tiles_of(cur.rows);
+      const int n_tiles = tiles_of<D>(cur.rows);
 #pragma unroll 1
       for (int t = 0; t < n_tiles; ++t, ++j) {
         const int box0 = t * boxes_per_tile;
@@ -603,15 +612,15 @@ decode_e4m3_kernel(const __grid_constant__ CUtensorMap tmap_k, const __grid_cons
         if (lane < n_box)
           tma_load_2d(smem + C::kOffV + stage * C::kTileBytes + lane * R * D, &tmap_v, 0, grow, &s_v_full[stage]);
         {
-          // lanes 0-7: scales of the tile's eight blocks of K rows, lanes 8-15: of V rows
-          const int blk = lane & 7;
+          // the first lanes: scales of the tile's blocks of K rows, the next ones: of V rows
+          const int blk = lane % kTileBlocks;
           const int in_box = (blk * kScaleBlock) >> p.box_shift;
           int bg = __shfl_sync(0xffffffffu, grow, in_box);
           bg = bg / kScaleBlock + blk - (in_box << p.box_shift) / kScaleBlock;
-          if (lane < 16) {
+          if (lane < 2 * kTileBlocks) {
             const bool live = blk < n_blk;
-            float* dst = reinterpret_cast<float*>(smem + C::kOffScales) + stage * 16 + lane;
-            cp_async_4(dst, (lane < 8 ? p.k_scales : p.v_scales) + (live ? bg : 0), live);
+            float* dst = reinterpret_cast<float*>(smem + C::kOffScales) + stage * 2 * kTileBlocks + lane;
+            cp_async_4(dst, (lane < kTileBlocks ? p.k_scales : p.v_scales) + (live ? bg : 0), live);
           }
           cp_async_arrive(&s_scale_full[stage]);
         }
@@ -632,7 +641,7 @@ decode_e4m3_kernel(const __grid_constant__ CUtensorMap tmap_k, const __grid_cons
     // ================================================================ the MMAs
     // The whole warp walks, one elected lane issues: a branch on elect.sync costs 49 clocks an MMA, one on the lane
     // index 78 (measured, whatever the shape; the 128 x 16 x 32 product itself takes 42).
-    constexpr uint32_t kIdescS = idesc_e4m3(kTile, kN, false), kIdescO = idesc_e4m3(D, kN, true);
+    constexpr uint32_t kIdescS = idesc_e4m3(128, kN, false), kIdescO = idesc_e4m3(D, kN, true);
     uint32_t js = 0, jo = 0, n_item = 0;          // logit tiles issued, output tiles issued, items begun
     int slot = 0, t = 0, n_tiles = 0, last_rows = 0;   // of the logits
     int rows0 = kTile, rows1 = kTile;             // rows of the even and the odd tile between the two products
@@ -651,7 +660,7 @@ decode_e4m3_kernel(const __grid_constant__ CUtensorMap tmap_k, const __grid_cons
           if (!__all_sync(0xffffffffu, wait_bar(&s_q_full[slot], (n_item / kFifo) & 1, s_abort, p.wait_ns))) break;
           ++n_item;
           t = 0;
-          n_tiles = tiles_of(rows);
+          n_tiles = tiles_of<D>(rows);
           last_rows = rows - (n_tiles - 1) * kTile;
         }
         const int stage = js % C::kStages;
@@ -662,9 +671,12 @@ decode_e4m3_kernel(const __grid_constant__ CUtensorMap tmap_k, const __grid_cons
         if (elect_one()) {
           const uint64_t a = smem_desc<D>(smem_u32(smem + stage * C::kTileBytes));
           const uint64_t b = smem_desc<D>(smem_u32(smem + C::kOffQ + slot * C::kQBytes));
-          const uint32_t d = tmem + (js & 1) * kN;
+          const uint32_t d = tmem + (js & 1) * C::kSpans * kN;
 #pragma unroll
-          for (int k = 0; k < D / 32; ++k) umma_e4m3(d, a + 2 * k, b + 2 * k, kIdescS, k > 0);
+          for (int x = 0; x < C::kSpans; ++x)
+            if (x == 0 || !last || last_rows > 128 * x)
+#pragma unroll
+              for (int k = 0; k < D / 32; ++k) umma_e4m3(d + x * kN, a + x * (128 * D / 16) + 2 * k, b + 2 * k, kIdescS, k > 0);
           umma_commit(&s_s_full[js & 1]);
           umma_commit(&s_k_empty[stage]);
           if (last) umma_commit(&s_fifo_empty[slot]);
@@ -683,10 +695,10 @@ decode_e4m3_kernel(const __grid_constant__ CUtensorMap tmap_k, const __grid_cons
         if (elect_one()) {
           const uint64_t a = smem_desc<D>(smem_u32(smem + C::kOffV + stage * C::kTileBytes));
           const uint64_t b = smem_desc<128>(smem_u32(smem + C::kOffP + (jo & 1) * C::kPBytes));
-          const uint32_t d = tmem + 2 * kN + (jo & 1) * kN;
+          const uint32_t d = tmem + (2 * C::kSpans + (jo & 1)) * kN;
 #pragma unroll
           for (int k = 0; k < kTile / 32; ++k)    // whole groups of 32 rows; those behind the last row stay out
-            if (32 * k < rows) umma_e4m3(d, a + 2 * D * k, b + 2 * k, kIdescO, k > 0);
+            if (32 * k < rows) umma_e4m3(d, a + 2 * D * k, b + k / 4 * (C::kPSpan / 16) + k % 4 * 2, kIdescO, k > 0);
           umma_commit(&s_d_full[jo & 1]);
           umma_commit(&s_v_empty[stage]);
         }
@@ -715,7 +727,7 @@ decode_e4m3_kernel(const __grid_constant__ CUtensorMap tmap_k, const __grid_cons
         it.h = s_end_cut.y;
         it.rows = (stop_at - g0 + kTileBlocks - 1) / kTileBlocks * kTile;
         it.first_cta = (int)blockIdx.x;
-        it.n_pieces = share.part_of(g0 + (tiles_of(s_end_cut.w) - 1) * kTileBlocks) - it.first_cta + 1;
+        it.n_pieces = share.part_of(g0 + (tiles_of<D>(s_end_cut.w) - 1) * kTileBlocks) - it.first_cta + 1;
         return it;
       }
 #pragma unroll 1
@@ -729,7 +741,7 @@ decode_e4m3_kernel(const __grid_constant__ CUtensorMap tmap_k, const __grid_cons
           rows = unit_rows(p, e);
           cost = cost_of(rows);
         }
-        const int g0 = unit_at + h * cost, nt = tiles_of(rows);
+        const int g0 = unit_at + h * cost, nt = tiles_of<D>(rows);
         const int t0 = (at - g0 + kTileBlocks - 1) / kTileBlocks;                       // first tile that starts at or behind `at`
         const int t1 = min(nt, (min(walk_end, g0 + cost) - g0 + kTileBlocks - 1) / kTileBlocks);   // first one behind the piece
         const int this_h = h;
@@ -891,38 +903,47 @@ decode_e4m3_kernel(const __grid_constant__ CUtensorMap tmap_k, const __grid_cons
         wait_bar(&s_d_full[jd & 1], (jd / 2) & 1, s_abort, p.wait_ns);
         tc_fence_after_sync();
         float d[2 * GP];
-        tmem_ld<2 * GP>(tmem + 2 * kN + (jd & 1) * kN + lane_base, d);
+        tmem_ld<2 * GP>(tmem + (2 * C::kSpans + (jd & 1)) * kN + lane_base, d);
 #pragma unroll
         for (int g = 0; g < GP; ++g) acc[g] = fmaf(fmaf(d[GP + g], 1.f / kPart, d[g]), f[g], acc[g]);
       };
-      const int n_tiles = tiles_of(it.rows);
+      const int n_tiles = tiles_of<D>(it.rows);
 #pragma unroll 1
       for (int t = 0; t < n_tiles; ++t, ++j) {
         const int stage = j % C::kStages;
         const int left = it.rows - t * kTile;
-        const bool live = tid < left;
         wait_bar(&s_scale_full[stage], (j / C::kStages) & 1, s_abort, p.wait_ns);
-        const float* sc = reinterpret_cast<const float*>(smem + C::kOffScales) + stage * 16;
-        const float ks = sc[blk], vs = sc[8 + blk];
-        const float4 va = *reinterpret_cast<const float4*>(sc + 8), vb = *reinterpret_cast<const float4*>(sc + 12);
-        const float vmax = fmaxf(fmaxf(fmaxf(fmaxf(va.x, va.y), fmaxf(va.z, va.w)),
-                                       fmaxf(fmaxf(vb.x, vb.y), fmaxf(vb.z, vb.w))), 0x1p-110f);
-        const float vr = vs * (256.f * __frcp_rn(vmax));
+        const float* sc = reinterpret_cast<const float*>(smem + C::kOffScales) + stage * 2 * kTileBlocks;
+        const float vmax = fmaxf(warp_max(sc[kTileBlocks + lane % kTileBlocks]), 0x1p-110f);
+        const float to_code = 256.f * __frcp_rn(vmax);
         wait_bar(&s_s_full[j & 1], (j / 2) & 1, s_abort, p.wait_ns);
         tc_fence_after_sync();
-        float s[GP], mt[GP];
-        {
-          float r[2 * GP];
-          tmem_ld<2 * GP>(tmem + (j & 1) * kN + lane_base, r);
+        float s[C::kSpans][GP], mt[GP];                           // logits, then weights, of rows tid and tid + 128
 #pragma unroll
-          for (int g = 0; g < GP; ++g) {
-            s[g] = fmaf(r[GP + g], 1.f / kPart, r[g]) * (ks * qs[g]);
-            if (!live) s[g] = -INFINITY;
+        for (int x = 0; x < C::kSpans; ++x) {
+          const bool live = x * 128 + tid < left;
+          if (x == 0 || left > 128 * x) {
+            float r[2 * GP];
+            tmem_ld<2 * GP>(tmem + ((j & 1) * C::kSpans + x) * kN + lane_base, r);
+            const float ks = sc[x * 8 + blk];
+#pragma unroll
+            for (int g = 0; g < GP; ++g) {
+              s[x][g] = fmaf(r[GP + g], 1.f / kPart, r[g]) * (ks * qs[g]);
+              if (!live) s[x][g] = -INFINITY;
+            }
+          } else {
+#pragma unroll
+            for (int g = 0; g < GP; ++g) s[x][g] = -INFINITY;
           }
         }
         // (heads from G on are left out by uniform branches: their columns hold nothing that is read)
 #pragma unroll
-        for (int g = 0; g < GP; ++g) mt[g] = g < G ? warp_max(s[g]) : 0.f;
+        for (int g = 0; g < GP; ++g) {
+          mt[g] = s[0][g];
+#pragma unroll
+          for (int x = 1; x < C::kSpans; ++x) mt[g] = fmaxf(mt[g], s[x][g]);
+          mt[g] = g < G ? warp_max(mt[g]) : 0.f;
+        }
         if (lane == 0) put_heads<GP>(s_max[j & 1][warp], mt);
         named_bar_sync(kBarSoft, kSoftThreads);
         // The tile's maximum of a head, and how the running sums move to the new reference maximum: for four heads and more
@@ -951,21 +972,30 @@ decode_e4m3_kernel(const __grid_constant__ CUtensorMap tmap_k, const __grid_cons
         }
         // weights relative to the tile's maximum; the codes also carry the V scale relative to the tile's largest
         uint8_t* pb = smem + C::kOffP + (j & 1) * C::kPBytes;
-        float w[GP];
+        float w[GP];                                              // sum of the weights of this thread's rows
 #pragma unroll
-        for (int g = 0; g < GP; ++g) w[g] = g < G ? fast_exp2(s[g] - mt[g]) : 0.f;
+        for (int x = 0; x < C::kSpans; ++x) {
+          if (x > 0 && left <= 128 * x) break;                    // the output's product does not reach this span
+          const float vr = sc[kTileBlocks + x * 8 + blk] * to_code;
+          uint8_t* px = pb + x * C::kPSpan;
 #pragma unroll
-        for (int g = 0; g < GP; g += 2) {
-          if (g >= G) break;
-          const float x = w[g] * vr, y = GP > 1 ? w[g + (GP > 1)] * vr : 0.f;
-          const uint32_t c1 = e4m3x2_from_f32(x, y);
-          const float2 b = f32_from_e4m3x2(c1);
-          const uint32_t c2 = e4m3x2_from_f32((x - b.x) * kPart, (y - b.y) * kPart);
-          pb[swizzled<128>(g, tid)] = (uint8_t)c1;
-          pb[swizzled<128>(GP + g, tid)] = (uint8_t)c2;
-          if (GP > 1) {
-            pb[swizzled<128>(g + 1, tid)] = (uint8_t)(c1 >> 8);
-            pb[swizzled<128>(GP + g + 1, tid)] = (uint8_t)(c2 >> 8);
+          for (int g = 0; g < GP; ++g) {
+            s[x][g] = g < G ? fast_exp2(s[x][g] - mt[g]) : 0.f;
+            w[g] = x == 0 ? s[x][g] : w[g] + s[x][g];
+          }
+#pragma unroll
+          for (int g = 0; g < GP; g += 2) {
+            if (g >= G) break;
+            const float a = s[x][g] * vr, b = GP > 1 ? s[x][g + (GP > 1)] * vr : 0.f;
+            const uint32_t c1 = e4m3x2_from_f32(a, b);
+            const float2 c = f32_from_e4m3x2(c1);
+            const uint32_t c2 = e4m3x2_from_f32((a - c.x) * kPart, (b - c.y) * kPart);
+            px[swizzled<128>(g, tid)] = (uint8_t)c1;
+            px[swizzled<128>(GP + g, tid)] = (uint8_t)c2;
+            if (GP > 1) {
+              px[swizzled<128>(g + 1, tid)] = (uint8_t)(c1 >> 8);
+              px[swizzled<128>(GP + g + 1, tid)] = (uint8_t)(c2 >> 8);
+            }
           }
         }
         if (left < kTile) {
@@ -1109,7 +1139,7 @@ decode_e4m3_kernel(const __grid_constant__ CUtensorMap tmap_k, const __grid_cons
     for (int i = 0; i < 1000; ++i) __nanosleep(1000);
   }
   tc_fence_after_sync();
-  if (warp == 5) tmem_dealloc(tmem, kTmemCols);
+  if (warp == 5) tmem_dealloc(tmem, C::kTmemCols);
 }
 
 bool make_tmap(CUtensorMap* tmap, void* base, int D, uint64_t rows, int box_rows) {
@@ -1173,13 +1203,14 @@ xkv_status decode_attn_e4m3(const xkv_dims* d, const xkv_cache* c, int layer_beg
                             cudaStream_t st) {
   const int n_units = n_layers * d->batch;
   int box = 16;
-  while (box < kTile && c->page_size % (2 * box) == 0) box *= 2;
+  const int tile = d->head_dim == 128 ? Cfg<128>::kTile : Cfg<64>::kTile;
+  while (box < tile && c->page_size % (2 * box) == 0) box *= 2;
   const uint64_t page_rows = (uint64_t)c->n_pages * d->n_kv_heads * c->page_size;
   CUtensorMap tk, tv;
   if (!make_tmap(&tk, c->k_pages, d->head_dim, page_rows, box) || !make_tmap(&tv, c->v_pages, d->head_dim, page_rows, box))
     return XKV_ERR_CUDA;
   const int64_t max_rows = (int64_t)c->max_pages_per_seq * c->page_size;
-  const int64_t caches = (int64_t)n_units * d->n_kv_heads, most = caches * ((max_rows + kTile - 1) / kTile);
+  const int64_t caches = (int64_t)n_units * d->n_kv_heads, most = caches * ((max_rows + tile - 1) / tile);
   if (caches * (max_rows / kScaleBlock + kCacheCost) >= (1ll << 31)) return XKV_ERR_UNSUPPORTED;
   xkv_status s;
   if (k_new != nullptr) {
