@@ -78,8 +78,7 @@ struct Cfg {
   static constexpr int kStages = 3;                             // 96 KB a CTA
   static constexpr int kTileBytes = kTile * D;
   static constexpr int kQBytes = kN * D;
-  static constexpr int kPBytes = kN * kTile;                    // spans one after the other
-  static constexpr int kPSpan = kN * 128;
+  static constexpr int kPBytes = kN * kTile;                    // 16 bytes a cache row
   static constexpr int kOffV = kStages * kTileBytes;
   static constexpr int kOffQ = 2 * kStages * kTileBytes;
   static constexpr int kOffP = kOffQ + kFifo * kQBytes;
@@ -170,9 +169,13 @@ __device__ __forceinline__ uint64_t smem_desc(uint32_t addr) {
   d |= (uint64_t)(kRowBytes == 128 ? 2 : 4) << 61;
   return d;
 }
-// e4m3 x e4m3 -> fp32, M x N; a_mn: the A operand is M-major
-__host__ __device__ constexpr uint32_t idesc_e4m3(int M, int N, bool a_mn) {
-  return (1u << 4) | (a_mn ? 1u << 15 : 0u) | ((uint32_t)(N >> 3) << 17) | ((uint32_t)(M >> 4) << 24);
+// An N-major operand of 16 N values of one byte: 16 bytes a row of K, no swizzle (groups of eight rows 128 bytes apart).
+__device__ __forceinline__ uint64_t smem_desc_rows16(uint32_t addr) {
+  return (uint64_t)((addr & 0x3ffffu) >> 4) | (uint64_t)(128 >> 4) << 16 | (uint64_t)(128 >> 4) << 32 | (uint64_t)1 << 46;
+}
+// e4m3 x e4m3 -> fp32, M x N; mn: the operands are M-major and N-major, else both K-major
+__host__ __device__ constexpr uint32_t idesc_e4m3(int M, int N, bool mn) {
+  return (1u << 4) | (mn ? 3u << 15 : 0u) | ((uint32_t)(N >> 3) << 17) | ((uint32_t)(M >> 4) << 24);
 }
 // byte offset of (row, column byte) in a swizzled operand
 template <int kRowBytes>
@@ -700,11 +703,11 @@ decode_e4m3_kernel(const __grid_constant__ CUtensorMap tmap_k, const __grid_cons
         const int rows = (jo & 1) ? rows1 : rows0;
         if (elect_one()) {
           const uint64_t a = smem_desc<D>(smem_u32(smem + C::kOffV + stage * C::kTileBytes));
-          const uint64_t b = smem_desc<128>(smem_u32(smem + C::kOffP + (jo & 1) * C::kPBytes));
+          const uint64_t b = smem_desc_rows16(smem_u32(smem + C::kOffP + (jo & 1) * C::kPBytes));
           const uint32_t d = tmem + (2 * C::kSpans + (jo & 1)) * kN;
 #pragma unroll
           for (int k = 0; k < kTile / 32; ++k)    // whole groups of 32 rows; those behind the last row stay out
-            if (32 * k < rows) umma_e4m3(d, a + 2 * D * k, b + k / 4 * (C::kPSpan / 16) + k % 4 * 2, kIdescO, k > 0);
+            if (32 * k < rows) umma_e4m3(d, a + 2 * D * k, b + 32 * k, kIdescO, k > 0);
           umma_commit(&s_d_full[jo & 1]);
           umma_commit(&s_v_empty[stage]);
         }
@@ -983,26 +986,31 @@ decode_e4m3_kernel(const __grid_constant__ CUtensorMap tmap_k, const __grid_cons
         for (int x = 0; x < C::kSpans; ++x) {
           if (x > 0 && left <= 128 * x) break;                    // the output's product does not reach this span
           const float vr = sc[kTileBlocks + x * 8 + blk] * to_code;
-          uint8_t* px = pb + x * C::kPSpan;
 #pragma unroll
           for (int g = 0; g < GP; ++g) {
             s[x][g] = g < G ? fast_exp2(s[x][g] - mt[g]) : 0.f;
             w[g] = x == 0 ? s[x][g] : w[g] + s[x][g];
           }
+          uint32_t c[GP < 4 ? 2 : GP / 2] = {};                   // pairs of first codes, then of second codes
 #pragma unroll
           for (int g = 0; g < GP; g += 2) {
             if (g >= G) break;
             const float a = s[x][g] * vr, b = GP > 1 ? s[x][g + (GP > 1)] * vr : 0.f;
             const uint32_t c1 = e4m3x2_from_f32(a, b);
-            const float2 c = f32_from_e4m3x2(c1);
-            const uint32_t c2 = e4m3x2_from_f32((a - c.x) * kPart, (b - c.y) * kPart);
-            px[swizzled<128>(g, tid)] = (uint8_t)c1;
-            px[swizzled<128>(GP + g, tid)] = (uint8_t)c2;
-            if (GP > 1) {
-              px[swizzled<128>(g + 1, tid)] = (uint8_t)(c1 >> 8);
-              px[swizzled<128>(GP + g + 1, tid)] = (uint8_t)(c2 >> 8);
+            const float2 y = f32_from_e4m3x2(c1);
+            const uint32_t c2 = e4m3x2_from_f32((a - y.x) * kPart, (b - y.y) * kPart);
+            if constexpr (GP < 4) {
+              c[0] = c1, c[1] = c2;
+            } else {
+              c[g / 4] |= c1 << (g % 4 * 8);
+              c[GP / 4 + g / 4] |= c2 << (g % 4 * 8);
             }
           }
+          uint8_t* row = pb + (x * 128 + tid) * kN;
+          if constexpr (GP == 8)      *reinterpret_cast<uint4*>(row) = make_uint4(c[0], c[1], c[2], c[3]);
+          else if constexpr (GP == 4) *reinterpret_cast<uint2*>(row) = make_uint2(c[0], c[1]);
+          else if constexpr (GP == 2) *reinterpret_cast<uint32_t*>(row) = __byte_perm(c[0], c[1], 0x5410);
+          else                        *reinterpret_cast<uint16_t*>(row) = (uint16_t)__byte_perm(c[0], c[1], 0x0040);
         }
         if (left < kTile) {
           // rows behind the last one hold whatever the page or the stage held before; the product runs over whole
