@@ -14,22 +14,25 @@
 // own factor; nothing in tensor memory is ever rescaled.
 //
 // Shape of the launch: two CTAs of eight warps per SM, no CTA waits for another one.  All (layer, sequence, KV head) caches
-// lie on one line, a cache as long as its blocks of 16 rows plus a constant for what a cache costs besides its bytes, and the
-// line is cut into equal segments, one per CTA, that every CTA derives for itself from the lengths.  A tile belongs to
+// lie on one line, a cache as long as the blocks of its tiles plus a constant for what a cache costs besides them (by tiles,
+// not by rows: 7168 caches of 84 to 157 rows with G = 7 take 107 us, by rows 116 us, other shapes the same), and the line
+// is cut into equal segments, one per CTA, that every CTA derives for itself from the lengths.  A tile belongs to
 // the segment in which it starts.  A cache cut by a boundary leaves partial results (m, l, O), at most two pieces a CTA, and
 // the CTA that finishes the last piece joins them in the order of the pieces, so the result does not depend on who
 // was when.  (Small segments at the ends of the shares that go to whoever is done first level the finishing times, but
 // what they add in pieces and joins costs more: 74.6 against 70.2 us for 363 MB, 150.8 against 140.2 us for 814 MB.)
 // Bound by HBM where caches are long, else by what a launch costs before the first and after the last byte (about 8 us: the
 // lengths, page ids and first tiles one after the other; the last tile's softmax, output, count and join).  Measured, device
-// time a call: 538 MB in two caches of 131 000 rows x 8 heads 93.3 us (0.88 of the measured copy rate; 7.4 TB/s between
-// the first tile and the last), 814 MB ragged batch 134.5 us (0.92), 363 MB of 2048 short caches 64.3 us (0.86), one request
-// of 2129 rows 12.7 us.
+// time a call: 538 MB in two caches of 131 000 rows x 8 heads 92.6 us (0.88 of the measured copy rate; 7.4 TB/s between
+// the first tile and the last), 814 MB ragged batch 133.5 us (0.93), 363 MB of 2048 short caches 63.8 us (0.87), one request
+// of 2129 rows 12.4 us.  With five to eight heads a group the softmax warps bound it where caches are short or d = 64 (a
+// third of the issue slots, the rest waits on what comes before): 246 MB in 7168 caches of 84-157 rows, G = 7, 107 us;
+// 214 MB of d = 64, G = 5, 53 us.
 //
 //   warp 6     finds the CTA's pieces of caches ("items") and lays out their queries as two codes per element
 //   warp 4     copies: TMA boxes of K and V, block scales
 //   warp 5     issues the MMAs: logits up to two tiles ahead of the outputs
-//   warps 0-3  one thread per cache row: logits out of tensor memory, the tile's maximum (one exchange among the four
+//   warps 0-3  one thread per cache row (two rows with d = 64): logits out of tensor memory, the tile's maximum (one exchange among the four
 //              warps), weights back as codes; then, as one thread per output column, O of the tile before
 //   warp 7     counts finished pieces of cut caches and joins those that are complete, by query heads; warps that
 //              have run out of tiles help
@@ -61,8 +64,8 @@ constexpr int kFifo = 3;              // items between the walk and the last rea
 constexpr int kCtasPerSm = 2;
 constexpr float kPart = 32.f;         // weight of the second code
 constexpr int kBarSoft = 1;           // named barrier of warps 0-3
-constexpr int kCacheCost = 12;        // what a cache costs besides its bytes, in blocks of 16 rows (2048 caches of 203 to 1101 rows:
-                                      // 66.6 us with 4, 64.9 with 8, 64.2 with 12, 64.9 with 16)
+constexpr int kCacheCost = 12;        // what a cache costs besides its tiles, in blocks of 16 rows (2048 caches of 203 to 1101 rows
+                                      // laid out by rows: 66.6 us with 4, 64.9 with 8, 64.2 with 12, 64.9 with 16)
 constexpr int kJobs = 32;             // joins a CTA may have open
 
 template <int D>
@@ -319,7 +322,10 @@ __device__ __forceinline__ int tiles_of(int rows) {
   return (rows + kTile - 1) / kTile;
 }
 // length of a cache on the line
-__device__ __forceinline__ int cost_of(int rows) { return rows > 0 ? (rows + kScaleBlock - 1) / kScaleBlock + kCacheCost : 0; }
+template <int D>
+__device__ __forceinline__ int cost_of(int rows) {
+  return rows > 0 ? tiles_of<D>(rows) * Cfg<D>::kTileBlocks + kCacheCost : 0;
+}
 
 // Caches that this CTA has found complete and is to join.
 struct Joins {
@@ -467,7 +473,7 @@ decode_e4m3_kernel(const __grid_constant__ CUtensorMap tmap_k, const __grid_cons
 #pragma unroll 8
   for (int i = 0; i < per; ++i) {
     const int e = tid * per + i;
-    if (e < p.n_units) mine += cost_of(unit_rows(p, e));
+    if (e < p.n_units) mine += cost_of<D>(unit_rows(p, e));
   }
   if (tid == 0) {
     for (int i = 0; i < C::kStages; ++i) {
@@ -531,7 +537,7 @@ decode_e4m3_kernel(const __grid_constant__ CUtensorMap tmap_k, const __grid_cons
     int at = my_begin;                            // this thread's run of units holds the begin or the end of the share
 #pragma unroll 1
     for (int i = 0; i < per; ++i) {
-      const int e = tid * per + i, rows = e < p.n_units ? unit_rows(p, e) : 0, cost = cost_of(rows), next = at + cost * Hkv;
+      const int e = tid * per + i, rows = e < p.n_units ? unit_rows(p, e) : 0, cost = cost_of<D>(rows), next = at + cost * Hkv;
       if (at <= begin && begin < next) s_first = make_int4(e, rows, at, 0);
       if (at <= stop_at && stop_at < next) {
         const int h = quotient(stop_at - at, cost), g0 = at + h * cost;
@@ -564,7 +570,7 @@ decode_e4m3_kernel(const __grid_constant__ CUtensorMap tmap_k, const __grid_cons
     Item guess = {-1, 0, 0, 0, 0, 0};
     if (works) {
       guess.e = s_first.x;
-      const int cost = cost_of(s_first.y), off = begin - s_first.z;
+      const int cost = cost_of<D>(s_first.y), off = begin - s_first.z;
       guess.row0 = (off - quotient(off, cost) * cost + kTileBlocks - 1) / kTileBlocks * kTile;
       guess.rows = s_first.y - guess.row0;
       if (s_end_cut.w > 0) {
@@ -721,7 +727,7 @@ decode_e4m3_kernel(const __grid_constant__ CUtensorMap tmap_k, const __grid_cons
     // ================================================================ the walk, and the queries as two codes per element
     int at = begin;                               // next position of the share
     int e = s_first.x, rows = s_first.y, unit_at = s_first.z;      // unit_at: where (e, head 0) begins
-    int cost = cost_of(rows), h = works ? quotient(begin - unit_at, cost) : 0;
+    int cost = cost_of<D>(rows), h = works ? quotient(begin - unit_at, cost) : 0;
     // The piece that the end of the share cuts comes first, then the one that its begin cuts, then the whole caches: counting
     // and joining pieces takes microseconds, which then lie under the copies of what follows.
     const int walk_end = s_end_cut.w > 0 ? s_end_cut.z : stop_at;
@@ -748,7 +754,7 @@ decode_e4m3_kernel(const __grid_constant__ CUtensorMap tmap_k, const __grid_cons
           h = 0;
           if (e >= p.n_units) return it;
           rows = unit_rows(p, e);
-          cost = cost_of(rows);
+          cost = cost_of<D>(rows);
         }
         const int g0 = unit_at + h * cost, nt = tiles_of<D>(rows);
         const int t0 = (at - g0 + kTileBlocks - 1) / kTileBlocks;                       // first tile that starts at or behind `at`
@@ -1225,7 +1231,7 @@ xkv_status decode_attn_e4m3(const xkv_dims* d, const xkv_cache* c, int layer_beg
     return XKV_ERR_CUDA;
   const int64_t max_rows = (int64_t)c->max_pages_per_seq * c->page_size;
   const int64_t caches = (int64_t)n_units * d->n_kv_heads, most = caches * ((max_rows + tile - 1) / tile);
-  if (caches * (max_rows / kScaleBlock + kCacheCost) >= (1ll << 31)) return XKV_ERR_UNSUPPORTED;
+  if (caches * ((max_rows + tile) / kScaleBlock + kCacheCost) >= (1ll << 31)) return XKV_ERR_UNSUPPORTED;
   xkv_status s;
   if (k_new != nullptr) {
     s = append_e4m3(d, c, layer_begin, n_units, k_new, v_new, ws.header, ws.clear, ws.n_clear, st);

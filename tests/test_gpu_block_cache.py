@@ -186,6 +186,27 @@ def test_decode_long_caches_are_split(chunk, H, G, d):
     assert torch.equal(out, again) and torch.equal(lse, lse2)
 
 
+@pytest.mark.parametrize("G", [1, 2, 3, 5, 8])
+def test_decode_tiles_of_narrow_heads(G):
+    """Heads of 64 elements: caches that end before, at and behind the middle and the end of a tile of 256 rows."""
+    pool = Pool([[383, 384, 385, 511, 512], [513, 640, 641, 769, 3969]], 2, 64, 48, seed=40 + G, big_k_row=600)
+    q = queries(2, 5, 2 * G, 64, 40 + G)
+    out, lse, st = run_decode(pool, 2 * G, q)
+    assert st == xkv.OK
+    check_all(pool, 2 * G, q, out, lse, pool.lens, what=f"G {G}")
+
+
+@pytest.mark.parametrize("G", [1, 7])
+def test_decode_many_caches_per_block(G):
+    """More caches than thread blocks, of one and of two tiles, so that queues of them run through every block."""
+    lens = [[84 + (37 * i + 11 * l) % 74 for i in range(12)] for l in range(3)]
+    pool = Pool(lens, 32, 128, 48, seed=50 + G)
+    q = queries(3, 12, 32 * G, 128, 50 + G)
+    out, lse, st = run_decode(pool, 32 * G, q)
+    assert st == xkv.OK
+    check_all(pool, 32 * G, q, out, lse, pool.lens, what=f"G {G}")
+
+
 def test_decode_small_weights_of_many_rows_count():
     """One row takes almost all of a tile's weight while thousands of rows far below it hold most of the mass."""
     n, d = 20000, 128
