@@ -452,7 +452,7 @@ decode_e4m3_kernel(const __grid_constant__ CUtensorMap tmap_k, const __grid_cons
       s_scale_full[C::kStages], s_s_full[2], s_p_full[2], s_d_full[2], s_fifo_full[kFifo], s_fifo_empty[kFifo],
       s_q_full[kFifo], s_done_full[kFifo], s_wake;
   __shared__ Item s_item[kFifo];
-  __shared__ float s_qscale[kFifo][8];
+  __shared__ __align__(16) float s_qscale[kFifo][8];              // heads from G on are never read for a result
   __shared__ __align__(16) float s_max[2][4][8];
   __shared__ __align__(16) float s_head[4][3][8];
   __shared__ __align__(16) float s_sum[2][16];    // reciprocal denominators, or (one or two heads) the warps' sums from [8] on
@@ -910,10 +910,10 @@ decode_e4m3_kernel(const __grid_constant__ CUtensorMap tmap_k, const __grid_cons
       float m[GP];                                               // four heads and more: m[0] of lane g is that of head g
 #pragma unroll
       for (int g = 0; g < GP; ++g) {
-        qs[g] = g < G ? s_qscale[slot][g] : 0.f;
         m[g] = -INFINITY;
         l[g] = acc[g] = f[g] = 0.f;
       }
+      get_heads<GP>(s_qscale[slot], qs);
       auto add_output = [&](uint32_t jd) {                       // O of tile jd
         wait_bar(&s_d_full[jd & 1], (jd / 2) & 1, s_abort, p.wait_ns);
         tc_fence_after_sync();
@@ -1064,39 +1064,43 @@ decode_e4m3_kernel(const __grid_constant__ CUtensorMap tmap_k, const __grid_cons
           }
         }
       }
-      add_output(j - 1);
-      // ---- denominators over the 128 rows' threads; the thread that has head g's also writes its statistics
+      // ---- denominators over the 128 rows' threads, while the last tile's output is on its way; the thread that has head
+      // g's also writes its statistics
       const size_t row0 = (size_t)it.e * p.n_q_heads + (size_t)it.h * G;
       const size_t piece = 2 * (size_t)blockIdx.x + ((int)blockIdx.x == it.first_cta ? 1 : 0);
-      const bool drop = *s_abort != 0;
       auto write_stats = [&](int g, float mg, float lg) {
         if (it.n_pieces > 1) __stcg(reinterpret_cast<float2*>(p.part_ml) + piece * G + g, make_float2(mg, lg));
-        else if (p.lse != nullptr && !drop) p.lse[row0 + g] = (mg + __log2f(lg)) * 0.6931471805599453f;
+        else if (p.lse != nullptr && !*s_abort) p.lse[row0 + g] = (mg + __log2f(lg)) * 0.6931471805599453f;
       };
       float* sum_at = s_sum[n_item & 1];
       if constexpr (GP >= 4) {
-        // through shared memory (the weights' buffers, which no product reads any more): 128 / GP threads a head.  (What
+        // Through shared memory (the weights' buffer that the last tile does not use): 128 / GP threads a head.  (What
         // runs once an item runs out of a cold instruction cache: shuffles of every head take four times the code.)
-        constexpr int kPer = 128 / GP;
-        float* part = reinterpret_cast<float*>(smem + C::kOffP);
+        constexpr int kPer = 128 / GP, kRow = GP == 8 ? 64 : 128;
+        static_assert(GP * kRow * 4 <= C::kPBytes && kRow == 4 * kPer, "fits, four values a thread");
+        float* part = reinterpret_cast<float*>(smem + C::kOffP + (j & 1) * C::kPBytes);
+        if constexpr (GP == 8) {                                  // each half of a warp takes four heads of both
+          const bool upper = lane >= 16;
 #pragma unroll
-        for (int g = 0; g < GP; ++g) part[g * 128 + tid] = l[g];
+          for (int g = 0; g < 4; ++g) {
+            const float theirs = __shfl_xor_sync(0xffffffffu, upper ? l[g] : l[(g + 4) % GP], 16);
+            part[(g + (upper ? 4 : 0)) * kRow + warp * 16 + (lane & 15)] = (upper ? l[(g + 4) % GP] : l[g]) + theirs;
+          }
+        } else {
+#pragma unroll
+          for (int g = 0; g < GP; ++g) part[g * kRow + tid] = l[g];
+        }
         if (lane < GP) s_head[warp][0][lane] = m[0];
         named_bar_sync(kBarSoft, kSoftThreads);
         const int g = tid / kPer;
-        float x = 0.f;
-#pragma unroll
-        for (int k = 0; k < GP; k += 4) {
-          const float4 v = *reinterpret_cast<const float4*>(part + g * 128 + tid % kPer * GP + k);
-          x += (v.x + v.y) + (v.z + v.w);
-        }
+        const float4 v = *reinterpret_cast<const float4*>(part + 4 * tid);
+        float x = (v.x + v.y) + (v.z + v.w);
 #pragma unroll
         for (int o = kPer / 2; o > 0; o >>= 1) x += __shfl_xor_sync(0xffffffffu, x, o);
         if (tid % kPer == 0 && g < G) {
           sum_at[g] = fast_rcp(x);
           write_stats(g, s_head[warp][0][g], x);
         }
-        named_bar_sync(kBarSoft, kSoftThreads);
       } else {
 #pragma unroll
         for (int g = 0; g < GP; ++g) {
@@ -1104,7 +1108,11 @@ decode_e4m3_kernel(const __grid_constant__ CUtensorMap tmap_k, const __grid_cons
           for (int o = 16; o > 0; o >>= 1) l[g] += __shfl_xor_sync(0xffffffffu, l[g], o);
           if (lane == 0) sum_at[8 + 4 * g + warp] = l[g];
         }
-        named_bar_sync(kBarSoft, kSoftThreads);
+      }
+      add_output(j - 1);
+      const bool drop = *s_abort != 0;
+      named_bar_sync(kBarSoft, kSoftThreads);
+      if constexpr (GP < 4) {
 #pragma unroll
         for (int g = 0; g < GP; ++g) {
           const float4 v = *reinterpret_cast<const float4*>(sum_at + 8 + 4 * g);
