@@ -26,7 +26,7 @@
 // time a call: 538 MB in two caches of 131 000 rows x 8 heads 92.8 us (0.88 of the measured copy rate; 7.4 TB/s between
 // the first tile and the last), 814 MB ragged batch 133.5 us (0.93), 363 MB of 2048 short caches 63.8 us (0.87), one request
 // of 2129 rows 12.4 us.  With five to eight heads a group the softmax warps bound it where caches are short or d = 64 (a
-// third of the issue slots, the rest waits on what comes before): 246 MB in 7168 caches of 84-157 rows, G = 7, 106 us;
+// third of the issue slots, the rest waits on what comes before): 246 MB in 7168 caches of 84-157 rows, G = 7, 103 us;
 // 214 MB of d = 64, G = 5, 53 us.
 //
 //   warp 6     finds the CTA's pieces of caches ("items") and lays out their queries as two codes per element
@@ -951,7 +951,8 @@ decode_e4m3_kernel(const __grid_constant__ CUtensorMap tmap_k, const __grid_cons
             for (int g = 0; g < GP; ++g) s[x][g] = -INFINITY;
           }
         }
-        // (heads from G on are left out by uniform branches: their columns hold nothing that is read)
+        // (heads from G on: no maximum, weight 0, codes 0; a branch a pair of heads would keep the codes of all pairs apart,
+        // 106 against 103 us for 7168 caches with G = 7)
 #pragma unroll
         for (int g = 0; g < GP; ++g) {
           mt[g] = s[0][g];
@@ -1000,7 +1001,6 @@ decode_e4m3_kernel(const __grid_constant__ CUtensorMap tmap_k, const __grid_cons
           uint32_t c[GP < 4 ? 2 : GP / 2] = {};                   // pairs of first codes, then of second codes
 #pragma unroll
           for (int g = 0; g < GP; g += 2) {
-            if (g >= G) break;
             const float a = s[x][g] * vr, b = GP > 1 ? s[x][g + (GP > 1)] * vr : 0.f;
             const uint32_t c1 = e4m3x2_from_f32(a, b);
             const float2 y = f32_from_e4m3x2(c1);
