@@ -611,6 +611,28 @@ def test_plan_append(L, B, page, hi, new_hi, per_layer):
         check_plan(want, *got)
 
 
+@pytest.mark.parametrize("page", [16, 48, 256])
+@pytest.mark.parametrize("pad", [0, 1, 2, 7])
+def test_plan_append_prompts(page, pad):
+    """Long stretches of one sequence, from odd and even rows on, into slot maps whose layers begin at odd and even places."""
+    lens = np.array([[0, 1, 15, 16, 33, 7], [2, 0, 31, 5, 16, 48], [1, 1, 1, 1, 1, 1]])
+    new = np.array([[700, 1, 901, 64, 2000, 65], [63, 3001, 0, 130, 257, 511], [1000, 999, 129, 128, 127, 3]])
+    cols = -(-(48 + 3001) // page) + 1
+    n_pages = int((-(-(lens + new) // page)).sum()) + 3
+    free = np.random.default_rng(page + pad).permutation(n_pages)
+    for kw in (dict(free=free), dict(free=None), dict(free=free, slots_stride=int(new.sum(1).max()) + pad)):
+        want, *got, status = plan(lens, new, page, cols, n_pages, used=0, **kw)
+        assert status == xkv.OK and want[4]
+        check_plan(want, *got)
+    # an id outside the pool in the middle of a stretch: no slot for its rows, the others as they were
+    free[20 if page == 16 else 2] = n_pages + 5
+    want, *_, slots, used, status = plan(lens, new, page, cols, n_pages, used=0, free=free)
+    assert status == xkv.ERR_INVALID_ARG
+    for l, row in enumerate(np.asarray(r) for r in want[2]):
+        assert np.array_equal(slots[l, :len(row)], np.where(row >= n_pages * page, -1, row))
+    assert any(r >= n_pages * page for row in want[2] for r in row)
+
+
 def test_plan_append_runs_out_of_pages():
     lens = np.array([[16, 10, 31, 0], [5, 16, 0, 64]])
     new = np.array([1, 6, 20, 16])
