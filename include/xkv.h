@@ -369,13 +369,13 @@ xkv_status xkv_build_block_table(const int32_t* first_page, const int32_t* n_pag
  * free_pages    dev int32 [n_free], the pages that may be handed out, in the order they are; NULL: pages 0 .. n_free-1
  * pages_used_before  dev int32 [1], entries of the list handed out so far; NULL: none. pages_used_after: dev out int32
  *               [1], may be NULL or the same pointer
- * slots         dev out int64, row l at slots + l * slots_stride; NULL: not wanted. Entries behind a layer's last token
- *               stay as they are
+ * slots         dev out int64, row l at slots + l * slots_stride, slots_stride below 2^31 - 1; NULL: not wanted. Entries
+ *               behind a layer's last token stay as they are
  * workspace     dev, at least xkv_workspace_bytes(XKV_OP_PLAN_APPEND, dims.batch = batch, n_layers) bytes, 256-byte aligned
  * A cache that cannot grow (more rows than max_pages_per_seq pages hold, or the free list ends) keeps its length, gets no
  * page and its tokens get slot -1; device status XKV_ERR_CAPACITY, also when a layer has more new tokens than
- * slots_stride. Negative counts are taken as 0 and page ids outside [0, n_pages) give slot -1; device status
- * XKV_ERR_INVALID_ARG. At most 16384 sequences a layer.
+ * slots_stride (those behind the map get pages where their cache can grow, and no slot). Negative counts are taken as 0
+ * and page ids outside [0, n_pages) give slot -1; device status XKV_ERR_INVALID_ARG. At most 16384 sequences a layer.
  */
 xkv_status xkv_plan_append(const xkv_cache* cache, int32_t batch, const int32_t* n_new, int32_t n_new_stride,
                            const int32_t* lens_before, const int32_t* free_pages, int32_t n_free,

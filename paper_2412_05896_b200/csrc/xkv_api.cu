@@ -249,7 +249,7 @@ xkv_status xkv_plan_append(const xkv_cache* cache, int32_t batch, const int32_t*
   if (s != XKV_OK) return s;
   if ((int64_t)cache->max_pages_per_seq * cache->page_size > (1 << 30)) return XKV_ERR_INVALID_ARG;
   if (n_new_stride != 0 && n_new_stride < batch) return XKV_ERR_INVALID_ARG;
-  if (slots != nullptr && (slots_stride <= 0 || slots_stride >= (1ll << 31))) return XKV_ERR_INVALID_ARG;
+  if (slots != nullptr && (slots_stride <= 0 || slots_stride >= (1ll << 31) - 1)) return XKV_ERR_INVALID_ARG;
   if (batch > plan_max_batch() || cache->n_layers > 65535 || (int64_t)batch * cache->n_layers >= (1ll << 31))
     return XKV_ERR_UNSUPPORTED;
   if (workspace_bytes < plan_workspace_bytes(cache->n_layers, batch)) return XKV_ERR_WORKSPACE;

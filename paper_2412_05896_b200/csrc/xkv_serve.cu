@@ -102,7 +102,7 @@ constexpr int kRounds = 8;                    // tokens a lane takes at a time
 template <bool kAll, class Id>
 __device__ __forceinline__ void write_batch(const PlanParams& p, int32_t* row, int64_t* out, int t, int end, int shift, Id id) {
   const int lane = threadIdx.x & 31;
-  const int pos0 = t + lane + shift, n = end - t - lane;          // rounds 32 k < n of this lane hold a token
+  const int pos0 = t + shift + lane, n = end - t - lane;          // rounds 32 k < n of this lane hold a token
   int64_t* dst = out + t + lane;
   int page[kRounds];
   uint32_t top = 0;
@@ -134,17 +134,17 @@ template <class Id>
 __device__ __forceinline__ void write_stretch(const PlanParams& p, int32_t* row, int64_t* out, int t, int end, int shift,
                                               Id id) {
 #pragma unroll 1
-  for (; t + 32 * kRounds <= end; t += 32 * kRounds) write_batch<true>(p, row, out, t, end, shift, id);
+  for (; end - t >= 32 * kRounds; t += 32 * kRounds) write_batch<true>(p, row, out, t, end, shift, id);
   if (t < end) write_batch<false>(p, row, out, t, end, shift, id);
 }
 
-// The new tokens [t, t_end) of a layer (a whole warp): their slots, and the table entries of the pages that begin with one
-// of them (every new page begins with a new token).  tok(b): tokens of the layer before sequence b (b <= batch),
-// start(b): where its new pages begin in the free list (-1: it cannot grow), len(b): its rows before the step.  The
-// layer's first n_slots tokens have a place in `out`.
+// The new tokens [t, t_end) of a layer (a whole warp), all of which have a place in `out`: their slots, and the table
+// entries of the pages that begin with one of them (every new page begins with a new token).  tok(b): tokens of the layer
+// before sequence b (b <= batch; more than 2^31 - 1 count as that many), start(b): where its new pages begin in the free
+// list (-1: it cannot grow), len(b): its rows before the step.  t_end may be 2^31 - 1: no token number behind it is formed.
 template <class Tok, class Start, class Len>
-__device__ __forceinline__ void write_range(const PlanParams& p, int32_t* table, int64_t* out, int t, int t_end, int n_slots,
-                                            Tok tok, Start start, Len len) {
+__device__ __forceinline__ void write_range(const PlanParams& p, int32_t* table, int64_t* out, int t, int t_end, Tok tok,
+                                            Start start, Len len) {
   const int lane = threadIdx.x & 31;
   constexpr int kMix = 2;
   auto search = [&](int lo, int x) -> int {    // the sequence that holds token x; lo: one at or before it
@@ -160,7 +160,7 @@ __device__ __forceinline__ void write_range(const PlanParams& p, int32_t* table,
 #pragma unroll 1
   while (t < t_end) {
     const int seq_end = (int)min((long long)tok(lo + 1), (long long)t_end);
-    if (seq_end - t >= 32 * kMix && seq_end <= n_slots && start(lo) >= 0) {
+    if (seq_end - t >= 32 * kMix && start(lo) >= 0) {
       // a stretch of one sequence (prompts), in new pages: the page ids of eight rounds in flight together
       const int n = len(lo), shift = n - (int)tok(lo), have = p.page_of(n + p.page_size - 1), first = start(lo) - have;
       if (t + shift >= have * p.page_size) {
@@ -173,13 +173,14 @@ __device__ __forceinline__ void write_range(const PlanParams& p, int32_t* table,
       }
     }
     // any mixture: every lane its own search (a decode step has one token per sequence)
+    const int left = t_end - t;
     int seq[kMix], page[kMix];
 #pragma unroll
     for (int k = 0; k < kMix; ++k) {
-      const int at = t + 32 * k + lane;
       seq[k] = -1;
       page[k] = -1;
-      if (at < t_end) {
+      if (32 * k + lane < left) {
+        const int at = t + 32 * k + lane;
         if (tok(lo + 1) <= at) lo = search(lo, at);
         const int st = start(lo);
         if (st >= 0) {
@@ -191,6 +192,7 @@ __device__ __forceinline__ void write_range(const PlanParams& p, int32_t* table,
     }
 #pragma unroll
     for (int k = 0; k < kMix; ++k) {
+      if (32 * k + lane >= left) continue;
       const int at = t + 32 * k + lane, b = seq[k];
       int64_t slot = -1;
       if (b >= 0) {
@@ -199,10 +201,11 @@ __device__ __forceinline__ void write_range(const PlanParams& p, int32_t* table,
         if ((unsigned)page[k] < (unsigned)p.n_pages) slot = (int64_t)page[k] * p.page_size + in_page;
         else record_status(p.hdr, XKV_ERR_INVALID_ARG);
       }
-      if (at < min(t_end, n_slots)) out[at] = slot;
+      out[at] = slot;
     }
+    if (left <= 32 * kMix) break;
     t += 32 * kMix;
-    if (t < t_end) lo = search(__shfl_sync(0xffffffffu, lo, 0), t);
+    lo = search(__shfl_sync(0xffffffffu, lo, 0), t);
   }
 }
 
@@ -308,16 +311,17 @@ __global__ void __launch_bounds__(kPlanThreads) plan_kernel(const PlanParams p) 
     int64_t* out = p.slots + layer * p.slots_stride;
     const int32_t* lens = p.lens_before != nullptr ? p.lens_before + (size_t)layer * p.batch : nullptr;
     // every warp one stretch: it looks up a sequence once and finds its page ids in the L1 cache
-    const int64_t stretch = ((int64_t)total + n_slices * kWarps - 1) / (n_slices * kWarps);
+    const int64_t stretch = ((int64_t)n_slots + n_slices * kWarps - 1) / (n_slices * kWarps);
     const int64_t t0 = (slice * kWarps + warp) * stretch;
-    write_range(p, table, out, (int)min(t0, (int64_t)total), (int)min(t0 + stretch, (int64_t)total), n_slots,
+    write_range(p, table, out, (int)min(t0, (int64_t)n_slots), (int)min(t0 + stretch, (int64_t)n_slots),
                 [&](int b) { return s_tok[b]; }, [&](int b) { return s_start[b]; },
                 [&](int b) { return lens != nullptr ? max(lens[b], 0) : 0; });
-  } else {
-    // ---- the new table entries: a warp per sequence
+  }
+  if (p.slots == nullptr || s_tok[p.batch] > p.slots_stride) {
+    // ---- the new table entries of sequences that have tokens without a place in the slot map: a warp per sequence
     for (int b = slice * kWarps + warp; b < p.batch; b += n_slices * kWarps) {
       const int start = s_start[b];
-      if (start < 0) continue;
+      if (start < 0 || (p.slots != nullptr && s_tok[b + 1] <= p.slots_stride)) continue;
       const Ask a = plan_ask(p, layer, layer * p.batch + b, b);
       write_pages(p, table + (size_t)b * p.max_pages_per_seq + p.page_of(a.len + p.page_size - 1), a.pages, start);
     }
@@ -423,23 +427,6 @@ __global__ void __launch_bounds__(kSmallThreads) plan_small_kernel(const PlanPar
   }
   end_max = (int)__reduce_max_sync(0xffffffffu, (unsigned)end_max);
   if (lane == 0) s_end[warp] = end_max;
-  if (p.slots == nullptr) {
-    // the new table entries: a warp one sequence after the other
-#pragma unroll
-    for (int i = 0; i < kPer; ++i) {
-      const int e = tid * per + i;
-      const int pages = max(a[i].pages, 0);
-      int32_t* at = p.block_table + (size_t)e * p.max_pages_per_seq + p.page_of(a[i].len + p.page_size - 1);
-      unsigned todo = __ballot_sync(0xffffffffu, pages > 0);
-      const int st = pages > 0 ? s_start[e] : 0;
-      while (todo != 0) {
-        const int w = __ffs(todo) - 1;
-        todo &= todo - 1;
-        write_pages(p, reinterpret_cast<int32_t*>(__shfl_sync(0xffffffffu, reinterpret_cast<unsigned long long>(at), w)),
-                    __shfl_sync(0xffffffffu, pages, w), __shfl_sync(0xffffffffu, st, w));
-      }
-    }
-  }
   bool few = true;                            // no cache takes more than kStepTokens
 #pragma unroll
   for (int i = 0; i < kPer; ++i) few = few && a[i].add <= kStepTokens;
@@ -449,7 +436,32 @@ __global__ void __launch_bounds__(kSmallThreads) plan_small_kernel(const PlanPar
     for (int w = 1; w < 32; ++w) end = max(end, s_end[w]);
     *p.used_after = end;
   }
-  if (p.slots == nullptr) return;
+  bool over = false;                          // a layer has more tokens than its slot map (every warp finds out by itself)
+  if (p.slots != nullptr) {
+    for (int l = lane; l < p.n_layers; l += 32) over |= s_tok64[(l + 1) * p.batch] - s_tok64[l * p.batch] > p.slots_stride;
+    over = __any_sync(0xffffffffu, over) != 0;
+  }
+  if (p.slots == nullptr || over) {
+    // the new table entries of sequences that have tokens without a place in the slot map: a warp one after the other
+#pragma unroll
+    for (int i = 0; i < kPer; ++i) {
+      const int e = tid * per + i;
+      const bool mine = i < per && e < n_units &&
+                        (p.slots == nullptr || s_tok64[e] + a[i].add - s_tok64[e / p.batch * p.batch] > p.slots_stride);
+      const int pages = mine ? max(a[i].pages, 0) : 0;
+      int32_t* at = p.block_table;
+      if (pages > 0) at += (size_t)e * p.max_pages_per_seq + p.page_of(a[i].len + p.page_size - 1);
+      unsigned todo = __ballot_sync(0xffffffffu, pages > 0);
+      const int st = pages > 0 ? s_start[e] : 0;
+      while (todo != 0) {
+        const int w = __ffs(todo) - 1;
+        todo &= todo - 1;
+        write_pages(p, reinterpret_cast<int32_t*>(__shfl_sync(0xffffffffu, reinterpret_cast<unsigned long long>(at), w)),
+                    __shfl_sync(0xffffffffu, pages, w), __shfl_sync(0xffffffffu, st, w));
+      }
+    }
+    if (p.slots == nullptr) return;
+  }
   if (few && !p.two_launches) {
     // a decode step: every thread the tokens of its own caches, all page ids in flight together
     int page[kPer][kStepTokens];
@@ -492,26 +504,19 @@ __global__ void __launch_bounds__(kSmallThreads) plan_small_kernel(const PlanPar
     }
     return;
   }
-  // The layers' runs, dealt out to the warps: first those that the slot maps have room for, then, where a layer has more
-  // tokens than that (the status says so), the others: they still get their pages.
+  // the runs of the layers' slot maps, dealt out to the warps
   const int runs = (int)((p.slots_stride + kSlotRun - 1) / kSlotRun);
-  auto do_run = [&](int l, int r) {
-    const int e0 = l * p.batch;
-    const long long first = s_tok64[e0];
-    const int total = (int)min(s_tok64[e0 + p.batch] - first, 0x7fffffffll);
+#pragma unroll 1
+  for (int w = warp; w < p.n_layers * runs; w += kSmallThreads / 32) {
+    const int l = w / runs, r = w % runs, e0 = l * p.batch;
+    const long long first = s_tok64[e0], total = s_tok64[e0 + p.batch] - first;
     if (r == 0 && lane == 0 && total > p.slots_stride) record_status(p.hdr, XKV_ERR_CAPACITY);
-    if ((long long)r * kSlotRun >= total) return false;
+    const int n_slots = (int)min(total, (long long)p.slots_stride);
+    if (r * kSlotRun >= n_slots) continue;
     write_range(p, p.block_table + (size_t)e0 * p.max_pages_per_seq, p.slots + l * p.slots_stride, r * kSlotRun,
-                min((r + 1) * kSlotRun, total), (int)min((int64_t)total, p.slots_stride), [&](int b) { return s_tok64[e0 + b] - first; },
+                min((r + 1) * kSlotRun, n_slots), [&](int b) { return s_tok64[e0 + b] - first; },
                 [&](int b) { return s_start[e0 + b]; }, [&](int b) { return s_len[e0 + b]; });
-    return true;
-  };
-#pragma unroll 1
-  for (int w = warp; w < p.n_layers * runs; w += kSmallThreads / 32) do_run(w / runs, w % runs);
-#pragma unroll 1
-  for (int l = warp; l < p.n_layers; l += kSmallThreads / 32)
-    for (int r = runs; do_run(l, r); ++r) {
-    }
+  }
 }
 
 // Slots and new table entries from what plan_small_kernel found.  grid = (slices, layers), a stretch of tokens per warp.
@@ -532,10 +537,10 @@ __global__ void __launch_bounds__(kPlanThreads) slots_kernel(const PlanParams p)
   __syncthreads();
   const int total = s_tok[p.batch], n_slots = (int)min((int64_t)total, p.slots_stride);
   if (blockIdx.x == 0 && tid == 0 && total > p.slots_stride) record_status(p.hdr, XKV_ERR_CAPACITY);
-  const int64_t stretch = ((int64_t)total + n_warps - 1) / n_warps;
+  const int64_t stretch = ((int64_t)n_slots + n_warps - 1) / n_warps;
   const int64_t t0 = (blockIdx.x * (kPlanThreads / 32) + (tid >> 5)) * stretch;
   write_range(p, p.block_table + (size_t)layer * p.batch * p.max_pages_per_seq, p.slots + layer * p.slots_stride,
-              (int)min(t0, (int64_t)total), (int)min(t0 + stretch, (int64_t)total), n_slots,
+              (int)min(t0, (int64_t)n_slots), (int)min(t0 + stretch, (int64_t)n_slots),
               [&](int b) { return s_tok[b]; }, [&](int b) { return s_start[b]; }, [&](int b) { return s_len[b]; });
 }
 
