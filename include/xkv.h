@@ -128,8 +128,10 @@ typedef struct xkv_dims {
  * raise it, the earlier rows' codes are re-expressed in the new scale, which is exact except for codes that fall below
  * 2^-6 (their step is 2^-9). The slots of a block are filled in ascending order: a row stored at the block's first slot
  * starts the block anew, whatever its scale was. xkv_decode_attn multiplies codes on the tensor cores as they are, with
- * fp32 accumulation: the query as a sum of two codes (exact for bf16 values within 2^-14 of the row's largest), the
- * weights as a sum of two codes (2^-8 of a weight, as if rounded to bf16). head_dim 64 and 128.
+ * fp32 accumulation: the query as a sum of two codes (exact for bf16 values within 2^-14 of the row's largest, 2^-22 of
+ * that largest below), a weight times its row's V scale as a sum of two codes (2^-8 of it, as if rounded to bf16, down to
+ * 2^-15 of the largest such product in its tile, 128 rows or 256 of 64 elements; 2^-23 of that product below; V scales below
+ * 2^-80 of a tile's largest count as that when the largest product is looked for). head_dim 64 and 128.
  *
  * Head-level budgets (XKV_BUDGET_PER_HEAD) give every KV head of a sequence a cache of its own length. The same
  * structure then describes B*Hkv caches of one KV head each per layer:

@@ -8,10 +8,12 @@
 // are K-major, V rows are M-major), fp32 accumulators in tensor memory.  The small operand has more bits than one code
 // holds, so it enters as two codes side by side on the N axis: q = a1 + a2 / 32 and p = b1 + b2 / 32, each part rounded to
 // nearest.  The query is scaled so that its largest element lies in [128, 256): a bf16 value (8 significant bits) is
-// exactly such a sum down to 2^-15, 2^-22 of the largest.  The weights of a tile are scaled so that its largest possible
-// one is 256: the sum keeps 2^-8 of a weight (the rounding of bf16) down to 2^-15, 2^-23 of the tile's largest.  Because that
-// range is per tile, every tile's product goes to fresh accumulators and is added in fp32 registers with the tile's
-// own factor; nothing in tensor memory is ever rescaled.
+// exactly such a sum down to 2^-15, 2^-22 of the largest.  The products s_v P of a tile are scaled so that the largest is 256:
+// the sum keeps 2^-8 of one (the rounding of bf16) down to 2^-15, 2^-23 of the tile's largest.  For that the softmax's
+// reference is not the tile's largest logit but its largest S + log2(s_v / max s_v), whichever row has it (a row of a large s_v and
+// no weight costs the others no bits); a weight may then exceed 1, by 2^80 at most, to where s_v / max s_v counts in it.
+// Because the range is per tile, every tile's product goes to fresh accumulators and is added in fp32 registers with the
+// tile's own factor; nothing in tensor memory is ever rescaled.
 //
 // Shape of the launch: two CTAs of eight warps per SM, no CTA waits for another one.  All (layer, sequence, KV head) caches
 // lie on one line, a cache as long as the blocks of its tiles plus a constant for what a cache costs besides them (by tiles,
@@ -63,6 +65,7 @@ constexpr int kSoftThreads = 128;
 constexpr int kFifo = 3;              // items between the walk and the last reader
 constexpr int kCtasPerSm = 2;
 constexpr float kPart = 32.f;         // weight of the second code
+constexpr float kMinShare = -80.f;    // log2 of the smallest s_v / max s_v of a tile that counts in the softmax's reference
 constexpr int kBarSoft = 1;           // named barrier of warps 0-3
 constexpr int kCacheCost = 12;        // what a cache costs besides its tiles, in blocks of 16 rows (2048 caches of 203 to 1101 rows
                                       // laid out by rows: 66.6 us with 4, 64.9 with 8, 64.2 with 12, 64.9 with 16)
@@ -930,10 +933,10 @@ decode_e4m3_kernel(const __grid_constant__ CUtensorMap tmap_k, const __grid_cons
         wait_bar(&s_scale_full[stage], (j / C::kStages) & 1, s_abort, p.wait_ns);
         const float* sc = reinterpret_cast<const float*>(smem + C::kOffScales) + stage * 2 * kTileBlocks;
         const float vmax = fmaxf(warp_max(sc[kTileBlocks + lane % kTileBlocks]), 0x1p-110f);
-        const float to_code = 256.f * fast_rcp(vmax);
+        const float inv_vmax = fast_rcp(vmax);
         wait_bar(&s_s_full[j & 1], (j / 2) & 1, s_abort, p.wait_ns);
         tc_fence_after_sync();
-        float s[C::kSpans][GP], mt[GP];                           // logits, then weights, of rows tid and tid + 128
+        float s[C::kSpans][GP], mt[GP];                           // logits, then weights, of rows tid and tid + 128; the reference
 #pragma unroll
         for (int x = 0; x < C::kSpans; ++x) {
           const bool live = x * 128 + tid < left;
@@ -941,10 +944,12 @@ decode_e4m3_kernel(const __grid_constant__ CUtensorMap tmap_k, const __grid_cons
             float r[2 * GP];
             tmem_ld<2 * GP>(tmem + ((j & 1) * C::kSpans + x) * kN + lane_base, r);
             const float ks = sc[x * 8 + blk];
+            const float share = fmaxf(__log2f(sc[kTileBlocks + x * 8 + blk] * inv_vmax), kMinShare);
 #pragma unroll
             for (int g = 0; g < GP; ++g) {
               s[x][g] = fmaf(r[GP + g], 1.f / kPart, r[g]) * (ks * qs[g]);
               if (!live) s[x][g] = -INFINITY;
+              mt[g] = x == 0 ? s[x][g] + share : fmaxf(mt[g], s[x][g] + share);
             }
           } else {
 #pragma unroll
@@ -954,17 +959,13 @@ decode_e4m3_kernel(const __grid_constant__ CUtensorMap tmap_k, const __grid_cons
         // (heads from G on: no maximum, weight 0, codes 0; a branch a pair of heads would keep the codes of all pairs apart,
         // 106 against 103 us for 7168 caches with G = 7)
 #pragma unroll
-        for (int g = 0; g < GP; ++g) {
-          mt[g] = s[0][g];
-#pragma unroll
-          for (int x = 1; x < C::kSpans; ++x) mt[g] = fmaxf(mt[g], s[x][g]);
-          mt[g] = g < G ? warp_max(mt[g]) : 0.f;
-        }
+        for (int g = 0; g < GP; ++g) mt[g] = g < G ? warp_max(mt[g]) : 0.f;
         if (lane == 0) put_heads<GP>(s_max[j & 1][warp], mt);
         named_bar_sync(kBarSoft, kSoftThreads);
-        // The tile's maximum of a head, and how the running sums move to the new reference maximum: for four heads and more
-        // lane g works for head g and hands the results round (the same arithmetic in every thread is six times the code).
-        bool grows_any;                                           // the reference maximum of some head has grown
+        // The tile's reference of a head, and how the running sums move to the new running reference, the largest so far: for
+        // four heads and more lane g works for head g and hands the results round (the same arithmetic in every thread is six
+        // times the code).
+        bool grows_any;                                           // the running reference of some head has grown
         if constexpr (GP >= 4) {
           bool grows = false;
           if (lane < GP) {
@@ -986,13 +987,13 @@ decode_e4m3_kernel(const __grid_constant__ CUtensorMap tmap_k, const __grid_cons
             mt[g] = fmaxf(fmaxf(s_max[j & 1][0][g], s_max[j & 1][1][g]), fmaxf(s_max[j & 1][2][g], s_max[j & 1][3][g]));
           grows_any = true;
         }
-        // weights relative to the tile's maximum; the codes also carry the V scale relative to the tile's largest
+        // weights relative to the tile's reference; the codes also carry the V scale relative to the tile's largest
         uint8_t* pb = smem + C::kOffP + (j & 1) * C::kPBytes;
         float w[GP];                                              // sum of the weights of this thread's rows
 #pragma unroll
         for (int x = 0; x < C::kSpans; ++x) {
           if (x > 0 && left <= 128 * x) break;                    // the output's product does not reach this span
-          const float vr = sc[kTileBlocks + x * 8 + blk] * to_code;
+          const float vr = sc[kTileBlocks + x * 8 + blk] * inv_vmax * 256.f;
 #pragma unroll
           for (int g = 0; g < GP; ++g) {
             s[x][g] = g < G ? fast_exp2(s[x][g] - mt[g]) : 0.f;
@@ -1032,7 +1033,7 @@ decode_e4m3_kernel(const __grid_constant__ CUtensorMap tmap_k, const __grid_cons
         __syncwarp();
         if (lane == 0) mbar_arrive(&s_p_full[j & 1]);
         if (t > 0) add_output(j - 1);
-        // on to the new reference maximum
+        // on to the new running reference
         if constexpr (GP >= 4) {
           float fw[GP];
           if (grows_any) {

@@ -1,12 +1,15 @@
 """Serving on a reduced cache at the edges of what the entry points document."""
+import math
+
 import numpy as np
 import pytest
+import torch
 
 from oracle import xkv_oracle as O
 from paper_2412_05896_b200 import xkv
 
-from gpu_util import require_lib
-from test_gpu_block_cache import check_plan, plan
+from gpu_util import f64, require_lib
+from test_gpu_block_cache import BF16_HALF, DEV, Pool, check_plan, plan, queries, run_decode
 
 pytestmark = pytest.mark.gpu
 
@@ -53,3 +56,87 @@ def test_plan_append_pages_of_tokens_behind_the_slot_map(L, B, stride):
     want, *got, status = plan(lens, new, page, cols, n_pages, used=0, slots_stride=stride, free=rng.permutation(n_pages))
     assert status == xkv.ERR_CAPACITY and want[4]
     check_plan(want, *got)
+
+
+# ------------------------------------------------------------------ V scales far apart
+def check_products(q, K, codes, scales, out, lse, what):
+    """One head's output where a cache's V scales differ: V = codes * scales[:, None].
+
+    As check_decode, but the bound's floor goes by the weights times their rows' scales, not by the largest |V|: such a
+    product enters as two codes, within 2^-8 of itself or, where it is small, within half a step of the smallest second
+    code, 2^-10 / 32 in units of which 256 stand for the tile's largest product: 2^-23 of that."""
+    z = K @ q / math.sqrt(len(q))
+    m = z.max()
+    p = np.exp(z - m)
+    y = p * scales
+    ref = (y @ codes) / p.sum()
+    mag = (y @ np.abs(codes)) / p.sum()
+    absqk = np.abs(K) @ np.abs(q) / math.sqrt(len(q))
+    dz = (len(q) + 8) * 2.0 ** -23 * absqk.max() + 2.0 ** -21 * np.abs(q).max() * np.abs(K).sum(1).max() / math.sqrt(len(q))
+    floor = 2.0 ** -23 * y.max() * np.abs(codes).sum(0) / p.sum()
+    bound = (2 * dz + BF16_HALF + 2.0 ** -20) * mag + floor + BF16_HALF * np.abs(ref) + 1e-35
+    assert np.all(np.isfinite(out)), what
+    worst = (np.abs(out - ref) / bound).max()
+    assert worst <= 1.0, f"{what}: {worst:.3f} of the bound"
+    want = m + math.log(p.sum())
+    assert abs(lse - want) <= dz + 2.0 ** -21 * (1 + abs(want)), f"{what}: lse {lse} for {want}"
+
+
+def check_scales(pool, Hq, q, out, lse, what):
+    G, qf, of, lf = Hq // pool.H, f64(q), f64(out), f64(lse)
+    s = pool.dev_s["v"].cpu().numpy().astype(np.float64)
+    for l in range(pool.L):
+        for b in range(pool.B):
+            n = np.arange(int(pool.lens[l, b]))
+            for g in range(pool.H):
+                sv = s[pool.table[l, b, n // pool.page], g, n % pool.page // 16]
+                K, V = pool.rows("k", l, b, g, len(n)), pool.rows("v", l, b, g, len(n))
+                codes = V / np.where(sv > 0, sv, 1.0)[:, None]
+                for h in range(g * G, (g + 1) * G):
+                    check_products(qf[l, b, h], K, codes, sv, of[l, b, h], lf[l, b, h], f"{what} l{l} b{b} h{h}")
+
+
+@pytest.mark.parametrize("d,G", [(128, 1), (128, 2), (128, 4), (128, 7), (64, 1), (64, 2), (64, 3), (64, 8)])
+@pytest.mark.parametrize("logit", [-40.0, 0.0, 15.0])
+def test_decode_scales_far_apart_in_a_tile(d, G, logit):
+    """Blocks whose V scales are up to 2^60 times the others' and whose weights are e^-40, alike, or e^15 times theirs: what
+    such rows do not weigh costs the others no bits."""
+    H, page = 2, 32
+    pool = Pool([[128, 33, 300], [600, 17, 200]], H, d, page, seed=G, spread=0)
+    codes, ks, vs = (t.cpu().numpy() for t in (pool.dev["k"], pool.dev_s["k"], pool.dev_s["v"]))
+    high = Pool._bytes(np.array([256.0]))[0]
+    for l in range(2):
+        for b in range(3):
+            for i in range(0, int(pool.lens[l, b]), 16):
+                pg, at = pool.table[l, b, i // page], i % page
+                codes[pg, :, at:at + 16, 0] = 0
+                if i // 16 % 5 == 1:                            # every fifth block: element 0 of its keys draws the logit
+                    ks[pg, :, at // 16] = 1.0
+                    codes[pg, :, at:at + 16] = 0
+                    vs[pg, :, at // 16] *= 2.0 ** [4, 5, 8, 12, 16, 20, 24, 60][(i // 80 + b) % 8]
+                    codes[pg, :, at:at + 16, 0] = high
+                elif i // 16 % 5 == 3:
+                    vs[pg, :, at // 16] *= 2.0 ** -6
+    for t, x in ((pool.dev["k"], codes), (pool.dev_s["k"], ks), (pool.dev_s["v"], vs)):
+        t.copy_(torch.from_numpy(x))
+    q = queries(2, 3, H * G, d, G, size=0.25)
+    q[..., 0] = math.sqrt(d) * logit / 256.0
+    out, lse, st = run_decode(pool, H * G, q)
+    assert st == xkv.OK
+    check_scales(pool, H * G, q, out, lse, f"d{d} G{G} logit {logit}")
+
+
+@pytest.mark.parametrize("d,G", [(128, 1), (128, 8), (64, 2), (64, 4)])
+def test_decode_scales_of_zero_and_at_both_ends(d, G):
+    """Blocks of scale 0, 2^-100 and 2^100 next to ordinary ones, and caches that hold nothing but blocks of scale 0."""
+    pool = Pool([[128, 300, 40], [256, 16, 77]], 2, d, 16, seed=G)
+    vs = pool.dev_s["v"].cpu().numpy()
+    for b in range(3):
+        for i in range(-(-int(pool.lens[0, b]) // 16)):
+            vs[pool.table[0, b, i]] *= [1.0, 0.0, 2.0 ** -93, 1.0, 2.0 ** 100][i % (5 if b == 0 else 4)]
+    vs[pool.table[1, 1]] = 0.0
+    pool.dev_s["v"].copy_(torch.from_numpy(vs))
+    q = queries(2, 3, 2 * G, d, G)
+    out, lse, st = run_decode(pool, 2 * G, q)
+    assert st == xkv.OK
+    check_scales(pool, 2 * G, q, out, lse, f"d{d} G{G}")
