@@ -436,13 +436,8 @@ __global__ void __launch_bounds__(kSmallThreads) plan_small_kernel(const PlanPar
     for (int w = 1; w < 32; ++w) end = max(end, s_end[w]);
     *p.used_after = end;
   }
-  bool over = false;                          // a layer has more tokens than its slot map (every warp finds out by itself)
-  if (p.slots != nullptr) {
-    for (int l = lane; l < p.n_layers; l += 32) over |= s_tok64[(l + 1) * p.batch] - s_tok64[l * p.batch] > p.slots_stride;
-    over = __any_sync(0xffffffffu, over) != 0;
-  }
-  if (p.slots == nullptr || over) {
-    // the new table entries of sequences that have tokens without a place in the slot map: a warp one after the other
+  // the new table entries of those of a warp's caches that have tokens without a place in the slot map, one after the other
+  auto write_tables = [&]() {
 #pragma unroll
     for (int i = 0; i < kPer; ++i) {
       const int e = tid * per + i;
@@ -460,7 +455,10 @@ __global__ void __launch_bounds__(kSmallThreads) plan_small_kernel(const PlanPar
                     __shfl_sync(0xffffffffu, pages, w), __shfl_sync(0xffffffffu, st, w));
       }
     }
-    if (p.slots == nullptr) return;
+  };
+  if (p.slots == nullptr) {
+    write_tables();
+    return;
   }
   if (few && !p.two_launches) {
     // a decode step: every thread the tokens of its own caches, all page ids in flight together
@@ -504,6 +502,7 @@ __global__ void __launch_bounds__(kSmallThreads) plan_small_kernel(const PlanPar
     }
     return;
   }
+  write_tables();
   // the runs of the layers' slot maps, dealt out to the warps
   const int runs = (int)((p.slots_stride + kSlotRun - 1) / kSlotRun);
 #pragma unroll 1
@@ -542,6 +541,15 @@ __global__ void __launch_bounds__(kPlanThreads) slots_kernel(const PlanParams p)
   write_range(p, p.block_table + (size_t)layer * p.batch * p.max_pages_per_seq, p.slots + layer * p.slots_stride,
               (int)min(t0, (int64_t)n_slots), (int)min(t0 + stretch, (int64_t)n_slots),
               [&](int b) { return s_tok[b]; }, [&](int b) { return s_start[b]; }, [&](int b) { return s_len[b]; });
+  if (total > p.slots_stride) {
+    // the new table entries of sequences that have tokens without a place in the slot map: a warp per sequence
+    for (int b = blockIdx.x * (kPlanThreads / 32) + (tid >> 5); b < p.batch; b += n_warps) {
+      if (s_start[b] < 0 || s_tok[b + 1] <= p.slots_stride) continue;
+      const int add = max(__ldg(&p.n_new[layer * p.n_new_stride + b]), 0);
+      const int have = p.page_of(s_len[b] + p.page_size - 1), need = p.page_of(s_len[b] + add + p.page_size - 1);
+      write_pages(p, p.block_table + ((size_t)layer * p.batch + b) * p.max_pages_per_seq + have, need - have, s_start[b]);
+    }
+  }
 }
 
 // ---------------------------------------------------------------------------------------------
