@@ -328,6 +328,9 @@ class XkvSession:
             k_lb = budgets.T if budgets.ndim == 2 else np.broadcast_to(budgets[:, None], (self.L, self.B))   # [L, B]
             rows = np.minimum(k_lb, prefix) + window
         if self.pages_on_demand:                             # the kept rows only: tables and lengths from nothing
+            n = -(-rows // self.page_size)
+            if int(n[n <= self.max_pages_per_seq].sum()) > self.n_pages:   # (longer caches get nothing: select_layer's status)
+                raise RuntimeError("page pool too small for these budgets")
             self.page_runs_host[0].numpy()[:] = rows
             self.page_runs[0].copy_(self.page_runs_host[0], non_blocking=True)
             xkv.plan_append(self.cache, self.n_caches, self.page_runs[0], self.n_caches, None, None, self.n_pages, None,
