@@ -16,6 +16,7 @@
 //   store_row_kernel    caches of bf16 or of 8-bit integers: D/8 lanes per (token, KV head)
 //   append_block_kernel one new row per (layer, sequence) and KV head of a cache of 8-bit floats, lengths advanced
 #include <algorithm>
+#include <atomic>
 
 #include "common.cuh"
 #include "e4m3.cuh"
@@ -699,6 +700,29 @@ __global__ void __launch_bounds__(kStoreThreads) append_block_kernel(const Appen
   if (threadIdx.x == 0) p.seq_lens[le] = n + 1;
 }
 
+// Shared memory of the plan kernels.
+size_t small_smem(int n_units) { return (size_t)(n_units + 1) * 8 + (size_t)n_units * 8; }
+size_t slots_smem(int batch) { return (size_t)(3 * batch + 1) * 4; }
+size_t plan_smem(int batch) { return (size_t)(2 * batch + 1) * 4; }
+
+// Opts in to the most shared memory that any call takes, once per device: the limit is one for all host threads, so that a
+// call that set it to its own size could take away another thread's between that one's setting and its launch.
+bool plan_set_up() {
+  int dev = 0;
+  if (cudaGetDevice(&dev) != cudaSuccess || dev < 0 || dev >= 64) return false;
+  static std::atomic<bool> done[64];   // idempotent: two threads doing it twice is harmless
+  if (done[dev].load(std::memory_order_acquire)) return true;
+  constexpr cudaFuncAttribute kMost = cudaFuncAttributeMaxDynamicSharedMemorySize;
+  if (cudaFuncSetAttribute(plan_small_kernel, kMost, (int)small_smem(kSmallUnits)) != cudaSuccess ||
+      cudaFuncSetAttribute(slots_kernel, kMost, (int)slots_smem(kSmallUnits)) != cudaSuccess ||
+      cudaFuncSetAttribute(plan_kernel, kMost, (int)plan_smem(kPlanMaxBatch)) != cudaSuccess) {
+    (void)cudaGetLastError();
+    return false;
+  }
+  done[dev].store(true, std::memory_order_release);
+  return true;
+}
+
 }  // namespace
 
 size_t plan_workspace_bytes(int n_layers, int batch) {
@@ -710,6 +734,7 @@ int plan_max_batch() { return kPlanMaxBatch; }
 xkv_status plan_append(const xkv_cache* c, int batch, const int32_t* n_new, int n_new_stride, const int32_t* lens_before,
                        const int32_t* free_pages, int n_free, const int32_t* pages_used_before, int32_t* pages_used_after,
                        int64_t* slots, int64_t slots_stride, void* workspace, cudaStream_t st) {
+  if (!plan_set_up()) return XKV_ERR_CUDA;
   PlanParams p;
   p.n_new = n_new;
   p.n_new_stride = n_new_stride;
@@ -746,27 +771,20 @@ xkv_status plan_append(const xkv_cache* c, int batch, const int32_t* n_new, int 
     // of layers x sequences x new tokens: steps 4 x 1 x 1: 3.2 / 4.3 us, 32 x 8 x 1: 3.3 / 4.7, 32 x 64 x 1: 5.5 / 7.0, 32 x 120 x 1:
     // 9.1 / 10.1; more tokens a cache 4 x 1 x 300: 4.2 / 4.5, 32 x 4 x 16: 5.0 / 4.5, 4 x 1 x 1000: 6.5 / 4.7, 32 x 64 x 4: 15.2 / 6.8.
     p.two_launches = c->n_layers * tokens > kSmallTokens ? 1 : 0;
-    const size_t small = (size_t)(n_units + 1) * 8 + (size_t)n_units * 8;
-    if (small > 40 * 1024 &&
-        cudaFuncSetAttribute(plan_small_kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)small) != cudaSuccess)
-      return XKV_ERR_CUDA;
-    plan_small_kernel<<<1, kSmallThreads, small, st>>>(p);
+    plan_small_kernel<<<1, kSmallThreads, small_smem((int)n_units), st>>>(p);
     count_launch();
     xkv_status s = check_launch();
     if (s != XKV_OK || !p.two_launches) return s;
     cudaLaunchConfig_t cfg = {};
     cfg.gridDim = grid;
     cfg.blockDim = dim3(kPlanThreads);
-    cfg.dynamicSmemBytes = (size_t)(3 * batch + 1) * 4;
+    cfg.dynamicSmemBytes = slots_smem(batch);
     cfg.stream = st;
     cudaLaunchAttribute attr;                 // its CTAs are in place when the first launch ends
     attr.id = cudaLaunchAttributeProgrammaticStreamSerialization;
     attr.val.programmaticStreamSerializationAllowed = 1;
     cfg.attrs = &attr;
     cfg.numAttrs = 1;
-    if (cfg.dynamicSmemBytes > 40 * 1024 &&
-        cudaFuncSetAttribute(slots_kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)cfg.dynamicSmemBytes) != cudaSuccess)
-      return XKV_ERR_CUDA;
     if (cudaLaunchKernelEx(&cfg, slots_kernel, p) != cudaSuccess) {
       (void)cudaGetLastError();
       return XKV_ERR_CUDA;
@@ -774,11 +792,7 @@ xkv_status plan_append(const xkv_cache* c, int batch, const int32_t* n_new, int 
     count_launch();
     return check_launch();
   }
-  const size_t smem = (size_t)(2 * batch + 1) * 4;
-  if (smem > 40 * 1024 &&
-      cudaFuncSetAttribute(plan_kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)smem) != cudaSuccess)
-    return XKV_ERR_CUDA;
-  plan_kernel<<<grid, kPlanThreads, smem, st>>>(p);
+  plan_kernel<<<grid, kPlanThreads, plan_smem(batch), st>>>(p);
   count_launch();
   return check_launch();
 }

@@ -1,5 +1,6 @@
 """Serving on a reduced cache at the edges of what the entry points document."""
 import math
+import threading
 
 import numpy as np
 import pytest
@@ -56,6 +57,36 @@ def test_plan_append_pages_of_tokens_behind_the_slot_map(L, B, stride):
     want, *got, status = plan(lens, new, page, cols, n_pages, used=0, slots_stride=stride, free=rng.permutation(n_pages))
     assert status == xkv.ERR_CAPACITY and want[4]
     check_plan(want, *got)
+
+
+@pytest.mark.parametrize("sizes", [((32, 128), (20, 130)), ((1, 16384), (1, 12000))])
+def test_plan_append_from_two_host_threads(sizes):
+    """Plans of different sizes from two threads, a stream and a workspace each: neither takes away the other's room."""
+    page, cols, steps, errors = 16, 4, 1500, []
+
+    def work(L, B):
+        try:
+            stream = torch.cuda.Stream(device=DEV)
+            with torch.cuda.stream(stream):
+                lens = torch.full((L, B), 15, dtype=torch.int32, device=DEV)
+                after, table = torch.zeros_like(lens), torch.zeros(L, B, cols, dtype=torch.int32, device=DEV)
+                new = torch.ones(B, dtype=torch.int32, device=DEV)
+                dims = xkv.Dims(B, 1, 1, 64, 1, 1, 0, 0.0, 64, 64)
+                ws = torch.zeros(xkv.workspace_bytes(xkv.OP_PLAN_APPEND, dims, n_layers=L), dtype=torch.uint8, device=DEV)
+            cache = xkv.Cache(None, None, table.data_ptr(), after.data_ptr(), L, page, cols, L * B * cols)
+            for _ in range(steps):
+                xkv.plan_append(cache, B, new, 0, lens, None, L * B * cols, None, None, None, 0, ws, stream=stream)
+            assert xkv.read_device_status(ws, stream=stream) == xkv.OK
+            assert torch.all(after == 16)
+        except Exception as e:                                  # noqa: BLE001
+            errors.append(e)
+
+    threads = [threading.Thread(target=work, args=s) for s in sizes]
+    for t in threads:
+        t.start()
+    for t in threads:
+        t.join()
+    assert not errors, errors
 
 
 # ------------------------------------------------------------------ V scales far apart
