@@ -316,7 +316,8 @@ __device__ __forceinline__ void cp_async_arrive(uint64_t* bar) {
 __device__ __forceinline__ void grid_dependency_wait() { asm volatile("griddepcontrol.wait;" ::: "memory"); }
 
 __device__ __forceinline__ int unit_rows(const Params& p, int e) {
-  const int n = __ldg(&p.seq_lens[(size_t)p.layer_begin * p.batch + e]);
+  // (not through the read-only path: the launch before this one may write lengths while this one is resident already)
+  const int n = p.seq_lens[(size_t)p.layer_begin * p.batch + e];
   return min(max(n, 0), p.max_pages_per_seq * p.page_size);
 }
 template <int D>

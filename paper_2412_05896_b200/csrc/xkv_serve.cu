@@ -527,11 +527,12 @@ __global__ void __launch_bounds__(kPlanThreads) slots_kernel(const PlanParams p)
   int32_t* s_len = s_start + p.batch;         // [batch]
   const int tid = threadIdx.x, layer = blockIdx.y, n_warps = gridDim.x * (kPlanThreads / 32);
   asm volatile("griddepcontrol.wait;" ::: "memory");
+  // (not through the read-only path: plan_small_kernel may write them while this kernel is resident already)
   for (int i = tid; i <= p.batch; i += kPlanThreads) {
-    s_tok[i] = __ldg(&p.ws_tok[(size_t)layer * (p.batch + 1) + i]);
+    s_tok[i] = p.ws_tok[(size_t)layer * (p.batch + 1) + i];
     if (i < p.batch) {
-      s_start[i] = __ldg(&p.ws_start[(size_t)layer * p.batch + i]);
-      s_len[i] = __ldg(&p.ws_len[(size_t)layer * p.batch + i]);
+      s_start[i] = p.ws_start[(size_t)layer * p.batch + i];
+      s_len[i] = p.ws_len[(size_t)layer * p.batch + i];
     }
   }
   __syncthreads();
