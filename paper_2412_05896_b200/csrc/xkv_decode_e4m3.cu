@@ -436,6 +436,7 @@ __device__ __noinline__ void join_open(const Params& p, Joins* joins) {
     claim = __shfl_sync(0xffffffffu, claim, 0);
     if (claim < 0) return;
     n = __shfl_sync(0xffffffffu, n, 0);
+    __syncwarp();                                 // what lane 0 has seen, all lanes see
     const int4 job = joins->job[claim / G % kJobs];
     if (job.w <= 4) join_heads<D, 4, 4>(p, job, claim % G);
     else            join_heads<D, 1, 16>(p, job, claim % G);
@@ -980,7 +981,8 @@ decode_e4m3_kernel(const __grid_constant__ CUtensorMap tmap_k, const __grid_cons
             s_head[warp][1][lane] = grows ? ex : 1.f;             // what the sums so far are multiplied by
             s_head[warp][2][lane] = grows ? 1.f : ex;             // and the tile's
           }
-          grows_any = __any_sync(0xffffffffu, grows);             // (orders the stores before the loads below)
+          grows_any = __any_sync(0xffffffffu, grows);
+          __syncwarp();                                           // the stores before the loads below
           get_heads<GP>(s_head[warp][0], mt);
         } else {
 #pragma unroll
