@@ -69,7 +69,7 @@ constexpr float kMinShare = -80.f;    // log2 of the smallest s_v / max s_v of a
 constexpr int kBarSoft = 1;           // named barrier of warps 0-3
 constexpr int kCacheCost = 12;        // what a cache costs besides its tiles, in blocks of 16 rows (2048 caches of 203 to 1101 rows
                                       // laid out by rows: 66.6 us with 4, 64.9 with 8, 64.2 with 12, 64.9 with 16)
-constexpr int kJobs = 32;             // joins a CTA may have open
+constexpr int kJobs = 2;              // joins of a CTA: only the pieces at the two ends of its share are of cut caches
 
 template <int D>
 struct Cfg {
@@ -334,7 +334,7 @@ __device__ __forceinline__ int cost_of(int rows) {
 // Caches that this CTA has found complete and is to join.
 struct Joins {
   int4 job[kJobs];                    // {unit, KV head, first CTA, pieces}
-  int n_jobs, claimed, joined;        // jobs so far, heads claimed and heads joined
+  int n_jobs, claimed;                // jobs so far, heads claimed
   int all;                            // no more jobs to come
 };
 
@@ -424,7 +424,7 @@ __device__ __noinline__ void join_open(const Params& p, Joins* joins) {
       __threadfence_block();                      // n_jobs before the jobs and, behind them, the pieces
       while (at < open) {
         // few pieces: four heads in one go; many: one head a warp, so that several warps share the job
-        n = joins->job[at / G % kJobs].w <= 4 ? min(4, G - at % G) : 1;
+        n = joins->job[at / G].w <= 4 ? min(4, G - at % G) : 1;
         const int was = atomicCAS(&joins->claimed, at, at + n);
         if (was == at) {
           claim = at;
@@ -437,11 +437,9 @@ __device__ __noinline__ void join_open(const Params& p, Joins* joins) {
     if (claim < 0) return;
     n = __shfl_sync(0xffffffffu, n, 0);
     __syncwarp();                                 // what lane 0 has seen, all lanes see
-    const int4 job = joins->job[claim / G % kJobs];
+    const int4 job = joins->job[claim / G];
     if (job.w <= 4) join_heads<D, 4, 4>(p, job, claim % G);
     else            join_heads<D, 1, 16>(p, job, claim % G);
-    __syncwarp();
-    if (lane == 0) atomicAdd(&joins->joined, n);
   }
 }
 
@@ -501,7 +499,7 @@ decode_e4m3_kernel(const __grid_constant__ CUtensorMap tmap_k, const __grid_cons
     }
     mbar_init(&s_wake, 1);
     s_abort_store = 0;
-    s_joins.n_jobs = s_joins.claimed = s_joins.joined = s_joins.all = 0;
+    s_joins.n_jobs = s_joins.claimed = s_joins.all = 0;
     fence_mbar_init();
     prefetch_tmap(&tmap_k);
     prefetch_tmap(&tmap_v);
@@ -875,12 +873,8 @@ decode_e4m3_kernel(const __grid_constant__ CUtensorMap tmap_k, const __grid_cons
       }
       if (__shfl_sync(0xffffffffu, last, 0)) {
         const int n = *(volatile int*)&s_joins.n_jobs;
-        if (n > 0 && n % kJobs == 0) {            // the job table comes round: let it run empty first
-          join_open<D>(p, &s_joins);
-          while (*(volatile int*)&s_joins.joined < n * G) __nanosleep(100);
-        }
         if (lane == 0) {
-          s_joins.job[n % kJobs] = make_int4(it.e, it.h, it.first_cta, it.n_pieces);
+          s_joins.job[n] = make_int4(it.e, it.h, it.first_cta, it.n_pieces);
           __threadfence_block();
           *(volatile int*)&s_joins.n_jobs = n + 1;
           if (!woken) mbar_arrive(&s_wake);
