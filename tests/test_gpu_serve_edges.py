@@ -171,3 +171,35 @@ def test_decode_scales_of_zero_and_at_both_ends(d, G):
     out, lse, st = run_decode(pool, 2 * G, q)
     assert st == xkv.OK
     check_scales(pool, 2 * G, q, out, lse, f"d{d} G{G}")
+
+
+# ------------------------------------------------------------------ NaN in cached rows
+@pytest.mark.parametrize("d,G", [(128, 1), (128, 2), (128, 4), (128, 8), (64, 1), (64, 3)])
+def test_decode_nan_in_cached_rows(d, G):
+    """A NaN in a row of K makes that KV head's outputs and lse NaN, one in a row of V that column of its outputs; nothing
+    else moves by a bit.  First, middle and last rows; caches of one tile, of several, and cut ones."""
+    H, page = 2, 16
+    pool = Pool([[5, 700, 6000], [130, 1, 259]], H, d, page, seed=G + d)
+    q = queries(2, 3, H * G, d, G)
+    want, want_lse, st = run_decode(pool, H * G, q)
+    assert st == xkv.OK
+    clean = {x: pool.dev[x].clone() for x in "kv"}
+    for x, code in (("k", 0x7F), ("k", 0xFF), ("v", 0x7F), ("v", 0xFF)):
+        nan, nan_lse = torch.zeros_like(want, dtype=torch.bool), torch.zeros_like(want_lse, dtype=torch.bool)
+        for l, b, g, row, col in ((0, 0, 1, 4, 0), (0, 1, 0, 0, d - 1), (0, 2, 1, 3001, 17), (1, 0, 0, 129, 5), (1, 2, 1, 0, 31),
+                                  (1, 2, 1, 258, 33)):
+            pool.dev[x][pool.table[l, b, row // page], g, row % page, col] = code
+            if x == "k":
+                nan[l, b, g * G:(g + 1) * G] = nan_lse[l, b, g * G:(g + 1) * G] = True
+            else:
+                nan[l, b, g * G:(g + 1) * G, col] = True
+        out, lse, st = run_decode(pool, H * G, q)
+        assert st == xkv.OK
+        assert torch.equal(torch.isnan(out), nan) and torch.equal(torch.isnan(lse), nan_lse), (x, code)
+        assert torch.equal(out[~nan], want[~nan]) and torch.equal(lse[~nan_lse], want_lse[~nan_lse]), (x, code)
+        pool.dev[x].copy_(clean[x])
+    pool.dev["k"][pool.table[0, 2, 10:30]] = 0x7F            # whole tiles of them
+    pool.dev["k"][pool.table[1, 0]] = 0x7F                   # a whole cache
+    out, lse, st = run_decode(pool, H * G, q)
+    assert st == xkv.OK and torch.isnan(out[0, 2]).all() and torch.isnan(lse[0, 2]).all() and torch.isnan(out[1, 0]).all()
+    assert torch.equal(out[0, :2], want[0, :2]) and torch.equal(out[1, 1:], want[1, 1:])
