@@ -392,9 +392,11 @@ xkv_status xkv_plan_append(const xkv_cache* cache, int32_t batch, const int32_t*
  *               (any); block_table and seq_lens are not touched
  * k, v          dev bf16, head g of token i at element offset i * kv_stride_token + g * kv_stride_head
  * slots         dev int64 [n_tokens] as xkv_plan_append writes them; a negative slot skips its token (padding)
- * A slot occurs at most once in a call. With XKV_KV_E4M3 the tokens of one block follow each other in slot order and
- * the block's rows before them are in place (what xkv_plan_append's order gives); a token whose slot does not follow its
- * predecessor's inside a block is not stored, nor is the rest of its run: device status XKV_ERR_INVALID_ARG. A slot
+ * A slot occurs at most once in a call. With XKV_KV_E4M3 the tokens of one block follow each other in slot order, without
+ * padding or other tokens between them, and the block's rows before them are in place (what xkv_plan_append's order
+ * gives); a token whose slot does not follow its predecessor's inside a block, or that up to 31 tokens of padding part from
+ * an earlier one of its block, is not stored, nor is the rest of its run: device status XKV_ERR_INVALID_ARG. (Tokens of one
+ * block further apart are not looked for: which of them the block then holds is not defined.) A slot
  * beyond the pool is not stored: device status XKV_ERR_CAPACITY. No slot but the given ones is written, except
  * that the earlier rows of a block whose scale grows are re-expressed.
  * workspace     dev, at least xkv_workspace_bytes(XKV_OP_STORE_ROWS, ...) bytes (the status word), 256-byte aligned

@@ -573,6 +573,18 @@ struct StoreParams {
   WorkspaceHeader* hdr;
 };
 
+// Whether up to 31 tokens of padding part token t, of slot s, from a token of the same block: another warp may be storing that
+// one.  (Not inlined: nothing that runs often asks.)
+__device__ __noinline__ bool behind_padding_of_its_block(const int64_t* slots, int64_t t, int64_t s) {
+  if (s % kScaleBlock == 0) return false;
+#pragma unroll 1
+  for (int64_t i = t - 2; i >= 0 && i >= t - 32; --i) {
+    const int64_t before = __ldg(&slots[i]);
+    if (before >= 0) return before / kScaleBlock == s / kScaleBlock;
+  }
+  return false;
+}
+
 // One warp: the runs that begin among tokens_per_warp consecutive tokens, of one KV head of K or of V.  A run is the
 // longest stretch of tokens whose slots follow each other inside one block; rows of the block before the run are there
 // already, rows behind it are not in use.
@@ -597,6 +609,10 @@ __global__ void __launch_bounds__(kStoreThreads, 4) store_block_kernel(const Sto
     }
     if (s >= 0 && prev >= 0 && prev / kScaleBlock == s / kScaleBlock && prev + 1 != s) {
       if (job == 0) record_status(p.hdr, XKV_ERR_INVALID_ARG);   // a block's tokens are not in slot order
+      s = -1;
+    }
+    if (s >= 0 && prev < 0 && behind_padding_of_its_block(p.slots, ti, s)) {
+      if (job == 0) record_status(p.hdr, XKV_ERR_INVALID_ARG);
       s = -1;
     }
   }

@@ -10,7 +10,7 @@ from oracle import xkv_oracle as O
 from paper_2412_05896_b200 import xkv
 
 from gpu_util import f64, require_lib
-from test_gpu_block_cache import BF16_HALF, DEV, Pool, check_plan, plan, queries, run_decode
+from test_gpu_block_cache import BF16_HALF, DEV, Pool, check_plan, expect_store, plan, queries, run_decode, same, store
 
 pytestmark = pytest.mark.gpu
 
@@ -203,3 +203,42 @@ def test_decode_nan_in_cached_rows(d, G):
     out, lse, st = run_decode(pool, H * G, q)
     assert st == xkv.OK and torch.isnan(out[0, 2]).all() and torch.isnan(lse[0, 2]).all() and torch.isnan(out[1, 0]).all()
     assert torch.equal(out[0, :2], want[0, :2]) and torch.equal(out[1, 1:], want[1, 1:])
+
+
+# ------------------------------------------------------------------ rows stored by slot
+@pytest.mark.parametrize("gap", [1, 2, 15, 31])
+@pytest.mark.parametrize("d,H,many", [(64, 1, 0), (128, 8, 0), (128, 8, 600), (64, 16, 2400)])
+def test_store_rows_padding_inside_a_block(gap, d, H, many):
+    """Padding between two tokens of one block: the second is not stored, nor the rest of its run, and the status says so;
+    padding between tokens of different blocks is nothing special.  A token, four and sixteen of them a warp."""
+    page = 32
+    pool = Pool([[7, 20] + [3] * 40], H, d, page, seed=gap, spare_rows=80, any_code=True)
+    at = lambda b, i: int(pool.table[0, b, i // page]) * page + i % page         # noqa: E731
+    slots = [at(0, 7), at(0, 8)] + [-1] * gap + [at(0, 9), at(0, 10)] + [-1] * gap + [at(1, 20)]
+    slots += [at(2 + i % 40, 3 + j) for i in range(40) for j in range(many // 40)]
+    kept = list(slots)
+    kept[2 + gap] = kept[3 + gap] = -1
+    slots, kept = (np.asarray(x, dtype=np.int64) for x in (slots, kept))
+    gen = torch.Generator().manual_seed(gap)
+    k, v = (torch.randn(len(slots), H, d, generator=gen).to(torch.bfloat16).to(DEV) for _ in "kv")
+    want = {x: expect_store(pool, x, f64(t), kept) for x, t in (("k", k), ("v", v))}
+    assert store(pool, k, v, torch.from_numpy(slots).to(DEV)) == xkv.ERR_INVALID_ARG
+    for x in "kv":
+        assert same(O.e4m3_values(pool.dev[x].cpu().numpy()), want[x][0]), x
+        assert same(pool.dev_s[x].cpu().numpy().astype(np.float64), want[x][1]), x
+
+
+def test_store_rows_behind_padding():
+    """Left-padded sequences: a run in the middle of a block behind padding is stored as ever."""
+    d, H, page = 64, 2, 16
+    pool = Pool([[5, 9, 33]], H, d, page, seed=1, spare_rows=20, any_code=True)
+    slots = np.concatenate([np.concatenate([np.full(pad, -1), pool.table[0, b, (n + np.arange(6)) // page] * page +
+                                            (n + np.arange(6)) % page])
+                            for b, (n, pad) in enumerate(((5, 3), (9, 40), (33, 1)))]).astype(np.int64)
+    gen = torch.Generator().manual_seed(2)
+    k, v = (torch.randn(len(slots), H, d, generator=gen).to(torch.bfloat16).to(DEV) for _ in "kv")
+    want = {x: expect_store(pool, x, f64(t), slots) for x, t in (("k", k), ("v", v))}
+    assert store(pool, k, v, torch.from_numpy(slots).to(DEV)) == xkv.OK
+    for x in "kv":
+        assert same(O.e4m3_values(pool.dev[x].cpu().numpy()), want[x][0]), x
+        assert same(pool.dev_s[x].cpu().numpy().astype(np.float64), want[x][1]), x
