@@ -128,6 +128,7 @@ class XkvSession:
         self.ws_plan = self.ws_store = None
         if self.pages_on_demand:
             self.pages_used = torch.zeros(1, dtype=torch.int32, device=self.device)
+            self.one_each = torch.ones(self.n_caches, dtype=torch.int32, device=self.device)   # a step's new rows
             self.ws_plan = self._ws(xkv.workspace_bytes(xkv.OP_PLAN_APPEND, self.dec_dims, n_layers=n_layers))
             self.ws_store = self._ws(xkv.workspace_bytes(xkv.OP_STORE_ROWS, self.dec_dims))
         self.chunk_rows = decode_chunk_rows
@@ -376,12 +377,11 @@ class XkvSession:
         Needs pages_on_demand.  Returns the slots, int64 [L, T] ([L, T*Hkv] in a head-level session)."""
         if not self.pages_on_demand:
             raise ValueError("append needs a session with pages_on_demand=True")
-        self.join()
         n_new = np.asarray(n_new, dtype=np.int32)
+        if n_new.shape != (self.B,) or int(n_new.min()) < 0:
+            raise ValueError("append: n_new is one count per sequence")
         T = int(n_new.sum())
-        if n_new.shape != (self.B,) or int(n_new.min()) < 0 or tuple(k.shape) != (self.L, T, self.Hkv, self.d) \
-                or k.shape != v.shape:
-            raise ValueError("append: k and v are [L, sum(n_new), Hkv, d], n_new one count per sequence")
+        self._check_rows(k, v, T)
         counts = n_new
         if self.head_level:                                  # caches (b, g): a sequence's tokens head by head
             counts = np.repeat(n_new, self.Hkv)
@@ -389,12 +389,26 @@ class XkvSession:
                 first = np.concatenate([[0], np.cumsum(n_new)[:-1]])
                 order = np.concatenate([((first[b] + np.arange(n_new[b]))[None, :] * self.Hkv +
                                          np.arange(self.Hkv)[:, None]).ravel() for b in range(self.B)])
-                order = torch.from_numpy(order.astype(np.int64)).to(self.device)
+                order = self._to_device(order.astype(np.int64))
                 k, v = (x.reshape(self.L, T * self.Hkv, self.d)[:, order] for x in (k, v))
-        n_tokens = int(counts.sum())
+        return self._store_new(k, v, self._to_device(counts), int(counts.sum()))
+
+    def _to_device(self, a: np.ndarray) -> torch.Tensor:
+        """Host integers on the device without waiting for it."""
+        return torch.from_numpy(a).pin_memory().to(self.device, non_blocking=True)
+
+    def _check_rows(self, k, v, T: int) -> None:
+        for x in (k, v):
+            if not isinstance(x, torch.Tensor) or tuple(x.shape) != (self.L, T, self.Hkv, self.d) \
+                    or x.dtype != torch.bfloat16 or x.device != self.k_pages.device:
+                raise ValueError(f"new rows are bf16 [{self.L}, {T}, {self.Hkv}, {self.d}] tensors on {self.k_pages.device}")
+
+    def _store_new(self, k: torch.Tensor, v: torch.Tensor, counts: torch.Tensor, n_tokens: int) -> torch.Tensor:
+        """counts: dev int32, rows to come of each of a layer's caches; k, v: [L, n_tokens, ..] in that order."""
+        self.join()
         slots = torch.empty(self.L, n_tokens, dtype=torch.int64, device=self.device)
-        xkv.plan_append(self.cache, self.n_caches, torch.from_numpy(counts).to(self.device), 0, self.seq_lens, None,
-                        self.n_pages, self.pages_used, self.pages_used, slots if n_tokens else None, n_tokens, self.ws_plan)
+        xkv.plan_append(self.cache, self.n_caches, counts, 0, self.seq_lens, None, self.n_pages, self.pages_used,
+                        self.pages_used, slots if n_tokens else None, n_tokens, self.ws_plan)
         # the layers' tokens are one list: their rows lie one after the other and so do their slots
         if n_tokens:
             xkv.store_rows(self.dec_dims, self.cache, k.contiguous(), v.contiguous(), slots, self.L * n_tokens,
@@ -410,7 +424,9 @@ class XkvSession:
         if self.pages_on_demand and k_new is not None:
             if (layer_begin, layer_end) != (0, self.L):
                 raise ValueError("with pages_on_demand a step plans all layers: append first, then decode layer by layer")
-            self.append(k_new, v_new, np.ones(self.B, dtype=np.int32))
+            # one row a cache, head by head in a head-level session: the order in which the rows lie
+            self._check_rows(k_new, v_new, self.B)
+            self._store_new(k_new, v_new, self.one_each, self.n_caches)
             k_new = v_new = None
         xkv.decode_attn(self.dec_dims, self.cache, layer_begin, layer_end, q, k_new, v_new, out,
                         self.lse if lse is None else lse,

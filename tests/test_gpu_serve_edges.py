@@ -242,3 +242,97 @@ def test_store_rows_behind_padding():
     for x in "kv":
         assert same(O.e4m3_values(pool.dev[x].cpu().numpy()), want[x][0]), x
         assert same(pool.dev_s[x].cpu().numpy().astype(np.float64), want[x][1]), x
+
+
+# ------------------------------------------------------------------ sessions with pages on demand
+def _session(head_level, fmt, steps=12):
+    from dataclasses import replace
+
+    from paper_2412_05896_b200 import workloads as WL
+    from paper_2412_05896_b200.pipeline import XkvSession
+    w = replace(WL.CONFIGS["mistral_7b_gqa"], n_layers=2, n_q_heads=4, n_kv_heads=2, head_dim=64, batch=3, prompt=(90, 300),
+                window=16, avg_budget=50, n_min=8, n_max=128, decode_steps=steps)
+    lengths = WL.prompt_lengths(w)
+    tens = [WL.layer_tensors(w, l, DEV, lengths, stress=True) for l in range(w.n_layers)]
+    N = w.n_layers * w.avg_budget * (2 if head_level else 1)
+    sess = XkvSession(2, 4, 2, 64, w.window, w.pool_kernel, lengths, max_new_tokens=80, max_budget=w.n_max, total_budget=N,
+                      curve_len=w.n_max, device=DEV, head_level=head_level, kv_format=fmt, pages_on_demand=True)
+    sess.prefill(*(list(x) for x in zip(*tens)), total=N, n_min=w.n_min, n_max=w.n_max)
+    torch.cuda.synchronize()
+    return w, sess, [WL.decode_tensors(w, i, DEV, stress=True) for i in range(steps)]
+
+
+def _counts_to_append(sess, w, seed):
+    n_new = [3, 0, 21]
+    gen = torch.Generator().manual_seed(seed)
+    return [torch.randn(2, sum(n_new), 2, 64, generator=gen).to(torch.bfloat16).to(DEV) for _ in "kv"] + [n_new]
+
+
+@pytest.mark.parametrize("fmt", [xkv.KV_E4M3, xkv.KV_BF16])
+@pytest.mark.parametrize("head_level", [False, True])
+def test_session_steps_in_a_graph(head_level, fmt):
+    """A captured step of a session with pages on demand, replayed, against the same steps of a twin without a graph; every
+    page of the caches grows on the way."""
+    w, sess, steps = _session(head_level, fmt, steps=20)
+    _, twin, _ = _session(head_level, fmt, steps=1)
+    q, k, v = (x.clone() for x in steps[0])
+    torch.cuda.synchronize()
+    graph = torch.cuda.CUDAGraph()
+    with torch.cuda.graph(graph):
+        out = sess.decode(q, k, v)
+    torch.cuda.synchronize()
+    assert torch.equal(sess.seq_lens, twin.seq_lens)            # nothing ran yet
+    for step in steps:
+        for t, x in zip((q, k, v), step):
+            t.copy_(x)
+        graph.replay()
+        want = twin.decode(*step)
+        torch.cuda.synchronize()
+        assert torch.equal(out, want) and torch.equal(sess.lse, twin.lse) and torch.equal(sess.seq_lens, twin.seq_lens)
+    assert torch.equal(sess.block_table, twin.block_table) and torch.equal(sess.pages_used, twin.pages_used)
+    assert sess.device_status("append") == xkv.OK and sess.device_status("decode") == xkv.OK
+
+
+@pytest.mark.parametrize("head_level", [False, True])
+def test_session_does_not_wait_for_the_device(head_level):
+    w, sess, steps = _session(head_level, xkv.KV_E4M3)
+    k, v, n_new = _counts_to_append(sess, w, 5)
+    before = sess.seq_lens.clone()
+    torch.cuda.synchronize()
+    torch.cuda.set_sync_debug_mode("error")
+    try:
+        sess.append(k, v, n_new)
+        sess.decode(*steps[0])
+        sess.append(k[:, :3], v[:, :3], [0, 3, 0])
+        sess.decode(*steps[1])
+    finally:
+        torch.cuda.set_sync_debug_mode("default")
+    torch.cuda.synchronize()
+    assert sess.device_status("append") == xkv.OK
+    grown = torch.tensor([5, 5, 23], dtype=torch.int32, device=DEV)
+    assert torch.equal(sess.seq_lens, before + (grown.repeat_interleave(2) if head_level else grown))
+
+
+def test_session_refuses_rows_of_another_type_or_shape():
+    w, sess, steps = _session(False, xkv.KV_E4M3, steps=1)
+    q, k, v = steps[0]
+    before = sess.seq_lens.clone()
+    for bad in ((k.float(), v), (k, v.half()), (k, None), (k.cpu(), v), (k[:, :2], v[:, :2]), (k, v.view(torch.uint8))):
+        with pytest.raises(ValueError):
+            sess.decode(q, *bad)
+        with pytest.raises(ValueError):
+            sess.append(*bad, [1, 1, 1])
+    for bad in ([1, 1], [1, -1, 3], [[1, 1, 1]]):
+        with pytest.raises(ValueError):
+            sess.append(k, v, bad)
+    assert torch.equal(sess.seq_lens, before) and sess.device_status("append") == xkv.OK
+
+
+def test_session_budgets_beyond_the_pool():
+    """Refused on the host; the caches that live in the pool stay as they are."""
+    w, sess, steps = _session(False, xkv.KV_E4M3, steps=1)
+    pages, lens = sess.k_pages.clone(), sess.seq_lens.clone()
+    sess.n_pages = int(sess.pages_used.item())                  # as many as the budgets so far took
+    with pytest.raises(RuntimeError, match="page pool too small"):
+        sess.assign_pages(np.asarray(sess.budgets) + 40)
+    assert torch.equal(sess.k_pages, pages) and torch.equal(sess.seq_lens, lens)
