@@ -112,11 +112,6 @@ class XkvSession:
             self.v_scales = torch.zeros(self.n_pages, page_heads, n_scales, **f32)
         self.block_table = torch.zeros(n_layers, self.n_caches, self.max_pages_per_seq, dtype=torch.int32,
                                        device=self.device)
-        # page runs of every (layer, cache): [0] first page, [1] number of pages; expanded on the device
-        self.page_runs_host = [torch.zeros(n_layers, self.n_caches, dtype=torch.int32, pin_memory=True)
-                               for _ in range(2)]
-        self.page_runs = [torch.zeros(n_layers, self.n_caches, dtype=torch.int32, device=self.device)
-                          for _ in range(2)]
         self.seq_lens = torch.zeros(n_layers, self.n_caches, dtype=torch.int32, device=self.device)
         self.cache = xkv.Cache(self.k_pages.data_ptr(), self.v_pages.data_ptr(), self.block_table.data_ptr(),
                                self.seq_lens.data_ptr(), n_layers, page_size, self.max_pages_per_seq,
@@ -143,6 +138,12 @@ class XkvSession:
 
     def _ws(self, nbytes: int) -> torch.Tensor:
         return torch.zeros(nbytes, dtype=torch.uint8, device=self.device)   # status word reads OK before first use
+
+    def _to_device(self, a: np.ndarray, dtype=np.int32) -> torch.Tensor:
+        """Host integers on the device without waiting for it, by a staging buffer of their own, which no later call
+        overwrites while the copy is still to come."""
+        a = np.ascontiguousarray(a, dtype=dtype)
+        return torch.from_numpy(a).pin_memory().to(self.device, non_blocking=True)
 
     # ------------------------------------------------------------------ prefill
     def _lane(self, layer: int, *tensors):
@@ -332,9 +333,7 @@ class XkvSession:
             n = -(-rows // self.page_size)
             if int(n[n <= self.max_pages_per_seq].sum()) > self.n_pages:   # (longer caches get nothing: select_layer's status)
                 raise RuntimeError("page pool too small for these budgets")
-            self.page_runs_host[0].numpy()[:] = rows
-            self.page_runs[0].copy_(self.page_runs_host[0], non_blocking=True)
-            xkv.plan_append(self.cache, self.n_caches, self.page_runs[0], self.n_caches, None, None, self.n_pages, None,
+            xkv.plan_append(self.cache, self.n_caches, self._to_device(rows), self.n_caches, None, None, self.n_pages, None,
                             self.pages_used, None, 0, self.ws_plan)
             return
         rows = rows + self.max_new
@@ -342,10 +341,8 @@ class XkvSession:
         start = np.concatenate([[0], np.cumsum(n.ravel())[:-1]]).reshape(self.L, self.n_caches)
         if int(start.ravel()[-1] + n.ravel()[-1]) > self.n_pages:
             raise RuntimeError("page pool too small for these budgets")
-        for dst, host, src in zip(self.page_runs, self.page_runs_host, (start, n)):
-            host.numpy()[:] = src
-            dst.copy_(host, non_blocking=True)
-        xkv.build_block_table(self.page_runs[0], self.page_runs[1], self.cache, self.n_caches)
+        # every (layer, cache): its first page and its number of pages; expanded on the device
+        xkv.build_block_table(self._to_device(start), self._to_device(n), self.cache, self.n_caches)
 
     def select_layer(self, layer: int, budget, k: torch.Tensor, v: torch.Tensor, sel: torch.Tensor | None = None,
                      per_sequence: bool = False) -> None:
@@ -389,13 +386,9 @@ class XkvSession:
                 first = np.concatenate([[0], np.cumsum(n_new)[:-1]])
                 order = np.concatenate([((first[b] + np.arange(n_new[b]))[None, :] * self.Hkv +
                                          np.arange(self.Hkv)[:, None]).ravel() for b in range(self.B)])
-                order = self._to_device(order.astype(np.int64))
+                order = self._to_device(order, np.int64)
                 k, v = (x.reshape(self.L, T * self.Hkv, self.d)[:, order] for x in (k, v))
         return self._store_new(k, v, self._to_device(counts), int(counts.sum()))
-
-    def _to_device(self, a: np.ndarray) -> torch.Tensor:
-        """Host integers on the device without waiting for it."""
-        return torch.from_numpy(a).pin_memory().to(self.device, non_blocking=True)
 
     def _check_rows(self, k, v, T: int) -> None:
         for x in (k, v):

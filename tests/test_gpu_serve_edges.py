@@ -245,7 +245,7 @@ def test_store_rows_behind_padding():
 
 
 # ------------------------------------------------------------------ sessions with pages on demand
-def _session(head_level, fmt, steps=12):
+def _session(head_level, fmt, steps=12, on_demand=True):
     from dataclasses import replace
 
     from paper_2412_05896_b200 import workloads as WL
@@ -256,7 +256,7 @@ def _session(head_level, fmt, steps=12):
     tens = [WL.layer_tensors(w, l, DEV, lengths, stress=True) for l in range(w.n_layers)]
     N = w.n_layers * w.avg_budget * (2 if head_level else 1)
     sess = XkvSession(2, 4, 2, 64, w.window, w.pool_kernel, lengths, max_new_tokens=80, max_budget=w.n_max, total_budget=N,
-                      curve_len=w.n_max, device=DEV, head_level=head_level, kv_format=fmt, pages_on_demand=True)
+                      curve_len=w.n_max, device=DEV, head_level=head_level, kv_format=fmt, pages_on_demand=on_demand)
     sess.prefill(*(list(x) for x in zip(*tens)), total=N, n_min=w.n_min, n_max=w.n_max)
     torch.cuda.synchronize()
     return w, sess, [WL.decode_tensors(w, i, DEV, stress=True) for i in range(steps)]
@@ -336,3 +336,25 @@ def test_session_budgets_beyond_the_pool():
     with pytest.raises(RuntimeError, match="page pool too small"):
         sess.assign_pages(np.asarray(sess.budgets) + 40)
     assert torch.equal(sess.k_pages, pages) and torch.equal(sess.seq_lens, lens)
+
+
+@pytest.mark.parametrize("on_demand", [False, True])
+def test_session_page_runs_of_two_requests_in_flight(on_demand):
+    """Pages assigned for one request and then for the next while the device is still busy: each gets its own."""
+    w, sess, _ = _session(False, xkv.KV_E4M3, steps=1, on_demand=on_demand)
+    one, two = np.array([20, 70]), np.array([60, 9])
+    seen = []
+    for busy in (False, True):
+        sess.block_table.fill_(-1)
+        sess.seq_lens.fill_(-1)
+        torch.cuda.synchronize()
+        if busy:
+            torch.cuda._sleep(200_000_000)                      # a tenth of a second of device time
+        for budgets in (one, two):
+            sess.assign_pages(budgets)
+            seen.append((sess.block_table.clone(), sess.seq_lens.clone()))
+            if not busy:
+                torch.cuda.synchronize()
+        torch.cuda.synchronize()
+    for a, b in zip(seen[:2], seen[2:]):
+        assert torch.equal(a[0], b[0]) and torch.equal(a[1], b[1])

@@ -24,15 +24,14 @@ def test_plan_append_refuses_slot_maps_of_2_31_tokens():
     assert call(2 ** 31 - 2) == xkv.ERR_WORKSPACE             # (the next check)
 
 
-def _session(head_level, on_demand, n_pages, planned):
-    """A session of 2 layers, 2 sequences, 2 KV heads as assign_pages sees it, without a device; calls go to `planned`."""
+def _session(head_level, on_demand, n_pages):
+    """A session of 2 layers, 2 sequences, 2 KV heads as assign_pages sees it, without a device."""
     from paper_2412_05896_b200.pipeline import XkvSession
     s = XkvSession.__new__(XkvSession)
     s.L, s.B, s.Hkv, s.W, s.max_new, s.page_size = 2, 2, 2, 4, 8, 16
     s.lengths, s.prefix, s.head_level, s.pages_on_demand = [100, 50], [96, 46], head_level, on_demand
     s.n_caches, s.n_pages, s.max_pages_per_seq = s.B * (s.Hkv if head_level else 1), n_pages, 7
-    s.page_runs_host = [torch.zeros(s.L, s.n_caches, dtype=torch.int32) for _ in range(2)]
-    s.page_runs = [torch.zeros(s.L, s.n_caches, dtype=torch.int32) for _ in range(2)]
+    s._to_device = lambda a, dtype=np.int32: torch.from_numpy(np.ascontiguousarray(a, dtype=dtype))
     s.cache = s.pages_used = s.ws_plan = None
     return s
 
@@ -48,17 +47,17 @@ def test_assign_pages_refuses_budgets_beyond_the_pool(monkeypatch, head_level, o
     kept = (np.minimum(budgets[:, None, :], np.array([96, 46])[None, :, None]) + 4).reshape(2, -1) if head_level else (
         np.minimum(budgets[:, None], np.array([[96, 46]])) + 4)
     need = int((-(-(kept + (0 if on_demand else 8)) // 16)).sum())
-    _session(head_level, on_demand, need, planned).assign_pages(budgets)
+    _session(head_level, on_demand, need).assign_pages(budgets)
     assert len(planned) == 1
     with pytest.raises(RuntimeError, match="page pool too small"):
-        _session(head_level, on_demand, need - 1, planned).assign_pages(budgets)
+        _session(head_level, on_demand, need - 1).assign_pages(budgets)
     assert len(planned) == 1                                  # nothing was planned
 
 
 def test_assign_pages_on_demand_counts_no_pages_for_caches_beyond_their_table(monkeypatch):
     planned = []
     monkeypatch.setattr(xkv, "plan_append", lambda *a, **k: planned.append(a))
-    s = _session(False, True, 4 + 1 + 1, planned)
+    s = _session(False, True, 4 + 1 + 1)
     s.max_pages_per_seq = 6                                   # 96 rows: the first cache keeps 100 and gets no page
     s.assign_pages(np.array([96, 6]))
-    assert len(planned) == 1 and s.page_runs[0].tolist() == [[100, 50], [10, 10]]
+    assert len(planned) == 1 and planned[0][2].tolist() == [[100, 50], [10, 10]]
