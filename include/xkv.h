@@ -430,6 +430,9 @@ xkv_status xkv_store_rows(const xkv_dims* dims, const xkv_cache* cache, const vo
  * residency. Larger problems run a separate append-and-plan kernel first. Over an XKV_KV_E4M3 cache the call is one small
  * kernel (appends the new rows, advances seq_lens, clears counters) and one attention kernel whatever the number of
  * units; the rows are cut into equal shares, chunk_rows only sizes the workspace (fewer partial results, fewer shares).
+ * XKV_ERR_UNSUPPORTED where the pool has 2^31 rows of a KV head and more, or, over an XKV_KV_E4M3 cache, the call's caches
+ * (layers x sequences x KV heads) times (max_pages_per_seq * page_size + 448) / 16 reach 2^31 (this many blocks could take
+ * part if every table were full).
  */
 xkv_status xkv_decode_attn(const xkv_dims* dims, const xkv_cache* cache, int32_t layer_begin,
                            int32_t layer_end, const void* q, const void* k_new, const void* v_new,

@@ -1232,12 +1232,13 @@ xkv_status decode_attn_e4m3(const xkv_dims* d, const xkv_cache* c, int layer_beg
   const int tile = d->head_dim == 128 ? Cfg<128>::kTile : Cfg<64>::kTile;
   while (box < tile && c->page_size % (2 * box) == 0) box *= 2;
   const uint64_t page_rows = (uint64_t)c->n_pages * d->n_kv_heads * c->page_size;
-  CUtensorMap tk, tv;
-  if (!make_tmap(&tk, c->k_pages, d->head_dim, page_rows, box) || !make_tmap(&tv, c->v_pages, d->head_dim, page_rows, box))
-    return XKV_ERR_CUDA;
+  // the line of all caches, as long as their tables allow, has 31-bit places
   const int64_t max_rows = (int64_t)c->max_pages_per_seq * c->page_size;
   const int64_t caches = (int64_t)n_units * d->n_kv_heads, most = caches * ((max_rows + tile - 1) / tile);
   if (caches * ((max_rows + tile) / kScaleBlock + kCacheCost) >= (1ll << 31)) return XKV_ERR_UNSUPPORTED;
+  CUtensorMap tk, tv;
+  if (!make_tmap(&tk, c->k_pages, d->head_dim, page_rows, box) || !make_tmap(&tv, c->v_pages, d->head_dim, page_rows, box))
+    return XKV_ERR_CUDA;
   xkv_status s;
   if (k_new != nullptr) {
     s = append_e4m3(d, c, layer_begin, n_units, k_new, v_new, ws.header, ws.clear, ws.n_clear, st);

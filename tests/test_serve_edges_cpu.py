@@ -24,6 +24,15 @@ def test_plan_append_refuses_slot_maps_of_2_31_tokens():
     assert call(2 ** 31 - 2) == xkv.ERR_WORKSPACE             # (the next check)
 
 
+def test_decode_refuses_more_blocks_than_it_can_count():
+    """The caches of a call, as long as their tables allow, in blocks of 16 rows: fewer than 2^31."""
+    cache = xkv.Cache(256, 512, 768, 1024, 8, 256, 1 << 13, 100, 2048, 4096, xkv.KV_E4M3, 0)      # 2^21 rows a table
+
+    dims = xkv.Dims(64, 32, 32, 128, 1, 1, 0, 0.0, 32 * 128, 128)
+    assert xkv.lib().xkv_decode_attn(ctypes.byref(dims), ctypes.byref(cache), 0, 8, 16, None, None, 16, None, 0, 256, 1 << 40,
+                                     None) == xkv.ERR_UNSUPPORTED                          # 2^14 caches of 2^17 blocks
+
+
 def _session(head_level, on_demand, n_pages):
     """A session of 2 layers, 2 sequences, 2 KV heads as assign_pages sees it, without a device."""
     from paper_2412_05896_b200.pipeline import XkvSession
