@@ -113,12 +113,12 @@ def check_products(q, K, codes, scales, out, lse, what):
     assert abs(lse - want) <= dz + 2.0 ** -21 * (1 + abs(want)), f"{what}: lse {lse} for {want}"
 
 
-def check_scales(pool, Hq, q, out, lse, what):
+def check_scales(pool, Hq, q, out, lse, what, lens=None):
     G, qf, of, lf = Hq // pool.H, f64(q), f64(out), f64(lse)
     s = pool.dev_s["v"].cpu().numpy().astype(np.float64)
     for l in range(pool.L):
         for b in range(pool.B):
-            n = np.arange(int(pool.lens[l, b]))
+            n = np.arange(int((pool.lens if lens is None else lens)[l, b]))
             for g in range(pool.H):
                 sv = s[pool.table[l, b, n // pool.page], g, n % pool.page // 16]
                 K, V = pool.rows("k", l, b, g, len(n)), pool.rows("v", l, b, g, len(n))
@@ -358,3 +358,39 @@ def test_session_page_runs_of_two_requests_in_flight(on_demand):
         torch.cuda.synchronize()
     for a, b in zip(seen[:2], seen[2:]):
         assert torch.equal(a[0], b[0]) and torch.equal(a[1], b[1])
+
+
+# ------------------------------------------------------------------ attention with the step's new rows in the call
+@pytest.mark.parametrize("d,G", [(128, 4), (64, 1), (128, 7)])
+def test_decode_with_new_rows_in_a_graph(d, G):
+    """A captured call that appends, replayed right behind the kernels that write its inputs, against calls on a twin cache;
+    one cache is full from the start, one becomes full on the way."""
+    H, page = 2, 16
+    lens = [[0, 15, 2500, 40], [300, 2505, 16, 2512]]           # 157 pages a table: 2512 rows
+    pools = [Pool(lens, H, d, page, seed=d + G) for _ in range(2)]
+    assert pools[0].cols * page == 2512
+    dims = xkv.Dims(4, H * G, H, d, 1, 1, 0, 0.0, H * d, d)
+    ws = torch.zeros(xkv.workspace_bytes(xkv.OP_DECODE_ATTN, dims, n_layers=2, max_cache_len=2512), dtype=torch.uint8,
+                     device=DEV)
+    q, kn, vn = (torch.zeros(2, 4, n, d, dtype=torch.bfloat16, device=DEV) for n in (H * G, H, H))
+    out, lse = torch.zeros_like(q), torch.zeros(2, 4, H * G, device=DEV)
+    handle = pools[0].handle()
+    graph = torch.cuda.CUDAGraph()
+    with torch.cuda.graph(graph):
+        xkv.decode_attn(dims, handle, 0, 2, q, kn, vn, out, lse, 0, ws)
+    assert pools[0].seq_lens.tolist() == lens
+    for step in range(10):
+        gen = torch.Generator(device=DEV).manual_seed(step)
+        for t in (q, kn, vn):
+            t.copy_(torch.randn(t.shape, generator=gen, device=DEV).to(torch.bfloat16))
+        graph.replay()
+        got, got_lse = out.clone(), lse.clone()
+        want, want_lse, status = run_decode(pools[1], H * G, q, kn=kn, vn=vn)
+        assert status == xkv.ERR_CAPACITY and xkv.read_device_status(ws) == xkv.ERR_CAPACITY
+        assert torch.equal(got, want) and torch.equal(got_lse, want_lse), step
+        for x in "kv":
+            assert torch.equal(pools[0].dev[x], pools[1].dev[x])
+            assert torch.equal(pools[0].dev_s[x].view(torch.int32), pools[1].dev_s[x].view(torch.int32))
+        grown = np.minimum(np.asarray(lens) + step + 1, 2512)
+        assert np.array_equal(pools[0].seq_lens.cpu().numpy(), grown)
+        check_scales(pools[0], H * G, q, got, got_lse, f"step {step}", grown)
