@@ -25,11 +25,12 @@
 // what they add in pieces and joins costs more: 74.6 against 70.2 us for 363 MB, 150.8 against 140.2 us for 814 MB.)
 // Bound by HBM where caches are long, else by what a launch costs before the first and after the last byte (about 8 us: the
 // lengths, page ids and first tiles one after the other; the last tile's softmax, output, count and join).  Measured, device
-// time a call: 538 MB in two caches of 131 000 rows x 8 heads 92.8 us (0.88 of the measured copy rate; 7.4 TB/s between
-// the first tile and the last), 814 MB ragged batch 133.5 us (0.93), 363 MB of 2048 short caches 63.8 us (0.87), one request
-// of 2129 rows 12.4 us.  With five to eight heads a group the softmax warps bound it where caches are short or d = 64 (a
-// third of the issue slots, the rest waits on what comes before): 246 MB in 7168 caches of 84-157 rows, G = 7, 103 us;
-// 214 MB of d = 64, G = 5, 53 us.
+// time a call: 538 MB in two caches of 131 000 rows x 8 heads 92.6 us (0.88 of the measured copy rate; 7.4 TB/s between
+// the first tile and the last), 814 MB ragged batch 133.3 us (0.93), 363 MB of 2048 short caches 63.8 us (0.87), one request
+// of 2129 rows 12.5 us.  With five to eight heads a group the softmax warps bound it where caches are short or d = 64 (a
+// third of the issue slots, the rest waits on what comes before): 246 MB in 7168 caches of 84-157 rows, G = 7, 105 us;
+// 214 MB of d = 64, G = 5, 53.3 us.  A call that also appends (two launches in series) takes 2 us more for one request, 14 us more
+// for the ragged batch (146 us).
 //
 //   warp 6     finds the CTA's pieces of caches ("items") and lays out their queries as two codes per element
 //   warp 4     copies: TMA boxes of K and V, block scales

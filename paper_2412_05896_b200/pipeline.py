@@ -371,7 +371,8 @@ class XkvSession:
     def append(self, k: torch.Tensor, v: torch.Tensor, n_new) -> torch.Tensor:
         """Stores n_new[b] more rows of every sequence in every layer (a further turn of a conversation, a generated
         token): k, v bf16 [L, T, Hkv, d], the sequences' tokens one after the other, T = sum(n_new) (host integers).
-        Needs pages_on_demand.  Returns the slots, int64 [L, T] ([L, T*Hkv] in a head-level session)."""
+        Needs pages_on_demand.  Returns the slots, int64 [L, T] ([L, T*Hkv] in a head-level session); a cache that cannot
+        grow keeps its length and its tokens get slot -1 (device_status("append"))."""
         if not self.pages_on_demand:
             raise ValueError("append needs a session with pages_on_demand=True")
         n_new = np.asarray(n_new, dtype=np.int32)
