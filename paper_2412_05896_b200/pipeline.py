@@ -341,8 +341,11 @@ class XkvSession:
         start = np.concatenate([[0], np.cumsum(n.ravel())[:-1]]).reshape(self.L, self.n_caches)
         if int(start.ravel()[-1] + n.ravel()[-1]) > self.n_pages:
             raise RuntimeError("page pool too small for these budgets")
-        # every (layer, cache): its first page and its number of pages; expanded on the device
-        xkv.build_block_table(self._to_device(start), self._to_device(n), self.cache, self.n_caches)
+        # every (layer, cache): its first page and its number of pages, each from a 16-byte boundary on; expanded on the device
+        runs = np.zeros((2, -(-n.size // 4) * 4), dtype=np.int32)
+        runs[0, :n.size], runs[1, :n.size] = start.ravel(), n.ravel()
+        runs = self._to_device(runs)
+        xkv.build_block_table(runs[0], runs[1], self.cache, self.n_caches)
 
     def select_layer(self, layer: int, budget, k: torch.Tensor, v: torch.Tensor, sel: torch.Tensor | None = None,
                      per_sequence: bool = False) -> None:
