@@ -20,6 +20,9 @@
  *                         new K/V appended first                                     (Eq. 1; Sec. IV-A, generation phase)
  *      xkv_plan_append    serving: block tables, slot maps and new lengths of a step, pages taken from a free list
  *      xkv_store_rows     serving: any number of new K/V rows per sequence stored at their slots
+ *      xkv_fork_caches    serving: caches that become forks of others (sharing pages), are cut or freed
+ *      xkv_compact_pages  serving: the pages in use moved to the front of the pool
+ *      xkv_copy_pages     serving: pages copied from one pool into another
  *
  * Conventions that hold for every entry point
  *   - Plain C types only. "dev" = pointer to device memory of the current CUDA device,
@@ -82,6 +85,9 @@ typedef int32_t xkv_status;
 #define XKV_OP_PREFILL_ATTN   3
 #define XKV_OP_PLAN_APPEND    4
 #define XKV_OP_STORE_ROWS     5
+#define XKV_OP_FORK_CACHES    6
+#define XKV_OP_COMPACT_PAGES  7
+#define XKV_OP_COPY_PAGES     8
 
 /* Problem shape shared by the device entry points. */
 typedef struct xkv_dims {
@@ -405,6 +411,75 @@ xkv_status xkv_store_rows(const xkv_dims* dims, const xkv_cache* cache, const vo
                           const int64_t* slots, int64_t n_tokens, void* workspace, size_t workspace_bytes, void* stream);
 
 /*
+ * xkv_fork_caches -- caches of a batch that go on from others', are cut or freed, in one step for all layers (bookkeeping of
+ * the reduced caches whose sizes differ per layer, Sec. IV-A: samples of one prompt, beams of a search, requests that start
+ * from a cached prompt, drafts that are rejected, requests that are done).
+ *
+ * For every layer l and cache b, with a = parent[b] and lengths and tables as they were before the call:
+ *   n' = 0 if a = -1, else min(seq_lens[l][a], keep[l][b])
+ *   block_table[l][b][0 .. ceil(n' / page_size) - 1] = those entries of (l, a);  seq_lens[l][b] = n'
+ * so a = b leaves a cache as it is or cuts it, a = -1 frees it, and any other a makes it a fork of a that shares a's pages. Rows
+ * are only ever added behind the last one, so whole pages can stay shared; a partly filled last page cannot. Where others
+ * hold that page too (a fork and its parent, a cache cut inside a page that forks of it hold whole) it is replaced by a page
+ * of the free list with a copy of its rows, unless all of its holders are caches whose partly filled last page it is: then one of
+ * these (one that stays, a = b, if there is one, else the one of the lowest b) keeps it. Pages that no cache holds any more go back to
+ * the list.
+ *
+ * shares        dev int32 [n_pages]: the table entries that hold a page beyond the first; 0 for pages held once and for free
+ *               ones, so zero-filled before the first call (and xkv_plan_append need not know of it). Entries that count are those
+ *               below ceil(seq_lens / page_size) in the tables of every xkv_cache over the pool
+ * free_pages    dev int32 [n_free], pages_used dev int32 [1]: the list and the count of xkv_plan_append, both updated. Pages
+ *               for copies are taken first, in the order of (l, b), from position pages_used on; then the pages that are
+ *               returned are written, in ascending order, before the position that leaves, which is where the list begins now
+ * parent        dev int32 [batch]; numbers outside [-1, batch) are taken as b, device status XKV_ERR_INVALID_ARG
+ * keep          dev int32, row l at keep + l * keep_stride; keep_stride 0: the same counts for every layer, else >= batch.
+ *               Negative counts and keep = NULL: everything
+ * dims          batch (caches per layer: B * Hkv of them with head-level caches), n_kv_heads, head_dim; cache: everything
+ * workspace     dev, at least xkv_workspace_bytes(XKV_OP_FORK_CACHES, ...) bytes, 256-byte aligned
+ * Table entries behind a cache's last page, and rows of a new page behind its last row, stay as they are. A cache that needs a page
+ * when the list has ended keeps its whole pages only: device status XKV_ERR_CAPACITY. Page ids outside [0, n_pages) in used
+ * entries are not counted, and counters that do not agree with the tables leave a page where it is: device status
+ * XKV_ERR_INVALID_ARG. At most 16384 caches a layer.
+ */
+xkv_status xkv_fork_caches(const xkv_dims* dims, const xkv_cache* cache, const int32_t* parent, const int32_t* keep,
+                           int32_t keep_stride, int32_t* shares, int32_t* free_pages, int32_t n_free, int32_t* pages_used,
+                           void* workspace, size_t workspace_bytes, void* stream);
+
+/*
+ * xkv_compact_pages -- moves the pages in use to the front of the pool, so that what lies behind can be given up or handed out in
+ * one run (bookkeeping of the reduced caches, Sec. IV-A).
+ *
+ * With n_live pages held by used table entries (shared ones count once): pages below n_live stay where they are; the i-th page
+ * (in ascending order) of those in use from n_live on moves, rows and scales, to the i-th page below n_live that is not in use.
+ *   cache->block_table = table_before with the moved pages' new ids in used entries, other entries as in table_before
+ *   shares = shares_before along with the pages, 0 for pages not in use;  free_pages[i] = i for i >= n_live;  pages_used = n_live
+ * The tables of `cache` hold all pages in use.
+ *
+ * table_before  dev int32 [n_layers][batch][max_pages_per_seq], may be cache->block_table itself
+ * shares_before dev int32 [n_pages], may be shares itself; both NULL: no page is shared
+ * free_pages    dev out int32 [n_pages], NULL: not wanted (the list of xkv_plan_append that is NULL);  pages_used dev out int32 [1]
+ * dims          batch (caches per layer), n_kv_heads, head_dim; cache: everything (seq_lens is read)
+ * workspace     dev, at least xkv_workspace_bytes(XKV_OP_COMPACT_PAGES, ...) bytes, 256-byte aligned
+ * Page ids outside [0, n_pages) in used entries stay as they are: device status XKV_ERR_INVALID_ARG.
+ */
+xkv_status xkv_compact_pages(const xkv_dims* dims, const xkv_cache* cache, const int32_t* table_before,
+                             const int32_t* shares_before, int32_t* shares, int32_t* free_pages, int32_t* pages_used,
+                             void* workspace, size_t workspace_bytes, void* stream);
+
+/*
+ * xkv_copy_pages -- page dst[i] of one pool becomes a copy of page src[i] of another or the same pool, K, V and scales (a cache handed
+ * to another pool, a pool that grows or shrinks, a cache set aside; no counterpart in the paper).
+ *
+ * from, to      pages, scales, page_size, n_pages and kv_format are used; page_size and kv_format are the same
+ * src, dst      dev int32 [n_copies]; no page is written twice, and in one pool none that is written is read
+ * dims          n_kv_heads, head_dim
+ * workspace     dev, at least xkv_workspace_bytes(XKV_OP_COPY_PAGES, ...) bytes (the status word), 256-byte aligned
+ * An id outside its pool leaves its pair out: device status XKV_ERR_INVALID_ARG.
+ */
+xkv_status xkv_copy_pages(const xkv_dims* dims, const xkv_cache* from, const int32_t* src, const xkv_cache* to,
+                          const int32_t* dst, int64_t n_copies, void* workspace, size_t workspace_bytes, void* stream);
+
+/*
  * xkv_decode_attn -- one generation step of attention over the reduced caches of layers
  * [layer_begin, layer_end) (Eq. 1 with one query row per head; Sec. IV-A generation phase).
  *
@@ -479,6 +554,9 @@ xkv_status xkv_decode_attn_static(const xkv_dims* dims, const xkv_cache* cache, 
  *   XKV_OP_SCORE, XKV_OP_SELECT_COMPACT: dims, max_seqlen, total_tokens
  *   XKV_OP_PREFILL_ATTN, XKV_OP_STORE_ROWS: dims
  *   XKV_OP_PLAN_APPEND: dims (its batch), n_layers
+ *   XKV_OP_FORK_CACHES: dims (its batch), n_layers, max_seqlen = max_pages_per_seq, total_tokens = n_pages
+ *   XKV_OP_COMPACT_PAGES: total_tokens = n_pages
+ *   XKV_OP_COPY_PAGES: dims
  *   XKV_OP_DECODE_ATTN: dims, n_layers (layers per call), max_cache_len (upper bound of any
  *                       seq_lens entry, e.g. max_pages_per_seq*page_size), chunk_rows as passed
  * Returns 0 for invalid arguments.

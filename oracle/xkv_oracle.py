@@ -554,3 +554,75 @@ def plan_append(n_new, lens_before, table, page_size: int, free_pages, used: int
                 row += [-1] * a
         slots.append(row)
     return table, lens, slots, end, ok
+
+
+def fork_caches(parent, keep, lens_before, table, page_size: int, shares, free_pages, used: int):
+    """Caches that go on from others', are cut or freed.  parent [B] (-1: freed), keep [L, B] or None (negative: everything),
+    table [L, B, max_pages], shares [n_pages], the free list and the count handed out.  Returns (table, lens, shares,
+    free_pages, used, copies, ok), copies = [(page, its copy, rows)]."""
+    before, old = np.asarray(table), np.asarray(lens_before)
+    table, lens, shares, free_pages = before.copy(), old.copy(), list(shares), list(free_pages)
+    L, B, _ = table.shape
+
+    def pages(n):
+        return -(-int(n) // page_size)
+
+    dropped, parts, ok = set(), {}, True
+    for l in range(L):
+        for b in range(B):
+            a = int(parent[b])
+            n = 0 if a < 0 else int(old[l, a])
+            if keep is not None and keep[l][b] >= 0:
+                n = min(n, int(keep[l][b]))
+            lens[l, b] = n
+            table[l, b, :pages(n)] = before[l, a, :pages(n)]
+            for p in before[l, b, :pages(old[l, b])]:
+                shares[p] -= 1
+                dropped.add(int(p))
+            for p in table[l, b, :pages(n)]:
+                shares[p] += 1
+            if n % page_size:
+                parts[l, b] = int(table[l, b, pages(n) - 1])
+    returned = sorted(p for p in dropped if shares[p] == -1)
+    stays = {}                                            # page -> the cache whose last page it remains
+    for p in set(parts.values()):
+        holders = [(int(parent[b]) != b, b) for (l, b), q in parts.items() if q == p]
+        if len(holders) == shares[p] + 1:
+            stays[p] = min(holders)[1]
+    copies, asked, freed = [], 0, []
+    for (l, b), p in parts.items():
+        if stays.get(p) == b or (p not in stays and shares[p] == 0):
+            continue
+        if used + asked < len(free_pages):
+            copies.append((p, int(free_pages[used + asked]), int(lens[l, b]) % page_size))
+            table[l, b, pages(lens[l, b]) - 1] = copies[-1][1]
+        else:
+            lens[l, b] -= lens[l, b] % page_size
+            ok = False
+        asked += 1
+        freed.append(p)
+    for p in freed:
+        shares[p] -= 1
+    for p in returned:
+        shares[p] = 0
+    used += len(copies) - len(returned)
+    free_pages[used:used + len(returned)] = returned
+    return table, lens, np.asarray(shares), np.asarray(free_pages), used, copies, ok
+
+
+def compact_pages(table, lens, page_size: int, shares, n_pages: int):
+    """Pages in use moved to the front.  Returns (table, shares, n_live, moves), moves = {page: where it goes}."""
+    before, table, shares = np.asarray(table), np.asarray(table).copy(), np.asarray(shares)
+    L, B, _ = table.shape
+    in_use = sorted({int(p) for l in range(L) for b in range(B) for p in before[l, b, :-(-int(lens[l][b]) // page_size)]})
+    n_live = len(in_use)
+    gaps = [p for p in range(n_live) if p not in set(in_use)]
+    moves = dict(zip([p for p in in_use if p >= n_live], gaps))
+    for l in range(L):
+        for b in range(B):
+            for i in range(-(-int(lens[l][b]) // page_size)):
+                table[l, b, i] = moves.get(int(table[l, b, i]), table[l, b, i])
+    after = np.zeros(n_pages, dtype=shares.dtype)
+    for p in in_use:
+        after[moves.get(p, p)] = shares[p]
+    return table, after, n_live, moves

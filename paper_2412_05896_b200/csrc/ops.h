@@ -70,6 +70,17 @@ xkv_status plan_append(const xkv_cache* c, int batch, const int32_t* n_new, int 
                        const int32_t* free_pages, int n_free, const int32_t* pages_used_before, int32_t* pages_used_after,
                        int64_t* slots, int64_t slots_stride, void* workspace, cudaStream_t st);
 
+size_t fork_workspace_bytes(int n_layers, int batch, int max_pages_per_seq, int64_t n_pages);
+xkv_status fork_caches(const xkv_dims* d, const xkv_cache* c, const int32_t* parent, const int32_t* keep, int keep_stride,
+                       int32_t* shares, int32_t* free_pages, int n_free, int32_t* pages_used, void* workspace,
+                       cudaStream_t st);
+size_t compact_workspace_bytes(int64_t n_pages);
+xkv_status compact_pages(const xkv_dims* d, const xkv_cache* c, const int32_t* table_before, const int32_t* shares_before,
+                         int32_t* shares, int32_t* free_pages, int32_t* pages_used, void* workspace, cudaStream_t st);
+size_t copy_workspace_bytes();
+xkv_status copy_pages(const xkv_dims* d, const xkv_cache* from, const int32_t* src, const xkv_cache* to, const int32_t* dst,
+                      int64_t n_copies, void* workspace, cudaStream_t st);
+
 void set_profile_events(cudaEvent_t start, cudaEvent_t stop);
 void get_profile_events(cudaEvent_t* start, cudaEvent_t* stop);
 

@@ -278,6 +278,61 @@ xkv_status xkv_store_rows(const xkv_dims* dims, const xkv_cache* cache, const vo
   return store_rows(dims, cache, k, v, slots, n_tokens, workspace, static_cast<cudaStream_t>(stream));
 }
 
+xkv_status xkv_fork_caches(const xkv_dims* dims, const xkv_cache* cache, const int32_t* parent, const int32_t* keep,
+                           int32_t keep_stride, int32_t* shares, int32_t* free_pages, int32_t n_free, int32_t* pages_used,
+                           void* workspace, size_t workspace_bytes, void* stream) {
+  xkv_status s = check_dims(dims);
+  if (s != XKV_OK) return s;
+  if ((s = check_cache(cache, dims)) != XKV_OK) return s;
+  if (parent == nullptr || shares == nullptr || free_pages == nullptr || pages_used == nullptr || workspace == nullptr)
+    return XKV_ERR_INVALID_ARG;
+  if (!aligned16(parent) || !aligned16(keep) || !aligned16(shares) || !aligned16(free_pages) || !aligned16(pages_used) ||
+      (reinterpret_cast<uintptr_t>(workspace) & 255u) != 0)
+    return XKV_ERR_INVALID_ARG;
+  if (n_free < 0 || keep_stride < 0 || (keep_stride != 0 && keep_stride < dims->batch)) return XKV_ERR_INVALID_ARG;
+  if (dims->batch > plan_max_batch() || (int64_t)dims->batch * cache->n_layers >= (1ll << 31)) return XKV_ERR_UNSUPPORTED;
+  if (workspace_bytes < fork_workspace_bytes(cache->n_layers, dims->batch, cache->max_pages_per_seq, cache->n_pages))
+    return XKV_ERR_WORKSPACE;
+  return fork_caches(dims, cache, parent, keep, keep_stride, shares, free_pages, n_free, pages_used, workspace,
+                     static_cast<cudaStream_t>(stream));
+}
+
+xkv_status xkv_compact_pages(const xkv_dims* dims, const xkv_cache* cache, const int32_t* table_before,
+                             const int32_t* shares_before, int32_t* shares, int32_t* free_pages, int32_t* pages_used,
+                             void* workspace, size_t workspace_bytes, void* stream) {
+  xkv_status s = check_dims(dims);
+  if (s != XKV_OK) return s;
+  if ((s = check_cache(cache, dims)) != XKV_OK) return s;
+  if (table_before == nullptr || pages_used == nullptr || workspace == nullptr ||
+      (shares == nullptr) != (shares_before == nullptr))
+    return XKV_ERR_INVALID_ARG;
+  if (!aligned16(table_before) || !aligned16(shares_before) || !aligned16(shares) || !aligned16(free_pages) ||
+      !aligned16(pages_used) || (reinterpret_cast<uintptr_t>(workspace) & 255u) != 0)
+    return XKV_ERR_INVALID_ARG;
+  if ((int64_t)dims->batch * cache->n_layers >= (1ll << 31)) return XKV_ERR_UNSUPPORTED;
+  if (workspace_bytes < compact_workspace_bytes(cache->n_pages)) return XKV_ERR_WORKSPACE;
+  return compact_pages(dims, cache, table_before, shares_before, shares, free_pages, pages_used, workspace,
+                       static_cast<cudaStream_t>(stream));
+}
+
+xkv_status xkv_copy_pages(const xkv_dims* dims, const xkv_cache* from, const int32_t* src, const xkv_cache* to,
+                          const int32_t* dst, int64_t n_copies, void* workspace, size_t workspace_bytes, void* stream) {
+  xkv_status s = check_dims(dims);
+  if (s != XKV_OK) return s;
+  if (from == nullptr || to == nullptr || src == nullptr || dst == nullptr || workspace == nullptr) return XKV_ERR_INVALID_ARG;
+  for (const xkv_cache* c : {from, to}) {
+    if (c->k_pages == nullptr || c->v_pages == nullptr || !aligned16(c->k_pages) || !aligned16(c->v_pages) || c->n_pages <= 0)
+      return XKV_ERR_INVALID_ARG;
+    if ((s = check_page_size(c->page_size)) != XKV_OK || (s = check_format(c)) != XKV_OK) return s;
+  }
+  if (from->page_size != to->page_size || from->kv_format != to->kv_format) return XKV_ERR_INVALID_ARG;
+  if (!aligned16(src) || !aligned16(dst) || (reinterpret_cast<uintptr_t>(workspace) & 255u) != 0) return XKV_ERR_INVALID_ARG;
+  if (n_copies < 0 || n_copies >= (1ll << 31)) return XKV_ERR_INVALID_ARG;
+  if (workspace_bytes < copy_workspace_bytes()) return XKV_ERR_WORKSPACE;
+  if (n_copies == 0) return XKV_OK;
+  return copy_pages(dims, from, src, to, dst, n_copies, workspace, static_cast<cudaStream_t>(stream));
+}
+
 xkv_status xkv_decode_attn(const xkv_dims* dims, const xkv_cache* cache, int32_t layer_begin, int32_t layer_end,
                            const void* q, const void* k_new, const void* v_new, void* out, float* lse,
                            int32_t chunk_rows, void* workspace, size_t workspace_bytes, void* stream) {
@@ -341,6 +396,15 @@ size_t xkv_workspace_bytes(int32_t op, const xkv_dims* dims, int32_t max_seqlen,
     case XKV_OP_STORE_ROWS:
       if (check_dims(dims) != XKV_OK) return 0;
       return store_workspace_bytes();
+    case XKV_OP_FORK_CACHES:
+      if (dims->batch <= 0 || n_layers <= 0 || max_seqlen <= 0 || total_tokens <= 0 || total_tokens >= (1ll << 31)) return 0;
+      return fork_workspace_bytes(n_layers, dims->batch, max_seqlen, total_tokens);
+    case XKV_OP_COMPACT_PAGES:
+      if (total_tokens <= 0 || total_tokens >= (1ll << 31)) return 0;
+      return compact_workspace_bytes(total_tokens);
+    case XKV_OP_COPY_PAGES:
+      if (check_dims(dims) != XKV_OK) return 0;
+      return copy_workspace_bytes();
     default:
       return 0;
   }

@@ -19,6 +19,7 @@ ERR_INVALID_ARG, ERR_UNSUPPORTED, ERR_WORKSPACE, ERR_BUDGET = -1, -2, -3, -4
 ERR_CUDA, ERR_TIMEOUT, ERR_CAPACITY = -5, -6, -7
 POOL_MAX, POOL_AVG = 0, 1
 OP_SCORE, OP_SELECT_COMPACT, OP_DECODE_ATTN, OP_PREFILL_ATTN, OP_PLAN_APPEND, OP_STORE_ROWS = 0, 1, 2, 3, 4, 5
+OP_FORK_CACHES, OP_COMPACT_PAGES, OP_COPY_PAGES = 6, 7, 8
 BUDGET_PER_LAYER, BUDGET_PER_SEQUENCE, BUDGET_PER_HEAD = 0, 1, 2
 KV_BF16, KV_INT8, KV_E4M3 = 0, 1, 2
 SCALE_BLOCK = 16                 # KV_E4M3: consecutive cache slots that share a scale
@@ -26,7 +27,7 @@ SCALE_BLOCK = 16                 # KV_E4M3: consecutive cache slots that share a
 STATIC_SCRATCH_BYTES = 16 << 20
 
 EXPORTS = ("xkv_score", "xkv_score_lse", "xkv_prefill_attn", "xkv_batch_curves", "xkv_head_curves", "xkv_build_block_table", "xkv_alloc_budgets", "xkv_average_budgets", "xkv_select_compact", "xkv_decode_attn", "xkv_decode_attn_static",
-           "xkv_plan_append", "xkv_store_rows",
+           "xkv_plan_append", "xkv_store_rows", "xkv_fork_caches", "xkv_compact_pages", "xkv_copy_pages",
            "xkv_workspace_bytes",
            "xkv_read_device_status", "xkv_profile_events", "xkv_test_hooks", "xkv_launch_count", "xkv_status_string",
            "xkv_version")
@@ -96,6 +97,12 @@ def lib() -> ctypes.CDLL:
     L.xkv_plan_append.argtypes = [ctypes.POINTER(Cache), i32, vp, i32, vp, vp, i32, vp, vp, vp, i64, vp, sz, vp]
     L.xkv_store_rows.restype = i32
     L.xkv_store_rows.argtypes = [ctypes.POINTER(Dims), ctypes.POINTER(Cache), vp, vp, vp, i64, vp, sz, vp]
+    L.xkv_fork_caches.restype = i32
+    L.xkv_fork_caches.argtypes = [ctypes.POINTER(Dims), ctypes.POINTER(Cache), vp, vp, i32, vp, vp, i32, vp, vp, sz, vp]
+    L.xkv_compact_pages.restype = i32
+    L.xkv_compact_pages.argtypes = [ctypes.POINTER(Dims), ctypes.POINTER(Cache), vp, vp, vp, vp, vp, vp, sz, vp]
+    L.xkv_copy_pages.restype = i32
+    L.xkv_copy_pages.argtypes = [ctypes.POINTER(Dims), ctypes.POINTER(Cache), vp, ctypes.POINTER(Cache), vp, i64, vp, sz, vp]
     L.xkv_workspace_bytes.restype = sz
     L.xkv_workspace_bytes.argtypes = [i32, ctypes.POINTER(Dims), i32, i64, i32, i32, i32]
     L.xkv_read_device_status.restype = i32
@@ -263,6 +270,30 @@ def store_rows(dims: Dims, cache: Cache, k, v, slots, n_tokens: int, workspace, 
     """k, v dev bf16 rows (strides of dims) stored at slots dev int64 [n_tokens]; negative slots are skipped."""
     _check(lib().xkv_store_rows(ctypes.byref(dims), ctypes.byref(cache), _ptr(k), _ptr(v), _ptr(slots), n_tokens,
                                 _ptr(workspace), _nbytes(workspace), _stream(stream)), "xkv_store_rows")
+
+
+def fork_caches(dims: Dims, cache: Cache, parent, keep, keep_stride: int, shares, free_pages, n_free: int, pages_used,
+                workspace, stream=None) -> None:
+    """Cache b of every layer becomes cache parent[b] (dev int32 [B], -1: freed) cut to keep rows (dev int32 [B] (stride 0)
+    or [L, keep_stride], None: all); shares dev int32 [n_pages], the free list and its count are updated."""
+    _check(lib().xkv_fork_caches(ctypes.byref(dims), ctypes.byref(cache), _ptr(parent), _ptr(keep), keep_stride, _ptr(shares),
+                                 _ptr(free_pages), n_free, _ptr(pages_used), _ptr(workspace), _nbytes(workspace),
+                                 _stream(stream)), "xkv_fork_caches")
+
+
+def compact_pages(dims: Dims, cache: Cache, table_before, shares_before, shares, free_pages, pages_used, workspace,
+                  stream=None) -> None:
+    """Pages in use move to the front of the pool; tables, shares, free list (dev int32 [n_pages] or None) and its count
+    follow."""
+    _check(lib().xkv_compact_pages(ctypes.byref(dims), ctypes.byref(cache), _ptr(table_before), _ptr(shares_before),
+                                   _ptr(shares), _ptr(free_pages), _ptr(pages_used), _ptr(workspace), _nbytes(workspace),
+                                   _stream(stream)), "xkv_compact_pages")
+
+
+def copy_pages(dims: Dims, from_cache: Cache, src, to_cache: Cache, dst, n_copies: int, workspace, stream=None) -> None:
+    """Page dst[i] of to_cache's pool becomes a copy of page src[i] of from_cache's (dev int32 [n_copies])."""
+    _check(lib().xkv_copy_pages(ctypes.byref(dims), ctypes.byref(from_cache), _ptr(src), ctypes.byref(to_cache), _ptr(dst),
+                                n_copies, _ptr(workspace), _nbytes(workspace), _stream(stream)), "xkv_copy_pages")
 
 
 def decode_attn(dims: Dims, cache: Cache, layer_begin: int, layer_end: int, q, k_new, v_new, out, lse,
