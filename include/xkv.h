@@ -18,6 +18,7 @@
  *                         rows into a ragged paged cache                             (Alg. 2 steps 5-7)
  *   4. xkv_decode_attn    per generation step: attention over the ragged compacted caches,
  *                         new K/V appended first                                     (Eq. 1; Sec. IV-A, generation phase)
+ *      xkv_diff_decode_attn  the same for heads that attend by the difference of two softmax maps
  *      xkv_plan_append    serving: block tables, slot maps and new lengths of a step, pages taken from a free list
  *      xkv_store_rows     serving: any number of new K/V rows per sequence stored at their slots
  *      xkv_fork_caches    serving: caches that become forks of others (sharing pages), are cut or freed
@@ -88,6 +89,7 @@ typedef int32_t xkv_status;
 #define XKV_OP_FORK_CACHES    6
 #define XKV_OP_COMPACT_PAGES  7
 #define XKV_OP_COPY_PAGES     8
+#define XKV_OP_DIFF_DECODE_ATTN  9
 
 /* Problem shape shared by the device entry points. */
 typedef struct xkv_dims {
@@ -515,6 +517,31 @@ xkv_status xkv_decode_attn(const xkv_dims* dims, const xkv_cache* cache, int32_t
                            void* workspace, size_t workspace_bytes, void* stream);
 
 /*
+ * xkv_diff_decode_attn -- xkv_decode_attn for a model whose heads attend by the difference of two softmax maps with learned
+ * weights (no counterpart in the paper: another form of Eq. 1 over the same caches).
+ *
+ * A differential head h has a query row [q1 | q2] and reads cache rows whose K is [k1 | k2], halves of d/2 elements, and whose V has d:
+ *   a_s[c] = softmax over c of scale * q_s . k_s[c]   (s = 1, 2; scale 0 selects 1/sqrt(d/2))
+ *   y      = sum over c of (a_1[c] - lambda[h] a_2[c]) V_c
+ *   out    = y, or with a gain y / sqrt(mean of y^2 over its d elements + eps) * gain (the head's norm; a factor
+ *            1 - lambda_init goes into the gain)
+ * [k1 | k2] is an ordinary cache row: xkv_plan_append, xkv_store_rows, the page operations and every kv_format serve it as they are.
+ *
+ * dims       n_q_heads: differential heads; head_dim: d. n_q_heads / n_kv_heads at most 8; a KV head with more than four heads is
+ *            read more than once
+ * lambda     dev fp32 [Lr][Hq]
+ * gain       dev fp32 [Lr][d], NULL: no norm;  eps >= 0, finite
+ * lse        dev out fp32 [Lr][B][Hq][2], may be NULL: of each map
+ * workspace  dev, at least xkv_workspace_bytes(XKV_OP_DIFF_DECODE_ATTN, ...) bytes
+ * Everything else (q, k_new, v_new, the append, out, chunk_rows, statuses, limits, rows of empty caches) as in xkv_decode_attn. The
+ * difference, its norm and everything before them are fp32; weights are rounded as there.
+ */
+xkv_status xkv_diff_decode_attn(const xkv_dims* dims, const xkv_cache* cache, int32_t layer_begin, int32_t layer_end,
+                                const void* q, const void* k_new, const void* v_new, const float* lambda, const float* gain,
+                                float eps, void* out, float* lse, int32_t chunk_rows, void* workspace, size_t workspace_bytes,
+                                void* stream);
+
+/*
  * xkv_decode_attn_static -- xkv_decode_attn for callers that cannot hand the library a workspace.
  * (The paper has no counterpart: this is the same operation with a different memory arrangement.)
  *
@@ -557,7 +584,7 @@ xkv_status xkv_decode_attn_static(const xkv_dims* dims, const xkv_cache* cache, 
  *   XKV_OP_FORK_CACHES: dims (its batch), n_layers, max_seqlen = max_pages_per_seq, total_tokens = n_pages
  *   XKV_OP_COMPACT_PAGES: total_tokens = n_pages
  *   XKV_OP_COPY_PAGES: dims
- *   XKV_OP_DECODE_ATTN: dims, n_layers (layers per call), max_cache_len (upper bound of any
+ *   XKV_OP_DECODE_ATTN, XKV_OP_DIFF_DECODE_ATTN: dims, n_layers (layers per call), max_cache_len (upper bound of any
  *                       seq_lens entry, e.g. max_pages_per_seq*page_size), chunk_rows as passed
  * Returns 0 for invalid arguments.
  */

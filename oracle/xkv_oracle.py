@@ -626,3 +626,24 @@ def compact_pages(table, lens, page_size: int, shares, n_pages: int):
     for p in in_use:
         after[moves.get(p, p)] = shares[p]
     return table, after, n_live, moves
+
+
+def diff_attention(q: np.ndarray, K: np.ndarray, V: np.ndarray, lam: float, gain: np.ndarray | None = None, eps: float = 0.0,
+                   scale: float | None = None) -> tuple[np.ndarray, np.ndarray]:
+    """One differential head: q [d] = [q1 | q2], K [n, d] of rows [k1 | k2], V [n, d].  Returns (out [d], log sums [2])."""
+    half = q.shape[0] // 2
+    scale = half ** -0.5 if scale is None else scale
+    if K.shape[0] == 0:
+        return np.zeros_like(q), np.full(2, -np.inf)
+    maps, sums = [], []
+    for part in (slice(0, half), slice(half, None)):
+        z = scale * (K[:, part] @ q[part])
+        top = z.max()
+        e = np.exp(z - top)
+        sums.append(top + np.log(e.sum()))
+        maps.append(e / e.sum())
+    y = (maps[0] - lam * maps[1]) @ V
+    if gain is not None:
+        ms = np.mean(y * y)
+        y = y / np.sqrt(ms + eps) * gain if ms > 0 else y
+    return y, np.array(sums)

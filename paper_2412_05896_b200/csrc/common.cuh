@@ -126,6 +126,12 @@ __device__ __forceinline__ void bf16x8_to_f32(const uint4& v, float (&x)[8]) {
   x[4] = bf16_lo(v.z); x[5] = bf16_hi(v.z); x[6] = bf16_lo(v.w); x[7] = bf16_hi(v.w);
 }
 
+// 1 / sqrt(mean square + eps) of D elements whose squares sum to sq (an all-zero row stays zero whatever eps is).
+template <int D>
+__device__ __forceinline__ float diff_norm(float sq, float eps) {
+  return sq > 0.f ? rsqrtf(fmaf(sq, 1.f / D, eps)) : 0.f;
+}
+
 // ---------------------------------------------------------------------------------------------
 // mbarrier (shared::cta) and TMA tensor loads.  Every wait is bounded.
 // ---------------------------------------------------------------------------------------------

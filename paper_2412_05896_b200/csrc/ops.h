@@ -34,10 +34,31 @@ xkv_status batch_curves(const float* gains, int n_layers, int batch, int curve_l
 xkv_status head_curves(const xkv_dims* d, const float* scores, const float* sorted, const int32_t* cu_seqlens,
                        int64_t total_tokens, int max_seqlen, float* out, int curve_len, cudaStream_t st);
 
-size_t decode_workspace_bytes(const xkv_dims* d, int n_layers, int max_cache_len, int chunk_rows);
+// Differential heads of a decode step.  A head's query row is [q1 | q2], a key row [k1 | k2]; its two maps are two query rows of
+// an ordinary group, [q1 | 0] and [0 | q2], and its output is the difference of their outputs, the second times lambda.  A
+// group has at most eight query rows, so a KV head with more than four heads is streamed `subs` times.
+struct DiffHeads {
+  const float* lambda;   // [layers of the call][n_q_heads]
+  const float* gain;     // [layers of the call][d], nullptr: no norm
+  float eps;
+  int32_t group;         // heads of a KV head
+  int32_t subs;          // times it is streamed
+  int32_t per_sub;       // heads of a streaming (the last may have fewer)
+#ifdef __CUDACC__
+  // of streaming h = KV head * subs + sub: its heads, and the first of them
+  __host__ __device__ int heads(int h) const { return min(per_sub, group - h % subs * per_sub); }
+  __host__ __device__ int first_head(int h) const { return h / subs * group + h % subs * per_sub; }
+#endif
+};
+DiffHeads diff_heads(const xkv_dims* d, const float* lambda, const float* gain, float eps);
+// The heads as a decode step streams them: n_kv_heads streamings a sequence with an ordinary group of query rows each.
+xkv_dims streamed_dims(const xkv_dims* d, const DiffHeads& h);
+
+size_t decode_workspace_bytes(const xkv_dims* d, int n_layers, int max_cache_len, int chunk_rows, bool diff);
 xkv_status decode_attn(const xkv_dims* d, const xkv_cache* c, int layer_begin, int layer_end, const void* q,
                        const void* k_new, const void* v_new, void* out, float* lse, int chunk_rows,
-                       void* workspace, size_t workspace_bytes, cudaStream_t st, bool clear_status = false);
+                       void* workspace, size_t workspace_bytes, cudaStream_t st, bool clear_status = false,
+                       const DiffHeads* diff = nullptr);
 
 xkv_status decode_attn_static(const xkv_dims* d, const xkv_cache* c, int layer_begin, int layer_end,
                               const void* q, const void* k_new, const void* v_new, void* out, float* lse,
@@ -54,7 +75,7 @@ struct DecodeScratch {
 };
 xkv_status decode_attn_e4m3(const xkv_dims* d, const xkv_cache* c, int layer_begin, int n_layers, const void* q,
                             const void* k_new, const void* v_new, void* out, float* lse, const DecodeScratch& ws,
-                            cudaStream_t st);
+                            cudaStream_t st, const DiffHeads* diff);
 // One new row per (layer, sequence) and KV head stored in a cache of 8-bit floats, lengths advanced; n_clear words are
 // cleared on the way.
 xkv_status append_e4m3(const xkv_dims* d, const xkv_cache* c, int layer_begin, int n_units, const void* k_new,

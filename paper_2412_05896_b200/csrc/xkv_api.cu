@@ -352,6 +352,28 @@ xkv_status xkv_decode_attn(const xkv_dims* dims, const xkv_cache* cache, int32_t
                      workspace_bytes, static_cast<cudaStream_t>(stream));
 }
 
+xkv_status xkv_diff_decode_attn(const xkv_dims* dims, const xkv_cache* cache, int32_t layer_begin, int32_t layer_end,
+                                const void* q, const void* k_new, const void* v_new, const float* lambda, const float* gain,
+                                float eps, void* out, float* lse, int32_t chunk_rows, void* workspace, size_t workspace_bytes,
+                                void* stream) {
+  xkv_status s = check_dims(dims);
+  if (s != XKV_OK) return s;
+  s = check_cache(cache, dims);
+  if (s != XKV_OK) return s;
+  if (q == nullptr || out == nullptr || workspace == nullptr || lambda == nullptr) return XKV_ERR_INVALID_ARG;
+  if ((k_new == nullptr) != (v_new == nullptr)) return XKV_ERR_INVALID_ARG;
+  if (!aligned16(q) || !aligned16(k_new) || !aligned16(v_new) || !aligned16(out) || !aligned16(lse) || !aligned16(lambda) ||
+      !aligned16(gain) || (reinterpret_cast<uintptr_t>(workspace) & 255u) != 0)
+    return XKV_ERR_INVALID_ARG;
+  if (!(eps >= 0.f) || std::isinf(eps)) return XKV_ERR_INVALID_ARG;
+  if (layer_begin < 0 || layer_end <= layer_begin || layer_end > cache->n_layers) return XKV_ERR_INVALID_ARG;
+  if (chunk_rows < 0 || chunk_rows % 64 != 0) return XKV_ERR_INVALID_ARG;
+  if (dims->n_q_heads / dims->n_kv_heads > 8) return XKV_ERR_UNSUPPORTED;
+  const DiffHeads diff = diff_heads(dims, lambda, gain, eps);
+  return decode_attn(dims, cache, layer_begin, layer_end, q, k_new, v_new, out, lse, chunk_rows, workspace, workspace_bytes,
+                     static_cast<cudaStream_t>(stream), /*clear_status=*/false, &diff);
+}
+
 xkv_status xkv_decode_attn_static(const xkv_dims* dims, const xkv_cache* cache, int32_t layer_begin,
                                   int32_t layer_end, const void* q, const void* k_new, const void* v_new,
                                   void* out, float* lse, int32_t chunk_rows, int32_t* status_out, void* stream) {
@@ -386,10 +408,11 @@ size_t xkv_workspace_bytes(int32_t op, const xkv_dims* dims, int32_t max_seqlen,
       if (check_dims(dims) != XKV_OK) return 0;
       return prefill_workspace_bytes();
     case XKV_OP_DECODE_ATTN:
+    case XKV_OP_DIFF_DECODE_ATTN:
       if (check_dims(dims) != XKV_OK || n_layers <= 0 || max_cache_len < 0 || chunk_rows < 0 ||
           chunk_rows % 64 != 0)
         return 0;
-      return decode_workspace_bytes(dims, n_layers, max_cache_len, chunk_rows);
+      return decode_workspace_bytes(dims, n_layers, max_cache_len, chunk_rows, op == XKV_OP_DIFF_DECODE_ATTN);
     case XKV_OP_PLAN_APPEND:
       if (dims->batch <= 0 || n_layers <= 0) return 0;
       return plan_workspace_bytes(n_layers, dims->batch);

@@ -69,7 +69,10 @@ struct DecodeParams {
   float* v_scales;
   const int32_t* block_table;
   int32_t* seq_lens;
-  int32_t layer_begin, n_layers, batch, n_q_heads, n_kv_heads, group;
+  // n_heads caches per (layer, sequence) are streamed with `group` query rows each.  Differential heads (see DiffHeads): the two
+  // maps of diff_group heads of a KV head are query rows, so a KV head with more than four heads is streamed more than once.
+  int32_t layer_begin, n_layers, batch, n_q_heads, n_kv_heads, n_heads, group;
+  DiffHeads diff;
   int32_t page_size, max_pages_per_seq, n_pages;
   int32_t chunk_rows_forced, max_items;
   int32_t fused_plan, do_append;   // fused_plan: the attention kernel plans in its own prologue and appends itself
@@ -213,7 +216,7 @@ __device__ void plan_items(const DecodeParams& p) {
   if (tid == 0) {
     long long total = 0;
     for (int w = 0; w < n_warps; ++w) total += s_red[w];
-    total *= p.n_kv_heads;
+    total *= p.n_heads;
     const int chunk = choose_chunk(total, p.chunk_rows_forced);
     s_chunk = chunk;
     s_carry = 0;
@@ -251,10 +254,10 @@ __device__ void plan_items(const DecodeParams& p) {
     const int excl = carry + s_scan[warp] + incl - nc;
     if (e < n_units && nc > 1) p.multi_list[atomicAdd(&s_multi, 1)] = e;
     if (e < n_units) {
-      const int first = excl * p.n_kv_heads;
+      const int first = excl * p.n_heads;
       p.unit_info[e] = make_int2(first, nc);
-      if (first + nc * p.n_kv_heads <= p.max_items) {
-        for (int h = 0; h < p.n_kv_heads; ++h)
+      if (first + nc * p.n_heads <= p.max_items) {
+        for (int h = 0; h < p.n_heads; ++h)
           for (int c = 0; c < nc; ++c) {
             const int rb = c * chunk;
             const int re = min(n, rb + chunk);
@@ -267,7 +270,7 @@ __device__ void plan_items(const DecodeParams& p) {
     __syncthreads();
   }
   if (tid == 0) {
-    const int n_items = s_carry * p.n_kv_heads;
+    const int n_items = s_carry * p.n_heads;
     if (n_items > p.max_items) {
       record_status(p.hdr, XKV_ERR_WORKSPACE);
       p.hdr->n_items = 0;
@@ -298,7 +301,7 @@ __global__ void __launch_bounds__(kPrepThreads) decode_prepare_kernel(DecodePara
 }
 
 // ---------------------------------------------------------------------------------------------
-template <int D, bool Q8>
+template <int D, bool Q8, bool Diff>
 __global__ void __launch_bounds__((Cfg<D, Q8>::kThreads), 1)
 decode_attn_kernel(const __grid_constant__ CUtensorMap tmap_k, const __grid_constant__ CUtensorMap tmap_v,
                    const DecodeParams p) {
@@ -334,6 +337,13 @@ decode_attn_kernel(const __grid_constant__ CUtensorMap tmap_k, const __grid_cons
 
   const bool fused = p.fused_plan != 0;
   const int n_units = p.n_layers * p.batch;
+  const int n_heads = Diff ? p.n_heads : p.n_kv_heads;
+  // KV head of a streamed cache, and its first query head's row of q and out
+  auto kv_head = [&](int h) -> int { return Diff ? h / p.diff.subs : h; };
+  auto first_row = [&](int e, int h) -> size_t {
+    if constexpr (Diff) return (size_t)e * p.n_q_heads + p.diff.first_head(h);
+    return (size_t)e * p.n_q_heads + (size_t)h * p.group;
+  };
   // Length of unit e as this launch sees it: the stored length, plus the row this call appends when it fits the
   // page table.  seq_lens itself is only advanced by the last CTA to leave, so this reads the same at any time.
   const int cap_rows = p.max_pages_per_seq * p.page_size;
@@ -363,7 +373,7 @@ decode_attn_kernel(const __grid_constant__ CUtensorMap tmap_k, const __grid_cons
     long long total = 0;
 #pragma unroll
     for (int w8 = 0; w8 < C::kWarps; ++w8) total += s_rows[w8];
-    const int chunk = choose_chunk(total * p.n_kv_heads, p.chunk_rows_forced);
+    const int chunk = choose_chunk(total * n_heads, p.chunk_rows_forced);
     int cnt = 0, mcnt = 0;
 #pragma unroll
     for (int i = 0; i < kPer; ++i) {
@@ -410,7 +420,7 @@ decode_attn_kernel(const __grid_constant__ CUtensorMap tmap_k, const __grid_cons
       s_excl[n_units] = all;
       s_plan[0] = chunk;
       s_plan[1] = mall;
-      s_plan[2] = ((long long)all * p.n_kv_heads <= (long long)p.max_items) ? all * p.n_kv_heads : -1;
+      s_plan[2] = ((long long)all * n_heads <= (long long)p.max_items) ? all * n_heads : -1;
       if (blockIdx.x == 0) {
         p.hdr->chunk_rows = chunk;
         p.hdr->n_items = s_plan[2] < 0 ? 0 : s_plan[2];
@@ -426,7 +436,7 @@ decode_attn_kernel(const __grid_constant__ CUtensorMap tmap_k, const __grid_cons
   // work item idx -> {unit e, KV head, first row, end row}
   auto item_desc = [&](int idx) -> int4 {
     if (!fused) return p.items[idx];
-    const int q = idx / p.n_kv_heads;
+    const int q = idx / n_heads;
     int lo = 0, hi = n_units;                      // s_excl[lo] <= q < s_excl[hi]
     while (hi - lo > 1) {
       const int mid = (lo + hi) >> 1;
@@ -434,7 +444,7 @@ decode_attn_kernel(const __grid_constant__ CUtensorMap tmap_k, const __grid_cons
       else hi = mid;
     }
     const int first_chunk = s_excl[lo], nc = s_excl[lo + 1] - first_chunk;
-    const int local = idx - first_chunk * p.n_kv_heads;
+    const int local = idx - first_chunk * n_heads;
     const int h = local / nc, c = local % nc;
     const int n = unit_len(lo);
     const int rb = c * plan_chunk;
@@ -443,7 +453,7 @@ decode_attn_kernel(const __grid_constant__ CUtensorMap tmap_k, const __grid_cons
   // {first work item of the unit's KV head 0, chunks per KV head}
   auto unit_info = [&](int e) -> int2 {
     if (!fused) return p.unit_info[e];
-    return make_int2(s_excl[e] * p.n_kv_heads, s_excl[e + 1] - s_excl[e]);
+    return make_int2(s_excl[e] * n_heads, s_excl[e + 1] - s_excl[e]);
   };
   const int gid = lane >> 2, tig = lane & 3;
   const int mat = lane >> 3, mrow = lane & 7;
@@ -495,7 +505,7 @@ decode_attn_kernel(const __grid_constant__ CUtensorMap tmap_k, const __grid_cons
       int page = __shfl_sync(0xffffffffu, p_pages, tile - p_page_tile0);
       page = min(max(page, 0), p.n_pages - 1);
       if (lane == 0) {
-        const int grow = (page * p.n_kv_heads + p_desc.y) * p.page_size + p_row % p.page_size;
+        const int grow = (page * p.n_kv_heads + kv_head(p_desc.y)) * p.page_size + p_row % p.page_size;
         const int s = issued % C::kStages;
         uint8_t* ks = ring + (size_t)s * C::kStageBytes;
         mbar_arrive_expect_tx(&full_bar[s], kTxBytes);
@@ -556,7 +566,8 @@ decode_attn_kernel(const __grid_constant__ CUtensorMap tmap_k, const __grid_cons
     --fifo_count;
     const int e = I.x, h = I.y;
     const int nc = unit_info(e).y;
-    const size_t q_row0 = ((size_t)e * p.n_q_heads + (size_t)h * G);
+    const size_t q_row0 = first_row(e, h);
+    const int n_rows = Diff ? 2 * p.diff.heads(h) : G;       // query rows that there are (Diff: row 2 j + s is map s of head j)
 
     // Q^T as the B operand: lane (gid, tig) holds head gid, columns 16*ks + 2*tig (+1) and + 8
     uint32_t qb[D / 16][2];
@@ -564,14 +575,16 @@ decode_attn_kernel(const __grid_constant__ CUtensorMap tmap_k, const __grid_cons
     for (int ks = 0; ks < D / 16; ++ks) {
       qb[ks][0] = 0u;
       qb[ks][1] = 0u;
-      if (gid < G) {
-        const __nv_bfloat16* qp = p.q + (q_row0 + gid) * D + 16 * ks + 2 * tig;
+      // Diff: the half of the head's row that is not the map's stays zero
+      if (gid < n_rows && (!Diff || (ks >= D / 32) == ((gid & 1) != 0))) {
+        const size_t q_row = q_row0 + (Diff ? gid >> 1 : gid);
+        const __nv_bfloat16* qp = p.q + q_row * D + 16 * ks + 2 * tig;
         qb[ks][0] = *reinterpret_cast<const uint32_t*>(qp);
         qb[ks][1] = *reinterpret_cast<const uint32_t*>(qp + 8);
         if constexpr (Q8) {
           // The 8-bit path multiplies in fp16, and a lane's K fragment of this k-step holds the four consecutive
           // columns 16*ks + 4*tig .. + 3 (two registers of two): the query columns follow that order.
-          const uint2 four = *reinterpret_cast<const uint2*>(p.q + (q_row0 + gid) * D + 16 * ks + 4 * tig);
+          const uint2 four = *reinterpret_cast<const uint2*>(p.q + q_row * D + 16 * ks + 4 * tig);
           qb[ks][0] = pack_f16(bf16_lo(four.x), bf16_hi(four.x));
           qb[ks][1] = pack_f16(bf16_lo(four.y), bf16_hi(four.y));
         }
@@ -661,11 +674,13 @@ decode_attn_kernel(const __grid_constant__ CUtensorMap tmap_k, const __grid_cons
     auto patch_new_row = [&](uint32_t idx) {
       constexpr int kPieces = D / 8;                     // 16-byte pieces of one row
       const int r = (new_slot - I.z) % kTileRows;
-      const size_t src = ((size_t)e * p.n_kv_heads + h) * D;
+      const int kvh = kv_head(h);
+      const size_t src = ((size_t)e * p.n_kv_heads + kvh) * D;
       const int le = (p.layer_begin + e / p.batch) * p.batch + e % p.batch;
       const int page = p.block_table[(size_t)le * p.max_pages_per_seq + new_slot / p.page_size];
-      const bool page_ok = page >= 0 && page < p.n_pages;
+      bool page_ok = page >= 0 && page < p.n_pages;
       if (!page_ok && lane == 0) record_status(p.hdr, XKV_ERR_CAPACITY);
+      if constexpr (Diff) page_ok = page_ok && h % p.diff.subs == 0;      // the KV head's first streaming stores the row
       if constexpr (Q8) {
         // The new row is quantised here (its D/8 pieces on consecutive lanes: K on the first D/8 lanes, V on the next
         // ones); its bytes and scales go into the landed raw tile and into the page.
@@ -681,7 +696,7 @@ decode_attn_kernel(const __grid_constant__ CUtensorMap tmap_k, const __grid_cons
           *reinterpret_cast<uint2*>(raw + off) = bytes;
           if (c == 0) raw_scales(st)[is_v * kTileRows + r] = sc;
           if (page_ok) {
-            const size_t slot = ((size_t)page * p.n_kv_heads + h) * p.page_size + new_slot % p.page_size;
+            const size_t slot = ((size_t)page * p.n_kv_heads + kvh) * p.page_size + new_slot % p.page_size;
             *reinterpret_cast<uint2*>(reinterpret_cast<uint8_t*>(is_v ? p.v_pages : p.k_pages) + slot * D + c * 8) = bytes;
             if (c == 0) (is_v ? p.v_scales : p.k_scales)[slot] = sc;
           }
@@ -694,7 +709,7 @@ decode_attn_kernel(const __grid_constant__ CUtensorMap tmap_k, const __grid_cons
           *reinterpret_cast<uint4*>(ks + is_v * C::kTileBytes + (c >> 3) * C::kBoxBytes + r * 128 +
                                     (((c & 7) ^ (r & 7)) << 4)) = val;
           if (page_ok) {
-            const size_t dst = (((size_t)page * p.n_kv_heads + h) * p.page_size + new_slot % p.page_size) * D + c * 8;
+            const size_t dst = (((size_t)page * p.n_kv_heads + kvh) * p.page_size + new_slot % p.page_size) * D + c * 8;
             *reinterpret_cast<uint4*>((is_v ? p.v_pages : p.k_pages) + dst) = val;
           }
         }
@@ -833,6 +848,50 @@ decode_attn_kernel(const __grid_constant__ CUtensorMap tmap_k, const __grid_cons
     auto store_out = [&](float (&acc)[D / 16][4], const float (&den)[2], const float (&mx)[2]) {
       const float inv0 = den[0] > 0.f ? 1.f / den[0] : 0.f;
       const float inv1 = den[1] > 0.f ? 1.f / den[1] : 0.f;
+      if constexpr (Diff) {
+        // The lane's two rows are the two maps of head tig: their difference and its norm stay in registers.
+        const bool live = 2 * tig < n_rows;
+        const int at = e / p.batch;                            // the unit's layer in the call
+        const size_t row = q_row0 + tig;
+        const float lam = live ? __ldg(&p.diff.lambda[(size_t)at * p.n_q_heads + p.diff.first_head(h) + tig]) * inv1 : 0.f;
+        float sq = 0.f;
+#pragma unroll
+        for (int mt = 0; mt < D / 16; ++mt)
+#pragma unroll
+          for (int i = 0; i < 2; ++i) {                        // the difference takes the place of the first map
+            float& y = acc[mt][2 * i];
+            y = y * inv0 - acc[mt][2 * i + 1] * lam;
+            sq = fmaf(y, y, sq);
+          }
+        if (p.diff.gain != nullptr) {
+#pragma unroll
+          for (int x = 4; x < 32; x <<= 1) sq += __shfl_xor_sync(0xffffffffu, sq, x);
+          const float r = diff_norm<D>(sq, p.diff.eps);
+          const float* gain = p.diff.gain + (size_t)at * D;
+#pragma unroll
+          for (int mt = 0; mt < D / 16; ++mt)
+#pragma unroll
+            for (int i = 0; i < 2; ++i) acc[mt][2 * i] *= r * __ldg(&gain[16 * mt + (Q8 ? 2 * gid + i : gid + 8 * i)]);
+        }
+#pragma unroll
+        for (int mt = 0; mt < D / 16; ++mt) {
+          const uint32_t w = pack_bf16(acc[mt][0], acc[mt][2]);
+          if constexpr (Q8) {
+            if (live) *reinterpret_cast<uint32_t*>(p.out + row * D + 16 * mt + 2 * gid) = w;
+          } else {
+            // columns 16 mt + gid and + 8 of head tig; transposed: of head gid / 2, columns 8 (gid & 1) + 2 tig and + 1
+            const uint32_t t = movmatrix_trans(w);
+            if (gid < n_rows)
+              *reinterpret_cast<uint32_t*>(p.out + (q_row0 + (gid >> 1)) * D + 16 * mt + 8 * (gid & 1) + 2 * tig) = t;
+          }
+        }
+        if (gid == 0 && live && p.lse != nullptr) {
+#pragma unroll
+          for (int hh = 0; hh < 2; ++hh)
+            p.lse[2 * row + hh] = den[hh] > 0.f ? (mx[hh] + log2f(den[hh])) * 0.6931471805599453f : -INFINITY;
+        }
+        return;
+      }
       __nv_bfloat16* orow = p.out + (q_row0 + gid) * D;
 #pragma unroll
       for (int mt = 0; mt < D / 16; ++mt) {
@@ -884,7 +943,7 @@ decode_attn_kernel(const __grid_constant__ CUtensorMap tmap_k, const __grid_cons
       __syncwarp();                 // the lanes' partial results are ordered before lane 0's fence (cumulative)
       if (lane == 0 && item != p.withhold_item) {
         __threadfence();
-        atomicAdd(&p.tickets[e * p.n_kv_heads + h], 1);     // one more chunk of this unit is published
+        atomicAdd(&p.tickets[e * n_heads + h], 1);     // one more chunk of this unit is published
       }
     }
   }
@@ -895,25 +954,32 @@ decode_attn_kernel(const __grid_constant__ CUtensorMap tmap_k, const __grid_cons
   // comes here only after it has finished every item it took) and streaming warps wait for nothing but their own
   // copies, so the bounded wait below ends.
   constexpr int kCols = D / 32;
-  const int n_jobs = n_multi * p.n_kv_heads * G;
+  constexpr int kMaps = Diff ? 2 : 1;             // query rows of a job
+  const int job_heads = G / kMaps;
+  const int n_jobs = n_multi * n_heads * job_heads;
   while (!aborted) {
     int job = 0;
     if (lane == 0) job = atomicAdd(&p.hdr->merge_counter, 1);
     job = __shfl_sync(0xffffffffu, job, 0);
     if (job >= n_jobs) break;
-    const int g = job % G, uh = job / G;
-    const int h = uh % p.n_kv_heads;
-    const int e = fused ? (int)s_multi[uh / p.n_kv_heads] : p.multi_list[uh / p.n_kv_heads];
+    const int g0 = job % job_heads, uh = job / job_heads;
+    const int h = uh % n_heads;
+    const int e = fused ? (int)s_multi[uh / n_heads] : p.multi_list[uh / n_heads];
+    if (Diff && g0 >= p.diff.heads(h)) continue;
     const int2 ui = unit_info(e);
     const int nc = ui.y, first = ui.x + h * nc;
     int ready = 1;
-    if (lane == 0) ready = spin_until_ge(&p.tickets[e * p.n_kv_heads + h], nc, p.wait_ns, 200) ? 1 : 0;
+    if (lane == 0) ready = spin_until_ge(&p.tickets[e * n_heads + h], nc, p.wait_ns, 200) ? 1 : 0;
     ready = __shfl_sync(0xffffffffu, ready, 0);
     if (!ready) {
       if (lane == 0) record_status(p.hdr, XKV_ERR_TIMEOUT);
       break;
     }
     __threadfence();
+    [[maybe_unused]] float y[kCols] = {};         // Diff: the difference of the two maps
+#pragma unroll 1
+    for (int map = 0; map < kMaps; ++map) {
+    const int g = g0 * kMaps + map;
     float m_run = -3.0e38f, den = 0.f, acc[kCols];
 #pragma unroll
     for (int j = 0; j < kCols; ++j) acc[j] = 0.f;
@@ -962,13 +1028,38 @@ decode_attn_kernel(const __grid_constant__ CUtensorMap tmap_k, const __grid_cons
         }
       }
     }
-    const size_t row = (size_t)e * p.n_q_heads + (size_t)h * G + g;
+    const size_t row = first_row(e, h) + g0;
     const float inv = den > 0.f ? 1.f / den : 0.f;
+    if constexpr (Diff) {
+      const int at = e / p.batch;
+      const float w = map == 0 ? inv : -inv * __ldg(&p.diff.lambda[(size_t)at * p.n_q_heads + p.diff.first_head(h) + g0]);
 #pragma unroll
-    for (int j = 0; j < kCols; j += 2)
-      *reinterpret_cast<uint32_t*>(p.out + row * D + lane * kCols + j) = pack_bf16(acc[j] * inv, acc[j + 1] * inv);
-    if (lane == 0 && p.lse != nullptr)
-      p.lse[row] = den > 0.f ? (m_run + log2f(den)) * 0.6931471805599453f : -INFINITY;
+      for (int j = 0; j < kCols; ++j) y[j] = fmaf(acc[j], w, y[j]);
+      if (map == 1) {
+        if (p.diff.gain != nullptr) {
+          float sq = 0.f;
+#pragma unroll
+          for (int j = 0; j < kCols; ++j) sq = fmaf(y[j], y[j], sq);
+#pragma unroll
+          for (int x = 16; x > 0; x >>= 1) sq += __shfl_xor_sync(0xffffffffu, sq, x);
+          const float r = diff_norm<D>(sq, p.diff.eps);
+#pragma unroll
+          for (int j = 0; j < kCols; ++j) y[j] *= r * __ldg(&p.diff.gain[(size_t)at * D + lane * kCols + j]);
+        }
+#pragma unroll
+        for (int j = 0; j < kCols; j += 2)
+          *reinterpret_cast<uint32_t*>(p.out + row * D + lane * kCols + j) = pack_bf16(y[j], y[j + 1]);
+      }
+      if (lane == 0 && p.lse != nullptr)
+        p.lse[2 * row + map] = den > 0.f ? (m_run + log2f(den)) * 0.6931471805599453f : -INFINITY;
+    } else {
+#pragma unroll
+      for (int j = 0; j < kCols; j += 2)
+        *reinterpret_cast<uint32_t*>(p.out + row * D + lane * kCols + j) = pack_bf16(acc[j] * inv, acc[j + 1] * inv);
+      if (lane == 0 && p.lse != nullptr)
+        p.lse[row] = den > 0.f ? (m_run + log2f(den)) * 0.6931471805599453f : -INFINITY;
+    }
+    }
   }
   if (aborted) {
     // let copies already issued land before this CTA's shared memory can be handed on
@@ -1069,7 +1160,7 @@ bool decode_layout(const xkv_dims* d, int n_layers, int max_cache_len, int chunk
 
 cudaEvent_t g_ev_start = nullptr, g_ev_stop = nullptr;
 
-template <int D, bool Q8>
+template <int D, bool Q8, bool Diff>
 xkv_status launch_attn(const CUtensorMap& tk, const CUtensorMap& tv, const DecodeParams& p, cudaStream_t st) {
   cudaError_t attr_err = cudaSuccess;
   // opt in to the large dynamic shared-memory carve-out once per process and device in use
@@ -1078,13 +1169,13 @@ xkv_status launch_attn(const CUtensorMap& tk, const CUtensorMap& tv, const Decod
   static std::atomic<bool> done[64];   // idempotent set-up: two threads doing it twice is harmless
   if (dev < 0 || dev >= 64) return XKV_ERR_CUDA;
   if (!done[dev].load(std::memory_order_acquire)) {
-    attr_err = cudaFuncSetAttribute(decode_attn_kernel<D, Q8>, cudaFuncAttributeMaxDynamicSharedMemorySize,
+    attr_err = cudaFuncSetAttribute(decode_attn_kernel<D, Q8, Diff>, cudaFuncAttributeMaxDynamicSharedMemorySize,
                                     Cfg<D, Q8>::kSmemBytes);
     if (attr_err != cudaSuccess) return XKV_ERR_CUDA;
     done[dev].store(true, std::memory_order_release);
   }
   if (g_ev_start != nullptr && g_ev_stop != nullptr) cudaEventRecord(g_ev_start, st);
-  decode_attn_kernel<D, Q8><<<sm_count(), Cfg<D, Q8>::kThreads, Cfg<D, Q8>::kSmemBytes, st>>>(tk, tv, p);
+  decode_attn_kernel<D, Q8, Diff><<<sm_count(), Cfg<D, Q8>::kThreads, Cfg<D, Q8>::kSmemBytes, st>>>(tk, tv, p);
   if (g_ev_start != nullptr && g_ev_stop != nullptr) cudaEventRecord(g_ev_stop, st);
   count_launch();
   return check_launch();
@@ -1102,22 +1193,44 @@ void get_profile_events(cudaEvent_t* start, cudaEvent_t* stop) {
   *stop = g_ev_stop;
 }
 
-size_t decode_workspace_bytes(const xkv_dims* d, int n_layers, int max_cache_len, int chunk_rows) {
+DiffHeads diff_heads(const xkv_dims* d, const float* lambda, const float* gain, float eps) {
+  const int G = d->n_q_heads / d->n_kv_heads;
+  DiffHeads h;
+  h.lambda = lambda;
+  h.gain = gain;
+  h.eps = eps;
+  h.group = G;
+  h.subs = (G + kMaxGroup / 2 - 1) / (kMaxGroup / 2);
+  h.per_sub = (G + h.subs - 1) / h.subs;
+  return h;
+}
+
+xkv_dims streamed_dims(const xkv_dims* d, const DiffHeads& h) {
+  xkv_dims v = *d;
+  v.n_kv_heads = d->n_kv_heads * h.subs;
+  v.n_q_heads = v.n_kv_heads * 2 * h.per_sub;
+  return v;
+}
+
+size_t decode_workspace_bytes(const xkv_dims* d, int n_layers, int max_cache_len, int chunk_rows, bool diff) {
   DecodeLayout L;
-  if (!decode_layout(d, n_layers, max_cache_len, chunk_rows, &L)) return 0;
+  const xkv_dims v = diff ? streamed_dims(d, diff_heads(d, nullptr, nullptr, 0.f)) : *d;
+  if (!decode_layout(&v, n_layers, max_cache_len, chunk_rows, &L)) return 0;
   return L.total;
 }
 
 xkv_status decode_attn(const xkv_dims* d, const xkv_cache* c, int layer_begin, int layer_end, const void* q,
                        const void* k_new, const void* v_new, void* out, float* lse, int chunk_rows,
-                       void* workspace, size_t workspace_bytes, cudaStream_t st, bool clear_status) {
+                       void* workspace, size_t workspace_bytes, cudaStream_t st, bool clear_status,
+                       const DiffHeads* diff) {
   const int Lr = layer_end - layer_begin;
-  const int G = d->n_q_heads / d->n_kv_heads;
-  if (G > kMaxGroup) return XKV_ERR_UNSUPPORTED;
+  if (d->n_q_heads / d->n_kv_heads > kMaxGroup) return XKV_ERR_UNSUPPORTED;
+  const xkv_dims streamed = diff != nullptr ? streamed_dims(d, *diff) : *d;
+  const int G = streamed.n_q_heads / streamed.n_kv_heads;
   if (chunk_rows < 0 || chunk_rows % kChunkAlign != 0) return XKV_ERR_INVALID_ARG;
   const int max_cache_len = c->max_pages_per_seq * c->page_size;
   DecodeLayout L;
-  if (!decode_layout(d, Lr, max_cache_len, chunk_rows, &L)) return XKV_ERR_INVALID_ARG;
+  if (!decode_layout(&streamed, Lr, max_cache_len, chunk_rows, &L)) return XKV_ERR_INVALID_ARG;
   if (workspace_bytes < L.total) return XKV_ERR_WORKSPACE;
   const uint64_t page_rows = (uint64_t)c->n_pages * d->n_kv_heads * c->page_size;
   if (page_rows >= (1ull << 31)) return XKV_ERR_UNSUPPORTED;
@@ -1128,7 +1241,7 @@ xkv_status decode_attn(const xkv_dims* d, const xkv_cache* c, int layer_begin, i
                                    reinterpret_cast<int32_t*>(base + L.tickets),
                                    reinterpret_cast<float*>(base + L.part_o), reinterpret_cast<float*>(base + L.part_ml),
                                    L.max_items};
-    return decode_attn_e4m3(d, c, layer_begin, Lr, q, k_new, v_new, out, lse, scratch, st);
+    return decode_attn_e4m3(d, c, layer_begin, Lr, q, k_new, v_new, out, lse, scratch, st, diff);
   }
 
   const bool q8 = c->kv_format == XKV_KV_INT8;
@@ -1155,13 +1268,15 @@ xkv_status decode_attn(const xkv_dims* d, const xkv_cache* c, int layer_begin, i
   p.batch = d->batch;
   p.n_q_heads = d->n_q_heads;
   p.n_kv_heads = d->n_kv_heads;
+  p.n_heads = streamed.n_kv_heads;
   p.group = G;
+  p.diff = diff != nullptr ? *diff : DiffHeads{};
   p.page_size = c->page_size;
   p.max_pages_per_seq = c->max_pages_per_seq;
   p.n_pages = c->n_pages;
   p.chunk_rows_forced = chunk_rows;
   p.max_items = (int32_t)L.max_items;
-  const float scale = d->scale != 0.f ? d->scale : 1.0f / sqrtf((float)d->head_dim);
+  const float scale = d->scale != 0.f ? d->scale : 1.0f / sqrtf((float)(diff != nullptr ? d->head_dim / 2 : d->head_dim));
   p.scale_log2 = scale * 1.4426950408889634f;
   p.wait_ns = wait_limit_ns();
   p.withhold_item = debug_withhold_item();
@@ -1189,8 +1304,13 @@ xkv_status decode_attn(const xkv_dims* d, const xkv_cache* c, int layer_begin, i
     xkv_status s = check_launch();
     if (s != XKV_OK) return s;
   }
-  if (q8) return d->head_dim == 128 ? launch_attn<128, true>(tk, tv, p, st) : launch_attn<64, true>(tk, tv, p, st);
-  return d->head_dim == 128 ? launch_attn<128, false>(tk, tv, p, st) : launch_attn<64, false>(tk, tv, p, st);
+  const bool wide = d->head_dim == 128;
+  if (diff != nullptr) {
+    if (q8) return wide ? launch_attn<128, true, true>(tk, tv, p, st) : launch_attn<64, true, true>(tk, tv, p, st);
+    return wide ? launch_attn<128, false, true>(tk, tv, p, st) : launch_attn<64, false, true>(tk, tv, p, st);
+  }
+  if (q8) return wide ? launch_attn<128, true, false>(tk, tv, p, st) : launch_attn<64, true, false>(tk, tv, p, st);
+  return wide ? launch_attn<128, false, false>(tk, tv, p, st) : launch_attn<64, false, false>(tk, tv, p, st);
 }
 
 // ---------------------------------------------------------------------------------------------
@@ -1216,7 +1336,7 @@ xkv_status decode_attn_static(const xkv_dims* d, const xkv_cache* c, int layer_b
     scratch = ptr;
   }
   const int max_cache_len = c->max_pages_per_seq * c->page_size;
-  const size_t need = decode_workspace_bytes(d, layer_end - layer_begin, max_cache_len, chunk_rows);
+  const size_t need = decode_workspace_bytes(d, layer_end - layer_begin, max_cache_len, chunk_rows, /*diff=*/false);
   if (need == 0) return XKV_ERR_INVALID_ARG;
   if (need > kStaticScratchBytes) return XKV_ERR_WORKSPACE;   // problem too large for the fixed scratch
   // decode_attn clears the part of the scratch that must start at zero (status word, tickets)

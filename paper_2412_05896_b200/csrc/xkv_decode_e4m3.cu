@@ -101,7 +101,9 @@ struct Params {
   const float* v_scales;
   const int32_t* block_table;
   const int32_t* seq_lens;
-  int32_t layer_begin, batch, n_units, n_q_heads, n_kv_heads, group, page_size, max_pages_per_seq, n_pages;
+  // n_heads caches a unit are streamed with `group` query rows each; differential heads: two rows a head, see DiffHeads
+  int32_t layer_begin, batch, n_units, n_q_heads, n_kv_heads, n_heads, group, page_size, max_pages_per_seq, n_pages;
+  DiffHeads diff;
   // row -> page: page_size is 8 n with n even, 2 <= n <= 32, and x / n = (x * ceil(2^32 / n)) >> 32 for x <= 2^27 + 32
   uint32_t page_mul;                  // ceil(2^32 / n)
   __device__ __forceinline__ int page_of(int row) const { return (int)__umulhi((uint32_t)row >> 3, page_mul); }
@@ -341,7 +343,7 @@ struct Joins {
 
 // Joins kHeads query heads from g on (those behind the last one are left out) of a cut cache, kPieces pieces at a time,
 // all loads of a batch in flight together; the lanes share the columns.
-template <int D, int kHeads, int kPieces>
+template <int D, int kHeads, int kPieces, bool Diff>
 __device__ __forceinline__ void join_heads(const Params& p, const int4 job, int g) {
   constexpr int kCols = D / 32;
   const int lane = threadIdx.x & 31, G = p.group;
@@ -400,20 +402,51 @@ __device__ __forceinline__ void join_heads(const Params& p, const int4 job, int 
       }
     }
   }
+  if constexpr (Diff) {                             // rows g + x and g + x + 1 are the two maps of a head
+    static_assert(kHeads % 2 == 0, "whole heads");
+    const int n_rows = 2 * p.diff.heads(job.y), at = job.x / p.batch;
 #pragma unroll
-  for (int x = 0; x < kHeads; ++x) {
-    if (g + x >= G) break;
-    const size_t row = (size_t)job.x * p.n_q_heads + (size_t)job.y * G + g + x;
-    const float inv = __frcp_rn(den[x]);
+    for (int x = 0; x < kHeads; x += 2) {
+      if (g + x >= n_rows) break;
+      const int head = p.diff.first_head(job.y) + (g + x) / 2;
+      const size_t row = (size_t)job.x * p.n_q_heads + head;
+      const float inv = __frcp_rn(den[x]), lam = __ldg(&p.diff.lambda[(size_t)at * p.n_q_heads + head]) * __frcp_rn(den[x + 1]);
+      float y[kCols], sq = 0.f;
 #pragma unroll
-    for (int c = 0; c < kCols; c += 2)
-      *reinterpret_cast<uint32_t*>(p.out + row * D + lane * kCols + c) = pack_bf16(o[x][c] * inv, o[x][c + 1] * inv);
-    if (lane == 0 && p.lse != nullptr) p.lse[row] = (mx[x] + __log2f(den[x])) * 0.6931471805599453f;
+      for (int c = 0; c < kCols; ++c) {
+        y[c] = o[x][c] * inv - o[x + 1][c] * lam;
+        sq = fmaf(y[c], y[c], sq);
+      }
+      if (p.diff.gain != nullptr) {
+#pragma unroll
+        for (int i = 16; i > 0; i >>= 1) sq += __shfl_xor_sync(0xffffffffu, sq, i);
+        const float r = diff_norm<D>(sq, p.diff.eps);
+#pragma unroll
+        for (int c = 0; c < kCols; ++c) y[c] *= r * __ldg(&p.diff.gain[(size_t)at * D + lane * kCols + c]);
+      }
+#pragma unroll
+      for (int c = 0; c < kCols; c += 2)
+        *reinterpret_cast<uint32_t*>(p.out + row * D + lane * kCols + c) = pack_bf16(y[c], y[c + 1]);
+      if (lane < 2 && p.lse != nullptr)
+        p.lse[2 * row + lane] = lane == 0 ? (mx[x] + __log2f(den[x])) * 0.6931471805599453f
+                                          : (mx[x + 1] + __log2f(den[x + 1])) * 0.6931471805599453f;
+    }
+  } else {
+#pragma unroll
+    for (int x = 0; x < kHeads; ++x) {
+      if (g + x >= G) break;
+      const size_t row = (size_t)job.x * p.n_q_heads + (size_t)job.y * G + g + x;
+      const float inv = __frcp_rn(den[x]);
+#pragma unroll
+      for (int c = 0; c < kCols; c += 2)
+        *reinterpret_cast<uint32_t*>(p.out + row * D + lane * kCols + c) = pack_bf16(o[x][c] * inv, o[x][c + 1] * inv);
+      if (lane == 0 && p.lse != nullptr) p.lse[row] = (mx[x] + __log2f(den[x])) * 0.6931471805599453f;
+    }
   }
 }
 
 // Takes query heads of open jobs, up to four of one job at a time, until none is left (a whole warp).
-template <int D>
+template <int D, bool Diff>
 __device__ __noinline__ void join_open(const Params& p, Joins* joins) {
   const int lane = threadIdx.x & 31, G = p.group;
 #pragma unroll 1
@@ -424,8 +457,8 @@ __device__ __noinline__ void join_open(const Params& p, Joins* joins) {
       const int open = *(volatile int*)&joins->n_jobs * G;
       __threadfence_block();                      // n_jobs before the jobs and, behind them, the pieces
       while (at < open) {
-        // few pieces: four heads in one go; many: one head a warp, so that several warps share the job
-        n = joins->job[at / G].w <= 4 ? min(4, G - at % G) : 1;
+        // few pieces: four query rows in one go; many: one row (the two of a head) a warp, so that several warps share the job
+        n = joins->job[at / G].w <= 4 ? min(4, G - at % G) : (Diff ? 2 : 1);
         const int was = atomicCAS(&joins->claimed, at, at + n);
         if (was == at) {
           claim = at;
@@ -439,12 +472,12 @@ __device__ __noinline__ void join_open(const Params& p, Joins* joins) {
     n = __shfl_sync(0xffffffffu, n, 0);
     __syncwarp();                                 // what lane 0 has seen, all lanes see
     const int4 job = joins->job[claim / G];
-    if (job.w <= 4) join_heads<D, 4, 4>(p, job, claim % G);
-    else            join_heads<D, 1, 16>(p, job, claim % G);
+    if (job.w <= 4) join_heads<D, 4, 4, Diff>(p, job, claim % G);
+    else            join_heads<D, Diff ? 2 : 1, Diff ? 8 : 16, Diff>(p, job, claim % G);
   }
 }
 
-template <int D, int GP>              // GP: query heads per KV head, rounded up to a power of two
+template <int D, int GP, bool Diff>   // GP: query rows per streamed cache, rounded up to a power of two
 __global__ void __launch_bounds__(kThreads, kCtasPerSm)
 decode_e4m3_kernel(const __grid_constant__ CUtensorMap tmap_k, const __grid_constant__ CUtensorMap tmap_v,
                    const __grid_constant__ Params p) {
@@ -460,6 +493,7 @@ decode_e4m3_kernel(const __grid_constant__ CUtensorMap tmap_k, const __grid_cons
   __shared__ __align__(16) float s_max[2][4][8];
   __shared__ __align__(16) float s_head[4][3][8];
   __shared__ __align__(16) float s_sum[2][16];    // reciprocal denominators, or (one or two heads) the warps' sums from [8] on
+  __shared__ __align__(16) float s_sq[2][Diff ? 2 * GP : 1];      // Diff: the warps' sums of squares of each head
   __shared__ int s_scan[kThreads / 32];
   __shared__ int4 s_first;                        // the unit in which the share begins: unit, rows, where it begins on the line
   __shared__ int4 s_end_cut;                      // the cache that the share's end cuts: unit, KV head, where it begins, rows
@@ -468,7 +502,7 @@ decode_e4m3_kernel(const __grid_constant__ CUtensorMap tmap_k, const __grid_cons
   __shared__ Joins s_joins;
   volatile int* s_abort = &s_abort_store;
   const int tid = threadIdx.x, lane = tid & 31, warp = tid >> 5;
-  const int Hkv = p.n_kv_heads, G = p.group;
+  const int Hkv = Diff ? p.n_heads : p.n_kv_heads, G = p.group;
 
   if (p.wait_first) grid_dependency_wait();
   // ---- the plan: each thread a run of units, and their length on the line
@@ -615,7 +649,8 @@ decode_e4m3_kernel(const __grid_constant__ CUtensorMap tmap_k, const __grid_cons
         const int row_of_box = cur.row0 + t * kTile + lane * R;
         int page = __shfl_sync(0xffffffffu, pages, (box0 + lane) & 31);
         page = min(max(page, 0), p.n_pages - 1);
-        const int grow = (page * Hkv + cur.h - p.page_of(row_of_box)) * p.page_size + row_of_box;
+        const int kvh = Diff ? quotient(cur.h, p.diff.subs) : cur.h;
+        const int grow = (page * p.n_kv_heads + kvh - p.page_of(row_of_box)) * p.page_size + row_of_box;
         if (j >= C::kStages) ok = wait_bar(&s_k_empty[stage], ph, s_abort, p.wait_ns);
         ok = __all_sync(0xffffffffu, ok);
         if (!ok) break;
@@ -793,20 +828,27 @@ decode_e4m3_kernel(const __grid_constant__ CUtensorMap tmap_k, const __grid_cons
       // D / 16 lanes a head, sixteen elements a lane, as many heads at a time as the warp holds
       constexpr int kLanes = D / 16, kHeads = 32 / kLanes, kPasses = (GP + kHeads - 1) / kHeads;
       const int c = lane % kLanes;
-      const __nv_bfloat16* q = p.q + ((size_t)it.e * p.n_q_heads + (size_t)it.h * G) * D + c * 16;
+      const size_t q_row0 = (size_t)it.e * p.n_q_heads + (Diff ? (size_t)p.diff.first_head(it.h) : (size_t)it.h * G);
+      const __nv_bfloat16* q = p.q + q_row0 * D + c * 16;
       uint8_t* dst = smem + C::kOffQ + slot * C::kQBytes;
       uint4 raw[kPasses][2];
 #pragma unroll
       for (int x = 0; x < kPasses; ++x) {
-        const int g = min(x * kHeads + lane / kLanes, G - 1);
+        int g = min(x * kHeads + lane / kLanes, G - 1);
+        if constexpr (Diff) g = min(g >> 1, p.diff.heads(it.h) - 1);
         raw[x][0] = __ldg(reinterpret_cast<const uint4*>(q + (size_t)g * D));
         raw[x][1] = __ldg(reinterpret_cast<const uint4*>(q + (size_t)g * D) + 1);
       }
 #pragma unroll
       for (int x = 0; x < kPasses; ++x) {
         const int g = x * kHeads + lane / kLanes;
-        const uint32_t v[8] = {raw[x][0].x, raw[x][0].y, raw[x][0].z, raw[x][0].w,
-                               raw[x][1].x, raw[x][1].y, raw[x][1].z, raw[x][1].w};
+        uint32_t v[8] = {raw[x][0].x, raw[x][0].y, raw[x][0].z, raw[x][0].w,
+                         raw[x][1].x, raw[x][1].y, raw[x][1].z, raw[x][1].w};
+        if constexpr (Diff) {                                  // the half of the head's row that is not the map's
+          if ((c >= kLanes / 2) != ((g & 1) != 0))
+#pragma unroll
+            for (int i = 0; i < 8; ++i) v[i] = 0u;
+        }
         uint32_t top = 0;
 #pragma unroll
         for (int i = 0; i < 8; ++i) top = __vmaxu2(top, v[i] & 0x7fff7fffu);
@@ -854,7 +896,7 @@ decode_e4m3_kernel(const __grid_constant__ CUtensorMap tmap_k, const __grid_cons
         reinterpret_cast<uint4*>(p.out + row0 * D)[i] = make_uint4(0u, 0u, 0u, 0u);
       if (p.lse != nullptr)
 #pragma unroll 1
-        for (int i = lane; i < p.n_q_heads; i += 32) p.lse[row0 + i] = -INFINITY;
+        for (int i = lane; i < (Diff ? 2 : 1) * p.n_q_heads; i += 32) p.lse[(Diff ? 2 : 1) * row0 + i] = -INFINITY;
     }
     if (!p.wait_first) grid_dependency_wait();    // the tickets are cleared by the launch before this one
 #pragma unroll 1
@@ -882,7 +924,7 @@ decode_e4m3_kernel(const __grid_constant__ CUtensorMap tmap_k, const __grid_cons
         }
         woken = true;
         __syncwarp();
-        join_open<D>(p, &s_joins);
+        join_open<D, Diff>(p, &s_joins);
       }
     }
     if (lane == 0) {
@@ -1065,11 +1107,13 @@ decode_e4m3_kernel(const __grid_constant__ CUtensorMap tmap_k, const __grid_cons
       }
       // ---- denominators over the 128 rows' threads, while the last tile's output is on its way; the thread that has head
       // g's also writes its statistics
-      const size_t row0 = (size_t)it.e * p.n_q_heads + (size_t)it.h * G;
+      const size_t row0 = (size_t)it.e * p.n_q_heads + (Diff ? (size_t)p.diff.first_head(it.h) : (size_t)it.h * G);
+      const int n_rows = Diff ? 2 * p.diff.heads(it.h) : G;      // query rows that there are
       const size_t piece = 2 * (size_t)blockIdx.x + ((int)blockIdx.x == it.first_cta ? 1 : 0);
       auto write_stats = [&](int g, float mg, float lg) {
         if (it.n_pieces > 1) __stcg(reinterpret_cast<float2*>(p.part_ml) + piece * G + g, make_float2(mg, lg));
-        else if (p.lse != nullptr && !*s_abort) p.lse[row0 + g] = (mg + __log2f(lg)) * 0.6931471805599453f;
+        else if (p.lse != nullptr && !*s_abort && (!Diff || g < n_rows))
+          p.lse[(Diff ? 2 : 1) * row0 + g] = (mg + __log2f(lg)) * 0.6931471805599453f;
       };
       float* sum_at = s_sum[n_item & 1];
       if constexpr (GP >= 4) {
@@ -1130,7 +1174,41 @@ decode_e4m3_kernel(const __grid_constant__ CUtensorMap tmap_k, const __grid_cons
 #pragma unroll
           for (int g = 0; g < GP; ++g) inv[g] = fast_rcp(l[g]);
         }
-        if (holds_col && !drop) {
+        if constexpr (Diff) {                                     // rows 2 j and 2 j + 1 are the two maps of head j
+          constexpr int kPairs = GP / 2;
+          const int at = it.e / p.batch;
+          const float* lambda = p.diff.lambda + (size_t)at * p.n_q_heads + p.diff.first_head(it.h);
+          float y[kPairs];
+#pragma unroll
+          for (int i = 0; i < kPairs; ++i) {
+            const float lam = 2 * i < n_rows ? __ldg(&lambda[i]) : 0.f;
+            y[i] = acc[2 * i] * inv[2 * i] - lam * (acc[2 * i + 1] * inv[2 * i + 1]);
+            if (2 * i >= n_rows || !holds_col) y[i] = 0.f;
+          }
+          if (p.diff.gain != nullptr) {
+            float* sq_at = s_sq[n_item & 1];
+#pragma unroll
+            for (int i = 0; i < kPairs; ++i) {
+              float sq = y[i] * y[i];
+#pragma unroll
+              for (int o = 16; o > 0; o >>= 1) sq += __shfl_xor_sync(0xffffffffu, sq, o);
+              if (lane == 0) sq_at[4 * i + warp] = sq;
+            }
+            named_bar_sync(kBarSoft, kSoftThreads);
+            const float gain = holds_col ? __ldg(&p.diff.gain[(size_t)at * D + col]) : 0.f;
+#pragma unroll
+            for (int i = 0; i < kPairs; ++i) {
+              const float4 v = *reinterpret_cast<const float4*>(sq_at + 4 * i);
+              y[i] *= gain * diff_norm<D>((v.x + v.y) + (v.z + v.w), p.diff.eps);
+            }
+          }
+          if (holds_col && !drop) {
+            __nv_bfloat16* o = p.out + row0 * D + col;
+#pragma unroll
+            for (int i = 0; i < kPairs; ++i)
+              if (2 * i < n_rows) o[i * D] = __float2bfloat16(y[i]);
+          }
+        } else if (holds_col && !drop) {
           __nv_bfloat16* o = p.out + row0 * D + col;
 #pragma unroll
           for (int g = 0; g < GP; ++g) {
@@ -1155,7 +1233,7 @@ decode_e4m3_kernel(const __grid_constant__ CUtensorMap tmap_k, const __grid_cons
 #pragma unroll 1
   while (warp != 7) {
     const bool over = __any_sync(0xffffffffu, *(volatile int*)&s_joins.all != 0);   // set on every way out of warp 7's loop
-    join_open<D>(p, &s_joins);
+    join_open<D, Diff>(p, &s_joins);
     if (over) break;
     __nanosleep(40);
   }
@@ -1181,13 +1259,13 @@ bool make_tmap(CUtensorMap* tmap, void* base, int D, uint64_t rows, int box_rows
              CU_TENSOR_MAP_FLOAT_OOB_FILL_NONE) == CUDA_SUCCESS;
 }
 
-template <int D, int GP>
+template <int D, int GP, bool Diff>
 xkv_status launch(const CUtensorMap& tk, const CUtensorMap& tv, const Params& p, int grid, cudaStream_t st) {
   int dev = 0;
   if (cudaGetDevice(&dev) != cudaSuccess || dev < 0 || dev >= 64) return XKV_ERR_CUDA;
   static std::atomic<bool> done[64];   // idempotent set-up: two threads doing it twice is harmless
   if (!done[dev].load(std::memory_order_acquire)) {
-    if (cudaFuncSetAttribute(decode_e4m3_kernel<D, GP>, cudaFuncAttributeMaxDynamicSharedMemorySize,
+    if (cudaFuncSetAttribute(decode_e4m3_kernel<D, GP, Diff>, cudaFuncAttributeMaxDynamicSharedMemorySize,
                              Cfg<D>::kSmemBytes) != cudaSuccess)
       return XKV_ERR_CUDA;
     done[dev].store(true, std::memory_order_release);
@@ -1207,7 +1285,7 @@ xkv_status launch(const CUtensorMap& tk, const CUtensorMap& tv, const Params& p,
   attr.val.programmaticStreamSerializationAllowed = 1;
   cfg.attrs = &attr;
   cfg.numAttrs = timed ? 0 : 1;
-  const cudaError_t err = cudaLaunchKernelEx(&cfg, decode_e4m3_kernel<D, GP>, tk, tv, p);
+  const cudaError_t err = cudaLaunchKernelEx(&cfg, decode_e4m3_kernel<D, GP, Diff>, tk, tv, p);
   if (timed) cudaEventRecord(stop, st);
   count_launch();
   if (err != cudaSuccess) {
@@ -1227,7 +1305,8 @@ __global__ void clear_kernel(int32_t* words, int n) {
 
 xkv_status decode_attn_e4m3(const xkv_dims* d, const xkv_cache* c, int layer_begin, int n_layers, const void* q,
                             const void* k_new, const void* v_new, void* out, float* lse, const DecodeScratch& ws,
-                            cudaStream_t st) {
+                            cudaStream_t st, const DiffHeads* diff) {
+  const xkv_dims streamed = diff != nullptr ? streamed_dims(d, *diff) : *d;
   const int n_units = n_layers * d->batch;
   int box = 16;
   const int tile = d->head_dim == 128 ? Cfg<128>::kTile : Cfg<64>::kTile;
@@ -1235,7 +1314,7 @@ xkv_status decode_attn_e4m3(const xkv_dims* d, const xkv_cache* c, int layer_beg
   const uint64_t page_rows = (uint64_t)c->n_pages * d->n_kv_heads * c->page_size;
   // the line of all caches, as long as their tables allow, has 31-bit places
   const int64_t max_rows = (int64_t)c->max_pages_per_seq * c->page_size;
-  const int64_t caches = (int64_t)n_units * d->n_kv_heads, most = caches * ((max_rows + tile - 1) / tile);
+  const int64_t caches = (int64_t)n_units * streamed.n_kv_heads, most = caches * ((max_rows + tile - 1) / tile);
   if (caches * ((max_rows + tile) / kScaleBlock + kCacheCost) >= (1ll << 31)) return XKV_ERR_UNSUPPORTED;
   CUtensorMap tk, tv;
   if (!make_tmap(&tk, c->k_pages, d->head_dim, page_rows, box) || !make_tmap(&tv, c->v_pages, d->head_dim, page_rows, box))
@@ -1263,7 +1342,9 @@ xkv_status decode_attn_e4m3(const xkv_dims* d, const xkv_cache* c, int layer_beg
   p.n_units = n_units;
   p.n_q_heads = d->n_q_heads;
   p.n_kv_heads = d->n_kv_heads;
-  p.group = d->n_q_heads / d->n_kv_heads;
+  p.n_heads = streamed.n_kv_heads;
+  p.group = streamed.n_q_heads / streamed.n_kv_heads;
+  p.diff = diff != nullptr ? *diff : DiffHeads{};
   p.page_size = c->page_size;
   p.max_pages_per_seq = c->max_pages_per_seq;
   p.n_pages = c->n_pages;
@@ -1274,7 +1355,7 @@ xkv_status decode_attn_e4m3(const xkv_dims* d, const xkv_cache* c, int layer_beg
   const int64_t room = ws.max_items / 2;
   p.max_ctas = (int32_t)(room < 1 ? 1 : (room < (1 << 20) ? room : 1 << 20));
   p.wait_first = k_new != nullptr ? 1 : 0;
-  p.scale_log2 = (d->scale != 0.f ? d->scale : 1.0f / sqrtf((float)d->head_dim)) * 1.4426950408889634f;
+  p.scale_log2 = (d->scale != 0.f ? d->scale : 1.0f / sqrtf((float)(diff != nullptr ? d->head_dim / 2 : d->head_dim))) * 1.4426950408889634f;
   p.withhold_cta = debug_withhold_item();
   p.wait_ns = wait_limit_ns();
   p.hdr = static_cast<WorkspaceHeader*>(ws.header);
@@ -1285,16 +1366,26 @@ xkv_status decode_attn_e4m3(const xkv_dims* d, const xkv_cache* c, int layer_beg
   const int64_t full = (int64_t)kCtasPerSm * sm_count();
   const int grid = (int)(most < full ? most : full);
   const int G = p.group;
-  if (d->head_dim == 128) {
-    if (G == 1) return launch<128, 1>(tk, tv, p, grid, st);
-    if (G == 2) return launch<128, 2>(tk, tv, p, grid, st);
-    if (G <= 4) return launch<128, 4>(tk, tv, p, grid, st);
-    return launch<128, 8>(tk, tv, p, grid, st);
+  if (diff != nullptr) {
+    if (d->head_dim == 128) {
+      if (G == 2) return launch<128, 2, true>(tk, tv, p, grid, st);
+      if (G == 4) return launch<128, 4, true>(tk, tv, p, grid, st);
+      return launch<128, 8, true>(tk, tv, p, grid, st);
+    }
+    if (G == 2) return launch<64, 2, true>(tk, tv, p, grid, st);
+    if (G == 4) return launch<64, 4, true>(tk, tv, p, grid, st);
+    return launch<64, 8, true>(tk, tv, p, grid, st);
   }
-  if (G == 1) return launch<64, 1>(tk, tv, p, grid, st);
-  if (G == 2) return launch<64, 2>(tk, tv, p, grid, st);
-  if (G <= 4) return launch<64, 4>(tk, tv, p, grid, st);
-  return launch<64, 8>(tk, tv, p, grid, st);
+  if (d->head_dim == 128) {
+    if (G == 1) return launch<128, 1, false>(tk, tv, p, grid, st);
+    if (G == 2) return launch<128, 2, false>(tk, tv, p, grid, st);
+    if (G <= 4) return launch<128, 4, false>(tk, tv, p, grid, st);
+    return launch<128, 8, false>(tk, tv, p, grid, st);
+  }
+  if (G == 1) return launch<64, 1, false>(tk, tv, p, grid, st);
+  if (G == 2) return launch<64, 2, false>(tk, tv, p, grid, st);
+  if (G <= 4) return launch<64, 4, false>(tk, tv, p, grid, st);
+  return launch<64, 8, false>(tk, tv, p, grid, st);
 }
 
 }  // namespace xkv

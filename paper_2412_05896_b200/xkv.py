@@ -19,7 +19,7 @@ ERR_INVALID_ARG, ERR_UNSUPPORTED, ERR_WORKSPACE, ERR_BUDGET = -1, -2, -3, -4
 ERR_CUDA, ERR_TIMEOUT, ERR_CAPACITY = -5, -6, -7
 POOL_MAX, POOL_AVG = 0, 1
 OP_SCORE, OP_SELECT_COMPACT, OP_DECODE_ATTN, OP_PREFILL_ATTN, OP_PLAN_APPEND, OP_STORE_ROWS = 0, 1, 2, 3, 4, 5
-OP_FORK_CACHES, OP_COMPACT_PAGES, OP_COPY_PAGES = 6, 7, 8
+OP_FORK_CACHES, OP_COMPACT_PAGES, OP_COPY_PAGES, OP_DIFF_DECODE_ATTN = 6, 7, 8, 9
 BUDGET_PER_LAYER, BUDGET_PER_SEQUENCE, BUDGET_PER_HEAD = 0, 1, 2
 KV_BF16, KV_INT8, KV_E4M3 = 0, 1, 2
 SCALE_BLOCK = 16                 # KV_E4M3: consecutive cache slots that share a scale
@@ -28,6 +28,7 @@ STATIC_SCRATCH_BYTES = 16 << 20
 
 EXPORTS = ("xkv_score", "xkv_score_lse", "xkv_prefill_attn", "xkv_batch_curves", "xkv_head_curves", "xkv_build_block_table", "xkv_alloc_budgets", "xkv_average_budgets", "xkv_select_compact", "xkv_decode_attn", "xkv_decode_attn_static",
            "xkv_plan_append", "xkv_store_rows", "xkv_fork_caches", "xkv_compact_pages", "xkv_copy_pages",
+           "xkv_diff_decode_attn",
            "xkv_workspace_bytes",
            "xkv_read_device_status", "xkv_profile_events", "xkv_test_hooks", "xkv_launch_count", "xkv_status_string",
            "xkv_version")
@@ -93,6 +94,9 @@ def lib() -> ctypes.CDLL:
     L.xkv_decode_attn_static.restype = i32
     L.xkv_decode_attn_static.argtypes = [ctypes.POINTER(Dims), ctypes.POINTER(Cache), i32, i32, vp, vp, vp, vp,
                                          vp, i32, vp, vp]
+    L.xkv_diff_decode_attn.restype = i32
+    L.xkv_diff_decode_attn.argtypes = [ctypes.POINTER(Dims), ctypes.POINTER(Cache), i32, i32, vp, vp, vp, vp, vp,
+                                       ctypes.c_float, vp, vp, i32, vp, sz, vp]
     L.xkv_plan_append.restype = i32
     L.xkv_plan_append.argtypes = [ctypes.POINTER(Cache), i32, vp, i32, vp, vp, i32, vp, vp, vp, i64, vp, sz, vp]
     L.xkv_store_rows.restype = i32
@@ -301,6 +305,15 @@ def decode_attn(dims: Dims, cache: Cache, layer_begin: int, layer_end: int, q, k
     _check(lib().xkv_decode_attn(ctypes.byref(dims), ctypes.byref(cache), layer_begin, layer_end, _ptr(q),
                                  _ptr(k_new), _ptr(v_new), _ptr(out), _ptr(lse), chunk_rows, _ptr(workspace),
                                  _nbytes(workspace), _stream(stream)), "xkv_decode_attn")
+
+
+def diff_decode_attn(dims: Dims, cache: Cache, layer_begin: int, layer_end: int, q, k_new, v_new, lam, gain, eps: float, out,
+                     lse, chunk_rows: int, workspace, stream=None) -> None:
+    """decode_attn of differential heads: q rows [q1 | q2], cached K rows [k1 | k2]; lam dev fp32 [Lr, Hq], gain dev fp32
+    [Lr, d] or None, lse dev fp32 [Lr, B, Hq, 2] or None."""
+    _check(lib().xkv_diff_decode_attn(ctypes.byref(dims), ctypes.byref(cache), layer_begin, layer_end, _ptr(q), _ptr(k_new),
+                                      _ptr(v_new), _ptr(lam), _ptr(gain), eps, _ptr(out), _ptr(lse), chunk_rows,
+                                      _ptr(workspace), _nbytes(workspace), _stream(stream)), "xkv_diff_decode_attn")
 
 
 def decode_attn_static(dims: Dims, cache: Cache, layer_begin: int, layer_end: int, q, k_new, v_new, out, lse,

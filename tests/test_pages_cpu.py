@@ -118,3 +118,24 @@ def test_copy_pages_refuses():
     assert call(d=_dims(head_dim=32)) == xkv.ERR_UNSUPPORTED
     assert call(nb=8) == xkv.ERR_WORKSPACE
     assert call(n=0) == xkv.OK                              # nothing to copy, nothing launched
+
+
+def test_diff_decode_attn_refuses():
+    lib = xkv.lib()
+
+    def call(d=None, c=None, l0=0, l1=2, q=16, kn=None, vn=None, lam=16, gain=16, eps=1e-5, out=16, lse=16, chunk=0, ws=256,
+             nb=1 << 32):
+        return lib.xkv_diff_decode_attn(ctypes.byref(d or _dims()), ctypes.byref(c or _cache()), l0, l1, q, kn, vn, lam, gain,
+                                        eps, out, lse, chunk, ws, nb, None)
+
+    for bad in (dict(q=None), dict(out=None), dict(lam=None), dict(ws=None), dict(q=8), dict(lam=4), dict(gain=8), dict(lse=4),
+                dict(out=2), dict(ws=16), dict(kn=16), dict(vn=16), dict(kn=16, vn=8), dict(eps=-1.0), dict(eps=float("nan")),
+                dict(eps=float("inf")), dict(l0=-1), dict(l1=0), dict(l1=5), dict(chunk=32), dict(chunk=-64),
+                dict(c=_cache(k_scales=None)), dict(c=_cache(page_size=40)), dict(d=_dims(n_kv_heads=3)), dict(d=_dims(scale=-1.0))):
+        assert call(**bad) == xkv.ERR_INVALID_ARG, bad
+    assert call(d=_dims(head_dim=96)) == xkv.ERR_UNSUPPORTED
+    assert call(d=_dims(n_q_heads=18)) == xkv.ERR_UNSUPPORTED          # nine heads a KV head
+    assert call(nb=256) == xkv.ERR_WORKSPACE
+    one = xkv.workspace_bytes(xkv.OP_DECODE_ATTN, _dims(), n_layers=2, max_cache_len=1024)
+    two = xkv.workspace_bytes(xkv.OP_DIFF_DECODE_ATTN, _dims(), n_layers=2, max_cache_len=1024)
+    assert two > one                                                   # partial results of both maps
