@@ -5,6 +5,7 @@
  * The path, in call order:
  *   0. xkv_prefill_attn   optional, the step before the path: causal attention of the whole prompt, which also
  *                         yields the softmax normalisers of the window rows   (Eq. 1, Eq. 2; Alg. 2 step 1)
+ *      xkv_diff_prefill_attn  the same for heads that attend by the difference of two softmax maps
  *   1. xkv_score          per layer: observation-window attention weights -> pooled importance
  *                         scores per KV head, their descending sort, and the layer's
  *                         retained-importance curve               (Eq. 2, Eq. 3, Eq. 4; Alg. 2 steps 1-4)
@@ -90,6 +91,7 @@ typedef int32_t xkv_status;
 #define XKV_OP_COMPACT_PAGES  7
 #define XKV_OP_COPY_PAGES     8
 #define XKV_OP_DIFF_DECODE_ATTN  9
+#define XKV_OP_DIFF_PREFILL_ATTN 10
 
 /* Problem shape shared by the device entry points. */
 typedef struct xkv_dims {
@@ -224,6 +226,31 @@ xkv_status xkv_score(const xkv_dims* dims, const void* q_win, const void* k,
 xkv_status xkv_prefill_attn(const xkv_dims* dims, const void* q, const void* k, const void* v,
                             const int32_t* cu_seqlens, int64_t total_tokens, int32_t max_seqlen, void* out,
                             float* lse, void* workspace, size_t workspace_bytes, void* stream);
+
+/*
+ * xkv_diff_prefill_attn -- xkv_prefill_attn for a model whose heads attend by the difference of two softmax maps with learned
+ * weights (no counterpart in the paper: another form of Eq. 1).
+ *
+ * For every sequence b, differential head h (query rows [q1 | q2], key rows [k1 | k2], halves of d/2 elements; g = h / G) and
+ * position i < t_b:
+ *   a_s[c] = softmax over the keys c <= i of scale * q_s[i,h,:] . k_s[c,g,:]      (s = 1, 2; scale 0 selects 1/sqrt(d/2))
+ *   y      = sum over c of (a_1[c] - lambda[h] a_2[c]) v[c,g,:]
+ *   out[i,h,:] = y, or with a gain y / sqrt(mean of y^2 over its d elements + eps) * gain (the head's norm; a factor
+ *            1 - lambda_init goes into the gain)
+ *   lse[h][s][i] = natural log of the sum over c <= i of exp(scale * q_s . k_s[c])
+ *
+ * q          dev bf16 [T][Hq][d];  k, v  dev bf16, layout and strides of xkv_score;  head_dim: d
+ * lambda     dev fp32 [Hq];  gain  dev fp32 [d], NULL: no norm;  eps >= 0, finite
+ * out        dev out bf16 [T][Hq][d];  lse  dev out fp32 [Hq][2][T], may be NULL
+ * workspace  dev, at least xkv_workspace_bytes(XKV_OP_DIFF_PREFILL_ATTN, ...) bytes (the status word), 256-byte aligned
+ * bf16 inputs, fp32 accumulation, difference and norm, the weights rounded to bf16 before they multiply v, bf16 output. A value v
+ * that is not finite also reaches rows of its own sequence up to 127 positions before it (0 * v), never another sequence's.
+ * Everything else as in xkv_prefill_attn.
+ */
+xkv_status xkv_diff_prefill_attn(const xkv_dims* dims, const void* q, const void* k, const void* v, const float* lambda,
+                                 const float* gain, float eps, const int32_t* cu_seqlens, int64_t total_tokens,
+                                 int32_t max_seqlen, void* out, float* lse, void* workspace, size_t workspace_bytes,
+                                 void* stream);
 
 /*
  * xkv_score_lse -- xkv_score when the normalisers of the window rows are already known (Alg. 2 step 1 takes
@@ -579,7 +606,7 @@ xkv_status xkv_decode_attn_static(const xkv_dims* dims, const xkv_cache* cache, 
 /*
  * Workspace size in bytes for one call of `op` (XKV_OP_*). Unused arguments may be 0.
  *   XKV_OP_SCORE, XKV_OP_SELECT_COMPACT: dims, max_seqlen, total_tokens
- *   XKV_OP_PREFILL_ATTN, XKV_OP_STORE_ROWS: dims
+ *   XKV_OP_PREFILL_ATTN, XKV_OP_DIFF_PREFILL_ATTN, XKV_OP_STORE_ROWS: dims
  *   XKV_OP_PLAN_APPEND: dims (its batch), n_layers
  *   XKV_OP_FORK_CACHES: dims (its batch), n_layers, max_seqlen = max_pages_per_seq, total_tokens = n_pages
  *   XKV_OP_COMPACT_PAGES: total_tokens = n_pages

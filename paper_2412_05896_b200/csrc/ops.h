@@ -20,6 +20,10 @@ xkv_status prefill_attn(const xkv_dims* d, const void* q, const void* k, const v
                         int64_t total_tokens, int max_seqlen, void* out, float* lse, void* workspace,
                         cudaStream_t st);
 
+xkv_status diff_prefill_attn(const xkv_dims* d, const void* q, const void* k, const void* v, const float* lambda,
+                             const float* gain, float eps, const int32_t* cu_seqlens, int64_t total_tokens, int max_seqlen,
+                             void* out, float* lse, void* workspace, cudaStream_t st);
+
 size_t select_workspace_bytes(const xkv_dims* d, int max_seqlen, int64_t total_tokens);
 xkv_status select_compact(const xkv_dims* d, int layer, const int32_t* budget, int per_sequence,
                           const float* scores, const float* sorted, const void* k, const void* v,

@@ -162,6 +162,29 @@ xkv_status xkv_prefill_attn(const xkv_dims* dims, const void* q, const void* k, 
                       static_cast<cudaStream_t>(stream));
 }
 
+xkv_status xkv_diff_prefill_attn(const xkv_dims* dims, const void* q, const void* k, const void* v, const float* lambda,
+                                 const float* gain, float eps, const int32_t* cu_seqlens, int64_t total_tokens,
+                                 int32_t max_seqlen, void* out, float* lse, void* workspace, size_t workspace_bytes,
+                                 void* stream) {
+  xkv_status s = check_dims(dims);
+  if (s != XKV_OK) return s;
+  if (q == nullptr || k == nullptr || v == nullptr || lambda == nullptr || cu_seqlens == nullptr || out == nullptr ||
+      workspace == nullptr)
+    return XKV_ERR_INVALID_ARG;
+  if (!aligned16(q) || !aligned16(k) || !aligned16(v) || !aligned16(lambda) || !aligned16(gain) || !aligned16(cu_seqlens) ||
+      !aligned16(out) || !aligned16(lse) || (reinterpret_cast<uintptr_t>(workspace) & 255u) != 0)
+    return XKV_ERR_INVALID_ARG;
+  if (!(eps >= 0.f) || std::isinf(eps)) return XKV_ERR_INVALID_ARG;
+  if (dims->kv_stride_head < dims->head_dim || dims->kv_stride_head % 8 != 0 ||
+      dims->kv_stride_token < (int64_t)dims->n_kv_heads * dims->head_dim || dims->kv_stride_token % 8 != 0)
+    return XKV_ERR_INVALID_ARG;
+  if (total_tokens <= 0 || total_tokens >= (1ll << 31) || max_seqlen <= 0 || max_seqlen > total_tokens)
+    return XKV_ERR_INVALID_ARG;
+  if (workspace_bytes < prefill_workspace_bytes()) return XKV_ERR_WORKSPACE;
+  return diff_prefill_attn(dims, q, k, v, lambda, gain, eps, cu_seqlens, total_tokens, max_seqlen, out, lse, workspace,
+                           static_cast<cudaStream_t>(stream));
+}
+
 xkv_status xkv_select_compact(const xkv_dims* dims, int32_t layer, const int32_t* budget, int32_t per_sequence,
                               const float* scores, const float* sorted, const void* k, const void* v,
                               const int32_t* cu_seqlens, int64_t total_tokens, int32_t max_seqlen,
@@ -405,6 +428,7 @@ size_t xkv_workspace_bytes(int32_t op, const xkv_dims* dims, int32_t max_seqlen,
       if (check_prefill_dims(dims) != XKV_OK || max_seqlen <= 0 || total_tokens <= 0) return 0;
       return select_workspace_bytes(dims, max_seqlen, total_tokens);
     case XKV_OP_PREFILL_ATTN:
+    case XKV_OP_DIFF_PREFILL_ATTN:
       if (check_dims(dims) != XKV_OK) return 0;
       return prefill_workspace_bytes();
     case XKV_OP_DECODE_ATTN:

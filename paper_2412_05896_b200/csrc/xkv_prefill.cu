@@ -64,79 +64,6 @@ struct PfCfg {
   static_assert(2 * (kSmemBytes + 1024) <= 233472, "two CTAs per SM");
 };
 
-__device__ __forceinline__ void tmem_wait_st() { asm volatile("tcgen05.wait::st.sync.aligned;" ::: "memory"); }
-
-// 32 consecutive 32-bit columns of this thread's TMEM lane from registers (here: 64 bf16 values of a row of P).
-__device__ __forceinline__ void tmem_st32u(uint32_t taddr, const uint32_t (&v)[32]) {
-  asm volatile(
-      "tcgen05.st.sync.aligned.32x32b.x32.b32 [%0], "
-      "{%1, %2, %3, %4, %5, %6, %7, %8, %9, %10, %11, %12, %13, %14, %15, %16, "
-      "%17, %18, %19, %20, %21, %22, %23, %24, %25, %26, %27, %28, %29, %30, %31, %32};"
-      ::"r"(taddr), "r"(v[0]), "r"(v[1]), "r"(v[2]), "r"(v[3]), "r"(v[4]), "r"(v[5]), "r"(v[6]), "r"(v[7]), "r"(v[8]),
-        "r"(v[9]), "r"(v[10]), "r"(v[11]), "r"(v[12]), "r"(v[13]), "r"(v[14]), "r"(v[15]), "r"(v[16]), "r"(v[17]),
-        "r"(v[18]), "r"(v[19]), "r"(v[20]), "r"(v[21]), "r"(v[22]), "r"(v[23]), "r"(v[24]), "r"(v[25]), "r"(v[26]),
-        "r"(v[27]), "r"(v[28]), "r"(v[29]), "r"(v[30]), "r"(v[31])
-      : "memory");
-}
-
-// D[tmem] (+)= A[tmem] * B[smem desc], bf16 inputs, fp32 accumulate; A is 128 rows (one per TMEM lane) of K-major
-// bf16 pairs, one pair per 32-bit column (16 K elements = 8 columns a step); issued by one thread.
-__device__ __forceinline__ void umma_bf16_a_tmem(uint32_t tmem_d, uint32_t tmem_a, uint64_t bdesc, uint32_t idesc,
-                                                 uint32_t accumulate) {
-  asm volatile(
-      "{\n\t"
-      ".reg .pred p;\n\t"
-      "setp.ne.b32 p, %4, 0;\n\t"
-      "tcgen05.mma.cta_group::1.kind::f16 [%0], [%1], %2, %3, {%5, %5, %5, %5}, p;\n\t"
-      "}\n" ::"r"(tmem_d),
-      "r"(tmem_a), "l"(bdesc), "r"(idesc), "r"(accumulate), "r"(0u)
-      : "memory");
-}
-
-// 16 consecutive fp32 columns of this thread's TMEM lane (the rescale of O works in these smaller pieces so that the
-// tile's logits can stay in registers beside it).
-__device__ __forceinline__ void tmem_ld16(uint32_t taddr, float (&v)[16]) {
-  uint32_t r[16];
-  asm volatile(
-      "tcgen05.ld.sync.aligned.32x32b.x16.b32 "
-      "{%0, %1, %2, %3, %4, %5, %6, %7, %8, %9, %10, %11, %12, %13, %14, %15}, [%16];"
-      : "=r"(r[0]), "=r"(r[1]), "=r"(r[2]), "=r"(r[3]), "=r"(r[4]), "=r"(r[5]), "=r"(r[6]), "=r"(r[7]), "=r"(r[8]),
-        "=r"(r[9]), "=r"(r[10]), "=r"(r[11]), "=r"(r[12]), "=r"(r[13]), "=r"(r[14]), "=r"(r[15])
-      : "r"(taddr)
-      : "memory");
-#pragma unroll
-  for (int i = 0; i < 16; ++i) v[i] = __uint_as_float(r[i]);
-}
-__device__ __forceinline__ void tmem_st16(uint32_t taddr, const float (&v)[16]) {
-  asm volatile(
-      "tcgen05.st.sync.aligned.32x32b.x16.b32 [%0], "
-      "{%1, %2, %3, %4, %5, %6, %7, %8, %9, %10, %11, %12, %13, %14, %15, %16};"
-      ::"r"(taddr), "r"(__float_as_uint(v[0])), "r"(__float_as_uint(v[1])), "r"(__float_as_uint(v[2])),
-        "r"(__float_as_uint(v[3])), "r"(__float_as_uint(v[4])), "r"(__float_as_uint(v[5])),
-        "r"(__float_as_uint(v[6])), "r"(__float_as_uint(v[7])), "r"(__float_as_uint(v[8])),
-        "r"(__float_as_uint(v[9])), "r"(__float_as_uint(v[10])), "r"(__float_as_uint(v[11])),
-        "r"(__float_as_uint(v[12])), "r"(__float_as_uint(v[13])), "r"(__float_as_uint(v[14])),
-        "r"(__float_as_uint(v[15]))
-      : "memory");
-}
-
-// Shared-memory descriptor of an MN-major operand tile stored as rows of 128 bytes (64 bf16 along MN) per K index
-// with the 128-byte swizzle: eight K rows form a 1024-byte group (stride byte offset), the next 64 MN elements
-// start `mn_block_bytes` further (leading byte offset).  This is what a TMA box {64, rows} of a [keys][d] tile is
-// when d is the MMA's N and the keys its K.
-__device__ __forceinline__ uint64_t umma_desc_mn128(uint32_t smem_addr, uint32_t mn_block_bytes) {
-  uint64_t d = 0;
-  d |= (uint64_t)((smem_addr & 0x3ffffu) >> 4);
-  d |= (uint64_t)(mn_block_bytes >> 4) << 16;     // leading byte offset: next block of 64 MN elements
-  d |= (uint64_t)(1024 >> 4) << 32;               // stride byte offset: next group of eight K rows
-  d |= (uint64_t)1 << 46;
-  d |= (uint64_t)2 << 61;                         // SWIZZLE_128B
-  return d;
-}
-
-// bf16 x bf16 -> fp32, A K-major, B MN-major.
-__host__ __device__ constexpr uint32_t umma_idesc_b_mn(int M, int N) { return umma_idesc(M, N) | (1u << 16); }
-
 // The (sequence, query tile) of CTA-tile index `idx`, counted from the end so that the long tiles of the last
 // sequence start first; false when idx is beyond the tiles that exist.  Computed by every warp for itself: a lane
 // takes one sequence, a warp scan gives the tiles before it.
@@ -478,15 +405,6 @@ xkv_status pf_launch(const CUtensorMap& tq, const CUtensorMap& tk, const CUtenso
   return check_launch();
 }
 
-// 3-D map {d, heads, tokens} with box {64, 1, box_rows} over a packed [T][heads][d] bf16 tensor.
-bool pf_make_tmap(CUtensorMap* tmap, const void* base, int head_dim, int heads, int64_t tokens, int64_t stride_token,
-                  int64_t stride_head, int box_rows) {
-  const cuuint64_t dims[3] = {(cuuint64_t)head_dim, (cuuint64_t)heads, (cuuint64_t)tokens};
-  const cuuint64_t strides[2] = {(cuuint64_t)stride_head * 2, (cuuint64_t)stride_token * 2};
-  const cuuint32_t box[3] = {64u, 1u, (cuuint32_t)box_rows};
-  return tc_make_tmap(tmap, base, 3, dims, strides, box);
-}
-
 }  // namespace
 
 size_t prefill_workspace_bytes() { return kHeaderBytes; }
@@ -509,10 +427,10 @@ xkv_status prefill_attn(const xkv_dims* d, const void* q, const void* k, const v
   p.scale_log2 = scale * 1.4426950408889634f;
   p.wait_ns = wait_limit_ns();
   CUtensorMap tq, tk, tv;
-  if (!pf_make_tmap(&tq, q, d->head_dim, d->n_q_heads, total_tokens, (int64_t)d->n_q_heads * d->head_dim, d->head_dim,
+  if (!tc_make_token_tmap(&tq, q, d->head_dim, d->n_q_heads, total_tokens, (int64_t)d->n_q_heads * d->head_dim, d->head_dim,
                     kPfRows) ||
-      !pf_make_tmap(&tk, k, d->head_dim, d->n_kv_heads, total_tokens, d->kv_stride_token, d->kv_stride_head, kPfKeys) ||
-      !pf_make_tmap(&tv, v, d->head_dim, d->n_kv_heads, total_tokens, d->kv_stride_token, d->kv_stride_head, kPfKeys))
+      !tc_make_token_tmap(&tk, k, d->head_dim, d->n_kv_heads, total_tokens, d->kv_stride_token, d->kv_stride_head, kPfKeys) ||
+      !tc_make_token_tmap(&tv, v, d->head_dim, d->n_kv_heads, total_tokens, d->kv_stride_token, d->kv_stride_head, kPfKeys))
     return XKV_ERR_CUDA;
   // an upper bound of the query tiles that exist: every sequence adds at most one partial tile
   const int64_t tiles = total_tokens / kPfRows + d->batch;

@@ -19,7 +19,7 @@ ERR_INVALID_ARG, ERR_UNSUPPORTED, ERR_WORKSPACE, ERR_BUDGET = -1, -2, -3, -4
 ERR_CUDA, ERR_TIMEOUT, ERR_CAPACITY = -5, -6, -7
 POOL_MAX, POOL_AVG = 0, 1
 OP_SCORE, OP_SELECT_COMPACT, OP_DECODE_ATTN, OP_PREFILL_ATTN, OP_PLAN_APPEND, OP_STORE_ROWS = 0, 1, 2, 3, 4, 5
-OP_FORK_CACHES, OP_COMPACT_PAGES, OP_COPY_PAGES, OP_DIFF_DECODE_ATTN = 6, 7, 8, 9
+OP_FORK_CACHES, OP_COMPACT_PAGES, OP_COPY_PAGES, OP_DIFF_DECODE_ATTN, OP_DIFF_PREFILL_ATTN = 6, 7, 8, 9, 10
 BUDGET_PER_LAYER, BUDGET_PER_SEQUENCE, BUDGET_PER_HEAD = 0, 1, 2
 KV_BF16, KV_INT8, KV_E4M3 = 0, 1, 2
 SCALE_BLOCK = 16                 # KV_E4M3: consecutive cache slots that share a scale
@@ -28,7 +28,7 @@ STATIC_SCRATCH_BYTES = 16 << 20
 
 EXPORTS = ("xkv_score", "xkv_score_lse", "xkv_prefill_attn", "xkv_batch_curves", "xkv_head_curves", "xkv_build_block_table", "xkv_alloc_budgets", "xkv_average_budgets", "xkv_select_compact", "xkv_decode_attn", "xkv_decode_attn_static",
            "xkv_plan_append", "xkv_store_rows", "xkv_fork_caches", "xkv_compact_pages", "xkv_copy_pages",
-           "xkv_diff_decode_attn",
+           "xkv_diff_decode_attn", "xkv_diff_prefill_attn",
            "xkv_workspace_bytes",
            "xkv_read_device_status", "xkv_profile_events", "xkv_test_hooks", "xkv_launch_count", "xkv_status_string",
            "xkv_version")
@@ -94,6 +94,8 @@ def lib() -> ctypes.CDLL:
     L.xkv_decode_attn_static.restype = i32
     L.xkv_decode_attn_static.argtypes = [ctypes.POINTER(Dims), ctypes.POINTER(Cache), i32, i32, vp, vp, vp, vp,
                                          vp, i32, vp, vp]
+    L.xkv_diff_prefill_attn.restype = i32
+    L.xkv_diff_prefill_attn.argtypes = [ctypes.POINTER(Dims), vp, vp, vp, vp, vp, ctypes.c_float, vp, i64, i32, vp, vp, vp, sz, vp]
     L.xkv_diff_decode_attn.restype = i32
     L.xkv_diff_decode_attn.argtypes = [ctypes.POINTER(Dims), ctypes.POINTER(Cache), i32, i32, vp, vp, vp, vp, vp,
                                        ctypes.c_float, vp, vp, i32, vp, sz, vp]
@@ -207,6 +209,15 @@ def prefill_attn(dims: Dims, q, k, v, cu_seqlens, total_tokens: int, max_seqlen:
     _check(lib().xkv_prefill_attn(ctypes.byref(dims), _ptr(q), _ptr(k), _ptr(v), _ptr(cu_seqlens), total_tokens,
                                   max_seqlen, _ptr(out), _ptr(lse), _ptr(workspace), _nbytes(workspace),
                                   _stream(stream)), "xkv_prefill_attn")
+
+
+def diff_prefill_attn(dims: Dims, q, k, v, lam, gain, eps: float, cu_seqlens, total_tokens: int, max_seqlen: int, out, lse,
+                      workspace, stream=None) -> None:
+    """prefill_attn of differential heads: q rows [q1 | q2], k rows [k1 | k2]; lam dev fp32 [Hq], gain dev fp32 [d] or None,
+    lse dev fp32 [Hq, 2, T] or None."""
+    _check(lib().xkv_diff_prefill_attn(ctypes.byref(dims), _ptr(q), _ptr(k), _ptr(v), _ptr(lam), _ptr(gain), eps,
+                                       _ptr(cu_seqlens), total_tokens, max_seqlen, _ptr(out), _ptr(lse), _ptr(workspace),
+                                       _nbytes(workspace), _stream(stream)), "xkv_diff_prefill_attn")
 
 
 def batch_curves(gains, n_layers: int, batch: int, curve_len: int, divisor: int, out, stream=None) -> None:

@@ -122,3 +122,38 @@ def small_weight(fmt, n):
     # int8: fp16 products of weight and scale (2^-5.5 .. 2^-4.5 here), 2^-25 absolute below 2^-14; e4m3: 2^-23 of a tile's
     # largest product of weight and scale (scales within 2^3 of each other here)
     return {"bf16": 0.0, "int8": 2.0 ** -25 * 2.0 ** 5.5, "e4m3": 2.0 ** -23 * 8}[fmt]
+
+
+def check_causal(out, lse, Q, K, V, lam, gain, eps, scale=None, what="", rows=None):
+    """All rows of one head of one prompt, out [n, d] and lse [2, n], with check_head's bounds (16-bit rows)."""
+    n, d = Q.shape
+    rows = np.arange(n) if rows is None else rows
+    half, s = d // 2, (d // 2) ** -0.5 if scale is None else scale
+    dead = np.arange(n)[None, :] > rows[:, None]
+    y, size = np.zeros((len(rows), d)), np.zeros((len(rows), d))
+    for i, (part, sign) in enumerate(((slice(0, half), 1.0), (slice(half, None), -lam))):
+        z = s * (Q[rows][:, part] @ K[:, part].T)
+        z[dead] = -np.inf
+        top = z.max(1, keepdims=True)
+        e = np.exp(z - top)
+        total = e.sum(1, keepdims=True)
+        y += sign * (e @ V) / total
+        size += abs(sign) * 2.0 ** -8 * 1.0625 * (e @ np.abs(V)) / total
+        if lse is not None:
+            tol = 2.0 ** -19 * s * np.where(dead, 0.0, np.abs(Q[rows][:, part]) @ np.abs(K[:, part]).T).max(1) + 2e-5
+            err = np.abs(lse[i][rows] - (top + np.log(total))[:, 0])
+            assert np.all(err <= tol), f"{what}: lse of map {i + 1} off by {(err / tol).max():.3g} of the bound"
+    bound, ref = size, y
+    if gain is not None:
+        ms = (y * y).mean(1, keepdims=True)
+        r = np.where(ms > 0, 1.0 / np.sqrt(np.maximum(ms, 1e-300) + eps), 0.0)
+        ref = y * r * gain
+        rho = np.linalg.norm(size, axis=1, keepdims=True) / np.maximum(np.linalg.norm(y, axis=1, keepdims=True), 1e-300)
+        # rows whose maps cancel too far for the bound (y is then mostly rounding) are only asked to be finite
+        fine = rho < 0.5
+        assert fine.mean() > 0.9, what
+        bound = np.where(fine, np.abs(gain) * r * (size + np.abs(y) * rho) / (1 - np.minimum(rho, 0.5)), np.inf)
+    bound = bound + 2.0 ** -8 * np.abs(ref) + 1e-30
+    assert np.all(np.isfinite(out[rows])), what
+    worst = float((np.abs(out[rows] - ref) / bound).max())
+    assert worst <= 1.0, f"{what}: {worst:.3g} of the bound"
