@@ -10,14 +10,17 @@
 //
 // Shape of the launch: one persistent CTA per SM takes (query tile, head) items, long ones first and in alternating direction, so
 // that the CTAs' sums differ by little; the heads of a tile lie next to each other, so that a KV head's tiles meet in L2.  Tensor
-// memory holds O_1 and O_2 (d columns each) and two 64-column buffers of logits per map.
+// memory holds per map O_s (d columns), one 64-column buffer of logits and two 32-column buffers of weights: the next tile's logits
+// are formed as soon as this tile's are in registers, so the softmax warps wait for no product.  (Weights over their logits, and
+// two such buffers, or one of 128 keys: the chain weights - product - logits is then in the way, 980 and 1010 us for the largest case.)
 //   warps 0-3  softmax of map 1, warps 4-7 of map 2: thread = query row = tensor-memory lane.  A row's 64 logits leave tensor memory
 //              once; the reference maximum is exact on the first tile and raised lazily (by 2^8) afterwards, which is when O_s is
 //              rescaled; P_s goes back as bf16 pairs over the tile's logits, the A operand of O_s += P_s V.  At the end of an item
 //              each map's warps take half of the columns of both O_1 and O_2.
 //   warp 8     Q tiles (two buffers, so that the next item's logits start under this item's last products) and K tiles by TMA
-//   warp 9     issues the logits, up to two tiles ahead
-//   warp 10    issues the outputs; clears the V rows behind a prompt's last token (the next prompt's, or 0 * NaN)
+//   warps 9, 10   issue the logits of map 1 and of map 2, warps 12, 13 the outputs (a warp of its own each: what runs once a tile runs out
+//              of a cold instruction cache, and one warp for both took longer than the softmax); warp 12 clears the V rows
+//              behind a prompt's last token (the next prompt's, or 0 * NaN)
 //   warp 11    finds the items, V tiles by TMA
 // Every wait is bounded and ends when another role has given up; an expired one sets the status word and lets the CTA drain.
 #include <atomic>
@@ -30,14 +33,18 @@ namespace {
 
 using namespace tc;
 
-constexpr int kThreads = 384;
+constexpr int kThreads = 512;
 constexpr int kSoftWarps = 8;
 constexpr int kRows = 128;            // query rows of an item
 constexpr int kKeys = 64;             // keys of a tile
 constexpr int kStages = 4;            // K tiles, and V tiles
 constexpr int kItems = 4;             // items between the walk and the last reader
-constexpr int kItemReaders = 3 + kSoftWarps;
+constexpr int kItemReaders = 5 + kSoftWarps;   // all but the walk itself
 constexpr float kLazy = 8.f;          // log2 slack before the reference maximum is raised
+// Registers a thread: the launch has 128 for each of its 512; a softmax thread, which holds a row's logits, takes 176 and leaves the
+// other roles' threads 80.
+constexpr int kLaunchRegs = 128, kSoftRegs = 176, kRoleRegs = 80;
+static_assert(256 * kSoftRegs + 256 * kRoleRegs <= kThreads * kLaunchRegs, "no more than the launch has");
 
 struct Params {
   const int32_t* cu_seqlens;
@@ -65,7 +72,8 @@ struct Cfg {
   static constexpr int kKvHalfBytes = kKeys * 128;
   static constexpr int kKvBytes = kHalves * kKvHalfBytes;
   static constexpr uint32_t kTmemCols = 512;
-  static constexpr uint32_t kSCol = 256;                     // O_s at 128 s, logits of (map, buffer) at 256 + 128 map + 64 buffer
+  // of a map's 256 columns: O_s, logits, weights of even and of odd tiles
+  static constexpr uint32_t kMapCols = 256, kSCol = 128, kPCol = 192;
   static constexpr size_t kSmemBytes = 1024 + 2 * (size_t)kQBytes + 2 * (size_t)kStages * kKvBytes;
 };
 
@@ -73,6 +81,49 @@ __device__ __forceinline__ bool elect_one() {
   uint32_t r;
   asm volatile("{\n\t.reg .pred q;\n\telect.sync _|q, 0xffffffff;\n\tselp.u32 %0, 1, 0, q;\n\t}" : "=r"(r));
   return r != 0;
+}
+
+__device__ __forceinline__ float max3(float a, float b, float c) {
+  float r;
+  asm("max.f32 %0, %1, %2, %3;" : "=f"(r) : "f"(a), "f"(b), "f"(c));
+  return r;
+}
+
+// Two fp32 operations in one instruction.
+__device__ __forceinline__ float2 fma2(float2 a, float2 b, float2 c) {
+  float2 r;
+  asm("{\n\t.reg .b64 x, y, z, w;\n\t"
+      "mov.b64 x, {%2, %3};\n\tmov.b64 y, {%4, %5};\n\tmov.b64 z, {%6, %7};\n\t"
+      "fma.rn.f32x2 w, x, y, z;\n\t"
+      "mov.b64 {%0, %1}, w;\n\t}"
+      : "=f"(r.x), "=f"(r.y)
+      : "f"(a.x), "f"(a.y), "f"(b.x), "f"(b.y), "f"(c.x), "f"(c.y));
+  return r;
+}
+__device__ __forceinline__ float2 add2(float2 a, float2 b) {
+  float2 r;
+  asm("{\n\t.reg .b64 x, y, w;\n\t"
+      "mov.b64 x, {%2, %3};\n\tmov.b64 y, {%4, %5};\n\t"
+      "add.rn.f32x2 w, x, y;\n\t"
+      "mov.b64 {%0, %1}, w;\n\t}"
+      : "=f"(r.x), "=f"(r.y)
+      : "f"(a.x), "f"(a.y), "f"(b.x), "f"(b.y));
+  return r;
+}
+
+// The slow side of a bounded wait, a short rolled loop: the kernel waits in two dozen places, and its roles share the instruction
+// cache.
+__device__ __forceinline__ bool wait_on(uint64_t* bar, uint32_t parity, volatile int* abort_flag, uint64_t limit_ns) {
+  const uint64_t t0 = global_timer_ns();
+#pragma unroll 1
+  while (!mbar_try_wait(bar, parity)) {
+    if (*abort_flag) return false;
+    if (global_timer_ns() - t0 > limit_ns) {
+      *abort_flag = 1;
+      return false;
+    }
+  }
+  return true;
 }
 
 // Item number idx: query tiles in the order of their rows, last rows first, over all sequences; the heads of a tile one after
@@ -130,7 +181,8 @@ diff_prefill_kernel(const __grid_constant__ CUtensorMap tmap_q, const __grid_con
   uint8_t* k_s = q_s + 2 * C::kQBytes;
   uint8_t* v_s = k_s + kStages * C::kKvBytes;
   __shared__ uint64_t s_item_full[kItems], s_item_empty[kItems], s_q_full[2], s_q_empty[2], s_k_full[kStages], s_k_empty[kStages],
-      s_v_full[kStages], s_v_empty[kStages], s_s_full[2][2], s_p_full[2][2], s_o_full[2][2], s_o_free, s_inv_full, s_sq_full;
+      s_v_full[kStages], s_v_clear, s_v_empty[kStages], s_s_full[2], s_s_free[2], s_p_full[2][2], s_o_full[2][2], s_o_free, s_inv_full,
+      s_sq_full;
   __shared__ Item s_item[kItems];
   __shared__ float s_inv[2][kRows], s_sq[2][kRows];
   __shared__ uint32_t s_tmem;
@@ -145,19 +197,21 @@ diff_prefill_kernel(const __grid_constant__ CUtensorMap tmap_q, const __grid_con
     }
     for (int i = 0; i < kStages; ++i) {
       mbar_init(&s_k_full[i], 1);
-      mbar_init(&s_k_empty[i], 1);
+      mbar_init(&s_k_empty[i], 2);
       mbar_init(&s_v_full[i], 1);
-      mbar_init(&s_v_empty[i], 1);
+      mbar_init(&s_v_empty[i], 2);
     }
     for (int i = 0; i < 2; ++i) {
       mbar_init(&s_q_full[i], 1);
-      mbar_init(&s_q_empty[i], 1);
+      mbar_init(&s_q_empty[i], 2);
+      mbar_init(&s_s_full[i], 1);
+      mbar_init(&s_s_free[i], kSoftWarps / 2);
       for (int b = 0; b < 2; ++b) {
-        mbar_init(&s_s_full[i][b], 1);
         mbar_init(&s_p_full[i][b], kSoftWarps / 2);
         mbar_init(&s_o_full[i][b], 1);
       }
     }
+    mbar_init(&s_v_clear, 1);
     mbar_init(&s_o_free, kSoftWarps);
     mbar_init(&s_inv_full, kSoftWarps);
     mbar_init(&s_sq_full, kSoftWarps);
@@ -177,7 +231,10 @@ diff_prefill_kernel(const __grid_constant__ CUtensorMap tmap_q, const __grid_con
   const uint32_t tmem = s_tmem;
 
   auto wait = [&](uint64_t* bar, uint32_t parity) -> bool {
-    return __all_sync(0xffffffffu, ws_wait(bar, parity & 1u, s_abort, p.wait_ns));
+    bool ok = true;
+    if (__builtin_expect(!mbar_try_wait(bar, parity & 1u), 0)) ok = wait_on(bar, parity & 1u, s_abort, p.wait_ns);
+    __syncwarp();
+    return ok;
   };
   // the n-th item; false when there is none (or a wait has expired)
   auto get_item = [&](uint32_t n, Item* it) -> bool {
@@ -190,6 +247,8 @@ diff_prefill_kernel(const __grid_constant__ CUtensorMap tmap_q, const __grid_con
     if (lane == 0) mbar_arrive(&s_item_empty[n % kItems]);
   };
 
+  if (warp >= kSoftWarps) {
+  asm volatile("setmaxnreg.dec.sync.aligned.u32 %0;" ::"n"(kRoleRegs));
   if (warp == 8) {
     // ================================================================ Q and K tiles
     uint32_t jj = 0;
@@ -254,96 +313,98 @@ diff_prefill_kernel(const __grid_constant__ CUtensorMap tmap_q, const __grid_con
       if (!ok) break;
       it = next;
     }
-  } else if (warp == 9) {
-    // ================================================================ the logits
+  } else if (warp == 9 || warp == 10) {
+    // ================================================================ the logits of a map
+    const int map = warp - 9;
     constexpr uint32_t kIdesc = umma_idesc(kRows, kKeys);
+    const uint32_t s_at = tmem + map * C::kMapCols + C::kSCol;
     uint32_t jj = 0;
     Item it;
-    for (uint32_t n = 0; get_item(n, &it); ++n) {
+    bool ok = true;
+    for (uint32_t n = 0; ok && get_item(n, &it); ++n) {
       done_item(n);
       const int n_kt = key_tiles(it);
-      if (!wait(&s_q_full[n & 1], n / 2)) break;
+      ok = wait(&s_q_full[n & 1], n / 2);
       const uint64_t q_desc = umma_desc_k128(smem_u32(q_s + (n & 1) * C::kQBytes));
-      bool ok = true;
       for (int j = 0; j < n_kt; ++j, ++jj) {
-        const uint32_t s = jj % kStages, b = jj & 1;
-        ok = wait(&s_k_full[s], jj / kStages);
+        const uint32_t s = jj % kStages;
+        ok = ok && wait(&s_k_full[s], jj / kStages);
+        if (jj > 0) ok = ok && wait(&s_s_free[map], jj - 1);            // the tile before is in registers
+        // the product of the tile before that has read its weights, whose buffer this tile's go to
+        if (jj > 1) ok = ok && wait(&s_o_full[map][jj & 1], jj / 2 - 1);
         if (!ok) break;
-        const uint64_t k_desc = umma_desc_k128(smem_u32(k_s + s * C::kKvBytes));
+        tc_fence_after_sync();
+        if (elect_one()) {
+          const uint64_t k_desc = umma_desc_k128(smem_u32(k_s + s * C::kKvBytes));
 #pragma unroll
-        for (int map = 0; map < 2; ++map) {
-          // the buffer holds P of tile jj - 2 until that tile's product has read it
-          if (jj >= 2 && ok) ok = wait(&s_o_full[map][b], jj / 2 - 1);
-          if (!ok) break;
-          tc_fence_after_sync();
-          if (elect_one()) {
-#pragma unroll
-            for (int x = 0; x < C::kMapSteps; ++x) {
-              const int k = map * C::kMapSteps + x;
-              const uint64_t q_off = (uint64_t)(((k / 4) * C::kQHalfBytes + (k % 4) * 32) >> 4);
-              const uint64_t k_off = (uint64_t)(((k / 4) * C::kKvHalfBytes + (k % 4) * 32) >> 4);
-              umma_bf16(tmem + C::kSCol + map * 128 + b * 64, q_desc + q_off, k_desc + k_off, kIdesc, x > 0 ? 1u : 0u);
-            }
-            umma_commit(&s_s_full[map][b]);
-            if (map == 1) {
-              umma_commit(&s_k_empty[s]);
-              if (j == n_kt - 1) umma_commit(&s_q_empty[n & 1]);
-            }
+          for (int x = 0; x < C::kMapSteps; ++x) {
+            const int k = map * C::kMapSteps + x;
+            const uint64_t q_off = (uint64_t)(((k / 4) * C::kQHalfBytes + (k % 4) * 32) >> 4);
+            const uint64_t k_off = (uint64_t)(((k / 4) * C::kKvHalfBytes + (k % 4) * 32) >> 4);
+            umma_bf16(s_at, q_desc + q_off, k_desc + k_off, kIdesc, x > 0 ? 1u : 0u);
           }
-          __syncwarp();
+          umma_commit(&s_s_full[map]);
+          umma_commit(&s_k_empty[s]);
+          if (j == n_kt - 1) umma_commit(&s_q_empty[n & 1]);
         }
-        if (!ok) break;
+        __syncwarp();
       }
-      if (!ok) break;
     }
-  } else if (warp == 10) {
-    // ================================================================ the outputs
+  } else if (warp == 12 || warp == 13) {
+    // ================================================================ the outputs of a map
+    const int map = warp - 12;
     constexpr uint32_t kIdesc = umma_idesc_b_mn(kRows, D);
-    uint32_t jj = 0;
+    const uint32_t o_at = tmem + map * C::kMapCols, p_at = o_at + C::kPCol;
+    uint32_t jj = 0, n_clear = 0;
     Item it;
-    for (uint32_t n = 0; get_item(n, &it); ++n) {
+    bool ok = true;
+    for (uint32_t n = 0; ok && get_item(n, &it); ++n) {
       done_item(n);
       const int n_kt = key_tiles(it);
-      bool ok = true;
+      // the item before has read its O (which also keeps the two warps within one clearing of each other)
+      if (n > 0) ok = wait(&s_o_free, n - 1);
       for (int j = 0; j < n_kt; ++j, ++jj) {
         const uint32_t s = jj % kStages, b = jj & 1;
-        ok = wait(&s_v_full[s], jj / kStages);
+        ok = ok && wait(&s_v_full[s], jj / kStages);
         if (!ok) break;
         const int left = it.t - j * kKeys;
         if (left < kKeys) {                                  // rows behind the prompt's last one
-          uint4* v = reinterpret_cast<uint4*>(v_s + s * C::kKvBytes);
-          for (int i = left * 8 + lane; i < kKeys * 8; i += 32)
+          if (map == 0) {
+            uint4* v = reinterpret_cast<uint4*>(v_s + s * C::kKvBytes);
+            for (int i = left * 8 + lane; i < kKeys * 8; i += 32)
 #pragma unroll
-            for (int hf = 0; hf < C::kHalves; ++hf) v[hf * (C::kKvHalfBytes / 16) + i] = make_uint4(0u, 0u, 0u, 0u);
-          fence_proxy_async_smem();
-          __syncwarp();
-        }
-        const uint32_t v_base = smem_u32(v_s + s * C::kKvBytes);
-#pragma unroll
-        for (int map = 0; map < 2; ++map) {
-          ok = wait(&s_p_full[map][b], jj / 2);
-          if (ok && j == 0 && map == 0 && n > 0) ok = wait(&s_o_free, n - 1);     // the item before has read its O
-          if (!ok) break;
-          tc_fence_after_sync();
-          if (elect_one()) {
-#pragma unroll
-            for (int k = 0; k < kKeys / 16; ++k)
-              umma_bf16_a_tmem(tmem + map * 128, tmem + C::kSCol + map * 128 + b * 64 + k * 8,
-                               umma_desc_mn128(v_base + k * 16 * 128, C::kKvHalfBytes), kIdesc, (j > 0 || k > 0) ? 1u : 0u);
-            umma_commit(&s_o_full[map][b]);
-            if (map == 1) umma_commit(&s_v_empty[s]);
+              for (int hf = 0; hf < C::kHalves; ++hf) v[hf * (C::kKvHalfBytes / 16) + i] = make_uint4(0u, 0u, 0u, 0u);
+            fence_proxy_async_smem();
+            __syncwarp();
+            if (lane == 0) mbar_arrive(&s_v_clear);
+          } else {
+            ok = wait(&s_v_clear, n_clear);
+            fence_proxy_async_smem();
           }
-          __syncwarp();
+          ++n_clear;
         }
+        ok = ok && wait(&s_p_full[map][b], jj / 2);
         if (!ok) break;
+        tc_fence_after_sync();
+        if (elect_one()) {
+          const uint64_t v_desc = umma_desc_mn128(smem_u32(v_s + s * C::kKvBytes), C::kKvHalfBytes);
+#pragma unroll
+          for (int k = 0; k < kKeys / 16; ++k)
+            umma_bf16_a_tmem(o_at, p_at + b * 32 + k * 8, v_desc + (uint64_t)(k * 16 * 128 >> 4), kIdesc,
+                             (j > 0 || k > 0) ? 1u : 0u);
+          umma_commit(&s_o_full[map][b]);
+          umma_commit(&s_v_empty[s]);
+        }
+        __syncwarp();
       }
-      if (!ok) break;
     }
+  }
   } else {
     // ================================================================ softmax of map `map`
+    asm volatile("setmaxnreg.inc.sync.aligned.u32 %0;" ::"n"(kSoftRegs));
     const int map = warp >> 2, r = tid & (kRows - 1);
     const uint32_t lanes = tmem + ((uint32_t)(32 * (warp & 3)) << 16);
-    const uint32_t o_at = lanes + map * 128, s_at = lanes + C::kSCol + map * 128;
+    const uint32_t o_at = lanes + map * C::kMapCols, s_at = o_at + C::kSCol, p_at = o_at + C::kPCol;
     uint32_t jj = 0;
     Item it;
     for (uint32_t n = 0; get_item(n, &it); ++n) {
@@ -353,29 +414,27 @@ diff_prefill_kernel(const __grid_constant__ CUtensorMap tmap_q, const __grid_con
       bool ok = true;
       for (int j = 0; j < n_kt; ++j, ++jj) {
         const uint32_t b = jj & 1;
-        ok = wait(&s_s_full[map][b], jj / 2);
+        ok = wait(&s_s_full[map], jj);
         if (!ok) break;
         tc_fence_after_sync();
         float v[2][32];
-        tmem_ld32(s_at + b * 64, v[0]);
-        tmem_ld32(s_at + b * 64 + 32, v[1]);
+        tmem_ld32(s_at, v[0]);
+        tmem_ld32(s_at + 32, v[1]);
         tmem_wait_ld();
+        tc_fence_before_sync();
+        __syncwarp();
+        if (lane == 0) mbar_arrive(&s_s_free[map]);
         const int c0 = j * kKeys;
         if (c0 + kKeys - 1 > it.q0) {                        // the tile holds keys behind some row
 #pragma unroll
-          for (int i = 0; i < 32; ++i) {
-            if (c0 + i > row) v[0][i] = -INFINITY;
-            if (c0 + 32 + i > row) v[1][i] = -INFINITY;
-          }
+          for (int i = 0; i < kKeys; ++i)
+            if (c0 + i > row) v[i >> 5][i & 31] = -INFINITY;
         }
         float m4[4] = {-INFINITY, -INFINITY, -INFINITY, -INFINITY};
 #pragma unroll
-        for (int i = 0; i < 32; i += 4) {
-          m4[0] = fmaxf(m4[0], fmaxf(v[0][i], v[1][i]));
-          m4[1] = fmaxf(m4[1], fmaxf(v[0][i + 1], v[1][i + 1]));
-          m4[2] = fmaxf(m4[2], fmaxf(v[0][i + 2], v[1][i + 2]));
-          m4[3] = fmaxf(m4[3], fmaxf(v[0][i + 3], v[1][i + 3]));
-        }
+        for (int i = 0; i < kKeys; i += 8)
+#pragma unroll
+          for (int x = 0; x < 4; ++x) m4[x] = max3(m4[x], v[i >> 5][(i & 31) + x], v[i >> 5][(i & 31) + x + 4]);
         const float mx = fmaxf(fmaxf(m4[0], m4[1]), fmaxf(m4[2], m4[3])) * p.scale_log2;   // key 0 is visible to every row
         const bool grow = mx > m_ref + kLazy;                // also on the first tile
         float alpha = 1.f;
@@ -399,21 +458,23 @@ diff_prefill_kernel(const __grid_constant__ CUtensorMap tmap_q, const __grid_con
           }
           tmem_wait_st();
         }
-        float sm[4] = {0.f, 0.f, 0.f, 0.f};
+        float2 sm[2] = {{0.f, 0.f}, {0.f, 0.f}};
+        const float2 scale2 = {p.scale_log2, p.scale_log2}, ref2 = {-m_ref, -m_ref};
         uint32_t packed[32];
 #pragma unroll
         for (int c = 0; c < kKeys; c += 4) {
-          float e[4];
 #pragma unroll
-          for (int i = 0; i < 4; ++i) {
-            e[i] = fast_exp2(fmaf(v[c >> 5][(c & 31) + i], p.scale_log2, -m_ref));
-            sm[i] += e[i];
+          for (int x = 0; x < 2; ++x) {
+            const int i = c + 2 * x;
+            float2 e = fma2({v[i >> 5][i & 31], v[i >> 5][(i & 31) + 1]}, scale2, ref2);
+            e = {fast_exp2(e.x), fast_exp2(e.y)};
+            sm[x] = add2(sm[x], e);
+            packed[i >> 1] = pack_bf16(e.x, e.y);
           }
-          packed[c >> 1] = pack_bf16(e[0], e[1]);
-          packed[(c >> 1) + 1] = pack_bf16(e[2], e[3]);
         }
-        tmem_st32u(s_at + b * 64, packed);
-        l += (sm[0] + sm[1]) + (sm[2] + sm[3]);
+        // (the buffer is free: this tile's logits were issued after the product of the tile before the last)
+        tmem_st32u(p_at + b * 32, packed);
+        l += (sm[0].x + sm[0].y) + (sm[1].x + sm[1].y);
         tmem_wait_st();
         tc_fence_before_sync();
         __syncwarp();
@@ -437,7 +498,7 @@ diff_prefill_kernel(const __grid_constant__ CUtensorMap tmap_q, const __grid_con
       for (int c = 0; c < D / 2; c += 32) {
         float a[32], x[32];
         tmem_ld32(lanes + map * (D / 2) + c, a);
-        tmem_ld32(lanes + 128 + map * (D / 2) + c, x);
+        tmem_ld32(lanes + C::kMapCols + map * (D / 2) + c, x);
         tmem_wait_ld();
 #pragma unroll
         for (int i = 0; i < 32; ++i) {
@@ -493,8 +554,10 @@ xkv_status launch(const CUtensorMap& tq, const CUtensorMap& tk, const CUtensorMa
   int dev = 0;
   if (cudaGetDevice(&dev) != cudaSuccess || dev < 0 || dev >= 64) return XKV_ERR_CUDA;
   if (!done[dev].load(std::memory_order_acquire)) {
-    if (cudaFuncSetAttribute(diff_prefill_kernel<D>, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)Cfg<D>::kSmemBytes) !=
-        cudaSuccess) {
+    cudaFuncAttributes attr;           // the split of the registers counts on the launch's
+    if (cudaFuncGetAttributes(&attr, diff_prefill_kernel<D>) != cudaSuccess || attr.numRegs != kLaunchRegs ||
+        cudaFuncSetAttribute(diff_prefill_kernel<D>, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)Cfg<D>::kSmemBytes) !=
+            cudaSuccess) {
       (void)cudaGetLastError();
       return XKV_ERR_CUDA;
     }
