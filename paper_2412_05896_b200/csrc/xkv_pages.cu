@@ -45,61 +45,73 @@ struct CopyParams {
   int32_t scale_rows;                 // rows a scale stands for, 0: no scales
 };
 
-// One warp: piece `unit` of a list of row copies, numbered copy by copy, K before V, head by head.
-__device__ __forceinline__ void copy_piece(const CopyParams& p, const RowCopy& c, int part) {
+// One warp: the rows of one head, of K (part < n_kv_heads) or of V, from piece `piece` on, every `step`-th.
+__device__ __forceinline__ void copy_head(const CopyParams& p, const RowCopy& c, int part, int piece, int step) {
   const int lane = threadIdx.x & 31;
-  const int piece = part % p.pieces, rest = part / p.pieces;
-  const int h = rest % p.n_kv_heads, kv = rest / p.n_kv_heads;
-  const int bytes = c.rows * p.row_bytes - piece * kPiece;
-  if (bytes <= 0) return;
+  const bool is_v = part >= p.n_kv_heads;
+  const int h = is_v ? part - p.n_kv_heads : part, bytes = c.rows * p.row_bytes;
   const size_t from = (size_t)c.src * p.n_kv_heads + h, to = (size_t)c.dst * p.n_kv_heads + h;
   const size_t page_bytes = (size_t)p.page_size * p.row_bytes;
-  const uint4* s = reinterpret_cast<const uint4*>((kv ? p.from.v_pages : p.from.k_pages) + from * page_bytes + (size_t)piece * kPiece);
-  uint4* d = reinterpret_cast<uint4*>((kv ? p.to.v_pages : p.to.k_pages) + to * page_bytes + (size_t)piece * kPiece);
-  const int n = min(bytes, kPiece) / 16;
-  uint4 v[kPiece / 512];
+  const uint8_t* s = (is_v ? p.from.v_pages : p.from.k_pages) + from * page_bytes;
+  uint8_t* d = (is_v ? p.to.v_pages : p.to.k_pages) + to * page_bytes;
+  if (p.scale_rows > 0 && piece == 0) {
+    const int n = (c.rows + p.scale_rows - 1) / p.scale_rows, per = p.page_size / p.scale_rows;
+    const float* ss = (is_v ? p.from.v_scales : p.from.k_scales) + from * per;
+    float* ds = (is_v ? p.to.v_scales : p.to.k_scales) + to * per;
+    for (int i = lane; i < n; i += 32) ds[i] = ss[i];
+  }
+#pragma unroll 1
+  for (int at = piece * kPiece; at < bytes; at += step * kPiece) {
+    const uint4* s4 = reinterpret_cast<const uint4*>(s + at) + lane;
+    uint4* d4 = reinterpret_cast<uint4*>(d + at) + lane;
+    const int n = min(bytes - at, kPiece) / 16;
+    uint4 v[kPiece / 512];
 #pragma unroll
-  for (int i = 0; i < kPiece / 512; ++i)
-    if (i * 32 + lane < n) v[i] = __ldcs(s + i * 32 + lane);
-  float sc[8];
-  const int n_scales = piece == 0 && p.scale_rows > 0 ? (c.rows + p.scale_rows - 1) / p.scale_rows : 0;
-  const int page_scales = p.scale_rows > 0 ? p.page_size / p.scale_rows : 0;
+    for (int i = 0; i < kPiece / 512; ++i)
+      if (i * 32 + lane < n) v[i] = __ldcs(s4 + i * 32);
 #pragma unroll
-  for (int i = 0; i < 8; ++i)         // a page has at most 256 rows
-    if (i * 32 + lane < n_scales) sc[i] = (kv ? p.from.v_scales : p.from.k_scales)[from * page_scales + i * 32 + lane];
-#pragma unroll
-  for (int i = 0; i < kPiece / 512; ++i)
-    if (i * 32 + lane < n) d[i * 32 + lane] = v[i];
-#pragma unroll
-  for (int i = 0; i < 8; ++i)
-    if (i * 32 + lane < n_scales) (kv ? p.to.v_scales : p.to.k_scales)[to * page_scales + i * 32 + lane] = sc[i];
+    for (int i = 0; i < kPiece / 512; ++i)
+      if (i * 32 + lane < n) d4[i * 32] = v[i];
+  }
+}
+
+// Calls f(copy, part, piece, step) for this warp's share of n copies: a head's rows go to as many warps as a page has pieces,
+// which take every step-th piece (whole pages) or all to one warp (the first rows of pages, often less than a piece).
+template <typename F>
+__device__ __forceinline__ void each_head(const CopyParams& p, int64_t n, bool whole, F f) {
+  const int step = whole ? p.pieces : 1, per = 2 * p.n_kv_heads * step;
+  const int64_t warp = (int64_t)blockIdx.x * (kCopyThreads / 32) + (threadIdx.x >> 5);
+  const int64_t n_warps = (int64_t)gridDim.x * (kCopyThreads / 32), end = n * per;
+  if (end <= 0x7fffffffll - n_warps) {
+    for (int u = (int)warp; u < (int)end; u += (int)n_warps) {
+      const int c = u / per, rest = u - c * per;
+      f(c, rest / step, rest % step, step);
+    }
+  } else {
+    for (int64_t u = warp; u < end; u += n_warps) f(u / per, (int)(u % per) / step, (int)(u % per) % step, step);
+  }
 }
 
 // The list that a plan has made: entries and their number in the workspace.
 __global__ void __launch_bounds__(kCopyThreads) copy_rows_kernel(const CopyParams p, const RowCopy* list, const int32_t* n_list) {
   asm volatile("griddepcontrol.wait;" ::: "memory");
-  const int64_t per = 2 * (int64_t)p.n_kv_heads * p.pieces, n = __ldcg(n_list) * per;
-  const int64_t step = (int64_t)gridDim.x * (kCopyThreads / 32);
-  for (int64_t u = (int64_t)blockIdx.x * (kCopyThreads / 32) + (threadIdx.x >> 5); u < n; u += step) {
-    const RowCopy c = {__ldcg(&list[u / per].src), __ldcg(&list[u / per].dst), __ldcg(&list[u / per].rows)};
-    copy_piece(p, c, (int)(u % per));
-  }
+  each_head(p, __ldcg(n_list), false, [&](int64_t i, int part, int piece, int step) {
+    copy_head(p, {__ldcg(&list[i].src), __ldcg(&list[i].dst), __ldcg(&list[i].rows)}, part, piece, step);
+  });
 }
 
 // Page ids that a caller gives.
 __global__ void __launch_bounds__(kCopyThreads) copy_pages_kernel(const CopyParams p, const int32_t* src, const int32_t* dst,
                                                                   int64_t n_copies, int32_t n_from, int32_t n_to,
                                                                   WorkspaceHeader* hdr) {
-  const int64_t per = 2 * (int64_t)p.n_kv_heads * p.pieces, n = n_copies * per;
-  const int64_t step = (int64_t)gridDim.x * (kCopyThreads / 32);
-  for (int64_t u = (int64_t)blockIdx.x * (kCopyThreads / 32) + (threadIdx.x >> 5); u < n; u += step) {
-    const RowCopy c = {__ldg(&src[u / per]), __ldg(&dst[u / per]), p.page_size};
+  each_head(p, n_copies, true, [&](int64_t i, int part, int piece, int step) {
+    const RowCopy c = {__ldg(&src[i]), __ldg(&dst[i]), p.page_size};
     if (c.src < 0 || c.src >= n_from || c.dst < 0 || c.dst >= n_to) {
-      if (u % per == 0 && (threadIdx.x & 31) == 0) record_status(hdr, XKV_ERR_INVALID_ARG);
-      continue;
+      if (part == 0 && piece == 0 && (threadIdx.x & 31) == 0) record_status(hdr, XKV_ERR_INVALID_ARG);
+      return;
     }
-    copy_piece(p, c, (int)(u % per));
-  }
+    copy_head(p, c, part, piece, step);
+  });
 }
 
 CopyParams copy_params(const xkv_dims* d, const xkv_cache* from, const xkv_cache* to) {
@@ -114,8 +126,8 @@ CopyParams copy_params(const xkv_dims* d, const xkv_cache* from, const xkv_cache
   return p;
 }
 
-int copy_grid(const CopyParams& p, int64_t most_copies) {
-  const int64_t warps = most_copies * 2 * p.n_kv_heads * p.pieces;
+int copy_grid(const CopyParams& p, int64_t most_copies, bool whole) {
+  const int64_t warps = most_copies * 2 * p.n_kv_heads * (whole ? p.pieces : 1);
   const int64_t ctas = (warps + kCopyThreads / 32 - 1) / (kCopyThreads / 32);
   return (int)std::max<int64_t>(1, std::min<int64_t>(ctas, 8 * (int64_t)sm_count()));
 }
@@ -176,14 +188,16 @@ struct ForkParams {
   int32_t* free_pages;
   int32_t n_free;
   int32_t* used;
-  int32_t n_layers, batch, cols, page_size, n_pages;
+  int32_t n_rows, batch, cols, page_size, n_pages;    // n_rows: caches, L * B
   WorkspaceHeader* hdr;
   int32_t* n_copies;                  // of the list
   int32_t* counts;                    // [2][kMaxCluster] copies and returned pages of the CTAs
   RowCopy* list;                      // [L * B]
+  int4* rows;                         // [L * B] a ForkRow each
   int32_t* last;                      // [L * B] partly filled last page, -1: none
   int32_t* rank;                      // [L * B] place among the CTA's copies, -1: no copy
   uint32_t* gone;                     // a bit a page: nobody holds it any more; zero between calls
+  int32_t* word_at;                   // bits before each of its words, within a CTA's share of them
   int32_t* fresh;                     // [L][B][cols] entries of caches that become forks
 };
 
@@ -192,116 +206,103 @@ __device__ __forceinline__ bool in_pool(const ForkParams& p, int page) { return 
 struct ForkRow {
   int32_t parent, rows, have, need;   // parent -1: freed; rows after the step; pages before and after it
 };
+__device__ __forceinline__ ForkRow as_row(int4 x) { return {x.x, x.y, x.z, x.w}; }
 
 __device__ __forceinline__ int parent_of(const ForkParams& p, int b) {
   const int a = __ldg(&p.parent[b]);
   return a >= -1 && a < p.batch ? a : b;
 }
 
-// What becomes of cache (l, b); lengths as they were before the step.
-__device__ __forceinline__ ForkRow fork_row(const ForkParams& p, int l, int b) {
-  const int most = p.cols * p.page_size;
-  ForkRow r;
-  r.parent = parent_of(p, b);
-  const int n = min(max(__ldcg(&p.lens[(size_t)l * p.batch + b]), 0), most);
-  r.rows = r.parent < 0 ? 0 : (r.parent == b ? n : min(max(__ldcg(&p.lens[(size_t)l * p.batch + r.parent]), 0), most));
-  if (p.keep != nullptr) {
-    const int k = __ldg(&p.keep[(size_t)l * p.keep_stride + b]);
-    if (k >= 0) r.rows = min(r.rows, k);
-  }
-  r.have = (n + p.page_size - 1) / p.page_size;
-  r.need = (r.rows + p.page_size - 1) / p.page_size;
-  return r;
+// What becomes of a cache; lengths as they were before the step.
+__device__ __forceinline__ int4 fork_row(const ForkParams& p, int row) {
+  const int l = row / p.batch, b = row - l * p.batch, most = p.cols * p.page_size;
+  const int own = __ldcg(&p.lens[row]), k = p.keep != nullptr ? __ldg(&p.keep[(size_t)l * p.keep_stride + b]) : -1;
+  const int asked = __ldg(&p.parent[b]), a = asked >= -1 && asked < p.batch ? asked : b;
+  if (a != asked) record_status(p.hdr, XKV_ERR_INVALID_ARG);
+  const int n = min(max(own, 0), most);
+  int rows = a < 0 ? 0 : (a == b ? n : min(max(__ldcg(&p.lens[(size_t)l * p.batch + a]), 0), most));
+  if (k >= 0) rows = min(rows, k);
+  return make_int4(a, rows, (n + p.page_size - 1) / p.page_size, (rows + p.page_size - 1) / p.page_size);
 }
 
-__global__ void __launch_bounds__(kPlanThreads, 1) fork_kernel(const ForkParams p) {
-  asm volatile("griddepcontrol.launch_dependents;");
-  __shared__ int s_scan[kPlanWarps + 1];
-  const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5;
-  const int n_rows = p.n_layers * p.batch, n_warps = gridDim.x * kPlanWarps, w0 = blockIdx.x * kPlanWarps + warp;
+// A warp: holders that come are counted, before any that go (so that no page seems to be free in between); the parent's entries
+// are read before any table changes.
+__device__ __forceinline__ void count_new(const ForkParams& p, int row, const ForkRow& r) {
+  const int lane = threadIdx.x & 31, b = row % p.batch;
+  const int32_t* mine = p.table + (size_t)row * p.cols;
+  const int32_t* theirs = p.table + ((size_t)(row - b) + max(r.parent, 0)) * p.cols;
+  int32_t* fresh = p.fresh + (size_t)row * p.cols;
+  if (lane == 0) {
+    const int e = r.rows % p.page_size != 0 ? __ldcg(&theirs[r.need - 1]) : -1;
+    p.last[row] = in_pool(p, e) ? e : -1;
+  }
+  if (r.parent == b) return;
+#pragma unroll 4
+  for (int i = lane; i < r.need; i += 32) {
+    const int e = __ldcg(&theirs[i]);
+    const int was = i < r.have ? __ldcg(&mine[i]) : e - 1;
+    fresh[i] = e;
+    if (!in_pool(p, e)) record_status(p.hdr, XKV_ERR_INVALID_ARG);
+    else if (was != e) atomicAdd(&p.shares[e], 1);
+  }
+}
 
-  // ---- holders to come are counted first, so that no page seems to be free in between; the parents' entries are read
-  //      before any table changes
-  for (int row = w0; row < n_rows; row += n_warps) {
-    const int l = row / p.batch, b = row % p.batch;
-    const ForkRow r = fork_row(p, l, b);
-    const int32_t* mine = p.table + (size_t)row * p.cols;
-    const int32_t* theirs = p.table + ((size_t)l * p.batch + max(r.parent, 0)) * p.cols;
-    int32_t* fresh = p.fresh + (size_t)row * p.cols;
-    if (r.parent != b && lane == 0 && __ldg(&p.parent[b]) != r.parent) record_status(p.hdr, XKV_ERR_INVALID_ARG);
-    if (r.parent == b && lane == 0 && __ldg(&p.parent[b]) != b) record_status(p.hdr, XKV_ERR_INVALID_ARG);
-    if (r.parent != b) {
-      for (int i = lane; i < r.need; i += 32) {
-        const int e = __ldcg(&theirs[i]);
-        fresh[i] = e;
-        if (in_pool(p, e)) {
-          if (i >= r.have || __ldcg(&mine[i]) != e) atomicAdd(&p.shares[e], 1);
-        } else {
-          record_status(p.hdr, XKV_ERR_INVALID_ARG);
-        }
-      }
+// A warp: entries that go, and the table.
+__device__ __forceinline__ void drop_old(const ForkParams& p, int row, const ForkRow& r) {
+  const int lane = threadIdx.x & 31, b = row % p.batch;
+  int32_t* mine = p.table + (size_t)row * p.cols;
+  const int32_t* fresh = p.fresh + (size_t)row * p.cols;
+#pragma unroll 4
+  for (int i = (r.parent == b ? r.need : 0) + lane; i < max(r.have, r.need); i += 32) {
+    const int now = i < r.need ? __ldcg(&fresh[i]) : -1;
+    const int was = i < r.have ? __ldcg(&mine[i]) : -1;
+    if (i < r.need && i < r.have && was == now) continue;
+    if (i < r.need) mine[i] = now;
+    if (i >= r.have) continue;
+    if (!in_pool(p, was)) {
+      record_status(p.hdr, XKV_ERR_INVALID_ARG);
+      continue;
     }
-    if (lane == 0) {
-      const int e = r.rows % p.page_size != 0 ? __ldcg(&theirs[r.need - 1]) : -1;
-      p.last[row] = in_pool(p, e) ? e : -1;
-    }
+    const int others = atomicSub(&p.shares[was], 1);
+    if (others == 0) atomicOr(&p.gone[was >> 5], 1u << (was & 31));
+    if (others < 0) record_status(p.hdr, XKV_ERR_INVALID_ARG);
   }
-  // lengths are read again below, and change only behind the next barrier
-  phase();
-  // ---- entries that go, tables
-  for (int row = w0; row < n_rows; row += n_warps) {
-    const int l = row / p.batch, b = row % p.batch;
-    const ForkRow r = fork_row(p, l, b);
-    int32_t* mine = p.table + (size_t)row * p.cols;
-    const int32_t* fresh = p.fresh + (size_t)row * p.cols;
-    for (int i = (r.parent == b ? r.need : 0) + lane; i < max(r.have, r.need); i += 32) {
-      const int now = i < r.need ? __ldcg(&fresh[i]) : -1;
-      if (i < r.have) {
-        const int was = __ldcg(&mine[i]);
-        if (i < r.need && was == now) continue;
-        if (in_pool(p, was)) {
-          const int others = atomicSub(&p.shares[was], 1);
-          if (others == 0) atomicOr(&p.gone[was >> 5], 1u << (was & 31));
-          if (others < 0) record_status(p.hdr, XKV_ERR_INVALID_ARG);
-        } else {
-          record_status(p.hdr, XKV_ERR_INVALID_ARG);
-        }
-      }
-      if (i < r.need) mine[i] = now;
-    }
-  }
-  phase();
+}
+
+// The whole cluster: pages for copies, lengths, and pages back to the list.  row_at(row): its ForkRow.
+template <typename RowAt>
+__device__ __forceinline__ void fork_decide(const ForkParams& p, int* s_scan, RowAt row_at) {
   // ---- last pages that need a copy: those that others hold too, unless all holders are such last pages, of which one
-  //      (the cache that stays, else the first) keeps it
+  //      (the cache that stays, else the first) keeps it.  A warp a cache.
+  const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5;
   int64_t row0, row1;
-  cta_run(n_rows, &row0, &row1);
-  int copies = 0;
-  for (int64_t base = row0; base < row1; base += kPlanThreads) {
-    const int row = (int)base + threadIdx.x;
-    const int page = row < row1 ? __ldcg(&p.last[row]) : -1;
+  cta_run(p.n_rows, &row0, &row1);
+  for (int row = (int)row0 + warp; row < (int)row1; row += kPlanWarps) {
+    const int page = __ldcg(&p.last[row]);
     const int others = page >= 0 ? __ldcg(&p.shares[page]) : 0;
     bool copy = false;
-    unsigned asked = __ballot_sync(0xffffffffu, others > 0);
-    while (asked != 0) {
-      const int src = __ffs(asked) - 1;
-      asked &= asked - 1;
-      const int q = __shfl_sync(0xffffffffu, page, src), at = __shfl_sync(0xffffffffu, row, src);
-      const int n_others = __shfl_sync(0xffffffffu, others, src);
-      const int l0 = at / p.batch * p.batch;
+    if (others > 0) {
+      const int b0 = row % p.batch;
       int n = 0, first = 0x7fffffff;
       for (int b = lane; b < p.batch; b += 32)
-        if (__ldcg(&p.last[l0 + b]) == q) {
+        if (__ldcg(&p.last[row - b0 + b]) == page) {
           ++n;
           first = min(first, b + (parent_of(p, b) == b ? 0 : p.batch));
         }
       n = __reduce_add_sync(0xffffffffu, n);
       first = __reduce_min_sync(0xffffffffu, first);
-      const int b = at - l0, key = b + (parent_of(p, b) == b ? 0 : p.batch);
-      if (lane == src) copy = !(n == n_others + 1 && key == first);
+      copy = !(n == others + 1 && (first == b0 || first == b0 + p.batch));
     }
+    if (lane == 0) p.rank[row] = copy ? 0 : -1;
+  }
+  __syncthreads();
+  int copies = 0;
+  for (int64_t base = row0; base < row1; base += kPlanThreads) {
+    const int row = (int)base + threadIdx.x;
+    const bool copy = row < row1 && p.rank[row] >= 0;
     int total;
     const int before = block_scan(copy ? 1 : 0, s_scan, &total);
-    if (row < row1) p.rank[row] = copy ? copies + before : -1;
+    if (copy) p.rank[row] = copies + before;
     copies += total;
   }
   const int n_words = (p.n_pages + 31) / 32;
@@ -311,72 +312,108 @@ __global__ void __launch_bounds__(kPlanThreads, 1) fork_kernel(const ForkParams 
   for (int64_t base = word0; base < word1; base += kPlanThreads) {
     const int64_t w = base + threadIdx.x;
     int total;
-    block_scan(w < word1 ? __popc(__ldcg(&p.gone[w])) : 0, s_scan, &total);
+    const int before = block_scan(w < word1 ? __popc(__ldcg(&p.gone[w])) : 0, s_scan, &total);
+    if (w < word1) p.word_at[w] = back + before;
     back += total;
   }
   if (threadIdx.x == 0) {
     p.counts[blockIdx.x] = copies;
     p.counts[kMaxCluster + blockIdx.x] = back;
   }
+  const int used = min(max(__ldcg(p.used), 0), p.n_free);
   phase();
-  // ---- pages for the copies, from the list as it was
+  // ---- pages for the copies, from the list as it was; lengths (read for the last time before the phases here)
   int copies_before = 0, back_before = 0, all_copies = 0, all_back = 0;
   for (int i = 0; i < (int)gridDim.x; ++i) {
     const int c = __ldcg(&p.counts[i]), r = __ldcg(&p.counts[kMaxCluster + i]);
     if (i < (int)blockIdx.x) copies_before += c, back_before += r;
     all_copies += c, all_back += r;
   }
-  const int used = min(max(__ldcg(p.used), 0), p.n_free);
   for (int64_t base = row0; base < row1; base += kPlanThreads) {
     const int row = (int)base + threadIdx.x;
     if (row >= row1) continue;
-    const ForkRow r = fork_row(p, row / p.batch, row % p.batch);
+    const ForkRow r = row_at(row);
     const int rank = p.rank[row];
-    if (rank < 0) continue;
-    const int i = copies_before + rank, page = p.last[row];
-    const int to = i < p.n_free - used ? __ldcg(&p.free_pages[used + i]) : -1;
-    atomicSub(&p.shares[page], 1);
-    RowCopy c = {page, to, r.rows % p.page_size};
-    if (in_pool(p, to)) {
-      p.table[(size_t)row * p.cols + r.need - 1] = to;
-    } else {                          // no page: only whole pages stay (see below)
-      record_status(p.hdr, i < p.n_free - used ? XKV_ERR_INVALID_ARG : XKV_ERR_CAPACITY);
-      c = {0, 0, 0};
-      p.rank[row] = -2;
+    int rows = r.rows;
+    if (rank >= 0) {
+      const int i = copies_before + rank, page = p.last[row];
+      const int to = i < p.n_free - used ? __ldcg(&p.free_pages[used + i]) : -1;
+      atomicSub(&p.shares[page], 1);
+      RowCopy c = {page, to, r.rows % p.page_size};
+      if (in_pool(p, to)) {
+        p.table[(size_t)row * p.cols + r.need - 1] = to;
+      } else {                        // no page: only whole pages stay
+        record_status(p.hdr, i < p.n_free - used ? XKV_ERR_INVALID_ARG : XKV_ERR_CAPACITY);
+        c = {0, 0, 0};
+        rows -= rows % p.page_size;
+      }
+      p.list[i] = c;
     }
-    p.list[i] = c;
+    p.lens[row] = rows;
   }
   phase();
-  // ---- lengths, and pages back to the list in ascending order
-  for (int row = blockIdx.x * kPlanThreads + threadIdx.x; row < n_rows; row += gridDim.x * kPlanThreads) {
-    // (a cache's own length is read by its forks above)
-    const ForkRow r = fork_row(p, row / p.batch, row % p.batch);
-    p.last[row] = __ldcg(&p.rank[row]) == -2 ? r.rows / p.page_size * p.page_size : r.rows;
-  }
+  // ---- pages back to the list, in ascending order
   const int taken = min(all_copies, p.n_free - used);
   const int top = used + taken - all_back;
-  back = back_before;
-  for (int64_t base = word0; base < word1; base += kPlanThreads) {
-    const int64_t w = base + threadIdx.x;
-    uint32_t bits = w < word1 ? __ldcg(&p.gone[w]) : 0u;
-    int total;
-    int at = top + back + block_scan(__popc(bits), s_scan, &total);
-    if (bits != 0) p.gone[w] = 0u;
-    for (; bits != 0; bits &= bits - 1, ++at) {
+  for (int64_t w = word0 + threadIdx.x; w < word1; w += kPlanThreads) {
+    uint32_t bits = __ldcg(&p.gone[w]);
+    if (bits == 0) continue;
+    p.gone[w] = 0u;
+    for (int at = top + back_before + p.word_at[w]; bits != 0; bits &= bits - 1, ++at) {
       const int page = (int)w * 32 + __ffs(bits) - 1;
       p.shares[page] = 0;
       if (at >= 0) p.free_pages[at] = page;
     }
-    back += total;
   }
   if (blockIdx.x == 0 && threadIdx.x == 0) {
     if (top < 0) record_status(p.hdr, XKV_ERR_INVALID_ARG);    // more came back than were handed out
     *p.used = max(top, 0);
     *p.n_copies = all_copies;
   }
+}
+
+// All of a step in one cluster; what becomes of a CTA's caches stays in its shared memory.
+constexpr int kClusterRows = 1024;    // a CTA
+__global__ void __launch_bounds__(kPlanThreads, 1) fork_kernel(const ForkParams p) {
+  asm volatile("griddepcontrol.wait;" ::: "memory");
+  asm volatile("griddepcontrol.launch_dependents;");
+  __shared__ int s_scan[kPlanWarps + 1];
+  __shared__ int4 s_rows[kClusterRows];
+  int64_t row0, row1;
+  cta_run(p.n_rows, &row0, &row1);
+  const int n = (int)(row1 - row0), warp = threadIdx.x >> 5;
+  for (int i = threadIdx.x; i < n; i += kPlanThreads) s_rows[i] = fork_row(p, (int)row0 + i);
+  __syncthreads();
+  for (int i = warp; i < n; i += kPlanWarps) count_new(p, (int)row0 + i, as_row(s_rows[i]));
   phase();
-  for (int row = blockIdx.x * kPlanThreads + threadIdx.x; row < n_rows; row += gridDim.x * kPlanThreads)
-    p.lens[row] = __ldcg(&p.last[row]);
+  for (int i = warp; i < n; i += kPlanWarps) drop_old(p, (int)row0 + i, as_row(s_rows[i]));
+  phase();
+  fork_decide(p, s_scan, [&](int row) { return as_row(s_rows[row - row0]); });
+}
+
+// The same in three launches, whose first two take all SMs.
+__global__ void __launch_bounds__(kCopyThreads) fork_count_kernel(const ForkParams p) {
+  asm volatile("griddepcontrol.wait;" ::: "memory");
+  asm volatile("griddepcontrol.launch_dependents;");
+  const int n_warps = gridDim.x * (kCopyThreads / 32);
+  for (int row = blockIdx.x * (kCopyThreads / 32) + (threadIdx.x >> 5); row < p.n_rows; row += n_warps) {
+    const int4 r = fork_row(p, row);
+    if ((threadIdx.x & 31) == 0) p.rows[row] = r;
+    count_new(p, row, as_row(r));
+  }
+}
+__global__ void __launch_bounds__(kCopyThreads) fork_drop_kernel(const ForkParams p) {
+  asm volatile("griddepcontrol.wait;" ::: "memory");
+  asm volatile("griddepcontrol.launch_dependents;");
+  const int n_warps = gridDim.x * (kCopyThreads / 32);
+  for (int row = blockIdx.x * (kCopyThreads / 32) + (threadIdx.x >> 5); row < p.n_rows; row += n_warps)
+    drop_old(p, row, as_row(__ldcg(&p.rows[row])));
+}
+__global__ void __launch_bounds__(kPlanThreads, 1) fork_decide_kernel(const ForkParams p) {
+  asm volatile("griddepcontrol.wait;" ::: "memory");
+  asm volatile("griddepcontrol.launch_dependents;");
+  __shared__ int s_scan[kPlanWarps + 1];
+  fork_decide(p, s_scan, [&](int row) { return as_row(__ldcg(&p.rows[row])); });
 }
 
 // ---------------------------------------------------------------------------------------------
@@ -390,23 +427,49 @@ struct CompactParams {
   int32_t* shares;
   int32_t* free_pages;
   int32_t* used;
-  int32_t n_layers, batch, cols, page_size, n_pages;
+  int32_t n_rows, cols, page_size, n_pages;           // n_rows: caches, L * B
   WorkspaceHeader* hdr;
-  int32_t* n_live;
+  int32_t* n_live;                    // pages in use, and those of them from n_live on
   int32_t* n_moved;
-  int32_t* counts;                    // [3][kMaxCluster] pages in use, gaps, pages that move, of the CTAs
+  int32_t* counts;                    // [kMaxCluster] pages in use of the CTAs' words
   uint32_t* live;                     // a bit a page: in use; zero between calls
+  int32_t* word_at;                   // pages in use before each of its words
   RowCopy* list;                      // [n_pages] src and dst of the pages that move, in ascending order
   int32_t* place;                     // [n_pages] of a page that moves: its place in the list
 };
 
+// Pages that cache `row` holds.
+__device__ __forceinline__ int held(const CompactParams& p, int64_t row) {
+  return (min(max(__ldg(&p.lens[row]), 0), p.cols * p.page_size) + p.page_size - 1) / p.page_size;
+}
+
+// A thread: where page `page` goes.  bits: its word of `live`, at: pages in use before that word, low: pages in use below n_live.
+__device__ __forceinline__ void place_page(const CompactParams& p, int page, uint32_t bits, int at, int n_live, int low) {
+  const bool in_use = (bits >> (page & 31)) & 1u;
+  const int rank = at + __popc(bits & ((1u << (page & 31)) - 1u));        // pages in use below it
+  if (page < n_live) {
+    if (!in_use) p.list[page - rank].dst = page;
+    else if (p.shares != nullptr) p.shares[page] = p.shares_before[page];
+  } else if (in_use) {
+    p.list[rank - low].src = page;
+    p.list[rank - low].rows = p.page_size;
+    p.place[page] = rank - low;
+  } else if (p.shares != nullptr) {
+    p.shares[page] = 0;
+  }
+}
+
+// Which pages are in use, how many before each word of the map; and, unless that is left to the next launch (kPlace false), where the
+// pages go.
+template <bool kPlace>
 __global__ void __launch_bounds__(kPlanThreads, 1) compact_kernel(const CompactParams p) {
+  asm volatile("griddepcontrol.wait;" ::: "memory");
   asm volatile("griddepcontrol.launch_dependents;");
   __shared__ int s_scan[kPlanWarps + 1];
-  const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5;
-  const int n_rows = p.n_layers * p.batch, n_warps = gridDim.x * kPlanWarps;
-  for (int row = blockIdx.x * kPlanWarps + warp; row < n_rows; row += n_warps) {
-    const int have = (min(max(__ldg(&p.lens[row]), 0), p.cols * p.page_size) + p.page_size - 1) / p.page_size;
+  const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5, n_warps = gridDim.x * kPlanWarps;
+  for (int row = blockIdx.x * kPlanWarps + warp; row < p.n_rows; row += n_warps) {
+    const int have = held(p, row);
+#pragma unroll 4
     for (int i = lane; i < have; i += 32) {
       const int e = p.before[(size_t)row * p.cols + i];
       if (e >= 0 && e < p.n_pages) atomicOr(&p.live[e >> 5], 1u << (e & 31));
@@ -421,70 +484,49 @@ __global__ void __launch_bounds__(kPlanThreads, 1) compact_kernel(const CompactP
   for (int64_t base = word0; base < word1; base += kPlanThreads) {
     const int64_t w = base + threadIdx.x;
     int total;
-    block_scan(w < word1 ? __popc(__ldcg(&p.live[w])) : 0, s_scan, &total);
+    const int before = block_scan(w < word1 ? __popc(__ldcg(&p.live[w])) : 0, s_scan, &total);
+    if (w < word1) p.word_at[w] = mine + before;
     mine += total;
   }
   if (threadIdx.x == 0) p.counts[blockIdx.x] = mine;
   phase();
-  int n_live = 0;
-  for (int i = 0; i < (int)gridDim.x; ++i) n_live += __ldcg(&p.counts[i]);
-  // bits of word w below and from n_live on
-  auto below = [&](int64_t w) -> uint32_t {
-    const int64_t at = (int64_t)n_live - w * 32;
-    return at >= 32 ? 0xffffffffu : (at <= 0 ? 0u : (1u << at) - 1u);
-  };
-  int gaps = 0, moved = 0;
-  for (int64_t base = word0; base < word1; base += kPlanThreads) {
-    const int64_t w = base + threadIdx.x;
-    const uint32_t bits = w < word1 ? __ldcg(&p.live[w]) : 0u, low = w < word1 ? below(w) : 0u;
-    int t0, t1;
-    block_scan(__popc(~bits & low), s_scan, &t0);
-    block_scan(__popc(bits & ~low), s_scan, &t1);
-    gaps += t0;
-    moved += t1;
+  int n_live = 0, before = 0;
+  for (int i = 0; i < (int)gridDim.x; ++i) {
+    const int n = __ldcg(&p.counts[i]);
+    if (i < (int)blockIdx.x) before += n;
+    n_live += n;
   }
-  if (threadIdx.x == 0) {
-    p.counts[kMaxCluster + blockIdx.x] = gaps;
-    p.counts[2 * kMaxCluster + blockIdx.x] = moved;
+  if (gridDim.x > 1) {
+    for (int64_t w = word0 + threadIdx.x; w < word1; w += kPlanThreads) p.word_at[w] += before;
+    phase();
   }
-  phase();
-  gaps = moved = 0;
-  for (int i = 0; i < (int)blockIdx.x; ++i) {
-    gaps += __ldcg(&p.counts[kMaxCluster + i]);
-    moved += __ldcg(&p.counts[2 * kMaxCluster + i]);
-  }
-  for (int64_t base = word0; base < word1; base += kPlanThreads) {
-    const int64_t w = base + threadIdx.x;
-    const uint32_t bits = w < word1 ? __ldcg(&p.live[w]) : 0u, low = w < word1 ? below(w) : 0u;
-    int t0, t1;
-    int gap = gaps + block_scan(__popc(~bits & low), s_scan, &t0), go = moved + block_scan(__popc(bits & ~low), s_scan, &t1);
-    gaps += t0;
-    moved += t1;
-    if (w < word1) {
-      p.live[w] = 0u;
-      const int n = (int)min((int64_t)32, p.n_pages - w * 32);
-      for (int i = 0; i < n; ++i) {
-        const int page = (int)w * 32 + i;
-        const bool in_use = (bits >> i) & 1u, in_front = (low >> i) & 1u;
-        if (in_front) {
-          if (!in_use) p.list[gap++].dst = page;
-          else if (p.shares != nullptr) p.shares[page] = p.shares_before[page];
-        } else if (in_use) {
-          p.list[go].src = page;
-          p.list[go].rows = p.page_size;
-          p.place[page] = go++;
-        } else if (p.shares != nullptr) {
-          p.shares[page] = 0;
-        }
-      }
-    }
-  }
+  int low = n_live;                   // pages in use below n_live
+  if ((n_live >> 5) < n_words)
+    low = __ldcg(&p.word_at[n_live >> 5]) + __popc(__ldcg(&p.live[n_live >> 5]) & ((1u << (n_live & 31)) - 1u));
   if (blockIdx.x == 0 && threadIdx.x == 0) {
-    int all = 0;
-    for (int i = 0; i < (int)gridDim.x; ++i) all += __ldcg(&p.counts[2 * kMaxCluster + i]);
     *p.n_live = n_live;
-    *p.n_moved = all;
+    *p.n_moved = n_live - low;
     *p.used = n_live;
+  }
+  if constexpr (kPlace) {
+    for (int page = blockIdx.x * kPlanThreads + threadIdx.x; page < p.n_pages; page += gridDim.x * kPlanThreads)
+      place_page(p, page, __ldcg(&p.live[page >> 5]), __ldcg(&p.word_at[page >> 5]), n_live, low);
+    phase();
+    for (int64_t w = word0 + threadIdx.x; w < word1; w += kPlanThreads) p.live[w] = 0u;
+  }
+}
+
+// Where the pages of a large pool go.
+__global__ void __launch_bounds__(kCopyThreads) compact_place_kernel(const CompactParams p) {
+  asm volatile("griddepcontrol.wait;" ::: "memory");
+  asm volatile("griddepcontrol.launch_dependents;");
+  const int n_live = __ldcg(p.n_live), low = n_live - __ldcg(p.n_moved);
+  const int64_t step = (int64_t)gridDim.x * kCopyThreads;
+  for (int64_t page = (int64_t)blockIdx.x * kCopyThreads + threadIdx.x; page < (p.n_pages + 31) / 32 * 32ll; page += step) {
+    const uint32_t bits = __ldcg(&p.live[page >> 5]);
+    if (page < p.n_pages) place_page(p, (int)page, bits, __ldcg(&p.word_at[page >> 5]), n_live, low);
+    __syncwarp();                     // a word's 32 pages are a warp's
+    if ((page & 31) == 0) p.live[page >> 5] = 0u;
   }
 }
 
@@ -493,14 +535,13 @@ __global__ void __launch_bounds__(kCopyThreads) compact_move_kernel(const Compac
   asm volatile("griddepcontrol.wait;" ::: "memory");
   const int n_live = __ldcg(p.n_live), n_moved = __ldcg(p.n_moved);
   const int64_t tid = (int64_t)blockIdx.x * kCopyThreads + threadIdx.x, step = (int64_t)gridDim.x * kCopyThreads;
-  const int64_t n_entries = (int64_t)p.n_layers * p.batch * p.cols;
+  const int64_t n_entries = (int64_t)p.n_rows * p.cols;
   for (int64_t i = tid; i < n_entries; i += step) {
-    const int64_t row = i / p.cols;
     const int e = p.before[i];
     int now = e;
     if (e >= n_live && e < p.n_pages) {
-      const int have = (min(max(__ldg(&p.lens[row]), 0), p.cols * p.page_size) + p.page_size - 1) / p.page_size;
-      if (i - row * p.cols < have) now = __ldcg(&p.list[__ldcg(&p.place[e])].dst);
+      const int64_t row = i / p.cols;
+      if (i - row * p.cols < held(p, row)) now = __ldcg(&p.list[__ldcg(&p.place[e])].dst);
     }
     p.table[i] = now;
   }
@@ -508,22 +549,20 @@ __global__ void __launch_bounds__(kCopyThreads) compact_move_kernel(const Compac
     for (int64_t i = n_live + tid; i < p.n_pages; i += step) p.free_pages[i] = (int)i;
   if (p.shares != nullptr)
     for (int64_t i = tid; i < n_moved; i += step) {
-      const int src = __ldcg(&p.list[i].src), held = p.shares_before[src];
+      const int src = __ldcg(&p.list[i].src), others = p.shares_before[src];
       p.shares[src] = 0;
-      p.shares[__ldcg(&p.list[i].dst)] = held;
+      p.shares[__ldcg(&p.list[i].dst)] = others;
     }
-  const int64_t per = 2 * (int64_t)c.n_kv_heads * c.pieces, n = n_moved * per;
-  for (int64_t u = tid >> 5; u < n; u += step >> 5) {
-    const RowCopy x = {__ldcg(&p.list[u / per].src), __ldcg(&p.list[u / per].dst), c.page_size};
-    copy_piece(c, x, (int)(u % per));
-  }
+  each_head(c, n_moved, true, [&](int64_t i, int part, int piece, int n) {
+    copy_head(c, {__ldcg(&p.list[i].src), __ldcg(&p.list[i].dst), c.page_size}, part, piece, n);
+  });
 }
 
 // ---------------------------------------------------------------------------------------------
 // Host side
 // ---------------------------------------------------------------------------------------------
 struct Layout {
-  size_t counts, list, a, b, bits, fresh, total;
+  size_t counts, list, a, b, rows, bits, words, fresh, total;
 };
 
 Layout fork_layout(int64_t n_rows, int cols, int64_t n_pages) {
@@ -531,9 +570,11 @@ Layout fork_layout(int64_t n_rows, int cols, int64_t n_pages) {
   size_t off = kHeaderBytes;
   L.counts = off; off = align_up(off + (8 + 2 * kMaxCluster) * 4, 256);
   L.bits = off;   off = align_up(off + (size_t)(n_pages + 31) / 32 * 4, 256);
+  L.words = off;  off = align_up(off + (size_t)(n_pages + 31) / 32 * 4, 256);
   L.list = off;   off = align_up(off + (size_t)n_rows * sizeof(RowCopy), 256);
   L.a = off;      off = align_up(off + (size_t)n_rows * 4, 256);
   L.b = off;      off = align_up(off + (size_t)n_rows * 4, 256);
+  L.rows = off;   off = align_up(off + (size_t)n_rows * sizeof(int4), 256);
   L.fresh = off;  off = align_up(off + (size_t)n_rows * cols * 4, 256);
   L.total = off;
   return L;
@@ -542,45 +583,30 @@ Layout fork_layout(int64_t n_rows, int cols, int64_t n_pages) {
 Layout compact_layout(int64_t n_pages) {
   Layout L = {};
   size_t off = kHeaderBytes;
-  L.counts = off; off = align_up(off + (8 + 3 * kMaxCluster) * 4, 256);
+  L.counts = off; off = align_up(off + (8 + kMaxCluster) * 4, 256);
   L.bits = off;   off = align_up(off + (size_t)(n_pages + 31) / 32 * 4, 256);
+  L.words = off;  off = align_up(off + (size_t)(n_pages + 31) / 32 * 4, 256);
   L.list = off;   off = align_up(off + (size_t)n_pages * sizeof(RowCopy), 256);
   L.a = off;      off = align_up(off + (size_t)n_pages * 4, 256);
   L.total = off;
   return L;
 }
 
-template <typename P>
-xkv_status launch_cluster(void (*kernel)(P), const P& p, int ctas, cudaStream_t st) {
-  cudaLaunchConfig_t cfg = {};
-  cfg.gridDim = dim3((unsigned)ctas);
-  cfg.blockDim = dim3(kPlanThreads);
-  cfg.stream = st;
-  cudaLaunchAttribute attr;
-  attr.id = cudaLaunchAttributeClusterDimension;
-  attr.val.clusterDim.x = (unsigned)ctas;
-  attr.val.clusterDim.y = attr.val.clusterDim.z = 1;
-  cfg.attrs = &attr;
-  cfg.numAttrs = 1;
-  if (cudaLaunchKernelEx(&cfg, kernel, p) != cudaSuccess) {
-    (void)cudaGetLastError();
-    return XKV_ERR_CUDA;
-  }
-  count_launch();
-  return check_launch();
-}
-
+// All launches here wait for the one before them on the device, so that their CTAs may be in place when it ends.
 template <typename... Args>
-xkv_status launch_after(void (*kernel)(Args...), int grid, cudaStream_t st, Args... args) {
+xkv_status launch_after(void (*kernel)(Args...), int grid, int threads, bool cluster, cudaStream_t st, Args... args) {
   cudaLaunchConfig_t cfg = {};
   cfg.gridDim = dim3((unsigned)grid);
-  cfg.blockDim = dim3(kCopyThreads);
+  cfg.blockDim = dim3((unsigned)threads);
   cfg.stream = st;
-  cudaLaunchAttribute attr;           // its CTAs are in place when the plan ends
-  attr.id = cudaLaunchAttributeProgrammaticStreamSerialization;
-  attr.val.programmaticStreamSerializationAllowed = 1;
-  cfg.attrs = &attr;
-  cfg.numAttrs = 1;
+  cudaLaunchAttribute attr[2];
+  attr[0].id = cudaLaunchAttributeProgrammaticStreamSerialization;
+  attr[0].val.programmaticStreamSerializationAllowed = 1;
+  attr[1].id = cudaLaunchAttributeClusterDimension;
+  attr[1].val.clusterDim.x = (unsigned)grid;
+  attr[1].val.clusterDim.y = attr[1].val.clusterDim.z = 1;
+  cfg.attrs = attr;
+  cfg.numAttrs = cluster ? 2 : 1;
   if (cudaLaunchKernelEx(&cfg, kernel, args...) != cudaSuccess) {
     (void)cudaGetLastError();
     return XKV_ERR_CUDA;
@@ -591,6 +617,10 @@ xkv_status launch_after(void (*kernel)(Args...), int grid, cudaStream_t st, Args
 
 // CTAs of a plan: one (whose barriers are cheapest) for a few hundred caches of short tables, else a cluster.
 int plan_ctas(int64_t n_rows, int cols) { return n_rows * ((cols + 31) / 32) <= 2 * kPlanWarps ? 1 : kMaxCluster; }
+// Table entries from which on a step's forks take all SMs.
+constexpr int64_t kManyEntries = 16384;
+// Pages of a pool from which on all SMs find their places.
+constexpr int kManyPages = 32768;
 
 }  // namespace
 
@@ -616,7 +646,7 @@ xkv_status fork_caches(const xkv_dims* d, const xkv_cache* c, const int32_t* par
   p.free_pages = free_pages;
   p.n_free = n_free;
   p.used = pages_used;
-  p.n_layers = c->n_layers;
+  p.n_rows = (int32_t)n_rows;
   p.batch = d->batch;
   p.cols = c->max_pages_per_seq;
   p.page_size = c->page_size;
@@ -627,12 +657,23 @@ xkv_status fork_caches(const xkv_dims* d, const xkv_cache* c, const int32_t* par
   p.list = reinterpret_cast<RowCopy*>(ws + L.list);
   p.last = reinterpret_cast<int32_t*>(ws + L.a);
   p.rank = reinterpret_cast<int32_t*>(ws + L.b);
+  p.rows = reinterpret_cast<int4*>(ws + L.rows);
   p.gone = reinterpret_cast<uint32_t*>(ws + L.bits);
+  p.word_at = reinterpret_cast<int32_t*>(ws + L.words);
   p.fresh = reinterpret_cast<int32_t*>(ws + L.fresh);
-  xkv_status s = launch_cluster(fork_kernel, p, plan_ctas(n_rows, p.cols), st);
+  xkv_status s;
+  if (n_rows * p.cols <= kManyEntries && n_rows <= kClusterRows) {
+    s = launch_after(fork_kernel, plan_ctas(n_rows, p.cols), kPlanThreads, true, st, p);
+  } else {
+    const int grid = (int)std::min<int64_t>((n_rows + kCopyThreads / 32 - 1) / (kCopyThreads / 32), 8 * (int64_t)sm_count());
+    s = launch_after(fork_count_kernel, grid, kCopyThreads, false, st, p);
+    if (s == XKV_OK) s = launch_after(fork_drop_kernel, grid, kCopyThreads, false, st, p);
+    if (s == XKV_OK) s = launch_after(fork_decide_kernel, kMaxCluster, kPlanThreads, true, st, p);
+  }
   if (s != XKV_OK) return s;
   const CopyParams cp = copy_params(d, c, c);
-  return launch_after(copy_rows_kernel, copy_grid(cp, n_rows), st, cp, (const RowCopy*)p.list, (const int32_t*)p.n_copies);
+  return launch_after(copy_rows_kernel, copy_grid(cp, n_rows, false), kCopyThreads, false, st, cp, (const RowCopy*)p.list,
+                      (const int32_t*)p.n_copies);
 }
 
 xkv_status compact_pages(const xkv_dims* d, const xkv_cache* c, const int32_t* table_before, const int32_t* shares_before,
@@ -648,8 +689,7 @@ xkv_status compact_pages(const xkv_dims* d, const xkv_cache* c, const int32_t* t
   p.shares = shares;
   p.free_pages = free_pages;
   p.used = pages_used;
-  p.n_layers = c->n_layers;
-  p.batch = d->batch;
+  p.n_rows = (int32_t)n_rows;
   p.cols = c->max_pages_per_seq;
   p.page_size = c->page_size;
   p.n_pages = c->n_pages;
@@ -658,21 +698,30 @@ xkv_status compact_pages(const xkv_dims* d, const xkv_cache* c, const int32_t* t
   p.n_moved = p.n_live + 1;
   p.counts = p.n_live + 8;
   p.live = reinterpret_cast<uint32_t*>(ws + L.bits);
+  p.word_at = reinterpret_cast<int32_t*>(ws + L.words);
   p.list = reinterpret_cast<RowCopy*>(ws + L.list);
   p.place = reinterpret_cast<int32_t*>(ws + L.a);
-  xkv_status s = launch_cluster(compact_kernel, p, plan_ctas(n_rows, p.cols), st);
+  xkv_status s;
+  if (p.n_pages <= kManyPages) {
+    s = launch_after(compact_kernel<true>, plan_ctas(n_rows, p.cols), kPlanThreads, true, st, p);
+  } else {
+    s = launch_after(compact_kernel<false>, kMaxCluster, kPlanThreads, true, st, p);
+    const int64_t ctas = (p.n_pages + kCopyThreads - 1) / kCopyThreads;
+    if (s == XKV_OK)
+      s = launch_after(compact_place_kernel, (int)std::min<int64_t>(ctas, 8 * (int64_t)sm_count()), kCopyThreads, false, st, p);
+  }
   if (s != XKV_OK) return s;
   const CopyParams cp = copy_params(d, c, c);
   const int64_t entries = (n_rows * p.cols + 31) / 32;
-  const int grid = std::max(copy_grid(cp, std::min<int64_t>(c->n_pages, n_rows * p.cols)),
+  const int grid = std::max(copy_grid(cp, std::min<int64_t>(c->n_pages, n_rows * p.cols), true),
                             (int)std::min<int64_t>(entries / (kCopyThreads / 32), sm_count()));
-  return launch_after(compact_move_kernel, grid, st, p, cp);
+  return launch_after(compact_move_kernel, grid, kCopyThreads, false, st, p, cp);
 }
 
 xkv_status copy_pages(const xkv_dims* d, const xkv_cache* from, const int32_t* src, const xkv_cache* to, const int32_t* dst,
                       int64_t n_copies, void* workspace, cudaStream_t st) {
   const CopyParams p = copy_params(d, from, to);
-  copy_pages_kernel<<<copy_grid(p, n_copies), kCopyThreads, 0, st>>>(p, src, dst, n_copies, from->n_pages, to->n_pages,
+  copy_pages_kernel<<<copy_grid(p, n_copies, true), kCopyThreads, 0, st>>>(p, src, dst, n_copies, from->n_pages, to->n_pages,
                                                                      static_cast<WorkspaceHeader*>(workspace));
   count_launch();
   return check_launch();
