@@ -80,8 +80,8 @@ __device__ __forceinline__ void copy_head(const CopyParams& p, const RowCopy& c,
 template <typename F>
 __device__ __forceinline__ void each_head(const CopyParams& p, int64_t n, bool whole, F f) {
   const int step = whole ? p.pieces : 1, per = 2 * p.n_kv_heads * step;
-  const int64_t warp = (int64_t)blockIdx.x * (kCopyThreads / 32) + (threadIdx.x >> 5);
-  const int64_t n_warps = (int64_t)gridDim.x * (kCopyThreads / 32), end = n * per;
+  const int64_t warp = (int64_t)blockIdx.x * (blockDim.x >> 5) + (threadIdx.x >> 5);
+  const int64_t n_warps = (int64_t)gridDim.x * (blockDim.x >> 5), end = n * per;
   if (end <= 0x7fffffffll - n_warps) {
     for (int u = (int)warp; u < (int)end; u += (int)n_warps) {
       const int c = u / per, rest = u - c * per;
@@ -93,11 +93,14 @@ __device__ __forceinline__ void each_head(const CopyParams& p, int64_t n, bool w
 }
 
 // The list that a plan has made: entries and their number in the workspace.
-__global__ void __launch_bounds__(kCopyThreads) copy_rows_kernel(const CopyParams p, const RowCopy* list, const int32_t* n_list) {
-  asm volatile("griddepcontrol.wait;" ::: "memory");
-  each_head(p, __ldcg(n_list), false, [&](int64_t i, int part, int piece, int step) {
+__device__ __forceinline__ void copy_rows(const CopyParams& p, const RowCopy* list, int n) {
+  each_head(p, n, false, [&](int64_t i, int part, int piece, int step) {
     copy_head(p, {__ldcg(&list[i].src), __ldcg(&list[i].dst), __ldcg(&list[i].rows)}, part, piece, step);
   });
+}
+__global__ void __launch_bounds__(kCopyThreads) copy_rows_kernel(const CopyParams p, const RowCopy* list, const int32_t* n_list) {
+  asm volatile("griddepcontrol.wait;" ::: "memory");
+  copy_rows(p, list, __ldcg(n_list));
 }
 
 // Page ids that a caller gives.
@@ -372,9 +375,10 @@ __device__ __forceinline__ void fork_decide(const ForkParams& p, int* s_scan, Ro
   }
 }
 
-// All of a step in one cluster; what becomes of a CTA's caches stays in its shared memory.
+// All of a step in one cluster; what becomes of a CTA's caches stays in its shared memory.  kCopy: the rows are copied here, too.
 constexpr int kClusterRows = 1024;    // a CTA
-__global__ void __launch_bounds__(kPlanThreads, 1) fork_kernel(const ForkParams p) {
+template <bool kCopy>
+__global__ void __launch_bounds__(kPlanThreads, 1) fork_kernel(const ForkParams p, const CopyParams c) {
   asm volatile("griddepcontrol.wait;" ::: "memory");
   asm volatile("griddepcontrol.launch_dependents;");
   __shared__ int s_scan[kPlanWarps + 1];
@@ -389,6 +393,10 @@ __global__ void __launch_bounds__(kPlanThreads, 1) fork_kernel(const ForkParams 
   for (int i = warp; i < n; i += kPlanWarps) drop_old(p, (int)row0 + i, as_row(s_rows[i]));
   phase();
   fork_decide(p, s_scan, [&](int row) { return as_row(s_rows[row - row0]); });
+  if constexpr (kCopy) {
+    phase();
+    copy_rows(c, p.list, __ldcg(p.n_copies));
+  }
 }
 
 // The same in three launches, whose first two take all SMs.
@@ -459,10 +467,75 @@ __device__ __forceinline__ void place_page(const CompactParams& p, int page, uin
   }
 }
 
-// Which pages are in use, how many before each word of the map; and, unless that is left to the next launch (kPlace false), where the
-// pages go.
-template <bool kPlace>
-__global__ void __launch_bounds__(kPlanThreads, 1) compact_kernel(const CompactParams p) {
+// Tables, counters of the pages that move, the list; then the pages.
+__device__ __forceinline__ void compact_move(const CompactParams& p, const CopyParams& c, int n_live, int n_moved) {
+  const int64_t tid = (int64_t)blockIdx.x * blockDim.x + threadIdx.x, step = (int64_t)gridDim.x * blockDim.x;
+  const int64_t n_entries = (int64_t)p.n_rows * p.cols;
+  for (int64_t i = tid; i < n_entries; i += step) {
+    const int e = p.before[i];
+    int now = e;
+    if (e >= n_live && e < p.n_pages) {
+      const int64_t row = i / p.cols;
+      if (i - row * p.cols < held(p, row)) now = __ldcg(&p.list[__ldcg(&p.place[e])].dst);
+    }
+    p.table[i] = now;
+  }
+  if (p.free_pages != nullptr)
+    for (int64_t i = n_live + tid; i < p.n_pages; i += step) p.free_pages[i] = (int)i;
+  if (p.shares != nullptr)
+    for (int64_t i = tid; i < n_moved; i += step) {
+      const int src = __ldcg(&p.list[i].src), others = p.shares_before[src];
+      p.shares[src] = 0;
+      p.shares[__ldcg(&p.list[i].dst)] = others;
+    }
+  each_head(c, n_moved, true, [&](int64_t i, int part, int piece, int n) {
+    copy_head(c, {__ldcg(&p.list[i].src), __ldcg(&p.list[i].dst), c.page_size}, part, piece, n);
+  });
+}
+
+// Pools of up to kSmallWords words of a bit a page: every CTA of the cluster finds all pages in use for itself, in its shared memory,
+// and places its share of them.  kMove: the move, too.
+constexpr int kSmallWords = kPlanThreads;
+template <bool kMove>
+__global__ void __launch_bounds__(kPlanThreads, 1) compact_small_kernel(const CompactParams p, const CopyParams c) {
+  asm volatile("griddepcontrol.wait;" ::: "memory");
+  asm volatile("griddepcontrol.launch_dependents;");
+  __shared__ int s_scan[kPlanWarps + 1];
+  __shared__ uint32_t s_live[kSmallWords];
+  __shared__ int s_at[kSmallWords];
+  const int tid = threadIdx.x, lane = tid & 31, warp = tid >> 5, n_words = (p.n_pages + 31) / 32;
+  s_live[tid] = 0u;
+  __syncthreads();
+  for (int row = warp; row < p.n_rows; row += kPlanWarps) {
+    const int have = held(p, row);
+#pragma unroll 4
+    for (int i = lane; i < have; i += 32) {
+      const int e = p.before[(size_t)row * p.cols + i];
+      if (e >= 0 && e < p.n_pages) atomicOr(&s_live[e >> 5], 1u << (e & 31));
+      else record_status(p.hdr, XKV_ERR_INVALID_ARG);
+    }
+  }
+  __syncthreads();
+  int n_live;
+  s_at[tid] = block_scan(__popc(s_live[tid]), s_scan, &n_live);
+  __syncthreads();
+  int low = n_live;                   // pages in use below n_live
+  if ((n_live >> 5) < n_words) low = s_at[n_live >> 5] + __popc(s_live[n_live >> 5] & ((1u << (n_live & 31)) - 1u));
+  for (int page = blockIdx.x * kPlanThreads + tid; page < p.n_pages; page += gridDim.x * kPlanThreads)
+    place_page(p, page, s_live[page >> 5], s_at[page >> 5], n_live, low);
+  if (blockIdx.x == 0 && tid == 0) {
+    *p.n_live = n_live;
+    *p.n_moved = n_live - low;
+    *p.used = n_live;
+  }
+  if constexpr (kMove) {
+    phase();                          // (also: every CTA has read the tables)
+    compact_move(p, c, n_live, n_live - low);
+  }
+}
+
+// The same for any pool, by a map in the workspace: which pages are in use, how many before each of its words.
+__global__ void __launch_bounds__(kPlanThreads, 1) compact_count_kernel(const CompactParams p) {
   asm volatile("griddepcontrol.wait;" ::: "memory");
   asm volatile("griddepcontrol.launch_dependents;");
   __shared__ int s_scan[kPlanWarps + 1];
@@ -496,27 +569,19 @@ __global__ void __launch_bounds__(kPlanThreads, 1) compact_kernel(const CompactP
     if (i < (int)blockIdx.x) before += n;
     n_live += n;
   }
-  if (gridDim.x > 1) {
-    for (int64_t w = word0 + threadIdx.x; w < word1; w += kPlanThreads) p.word_at[w] += before;
-    phase();
-  }
-  int low = n_live;                   // pages in use below n_live
-  if ((n_live >> 5) < n_words)
-    low = __ldcg(&p.word_at[n_live >> 5]) + __popc(__ldcg(&p.live[n_live >> 5]) & ((1u << (n_live & 31)) - 1u));
+  for (int64_t w = word0 + threadIdx.x; w < word1; w += kPlanThreads) p.word_at[w] += before;
+  phase();
   if (blockIdx.x == 0 && threadIdx.x == 0) {
+    int low = n_live;                 // pages in use below n_live
+    if ((n_live >> 5) < n_words)
+      low = __ldcg(&p.word_at[n_live >> 5]) + __popc(__ldcg(&p.live[n_live >> 5]) & ((1u << (n_live & 31)) - 1u));
     *p.n_live = n_live;
     *p.n_moved = n_live - low;
     *p.used = n_live;
   }
-  if constexpr (kPlace) {
-    for (int page = blockIdx.x * kPlanThreads + threadIdx.x; page < p.n_pages; page += gridDim.x * kPlanThreads)
-      place_page(p, page, __ldcg(&p.live[page >> 5]), __ldcg(&p.word_at[page >> 5]), n_live, low);
-    phase();
-    for (int64_t w = word0 + threadIdx.x; w < word1; w += kPlanThreads) p.live[w] = 0u;
-  }
 }
 
-// Where the pages of a large pool go.
+// Where its pages go.
 __global__ void __launch_bounds__(kCopyThreads) compact_place_kernel(const CompactParams p) {
   asm volatile("griddepcontrol.wait;" ::: "memory");
   asm volatile("griddepcontrol.launch_dependents;");
@@ -530,32 +595,9 @@ __global__ void __launch_bounds__(kCopyThreads) compact_place_kernel(const Compa
   }
 }
 
-// Tables, counters of the pages that move, the list; then the pages.
 __global__ void __launch_bounds__(kCopyThreads) compact_move_kernel(const CompactParams p, const CopyParams c) {
   asm volatile("griddepcontrol.wait;" ::: "memory");
-  const int n_live = __ldcg(p.n_live), n_moved = __ldcg(p.n_moved);
-  const int64_t tid = (int64_t)blockIdx.x * kCopyThreads + threadIdx.x, step = (int64_t)gridDim.x * kCopyThreads;
-  const int64_t n_entries = (int64_t)p.n_rows * p.cols;
-  for (int64_t i = tid; i < n_entries; i += step) {
-    const int e = p.before[i];
-    int now = e;
-    if (e >= n_live && e < p.n_pages) {
-      const int64_t row = i / p.cols;
-      if (i - row * p.cols < held(p, row)) now = __ldcg(&p.list[__ldcg(&p.place[e])].dst);
-    }
-    p.table[i] = now;
-  }
-  if (p.free_pages != nullptr)
-    for (int64_t i = n_live + tid; i < p.n_pages; i += step) p.free_pages[i] = (int)i;
-  if (p.shares != nullptr)
-    for (int64_t i = tid; i < n_moved; i += step) {
-      const int src = __ldcg(&p.list[i].src), others = p.shares_before[src];
-      p.shares[src] = 0;
-      p.shares[__ldcg(&p.list[i].dst)] = others;
-    }
-  each_head(c, n_moved, true, [&](int64_t i, int part, int piece, int n) {
-    copy_head(c, {__ldcg(&p.list[i].src), __ldcg(&p.list[i].dst), c.page_size}, part, piece, n);
-  });
+  compact_move(p, c, __ldcg(p.n_live), __ldcg(p.n_moved));
 }
 
 // ---------------------------------------------------------------------------------------------
@@ -616,11 +658,14 @@ xkv_status launch_after(void (*kernel)(Args...), int grid, int threads, bool clu
 }
 
 // CTAs of a plan: one (whose barriers are cheapest) for a few hundred caches of short tables, else a cluster.
-int plan_ctas(int64_t n_rows, int cols) { return n_rows * ((cols + 31) / 32) <= 2 * kPlanWarps ? 1 : kMaxCluster; }
+int plan_ctas(int64_t n_rows, int cols) {
+  const int64_t steps = n_rows * ((cols + 31) / 32);         // of a warp
+  return steps <= 2 * kPlanWarps ? 1 : (steps <= 16 * kPlanWarps ? kMaxCluster / 2 : kMaxCluster);
+}
 // Table entries from which on a step's forks take all SMs.
 constexpr int64_t kManyEntries = 16384;
-// Pages of a pool from which on all SMs find their places.
-constexpr int kManyPages = 32768;
+// Bytes that a plan's cluster copies itself: a second launch takes the device 2 us and the host 4.
+constexpr int64_t kFewBytes = 2 << 20;
 
 }  // namespace
 
@@ -661,9 +706,14 @@ xkv_status fork_caches(const xkv_dims* d, const xkv_cache* c, const int32_t* par
   p.gone = reinterpret_cast<uint32_t*>(ws + L.bits);
   p.word_at = reinterpret_cast<int32_t*>(ws + L.words);
   p.fresh = reinterpret_cast<int32_t*>(ws + L.fresh);
+  const CopyParams cp = copy_params(d, c, c);
   xkv_status s;
   if (n_rows * p.cols <= kManyEntries && n_rows <= kClusterRows) {
-    s = launch_after(fork_kernel, plan_ctas(n_rows, p.cols), kPlanThreads, true, st, p);
+    const int ctas = plan_ctas(n_rows, p.cols);
+    // rows of every cache's last page at most
+    if (n_rows * 2 * cp.n_kv_heads * cp.page_size * cp.row_bytes <= kFewBytes)
+      return launch_after(fork_kernel<true>, ctas, kPlanThreads, true, st, p, cp);
+    s = launch_after(fork_kernel<false>, ctas, kPlanThreads, true, st, p, cp);
   } else {
     const int grid = (int)std::min<int64_t>((n_rows + kCopyThreads / 32 - 1) / (kCopyThreads / 32), 8 * (int64_t)sm_count());
     s = launch_after(fork_count_kernel, grid, kCopyThreads, false, st, p);
@@ -671,7 +721,6 @@ xkv_status fork_caches(const xkv_dims* d, const xkv_cache* c, const int32_t* par
     if (s == XKV_OK) s = launch_after(fork_decide_kernel, kMaxCluster, kPlanThreads, true, st, p);
   }
   if (s != XKV_OK) return s;
-  const CopyParams cp = copy_params(d, c, c);
   return launch_after(copy_rows_kernel, copy_grid(cp, n_rows, false), kCopyThreads, false, st, cp, (const RowCopy*)p.list,
                       (const int32_t*)p.n_copies);
 }
@@ -701,17 +750,19 @@ xkv_status compact_pages(const xkv_dims* d, const xkv_cache* c, const int32_t* t
   p.word_at = reinterpret_cast<int32_t*>(ws + L.words);
   p.list = reinterpret_cast<RowCopy*>(ws + L.list);
   p.place = reinterpret_cast<int32_t*>(ws + L.a);
+  const CopyParams cp = copy_params(d, c, c);
   xkv_status s;
-  if (p.n_pages <= kManyPages) {
-    s = launch_after(compact_kernel<true>, plan_ctas(n_rows, p.cols), kPlanThreads, true, st, p);
+  if (p.n_pages <= 32 * kSmallWords && n_rows * p.cols <= 4 * kManyEntries) {
+    if ((int64_t)p.n_pages * 2 * cp.n_kv_heads * cp.page_size * cp.row_bytes <= kFewBytes)
+      return launch_after(compact_small_kernel<true>, kMaxCluster, kPlanThreads, true, st, p, cp);
+    s = launch_after(compact_small_kernel<false>, kMaxCluster, kPlanThreads, true, st, p, cp);
   } else {
-    s = launch_after(compact_kernel<false>, kMaxCluster, kPlanThreads, true, st, p);
+    s = launch_after(compact_count_kernel, kMaxCluster, kPlanThreads, true, st, p);
     const int64_t ctas = (p.n_pages + kCopyThreads - 1) / kCopyThreads;
     if (s == XKV_OK)
       s = launch_after(compact_place_kernel, (int)std::min<int64_t>(ctas, 8 * (int64_t)sm_count()), kCopyThreads, false, st, p);
   }
   if (s != XKV_OK) return s;
-  const CopyParams cp = copy_params(d, c, c);
   const int64_t entries = (n_rows * p.cols + 31) / 32;
   const int grid = std::max(copy_grid(cp, std::min<int64_t>(c->n_pages, n_rows * p.cols), true),
                             (int)std::min<int64_t>(entries / (kCopyThreads / 32), sm_count()));

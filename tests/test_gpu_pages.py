@@ -223,6 +223,19 @@ def test_copy_pages(fmt, n):
         assert torch.equal(w, t)
 
 
+def test_large_pool():
+    """More pages than one CTA maps in shared memory, more table entries than one cluster handles."""
+    rng = np.random.default_rng(5)
+    L, B, page, cols = 6, 40, 16, 300
+    pool = PagePool(L, B, 1, 64, page, cols, 60000, lens=rng.integers(0, cols * page // 2, (L, B)))
+    pool.fork([int(b) for b in rng.integers(-1, B, B)])
+    n_live, moves = pool.compact()
+    assert moves and n_live < pool.n_pages
+    pool.fork(list(range(B)), rng.integers(0, cols * page // 2, (L, B)))
+    pool.compact(in_place=False)
+    assert not pool.compact()[1]                            # nothing is left to move
+
+
 def test_captured_and_replayed():
     pool = PagePool(4, 6, 2, 64, 16, 4, 200, lens=np.tile([[50, 0, 0, 33, 0, 0]], (4, 1)))
     fork = torch.tensor([0, 0, 0, 3, 3, 3], dtype=torch.int32, device=DEV)
