@@ -228,6 +228,13 @@ __device__ __forceinline__ int4 fork_row(const ForkParams& p, int row) {
   return make_int4(a, rows, (n + p.page_size - 1) / p.page_size, (rows + p.page_size - 1) / p.page_size);
 }
 
+// The page that a cache's partly filled last rows are in, as its parent's table has it; -1: none.
+__device__ __forceinline__ int last_page(const ForkParams& p, int row, const ForkRow& r) {
+  if (r.rows % p.page_size == 0) return -1;
+  const int b = row % p.batch, e = __ldcg(&p.table[((size_t)(row - b) + r.parent) * p.cols + r.need - 1]);
+  return in_pool(p, e) ? e : -1;
+}
+
 // A warp: holders that come are counted, before any that go (so that no page seems to be free in between); the parent's entries
 // are read before any table changes.
 __device__ __forceinline__ void count_new(const ForkParams& p, int row, const ForkRow& r) {
@@ -235,10 +242,6 @@ __device__ __forceinline__ void count_new(const ForkParams& p, int row, const Fo
   const int32_t* mine = p.table + (size_t)row * p.cols;
   const int32_t* theirs = p.table + ((size_t)(row - b) + max(r.parent, 0)) * p.cols;
   int32_t* fresh = p.fresh + (size_t)row * p.cols;
-  if (lane == 0) {
-    const int e = r.rows % p.page_size != 0 ? __ldcg(&theirs[r.need - 1]) : -1;
-    p.last[row] = in_pool(p, e) ? e : -1;
-  }
   if (r.parent == b) return;
 #pragma unroll 4
   for (int i = lane; i < r.need; i += 32) {
@@ -274,19 +277,29 @@ __device__ __forceinline__ void drop_old(const ForkParams& p, int row, const For
 
 // The whole cluster: pages for copies, lengths, and pages back to the list.  row_at(row): its ForkRow.
 template <typename RowAt>
-__device__ __forceinline__ void fork_decide(const ForkParams& p, int* s_scan, RowAt row_at) {
+__device__ __forceinline__ void fork_decide(const ForkParams& p, RowAt row_at) {
+  __shared__ int s_scan[kPlanWarps + 1];
+  __shared__ int s_held[kPlanThreads];
+  __shared__ int s_copy[kPlanThreads];
   // ---- last pages that need a copy: those that others hold too, unless all holders are such last pages, of which one
-  //      (the cache that stays, else the first) keeps it.  A warp a cache.
+  //      (the cache that stays, else the first) keeps it.  A thread a cache; a warp for each that others hold.
   const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5;
   int64_t row0, row1;
   cta_run(p.n_rows, &row0, &row1);
-  for (int row = (int)row0 + warp; row < (int)row1; row += kPlanWarps) {
-    const int page = __ldcg(&p.last[row]);
-    const int others = page >= 0 ? __ldcg(&p.shares[page]) : 0;
-    bool copy = false;
-    if (others > 0) {
-      const int b0 = row % p.batch;
+  int copies = 0;
+  for (int64_t base = row0; base < row1; base += kPlanThreads) {
+    const int mine = (int)base + threadIdx.x;
+    const int own = mine < row1 ? __ldcg(&p.last[mine]) : -1;
+    const bool held_by_others = own >= 0 && __ldcg(&p.shares[own]) > 0;
+    s_copy[threadIdx.x] = 0;
+    int n_held, total;
+    const int place = block_scan(held_by_others ? 1 : 0, s_scan, &n_held);
+    if (held_by_others) s_held[place] = mine;
+    __syncthreads();
+    for (int i = warp; i < n_held; i += kPlanWarps) {
+      const int row = s_held[i], page = __ldcg(&p.last[row]), others = __ldcg(&p.shares[page]), b0 = row % p.batch;
       int n = 0, first = 0x7fffffff;
+#pragma unroll 4
       for (int b = lane; b < p.batch; b += 32)
         if (__ldcg(&p.last[row - b0 + b]) == page) {
           ++n;
@@ -294,18 +307,11 @@ __device__ __forceinline__ void fork_decide(const ForkParams& p, int* s_scan, Ro
         }
       n = __reduce_add_sync(0xffffffffu, n);
       first = __reduce_min_sync(0xffffffffu, first);
-      copy = !(n == others + 1 && (first == b0 || first == b0 + p.batch));
+      if (lane == 0) s_copy[row - base] = !(n == others + 1 && (first == b0 || first == b0 + p.batch));
     }
-    if (lane == 0) p.rank[row] = copy ? 0 : -1;
-  }
-  __syncthreads();
-  int copies = 0;
-  for (int64_t base = row0; base < row1; base += kPlanThreads) {
-    const int row = (int)base + threadIdx.x;
-    const bool copy = row < row1 && p.rank[row] >= 0;
-    int total;
-    const int before = block_scan(copy ? 1 : 0, s_scan, &total);
-    if (copy) p.rank[row] = copies + before;
+    __syncthreads();
+    const int copy = s_copy[threadIdx.x], before = block_scan(copy, s_scan, &total);
+    if (mine < row1) p.rank[mine] = copy ? copies + before : -1;
     copies += total;
   }
   const int n_words = (p.n_pages + 31) / 32;
@@ -375,28 +381,164 @@ __device__ __forceinline__ void fork_decide(const ForkParams& p, int* s_scan, Ro
   }
 }
 
-// All of a step in one cluster; what becomes of a CTA's caches stays in its shared memory.  kCopy: the rows are copied here, too.
-constexpr int kClusterRows = 1024;    // a CTA
-template <bool kCopy>
-__global__ void __launch_bounds__(kPlanThreads, 1) fork_kernel(const ForkParams p, const CopyParams c) {
+// All of a step in one launch: the first CTA of a cluster plans with the pool's counters and the caches' new entries in its shared
+// memory (three round trips to global memory: lengths and counters, entries, free pages), then all of them copy the rows.
+struct SmallFork {                    // its shared memory, in ints
+  int32_t holders, fresh, lens, last, copy, words, rows, total;
+};
+__host__ __device__ inline SmallFork small_fork(int n_rows, int cols, int n_pages) {
+  SmallFork s;
+  int at = 0;
+  s.rows = at;    at += 4 * n_rows;
+  s.holders = at; at += n_pages;                     // beyond the first
+  s.fresh = at;   at += n_rows * cols;
+  s.lens = at;    at += n_rows;
+  s.last = at;    at += n_rows;
+  s.copy = at;    at += n_rows;                      // page of the copy, -1: none, -2: wanted, -3: there was no page
+  s.words = at;   at += (n_pages + 31) / 32;         // a bit a page: dropped by a cache
+  s.total = at;
+  return s;
+}
+
+__global__ void __launch_bounds__(kPlanThreads, 1) fork_small_kernel(const ForkParams p, const CopyParams c) {
   asm volatile("griddepcontrol.wait;" ::: "memory");
   asm volatile("griddepcontrol.launch_dependents;");
+  extern __shared__ int32_t s_mem[];
   __shared__ int s_scan[kPlanWarps + 1];
-  __shared__ int4 s_rows[kClusterRows];
-  int64_t row0, row1;
-  cta_run(p.n_rows, &row0, &row1);
-  const int n = (int)(row1 - row0), warp = threadIdx.x >> 5;
-  for (int i = threadIdx.x; i < n; i += kPlanThreads) s_rows[i] = fork_row(p, (int)row0 + i);
-  __syncthreads();
-  for (int i = warp; i < n; i += kPlanWarps) count_new(p, (int)row0 + i, as_row(s_rows[i]));
-  phase();
-  for (int i = warp; i < n; i += kPlanWarps) drop_old(p, (int)row0 + i, as_row(s_rows[i]));
-  phase();
-  fork_decide(p, s_scan, [&](int row) { return as_row(s_rows[row - row0]); });
-  if constexpr (kCopy) {
-    phase();
-    copy_rows(c, p.list, __ldcg(p.n_copies));
+  __shared__ int s_busy[kPlanThreads];
+  const int tid = threadIdx.x, lane = tid & 31, warp = tid >> 5;
+  if (blockIdx.x == 0) {
+    const SmallFork at = small_fork(p.n_rows, p.cols, p.n_pages);
+    int4* s_rows = reinterpret_cast<int4*>(s_mem + at.rows);
+    int *s_holders = s_mem + at.holders, *s_fresh = s_mem + at.fresh, *s_lens = s_mem + at.lens, *s_last = s_mem + at.last;
+    int* s_copy = s_mem + at.copy;
+    uint32_t* s_words = reinterpret_cast<uint32_t*>(s_mem + at.words);
+    const int n_words = (p.n_pages + 31) / 32, most = p.cols * p.page_size;
+    const int used = min(max(__ldcg(p.used), 0), p.n_free);
+    for (int i = tid; i < p.n_rows; i += kPlanThreads) s_lens[i] = min(max(__ldcg(&p.lens[i]), 0), most);
+#pragma unroll 4
+    for (int i = tid; i < p.n_pages; i += kPlanThreads) s_holders[i] = __ldcg(&p.shares[i]);
+    for (int i = tid; i < n_words; i += kPlanThreads) s_words[i] = 0u;
+    __syncthreads();
+    for (int row = tid; row < p.n_rows; row += kPlanThreads) {
+      const int l = row / p.batch, b = row - l * p.batch, asked = __ldg(&p.parent[b]);
+      const int a = asked >= -1 && asked < p.batch ? asked : b;
+      if (a != asked) record_status(p.hdr, XKV_ERR_INVALID_ARG);
+      int rows = a < 0 ? 0 : s_lens[row - b + a];
+      if (p.keep != nullptr) {
+        const int k = __ldg(&p.keep[(size_t)l * p.keep_stride + b]);
+        if (k >= 0) rows = min(rows, k);
+      }
+      const ForkRow r = {a, rows, (s_lens[row] + p.page_size - 1) / p.page_size, (rows + p.page_size - 1) / p.page_size};
+      s_rows[row] = make_int4(r.parent, r.rows, r.have, r.need);
+      s_last[row] = last_page(p, row, r);
+      s_copy[row] = -1;
+    }
+    __syncthreads();
+    // ---- holders that come and go (a page is free if none is left at the end, in whatever order), of caches that change
+    int n_busy;
+    {
+      const ForkRow r = tid < p.n_rows ? as_row(s_rows[tid]) : ForkRow{0, 0, 0, 0};
+      const bool busy = tid < p.n_rows && (r.parent != tid % p.batch || r.have > r.need);
+      const int place = block_scan(busy ? 1 : 0, s_scan, &n_busy);
+      if (busy) s_busy[place] = tid;
+      __syncthreads();
+    }
+    for (int i_row = warp; i_row < n_busy; i_row += kPlanWarps) {
+      const int row = s_busy[i_row], b = row % p.batch;
+      const ForkRow r = as_row(s_rows[row]);
+      const int32_t* mine = p.table + (size_t)row * p.cols;
+      const int32_t* theirs = p.table + ((size_t)(row - b) + max(r.parent, 0)) * p.cols;
+#pragma unroll 4
+      for (int i = (r.parent == b ? r.need : 0) + lane; i < max(r.have, r.need); i += 32) {
+        const int was = i < r.have ? __ldcg(&mine[i]) : -1, now = i < r.need ? __ldcg(&theirs[i]) : -1;
+        if (i < r.need) s_fresh[row * p.cols + i] = now;
+        if ((i < r.have && !in_pool(p, was)) || (i < r.need && !in_pool(p, now))) record_status(p.hdr, XKV_ERR_INVALID_ARG);
+        if (i < r.have && i < r.need && was == now) continue;
+        if (i < r.need && in_pool(p, now)) atomicAdd(&s_holders[now], 1);
+        if (i < r.have && in_pool(p, was)) {
+          atomicSub(&s_holders[was], 1);
+          atomicOr(&s_words[was >> 5], 1u << (was & 31));
+        }
+      }
+    }
+    __syncthreads();
+    // ---- tables; last pages that others hold too (see fork_decide)
+    for (int row = warp; row < p.n_rows; row += kPlanWarps) {
+      const ForkRow r = as_row(s_rows[row]);
+      const int b0 = row % p.batch, page = s_last[row];
+      if (r.parent != b0)
+        for (int i = lane; i < r.need; i += 32) p.table[(size_t)row * p.cols + i] = s_fresh[row * p.cols + i];
+      const int others = page >= 0 ? s_holders[page] : 0;
+      if (others <= 0) continue;
+      int n = 0, first = 0x7fffffff;
+      for (int b = lane; b < p.batch; b += 32)
+        if (s_last[row - b0 + b] == page) {
+          ++n;
+          first = min(first, b + (s_rows[row - b0 + b].x == b ? 0 : p.batch));
+        }
+      n = __reduce_add_sync(0xffffffffu, n);
+      first = __reduce_min_sync(0xffffffffu, first);
+      if (lane == 0 && !(n == others + 1 && (first == b0 || first == b0 + p.batch))) s_copy[row] = -2;
+    }
+    __syncthreads();
+    // ---- pages for the copies, from the list as it was
+    int copies = 0;
+    for (int base = 0; base < p.n_rows; base += kPlanThreads) {
+      const int row = base + tid;
+      const bool copy = row < p.n_rows && s_copy[row] == -2;
+      int total;
+      const int i = copies + block_scan(copy ? 1 : 0, s_scan, &total);
+      copies += total;
+      if (row >= p.n_rows) continue;
+      const ForkRow r = as_row(s_rows[row]);
+      int rows = r.rows;
+      if (copy) {
+        const int page = s_last[row], to = i < p.n_free - used ? __ldcg(&p.free_pages[used + i]) : -1;
+        atomicSub(&s_holders[page], 1);
+        RowCopy x = {page, to, r.rows % p.page_size};
+        if (in_pool(p, to)) {
+          p.table[(size_t)row * p.cols + r.need - 1] = to;
+        } else {                      // no page: only whole pages stay
+          record_status(p.hdr, i < p.n_free - used ? XKV_ERR_INVALID_ARG : XKV_ERR_CAPACITY);
+          x = {0, 0, 0};
+          rows -= rows % p.page_size;
+        }
+        p.list[i] = x;
+      }
+      p.lens[row] = rows;
+    }
+    // ---- pages back to the list, in ascending order, and the counters: a thread a page, a warp a word of the map
+    __syncthreads();
+    for (int base = 0; base < p.n_pages; base += kPlanThreads) {
+      const int page = base + tid;
+      const bool gone = page < p.n_pages && ((s_words[page >> 5] >> lane) & 1u) != 0 && s_holders[page] < 0;
+      const uint32_t word = __ballot_sync(0xffffffffu, gone);
+      if (lane == 0 && page < p.n_pages) s_words[page >> 5] = word;
+      if (page < p.n_pages) {
+        if (gone && s_holders[page] < -1) record_status(p.hdr, XKV_ERR_INVALID_ARG);   // dropped more often than it was held
+        p.shares[page] = max(s_holders[page], 0);
+      }
+    }
+    __syncthreads();
+    int back;                         // (at most kPlanThreads words)
+    const int before = block_scan(tid < n_words ? __popc(s_words[tid]) : 0, s_scan, &back);
+    if (tid < n_words) s_busy[tid] = before;
+    __syncthreads();
+    const int top = used + min(copies, p.n_free - used) - back;
+    for (int page = tid; page < p.n_pages; page += kPlanThreads) {
+      const uint32_t word = s_words[page >> 5];
+      const int at_list = top + s_busy[page >> 5] + __popc(word & ((1u << lane) - 1u));
+      if (((word >> lane) & 1u) != 0 && at_list >= 0) p.free_pages[at_list] = page;
+    }
+    if (tid == 0) {
+      if (top < 0) record_status(p.hdr, XKV_ERR_INVALID_ARG);      // more came back than were handed out
+      *p.used = max(top, 0);
+      *p.n_copies = copies;
+    }
   }
+  phase();
+  copy_rows(c, p.list, __ldcg(p.n_copies));
 }
 
 // The same in three launches, whose first two take all SMs.
@@ -406,7 +548,10 @@ __global__ void __launch_bounds__(kCopyThreads) fork_count_kernel(const ForkPara
   const int n_warps = gridDim.x * (kCopyThreads / 32);
   for (int row = blockIdx.x * (kCopyThreads / 32) + (threadIdx.x >> 5); row < p.n_rows; row += n_warps) {
     const int4 r = fork_row(p, row);
-    if ((threadIdx.x & 31) == 0) p.rows[row] = r;
+    if ((threadIdx.x & 31) == 0) {
+      p.rows[row] = r;
+      p.last[row] = last_page(p, row, as_row(r));
+    }
     count_new(p, row, as_row(r));
   }
 }
@@ -420,8 +565,7 @@ __global__ void __launch_bounds__(kCopyThreads) fork_drop_kernel(const ForkParam
 __global__ void __launch_bounds__(kPlanThreads, 1) fork_decide_kernel(const ForkParams p) {
   asm volatile("griddepcontrol.wait;" ::: "memory");
   asm volatile("griddepcontrol.launch_dependents;");
-  __shared__ int s_scan[kPlanWarps + 1];
-  fork_decide(p, s_scan, [&](int row) { return as_row(__ldcg(&p.rows[row])); });
+  fork_decide(p, [&](int row) { return as_row(__ldcg(&p.rows[row])); });
 }
 
 // ---------------------------------------------------------------------------------------------
@@ -636,8 +780,10 @@ Layout compact_layout(int64_t n_pages) {
 
 // All launches here wait for the one before them on the device, so that their CTAs may be in place when it ends.
 template <typename... Args>
-xkv_status launch_after(void (*kernel)(Args...), int grid, int threads, bool cluster, cudaStream_t st, Args... args) {
+xkv_status launch_after(void (*kernel)(Args...), int grid, int threads, bool cluster, cudaStream_t st, size_t smem,
+                        Args... args) {
   cudaLaunchConfig_t cfg = {};
+  cfg.dynamicSmemBytes = smem;
   cfg.gridDim = dim3((unsigned)grid);
   cfg.blockDim = dim3((unsigned)threads);
   cfg.stream = st;
@@ -657,13 +803,10 @@ xkv_status launch_after(void (*kernel)(Args...), int grid, int threads, bool clu
   return check_launch();
 }
 
-// CTAs of a plan: one (whose barriers are cheapest) for a few hundred caches of short tables, else a cluster.
-int plan_ctas(int64_t n_rows, int cols) {
-  const int64_t steps = n_rows * ((cols + 31) / 32);         // of a warp
-  return steps <= 2 * kPlanWarps ? 1 : (steps <= 16 * kPlanWarps ? kMaxCluster / 2 : kMaxCluster);
-}
-// Table entries from which on a step's forks take all SMs.
+// Table entries, and pages of a pool, up to which one CTA plans a step's forks.
 constexpr int64_t kManyEntries = 16384;
+static_assert(kManyEntries / 32 <= kPlanThreads, "a thread a word of the map");
+constexpr int kSmallForkBytes = 4 * (2 * kManyEntries + kManyEntries / 32 + 7 * kPlanThreads);
 // Bytes that a plan's cluster copies itself: a second launch takes the device 2 us and the host 4.
 constexpr int64_t kFewBytes = 2 << 20;
 
@@ -708,20 +851,28 @@ xkv_status fork_caches(const xkv_dims* d, const xkv_cache* c, const int32_t* par
   p.fresh = reinterpret_cast<int32_t*>(ws + L.fresh);
   const CopyParams cp = copy_params(d, c, c);
   xkv_status s;
-  if (n_rows * p.cols <= kManyEntries && n_rows <= kClusterRows) {
-    const int ctas = plan_ctas(n_rows, p.cols);
-    // rows of every cache's last page at most
-    if (n_rows * 2 * cp.n_kv_heads * cp.page_size * cp.row_bytes <= kFewBytes)
-      return launch_after(fork_kernel<true>, ctas, kPlanThreads, true, st, p, cp);
-    s = launch_after(fork_kernel<false>, ctas, kPlanThreads, true, st, p, cp);
-  } else {
-    const int grid = (int)std::min<int64_t>((n_rows + kCopyThreads / 32 - 1) / (kCopyThreads / 32), 8 * (int64_t)sm_count());
-    s = launch_after(fork_count_kernel, grid, kCopyThreads, false, st, p);
-    if (s == XKV_OK) s = launch_after(fork_drop_kernel, grid, kCopyThreads, false, st, p);
-    if (s == XKV_OK) s = launch_after(fork_decide_kernel, kMaxCluster, kPlanThreads, true, st, p);
+  // Few bytes of last rows at most, and little enough for one CTA's shared memory.
+  if (n_rows * p.cols <= kManyEntries && n_rows <= kPlanThreads && p.n_pages <= kManyEntries &&
+      n_rows * 2 * cp.n_kv_heads * cp.page_size * cp.row_bytes <= kFewBytes) {
+    static std::atomic<bool> done[64];   // idempotent set-up: two threads doing it twice is harmless
+    int dev = 0;
+    if (cudaGetDevice(&dev) != cudaSuccess || dev < 0 || dev >= 64) return XKV_ERR_CUDA;
+    if (!done[dev].load(std::memory_order_acquire)) {
+      if (cudaFuncSetAttribute(fork_small_kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, kSmallForkBytes) != cudaSuccess) {
+        (void)cudaGetLastError();
+        return XKV_ERR_CUDA;
+      }
+      done[dev].store(true, std::memory_order_release);
+    }
+    return launch_after(fork_small_kernel, kMaxCluster, kPlanThreads, true, st,
+                        4 * (size_t)small_fork((int)n_rows, p.cols, p.n_pages).total, p, cp);
   }
+  const int grid = (int)std::min<int64_t>((n_rows + kCopyThreads / 32 - 1) / (kCopyThreads / 32), 8 * (int64_t)sm_count());
+  s = launch_after(fork_count_kernel, grid, kCopyThreads, false, st, 0, p);
+  if (s == XKV_OK) s = launch_after(fork_drop_kernel, grid, kCopyThreads, false, st, 0, p);
+  if (s == XKV_OK) s = launch_after(fork_decide_kernel, kMaxCluster, kPlanThreads, true, st, 0, p);
   if (s != XKV_OK) return s;
-  return launch_after(copy_rows_kernel, copy_grid(cp, n_rows, false), kCopyThreads, false, st, cp, (const RowCopy*)p.list,
+  return launch_after(copy_rows_kernel, copy_grid(cp, n_rows, false), kCopyThreads, false, st, 0, cp, (const RowCopy*)p.list,
                       (const int32_t*)p.n_copies);
 }
 
@@ -754,19 +905,19 @@ xkv_status compact_pages(const xkv_dims* d, const xkv_cache* c, const int32_t* t
   xkv_status s;
   if (p.n_pages <= 32 * kSmallWords && n_rows * p.cols <= 4 * kManyEntries) {
     if ((int64_t)p.n_pages * 2 * cp.n_kv_heads * cp.page_size * cp.row_bytes <= kFewBytes)
-      return launch_after(compact_small_kernel<true>, kMaxCluster, kPlanThreads, true, st, p, cp);
-    s = launch_after(compact_small_kernel<false>, kMaxCluster, kPlanThreads, true, st, p, cp);
+      return launch_after(compact_small_kernel<true>, kMaxCluster, kPlanThreads, true, st, 0, p, cp);
+    s = launch_after(compact_small_kernel<false>, kMaxCluster, kPlanThreads, true, st, 0, p, cp);
   } else {
-    s = launch_after(compact_count_kernel, kMaxCluster, kPlanThreads, true, st, p);
+    s = launch_after(compact_count_kernel, kMaxCluster, kPlanThreads, true, st, 0, p);
     const int64_t ctas = (p.n_pages + kCopyThreads - 1) / kCopyThreads;
     if (s == XKV_OK)
-      s = launch_after(compact_place_kernel, (int)std::min<int64_t>(ctas, 8 * (int64_t)sm_count()), kCopyThreads, false, st, p);
+      s = launch_after(compact_place_kernel, (int)std::min<int64_t>(ctas, 8 * (int64_t)sm_count()), kCopyThreads, false, st, 0, p);
   }
   if (s != XKV_OK) return s;
   const int64_t entries = (n_rows * p.cols + 31) / 32;
   const int grid = std::max(copy_grid(cp, std::min<int64_t>(c->n_pages, n_rows * p.cols), true),
                             (int)std::min<int64_t>(entries / (kCopyThreads / 32), sm_count()));
-  return launch_after(compact_move_kernel, grid, kCopyThreads, false, st, p, cp);
+  return launch_after(compact_move_kernel, grid, kCopyThreads, false, st, 0, p, cp);
 }
 
 xkv_status copy_pages(const xkv_dims* d, const xkv_cache* from, const int32_t* src, const xkv_cache* to, const int32_t* dst,
