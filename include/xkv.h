@@ -240,7 +240,7 @@ xkv_status xkv_prefill_attn(const xkv_dims* dims, const void* q, const void* k, 
  *   lse[h][s][i] = natural log of the sum over c <= i of exp(scale * q_s . k_s[c])
  *
  * q          dev bf16 [T][Hq][d];  k, v  dev bf16, layout and strides of xkv_score;  head_dim: d
- * lambda     dev fp32 [Hq];  gain  dev fp32 [d], NULL: no norm;  eps >= 0, finite
+ * lambda     dev fp32 [Hq], 4-byte aligned;  gain  dev fp32 [d], NULL: no norm;  eps >= 0, finite
  * out        dev out bf16 [T][Hq][d];  lse  dev out fp32 [Hq][2][T], may be NULL
  * workspace  dev, at least xkv_workspace_bytes(XKV_OP_DIFF_PREFILL_ATTN, ...) bytes (the status word), 256-byte aligned
  * bf16 inputs, fp32 accumulation, difference and norm, the weights rounded to bf16 before they multiply v, bf16 output. A value v
@@ -556,7 +556,7 @@ xkv_status xkv_decode_attn(const xkv_dims* dims, const xkv_cache* cache, int32_t
  *
  * dims       n_q_heads: differential heads; head_dim: d. n_q_heads / n_kv_heads at most 8; a KV head with more than four heads is
  *            read more than once
- * lambda     dev fp32 [Lr][Hq]
+ * lambda     dev fp32 [Lr][Hq], 4-byte aligned (a layer's row of a larger array will do)
  * gain       dev fp32 [Lr][d], NULL: no norm;  eps >= 0, finite
  * lse        dev out fp32 [Lr][B][Hq][2], may be NULL: of each map
  * workspace  dev, at least xkv_workspace_bytes(XKV_OP_DIFF_DECODE_ATTN, ...) bytes

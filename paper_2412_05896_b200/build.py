@@ -11,7 +11,7 @@ CSRC = os.path.join(HERE, "csrc")
 LIB = os.path.join(HERE, "libxkv.so")
 SOURCES = ["xkv_api.cu", "xkv_score.cu", "xkv_score_tc.cu", "xkv_score_fused.cu", "xkv_select.cu", "xkv_decode.cu", "xkv_prefill.cu",
            "xkv_serve.cu", "xkv_decode_e4m3.cu", "xkv_pages.cu",
-           "xkv_diff_prefill.cu"]
+           "xkv_diff_prefill.cu", "xkv_diff_decode.cu"]
 HEADERS = ["common.cuh", "ops.h", "score_params.h", "tc_common.cuh", "e4m3.cuh", os.path.join("..", "..", "include", "xkv.h")]
 
 

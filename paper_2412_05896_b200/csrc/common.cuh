@@ -24,7 +24,8 @@ struct WorkspaceHeader {
   int32_t grid_arrivals; // decode: CTAs of the self-planning launch that have finished all their work
   int32_t plan_ticket;   // step plan: CTAs that have finished (zero between calls)
   int32_t plan_used;     // step plan: free-list position behind the last page handed out (zero between calls)
-  int32_t reserved[54];
+  int32_t few_tickets[48]; // decode of little: CTAs of a cache that have finished (zero between calls)
+  int32_t reserved[6];
 };
 static_assert(sizeof(WorkspaceHeader) == 256, "header is 256 bytes");
 
@@ -42,6 +43,7 @@ uint64_t wait_limit_ns();
 int32_t debug_withhold_item();
 
 inline bool aligned16(const void* p) { return (reinterpret_cast<uintptr_t>(p) & 15u) == 0; }
+inline bool aligned4(const void* p) { return (reinterpret_cast<uintptr_t>(p) & 3u) == 0; }
 
 __device__ __forceinline__ void record_status(WorkspaceHeader* hdr, int32_t code) {
   atomicCAS(&hdr->status, XKV_OK, code);

@@ -171,7 +171,7 @@ xkv_status xkv_diff_prefill_attn(const xkv_dims* dims, const void* q, const void
   if (q == nullptr || k == nullptr || v == nullptr || lambda == nullptr || cu_seqlens == nullptr || out == nullptr ||
       workspace == nullptr)
     return XKV_ERR_INVALID_ARG;
-  if (!aligned16(q) || !aligned16(k) || !aligned16(v) || !aligned16(lambda) || !aligned16(gain) || !aligned16(cu_seqlens) ||
+  if (!aligned16(q) || !aligned16(k) || !aligned16(v) || !aligned4(lambda) || !aligned16(gain) || !aligned16(cu_seqlens) ||
       !aligned16(out) || !aligned16(lse) || (reinterpret_cast<uintptr_t>(workspace) & 255u) != 0)
     return XKV_ERR_INVALID_ARG;
   if (!(eps >= 0.f) || std::isinf(eps)) return XKV_ERR_INVALID_ARG;
@@ -385,7 +385,7 @@ xkv_status xkv_diff_decode_attn(const xkv_dims* dims, const xkv_cache* cache, in
   if (s != XKV_OK) return s;
   if (q == nullptr || out == nullptr || workspace == nullptr || lambda == nullptr) return XKV_ERR_INVALID_ARG;
   if ((k_new == nullptr) != (v_new == nullptr)) return XKV_ERR_INVALID_ARG;
-  if (!aligned16(q) || !aligned16(k_new) || !aligned16(v_new) || !aligned16(out) || !aligned16(lse) || !aligned16(lambda) ||
+  if (!aligned16(q) || !aligned16(k_new) || !aligned16(v_new) || !aligned16(out) || !aligned16(lse) || !aligned4(lambda) ||
       !aligned16(gain) || (reinterpret_cast<uintptr_t>(workspace) & 255u) != 0)
     return XKV_ERR_INVALID_ARG;
   if (!(eps >= 0.f) || std::isinf(eps)) return XKV_ERR_INVALID_ARG;

@@ -1234,14 +1234,18 @@ xkv_status decode_attn(const xkv_dims* d, const xkv_cache* c, int layer_begin, i
   if (workspace_bytes < L.total) return XKV_ERR_WORKSPACE;
   const uint64_t page_rows = (uint64_t)c->n_pages * d->n_kv_heads * c->page_size;
   if (page_rows >= (1ull << 31)) return XKV_ERR_UNSUPPORTED;
-  if (c->kv_format == XKV_KV_E4M3) {
+  if (c->kv_format == XKV_KV_E4M3 || diff != nullptr) {
     uint8_t* base = static_cast<uint8_t*>(workspace);
     const size_t keep = clear_status ? 0 : sizeof(int32_t);   // see below
     const DecodeScratch scratch = {base, reinterpret_cast<int32_t*>(base + keep), (int32_t)((L.unit_info - keep) / 4),
                                    reinterpret_cast<int32_t*>(base + L.tickets),
                                    reinterpret_cast<float*>(base + L.part_o), reinterpret_cast<float*>(base + L.part_ml),
                                    L.max_items};
-    return decode_attn_e4m3(d, c, layer_begin, Lr, q, k_new, v_new, out, lse, scratch, st, diff);
+    if (c->kv_format != XKV_KV_E4M3 && k_new == nullptr && chunk_rows == 0 &&
+        diff_decode_is_few(d, Lr, max_cache_len, L.max_items * G))
+      return diff_decode_few(d, c, layer_begin, Lr, q, out, lse, *diff, scratch, st);
+    if (c->kv_format == XKV_KV_E4M3)
+      return decode_attn_e4m3(d, c, layer_begin, Lr, q, k_new, v_new, out, lse, scratch, st, diff);
   }
 
   const bool q8 = c->kv_format == XKV_KV_INT8;

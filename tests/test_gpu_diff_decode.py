@@ -61,15 +61,15 @@ CASES = [  # L, B, KV heads, group, d, page, lengths
 
 @pytest.mark.parametrize("fmt", ["bf16", "int8", "e4m3"])
 @pytest.mark.parametrize("L,B,H,G,d,page,lens", CASES)
-@pytest.mark.parametrize("norm", [True, False])
-def test_against_definition(fmt, L, B, H, G, d, page, lens, norm):
+@pytest.mark.parametrize("norm,chunk", [(True, 0), (True, 64), (False, 0)])
+def test_against_definition(fmt, L, B, H, G, d, page, lens, norm, chunk):
     c = RowCache(fmt, L, B, H, d, lens, page, seed=L + G)
     lam, gain = weights(L, H * G, d, 7, norm)
     q = queries(L, B, H * G, d, 11)
     lam, gain = lam.to(DEV), None if gain is None else gain.to(DEV)
-    out, sums = attend(c, H * G, q, lam, gain)
+    out, sums = attend(c, H * G, q, lam, gain, chunk=chunk)
     check(c, H * G, q, lam, gain, out, sums)
-    again, _ = attend(c, H * G, q, lam, gain, lse=False)
+    again, _ = attend(c, H * G, q, lam, gain, lse=False, chunk=chunk)
     assert torch.equal(out, again)
 
 
@@ -106,7 +106,8 @@ def test_new_rows_are_appended_first(fmt, G):
         for a, b in zip(c.pages + c.scales, twin.pages + twin.scales):
             if a is not None:
                 assert torch.equal(a.view(torch.uint8), b.view(torch.uint8))
-        after, _ = attend(c, H * G, q, lam, gain)           # the rows are in the pages now: the same values
+        # the rows are in the pages now: the same values (from the same kernel: with chunks given, the one that also appends)
+        after, _ = attend(c, H * G, q, lam, gain, chunk=256)
         assert torch.equal(after, out)
 
 
@@ -179,3 +180,27 @@ def test_captured_and_replayed(fmt):
         torch.cuda.synchronize()
         assert torch.equal(out, want) and torch.equal(sums, want_lse)
     assert xkv.read_device_status(ws) == xkv.OK
+
+
+@pytest.mark.parametrize("fmt", ["bf16", "int8"])
+def test_one_workspace_for_small_and_large_calls(fmt):
+    """Calls that take the kernel for few rows and the streaming one in turn, layer by layer and all at once, share a workspace."""
+    L, B, H, G, d, page = 3, 1, 2, 3, 64, 16
+    small = RowCache(fmt, L, B, H, d, [[300], [1000], [129]], page, seed=1)
+    large = RowCache(fmt, L, 40, H, d, np.random.default_rng(1).integers(1, 900, (L, 40)), page, seed=2)
+    lam, gain = (t.to(DEV) for t in weights(L, H * G, d, 5))
+    qs, ql = queries(L, B, H * G, d, 6), queries(L, 40, H * G, d, 7)
+    dims = xkv.Dims(40, H * G, H, d, 1, 1, 0, 0.0, H * d, d)
+    ws = torch.zeros(xkv.workspace_bytes(xkv.OP_DIFF_DECODE_ATTN, dims, n_layers=L, max_cache_len=1024), dtype=torch.uint8,
+                     device=DEV)
+    want_s, want_l = attend(small, H * G, qs, lam, gain), attend(large, H * G, ql, lam, gain)
+    check(small, H * G, qs, lam, gain, *want_s)
+    for _ in range(5):
+        got = attend(small, H * G, qs, lam, gain, ws=ws)
+        assert torch.equal(got[0], want_s[0]) and torch.equal(got[1], want_s[1])
+        got = attend(large, H * G, ql, lam, gain, ws=ws)
+        assert torch.equal(got[0], want_l[0]) and torch.equal(got[1], want_l[1])
+        for l in range(L):
+            got = attend(small, H * G, qs[l:l + 1].contiguous(), lam[l:l + 1].contiguous(), gain[l:l + 1].contiguous(), l0=l,
+                         l1=l + 1, ws=ws)
+            assert torch.equal(got[0][0], want_s[0][l])

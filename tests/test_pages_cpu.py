@@ -128,7 +128,7 @@ def test_diff_decode_attn_refuses():
         return lib.xkv_diff_decode_attn(ctypes.byref(d or _dims()), ctypes.byref(c or _cache()), l0, l1, q, kn, vn, lam, gain,
                                         eps, out, lse, chunk, ws, nb, None)
 
-    for bad in (dict(q=None), dict(out=None), dict(lam=None), dict(ws=None), dict(q=8), dict(lam=4), dict(gain=8), dict(lse=4),
+    for bad in (dict(q=None), dict(out=None), dict(lam=None), dict(ws=None), dict(q=8), dict(lam=2), dict(gain=8), dict(lse=4),
                 dict(out=2), dict(ws=16), dict(kn=16), dict(vn=16), dict(kn=16, vn=8), dict(eps=-1.0), dict(eps=float("nan")),
                 dict(eps=float("inf")), dict(l0=-1), dict(l1=0), dict(l1=5), dict(chunk=32), dict(chunk=-64),
                 dict(c=_cache(k_scales=None)), dict(c=_cache(page_size=40)), dict(d=_dims(n_kv_heads=3)), dict(d=_dims(scale=-1.0))):
