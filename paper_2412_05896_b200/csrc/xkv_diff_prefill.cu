@@ -184,7 +184,7 @@ diff_prefill_kernel(const __grid_constant__ CUtensorMap tmap_q, const __grid_con
       s_v_full[kStages], s_v_clear, s_v_empty[kStages], s_s_full[2], s_s_free[2], s_p_full[2][2], s_o_full[2][2], s_o_free, s_inv_full,
       s_sq_full;
   __shared__ Item s_item[kItems];
-  __shared__ float s_inv[2][kRows], s_sq[2][kRows];
+  __shared__ float s_inv[2][2][kRows], s_sq[2][kRows];      // s_inv: of even and of odd items, a warp may still read the item before
   __shared__ uint32_t s_tmem;
   __shared__ int s_abort_store;
   volatile int* s_abort = &s_abort_store;
@@ -484,15 +484,17 @@ diff_prefill_kernel(const __grid_constant__ CUtensorMap tmap_q, const __grid_con
       // ---- both maps' O are complete; this map's warps take columns [map D/2, (map + 1) D/2) of their rows
       const uint32_t last = jj - 1;
       const bool live = row < it.t;
-      s_inv[map][r] = l > 0.f ? 1.f / l : 0.f;
+      s_inv[n & 1][map][r] = l > 0.f ? 1.f / l : 0.f;
       if (live && p.lse != nullptr)
         p.lse[((size_t)it.h * 2 + map) * p.total_tokens + it.cu + row] = (m_ref + log2f(l)) * 0.6931471805599453f;
       __syncwarp();
       if (lane == 0) mbar_arrive(&s_inv_full);
-      ok = wait(&s_o_full[0][last & 1], last / 2) && wait(&s_o_full[1][last & 1], last / 2) && wait(&s_inv_full, n);
+      // First that every warp has come to its last tile: the other map may be tiles behind, and a wait by parity would then take
+      // the phase two back for the one meant.
+      ok = wait(&s_inv_full, n) && wait(&s_o_full[0][last & 1], last / 2) && wait(&s_o_full[1][last & 1], last / 2);
       if (!ok) break;
       tc_fence_after_sync();
-      const float w1 = s_inv[0][r], w2 = -__ldg(&p.lambda[it.h]) * s_inv[1][r];
+      const float w1 = s_inv[n & 1][0][r], w2 = -__ldg(&p.lambda[it.h]) * s_inv[n & 1][1][r];
       float y[D / 2], sq = 0.f;
 #pragma unroll
       for (int c = 0; c < D / 2; c += 32) {

@@ -98,6 +98,21 @@ def test_repeated_calls_are_the_same():
         assert torch.equal(out, again) and torch.equal(sums, s)
 
 
+@pytest.mark.parametrize("lens,d,norm", [([2399, 4287, 3917], 128, True), ([4100, 3000], 64, False), ([100] * 300, 128, False)])
+def test_maps_that_drift_apart(lens, d, norm):
+    """Long items on every SM, where one map's warps run tiles ahead of the other's, and short ones after one another: the same
+    result in every call, and the definition's."""
+    H, G = 8, 4
+    q, k, v = prompts(lens, H * G, H, d, 8)
+    lam, gain = weights(1, H * G, d, 7, norm)
+    lam, gain = lam[0].to(DEV), None if gain is None else gain[0].to(DEV)
+    out, sums = attend(lens, q, k, v, H, lam, gain)
+    check(lens, q, k, v, H, lam, gain, out, sums, heads=(3, 30), rows=np.arange(90, max(lens), 101))
+    for _ in range(30):
+        again, s = attend(lens, q, k, v, H, lam, gain)
+        assert torch.equal(out, again) and torch.equal(sums, s)
+
+
 def test_what_is_not_finite_stays_in_its_sequence():
     """NaN and infinities in the next prompt's rows, and rows of the K and V tensors behind the last token."""
     lens = [70, 130, 33]
