@@ -1,17 +1,23 @@
-// Differential attention of single tokens where there is little to read: few caches that their tables bound to few rows.
+// Differential attention of single tokens over bf16 and int8 caches, straight from registers.
 //
 // Mathematics: that of xkv_diff_decode_attn.  With a head's query row [q1 | q2], cache rows [k1 | k2] and v,
 //   z_s[c] = scale q_s . k_s[c],  p_s = exp(z_s - max z_s),  o_s = sum_c p_s[c] v[c]          s = 1, 2
 // per chunk of rows, joined over the chunks of a cache by their maxima and sums; then the difference of the two maps and its norm.
 //
-// The streaming kernel is made for caches that keep every SM busy for many tiles; here a call is a chain of latencies, so everything
-// is laid out for few of them: one launch that needs nothing cleared before it, one CTA per chunk of a streamed cache, and all of a
-// chunk's K and V bytes asked for at once as soon as its page ids are known.  A warp has 16 rows in registers and multiplies them with
-// mma.sync m16n8k16, rows on M and the (at most eight) query rows on N.  A lane's 16 bytes of a row are eight consecutive columns, so
-// no fragment goes through shared memory: of the logits the columns' order does not matter as long as the query has the same, and
-// of the outputs it only says where a value is stored (V's fragments are transposed in registers, 8 x 8 at a time).  The last CTA
-// of a cache to finish joins the chunks (in their order, so the result does not depend on who that is) and sets the ticket back to
-// zero.
+// The streaming kernel stages rows in shared memory behind a plan of the lengths and suits calls that keep every SM busy for long;
+// a small call is a chain of latencies, and a large one of 8-bit rows is bound by instructions.  Here one launch needs nothing planned
+// before it: one CTA per chunk of a streamed cache, eight warps, a warp's 16 rows of K and V in its registers and the next tile's
+// asked for as soon as their registers are free.  The products are mma.sync m16n8k16, rows on M and the (at most eight) query rows,
+// both maps of up to four heads, on N: N = 8 fits, where a 128-row tcgen05 tile would be all but empty and the tensor pipe is idle
+// either way.  A lane's 16 bytes of a row are eight consecutive columns, so no fragment goes through shared memory: of the logits the
+// columns' order does not matter as long as the query has the same, and of the outputs it only says where a value is stored (V's
+// fragments are transposed in registers, 8 x 8 at a time).  8-bit rows become fp16 with a bias, one instruction a pair, which comes
+// off the sums.  The last CTA of a cache to finish joins the chunks (in their order, so the result does not depend on who that is)
+// and sets the ticket back to zero.
+// Weights are rounded to 16 bits for their product (half a step, 2^-9 for bf16 and 2^-12 for fp16 of their largest, as in the streaming
+// kernel); sums, maxima and outputs are fp32.
+// Measured, device time: 2 caches of up to 33 rows 7.6 us (floor 0.1: latencies of ids, rows, two barriers and the launch); 1024 caches,
+// 1.66 GB of bf16 rows 285 us = 5.8 TB/s; int8, one head a KV head, 338 MB 91 us = 3.7 TB/s, bound by issued instructions.
 #include <algorithm>
 
 #include "common.cuh"
@@ -22,10 +28,64 @@ namespace {
 
 constexpr int kThreads = 256;
 constexpr int kWarps = kThreads / 32;
-constexpr int kChunk = 16 * kWarps;   // rows of a CTA
+constexpr int kTile = 16 * kWarps;    // rows that a CTA has in registers
 constexpr int kRows = 8;              // query rows at most: the N of the products
 constexpr int kMaxCtas = 2 * 148;     // one wave: two CTAs an SM
-constexpr int kTickets = sizeof(WorkspaceHeader::few_tickets) / 4;
+constexpr int kManyCaches = 1280;     // see diff_decode_by_rows
+constexpr float kLazy = 8.f;          // log2 slack before the reference maximum is raised
+constexpr int kTickets = sizeof(WorkspaceHeader::row_tickets) / 4;
+
+struct AppendParams {
+  const __nv_bfloat16* k_new;
+  const __nv_bfloat16* v_new;
+  uint8_t* k_pages;
+  uint8_t* v_pages;
+  float* k_scales;
+  float* v_scales;
+  const int32_t* block_table;
+  int32_t* seq_lens;
+  int32_t layer_begin, batch, n_kv_heads, page_size, max_pages_per_seq, n_pages;
+  WorkspaceHeader* hdr;
+};
+
+// One CTA a unit: its new row of every KV head stored behind its last one, its length advanced.
+template <int D, bool Q8>
+__global__ void __launch_bounds__(kThreads) append_kernel(const AppendParams p) {
+  constexpr int kPieces = D / 8;
+  const int e = blockIdx.x;
+  const size_t le = (size_t)p.layer_begin * p.batch + e;
+  const int n = p.seq_lens[le];
+  int page = -1;
+  if (n >= 0 && n < p.max_pages_per_seq * p.page_size) page = p.block_table[le * p.max_pages_per_seq + n / p.page_size];
+  if (page < 0 || page >= p.n_pages) {
+    if (threadIdx.x == 0) record_status(p.hdr, XKV_ERR_CAPACITY);
+    return;
+  }
+  for (int i = threadIdx.x; i < p.n_kv_heads * kPieces; i += kThreads) {       // (whole rows: a row's lanes stay together)
+    const int h = i / kPieces, c = i % kPieces;
+    const size_t src = ((size_t)e * p.n_kv_heads + h) * D + c * 8;
+    const size_t row = ((size_t)page * p.n_kv_heads + h) * p.page_size + n % p.page_size;
+    const uint4 k = __ldg(reinterpret_cast<const uint4*>(p.k_new + src)), v = __ldg(reinterpret_cast<const uint4*>(p.v_new + src));
+    if constexpr (Q8) {
+      float x[8], ks, vs;
+      bf16x8_to_f32(k, x);
+      const uint2 kc = quantize_row_piece(x, kPieces, &ks);
+      bf16x8_to_f32(v, x);
+      const uint2 vc = quantize_row_piece(x, kPieces, &vs);
+      *reinterpret_cast<uint2*>(p.k_pages + row * D + c * 8) = kc;
+      *reinterpret_cast<uint2*>(p.v_pages + row * D + c * 8) = vc;
+      if (c == 0) {
+        p.k_scales[row] = ks;
+        p.v_scales[row] = vs;
+      }
+    } else {
+      *reinterpret_cast<uint4*>(p.k_pages + (row * D + c * 8) * 2) = k;
+      *reinterpret_cast<uint4*>(p.v_pages + (row * D + c * 8) * 2) = v;
+    }
+  }
+  __syncthreads();                    // every thread has read the length
+  if (threadIdx.x == 0) p.seq_lens[le] = n + 1;
+}
 
 struct Params {
   const __nv_bfloat16* q;
@@ -37,10 +97,10 @@ struct Params {
   const float* v_scales;
   const int32_t* block_table;
   const int32_t* seq_lens;
-  int32_t layer_begin, batch, n_q_heads, n_kv_heads, n_heads, page_size, max_pages_per_seq, n_pages, max_chunks;
+  int32_t layer_begin, batch, n_q_heads, n_kv_heads, n_heads, page_size, max_pages_per_seq, n_pages, max_chunks, chunk;   // chunk: rows of a CTA
   float scale_log2;
   DiffHeads diff;
-  int32_t* tickets;                   // [units * n_heads], zero between calls; not used where max_chunks is 1
+  int32_t* tickets;                   // [units * n_heads], zero; not used where max_chunks is 1
   float* part_o;                      // [CTAs][kRows][D]
   float2* part_ml;                    // [CTAs][kRows] largest logit (log2), sum
 };
@@ -63,30 +123,23 @@ __device__ __forceinline__ uint32_t pack16(float lo, float hi) {
   asm("cvt.rn.f16x2.f32 %0, %1, %2;" : "=r"(r) : "f"(hi), "f"(lo));
   return r;
 }
-// Eight consecutive elements of a cached row as four pairs: bf16 as they lie, 8-bit integers as fp16.
+// Eight consecutive elements of a cached row, as they lie: four words of bf16 or two of stored bytes.
 template <bool Q8>
-__device__ __forceinline__ void load_piece(uint32_t (&x)[4], const uint8_t* pages, size_t element) {
-  if constexpr (Q8) {
-    const uint2 r = __ldg(reinterpret_cast<const uint2*>(pages + element));
-    x[0] = r.x, x[1] = r.y;           // (expanded where it is used, so that the load does not have to be waited for here)
-  } else {
-    const uint4 r = __ldg(reinterpret_cast<const uint4*>(pages + element * 2));
-    x[0] = r.x, x[1] = r.y, x[2] = r.z, x[3] = r.w;
+struct Piece {
+  uint32_t x[Q8 ? 2 : 4];
+  __device__ __forceinline__ void load(const uint8_t* pages, size_t element) {
+    if constexpr (Q8) {
+      const uint2 r = __ldg(reinterpret_cast<const uint2*>(pages + element));
+      x[0] = r.x, x[1] = r.y;
+    } else {
+      const uint4 r = __ldg(reinterpret_cast<const uint4*>(pages + element * 2));
+      x[0] = r.x, x[1] = r.y, x[2] = r.z, x[3] = r.w;
+    }
   }
-}
-template <bool Q8>
-__device__ __forceinline__ void expand(uint32_t (&x)[4]) {
-  if constexpr (Q8) {
-    const uint32_t lo = x[0], hi = x[1];
-    x[0] = int8x2_to_f16x2<0x5140>(lo);
-    x[1] = int8x2_to_f16x2<0x5342>(lo);
-    x[2] = int8x2_to_f16x2<0x5140>(hi);
-    x[3] = int8x2_to_f16x2<0x5342>(hi);
-  }
-}
+};
 
 template <int D, bool Q8>
-__global__ void __launch_bounds__(kThreads, 2) diff_decode_few_kernel(const Params p) {
+__global__ void __launch_bounds__(kThreads, 2) diff_decode_rows_kernel(const Params p) {
   constexpr int kPieces = D / 32;                    // pieces of eight columns that a lane has of a row
   __shared__ float s_o[kWarps][kRows][D];            // the warps' outputs, then in [0] the CTA's
   __shared__ float s_m[kWarps][kRows], s_l[kWarps][kRows];
@@ -98,30 +151,41 @@ __global__ void __launch_bounds__(kThreads, 2) diff_decode_few_kernel(const Para
   const int h = unit_head % p.n_heads, e = unit_head / p.n_heads, kvh = h / p.diff.subs;
   const size_t le = (size_t)p.layer_begin * p.batch + e;
   const int n = min(max(__ldg(&p.seq_lens[le]), 0), p.max_pages_per_seq * p.page_size);
-  const int n_chunks = max((n + kChunk - 1) / kChunk, 1);
+  const int n_chunks = max((n + p.chunk - 1) / p.chunk, 1);
   if (chunk >= n_chunks) return;
   const int n_rows = 2 * p.diff.heads(h);            // row 2 j + s is map s of head j
   const size_t head0 = (size_t)e * p.n_q_heads + p.diff.first_head(h);
-  // ---- page ids of this warp's 16 rows, then everything at once: rows gid and gid + 8, columns 8 (tig + 4 j) .. + 7
-  const int row0 = chunk * kChunk + 16 * warp, rows = min(16, n - row0);
-  uint32_t k[2][kPieces][4], v[2][kPieces][4];
+  // ---- this warp's tiles of 16 rows, kTile apart; of a tile a lane has rows gid and gid + 8, columns 8 (tig + 4 j) .. + 7
+  const int end = min(n, (chunk + 1) * p.chunk);
+  int row0 = chunk * p.chunk + 16 * warp;
+  Piece<Q8> k[2][kPieces], v[2][kPieces];
   float ks[2] = {1.f, 1.f}, vs[2] = {1.f, 1.f};
-  if (rows > 0) {
-    // (page_size is a multiple of 16: the 16 rows share a page)
-    const int page = min(max(__ldg(&p.block_table[le * p.max_pages_per_seq + row0 / p.page_size]), 0), p.n_pages - 1);
-    const size_t first = ((size_t)page * p.n_kv_heads + kvh) * p.page_size + row0 % p.page_size;
+  const int32_t* table = p.block_table + le * p.max_pages_per_seq;
+  // first row of a tile in the page pool (page_size is a multiple of 16: its rows share a page)
+  auto pool_row = [&](int at) -> size_t {
+    const int page = at < end ? min(max(__ldg(&table[at / p.page_size]), 0), p.n_pages - 1) : 0;
+    return ((size_t)page * p.n_kv_heads + kvh) * p.page_size + at % p.page_size + gid;
+  };
+  auto load_k = [&](size_t first) {
 #pragma unroll
     for (int y = 0; y < 2; ++y) {
-      const size_t row = first + gid + 8 * y;
 #pragma unroll
-      for (int j = 0; j < kPieces; ++j) load_piece<Q8>(k[y][j], p.k_pages, row * D + 8 * (tig + 4 * j));
-#pragma unroll
-      for (int j = 0; j < kPieces; ++j) load_piece<Q8>(v[y][j], p.v_pages, row * D + 8 * (tig + 4 * j));
-      if constexpr (Q8) {
-        ks[y] = __ldg(&p.k_scales[row]);
-        vs[y] = __ldg(&p.v_scales[row]);
-      }
+      for (int j = 0; j < kPieces; ++j) k[y][j].load(p.k_pages, (first + 8 * y) * D + 8 * (tig + 4 * j));
+      if constexpr (Q8) ks[y] = __ldg(&p.k_scales[first + 8 * y]);
     }
+  };
+  auto load_v = [&](size_t first) {
+#pragma unroll
+    for (int y = 0; y < 2; ++y) {
+#pragma unroll
+      for (int j = 0; j < kPieces; ++j) v[y][j].load(p.v_pages, (first + 8 * y) * D + 8 * (tig + 4 * j));
+      if constexpr (Q8) vs[y] = __ldg(&p.v_scales[first + 8 * y]);
+    }
+  };
+  size_t now = pool_row(row0);
+  if (row0 < end) {
+    load_k(now);
+    load_v(now);
   }
   // ---- the query row of this lane: the half that is not its map's is zero
   uint32_t q[kPieces][4];
@@ -136,67 +200,120 @@ __global__ void __launch_bounds__(kThreads, 2) diff_decode_few_kernel(const Para
       for (int i = 0; i < 4; ++i) q[j][i] = pack16<true>(bf16_lo(q[j][i]), bf16_hi(q[j][i]));
     }
   }
-  float m[2] = {-INFINITY, -INFINITY}, l[2] = {0.f, 0.f};     // of query rows 2 tig and 2 tig + 1
+  // 8-bit rows enter the products as kInt8Bias + integer (one instruction a pair): kInt8Bias times the query's sum comes off every logit,
+  // kInt8Bias times the sum of the weights off every output.  Both sums are products with ones, rounded like what they correct.
+  const uint32_t ones[4] = {0x3c003c00u, 0x3c003c00u, 0x3c003c00u, 0x3c003c00u};
+  float q_bias[4] = {0.f, 0.f, 0.f, 0.f}, w_sum[4] = {0.f, 0.f, 0.f, 0.f};
+  if constexpr (Q8) {
+#pragma unroll
+    for (int j = 0; j < kPieces; ++j) {
+      mma_f16(q_bias, ones, q[j][0], q[j][1]);
+      mma_f16(q_bias, ones, q[j][2], q[j][3]);
+    }
+  }
+  float m[2] = {-INFINITY, -INFINITY}, l[2] = {0.f, 0.f};     // of query rows 2 tig and 2 tig + 1; l: of this lane's rows
   float o[D / 16][4];
 #pragma unroll
   for (int x = 0; x < D / 16; ++x) o[x][0] = o[x][1] = o[x][2] = o[x][3] = 0.f;
-  if (rows > 0) {
+#pragma unroll 1
+  for (; row0 < end; row0 += kTile) {
+    const int rows = end - row0;
+    const bool more = row0 + kTile < end;
+    const size_t next = pool_row(row0 + kTile);
     float z[4] = {0.f, 0.f, 0.f, 0.f};
 #pragma unroll
-    for (int j = 0; j < kPieces; ++j) {
-      expand<Q8>(k[0][j]);
-      expand<Q8>(k[1][j]);
-      const uint32_t a0[4] = {k[0][j][0], k[1][j][0], k[0][j][1], k[1][j][1]};
-      const uint32_t a1[4] = {k[0][j][2], k[1][j][2], k[0][j][3], k[1][j][3]};
-      mma<Q8>(z, a0, q[j][0], q[j][1]);
-      mma<Q8>(z, a1, q[j][2], q[j][3]);
+    for (int j = 0; j < kPieces; ++j)
+#pragma unroll
+      for (int i = 0; i < 2; ++i) {
+        uint32_t a[4];
+        if constexpr (Q8) {
+          a[0] = int8x2_to_biased_f16x2<0x5140>(k[0][j].x[i]), a[1] = int8x2_to_biased_f16x2<0x5140>(k[1][j].x[i]);
+          a[2] = int8x2_to_biased_f16x2<0x5342>(k[0][j].x[i]), a[3] = int8x2_to_biased_f16x2<0x5342>(k[1][j].x[i]);
+        } else {
+          a[0] = k[0][j].x[2 * i], a[1] = k[1][j].x[2 * i], a[2] = k[0][j].x[2 * i + 1], a[3] = k[1][j].x[2 * i + 1];
+        }
+        mma<Q8>(z, a, q[j][2 * i], q[j][2 * i + 1]);
+      }
+#pragma unroll
+    for (int i = 0; i < 4; ++i) {
+      if constexpr (Q8) z[i] = fmaf(-kInt8Bias, q_bias[i], z[i]) * ks[i >> 1];
+      z[i] = gid + 8 * (i >> 1) < rows ? z[i] * p.scale_log2 : -INFINITY;
     }
+    if (more) load_k(next);           // under the softmax and the outputs
+    // the warp's reference is exact on its first tile and raised lazily (by 2^8) afterwards
+    float top[2] = {fmaxf(z[0], z[2]), fmaxf(z[1], z[3])};
+    if (__any_sync(0xffffffffu, top[0] > m[0] + kLazy || top[1] > m[1] + kLazy)) {
+      float al[2];
 #pragma unroll
-    for (int i = 0; i < 4; ++i) z[i] = gid + 8 * (i >> 1) < rows ? z[i] * ks[i >> 1] * p.scale_log2 : -INFINITY;
+      for (int i = 0; i < 2; ++i) {
 #pragma unroll
-    for (int i = 0; i < 2; ++i) {
-      m[i] = fmaxf(z[i], z[i + 2]);
+        for (int x = 4; x < 32; x <<= 1) top[i] = fmaxf(top[i], __shfl_xor_sync(0xffffffffu, top[i], x));
+        top[i] = fmaxf(top[i], m[i]);
+        al[i] = m[i] == -INFINITY ? 0.f : fast_exp2(m[i] - top[i]);
+        m[i] = top[i];
+        l[i] *= al[i];
+      }
 #pragma unroll
-      for (int x = 4; x < 32; x <<= 1) m[i] = fmaxf(m[i], __shfl_xor_sync(0xffffffffu, m[i], x));
+      for (int x = 0; x < D / 16; ++x) {
+        o[x][0] *= al[0];
+        o[x][1] *= al[1];
+        o[x][2] *= al[0];
+        o[x][3] *= al[1];
+      }
+#pragma unroll
+      for (int i = 0; i < 4; ++i) w_sum[i] *= al[i & 1];
     }
     float w[4];
 #pragma unroll
     for (int i = 0; i < 4; ++i) w[i] = fast_exp2(z[i] - (m[i & 1] == -INFINITY ? 0.f : m[i & 1]));
-#pragma unroll
-    for (int i = 0; i < 2; ++i) {
-      l[i] = w[i] + w[i + 2];
-#pragma unroll
-      for (int x = 4; x < 32; x <<= 1) l[i] += __shfl_xor_sync(0xffffffffu, l[i], x);
-    }
+    l[0] += w[0] + w[2];
+    l[1] += w[1] + w[3];
     // the weights as the B operand (rounded to 16 bits, 8-bit rows: times the row's scale); rows behind the last one: no weight
     // and no value, whatever lies there
+    if (rows < 16) {
 #pragma unroll
-    for (int y = 0; y < 2; ++y)
-      if (gid + 8 * y >= rows) {
-        vs[y] = 0.f;
+      for (int y = 0; y < 2; ++y)
+        if (gid + 8 * y >= rows) {
+          vs[y] = 0.f;
+          if constexpr (!Q8) {
 #pragma unroll
-        for (int j = 0; j < kPieces; ++j) v[y][j][0] = v[y][j][1] = v[y][j][2] = v[y][j][3] = Q8 ? 0x80808080u : 0u;
-      }
+            for (int j = 0; j < kPieces; ++j) v[y][j].x[0] = v[y][j].x[1] = v[y][j].x[2] = v[y][j].x[3] = 0u;
+          }
+        }
+    }
     const uint32_t b0 = movmatrix_trans(pack16<Q8>(Q8 ? w[0] * vs[0] : w[0], Q8 ? w[1] * vs[0] : w[1]));
     const uint32_t b1 = movmatrix_trans(pack16<Q8>(Q8 ? w[2] * vs[1] : w[2], Q8 ? w[3] * vs[1] : w[3]));
 #pragma unroll
-    for (int j = 0; j < kPieces; ++j) {
-      expand<Q8>(v[0][j]);
-      expand<Q8>(v[1][j]);
+    for (int j = 0; j < kPieces; ++j)
 #pragma unroll
       for (int i = 0; i < 2; ++i) {
-        const uint32_t a[4] = {movmatrix_trans(v[0][j][2 * i]), movmatrix_trans(v[0][j][2 * i + 1]),
-                               movmatrix_trans(v[1][j][2 * i]), movmatrix_trans(v[1][j][2 * i + 1])};
+        uint32_t a[4];
+        if constexpr (Q8) {           // two neighbouring columns travel as one 16-bit element
+          const uint32_t t0 = movmatrix_trans(v[0][j].x[i]), t1 = movmatrix_trans(v[1][j].x[i]);
+          a[0] = int8x2_to_biased_f16x2<0x5240>(t0), a[1] = int8x2_to_biased_f16x2<0x5341>(t0);
+          a[2] = int8x2_to_biased_f16x2<0x5240>(t1), a[3] = int8x2_to_biased_f16x2<0x5341>(t1);
+        } else {
+          a[0] = movmatrix_trans(v[0][j].x[2 * i]), a[1] = movmatrix_trans(v[0][j].x[2 * i + 1]);
+          a[2] = movmatrix_trans(v[1][j].x[2 * i]), a[3] = movmatrix_trans(v[1][j].x[2 * i + 1]);
+        }
         mma<Q8>(o[2 * j + i], a, b0, b1);
       }
-    }
+    if constexpr (Q8) mma_f16(w_sum, ones, b0, b1);
+    if (more) load_v(next);           // under the next tile's logits
   }
-  // accumulator row gid (+ 8) of block (j, i) is column 8 (gid / 2 + 4 j) + 4 i + gid % 2 (+ 2)
+#pragma unroll
+  for (int i = 0; i < 2; ++i)
+#pragma unroll
+    for (int x = 4; x < 32; x <<= 1) l[i] += __shfl_xor_sync(0xffffffffu, l[i], x);
+  // accumulator row gid of block (j, i) is column 8 (gid / 2 + 4 j) + 4 i + gid % 2, row gid + 8 the one 2 further; 8-bit rows: + 2 (gid % 2),
+  // and the next one
 #pragma unroll
   for (int x = 0; x < D / 16; ++x)
 #pragma unroll
-    for (int i = 0; i < 4; ++i)
-      s_o[warp][2 * tig + (i & 1)][8 * ((gid >> 1) + 4 * (x >> 1)) + 4 * (x & 1) + 2 * (i >> 1) + (gid & 1)] = o[x][i];
+    for (int i = 0; i < 4; ++i) {
+      const int col = 8 * ((gid >> 1) + 4 * (x >> 1)) + 4 * (x & 1) + (Q8 ? 2 * (gid & 1) + (i >> 1) : 2 * (i >> 1) + (gid & 1));
+      s_o[warp][2 * tig + (i & 1)][col] = Q8 ? fmaf(-kInt8Bias, w_sum[i], o[x][i]) : o[x][i];
+    }
   if (gid == 0) {
 #pragma unroll
     for (int i = 0; i < 2; ++i) {
@@ -314,29 +431,67 @@ __global__ void __launch_bounds__(kThreads, 2) diff_decode_few_kernel(const Para
 
 template <int D, bool Q8>
 xkv_status launch(const Params& p, int ctas, cudaStream_t st) {
-  diff_decode_few_kernel<D, Q8><<<ctas, kThreads, 0, st>>>(p);
+  diff_decode_rows_kernel<D, Q8><<<ctas, kThreads, 0, st>>>(p);
   count_launch();
   return check_launch();
 }
 
-int64_t few_ctas(const xkv_dims& streamed, int n_layers, int max_cache_len) {
-  return (int64_t)n_layers * streamed.batch * streamed.n_kv_heads * std::max(1, (max_cache_len + kChunk - 1) / kChunk);
+struct Cut {
+  int chunk, max_chunks;              // rows of a CTA, CTAs of the longest cache that its table allows
+  int64_t ctas;
+};
+// As many chunks as fill the SMs once, but no more than about the root of eight times a cache's tiles: one CTA joins them, at some
+// 0.2 us a chunk, where a tile takes 1.5 us (32 000 rows of one KV head: 251 chunks 59 us, 42 chunks 25 us).
+Cut cut(const xkv_dims& streamed, int n_layers, int max_cache_len) {
+  const int64_t caches = (int64_t)n_layers * streamed.batch * streamed.n_kv_heads;
+  const int64_t tiles = std::max(1, (max_cache_len + kTile - 1) / kTile);
+  int64_t per = std::max<int64_t>(1, (caches * tiles + kMaxCtas - 1) / kMaxCtas);
+  while (per * per * 8 < tiles) ++per;
+  Cut c;
+  c.max_chunks = (int)((tiles + per - 1) / per);
+  c.chunk = (int)((tiles + c.max_chunks - 1) / c.max_chunks) * kTile;
+  c.ctas = caches * c.max_chunks;
+  return c;
 }
 
 }  // namespace
 
-bool diff_decode_is_few(const xkv_dims* streamed, int n_layers, int max_cache_len, int64_t max_rows) {
-  const int64_t ctas = few_ctas(*streamed, n_layers, max_cache_len);
-  if (ctas > kMaxCtas) return false;
-  return max_cache_len <= kChunk ||
-         ((int64_t)n_layers * streamed->batch * streamed->n_kv_heads <= kTickets && ctas * kRows <= max_rows);
+// Whether this kernel or the streaming one takes a call.  Device time of both, us:
+//   bf16, G = 4, d = 128: 8 caches of 2129 rows 13.0 / 30.5, 64 of 2000 24.3 / 37.8, 2048 of 1000 193 / 214, 4096 of 1500 530 / 566
+//   int8, the same: 12.5 / 47.9, 21.0 / 51.3, 124 / 152, 320 / 402;  int8, G = 1: 2048 of 1000 121 / 143
+// It loses where there are many caches and little to each (2048 of 120 rows 54 / 37: a CTA's chain of latencies takes 7 us), and with
+// one head a KV head over many bf16 caches (2048 of 1000 190 / 183).
+bool diff_decode_by_rows(const xkv_dims* streamed, int n_layers, int max_cache_len, bool q8, int64_t max_rows) {
+  const int64_t caches = (int64_t)n_layers * streamed->batch * streamed->n_kv_heads;
+  if (caches >= kManyCaches && (max_cache_len <= 2 * kTile || (!q8 && streamed->n_q_heads == 2 * streamed->n_kv_heads))) return false;
+  const Cut c = cut(*streamed, n_layers, max_cache_len);
+  return c.ctas < (1 << 30) && (c.max_chunks == 1 || c.ctas * kRows <= max_rows);
 }
 
-xkv_status diff_decode_few(const xkv_dims* d, const xkv_cache* c, int layer_begin, int n_layers, const void* q, void* out,
-                           float* lse, const DiffHeads& diff, const DecodeScratch& ws, cudaStream_t st) {
+xkv_status diff_decode_rows(const xkv_dims* d, const xkv_cache* c, int layer_begin, int n_layers, const void* q,
+                           const void* k_new, const void* v_new, void* out, float* lse, const DiffHeads& diff,
+                           const DecodeScratch& ws, cudaStream_t st) {
+  const bool q8 = c->kv_format == XKV_KV_INT8, wide = d->head_dim == 128;
+  if (k_new != nullptr) {
+    const AppendParams a = {static_cast<const __nv_bfloat16*>(k_new), static_cast<const __nv_bfloat16*>(v_new),
+                            static_cast<uint8_t*>(c->k_pages), static_cast<uint8_t*>(c->v_pages), c->k_scales, c->v_scales,
+                            c->block_table, c->seq_lens, layer_begin, d->batch, d->n_kv_heads, c->page_size,
+                            c->max_pages_per_seq, c->n_pages, static_cast<WorkspaceHeader*>(ws.header)};
+    const int units = n_layers * d->batch;
+    if (wide) {
+      if (q8) append_kernel<128, true><<<units, kThreads, 0, st>>>(a);
+      else    append_kernel<128, false><<<units, kThreads, 0, st>>>(a);
+    } else {
+      if (q8) append_kernel<64, true><<<units, kThreads, 0, st>>>(a);
+      else    append_kernel<64, false><<<units, kThreads, 0, st>>>(a);
+    }
+    count_launch();
+    const xkv_status s = check_launch();
+    if (s != XKV_OK) return s;
+  }
   const int max_cache_len = c->max_pages_per_seq * c->page_size;
   const xkv_dims streamed = streamed_dims(d, diff);
-  const int64_t ctas = few_ctas(streamed, n_layers, max_cache_len);
+  const Cut how = cut(streamed, n_layers, max_cache_len);
   Params p;
   p.q = static_cast<const __nv_bfloat16*>(q);
   p.out = static_cast<__nv_bfloat16*>(out);
@@ -355,15 +510,21 @@ xkv_status diff_decode_few(const xkv_dims* d, const xkv_cache* c, int layer_begi
   p.page_size = c->page_size;
   p.max_pages_per_seq = c->max_pages_per_seq;
   p.n_pages = c->n_pages;
-  p.max_chunks = std::max(1, (max_cache_len + kChunk - 1) / kChunk);
+  p.max_chunks = how.max_chunks;
+  p.chunk = how.chunk;
   p.scale_log2 = (d->scale != 0.f ? d->scale : 1.0f / sqrtf((float)(d->head_dim / 2))) * 1.4426950408889634f;
   p.diff = diff;
-  p.tickets = static_cast<WorkspaceHeader*>(ws.header)->few_tickets;
+  // Tickets that stay zero between calls, where they suffice; others are cleared first (a launch more, 2 us).
+  p.tickets = static_cast<WorkspaceHeader*>(ws.header)->row_tickets;
+  const int64_t caches = (int64_t)n_layers * d->batch * p.n_heads;
+  if (p.max_chunks > 1 && caches > kTickets) {
+    p.tickets = ws.tickets;
+    if (cudaMemsetAsync(p.tickets, 0, caches * 4, st) != cudaSuccess) return XKV_ERR_CUDA;
+  }
   p.part_o = ws.part_o;
   p.part_ml = reinterpret_cast<float2*>(ws.part_ml);
-  const bool q8 = c->kv_format == XKV_KV_INT8;
-  if (d->head_dim == 128) return q8 ? launch<128, true>(p, (int)ctas, st) : launch<128, false>(p, (int)ctas, st);
-  return q8 ? launch<64, true>(p, (int)ctas, st) : launch<64, false>(p, (int)ctas, st);
+  if (wide) return q8 ? launch<128, true>(p, (int)how.ctas, st) : launch<128, false>(p, (int)how.ctas, st);
+  return q8 ? launch<64, true>(p, (int)how.ctas, st) : launch<64, false>(p, (int)how.ctas, st);
 }
 
 }  // namespace xkv

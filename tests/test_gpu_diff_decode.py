@@ -85,8 +85,8 @@ def test_cut_caches_are_joined(fmt, chunk, G):
 
 
 @pytest.mark.parametrize("fmt", ["bf16", "int8", "e4m3"])
-@pytest.mark.parametrize("G", [2, 8])
-def test_new_rows_are_appended_first(fmt, G):
+@pytest.mark.parametrize("G,chunk", [(2, 0), (8, 0), (2, 256), (8, 64)])
+def test_new_rows_are_appended_first(fmt, G, chunk):
     """As xkv_decode_attn appends: the same pages, scales and lengths behind it, and the new row takes part."""
     L, B, H, d, page = 2, 4, 2, 64, 16
     lens = [[0, 15, 16, 31], [100, 1, 47, 64]]
@@ -99,15 +99,14 @@ def test_new_rows_are_appended_first(fmt, G):
                      device=DEV)
     for _ in range(2):
         kn, vn = (torch.randn(L, B, H, d, generator=g).to(torch.bfloat16).to(DEV) for _ in range(2))
-        out, sums = attend(c, H * G, q, lam, gain, kn, vn)
+        out, sums = attend(c, H * G, q, lam, gain, kn, vn, chunk=chunk)
         xkv.decode_attn(dims, twin.handle(), 0, L, q1, kn, vn, torch.empty_like(q1), None, 0, ws)
         torch.cuda.synchronize()
         assert torch.equal(c.d_lens, twin.d_lens)
         for a, b in zip(c.pages + c.scales, twin.pages + twin.scales):
             if a is not None:
                 assert torch.equal(a.view(torch.uint8), b.view(torch.uint8))
-        # the rows are in the pages now: the same values (from the same kernel: with chunks given, the one that also appends)
-        after, _ = attend(c, H * G, q, lam, gain, chunk=256)
+        after, _ = attend(c, H * G, q, lam, gain, chunk=chunk)           # the rows are in the pages now: the same values
         assert torch.equal(after, out)
 
 
@@ -120,7 +119,11 @@ def test_some_layers_scale_and_many_units(fmt):
     q = queries(L, B, G, d, 6)
     out, sums = attend(c, G, q, lam, gain, scale=0.3)
     check(c, G, q, lam, gain, out, sums, every=17, scale=float(np.float32(0.3)))
-    part, ps = attend(c, G, q[2:4].contiguous(), lam[2:4].contiguous(), gain[2:4].contiguous(), l0=2, l1=4, scale=0.3)
+    args = q[2:4].contiguous(), lam[2:4].contiguous(), gain[2:4].contiguous()
+    part, ps = attend(c, G, *args, l0=2, l1=4, scale=0.3)              # (fewer caches: not the same kernel for every format)
+    check(c, G, *args, part, ps, l0=2, every=17, scale=float(np.float32(0.3)))
+    out, sums = attend(c, G, q, lam, gain, scale=0.3, chunk=64)        # with chunks given, one kernel serves both
+    part, ps = attend(c, G, *args, l0=2, l1=4, scale=0.3, chunk=64)
     assert torch.equal(part, out[2:4]) and torch.equal(ps, sums[2:4])
 
 
