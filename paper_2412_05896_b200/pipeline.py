@@ -3,7 +3,7 @@ memory and streams only) and drives the four library entry points in order.
 
     sess = XkvSession(...); sess.prefill(q_win, k, v, total=...); sess.decode(q, k_new, v_new)
 
-Every computation happens inside libxkv.so; this file allocates, copies and calls.
+Every computation happens inside libxkv.so; this file allocates, copies and calls (and lays out a few counts).
 """
 from __future__ import annotations
 
@@ -18,6 +18,9 @@ from . import xkv
 
 
 class XkvSession:
+    # (until caches are forked pages are handed out in their order, each to one cache)
+    free_pages = shares = None
+
     def __init__(self, n_layers: int, n_q_heads: int, n_kv_heads: int, head_dim: int, window: int,
                  pool_kernel: int, lengths: list[int], pool_mode: int = xkv.POOL_MAX, page_size: int = 16,
                  max_new_tokens: int = 0, max_budget: int | None = None, total_budget: int | None = None,
@@ -120,7 +123,8 @@ class XkvSession:
         # decode sees the head-level caches as B*Hkv sequences of one KV head with G query heads each
         self.dec_dims = self.dims if not self.head_level else xkv.Dims(
             self.n_caches, self.G, 1, head_dim, window, pool_kernel, pool_mode, scale, head_dim, head_dim)
-        self.ws_plan = self.ws_store = None
+        self.ws_plan = self.ws_store = self.ws_fork = self.ws_compact = self.ws_copy = None
+        self.live = [True] * self.B                          # sequences that take part in a step with new rows
         if self.pages_on_demand:
             self.pages_used = torch.zeros(1, dtype=torch.int32, device=self.device)
             self.one_each = torch.ones(self.n_caches, dtype=torch.int32, device=self.device)   # a step's new rows
@@ -132,6 +136,7 @@ class XkvSession:
                                                       chunk_rows=decode_chunk_rows))
         self.out = torch.empty(n_layers, self.B, n_q_heads, head_dim, **bf16)
         self.lse = torch.empty(n_layers, self.B, n_q_heads, **f32)
+        self.ws_diff_decode = self.ws_diff_prefill = self.diff_lse = None
         self.budgets: np.ndarray | None = None
         self.last_solver_ms: float | None = None      # host time of the last xkv_alloc_budgets call
         self.r_avg: float | None = None
@@ -228,6 +233,30 @@ class XkvSession:
             self.ws_prefill = self._ws(xkv.workspace_bytes(xkv.OP_PREFILL_ATTN, self.dims))
         xkv.prefill_attn(self.dims, q, k, v, self.cu, self.T, self.max_seqlen, out, lse, self.ws_prefill)
         return out, lse
+
+    def diff_prefill_attention(self, q: torch.Tensor, k: torch.Tensor, v: torch.Tensor, lam: torch.Tensor,
+                               gain: torch.Tensor | None = None, eps: float = 1e-5, out: torch.Tensor | None = None,
+                               lse: torch.Tensor | None = None):
+        """prefill_attention of heads that attend by the difference of two softmax maps: rows of q [q1 | q2], of k
+        [k1 | k2]; lam fp32 [Hq], gain fp32 [d] (the heads' norm) or None -> (out [T, Hq, d] bf16, lse [Hq, 2, T] fp32)."""
+        self._check_diff(lam, gain, (self.Hq,), (self.d,))
+        if out is None:
+            out = torch.empty_like(q)
+        if lse is None:
+            lse = torch.empty(self.Hq, 2, self.T, dtype=torch.float32, device=self.device)
+        if self.ws_diff_prefill is None:
+            self.ws_diff_prefill = self._ws(xkv.workspace_bytes(xkv.OP_DIFF_PREFILL_ATTN, self.dims))
+        xkv.diff_prefill_attn(self.dims, q, k, v, lam, gain, eps, self.cu, self.T, self.max_seqlen, out, lse,
+                              self.ws_diff_prefill)
+        return out, lse
+
+    def _check_diff(self, lam, gain, heads: tuple, norm: tuple) -> None:
+        for x, shape, name in ((lam, heads, "lam"), (gain, norm, "gain")):
+            if x is None and name == "gain":
+                continue
+            if not isinstance(x, torch.Tensor) or tuple(x.shape) != shape or x.dtype != torch.float32 \
+                    or x.device != self.k_pages.device or not x.is_contiguous():
+                raise ValueError(f"{name} is a contiguous fp32 {list(shape)} tensor on {self.k_pages.device}")
 
     def select_layers(self, budgets, k: list[torch.Tensor], v: list[torch.Tensor]) -> None:
         """select_layer for every layer under one budget per layer ([L]), or per (layer, KV head) ([L, Hkv]) with
@@ -333,6 +362,9 @@ class XkvSession:
             n = -(-rows // self.page_size)
             if int(n[n <= self.max_pages_per_seq].sum()) > self.n_pages:   # (longer caches get nothing: select_layer's status)
                 raise RuntimeError("page pool too small for these budgets")
+            self.live = [True] * self.B
+            if self.free_pages is not None:                  # all pages are free again
+                self._reset_pages()
             xkv.plan_append(self.cache, self.n_caches, self._to_device(rows), self.n_caches, None, None, self.n_pages, None,
                             self.pages_used, None, 0, self.ws_plan)
             return
@@ -383,6 +415,7 @@ class XkvSession:
             raise ValueError("append: n_new is one count per sequence")
         T = int(n_new.sum())
         self._check_rows(k, v, T)
+        self.live = [a or int(n) > 0 for a, n in zip(self.live, n_new)]
         counts = n_new
         if self.head_level:                                  # caches (b, g): a sequence's tokens head by head
             counts = np.repeat(n_new, self.Hkv)
@@ -404,7 +437,7 @@ class XkvSession:
         """counts: dev int32, rows to come of each of a layer's caches; k, v: [L, n_tokens, ..] in that order."""
         self.join()
         slots = torch.empty(self.L, n_tokens, dtype=torch.int64, device=self.device)
-        xkv.plan_append(self.cache, self.n_caches, counts, 0, self.seq_lens, None, self.n_pages, self.pages_used,
+        xkv.plan_append(self.cache, self.n_caches, counts, 0, self.seq_lens, self.free_pages, self.n_pages, self.pages_used,
                         self.pages_used, slots if n_tokens else None, n_tokens, self.ws_plan)
         # the layers' tokens are one list: their rows lie one after the other and so do their slots
         if n_tokens:
@@ -418,25 +451,164 @@ class XkvSession:
         self.join()
         out = self.out if out is None else out
         layer_end = self.L if layer_end is None else layer_end
-        if self.pages_on_demand and k_new is not None:
-            if (layer_begin, layer_end) != (0, self.L):
-                raise ValueError("with pages_on_demand a step plans all layers: append first, then decode layer by layer")
-            # one row a cache, head by head in a head-level session: the order in which the rows lie
-            self._check_rows(k_new, v_new, self.B)
-            self._store_new(k_new, v_new, self.one_each, self.n_caches)
-            k_new = v_new = None
+        k_new, v_new = self._store_step(k_new, v_new, layer_begin, layer_end)
         xkv.decode_attn(self.dec_dims, self.cache, layer_begin, layer_end, q, k_new, v_new, out,
                         self.lse if lse is None else lse,
                         self.chunk_rows if chunk_rows is None else chunk_rows, self.ws_decode)
         return out
 
+    def _store_step(self, k_new, v_new, layer_begin: int, layer_end: int):
+        """A step's new rows: stored here with pages_on_demand (those of live sequences), else left to the attention."""
+        if not self.pages_on_demand or k_new is None:
+            return k_new, v_new
+        if (layer_begin, layer_end) != (0, self.L):
+            raise ValueError("with pages_on_demand a step plans all layers: append first, then decode layer by layer")
+        self._check_rows(k_new, v_new, self.B)
+        if all(self.live):
+            # one row a cache, head by head in a head-level session: the order in which the rows lie
+            self._store_new(k_new, v_new, self.one_each, self.n_caches)
+        elif any(self.live):
+            rows = self._to_device(np.flatnonzero(self.live), np.int64)
+            counts = np.repeat(np.asarray(self.live, dtype=np.int32), self.n_caches // self.B)
+            self._store_new(k_new[:, rows], v_new[:, rows], self._to_device(counts), int(counts.sum()))
+        return None, None
+
+    def diff_decode(self, q: torch.Tensor, k_new: torch.Tensor | None, v_new: torch.Tensor | None, lam: torch.Tensor,
+                    gain: torch.Tensor | None = None, eps: float = 1e-5, out: torch.Tensor | None = None,
+                    lse: torch.Tensor | None = None, layer_begin: int = 0, layer_end: int | None = None,
+                    chunk_rows: int | None = None) -> torch.Tensor:
+        """decode of heads that attend by the difference of two softmax maps: q rows [q1 | q2], cached K rows [k1 | k2];
+        lam fp32 [layers, Hq], gain fp32 [layers, d] (the heads' norm) or None, lse fp32 [layers, B, Hq, 2]."""
+        if self.head_level:
+            raise ValueError("diff_decode: lam is given per head of a layer, head-level caches are read as sequences of their own")
+        self.join()
+        layer_end = self.L if layer_end is None else layer_end
+        n = layer_end - layer_begin
+        self._check_diff(lam, gain, (n, self.Hq), (n, self.d))
+        out = self.out if out is None else out
+        if self.ws_diff_decode is None:
+            self.ws_diff_decode = self._ws(xkv.workspace_bytes(
+                xkv.OP_DIFF_DECODE_ATTN, self.dec_dims, n_layers=self.L,
+                max_cache_len=self.max_pages_per_seq * self.page_size, chunk_rows=self.chunk_rows))
+            self.diff_lse = torch.empty(self.L, self.B, self.Hq, 2, dtype=torch.float32, device=self.device)
+        k_new, v_new = self._store_step(k_new, v_new, layer_begin, layer_end)
+        xkv.diff_decode_attn(self.dec_dims, self.cache, layer_begin, layer_end, q, k_new, v_new, lam, gain, eps, out,
+                             self.diff_lse if lse is None else lse,
+                             self.chunk_rows if chunk_rows is None else chunk_rows, self.ws_diff_decode)
+        return out
+
+    # ------------------------------------------------------------------ caches that share pages
+    def _reset_pages(self) -> None:
+        self.free_pages = torch.arange(self.n_pages, dtype=torch.int32, device=self.device)
+        self.shares = torch.zeros(self.n_pages, dtype=torch.int32, device=self.device)
+
+    def _per_cache(self, x, name: str, layers: bool) -> torch.Tensor:
+        """Host integers or a dev int32 tensor, [B] (or [L, B]), as dev int32 of a layer's caches."""
+        if isinstance(x, torch.Tensor):
+            if x.dtype != torch.int32 or x.device != self.k_pages.device:
+                raise ValueError(f"{name}: host integers or an int32 tensor on {self.k_pages.device}")
+        else:
+            x = np.asarray(x)
+            if x.dtype.kind not in "iu":
+                raise ValueError(f"{name}: integers")
+        if tuple(x.shape) != (self.B,) and not (layers and tuple(x.shape) == (self.L, self.B)):
+            raise ValueError(f"{name}: one count per sequence" + (" or per layer and sequence" if layers else ""))
+        x = x if isinstance(x, torch.Tensor) else self._to_device(np.clip(x, -1, 2 ** 31 - 1))
+        return x.repeat_interleave(self.Hkv, dim=-1) if self.head_level else x.contiguous()
+
+    def fork(self, parent, keep=None) -> None:
+        """Sequence b goes on as sequence parent[b] (samples of one prompt, beams, a request that starts from another's
+        cache), sharing its pages; -1 frees it.  keep: rows of a cache that stay, [B] or [L, B], negative: all.  Host
+        integers or dev int32 tensors.  A freed sequence takes no part in later steps until it goes on as another one or
+        append gives it rows -- where parent is host integers: a tensor is not read here, and then every sequence takes part
+        (a freed one begins again with the next step's row).  Needs pages_on_demand; device_status("pages")."""
+        if not self.pages_on_demand:
+            raise ValueError("fork needs a session with pages_on_demand=True")
+        live = [True] * self.B
+        if not isinstance(parent, torch.Tensor):
+            parent = np.asarray(parent)
+            if parent.shape == (self.B,) and (int(parent.min()) < -1 or int(parent.max()) >= self.B):
+                raise ValueError("fork: a parent is a sequence of the batch, or -1")
+            live = [int(a) >= 0 and self.live[int(a)] for a in parent.ravel()]
+        par = self._per_cache(parent, "fork: parent", layers=False)
+        if self.head_level:
+            heads = torch.arange(self.Hkv, dtype=torch.int32, device=self.device).repeat(self.B)
+            par = torch.where(par == -1, par, par * self.Hkv + heads)
+        kept = None if keep is None else self._per_cache(keep, "fork: keep", layers=True)
+        self._fork(par, kept)
+        self.live = live
+
+    def cut(self, n_rows) -> None:
+        """The last n_rows[b] rows of every cache of sequence b are taken back (drafted tokens that were rejected): host
+        integers or a dev int32 tensor [B].  Needs pages_on_demand; device_status("pages")."""
+        if not self.pages_on_demand:
+            raise ValueError("cut needs a session with pages_on_demand=True")
+        if not isinstance(n_rows, torch.Tensor) and np.asarray(n_rows).size and int(np.asarray(n_rows).min()) < 0:
+            raise ValueError("cut: counts are not negative")
+        drop = self._per_cache(n_rows, "cut", layers=False)
+        same = torch.arange(self.n_caches, dtype=torch.int32, device=self.device)
+        self.join()
+        self._fork(same, (self.seq_lens - drop.clamp(min=0)).clamp(min=0))
+
+    def _fork(self, parent: torch.Tensor, keep: torch.Tensor | None) -> None:
+        self.join()
+        if self.free_pages is None:
+            self._reset_pages()
+        if self.ws_fork is None:
+            self.ws_fork = self._ws(xkv.workspace_bytes(xkv.OP_FORK_CACHES, self.dec_dims, max_seqlen=self.max_pages_per_seq,
+                                                        total_tokens=self.n_pages, n_layers=self.L))
+        stride = 0 if keep is None or keep.dim() == 1 else self.n_caches
+        xkv.fork_caches(self.dec_dims, self.cache, parent, keep, stride, self.shares, self.free_pages, self.n_pages,
+                        self.pages_used, self.ws_fork)
+
+    def compact(self) -> None:
+        """Moves the pages in use to the front of the pool.  Needs pages_on_demand; device_status("pages")."""
+        if not self.pages_on_demand:
+            raise ValueError("compact needs a session with pages_on_demand=True")
+        self.join()
+        if self.ws_compact is None:
+            self.ws_compact = self._ws(xkv.workspace_bytes(xkv.OP_COMPACT_PAGES, self.dec_dims,
+                                                           max_seqlen=self.max_pages_per_seq, total_tokens=self.n_pages,
+                                                           n_layers=self.L))
+        xkv.compact_pages(self.dec_dims, self.cache, self.block_table, self.shares, self.shares, self.free_pages,
+                          self.pages_used, self.ws_compact)
+
+    def resize_pool(self, n_pages: int) -> None:
+        """The pages in use in a new pool of n_pages, the old one given up (waits for the device).  Needs
+        pages_on_demand; ValueError, and the pool as it was, when they do not fit; an error that device_status("pages") has
+        not reported yet is raised."""
+        self.compact()
+        used, st = int(self.pages_used.item()), self.device_status("pages")
+        if st != xkv.OK:
+            raise xkv.XkvError(st, "resize_pool")
+        if not max(used, 1) <= n_pages < 2 ** 31:
+            raise ValueError(f"resize_pool: {used} pages are in use")
+        if self.free_pages is None:
+            self._reset_pages()
+        old, old_cache = (self.k_pages, self.v_pages, self.k_scales, self.v_scales), self.cache
+        new = [None if x is None else torch.zeros(n_pages, *x.shape[1:], dtype=x.dtype, device=x.device) for x in old]
+        ptrs = [None if x is None else x.data_ptr() for x in new]
+        cache = xkv.Cache(ptrs[0], ptrs[1], self.block_table.data_ptr(), self.seq_lens.data_ptr(), self.L, self.page_size,
+                          self.max_pages_per_seq, n_pages, ptrs[2], ptrs[3], self.kv_format, 0)
+        ids = torch.arange(n_pages, dtype=torch.int32, device=self.device)
+        if used:
+            if self.ws_copy is None:
+                self.ws_copy = self._ws(xkv.workspace_bytes(xkv.OP_COPY_PAGES, self.dec_dims))
+            xkv.copy_pages(self.dec_dims, old_cache, ids, cache, ids, used, self.ws_copy)
+        self.k_pages, self.v_pages, self.k_scales, self.v_scales = new
+        shares = torch.zeros(n_pages, dtype=torch.int32, device=self.device)
+        shares[:used] = self.shares[:used]
+        self.cache, self.n_pages, self.free_pages, self.shares = cache, n_pages, ids, shares
+        self.ws_fork = self.ws_compact = None                # sized by the pool
+
     def device_status(self, which: str = "decode") -> int:
         """First error any call of that kind recorded since the last check (the status words are sticky and
         reading resets them), XKV_OK otherwise."""
         self.join()
-        ws = {"decode": [self.ws_decode], "score": self.ws_score, "select": self.ws_select,
-              "prefill": [] if self.ws_prefill is None else [self.ws_prefill],
-              "append": [] if self.ws_plan is None else [self.ws_plan, self.ws_store]}[which]
+        some = lambda *ws: [w for w in ws if w is not None]  # noqa: E731
+        ws = {"decode": some(self.ws_decode, self.ws_diff_decode), "score": self.ws_score, "select": self.ws_select,
+              "prefill": some(self.ws_prefill, self.ws_diff_prefill), "append": some(self.ws_plan, self.ws_store),
+              "pages": some(self.ws_fork, self.ws_compact, self.ws_copy)}[which]
         first = xkv.OK
         for w in ws:
             st = xkv.read_device_status(w)
