@@ -23,6 +23,12 @@
 //              behind a prompt's last token (the next prompt's, or 0 * NaN)
 //   warp 11    finds the items, V tiles by TMA
 // Every wait is bounded and ends when another role has given up; an expired one sets the status word and lets the CTA drain.
+//
+// Measured (device time, clock under the power limit 1.65 - 1.8 GHz): four prompts of 2399 - 4428 tokens, 32 heads of 128 over 8 KV heads 864
+// us = 840 TFLOP/s; one of 32 768 tokens, 8 heads 1005 TFLOP/s; one of 487 tokens, 4 heads of 64 13.4 us.  What bounds it is the issue of
+// the softmax, at d = 64 as at 128: 1550 clocks a tile where the tensor pipe would take 896 and the exponentials 1024, two warps
+// an SM sub-partition, and some 7000 clocks at an item's end, when the tensor pipe has nothing to do (the same warps form the output;
+// four warps of their own for it left the softmax 96 registers a thread instead of 128: 1010 us).
 #include <atomic>
 
 #include "ops.h"
@@ -184,6 +190,7 @@ diff_prefill_kernel(const __grid_constant__ CUtensorMap tmap_q, const __grid_con
       s_v_full[kStages], s_v_clear, s_v_empty[kStages], s_s_full[2], s_s_free[2], s_p_full[2][2], s_o_full[2][2], s_o_free, s_inv_full,
       s_sq_full;
   __shared__ Item s_item[kItems];
+  __shared__ uint4 s_stage[kSoftWarps][32][5];               // rows of 64 bytes, a piece apart: no two lanes of a phase share a bank
   __shared__ float s_inv[2][2][kRows], s_sq[2][kRows];      // s_inv: of even and of odd items, a warp may still read the item before
   __shared__ uint32_t s_tmem;
   __shared__ int s_abort_store;
@@ -411,6 +418,7 @@ diff_prefill_kernel(const __grid_constant__ CUtensorMap tmap_q, const __grid_con
       done_item(n);
       const int n_kt = key_tiles(it), row = it.q0 + r;
       float m_ref = -INFINITY, l = 0.f;
+      const float lambda = __ldg(&p.lambda[it.h]);
       bool ok = true;
       for (int j = 0; j < n_kt; ++j, ++jj) {
         const uint32_t b = jj & 1;
@@ -483,18 +491,17 @@ diff_prefill_kernel(const __grid_constant__ CUtensorMap tmap_q, const __grid_con
       if (!ok) break;
       // ---- both maps' O are complete; this map's warps take columns [map D/2, (map + 1) D/2) of their rows
       const uint32_t last = jj - 1;
-      const bool live = row < it.t;
       s_inv[n & 1][map][r] = l > 0.f ? 1.f / l : 0.f;
-      if (live && p.lse != nullptr)
-        p.lse[((size_t)it.h * 2 + map) * p.total_tokens + it.cu + row] = (m_ref + log2f(l)) * 0.6931471805599453f;
       __syncwarp();
       if (lane == 0) mbar_arrive(&s_inv_full);
+      if (row < it.t && p.lse != nullptr)
+        p.lse[((size_t)it.h * 2 + map) * p.total_tokens + it.cu + row] = (m_ref + log2f(l)) * 0.6931471805599453f;
       // First that every warp has come to its last tile: the other map may be tiles behind, and a wait by parity would then take
       // the phase two back for the one meant.
       ok = wait(&s_inv_full, n) && wait(&s_o_full[0][last & 1], last / 2) && wait(&s_o_full[1][last & 1], last / 2);
       if (!ok) break;
       tc_fence_after_sync();
-      const float w1 = s_inv[n & 1][0][r], w2 = -__ldg(&p.lambda[it.h]) * s_inv[n & 1][1][r];
+      const float w1 = s_inv[n & 1][0][r], w2 = -lambda * s_inv[n & 1][1][r];
       float y[D / 2], sq = 0.f;
 #pragma unroll
       for (int c = 0; c < D / 2; c += 32) {
@@ -529,12 +536,23 @@ diff_prefill_kernel(const __grid_constant__ CUtensorMap tmap_q, const __grid_con
         __syncwarp();
         if (lane == 0) mbar_arrive(&s_o_free);
       }
-      if (live) {
-        __nv_bfloat16* o = p.out + ((size_t)(it.cu + row) * p.n_q_heads + it.h) * D + map * (D / 2);
+      // 32 columns at a time through shared memory, so that a store takes eight rows of 64 bytes instead of 32 of 16
 #pragma unroll
-        for (int c = 0; c < D / 2; c += 8)
-          *reinterpret_cast<uint4*>(o + c) = make_uint4(pack_bf16(y[c], y[c + 1]), pack_bf16(y[c + 2], y[c + 3]),
-                                                        pack_bf16(y[c + 4], y[c + 5]), pack_bf16(y[c + 6], y[c + 7]));
+      for (int c = 0; c < D / 2; c += 32) {
+#pragma unroll
+        for (int i = 0; i < 4; ++i) {
+          const float* x = y + c + 8 * i;
+          s_stage[warp][lane][i] =
+              make_uint4(pack_bf16(x[0], x[1]), pack_bf16(x[2], x[3]), pack_bf16(x[4], x[5]), pack_bf16(x[6], x[7]));
+        }
+        __syncwarp();
+        const int first = it.q0 + 32 * (warp & 3) + (lane >> 2);
+        __nv_bfloat16* o = p.out + ((size_t)(it.cu + first) * p.n_q_heads + it.h) * D + map * (D / 2) + c + 8 * (lane & 3);
+#pragma unroll
+        for (int i = 0; i < 4; ++i)
+          if (first + 8 * i < it.t)
+            *reinterpret_cast<uint4*>(o + (size_t)(8 * i) * p.n_q_heads * D) = s_stage[warp][8 * i + (lane >> 2)][lane & 3];
+        __syncwarp();
       }
     }
   }
