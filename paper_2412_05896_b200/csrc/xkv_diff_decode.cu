@@ -16,8 +16,8 @@
 // and sets the ticket back to zero.
 // Weights are rounded to 16 bits for their product (half a step, 2^-9 for bf16 and 2^-12 for fp16 of their largest, as in the streaming
 // kernel); sums, maxima and outputs are fp32.
-// Measured, device time: 2 caches of up to 33 rows 7.6 us (floor 0.1: latencies of ids, rows, two barriers and the launch); 1024 caches,
-// 1.66 GB of bf16 rows 285 us = 5.8 TB/s; int8, one head a KV head, 338 MB 91 us = 3.7 TB/s, bound by issued instructions.
+// Measured, device time: 16 caches of 49 - 146 rows of 64 7.4 us (floor 0.1: latencies of ids, rows, barriers and the launch); 2048 caches,
+// 1.66 GB of bf16 rows 264 us = 6.3 TB/s, HBM; int8, one head a KV head, 338 MB 76 us = 4.4 TB/s.
 #include <algorithm>
 
 #include "common.cuh"
@@ -31,7 +31,7 @@ constexpr int kWarps = kThreads / 32;
 constexpr int kTile = 16 * kWarps;    // rows that a CTA has in registers
 constexpr int kRows = 8;              // query rows at most: the N of the products
 constexpr int kMaxCtas = 2 * 148;     // one wave: two CTAs an SM
-constexpr int kManyCaches = 1280;     // see diff_decode_by_rows
+constexpr int kManyCaches = 2560;     // of 8-bit rows, half of bf16; see diff_decode_by_rows
 constexpr float kLazy = 8.f;          // log2 slack before the reference maximum is raised
 constexpr int kTickets = sizeof(WorkspaceHeader::row_tickets) / 4;
 
@@ -123,25 +123,48 @@ __device__ __forceinline__ uint32_t pack16(float lo, float hi) {
   asm("cvt.rn.f16x2.f32 %0, %1, %2;" : "=r"(r) : "f"(hi), "f"(lo));
   return r;
 }
-// Eight consecutive elements of a cached row, as they lie: four words of bf16 or two of stored bytes.
-template <bool Q8>
-struct Piece {
-  uint32_t x[Q8 ? 2 : 4];
-  __device__ __forceinline__ void load(const uint8_t* pages, size_t element) {
-    if constexpr (Q8) {
-      const uint2 r = __ldg(reinterpret_cast<const uint2*>(pages + element));
-      x[0] = r.x, x[1] = r.y;
-    } else {
-      const uint4 r = __ldg(reinterpret_cast<const uint4*>(pages + element * 2));
-      x[0] = r.x, x[1] = r.y, x[2] = r.z, x[3] = r.w;
+// What a lane has of a cached row: pieces of eight elements as they lie (four words of bf16 or two of stored bytes), in runs of kRun
+// consecutive ones.  A run is 32 bytes (8-bit rows of 64: 16), so that the four lanes of a row take whole lines of it: of a load of eight rows L1
+// hands out a line at a time (16-byte pieces took 64 % of its data cycles: int8 batch 91 us, now 76; bf16 batch 285, now 267, and 264
+// with lines that L1 does not keep).
+template <int D, bool Q8>
+struct RowPart {
+  static constexpr int kPieces = D / 32, kWords = Q8 ? 2 : 4;         // words: of a piece
+  static constexpr int kRun = Q8 ? D / 4 : 16;
+  uint32_t x[kPieces][kWords];
+  // the first element of piece j of lane t of a row
+  static __device__ __forceinline__ int column(int t, int j) { return kRun * (t + 4 * (8 * j / kRun)) + 8 * j % kRun; }
+  __device__ __forceinline__ void load(const uint8_t* pages, size_t row, int t) {
+    uint32_t* w = &x[0][0];
+#pragma unroll
+    for (int r = 0; r < D / 4 / kRun; ++r) {
+      const uint8_t* at = pages + (row * D + kRun * (t + 4 * r)) * (Q8 ? 1 : 2);
+      if constexpr (kRun * (Q8 ? 1 : 2) == 32) {
+        asm volatile("ld.global.nc.L1::no_allocate.v8.b32 {%0, %1, %2, %3, %4, %5, %6, %7}, [%8];"
+                     : "=r"(w[8 * r]), "=r"(w[8 * r + 1]), "=r"(w[8 * r + 2]), "=r"(w[8 * r + 3]), "=r"(w[8 * r + 4]),
+                       "=r"(w[8 * r + 5]), "=r"(w[8 * r + 6]), "=r"(w[8 * r + 7])
+                     : "l"(at));
+      } else {
+        const uint4 v = __ldg(reinterpret_cast<const uint4*>(at));
+        w[0] = v.x, w[1] = v.y, w[2] = v.z, w[3] = v.w;
+      }
     }
   }
+};
+// The outputs' rows in shared memory: a gap of four floats every 32, and one that keeps rows apart, so that the lanes of a store meet in a
+// bank in twos at most.
+template <int D>
+struct OutRows {
+  static constexpr int kStride = D + D / 8 + (D == 128 ? 4 : 12);     // 4 modulo 16
+  static __device__ __forceinline__ int at(int col) { return col + 4 * (col >> 5); }
 };
 
 template <int D, bool Q8>
 __global__ void __launch_bounds__(kThreads, 2) diff_decode_rows_kernel(const Params p) {
   constexpr int kPieces = D / 32;                    // pieces of eight columns that a lane has of a row
-  __shared__ float s_o[kWarps][kRows][D];            // the warps' outputs, then in [0] the CTA's
+  using Part = RowPart<D, Q8>;
+  using Out = OutRows<D>;
+  __shared__ float s_o[kWarps][kRows][Out::kStride]; // the warps' outputs, then in [0] the CTA's
   __shared__ float s_m[kWarps][kRows], s_l[kWarps][kRows];
   __shared__ float s_top[kRows], s_sum[kRows];
   __shared__ float s_w[kRows][32];                   // a batch of chunks' weights
@@ -155,10 +178,10 @@ __global__ void __launch_bounds__(kThreads, 2) diff_decode_rows_kernel(const Par
   if (chunk >= n_chunks) return;
   const int n_rows = 2 * p.diff.heads(h);            // row 2 j + s is map s of head j
   const size_t head0 = (size_t)e * p.n_q_heads + p.diff.first_head(h);
-  // ---- this warp's tiles of 16 rows, kTile apart; of a tile a lane has rows gid and gid + 8, columns 8 (tig + 4 j) .. + 7
+  // ---- this warp's tiles of 16 rows, kTile apart; of a tile a lane has its part of rows gid and gid + 8
   const int end = min(n, (chunk + 1) * p.chunk);
   int row0 = chunk * p.chunk + 16 * warp;
-  Piece<Q8> k[2][kPieces], v[2][kPieces];
+  Part k[2], v[2];
   float ks[2] = {1.f, 1.f}, vs[2] = {1.f, 1.f};
   const int32_t* table = p.block_table + le * p.max_pages_per_seq;
   // first row of a tile in the page pool (page_size is a multiple of 16: its rows share a page)
@@ -169,16 +192,14 @@ __global__ void __launch_bounds__(kThreads, 2) diff_decode_rows_kernel(const Par
   auto load_k = [&](size_t first) {
 #pragma unroll
     for (int y = 0; y < 2; ++y) {
-#pragma unroll
-      for (int j = 0; j < kPieces; ++j) k[y][j].load(p.k_pages, (first + 8 * y) * D + 8 * (tig + 4 * j));
+      k[y].load(p.k_pages, first + 8 * y, tig);
       if constexpr (Q8) ks[y] = __ldg(&p.k_scales[first + 8 * y]);
     }
   };
   auto load_v = [&](size_t first) {
 #pragma unroll
     for (int y = 0; y < 2; ++y) {
-#pragma unroll
-      for (int j = 0; j < kPieces; ++j) v[y][j].load(p.v_pages, (first + 8 * y) * D + 8 * (tig + 4 * j));
+      v[y].load(p.v_pages, first + 8 * y, tig);
       if constexpr (Q8) vs[y] = __ldg(&p.v_scales[first + 8 * y]);
     }
   };
@@ -192,8 +213,9 @@ __global__ void __launch_bounds__(kThreads, 2) diff_decode_rows_kernel(const Par
 #pragma unroll
   for (int j = 0; j < kPieces; ++j) {
     uint4 r = make_uint4(0u, 0u, 0u, 0u);
-    if (gid < n_rows && (j >= kPieces / 2) == ((gid & 1) != 0))
-      r = __ldg(reinterpret_cast<const uint4*>(p.q + (head0 + (gid >> 1)) * D + 8 * (tig + 4 * j)));
+    const int col = Part::column(tig, j);
+    if (gid < n_rows && (col >= D / 2) == ((gid & 1) != 0))
+      r = __ldg(reinterpret_cast<const uint4*>(p.q + (head0 + (gid >> 1)) * D + col));
     q[j][0] = r.x, q[j][1] = r.y, q[j][2] = r.z, q[j][3] = r.w;
     if constexpr (Q8) {
 #pragma unroll
@@ -227,10 +249,10 @@ __global__ void __launch_bounds__(kThreads, 2) diff_decode_rows_kernel(const Par
       for (int i = 0; i < 2; ++i) {
         uint32_t a[4];
         if constexpr (Q8) {
-          a[0] = int8x2_to_biased_f16x2<0x5140>(k[0][j].x[i]), a[1] = int8x2_to_biased_f16x2<0x5140>(k[1][j].x[i]);
-          a[2] = int8x2_to_biased_f16x2<0x5342>(k[0][j].x[i]), a[3] = int8x2_to_biased_f16x2<0x5342>(k[1][j].x[i]);
+          a[0] = int8x2_to_biased_f16x2<0x5140>(k[0].x[j][i]), a[1] = int8x2_to_biased_f16x2<0x5140>(k[1].x[j][i]);
+          a[2] = int8x2_to_biased_f16x2<0x5342>(k[0].x[j][i]), a[3] = int8x2_to_biased_f16x2<0x5342>(k[1].x[j][i]);
         } else {
-          a[0] = k[0][j].x[2 * i], a[1] = k[1][j].x[2 * i], a[2] = k[0][j].x[2 * i + 1], a[3] = k[1][j].x[2 * i + 1];
+          a[0] = k[0].x[j][2 * i], a[1] = k[1].x[j][2 * i], a[2] = k[0].x[j][2 * i + 1], a[3] = k[1].x[j][2 * i + 1];
         }
         mma<Q8>(z, a, q[j][2 * i], q[j][2 * i + 1]);
       }
@@ -277,7 +299,7 @@ __global__ void __launch_bounds__(kThreads, 2) diff_decode_rows_kernel(const Par
           vs[y] = 0.f;
           if constexpr (!Q8) {
 #pragma unroll
-            for (int j = 0; j < kPieces; ++j) v[y][j].x[0] = v[y][j].x[1] = v[y][j].x[2] = v[y][j].x[3] = 0u;
+            for (int j = 0; j < kPieces; ++j) v[y].x[j][0] = v[y].x[j][1] = v[y].x[j][2] = v[y].x[j][3] = 0u;
           }
         }
     }
@@ -289,12 +311,12 @@ __global__ void __launch_bounds__(kThreads, 2) diff_decode_rows_kernel(const Par
       for (int i = 0; i < 2; ++i) {
         uint32_t a[4];
         if constexpr (Q8) {           // two neighbouring columns travel as one 16-bit element
-          const uint32_t t0 = movmatrix_trans(v[0][j].x[i]), t1 = movmatrix_trans(v[1][j].x[i]);
+          const uint32_t t0 = movmatrix_trans(v[0].x[j][i]), t1 = movmatrix_trans(v[1].x[j][i]);
           a[0] = int8x2_to_biased_f16x2<0x5240>(t0), a[1] = int8x2_to_biased_f16x2<0x5341>(t0);
           a[2] = int8x2_to_biased_f16x2<0x5240>(t1), a[3] = int8x2_to_biased_f16x2<0x5341>(t1);
         } else {
-          a[0] = movmatrix_trans(v[0][j].x[2 * i]), a[1] = movmatrix_trans(v[0][j].x[2 * i + 1]);
-          a[2] = movmatrix_trans(v[1][j].x[2 * i]), a[3] = movmatrix_trans(v[1][j].x[2 * i + 1]);
+          a[0] = movmatrix_trans(v[0].x[j][2 * i]), a[1] = movmatrix_trans(v[0].x[j][2 * i + 1]);
+          a[2] = movmatrix_trans(v[1].x[j][2 * i]), a[3] = movmatrix_trans(v[1].x[j][2 * i + 1]);
         }
         mma<Q8>(o[2 * j + i], a, b0, b1);
       }
@@ -305,14 +327,14 @@ __global__ void __launch_bounds__(kThreads, 2) diff_decode_rows_kernel(const Par
   for (int i = 0; i < 2; ++i)
 #pragma unroll
     for (int x = 4; x < 32; x <<= 1) l[i] += __shfl_xor_sync(0xffffffffu, l[i], x);
-  // accumulator row gid of block (j, i) is column 8 (gid / 2 + 4 j) + 4 i + gid % 2, row gid + 8 the one 2 further; 8-bit rows: + 2 (gid % 2),
-  // and the next one
+  // accumulator row gid of block (j, i) is column 4 i + gid % 2 of piece j of lane gid / 2, row gid + 8 the one 2 further; 8-bit rows:
+  // + 2 (gid % 2), and the next one
 #pragma unroll
   for (int x = 0; x < D / 16; ++x)
 #pragma unroll
     for (int i = 0; i < 4; ++i) {
-      const int col = 8 * ((gid >> 1) + 4 * (x >> 1)) + 4 * (x & 1) + (Q8 ? 2 * (gid & 1) + (i >> 1) : 2 * (i >> 1) + (gid & 1));
-      s_o[warp][2 * tig + (i & 1)][col] = Q8 ? fmaf(-kInt8Bias, w_sum[i], o[x][i]) : o[x][i];
+      const int col = Part::column(gid >> 1, x >> 1) + 4 * (x & 1) + (Q8 ? 2 * (gid & 1) + (i >> 1) : 2 * (i >> 1) + (gid & 1));
+      s_o[warp][2 * tig + (i & 1)][Out::at(col)] = Q8 ? fmaf(-kInt8Bias, w_sum[i], o[x][i]) : o[x][i];
     }
   if (gid == 0) {
 #pragma unroll
@@ -340,7 +362,7 @@ __global__ void __launch_bounds__(kThreads, 2) diff_decode_rows_kernel(const Par
   constexpr int kMine = kRows * D / kThreads;
 #pragma unroll
   for (int x = 0; x < kMine; ++x) {
-    const int i = x * kThreads + tid, r = i / D, col = i % D;
+    const int i = x * kThreads + tid, r = i / D, col = Out::at(i % D);
     float sum = 0.f;
 #pragma unroll
     for (int w = 0; w < kWarps; ++w) sum = fmaf(s_m[w][r], s_o[w][r][col], sum);
@@ -351,7 +373,10 @@ __global__ void __launch_bounds__(kThreads, 2) diff_decode_rows_kernel(const Par
   if (n_chunks > 1) {
     float* part = p.part_o + (size_t)blockIdx.x * kRows * D;
 #pragma unroll
-    for (int x = 0; x < kMine; ++x) __stcg(&part[x * kThreads + tid], (&s_o[0][0][0])[x * kThreads + tid]);
+    for (int x = 0; x < kMine; ++x) {
+      const int i = x * kThreads + tid;
+      __stcg(&part[i], s_o[0][i / D][Out::at(i % D)]);
+    }
     if (tid < kRows) __stcg(&p.part_ml[(size_t)blockIdx.x * kRows + tid], make_float2(s_top[tid], s_sum[tid]));
     __threadfence();
     __syncthreads();
@@ -397,7 +422,10 @@ __global__ void __launch_bounds__(kThreads, 2) diff_decode_rows_kernel(const Par
       }
     }
 #pragma unroll
-    for (int x = 0; x < kMine; ++x) (&s_o[0][0][0])[x * kThreads + tid] = acc[x];
+    for (int x = 0; x < kMine; ++x) {
+      const int i = x * kThreads + tid;
+      s_o[0][i / D][Out::at(i % D)] = acc[x];
+    }
     __syncthreads();
   }
   // ---- the difference and its norm: a warp a head
@@ -409,7 +437,8 @@ __global__ void __launch_bounds__(kThreads, 2) diff_decode_rows_kernel(const Par
     float y[D / 32], sq = 0.f;
 #pragma unroll
     for (int i = 0; i < D / 32; ++i) {
-      y[i] = fmaf(s_o[0][2 * g + 1][lane * (D / 32) + i], w2, s_o[0][2 * g][lane * (D / 32) + i] * w1);
+      const int col = Out::at(lane * (D / 32) + i);
+      y[i] = fmaf(s_o[0][2 * g + 1][col], w2, s_o[0][2 * g][col] * w1);
       sq = fmaf(y[i], y[i], sq);
     }
     if (p.diff.gain != nullptr) {
@@ -456,16 +485,18 @@ Cut cut(const xkv_dims& streamed, int n_layers, int max_cache_len) {
 
 }  // namespace
 
-// Whether this kernel or the streaming one takes a call.  Device time of both, us:
-//   bf16, G = 4, d = 128: 8 caches of 2129 rows 13.0 / 30.5, 64 of 2000 24.3 / 37.8, 2048 of 1000 193 / 214, 4096 of 1500 530 / 566
-//   int8, the same: 12.5 / 47.9, 21.0 / 51.3, 124 / 152, 320 / 402;  int8, G = 1: 2048 of 1000 121 / 143
-// It loses where there are many caches and little to each (2048 of 120 rows 54 / 37: a CTA's chain of latencies takes 7 us), and with
-// one head a KV head over many bf16 caches (2048 of 1000 190 / 183).
-bool diff_decode_by_rows(const xkv_dims* streamed, int n_layers, int max_cache_len, bool q8, int64_t max_rows) {
+// Whether this kernel or the streaming one takes a call.  Device time of both, us (rows of 128, G = 4 unless said):
+//   bf16: 8 caches of 2129 rows 12.7 / 28.8, 64 of 2000 20.5 / 36.3, 2048 of 1000 181 / 216, 4096 of 1500 498 / 576; G = 1: 2048 of
+//   1000 177 / 183;  int8: 11.5 / 47.4, 18.5 / 50.8, 109 / 152, 287 / 405; G = 1: 2048 of 1000 105 / 143
+// It loses where there are many caches and little to each, where a CTA's chain of latencies (7 us) is all there is: 2048 bf16 caches
+// of 120 rows 46 / 36 and 4096 int8 ones 74 / 48 (2048 of them 35 / 42).
+bool diff_decode_by_rows(const xkv_dims* streamed, const xkv_cache* c, int n_layers, int max_cache_len, int64_t max_rows) {
+  if (c->kv_format == XKV_KV_E4M3 || ((reinterpret_cast<uintptr_t>(c->k_pages) | reinterpret_cast<uintptr_t>(c->v_pages)) & 31u) != 0)
+    return false;                     // (a run is one load)
   const int64_t caches = (int64_t)n_layers * streamed->batch * streamed->n_kv_heads;
-  if (caches >= kManyCaches && (max_cache_len <= 2 * kTile || (!q8 && streamed->n_q_heads == 2 * streamed->n_kv_heads))) return false;
-  const Cut c = cut(*streamed, n_layers, max_cache_len);
-  return c.ctas < (1 << 30) && (c.max_chunks == 1 || c.ctas * kRows <= max_rows);
+  if (max_cache_len <= 2 * kTile && caches * (c->kv_format == XKV_KV_INT8 ? 1 : 2) >= kManyCaches) return false;
+  const Cut x = cut(*streamed, n_layers, max_cache_len);
+  return x.ctas < (1 << 30) && (x.max_chunks == 1 || x.ctas * kRows <= max_rows);
 }
 
 xkv_status diff_decode_rows(const xkv_dims* d, const xkv_cache* c, int layer_begin, int n_layers, const void* q,
