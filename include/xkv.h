@@ -562,9 +562,9 @@ xkv_status xkv_decode_attn(const xkv_dims* dims, const xkv_cache* cache, int32_t
  * workspace  dev, at least xkv_workspace_bytes(XKV_OP_DIFF_DECODE_ATTN, ...) bytes
  * Everything else (q, k_new, v_new, the append, out, chunk_rows, statuses, limits, rows of empty caches) as in xkv_decode_attn. The
  * difference, its norm and everything before them are fp32; weights are rounded as there.
- * Launches: with chunk_rows = 0 a bf16 or int8 cache is read by a kernel that plans nothing (one launch, one more for new rows, a memset
- * where more than 48 caches of a KV head are cut up), but for calls of very many short caches; those, calls with chunk_rows and
- * XKV_KV_E4M3 caches take the launches of xkv_decode_attn. The kernels add in different orders: their results agree within the
+ * Launches: with chunk_rows = 0 a bf16 or int8 cache whose pages start on 32 bytes is read by a kernel that plans nothing (one
+ * launch, one more for new rows, a memset where more than 48 caches of a KV head are cut up); calls with chunk_rows and XKV_KV_E4M3
+ * caches take the launches of xkv_decode_attn. The kernels add in different orders: their results agree within the
  * roundings, not to the bit.
  */
 xkv_status xkv_diff_decode_attn(const xkv_dims* dims, const xkv_cache* cache, int32_t layer_begin, int32_t layer_end,

@@ -81,10 +81,10 @@ xkv_status decode_attn_e4m3(const xkv_dims* d, const xkv_cache* c, int layer_beg
                             const void* k_new, const void* v_new, void* out, float* lse, const DecodeScratch& ws,
                             cudaStream_t st, const DiffHeads* diff);
 // Differential heads over bf16 or int8 caches straight from registers; max_rows: query rows that the partial results have room for.
-bool diff_decode_by_rows(const xkv_dims* streamed, const xkv_cache* c, int n_layers, int max_cache_len, int64_t max_rows);
+bool diff_decode_by_rows(const xkv_dims* streamed, const xkv_cache* c, int n_layers, int64_t max_rows);
 xkv_status diff_decode_rows(const xkv_dims* d, const xkv_cache* c, int layer_begin, int n_layers, const void* q,
                            const void* k_new, const void* v_new, void* out, float* lse, const DiffHeads& diff,
-                           const DecodeScratch& ws, cudaStream_t st);
+                           const DecodeScratch& ws, int64_t max_rows, cudaStream_t st);
 // One new row per (layer, sequence) and KV head stored in a cache of 8-bit floats, lengths advanced; n_clear words are
 // cleared on the way.
 xkv_status append_e4m3(const xkv_dims* d, const xkv_cache* c, int layer_begin, int n_units, const void* k_new,

@@ -1241,8 +1241,8 @@ xkv_status decode_attn(const xkv_dims* d, const xkv_cache* c, int layer_begin, i
                                    reinterpret_cast<int32_t*>(base + L.tickets),
                                    reinterpret_cast<float*>(base + L.part_o), reinterpret_cast<float*>(base + L.part_ml),
                                    L.max_items};
-    if (chunk_rows == 0 && diff_decode_by_rows(&streamed, c, Lr, max_cache_len, L.max_items * G))
-      return diff_decode_rows(d, c, layer_begin, Lr, q, k_new, v_new, out, lse, *diff, scratch, st);
+    if (chunk_rows == 0 && diff_decode_by_rows(&streamed, c, Lr, L.max_items * G))
+      return diff_decode_rows(d, c, layer_begin, Lr, q, k_new, v_new, out, lse, *diff, scratch, L.max_items * G, st);
     if (c->kv_format == XKV_KV_E4M3)
       return decode_attn_e4m3(d, c, layer_begin, Lr, q, k_new, v_new, out, lse, scratch, st, diff);
   }

@@ -6,7 +6,7 @@
 //
 // The streaming kernel stages rows in shared memory behind a plan of the lengths and suits calls that keep every SM busy for long;
 // a small call is a chain of latencies, and a large one of 8-bit rows is bound by instructions.  Here one launch needs nothing planned
-// before it: one CTA per chunk of a streamed cache, eight warps, a warp's 16 rows of K and V in its registers and the next tile's
+// before it: one CTA of four or eight warps per chunk of a streamed cache, a warp's 16 rows of K and V in its registers and the next tile's
 // asked for as soon as their registers are free.  The products are mma.sync m16n8k16, rows on M and the (at most eight) query rows,
 // both maps of up to four heads, on N: N = 8 fits, where a 128-row tcgen05 tile would be all but empty and the tensor pipe is idle
 // either way.  A lane's 16 bytes of a row are eight consecutive columns, so no fragment goes through shared memory: of the logits the
@@ -17,7 +17,8 @@
 // Weights are rounded to 16 bits for their product (half a step, 2^-9 for bf16 and 2^-12 for fp16 of their largest, as in the streaming
 // kernel); sums, maxima and outputs are fp32.
 // Measured, device time: 16 caches of 49 - 146 rows of 64 7.4 us (floor 0.1: latencies of ids, rows, barriers and the launch); 2048 caches,
-// 1.66 GB of bf16 rows 264 us = 6.3 TB/s, HBM; int8, one head a KV head, 338 MB 76 us = 4.4 TB/s.
+// 1.66 GB of bf16 rows 264 us = 6.3 TB/s, HBM; int8, one head a KV head, 338 MB 65 us = 5.2 TB/s, the chains
+// of latencies at a CTA's two ends (loads take 36 % of L1's cycles, instructions 47 % of the issue slots).
 #include <algorithm>
 
 #include "common.cuh"
@@ -26,12 +27,9 @@
 namespace xkv {
 namespace {
 
-constexpr int kThreads = 256;
-constexpr int kWarps = kThreads / 32;
-constexpr int kTile = 16 * kWarps;    // rows that a CTA has in registers
+constexpr int kThreads = 256;         // of the kernel that stores new rows
 constexpr int kRows = 8;              // query rows at most: the N of the products
-constexpr int kMaxCtas = 2 * 148;     // one wave: two CTAs an SM
-constexpr int kManyCaches = 2560;     // of 8-bit rows, half of bf16; see diff_decode_by_rows
+constexpr int kWarpsAll = 16 * 148;   // warps of the attention that run at the same time
 constexpr float kLazy = 8.f;          // log2 slack before the reference maximum is raised
 constexpr int kTickets = sizeof(WorkspaceHeader::row_tickets) / 4;
 
@@ -125,7 +123,7 @@ __device__ __forceinline__ uint32_t pack16(float lo, float hi) {
 }
 // What a lane has of a cached row: pieces of eight elements as they lie (four words of bf16 or two of stored bytes), in runs of kRun
 // consecutive ones.  A run is 32 bytes (8-bit rows of 64: 16), so that the four lanes of a row take whole lines of it: of a load of eight rows L1
-// hands out a line at a time (16-byte pieces took 64 % of its data cycles: int8 batch 91 us, now 76; bf16 batch 285, now 267, and 264
+// hands out a line at a time (16-byte pieces took 64 % of its data cycles: int8 batch 91 us, then 76; bf16 batch 285, then 267, and 264
 // with lines that L1 does not keep).
 template <int D, bool Q8>
 struct RowPart {
@@ -159,8 +157,10 @@ struct OutRows {
   static __device__ __forceinline__ int at(int col) { return col + 4 * (col >> 5); }
 };
 
-template <int D, bool Q8>
-__global__ void __launch_bounds__(kThreads, 2) diff_decode_rows_kernel(const Params p) {
+// W warps: 8 or 4.
+template <int D, bool Q8, int W>
+__global__ void __launch_bounds__(32 * W, 16 / W) diff_decode_rows_kernel(const Params p) {
+  constexpr int kWarps = W, kThreads = 32 * W, kTile = 16 * W;       // kTile: rows that the CTA has in registers
   constexpr int kPieces = D / 32;                    // pieces of eight columns that a lane has of a row
   using Part = RowPart<D, Q8>;
   using Out = OutRows<D>;
@@ -388,30 +388,30 @@ __global__ void __launch_bounds__(kThreads, 2) diff_decode_rows_kernel(const Par
     if (!s_last) return;
     __threadfence();
     const size_t first = (size_t)unit_head * p.max_chunks;
-    {                                                // a warp a query row: maximum and sum over all chunks
+    for (int r = warp; r < kRows; r += kWarps) {     // a warp a query row: maximum and sum over all chunks
       float top = -INFINITY, sum = 0.f;
-      for (int i = lane; i < n_chunks; i += 32) top = fmaxf(top, __ldcg(&p.part_ml[(first + i) * kRows + warp]).x);
+      for (int i = lane; i < n_chunks; i += 32) top = fmaxf(top, __ldcg(&p.part_ml[(first + i) * kRows + r]).x);
 #pragma unroll
       for (int x = 16; x > 0; x >>= 1) top = fmaxf(top, __shfl_xor_sync(0xffffffffu, top, x));
       for (int i = lane; i < n_chunks; i += 32) {
-        const float2 ml = __ldcg(&p.part_ml[(first + i) * kRows + warp]);
+        const float2 ml = __ldcg(&p.part_ml[(first + i) * kRows + r]);
         sum = fmaf(fast_exp2(ml.x - top), ml.y, sum);
       }
 #pragma unroll
       for (int x = 16; x > 0; x >>= 1) sum += __shfl_xor_sync(0xffffffffu, sum, x);
       if (lane == 0) {
-        s_top[warp] = top;
-        s_sum[warp] = sum;
+        s_top[r] = top;
+        s_sum[r] = sum;
       }
     }
-    static_assert(kWarps == kRows, "a warp a query row");
     float acc[kMine];
 #pragma unroll
     for (int x = 0; x < kMine; ++x) acc[x] = 0.f;
     for (int c0 = 0; c0 < n_chunks; c0 += 32) {
       const int nb = min(32, n_chunks - c0);
       __syncthreads();
-      if (lane < nb) s_w[warp][lane] = fast_exp2(__ldcg(&p.part_ml[(first + c0 + lane) * kRows + warp]).x - s_top[warp]);
+      for (int r = warp; r < kRows; r += kWarps)
+        if (lane < nb) s_w[r][lane] = fast_exp2(__ldcg(&p.part_ml[(first + c0 + lane) * kRows + r]).x - s_top[r]);
       __syncthreads();
 #pragma unroll
       for (int x = 0; x < kMine; ++x) {
@@ -459,49 +459,59 @@ __global__ void __launch_bounds__(kThreads, 2) diff_decode_rows_kernel(const Par
 }
 
 template <int D, bool Q8>
-xkv_status launch(const Params& p, int ctas, cudaStream_t st) {
-  diff_decode_rows_kernel<D, Q8><<<ctas, kThreads, 0, st>>>(p);
+xkv_status launch(const Params& p, int warps, int ctas, cudaStream_t st) {
+  if (warps == 8) diff_decode_rows_kernel<D, Q8, 8><<<ctas, 256, 0, st>>>(p);
+  else            diff_decode_rows_kernel<D, Q8, 4><<<ctas, 128, 0, st>>>(p);
   count_launch();
   return check_launch();
 }
 
 struct Cut {
-  int chunk, max_chunks;              // rows of a CTA, CTAs of the longest cache that its table allows
+  int warps, chunk, max_chunks;       // rows of a CTA, CTAs of the longest cache that its table allows
   int64_t ctas;
 };
-// As many chunks as fill the SMs once, but no more than about the root of eight times a cache's tiles: one CTA joins them, at some
-// 0.2 us a chunk, where a tile takes 1.5 us (32 000 rows of one KV head: 251 chunks 59 us, 42 chunks 25 us).
-Cut cut(const xkv_dims& streamed, int n_layers, int max_cache_len) {
+// Little to do (fewer than four tiles of 64 rows for each four-warp CTA that runs at the same time): eight warps a CTA, as many chunks as
+// run at the same time, but no more than about the root of eight times a cache's tiles, since one CTA joins them, at some 0.2 us a
+// chunk, where a tile takes 1.5 us (32 000 rows of one KV head: 251 chunks 59 us, 42 chunks 25 us).  More: four warps, whose CTAs start
+// and end under each other's loads (2048 int8 caches of 1000 rows 109 to 102 us, eight heads 184 to 152; but one request of 8 caches
+// 11.5 to 21), unless long bf16 rows are in not so many caches: CTAs of twice the speed wait less for the longest (2048 caches of 290 to
+// 2707 rows 264 us, with four warps 276).  With more caches than CTAs at a time a cache is one chunk, since joins cost (2048 caches
+// of 1000 rows cut in two 102 to 134 us), but for a last wave that is mostly empty (640 caches of 3000 rows 213 to 183 us).
+// max_rows: query rows that the partial results have room for.
+Cut cut(const xkv_dims& streamed, const xkv_cache& cache, int n_layers, int64_t max_rows) {
   const int64_t caches = (int64_t)n_layers * streamed.batch * streamed.n_kv_heads;
-  const int64_t tiles = std::max(1, (max_cache_len + kTile - 1) / kTile);
-  int64_t per = std::max<int64_t>(1, (caches * tiles + kMaxCtas - 1) / kMaxCtas);
-  while (per * per * 8 < tiles) ++per;
+  const int64_t rows = std::max<int64_t>(1, (int64_t)cache.max_pages_per_seq * cache.page_size);
   Cut c;
+  c.warps = caches * ((rows + 63) / 64) < 4 * (kWarpsAll / 4) ||
+            (cache.kv_format == XKV_KV_BF16 && rows > 1024 && caches < 4096) ? 8 : 4;
+  const int64_t tile = 16 * c.warps, tiles = (rows + tile - 1) / tile, slots = kWarpsAll / c.warps;
+  int64_t chunks = slots / caches;
+  if (caches > slots && 4 * caches < 3 * slots * ((caches + slots - 1) / slots))
+    chunks = std::min((4 * slots + caches - 1) / caches, tiles / 16);
+  chunks = std::max<int64_t>(std::min({chunks, tiles, max_rows / kRows / caches}), 1);
+  int64_t per = (tiles + chunks - 1) / chunks;
+  while (per * per * 8 < tiles) ++per;
   c.max_chunks = (int)((tiles + per - 1) / per);
-  c.chunk = (int)((tiles + c.max_chunks - 1) / c.max_chunks) * kTile;
+  c.chunk = (int)(((tiles + c.max_chunks - 1) / c.max_chunks) * tile);
   c.ctas = caches * c.max_chunks;
   return c;
 }
 
 }  // namespace
 
-// Whether this kernel or the streaming one takes a call.  Device time of both, us (rows of 128, G = 4 unless said):
-//   bf16: 8 caches of 2129 rows 12.7 / 28.8, 64 of 2000 20.5 / 36.3, 2048 of 1000 181 / 216, 4096 of 1500 498 / 576; G = 1: 2048 of
-//   1000 177 / 183;  int8: 11.5 / 47.4, 18.5 / 50.8, 109 / 152, 287 / 405; G = 1: 2048 of 1000 105 / 143
-// It loses where there are many caches and little to each, where a CTA's chain of latencies (7 us) is all there is: 2048 bf16 caches
-// of 120 rows 46 / 36 and 4096 int8 ones 74 / 48 (2048 of them 35 / 42).
-bool diff_decode_by_rows(const xkv_dims* streamed, const xkv_cache* c, int n_layers, int max_cache_len, int64_t max_rows) {
+// Whether this kernel or the streaming one takes a call without chunk_rows.  Device time of both, us (rows of 128, G = 4 unless said):
+//   bf16: 8 caches of 2129 rows 12.2 / 28.8, 64 of 2000 20.5 / 36.4, 2048 of 120 34.9 / 35.5, of 1000 177 / 215, 4096 of 1500 472 / 575;
+//   G = 1: 2048 of 1000 173 / 180
+//   int8, the same: 11.7 / 46.8, 18.6 / 50.1, 22.6 / 41.5, 102 / 152, 260 / 403;  G = 1: 98 / 142
+bool diff_decode_by_rows(const xkv_dims* streamed, const xkv_cache* c, int n_layers, int64_t max_rows) {
   if (c->kv_format == XKV_KV_E4M3 || ((reinterpret_cast<uintptr_t>(c->k_pages) | reinterpret_cast<uintptr_t>(c->v_pages)) & 31u) != 0)
     return false;                     // (a run is one load)
-  const int64_t caches = (int64_t)n_layers * streamed->batch * streamed->n_kv_heads;
-  if (max_cache_len <= 2 * kTile && caches * (c->kv_format == XKV_KV_INT8 ? 1 : 2) >= kManyCaches) return false;
-  const Cut x = cut(*streamed, n_layers, max_cache_len);
-  return x.ctas < (1 << 30) && (x.max_chunks == 1 || x.ctas * kRows <= max_rows);
+  return cut(*streamed, *c, n_layers, max_rows).ctas < (1 << 30);
 }
 
 xkv_status diff_decode_rows(const xkv_dims* d, const xkv_cache* c, int layer_begin, int n_layers, const void* q,
                            const void* k_new, const void* v_new, void* out, float* lse, const DiffHeads& diff,
-                           const DecodeScratch& ws, cudaStream_t st) {
+                           const DecodeScratch& ws, int64_t max_rows, cudaStream_t st) {
   const bool q8 = c->kv_format == XKV_KV_INT8, wide = d->head_dim == 128;
   if (k_new != nullptr) {
     const AppendParams a = {static_cast<const __nv_bfloat16*>(k_new), static_cast<const __nv_bfloat16*>(v_new),
@@ -520,9 +530,8 @@ xkv_status diff_decode_rows(const xkv_dims* d, const xkv_cache* c, int layer_beg
     const xkv_status s = check_launch();
     if (s != XKV_OK) return s;
   }
-  const int max_cache_len = c->max_pages_per_seq * c->page_size;
   const xkv_dims streamed = streamed_dims(d, diff);
-  const Cut how = cut(streamed, n_layers, max_cache_len);
+  const Cut how = cut(streamed, *c, n_layers, max_rows);
   Params p;
   p.q = static_cast<const __nv_bfloat16*>(q);
   p.out = static_cast<__nv_bfloat16*>(out);
@@ -554,8 +563,9 @@ xkv_status diff_decode_rows(const xkv_dims* d, const xkv_cache* c, int layer_beg
   }
   p.part_o = ws.part_o;
   p.part_ml = reinterpret_cast<float2*>(ws.part_ml);
-  if (wide) return q8 ? launch<128, true>(p, (int)how.ctas, st) : launch<128, false>(p, (int)how.ctas, st);
-  return q8 ? launch<64, true>(p, (int)how.ctas, st) : launch<64, false>(p, (int)how.ctas, st);
+  const int ctas = (int)how.ctas;
+  if (wide) return q8 ? launch<128, true>(p, how.warps, ctas, st) : launch<128, false>(p, how.warps, ctas, st);
+  return q8 ? launch<64, true>(p, how.warps, ctas, st) : launch<64, false>(p, how.warps, ctas, st);
 }
 
 }  // namespace xkv

@@ -207,3 +207,43 @@ def test_one_workspace_for_small_and_large_calls(fmt):
             got = attend(small, H * G, qs[l:l + 1].contiguous(), lam[l:l + 1].contiguous(), gain[l:l + 1].contiguous(), l0=l,
                          l1=l + 1, ws=ws)
             assert torch.equal(got[0][0], want_s[0][l])
+
+
+@pytest.mark.parametrize("fmt", ["bf16", "int8"])
+@pytest.mark.parametrize("L,B,H,G,d,page,longest", [
+    (1, 1, 1, 4, 128, 64, 20000),       # one long cache, cut up
+    (1, 3, 8, 4, 64, 16, 900),          # few caches in chunks, tickets of the workspace's head
+    (1, 8, 8, 2, 128, 32, 1000),        # 64 of them: cleared tickets
+    (2, 60, 4, 8, 64, 32, 300),         # four warps a CTA, two streamings of a KV head
+    (1, 160, 4, 3, 128, 64, 2200),      # bf16: eight warps and a cache a chunk; int8: cut for an even last wave
+    (4, 80, 2, 1, 128, 16, 90),         # short ones
+])
+def test_ways_to_cut_a_call(fmt, L, B, H, G, d, page, longest):
+    """One size of each way in which the rows are handed out; lengths from nothing to what the tables hold."""
+    rng = np.random.default_rng(L + B)
+    lens = rng.integers(0, longest + 1, (L, B))
+    lens.flat[0], lens.flat[-1] = longest, lens.flat[-1] // 16 * 16
+    c = RowCache(fmt, L, B, H, d, lens, page, seed=3)
+    lam, gain = (t.to(DEV) for t in weights(L, H * G, d, 5))
+    q = queries(L, B, H * G, d, 6)
+    out, sums = attend(c, H * G, q, lam, gain)
+    check(c, H * G, q, lam, gain, out, sums, every=max(1, B // 4))
+    for _ in range(3):
+        again, s = attend(c, H * G, q, lam, gain)
+        assert torch.equal(out, again) and torch.equal(sums, s)
+
+
+@pytest.mark.parametrize("fmt", ["bf16", "int8"])
+def test_pages_that_start_on_16_bytes(fmt):
+    c = RowCache(fmt, 2, 3, 2, 64, [[100, 0, 33], [257, 16, 90]], 16, seed=3)
+    lam, gain = (t.to(DEV) for t in weights(2, 4, 64, 5))
+    q = queries(2, 3, 4, 64, 6)
+    for i in range(2):
+        x = c.pages[i]
+        room = torch.empty(x.numel() * x.element_size() + 32, dtype=torch.uint8, device=DEV)
+        moved = room[16:-16].view(x.dtype).view(x.shape)
+        moved.copy_(x)
+        c.pages[i] = moved
+        assert moved.data_ptr() % 32 == 16
+    out, sums = attend(c, 4, q, lam, gain)
+    check(c, 4, q, lam, gain, out, sums)
