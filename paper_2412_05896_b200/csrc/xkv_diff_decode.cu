@@ -9,13 +9,13 @@
 // before it: one CTA of four or eight warps per chunk of a streamed cache, a warp's 16 rows of K and V in its registers and the next tile's
 // asked for as soon as their registers are free.  The products are mma.sync m16n8k16, rows on M and the (at most eight) query rows,
 // both maps of up to four heads, on N: N = 8 fits, where a 128-row tcgen05 tile would be all but empty and the tensor pipe is idle
-// either way.  A lane's 16 bytes of a row are eight consecutive columns, so no fragment goes through shared memory: of the logits the
+// either way.  A lane's part of a row is runs of consecutive columns, so no fragment goes through shared memory: of the logits the
 // columns' order does not matter as long as the query has the same, and of the outputs it only says where a value is stored (V's
 // fragments are transposed in registers, 8 x 8 at a time).  8-bit rows become fp16 with a bias, one instruction a pair, which comes
 // off the sums.  The last CTA of a cache to finish joins the chunks (in their order, so the result does not depend on who that is)
 // and sets the ticket back to zero.
-// Weights are rounded to 16 bits for their product (half a step, 2^-9 for bf16 and 2^-12 for fp16 of their largest, as in the streaming
-// kernel); sums, maxima and outputs are fp32.
+// Weights are rounded to 16 bits for their product: half a step, 2^-8 of a weight in bf16, 2^-11 of weight times row scale in fp16, and
+// below 2^-14 of the largest such product 2^-25; sums, maxima and outputs are fp32.
 // Measured, device time: 16 caches of 49 - 146 rows of 64 7.4 us (floor 0.1: latencies of ids, rows, barriers and the launch); 2048 caches,
 // 1.66 GB of bf16 rows 264 us = 6.3 TB/s, HBM; int8, one head a KV head, 338 MB 65 us = 5.2 TB/s, the chains
 // of latencies at a CTA's two ends (loads take 36 % of L1's cycles, instructions 47 % of the issue slots).
@@ -262,8 +262,13 @@ __global__ void __launch_bounds__(32 * W, 16 / W) diff_decode_rows_kernel(const 
       z[i] = gid + 8 * (i >> 1) < rows ? z[i] * p.scale_log2 : -INFINITY;
     }
     if (more) load_k(next);           // under the softmax and the outputs
-    // the warp's reference is exact on its first tile and raised lazily (by 2^8) afterwards
+    // the warp's reference is exact on its first tile and raised lazily (by 2^8) afterwards; 8-bit rows: of the logits plus log2 of V's
+    // scales, so that the largest weight times scale, which is rounded to fp16, is 1 to 2^8 whatever the scales are
     float top[2] = {fmaxf(z[0], z[2]), fmaxf(z[1], z[3])};
+    if constexpr (Q8) {
+      const float b0 = gid < rows ? __log2f(vs[0]) : 0.f, b1 = gid + 8 < rows ? __log2f(vs[1]) : 0.f;
+      top[0] = fmaxf(z[0] + b0, z[2] + b1), top[1] = fmaxf(z[1] + b0, z[3] + b1);
+    }
     if (__any_sync(0xffffffffu, top[0] > m[0] + kLazy || top[1] > m[1] + kLazy)) {
       float al[2];
 #pragma unroll

@@ -247,3 +247,19 @@ def test_pages_that_start_on_16_bytes(fmt):
         assert moved.data_ptr() % 32 == 16
     out, sums = attend(c, 4, q, lam, gain)
     check(c, 4, q, lam, gain, out, sums)
+
+
+@pytest.mark.parametrize("power", [-24, -14, 12, 30])
+def test_row_scales_of_any_size(power):
+    """8-bit V rows whose scales are far from 1, and a block of rows whose scales are far from the others'."""
+    c = RowCache("int8", 1, 3, 2, 128, [[400, 37, 1000]], 16, seed=3)
+    c.scales[1] *= 2.0 ** power
+    c.values[1] *= 2.0 ** power
+    first = c.table[0, :, 0].long()
+    c.scales[1][first] *= 2.0 ** -20
+    c.values[1][first] *= 2.0 ** -20
+    lam, gain = (t.to(DEV) for t in weights(1, 8, 128, 5))
+    q = queries(1, 3, 8, 128, 6)
+    for g in (gain, None):
+        out, sums = attend(c, 8, q, lam, g, eps=0.0)
+        check(c, 8, q, lam, g, out, sums, eps=0.0)
