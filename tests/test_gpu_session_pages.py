@@ -242,3 +242,38 @@ def test_a_captured_step_with_a_fork():
         assert torch.equal(one.s.shares, two.s.shares) and torch.equal(one.s.pages_used, two.s.pages_used)
     one.status()
     two.status()
+
+
+def test_a_run_on_another_stream():
+    side = torch.cuda.Stream()
+    with torch.cuda.stream(side):
+        test_a_run_together("int8", False, 64)
+
+
+def test_two_sessions_at_once():
+    """Two sessions on two streams, their steps issued in turn without waiting, against one that runs alone."""
+    def play(r, i):
+        s = r.s
+        q, k, v = (torch.randn(3, 4, n, 64, generator=torch.Generator().manual_seed(i)).to(torch.bfloat16).to(DEV) for n in (8, 2, 2))
+        if i % 5 == 2:
+            s.fork([[0, 0, 2, 3], [3, 1, 1, 0], [2, 2, -1, 1]][i % 3])
+        if i % 5 == 4:
+            s.cut([i % 3, 1, 0, 2])
+        if i % 7 == 6:
+            s.compact()
+        return s.diff_decode(q, k, v, r.lam, r.gain, EPS).clone()
+
+    alone, *both = (Run("bf16") for _ in range(3))
+    want = [play(alone, i) for i in range(40)]
+    torch.cuda.synchronize()
+    streams = [torch.cuda.Stream() for _ in both]
+    outs = [[], []]
+    for i in range(40):
+        for r, st, o in zip(both, streams, outs):
+            with torch.cuda.stream(st):
+                o.append(play(r, i))
+    torch.cuda.synchronize()
+    for r, o in zip(both, outs):
+        assert all(torch.equal(a, b) for a, b in zip(o, want))
+        assert torch.equal(r.s.seq_lens, alone.s.seq_lens) and torch.equal(r.s.pages_used, alone.s.pages_used)
+        r.status()
