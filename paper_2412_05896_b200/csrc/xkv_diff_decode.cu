@@ -29,7 +29,10 @@ namespace {
 
 constexpr int kThreads = 256;         // of the kernel that stores new rows
 constexpr int kRows = 8;              // query rows at most: the N of the products
-constexpr int kWarpsAll = 16 * 148;   // warps of the attention that run at the same time
+constexpr int kSms = 148;
+// CTAs of the attention that an SM takes at a time: two of eight warps; of four, four for rows of 128 and five for rows of 64, which fit in
+// fewer registers (2048 int8 caches of 1000 such rows 63 us, with four 82, with six 68; rows of 128 with five 128, with four 102).
+constexpr int ctas_of_an_sm(int head_dim, int warps) { return warps == 8 ? 2 : (head_dim == 64 ? 5 : 4); }
 constexpr float kLazy = 8.f;          // log2 slack before the reference maximum is raised
 constexpr int kTickets = sizeof(WorkspaceHeader::row_tickets) / 4;
 
@@ -159,7 +162,7 @@ struct OutRows {
 
 // W warps: 8 or 4.
 template <int D, bool Q8, int W>
-__global__ void __launch_bounds__(32 * W, 16 / W) diff_decode_rows_kernel(const Params p) {
+__global__ void __launch_bounds__(32 * W, ctas_of_an_sm(D, W)) diff_decode_rows_kernel(const Params p) {
   constexpr int kWarps = W, kThreads = 32 * W, kTile = 16 * W;       // kTile: rows that the CTA has in registers
   constexpr int kPieces = D / 32;                    // pieces of eight columns that a lane has of a row
   using Part = RowPart<D, Q8>;
@@ -487,9 +490,10 @@ Cut cut(const xkv_dims& streamed, const xkv_cache& cache, int n_layers, int64_t 
   const int64_t caches = (int64_t)n_layers * streamed.batch * streamed.n_kv_heads;
   const int64_t rows = std::max<int64_t>(1, (int64_t)cache.max_pages_per_seq * cache.page_size);
   Cut c;
-  c.warps = caches * ((rows + 63) / 64) < 4 * (kWarpsAll / 4) ||
+  c.warps = caches * ((rows + 63) / 64) < 4 * 4 * kSms ||
             (cache.kv_format == XKV_KV_BF16 && rows > 1024 && caches < 4096) ? 8 : 4;
-  const int64_t tile = 16 * c.warps, tiles = (rows + tile - 1) / tile, slots = kWarpsAll / c.warps;
+  const int64_t tile = 16 * c.warps, tiles = (rows + tile - 1) / tile;
+  const int64_t slots = ctas_of_an_sm(streamed.head_dim, c.warps) * kSms;
   int64_t chunks = slots / caches;
   if (caches > slots && 4 * caches < 3 * slots * ((caches + slots - 1) / slots))
     chunks = std::min((4 * slots + caches - 1) / caches, tiles / 16);
