@@ -6,9 +6,12 @@
 //   xkv_compact_pages  pages in use become pages 0 .. n_live-1 of the pool
 //   xkv_copy_pages     pages of one pool copied into another
 //
-// The first two are a plan, one thread-block cluster whose phases are separated by cluster barriers (a grid of separate
-// launches would pay a launch a phase), and a copy of rows or pages by the whole GPU whose CTAs are in place when the plan
-// ends.  The plan is bound by latency: dependent loads of lengths, table entries and counters; the copy by HBM.
+// The first two are a plan and a copy of rows or pages by the whole GPU whose CTAs are in place when the plan ends.  A plan of few
+// caches and pages is one CTA's, with the counters in its shared memory, in one launch with the copy (a cluster of eight; 96 caches
+// 14 us, 8 caches compacted 6.7); larger ones are counted and dropped by all SMs, and what has an order (pages off the list and back to it)
+// is decided by a cluster with barriers between its phases (1024 caches of 32 layers forked and ended 50 us, of which the rows 19).
+// A plan is bound by latency: dependent loads, and code that runs once out of a cold instruction cache, which is why its
+// loops are not unrolled further; the copy by HBM (527 MB 83 us = 0.97 of the measured copy rate).
 #include <algorithm>
 #include <atomic>
 
