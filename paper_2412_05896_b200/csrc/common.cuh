@@ -24,7 +24,7 @@ struct WorkspaceHeader {
   int32_t grid_arrivals; // decode: CTAs of the self-planning launch that have finished all their work
   int32_t plan_ticket;   // step plan: CTAs that have finished (zero between calls)
   int32_t plan_used;     // step plan: free-list position behind the last page handed out (zero between calls)
-  int32_t row_tickets[48]; // decode of little: CTAs of a cache that have finished (zero between calls)
+  int32_t row_tickets[48]; // decode by rows: CTAs of a cache that have finished (zero between calls)
   int32_t reserved[6];
 };
 static_assert(sizeof(WorkspaceHeader) == 256, "header is 256 bytes");

@@ -485,6 +485,8 @@ struct Cut {
 // 11.5 to 21), unless long bf16 rows are in not so many caches: CTAs of twice the speed wait less for the longest (2048 caches of 290 to
 // 2707 rows 264 us, with four warps 276).  With more caches than CTAs at a time a cache is one chunk, since joins cost (2048 caches
 // of 1000 rows cut in two 102 to 134 us), but for a last wave that is mostly empty (640 caches of 3000 rows 213 to 183 us).
+// Tables of more than 12 288 rows: chunks of 4096, as far as that makes eight waves of CTAs, most of which may find nothing (a sequence of
+// 65 536 rows among 15 short ones 437 to 80 us; 64 short sequences in tables of 32 768 rows 37 to 43, the streaming kernel 60).
 // max_rows: query rows that the partial results have room for.
 Cut cut(const xkv_dims& streamed, const xkv_cache& cache, int n_layers, int64_t max_rows) {
   const int64_t caches = (int64_t)n_layers * streamed.batch * streamed.n_kv_heads;
@@ -497,6 +499,7 @@ Cut cut(const xkv_dims& streamed, const xkv_cache& cache, int n_layers, int64_t 
   int64_t chunks = slots / caches;
   if (caches > slots && 4 * caches < 3 * slots * ((caches + slots - 1) / slots))
     chunks = std::min((4 * slots + caches - 1) / caches, tiles / 16);
+  if (rows > 12288) chunks = std::max(chunks, std::min((rows + 4095) / 4096, 8 * slots / caches));
   chunks = std::max<int64_t>(std::min({chunks, tiles, max_rows / kRows / caches}), 1);
   int64_t per = (tiles + chunks - 1) / chunks;
   while (per * per * 8 < tiles) ++per;

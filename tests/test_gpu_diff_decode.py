@@ -263,3 +263,17 @@ def test_row_scales_of_any_size(power):
     for g in (gain, None):
         out, sums = attend(c, 8, q, lam, g, eps=0.0)
         check(c, 8, q, lam, g, out, sums, eps=0.0)
+
+
+@pytest.mark.parametrize("fmt", ["bf16", "int8"])
+def test_a_long_cache_among_short_ones(fmt):
+    """Tables much longer than most caches: chunks that find nothing, one cache in many pieces."""
+    lens = np.random.default_rng(1).integers(0, 200, (1, 24))
+    lens[0, 5] = 17001
+    c = RowCache(fmt, 1, 24, 2, 64, lens, 64, seed=3)
+    lam, gain = (t.to(DEV) for t in weights(1, 8, 64, 5))
+    q = queries(1, 24, 8, 64, 6)
+    out, sums = attend(c, 8, q, lam, gain)
+    check(c, 8, q, lam, gain, out, sums)
+    again, _ = attend(c, 8, q, lam, gain)
+    assert torch.equal(out, again)
