@@ -499,8 +499,11 @@ class XkvSession:
 
     # ------------------------------------------------------------------ caches that share pages
     def _reset_pages(self) -> None:
-        self.free_pages = torch.arange(self.n_pages, dtype=torch.int32, device=self.device)
-        self.shares = torch.zeros(self.n_pages, dtype=torch.int32, device=self.device)
+        if self.free_pages is None:
+            self.free_pages = torch.empty(self.n_pages, dtype=torch.int32, device=self.device)
+            self.shares = torch.empty(self.n_pages, dtype=torch.int32, device=self.device)
+        torch.arange(self.n_pages, out=self.free_pages)      # in place: captured steps hold their addresses
+        self.shares.zero_()
 
     def _per_cache(self, x, name: str, layers: bool) -> torch.Tensor:
         """Host integers or a dev int32 tensor, [B] (or [L, B]), as dev int32 of a layer's caches."""
@@ -574,8 +577,8 @@ class XkvSession:
                           self.pages_used, self.ws_compact)
 
     def resize_pool(self, n_pages: int) -> None:
-        """The pages in use in a new pool of n_pages, the old one given up (waits for the device).  Needs
-        pages_on_demand; ValueError, and the pool as it was, when they do not fit; an error that device_status("pages") has
+        """The pages in use in a new pool of n_pages, the old one given up (waits for the device; steps captured
+        before it still read and write the old one).  Needs pages_on_demand; ValueError, and the pool as it was, when they do not fit; an error that device_status("pages") has
         not reported yet is raised."""
         self.compact()
         used, st = int(self.pages_used.item()), self.device_status("pages")

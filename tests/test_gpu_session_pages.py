@@ -240,6 +240,16 @@ def test_a_captured_step_with_a_fork():
         torch.cuda.synchronize()
         assert torch.equal(out, want) and torch.equal(one.s.seq_lens, two.s.seq_lens)
         assert torch.equal(one.s.shares, two.s.shares) and torch.equal(one.s.pages_used, two.s.pages_used)
+    parent.copy_(torch.tensor([1, 1, 3, 2], dtype=torch.int32))
+    for r in (one, two):                                      # another batch in the same session: the captured step goes on with it
+        r.s.prefill(*([t[i] for t in r.tens] for i in range(3)), budgets=r.budgets)
+    for _ in range(3):
+        graph.replay()
+        two.s.fork(parent)
+        want = two.s.diff_decode(q, k, v, two.lam, two.gain, EPS)
+        torch.cuda.synchronize()
+        assert torch.equal(out, want) and torch.equal(one.s.block_table, two.s.block_table)
+        assert torch.equal(one.s.shares, two.s.shares) and torch.equal(one.s.pages_used, two.s.pages_used)
     one.status()
     two.status()
 
