@@ -25,7 +25,7 @@
 // Every wait is bounded and ends when another role has given up; an expired one sets the status word and lets the CTA drain.
 //
 // Measured (device time, clock under the power limit 1.65 - 1.8 GHz): four prompts of 2399 - 4428 tokens, 32 heads of 128 over 8 KV heads 864
-// us = 840 TFLOP/s; one of 32 768 tokens, 8 heads 1005 TFLOP/s; one of 487 tokens, 4 heads of 64 13.4 us.  What bounds it is the issue of
+// us = 840 TFLOP/s (830 to 864 from GPU to GPU); one of 32 768 tokens, 8 heads 1020 TFLOP/s; one of 487 tokens, 4 heads of 64 13.4 us.  What bounds it is the issue of
 // the softmax, at d = 64 as at 128: 1550 clocks a tile where the tensor pipe would take 896 and the exponentials 1024, two warps
 // an SM sub-partition, and some 7000 clocks at an item's end, when the tensor pipe has nothing to do (the same warps form the output;
 // four warps of their own for it left the softmax 96 registers a thread instead of 128: 1010 us).
@@ -47,9 +47,9 @@ constexpr int kStages = 4;            // K tiles, and V tiles
 constexpr int kItems = 4;             // items between the walk and the last reader
 constexpr int kItemReaders = 5 + kSoftWarps;   // all but the walk itself
 constexpr float kLazy = 8.f;          // log2 slack before the reference maximum is raised
-// Registers a thread: the launch has 128 for each of its 512; a softmax thread, which holds a row's logits, takes 176 and leaves the
-// other roles' threads 80.
-constexpr int kLaunchRegs = 128, kSoftRegs = 176, kRoleRegs = 80;
+// Registers a thread: the launch has 128 for each of its 512; a softmax thread, which holds a row's logits, takes 192 and leaves the
+// other roles' threads 64 (a prompt of 32 768 tokens 3.23 ms, with 176 and 80 3.28; heads of 64 750 and 788 us).
+constexpr int kLaunchRegs = 128, kSoftRegs = 192, kRoleRegs = 64;
 static_assert(256 * kSoftRegs + 256 * kRoleRegs <= kThreads * kLaunchRegs, "no more than the launch has");
 
 struct Params {

@@ -128,11 +128,13 @@ def lib() -> ctypes.CDLL:
 
 
 def _ptr(x):
+    if x is None:
+        return None
     try:
         return x.data_ptr()   # torch tensor
     except AttributeError:
         pass
-    if x is None or isinstance(x, int):
+    if isinstance(x, int):
         return x
     return x.ctypes.data      # numpy array
 
