@@ -20,6 +20,7 @@ from . import xkv
 class XkvSession:
     # (until caches are forked pages are handed out in their order, each to one cache)
     free_pages = shares = None
+    _some = None                                             # live sequences of a step, their rows and counts on the device
 
     def __init__(self, n_layers: int, n_q_heads: int, n_kv_heads: int, head_dim: int, window: int,
                  pool_kernel: int, lengths: list[int], pool_mode: int = xkv.POOL_MAX, page_size: int = 16,
@@ -468,9 +469,12 @@ class XkvSession:
             # one row a cache, head by head in a head-level session: the order in which the rows lie
             self._store_new(k_new, v_new, self.one_each, self.n_caches)
         elif any(self.live):
-            rows = self._to_device(np.flatnonzero(self.live), np.int64)
-            counts = np.repeat(np.asarray(self.live, dtype=np.int32), self.n_caches // self.B)
-            self._store_new(k_new[:, rows], v_new[:, rows], self._to_device(counts), int(counts.sum()))
+            if self._some is None or self._some[0] != self.live:      # (so that a step can be captured after one like it)
+                counts = np.repeat(np.asarray(self.live, dtype=np.int32), self.n_caches // self.B)
+                self._some = (list(self.live), self._to_device(np.flatnonzero(self.live), np.int64),
+                              self._to_device(counts), int(counts.sum()))
+            _, rows, counts, n = self._some
+            self._store_new(k_new[:, rows], v_new[:, rows], counts, n)
         return None, None
 
     def diff_decode(self, q: torch.Tensor, k_new: torch.Tensor | None, v_new: torch.Tensor | None, lam: torch.Tensor,

@@ -287,3 +287,24 @@ def test_two_sessions_at_once():
         assert all(torch.equal(a, b) for a, b in zip(o, want))
         assert torch.equal(r.s.seq_lens, alone.s.seq_lens) and torch.equal(r.s.pages_used, alone.s.pages_used)
         r.status()
+
+
+def test_a_captured_step_of_some_sequences():
+    one, two = Run("int8"), Run("int8")
+    q, k, v = (torch.randn(3, 4, n, 64, generator=one.gen).to(torch.bfloat16).to(DEV) for n in (8, 2, 2))
+    for r in (one, two):
+        r.s.fork([0, -1, 2, 2])
+        r.s.diff_decode(q, k, v, r.lam, r.gain, EPS)
+    torch.cuda.synchronize()
+    graph = torch.cuda.CUDAGraph()
+    with torch.cuda.graph(graph):
+        out = one.s.diff_decode(q, k, v, one.lam, one.gain, EPS)
+    for _ in range(20):
+        for t in (q, k, v):
+            t.copy_(torch.randn(t.shape, generator=one.gen).to(torch.bfloat16))
+        graph.replay()
+        want = two.s.diff_decode(q, k, v, two.lam, two.gain, EPS)
+        torch.cuda.synchronize()
+        assert torch.equal(out, want) and torch.equal(one.s.seq_lens, two.s.seq_lens) and not one.s.seq_lens[:, 1].any()
+    one.status()
+    two.status()
