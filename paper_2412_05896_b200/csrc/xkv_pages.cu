@@ -101,10 +101,6 @@ __device__ __forceinline__ void copy_rows(const CopyParams& p, const RowCopy* li
     copy_head(p, {__ldcg(&list[i].src), __ldcg(&list[i].dst), __ldcg(&list[i].rows)}, part, piece, step);
   });
 }
-__global__ void __launch_bounds__(kCopyThreads) copy_rows_kernel(const CopyParams p, const RowCopy* list, const int32_t* n_list) {
-  asm volatile("griddepcontrol.wait;" ::: "memory");
-  copy_rows(p, list, __ldcg(n_list));
-}
 
 // Page ids that a caller gives.
 __global__ void __launch_bounds__(kCopyThreads) copy_pages_kernel(const CopyParams p, const int32_t* src, const int32_t* dst,
@@ -204,7 +200,7 @@ struct ForkParams {
   int4* rows;                         // [L * B] a ForkRow each
   int32_t* last;                      // [L * B] partly filled last page, -1: none
   int32_t* rank;                      // [L * B] place among the CTA's copies, -1: no copy
-  uint32_t* gone;                     // a bit a page: nobody holds it any more; zero between calls
+  uint32_t* gone;                     // a bit a page: it may have lost its last holder, then: it has; zero between calls
   int32_t* word_at;                   // bits before each of its words, within a CTA's share of them
   int32_t* fresh;                     // [L][B][cols] entries of caches that become forks
 };
@@ -240,43 +236,23 @@ __device__ __forceinline__ int last_page(const ForkParams& p, int row, const For
   return in_pool(p, e) ? e : -1;
 }
 
-// A warp: holders that come are counted, before any that go (so that no page seems to be free in between); the parent's entries
-// are read before any table changes.
-__device__ __forceinline__ void count_new(const ForkParams& p, int row, const ForkRow& r) {
+// A warp: holders that come and go, in whatever order (who is free shows at the end), and the entries that a fork gets.  No table
+// changes yet: others read their parents' entries.
+__device__ __forceinline__ void count_holders(const ForkParams& p, int row, const ForkRow& r) {
   const int lane = threadIdx.x & 31, b = row % p.batch;
   const int32_t* mine = p.table + (size_t)row * p.cols;
   const int32_t* theirs = p.table + ((size_t)(row - b) + max(r.parent, 0)) * p.cols;
   int32_t* fresh = p.fresh + (size_t)row * p.cols;
-  if (r.parent == b) return;
-#pragma unroll 4
-  for (int i = lane; i < r.need; i += 32) {
-    const int e = __ldcg(&theirs[i]);
-    const int was = i < r.have ? __ldcg(&mine[i]) : e - 1;
-    fresh[i] = e;
-    if (!in_pool(p, e)) record_status(p.hdr, XKV_ERR_INVALID_ARG);
-    else if (was != e) atomicAdd(&p.shares[e], 1);
-  }
-}
-
-// A warp: entries that go, and the table.
-__device__ __forceinline__ void drop_old(const ForkParams& p, int row, const ForkRow& r) {
-  const int lane = threadIdx.x & 31, b = row % p.batch;
-  int32_t* mine = p.table + (size_t)row * p.cols;
-  const int32_t* fresh = p.fresh + (size_t)row * p.cols;
 #pragma unroll 4
   for (int i = (r.parent == b ? r.need : 0) + lane; i < max(r.have, r.need); i += 32) {
-    const int now = i < r.need ? __ldcg(&fresh[i]) : -1;
-    const int was = i < r.have ? __ldcg(&mine[i]) : -1;
-    if (i < r.need && i < r.have && was == now) continue;
-    if (i < r.need) mine[i] = now;
-    if (i >= r.have) continue;
-    if (!in_pool(p, was)) {
-      record_status(p.hdr, XKV_ERR_INVALID_ARG);
-      continue;
-    }
-    const int others = atomicSub(&p.shares[was], 1);
-    if (others == 0) atomicOr(&p.gone[was >> 5], 1u << (was & 31));
-    if (others < 0) record_status(p.hdr, XKV_ERR_INVALID_ARG);
+    const bool had = i < r.have, gets = i < r.need;
+    const int was = had ? __ldcg(&mine[i]) : -1, now = gets ? __ldcg(&theirs[i]) : -1;
+    if (gets) fresh[i] = now;
+    if ((had && !in_pool(p, was)) || (gets && !in_pool(p, now))) record_status(p.hdr, XKV_ERR_INVALID_ARG);
+    if (had && gets && was == now) continue;
+    if (gets && in_pool(p, now)) atomicAdd(&p.shares[now], 1);
+    // (a page that ends without a holder has had one taken at no others, whatever came between)
+    if (had && in_pool(p, was) && atomicSub(&p.shares[was], 1) <= 0) atomicOr(&p.gone[was >> 5], 1u << (was & 31));
   }
 }
 
@@ -284,7 +260,7 @@ __device__ __forceinline__ void drop_old(const ForkParams& p, int row, const For
 template <typename RowAt>
 __device__ __forceinline__ void fork_decide(const ForkParams& p, RowAt row_at) {
   __shared__ int s_scan[kPlanWarps + 1];
-  __shared__ int s_held[kPlanThreads];
+  __shared__ int4 s_held[kPlanThreads];            // cache, its page, others that hold it
   __shared__ int s_copy[kPlanThreads];
   // ---- last pages that need a copy: those that others hold too, unless all holders are such last pages, of which one
   //      (the cache that stays, else the first) keeps it.  A thread a cache; a warp for each that others hold.
@@ -295,16 +271,19 @@ __device__ __forceinline__ void fork_decide(const ForkParams& p, RowAt row_at) {
   for (int64_t base = row0; base < row1; base += kPlanThreads) {
     const int mine = (int)base + threadIdx.x;
     const int own = mine < row1 ? __ldcg(&p.last[mine]) : -1;
-    const bool held_by_others = own >= 0 && __ldcg(&p.shares[own]) > 0;
+    const int own_others = own >= 0 ? __ldcg(&p.shares[own]) : 0;
+    const bool held_by_others = own_others > 0;
     s_copy[threadIdx.x] = 0;
     int n_held, total;
     const int place = block_scan(held_by_others ? 1 : 0, s_scan, &n_held);
-    if (held_by_others) s_held[place] = mine;
+    if (held_by_others) s_held[place] = make_int4(mine, own, own_others, 0);
     __syncthreads();
+#pragma unroll 2
     for (int i = warp; i < n_held; i += kPlanWarps) {
-      const int row = s_held[i], page = __ldcg(&p.last[row]), others = __ldcg(&p.shares[page]), b0 = row % p.batch;
+      const int4 h = s_held[i];
+      const int row = h.x, page = h.y, others = h.z, b0 = row % p.batch;
       int n = 0, first = 0x7fffffff;
-#pragma unroll 4
+#pragma unroll 2
       for (int b = lane; b < p.batch; b += 32)
         if (__ldcg(&p.last[row - b0 + b]) == page) {
           ++n;
@@ -323,6 +302,14 @@ __device__ __forceinline__ void fork_decide(const ForkParams& p, RowAt row_at) {
   int64_t word0, word1;
   cta_run(n_words, &word0, &word1);
   int back = 0;
+  for (int64_t w = word0 + warp; w < word1; w += kPlanWarps) {
+    const bool dropped = ((__ldcg(&p.gone[w]) >> lane) & 1u) != 0;
+    const int holders = dropped ? __ldcg(&p.shares[w * 32 + lane]) : 0;        // beyond the first
+    if (holders < -1) record_status(p.hdr, XKV_ERR_INVALID_ARG);               // dropped more often than it was held
+    const uint32_t word = __ballot_sync(0xffffffffu, holders < 0);
+    if (lane == 0) p.gone[w] = word;
+  }
+  __syncthreads();
   for (int64_t base = word0; base < word1; base += kPlanThreads) {
     const int64_t w = base + threadIdx.x;
     int total;
@@ -355,7 +342,7 @@ __device__ __forceinline__ void fork_decide(const ForkParams& p, RowAt row_at) {
       atomicSub(&p.shares[page], 1);
       RowCopy c = {page, to, r.rows % p.page_size};
       if (in_pool(p, to)) {
-        p.table[(size_t)row * p.cols + r.need - 1] = to;
+        (r.parent == row % p.batch ? p.table : p.fresh)[(size_t)row * p.cols + r.need - 1] = to;
       } else {                        // no page: only whole pages stay
         record_status(p.hdr, i < p.n_free - used ? XKV_ERR_INVALID_ARG : XKV_ERR_CAPACITY);
         c = {0, 0, 0};
@@ -546,7 +533,7 @@ __global__ void __launch_bounds__(kPlanThreads, 1) fork_small_kernel(const ForkP
   copy_rows(c, p.list, __ldcg(p.n_copies));
 }
 
-// The same in three launches, whose first two take all SMs.
+// The same in three launches, whose first and last take all SMs.
 __global__ void __launch_bounds__(kCopyThreads) fork_count_kernel(const ForkParams p) {
   asm volatile("griddepcontrol.wait;" ::: "memory");
   asm volatile("griddepcontrol.launch_dependents;");
@@ -557,20 +544,28 @@ __global__ void __launch_bounds__(kCopyThreads) fork_count_kernel(const ForkPara
       p.rows[row] = r;
       p.last[row] = last_page(p, row, as_row(r));
     }
-    count_new(p, row, as_row(r));
+    count_holders(p, row, as_row(r));
   }
-}
-__global__ void __launch_bounds__(kCopyThreads) fork_drop_kernel(const ForkParams p) {
-  asm volatile("griddepcontrol.wait;" ::: "memory");
-  asm volatile("griddepcontrol.launch_dependents;");
-  const int n_warps = gridDim.x * (kCopyThreads / 32);
-  for (int row = blockIdx.x * (kCopyThreads / 32) + (threadIdx.x >> 5); row < p.n_rows; row += n_warps)
-    drop_old(p, row, as_row(__ldcg(&p.rows[row])));
 }
 __global__ void __launch_bounds__(kPlanThreads, 1) fork_decide_kernel(const ForkParams p) {
   asm volatile("griddepcontrol.wait;" ::: "memory");
   asm volatile("griddepcontrol.launch_dependents;");
   fork_decide(p, [&](int row) { return as_row(__ldcg(&p.rows[row])); });
+}
+// Tables of the forks, then the copies.
+__global__ void __launch_bounds__(kCopyThreads) fork_finish_kernel(const ForkParams p, const CopyParams c) {
+  asm volatile("griddepcontrol.wait;" ::: "memory");
+  const int n_warps = gridDim.x * (kCopyThreads / 32);
+  for (int row = blockIdx.x * (kCopyThreads / 32) + (threadIdx.x >> 5); row < p.n_rows; row += n_warps) {
+    const ForkRow r = as_row(__ldcg(&p.rows[row]));
+    if (r.parent == row % p.batch) continue;
+#pragma unroll 4
+    for (int i = threadIdx.x & 31; i < r.need; i += 32) {
+      const size_t at = (size_t)row * p.cols + i;
+      p.table[at] = __ldcg(&p.fresh[at]);
+    }
+  }
+  copy_rows(c, p.list, __ldcg(p.n_copies));
 }
 
 // ---------------------------------------------------------------------------------------------
@@ -874,11 +869,9 @@ xkv_status fork_caches(const xkv_dims* d, const xkv_cache* c, const int32_t* par
   }
   const int grid = (int)std::min<int64_t>((n_rows + kCopyThreads / 32 - 1) / (kCopyThreads / 32), 8 * (int64_t)sm_count());
   s = launch_after(fork_count_kernel, grid, kCopyThreads, false, st, 0, p);
-  if (s == XKV_OK) s = launch_after(fork_drop_kernel, grid, kCopyThreads, false, st, 0, p);
   if (s == XKV_OK) s = launch_after(fork_decide_kernel, kMaxCluster, kPlanThreads, true, st, 0, p);
   if (s != XKV_OK) return s;
-  return launch_after(copy_rows_kernel, copy_grid(cp, n_rows, false), kCopyThreads, false, st, 0, cp, (const RowCopy*)p.list,
-                      (const int32_t*)p.n_copies);
+  return launch_after(fork_finish_kernel, std::max(grid, copy_grid(cp, n_rows, false)), kCopyThreads, false, st, 0, p, cp);
 }
 
 xkv_status compact_pages(const xkv_dims* d, const xkv_cache* c, const int32_t* table_before, const int32_t* shares_before,
