@@ -8,8 +8,9 @@
 //
 // The first two are a plan and a copy of rows or pages by the whole GPU whose CTAs are in place when the plan ends.  A plan of few
 // caches and pages is one CTA's, with the counters in its shared memory, in one launch with the copy (a cluster of eight; 96 caches
-// 14 us, 8 caches compacted 6.7); larger ones are counted and dropped by all SMs, and what has an order (pages off the list and back to it)
-// is decided by a cluster with barriers between its phases (1024 caches of 32 layers forked and ended 50 us, of which the rows 19).
+// 14 us, 8 caches compacted 6.7); of larger ones all SMs count the holders and write tables and rows, and what has an order (pages off the
+// list and back to it) is decided in between by a cluster with barriers between its phases (1024 caches of 32 layers forked and ended
+// 46 us, of which tables and rows 20).
 // A plan is bound by latency: dependent loads, and code that runs once out of a cold instruction cache, which is why its
 // loops are not unrolled further; the copy by HBM (527 MB 83 us = 0.97 of the measured copy rate).
 #include <algorithm>
@@ -267,6 +268,10 @@ __device__ __forceinline__ void fork_decide(const ForkParams& p, RowAt row_at) {
   const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5;
   int64_t row0, row1;
   cta_run(p.n_rows, &row0, &row1);
+  // of a thread's first cache and first word, which are the only ones in most calls: kept in registers past the barriers
+  const bool has = row0 + threadIdx.x < row1;
+  const ForkRow first_row = has ? row_at((int)row0 + threadIdx.x) : ForkRow{0, 0, 0, 0};
+  int first_last = -1, first_rank = -1;
   int copies = 0;
   for (int64_t base = row0; base < row1; base += kPlanThreads) {
     const int mine = (int)base + threadIdx.x;
@@ -295,26 +300,39 @@ __device__ __forceinline__ void fork_decide(const ForkParams& p, RowAt row_at) {
     }
     __syncthreads();
     const int copy = s_copy[threadIdx.x], before = block_scan(copy, s_scan, &total);
-    if (mine < row1) p.rank[mine] = copy ? copies + before : -1;
+    if (base == row0) {
+      first_last = own;
+      first_rank = copy ? before : -1;
+    } else if (mine < row1) {
+      p.rank[mine] = copy ? copies + before : -1;
+    }
     copies += total;
   }
   const int n_words = (p.n_pages + 31) / 32;
   int64_t word0, word1;
   cta_run(n_words, &word0, &word1);
-  int back = 0;
-  for (int64_t w = word0 + warp; w < word1; w += kPlanWarps) {
-    const bool dropped = ((__ldcg(&p.gone[w]) >> lane) & 1u) != 0;
-    const int holders = dropped ? __ldcg(&p.shares[w * 32 + lane]) : 0;        // beyond the first
-    if (holders < -1) record_status(p.hdr, XKV_ERR_INVALID_ARG);               // dropped more often than it was held
-    const uint32_t word = __ballot_sync(0xffffffffu, holders < 0);
-    if (lane == 0) p.gone[w] = word;
+  int back = 0, first_at = 0;
+  for (int64_t w0 = word0 + warp; w0 < word1; w0 += 4 * kPlanWarps) {           // four words of a warp are asked for together
+    uint32_t word[4];
+    int holders[4];                   // beyond the first
+#pragma unroll
+    for (int u = 0; u < 4; ++u) word[u] = w0 + u * kPlanWarps < word1 ? __ldcg(&p.gone[w0 + u * kPlanWarps]) : 0u;
+#pragma unroll
+    for (int u = 0; u < 4; ++u) holders[u] = (word[u] >> lane) & 1u ? __ldcg(&p.shares[(w0 + u * kPlanWarps) * 32 + lane]) : 0;
+#pragma unroll
+    for (int u = 0; u < 4; ++u) {
+      if (holders[u] < -1) record_status(p.hdr, XKV_ERR_INVALID_ARG);          // dropped more often than it was held
+      const uint32_t left = __ballot_sync(0xffffffffu, holders[u] < 0);
+      if (lane == 0 && left != word[u]) p.gone[w0 + u * kPlanWarps] = left;
+    }
   }
   __syncthreads();
   for (int64_t base = word0; base < word1; base += kPlanThreads) {
     const int64_t w = base + threadIdx.x;
     int total;
     const int before = block_scan(w < word1 ? __popc(__ldcg(&p.gone[w])) : 0, s_scan, &total);
-    if (w < word1) p.word_at[w] = back + before;
+    if (base == word0) first_at = before;
+    else if (w < word1) p.word_at[w] = back + before;
     back += total;
   }
   if (threadIdx.x == 0) {
@@ -333,11 +351,12 @@ __device__ __forceinline__ void fork_decide(const ForkParams& p, RowAt row_at) {
   for (int64_t base = row0; base < row1; base += kPlanThreads) {
     const int row = (int)base + threadIdx.x;
     if (row >= row1) continue;
-    const ForkRow r = row_at(row);
-    const int rank = p.rank[row];
+    const bool kept = base == row0;
+    const ForkRow r = kept ? first_row : row_at(row);
+    const int rank = kept ? first_rank : p.rank[row];
     int rows = r.rows;
     if (rank >= 0) {
-      const int i = copies_before + rank, page = p.last[row];
+      const int i = copies_before + rank, page = kept ? first_last : p.last[row];
       const int to = i < p.n_free - used ? __ldcg(&p.free_pages[used + i]) : -1;
       atomicSub(&p.shares[page], 1);
       RowCopy c = {page, to, r.rows % p.page_size};
@@ -352,7 +371,7 @@ __device__ __forceinline__ void fork_decide(const ForkParams& p, RowAt row_at) {
     }
     p.lens[row] = rows;
   }
-  phase();
+  if (all_copies > 0 && all_back > 0) phase();       // (the list is read above where it is written below; the same for all CTAs)
   // ---- pages back to the list, in ascending order
   const int taken = min(all_copies, p.n_free - used);
   const int top = used + taken - all_back;
@@ -360,7 +379,7 @@ __device__ __forceinline__ void fork_decide(const ForkParams& p, RowAt row_at) {
     uint32_t bits = __ldcg(&p.gone[w]);
     if (bits == 0) continue;
     p.gone[w] = 0u;
-    for (int at = top + back_before + p.word_at[w]; bits != 0; bits &= bits - 1, ++at) {
+    for (int at = top + back_before + (w < word0 + kPlanThreads ? first_at : p.word_at[w]); bits != 0; bits &= bits - 1, ++at) {
       const int page = (int)w * 32 + __ffs(bits) - 1;
       p.shares[page] = 0;
       if (at >= 0) p.free_pages[at] = page;
