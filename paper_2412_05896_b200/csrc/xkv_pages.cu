@@ -201,7 +201,9 @@ struct ForkParams {
   int4* rows;                         // [L * B] a ForkRow each
   int32_t* last;                      // [L * B] partly filled last page, -1: none
   int32_t* rank;                      // [L * B] place among the CTA's copies, -1: no copy
-  uint32_t* gone;                     // a bit a page: it may have lost its last holder, then: it has; zero between calls
+  // a bit a page: it may have lost its last holder, then: it has.  A call leaves it zero.  Bits that were there all the same (the workspace
+  // served another pool or operator) do no harm: fork_decide looks at the counter of each, and a page with holders drops out.
+  uint32_t* gone;
   int32_t* word_at;                   // bits before each of its words, within a CTA's share of them
   int32_t* fresh;                     // [L][B][cols] entries of caches that become forks
 };
@@ -318,7 +320,10 @@ __device__ __forceinline__ void fork_decide(const ForkParams& p, RowAt row_at) {
 #pragma unroll
     for (int u = 0; u < 4; ++u) word[u] = w0 + u * kPlanWarps < word1 ? __ldcg(&p.gone[w0 + u * kPlanWarps]) : 0u;
 #pragma unroll
-    for (int u = 0; u < 4; ++u) holders[u] = (word[u] >> lane) & 1u ? __ldcg(&p.shares[(w0 + u * kPlanWarps) * 32 + lane]) : 0;
+    for (int u = 0; u < 4; ++u) {
+      const int64_t page = (w0 + u * kPlanWarps) * 32 + lane;           // (the last word has bits behind the pool)
+      holders[u] = ((word[u] >> lane) & 1u) != 0 && page < p.n_pages ? __ldcg(&p.shares[page]) : 0;
+    }
 #pragma unroll
     for (int u = 0; u < 4; ++u) {
       if (holders[u] < -1) record_status(p.hdr, XKV_ERR_INVALID_ARG);          // dropped more often than it was held
@@ -603,7 +608,7 @@ struct CompactParams {
   int32_t* n_live;                    // pages in use, and those of them from n_live on
   int32_t* n_moved;
   int32_t* counts;                    // [kMaxCluster] pages in use of the CTAs' words
-  uint32_t* live;                     // a bit a page: in use; zero between calls
+  uint32_t* live;                     // a bit a page: in use
   int32_t* word_at;                   // pages in use before each of its words
   RowCopy* list;                      // [n_pages] src and dst of the pages that move, in ascending order
   int32_t* place;                     // [n_pages] of a page that moves: its place in the list
@@ -702,7 +707,10 @@ __global__ void __launch_bounds__(kPlanThreads, 1) compact_count_kernel(const Co
   asm volatile("griddepcontrol.wait;" ::: "memory");
   asm volatile("griddepcontrol.launch_dependents;");
   __shared__ int s_scan[kPlanWarps + 1];
-  const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5, n_warps = gridDim.x * kPlanWarps;
+  const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5, n_warps = gridDim.x * kPlanWarps, n_words = (p.n_pages + 31) / 32;
+  // (the map is cleared here, not at a call's end: another pool's or operator's call may have written over it since)
+  for (int w = blockIdx.x * kPlanThreads + threadIdx.x; w < n_words; w += gridDim.x * kPlanThreads) p.live[w] = 0u;
+  phase();
   for (int row = blockIdx.x * kPlanWarps + warp; row < p.n_rows; row += n_warps) {
     const int have = held(p, row);
 #pragma unroll 4
@@ -713,7 +721,6 @@ __global__ void __launch_bounds__(kPlanThreads, 1) compact_count_kernel(const Co
     }
   }
   phase();
-  const int n_words = (p.n_pages + 31) / 32;
   int64_t word0, word1;
   cta_run(n_words, &word0, &word1);
   int mine = 0;
@@ -750,12 +757,8 @@ __global__ void __launch_bounds__(kCopyThreads) compact_place_kernel(const Compa
   asm volatile("griddepcontrol.launch_dependents;");
   const int n_live = __ldcg(p.n_live), low = n_live - __ldcg(p.n_moved);
   const int64_t step = (int64_t)gridDim.x * kCopyThreads;
-  for (int64_t page = (int64_t)blockIdx.x * kCopyThreads + threadIdx.x; page < (p.n_pages + 31) / 32 * 32ll; page += step) {
-    const uint32_t bits = __ldcg(&p.live[page >> 5]);
-    if (page < p.n_pages) place_page(p, (int)page, bits, __ldcg(&p.word_at[page >> 5]), n_live, low);
-    __syncwarp();                     // a word's 32 pages are a warp's
-    if ((page & 31) == 0) p.live[page >> 5] = 0u;
-  }
+  for (int64_t page = (int64_t)blockIdx.x * kCopyThreads + threadIdx.x; page < p.n_pages; page += step)
+    place_page(p, (int)page, __ldcg(&p.live[page >> 5]), __ldcg(&p.word_at[page >> 5]), n_live, low);
 }
 
 __global__ void __launch_bounds__(kCopyThreads) compact_move_kernel(const CompactParams p, const CopyParams c) {
