@@ -15,7 +15,7 @@
 // off the sums.  The last CTA of a cache to finish joins the chunks (in their order, so the result does not depend on who that is)
 // and sets the ticket back to zero.
 // Weights are rounded to 16 bits for their product: half a step, 2^-8 of a weight in bf16, 2^-11 of weight times row scale in fp16, and
-// below 2^-14 of the largest such product 2^-25; sums, maxima and outputs are fp32.
+// below 2^-14 of the largest such product of a row that has a value 2^-25 (see ProductRef); sums, maxima and outputs are fp32.
 // Measured, device time: 16 caches of 49 - 146 rows of 64 7.4 us (floor 0.1: latencies of ids, rows, barriers and the launch); 2048 caches,
 // 1.66 GB of bf16 rows 264 us = 6.3 TB/s, HBM; int8, one head a KV head, 338 MB 65 us = 5.2 TB/s, the chains
 // of latencies at a CTA's two ends (loads take 36 % of L1's cycles, instructions 47 % of the issue slots).
@@ -237,6 +237,7 @@ __global__ void __launch_bounds__(32 * W, ctas_of_an_sm(D, W)) diff_decode_rows_
     }
   }
   float m[2] = {-INFINITY, -INFINITY}, l[2] = {0.f, 0.f};     // of query rows 2 tig and 2 tig + 1; l: of this lane's rows
+  ProductRef ref;                                             // 8-bit rows: of the products with V
   float o[D / 16][4];
 #pragma unroll
   for (int x = 0; x < D / 16; ++x) o[x][0] = o[x][1] = o[x][2] = o[x][3] = 0.f;
@@ -265,24 +266,52 @@ __global__ void __launch_bounds__(32 * W, ctas_of_an_sm(D, W)) diff_decode_rows_
       z[i] = gid + 8 * (i >> 1) < rows ? z[i] * p.scale_log2 : -INFINITY;
     }
     if (more) load_k(next);           // under the softmax and the outputs
-    // the warp's reference is exact on its first tile and raised lazily (by 2^8) afterwards; 8-bit rows: of the logits plus log2 of V's
-    // scales, so that the largest weight times scale, which is rounded to fp16, is 1 to 2^8 whatever the scales are
-    float top[2] = {fmaxf(z[0], z[2]), fmaxf(z[1], z[3])};
-    if constexpr (Q8) {
-      const float b0 = gid < rows ? __log2f(vs[0]) : 0.f, b1 = gid + 8 < rows ? __log2f(vs[1]) : 0.f;
-      top[0] = fmaxf(z[0] + b0, z[2] + b1), top[1] = fmaxf(z[1] + b0, z[3] + b1);
+    // rows behind the last one: no weight and no value, whatever lies there
+    if (rows < 16) {
+#pragma unroll
+      for (int y = 0; y < 2; ++y)
+        if (gid + 8 * y >= rows) {
+          vs[y] = 0.f;
+          if constexpr (!Q8) {
+#pragma unroll
+            for (int j = 0; j < kPieces; ++j) v[y].x[j][0] = v[y].x[j][1] = v[y].x[j][2] = v[y].x[j][3] = 0u;
+          }
+        }
     }
-    if (__any_sync(0xffffffffu, top[0] > m[0] + kLazy || top[1] > m[1] + kLazy)) {
+    // the warp's references are exact on its first tile and raised lazily (by 2^8) afterwards; 8-bit rows: that of the products as well
+    float top[2] = {fmaxf(z[0], z[2]), fmaxf(z[1], z[3])}, ptop[2] = {-INFINITY, -INFINITY};
+    bool grow = top[0] > m[0] + kLazy || top[1] > m[1] + kLazy;
+    if constexpr (Q8) {
+      const float b0 = __log2f(vs[0]), b1 = __log2f(vs[1]);
+      ptop[0] = fmaxf(z[0] + b0, z[2] + b1), ptop[1] = fmaxf(z[1] + b0, z[3] + b1);
+      grow = grow || ptop[0] > ref.mp[0] + kLazy || ptop[1] > ref.mp[1] + kLazy;
+    }
+    if (__any_sync(0xffffffffu, grow)) {
       float al[2];
+      if constexpr (Q8) {
+#pragma unroll
+        for (int y = 0; y < 2; ++y) {
+          uint32_t x = 0u;
+#pragma unroll
+          for (int j = 0; j < kPieces; ++j) x |= (v[y].x[j][0] ^ 0x80808080u) | (v[y].x[j][1] ^ 0x80808080u);
+          if (!row_has_value(x)) vs[y] = 0.f;
+        }
+        const float b0 = __log2f(vs[0]), b1 = __log2f(vs[1]);
+        ptop[0] = fmaxf(z[0] + b0, z[2] + b1), ptop[1] = fmaxf(z[1] + b0, z[3] + b1);
+      }
 #pragma unroll
       for (int i = 0; i < 2; ++i) {
 #pragma unroll
-        for (int x = 4; x < 32; x <<= 1) top[i] = fmaxf(top[i], __shfl_xor_sync(0xffffffffu, top[i], x));
+        for (int x = 4; x < 32; x <<= 1) {
+          top[i] = fmaxf(top[i], __shfl_xor_sync(0xffffffffu, top[i], x));
+          if constexpr (Q8) ptop[i] = fmaxf(ptop[i], __shfl_xor_sync(0xffffffffu, ptop[i], x));
+        }
         top[i] = fmaxf(top[i], m[i]);
         al[i] = m[i] == -INFINITY ? 0.f : fast_exp2(m[i] - top[i]);
         m[i] = top[i];
         l[i] *= al[i];
       }
+      if constexpr (Q8) ref.raise(m, ptop, al);
 #pragma unroll
       for (int x = 0; x < D / 16; ++x) {
         o[x][0] *= al[0];
@@ -298,21 +327,12 @@ __global__ void __launch_bounds__(32 * W, ctas_of_an_sm(D, W)) diff_decode_rows_
     for (int i = 0; i < 4; ++i) w[i] = fast_exp2(z[i] - (m[i & 1] == -INFINITY ? 0.f : m[i & 1]));
     l[0] += w[0] + w[2];
     l[1] += w[1] + w[3];
-    // the weights as the B operand (rounded to 16 bits, 8-bit rows: times the row's scale); rows behind the last one: no weight
-    // and no value, whatever lies there
-    if (rows < 16) {
+    // the weights as the B operand (rounded to 16 bits, 8-bit rows: times the row's scale)
+    if constexpr (Q8) {
 #pragma unroll
-      for (int y = 0; y < 2; ++y)
-        if (gid + 8 * y >= rows) {
-          vs[y] = 0.f;
-          if constexpr (!Q8) {
-#pragma unroll
-            for (int j = 0; j < kPieces; ++j) v[y].x[j][0] = v[y].x[j][1] = v[y].x[j][2] = v[y].x[j][3] = 0u;
-          }
-        }
+      for (int i = 0; i < 4; ++i) w[i] *= ref.f[i & 1] * vs[i >> 1];
     }
-    const uint32_t b0 = movmatrix_trans(pack16<Q8>(Q8 ? w[0] * vs[0] : w[0], Q8 ? w[1] * vs[0] : w[1]));
-    const uint32_t b1 = movmatrix_trans(pack16<Q8>(Q8 ? w[2] * vs[1] : w[2], Q8 ? w[3] * vs[1] : w[3]));
+    const uint32_t b0 = movmatrix_trans(pack16<Q8>(w[0], w[1])), b1 = movmatrix_trans(pack16<Q8>(w[2], w[3]));
 #pragma unroll
     for (int j = 0; j < kPieces; ++j)
 #pragma unroll
@@ -335,6 +355,7 @@ __global__ void __launch_bounds__(32 * W, ctas_of_an_sm(D, W)) diff_decode_rows_
   for (int i = 0; i < 2; ++i)
 #pragma unroll
     for (int x = 4; x < 32; x <<= 1) l[i] += __shfl_xor_sync(0xffffffffu, l[i], x);
+  const float back[2] = {ref.back(0, m[0]), ref.back(1, m[1])};
   // accumulator row gid of block (j, i) is column 4 i + gid % 2 of piece j of lane gid / 2, row gid + 8 the one 2 further; 8-bit rows:
   // + 2 (gid % 2), and the next one
 #pragma unroll
@@ -342,7 +363,7 @@ __global__ void __launch_bounds__(32 * W, ctas_of_an_sm(D, W)) diff_decode_rows_
 #pragma unroll
     for (int i = 0; i < 4; ++i) {
       const int col = Part::column(gid >> 1, x >> 1) + 4 * (x & 1) + (Q8 ? 2 * (gid & 1) + (i >> 1) : 2 * (i >> 1) + (gid & 1));
-      s_o[warp][2 * tig + (i & 1)][Out::at(col)] = Q8 ? fmaf(-kInt8Bias, w_sum[i], o[x][i]) : o[x][i];
+      s_o[warp][2 * tig + (i & 1)][Out::at(col)] = Q8 ? fmaf(-kInt8Bias, w_sum[i], o[x][i]) * back[i & 1] : o[x][i];
     }
   if (gid == 0) {
 #pragma unroll
