@@ -20,7 +20,7 @@ from . import xkv
 class XkvSession:
     # (until caches are forked pages are handed out in their order, each to one cache)
     free_pages = shares = None
-    _some = None                                             # live sequences of a step, their rows and counts on the device
+    _steps: dict | None = None                               # steps of some sequences, see _step_of_some
 
     def __init__(self, n_layers: int, n_q_heads: int, n_kv_heads: int, head_dim: int, window: int,
                  pool_kernel: int, lengths: list[int], pool_mode: int = xkv.POOL_MAX, page_size: int = 16,
@@ -469,13 +469,37 @@ class XkvSession:
             # one row a cache, head by head in a head-level session: the order in which the rows lie
             self._store_new(k_new, v_new, self.one_each, self.n_caches)
         elif any(self.live):
-            if self._some is None or self._some[0] != self.live:      # (so that a step can be captured after one like it)
-                counts = np.repeat(np.asarray(self.live, dtype=np.int32), self.n_caches // self.B)
-                self._some = (list(self.live), self._to_device(np.flatnonzero(self.live), np.int64),
-                              self._to_device(counts), int(counts.sum()))
-            _, rows, counts, n = self._some
+            rows, counts, n = self._step_of_some()
             self._store_new(k_new[:, rows], v_new[:, rows], counts, n)
         return None, None
+
+    KEPT_STEPS = 64
+
+    def _step_of_some(self):
+        """(live sequences, new rows of every cache, their sum) of a step, the first two on the device.  A captured step holds their
+        addresses, so those of a set of sequences that was captured stay for good; of others the last KEPT_STEPS sets do."""
+        key, captured = tuple(self.live), self._capturing()
+        if self._steps is None:
+            self._steps = {}
+        step = self._steps.pop(key, None)
+        if step is None:
+            if captured:                                     # (its copy from the host would be part of the graph)
+                raise RuntimeError("a step of some sequences can be captured after one of the same sequences has run")
+            counts = np.repeat(np.asarray(self.live, dtype=np.int32), self.n_caches // self.B)
+            step = [False, self._to_device(np.flatnonzero(self.live), np.int64), self._to_device(counts), int(counts.sum())]
+            spare = [k for k, other in self._steps.items() if not other[0]]
+            if len(spare) >= self.KEPT_STEPS:
+                del self._steps[spare[0]]
+        if captured:
+            step[0] = True
+        elif step[1].is_cuda:                                # (it may be dropped under a step on another stream)
+            for t in step[1:3]:
+                t.record_stream(torch.cuda.current_stream())
+        self._steps[key] = step                              # the last one used at the end
+        return step[1:]
+
+    def _capturing(self) -> bool:
+        return self.device.type == "cuda" and torch.cuda.is_current_stream_capturing()
 
     def diff_decode(self, q: torch.Tensor, k_new: torch.Tensor | None, v_new: torch.Tensor | None, lam: torch.Tensor,
                     gain: torch.Tensor | None = None, eps: float = 1e-5, out: torch.Tensor | None = None,

@@ -1,0 +1,78 @@
+"""Captured steps of a session whose live sequences change between replays."""
+import pytest
+import torch
+
+from paper_2412_05896_b200 import xkv
+
+from diff_util import DEV
+from test_gpu_session_pages import EPS, Run
+
+pytestmark = pytest.mark.gpu
+
+
+def test_captured_steps_of_several_sets():
+    """Two sets of live sequences captured each, steps of other sets in between and their tensors' memory written over; replays
+    against a twin that captures nothing."""
+    one, two = Run("int8"), Run("int8")
+    q, k, v = (torch.randn(3, 4, n, 64, generator=one.gen).to(torch.bfloat16).to(DEV) for n in (8, 2, 2))
+    step = lambda r: r.s.diff_decode(q, k, v, r.lam, r.gain, EPS)                 # noqa: E731
+    sets = {"a": [0, -1, 2, 3], "b": [-1, 1, 2, -1]}
+    graphs = {}
+
+    def again(r, counts):
+        kk, vv = (torch.full((3, sum(counts), 2, 64), 0.25, dtype=torch.bfloat16, device=DEV) for _ in "kv")
+        r.s.append(kk, vv, counts)
+
+    def to_set(r, name):
+        again(r, [1, 1, 1, 1])                                # all live
+        r.s.fork(sets[name])
+
+    for name in sets:
+        for r in (one, two):
+            to_set(r, name)
+            step(r)
+        torch.cuda.synchronize()
+        graphs[name] = torch.cuda.CUDAGraph()
+        with torch.cuda.graph(graphs[name]):
+            out = step(one)
+        graphs[name] = (graphs[name], out)
+    junk = []
+    for turn in range(6):
+        for other in ([0, 0, -1, -1], [-1, -1, -1, 3], [-1, 1, 2, 3]):
+            for r in (one, two):
+                again(r, [1, 1, 1, 1])
+                r.s.fork(other)
+                step(r)
+        junk += [torch.full((n,), 0x5A5A5A5A, dtype=torch.int32, device=DEV) for n in (4, 4, 6, 8, 16, 64, 128) * 8]
+        name = "ab"[turn % 2]
+        for r in (one, two):
+            to_set(r, name)
+        for t in (q, k, v):
+            t.copy_(torch.randn(t.shape, generator=one.gen).to(torch.bfloat16))
+        graph, out = graphs[name]
+        graph.replay()
+        want = step(two)
+        torch.cuda.synchronize()
+        assert torch.equal(out, want), turn
+        for x in ("seq_lens", "block_table", "shares", "pages_used", "free_pages"):
+            assert torch.equal(getattr(one.s, x), getattr(two.s, x)), (turn, x)
+    one.status()
+    two.status()
+
+
+def test_a_set_that_has_not_run_cannot_be_captured():
+    r = Run("bf16")
+    q, k, v = (torch.randn(3, 4, n, 64, generator=r.gen).to(torch.bfloat16).to(DEV) for n in (8, 2, 2))
+    r.s.diff_decode(q, k, v, r.lam, r.gain, EPS)
+    r.s.fork([0, -1, 2, 3])
+    torch.cuda.synchronize()
+    lens = r.s.seq_lens.clone()
+    graph = torch.cuda.CUDAGraph()
+    with pytest.raises(RuntimeError, match="captured"):
+        with torch.cuda.graph(graph):
+            r.s.diff_decode(q, k, v, r.lam, r.gain, EPS)
+    torch.cuda.synchronize()
+    assert torch.equal(lens, r.s.seq_lens)
+    r.s.diff_decode(q, k, v, r.lam, r.gain, EPS)
+    torch.cuda.synchronize()
+    assert r.s.device_status("append") == xkv.OK
