@@ -18,8 +18,7 @@ from . import xkv
 
 
 class XkvSession:
-    # (until caches are forked pages are handed out in their order, each to one cache)
-    free_pages = shares = None
+    free_pages = shares = None                               # with pages_on_demand: the list and the counters, in place from the start
     _steps: dict | None = None                               # steps of some sequences, see _step_of_some
 
     def __init__(self, n_layers: int, n_q_heads: int, n_kv_heads: int, head_dim: int, window: int,
@@ -131,6 +130,10 @@ class XkvSession:
             self.one_each = torch.ones(self.n_caches, dtype=torch.int32, device=self.device)   # a step's new rows
             self.ws_plan = self._ws(xkv.workspace_bytes(xkv.OP_PLAN_APPEND, self.dec_dims, n_layers=n_layers))
             self.ws_store = self._ws(xkv.workspace_bytes(xkv.OP_STORE_ROWS, self.dec_dims))
+            # (a step that is captured before the first fork hands pages out by the list that the fork changes, and a fork can be
+            # captured without one before it)
+            self._reset_pages()
+            self._page_workspaces()
         self.chunk_rows = decode_chunk_rows
         self.ws_decode = self._ws(xkv.workspace_bytes(xkv.OP_DECODE_ATTN, self.dec_dims, n_layers=n_layers,
                                                       max_cache_len=self.max_pages_per_seq * page_size,
@@ -533,6 +536,11 @@ class XkvSession:
         torch.arange(self.n_pages, out=self.free_pages)      # in place: captured steps hold their addresses
         self.shares.zero_()
 
+    def _page_workspaces(self) -> None:
+        sizes = dict(max_seqlen=self.max_pages_per_seq, total_tokens=self.n_pages, n_layers=self.L)
+        self.ws_fork = self._ws(xkv.workspace_bytes(xkv.OP_FORK_CACHES, self.dec_dims, **sizes))
+        self.ws_compact = self._ws(xkv.workspace_bytes(xkv.OP_COMPACT_PAGES, self.dec_dims, **sizes))
+
     def _per_cache(self, x, name: str, layers: bool) -> torch.Tensor:
         """Host integers or a dev int32 tensor, [B] (or [L, B]), as dev int32 of a layer's caches."""
         if isinstance(x, torch.Tensor):
@@ -585,9 +593,6 @@ class XkvSession:
         self.join()
         if self.free_pages is None:
             self._reset_pages()
-        if self.ws_fork is None:
-            self.ws_fork = self._ws(xkv.workspace_bytes(xkv.OP_FORK_CACHES, self.dec_dims, max_seqlen=self.max_pages_per_seq,
-                                                        total_tokens=self.n_pages, n_layers=self.L))
         stride = 0 if keep is None or keep.dim() == 1 else self.n_caches
         xkv.fork_caches(self.dec_dims, self.cache, parent, keep, stride, self.shares, self.free_pages, self.n_pages,
                         self.pages_used, self.ws_fork)
@@ -597,10 +602,6 @@ class XkvSession:
         if not self.pages_on_demand:
             raise ValueError("compact needs a session with pages_on_demand=True")
         self.join()
-        if self.ws_compact is None:
-            self.ws_compact = self._ws(xkv.workspace_bytes(xkv.OP_COMPACT_PAGES, self.dec_dims,
-                                                           max_seqlen=self.max_pages_per_seq, total_tokens=self.n_pages,
-                                                           n_layers=self.L))
         xkv.compact_pages(self.dec_dims, self.cache, self.block_table, self.shares, self.shares, self.free_pages,
                           self.pages_used, self.ws_compact)
 
@@ -614,8 +615,6 @@ class XkvSession:
             raise xkv.XkvError(st, "resize_pool")
         if not max(used, 1) <= n_pages < 2 ** 31:
             raise ValueError(f"resize_pool: {used} pages are in use")
-        if self.free_pages is None:
-            self._reset_pages()
         old, old_cache = (self.k_pages, self.v_pages, self.k_scales, self.v_scales), self.cache
         new = [None if x is None else torch.zeros(n_pages, *x.shape[1:], dtype=x.dtype, device=x.device) for x in old]
         ptrs = [None if x is None else x.data_ptr() for x in new]
@@ -630,7 +629,7 @@ class XkvSession:
         shares = torch.zeros(n_pages, dtype=torch.int32, device=self.device)
         shares[:used] = self.shares[:used]
         self.cache, self.n_pages, self.free_pages, self.shares = cache, n_pages, ids, shares
-        self.ws_fork = self.ws_compact = None                # sized by the pool
+        self._page_workspaces()                              # sized by the pool
 
     def device_status(self, which: str = "decode") -> int:
         """First error any call of that kind recorded since the last check (the status words are sticky and

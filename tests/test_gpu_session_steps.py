@@ -76,3 +76,63 @@ def test_a_set_that_has_not_run_cannot_be_captured():
     r.s.diff_decode(q, k, v, r.lam, r.gain, EPS)
     torch.cuda.synchronize()
     assert r.s.device_status("append") == xkv.OK
+
+
+def same_state(one, two):
+    for x in ("seq_lens", "block_table", "shares", "pages_used", "free_pages"):
+        assert torch.equal(getattr(one.s, x), getattr(two.s, x)), x
+
+
+def test_a_step_captured_before_the_first_fork():
+    """It goes on with the pages that forks, frees and cuts have given back, not with those of its own count."""
+    one, two = Run("bf16"), Run("bf16")
+    q, k, v = (torch.randn(3, 4, n, 64, generator=one.gen).to(torch.bfloat16).to(DEV) for n in (8, 2, 2))
+    for r in (one, two):
+        r.s.diff_decode(q, k, v, r.lam, r.gain, EPS)
+    torch.cuda.synchronize()
+    graph = torch.cuda.CUDAGraph()
+    with torch.cuda.graph(graph):
+        out = one.s.diff_decode(q, k, v, one.lam, one.gain, EPS)
+    for i in range(40):
+        for r in (one, two):
+            if i % 8 == 3:                                    # (beams: every sequence goes on)
+                r.s.fork([[1, 1, 0, 2], [3, 0, 2, 2]][i // 8 % 2])
+            if i % 8 == 6:
+                r.s.cut([5, 0, 11, 2])
+        for t in (q, k, v):
+            t.copy_(torch.randn(t.shape, generator=one.gen).to(torch.bfloat16))
+        graph.replay()
+        want = two.s.diff_decode(q, k, v, two.lam, two.gain, EPS)
+        torch.cuda.synchronize()
+        assert torch.equal(out, want), i
+        same_state(one, two)
+    one.status()
+    two.status()
+
+
+def test_the_first_fork_is_captured():
+    """Replays go on from each other's state, not from that of the capture."""
+    one, two = Run("int8"), Run("int8")
+    parent = torch.tensor([0, 1, 2, 3], dtype=torch.int32, device=DEV)
+    q, k, v = (torch.randn(3, 4, n, 64, generator=one.gen).to(torch.bfloat16).to(DEV) for n in (8, 2, 2))
+    for r in (one, two):
+        r.s.diff_decode(q, k, v, r.lam, r.gain, EPS)
+    torch.cuda.synchronize()
+    graph = torch.cuda.CUDAGraph()
+    with torch.cuda.graph(graph):
+        one.s.fork(parent)
+        out = one.s.diff_decode(q, k, v, one.lam, one.gain, EPS)
+    for p in ([0, 0, 1, 3], [3, 2, 1, 0], [1, 1, 1, -1], [0, 2, 2, 2]) * 3:
+        parent.copy_(torch.tensor(p, dtype=torch.int32))
+        graph.replay()
+        two.s.fork(parent)
+        want = two.s.diff_decode(q, k, v, two.lam, two.gain, EPS)
+        torch.cuda.synchronize()
+        assert torch.equal(out, want)
+        same_state(one, two)
+    one.s.compact()
+    two.s.compact()
+    torch.cuda.synchronize()
+    same_state(one, two)
+    one.status()
+    two.status()
