@@ -606,9 +606,9 @@ class XkvSession:
                           self.pages_used, self.ws_compact)
 
     def resize_pool(self, n_pages: int) -> None:
-        """The pages in use in a new pool of n_pages, the old one given up (waits for the device; steps captured
-        before it still read and write the old one).  Needs pages_on_demand; ValueError, and the pool as it was, when they do not fit; an error that device_status("pages") has
-        not reported yet is raised."""
+        """The pages in use in a new pool of n_pages, the old one given up (waits for the device).  Steps captured before it may not
+        be replayed any more: they read and write memory that is no longer the session's.  Needs pages_on_demand; ValueError,
+        and the pool as it was, when the pages do not fit; an error that device_status("pages") has not reported yet is raised."""
         self.compact()
         used, st = int(self.pages_used.item()), self.device_status("pages")
         if st != xkv.OK:
@@ -628,6 +628,9 @@ class XkvSession:
         self.k_pages, self.v_pages, self.k_scales, self.v_scales = new
         shares = torch.zeros(n_pages, dtype=torch.int32, device=self.device)
         shares[:used] = self.shares[:used]
+        for t in (*old, self.free_pages, self.shares, self.ws_fork, self.ws_compact):
+            if t is not None:                                # given up while the copy is still to come, on whatever stream
+                t.record_stream(torch.cuda.current_stream())
         self.cache, self.n_pages, self.free_pages, self.shares = cache, n_pages, ids, shares
         self._page_workspaces()                              # sized by the pool
 

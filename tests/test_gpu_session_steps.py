@@ -136,3 +136,34 @@ def test_the_first_fork_is_captured():
     same_state(one, two)
     one.status()
     two.status()
+
+
+def test_a_pool_resized_on_another_stream():
+    """The session is made on one stream and resized on another, which is late: the old pool's memory is not handed out before the
+    copy has read it."""
+    side = torch.cuda.Stream()
+    with torch.cuda.stream(side):
+        r = Run("int8", d=128)
+        s = r.s
+        s.resize_pool(6000)                                   # (allocated on this stream, in blocks of its own)
+        torch.cuda.synchronize()
+    used, old = int(s.pages_used.item()), {x.data_ptr() for x in (s.k_pages, s.v_pages, s.free_pages, s.shares)}
+    shapes = [(x.shape, x.dtype) for x in (s.k_pages, s.v_pages, s.k_scales, s.v_scales, s.free_pages, s.shares)]
+    late = xkv.copy_pages
+
+    def copy_pages(*args, **kw):
+        torch.cuda._sleep(400_000_000)                        # about a fifth of a second
+        return late(*args, **kw)
+
+    xkv.copy_pages = copy_pages
+    try:
+        s.resize_pool(used + 40)
+    finally:
+        xkv.copy_pages = late
+    with torch.cuda.stream(side):                             # the other stream's next allocations, of the sizes given up
+        taken = [torch.full(shape, 77, dtype=dtype, device=DEV) for shape, dtype in shapes for _ in range(2)]
+    assert not old & {x.data_ptr() for x in taken}
+    torch.cuda.synchronize()
+    r.expect(r.rows)
+    r.step([True] * 4)
+    r.status()
