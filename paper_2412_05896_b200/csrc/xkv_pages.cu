@@ -419,7 +419,7 @@ __host__ __device__ inline SmallFork small_fork(int n_rows, int cols, int n_page
 __global__ void __launch_bounds__(kPlanThreads, 1) fork_small_kernel(const ForkParams p, const CopyParams c) {
   asm volatile("griddepcontrol.wait;" ::: "memory");
   asm volatile("griddepcontrol.launch_dependents;");
-  extern __shared__ int32_t s_mem[];
+  extern __shared__ __align__(16) int32_t s_mem[];           // (rows are read as int4)
   __shared__ int s_scan[kPlanWarps + 1];
   __shared__ int s_busy[kPlanThreads];
   const int tid = threadIdx.x, lane = tid & 31, warp = tid >> 5;
