@@ -216,15 +216,15 @@ struct ForkRow {
 __device__ __forceinline__ ForkRow as_row(int4 x) { return {x.x, x.y, x.z, x.w}; }
 
 __device__ __forceinline__ int parent_of(const ForkParams& p, int b) {
-  const int a = __ldg(&p.parent[b]);
+  const int a = __ldcg(&p.parent[b]);
   return a >= -1 && a < p.batch ? a : b;
 }
 
 // What becomes of a cache; lengths as they were before the step.
 __device__ __forceinline__ int4 fork_row(const ForkParams& p, int row) {
   const int l = row / p.batch, b = row - l * p.batch, most = p.cols * p.page_size;
-  const int own = __ldcg(&p.lens[row]), k = p.keep != nullptr ? __ldg(&p.keep[(size_t)l * p.keep_stride + b]) : -1;
-  const int asked = __ldg(&p.parent[b]), a = asked >= -1 && asked < p.batch ? asked : b;
+  const int own = __ldcg(&p.lens[row]), k = p.keep != nullptr ? __ldcg(&p.keep[(size_t)l * p.keep_stride + b]) : -1;
+  const int asked = __ldcg(&p.parent[b]), a = asked >= -1 && asked < p.batch ? asked : b;
   if (a != asked) record_status(p.hdr, XKV_ERR_INVALID_ARG);
   const int n = min(max(own, 0), most);
   int rows = a < 0 ? 0 : (a == b ? n : min(max(__ldcg(&p.lens[(size_t)l * p.batch + a]), 0), most));
@@ -437,12 +437,12 @@ __global__ void __launch_bounds__(kPlanThreads, 1) fork_small_kernel(const ForkP
     for (int i = tid; i < n_words; i += kPlanThreads) s_words[i] = 0u;
     __syncthreads();
     for (int row = tid; row < p.n_rows; row += kPlanThreads) {
-      const int l = row / p.batch, b = row - l * p.batch, asked = __ldg(&p.parent[b]);
+      const int l = row / p.batch, b = row - l * p.batch, asked = __ldcg(&p.parent[b]);
       const int a = asked >= -1 && asked < p.batch ? asked : b;
       if (a != asked) record_status(p.hdr, XKV_ERR_INVALID_ARG);
       int rows = a < 0 ? 0 : s_lens[row - b + a];
       if (p.keep != nullptr) {
-        const int k = __ldg(&p.keep[(size_t)l * p.keep_stride + b]);
+        const int k = __ldcg(&p.keep[(size_t)l * p.keep_stride + b]);
         if (k >= 0) rows = min(rows, k);
       }
       const ForkRow r = {a, rows, (s_lens[row] + p.page_size - 1) / p.page_size, (rows + p.page_size - 1) / p.page_size};
@@ -616,7 +616,7 @@ struct CompactParams {
 
 // Pages that cache `row` holds.
 __device__ __forceinline__ int held(const CompactParams& p, int64_t row) {
-  return (min(max(__ldg(&p.lens[row]), 0), p.cols * p.page_size) + p.page_size - 1) / p.page_size;
+  return (min(max(__ldcg(&p.lens[row]), 0), p.cols * p.page_size) + p.page_size - 1) / p.page_size;
 }
 
 // A thread: where page `page` goes.  bits: its word of `live`, at: pages in use before that word, low: pages in use below n_live.
@@ -800,7 +800,9 @@ Layout compact_layout(int64_t n_pages) {
   return L;
 }
 
-// All launches here wait for the one before them on the device, so that their CTAs may be in place when it ends.
+// All launches here wait for the one before them on the device, so that their CTAs may be in place when it ends.  What it may still be
+// writing then (lengths, parents, counts) is read by ordinary loads, not through the read-only path, which is for data that nobody
+// writes while the kernel is there.
 template <typename... Args>
 xkv_status launch_after(void (*kernel)(Args...), int grid, int threads, bool cluster, cudaStream_t st, size_t smem,
                         Args... args) {
