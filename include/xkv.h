@@ -642,8 +642,8 @@ void xkv_profile_events(void* start, void* stop);
  * Test hook (no counterpart in the paper), process-wide: the limit of every bounded wait inside the kernels
  * (nanoseconds; <= 0 restores the default of two seconds), and the index of one decode work item whose
  * split-K merge ticket is never published (-1: none), so that a test can watch a wait run out: the kernel
- * returns, the device status reads XKV_ERR_TIMEOUT and the workspace stays usable. (Decode over XKV_KV_E4M3 caches has no
- * wait for a ticket: there the second argument is the index of a CTA whose copies are never issued.)
+ * returns, the device status reads XKV_ERR_TIMEOUT and the workspace stays usable. (Decode over XKV_KV_E4M3 caches and
+ * xkv_diff_prefill_attn have no wait for a ticket: there the second argument is the index of a CTA whose copies are never issued.)
  */
 void xkv_test_hooks(int64_t wait_limit_ns, int32_t withhold_decode_item);
 

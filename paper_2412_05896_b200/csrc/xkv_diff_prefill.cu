@@ -61,6 +61,7 @@ struct Params {
   WorkspaceHeader* hdr;
   int64_t total_tokens;
   int32_t batch, n_q_heads, group, max_seqlen;
+  int32_t withhold_cta;               // test hook: this CTA's Q and K tiles are never asked for, so that waits expire (-1: none)
   float scale_log2, eps;
   uint64_t wait_ns;
 };
@@ -262,6 +263,7 @@ diff_prefill_kernel(const __grid_constant__ CUtensorMap tmap_q, const __grid_con
     Item it;
     for (uint32_t n = 0; get_item(n, &it); ++n) {
       done_item(n);
+      if ((int)blockIdx.x == p.withhold_cta) break;
       const int n_kt = key_tiles(it), g = it.h / p.group;
       if (n >= 2 && !wait(&s_q_empty[n & 1], (n / 2) - 1)) break;
       if (elect_one()) {
@@ -608,6 +610,7 @@ xkv_status diff_prefill_attn(const xkv_dims* d, const void* q, const void* k, co
   p.scale_log2 = (d->scale != 0.f ? d->scale : 1.0f / sqrtf((float)(d->head_dim / 2))) * 1.4426950408889634f;
   p.eps = eps;
   p.wait_ns = wait_limit_ns();
+  p.withhold_cta = debug_withhold_item();
   CUtensorMap tq, tk, tv;
   if (!tc_make_token_tmap(&tq, q, d->head_dim, d->n_q_heads, total_tokens, (int64_t)d->n_q_heads * d->head_dim, d->head_dim,
                           kRows) ||
