@@ -135,12 +135,15 @@ class XkvSession:
             self._reset_pages()
             self._page_workspaces()
         self.chunk_rows = decode_chunk_rows
-        self.ws_decode = self._ws(xkv.workspace_bytes(xkv.OP_DECODE_ATTN, self.dec_dims, n_layers=n_layers,
-                                                      max_cache_len=self.max_pages_per_seq * page_size,
-                                                      chunk_rows=decode_chunk_rows))
+        # one workspace for both kinds of heads, made here: one that is made while a step is captured is zero only once the step is
+        # replayed, and a call before that would find whatever lies there
+        self.ws_decode = self.ws_diff_decode = self._ws(max(
+            xkv.workspace_bytes(op, self.dec_dims, n_layers=n_layers, max_cache_len=self.max_pages_per_seq * page_size,
+                                chunk_rows=decode_chunk_rows) for op in (xkv.OP_DECODE_ATTN, xkv.OP_DIFF_DECODE_ATTN)))
         self.out = torch.empty(n_layers, self.B, n_q_heads, head_dim, **bf16)
         self.lse = torch.empty(n_layers, self.B, n_q_heads, **f32)
-        self.ws_diff_decode = self.ws_diff_prefill = self.diff_lse = None
+        self.ws_diff_prefill = self._ws(xkv.workspace_bytes(xkv.OP_DIFF_PREFILL_ATTN, self.dims))
+        self.diff_lse = None
         self.budgets: np.ndarray | None = None
         self.last_solver_ms: float | None = None      # host time of the last xkv_alloc_budgets call
         self.r_avg: float | None = None
@@ -248,8 +251,6 @@ class XkvSession:
             out = torch.empty_like(q)
         if lse is None:
             lse = torch.empty(self.Hq, 2, self.T, dtype=torch.float32, device=self.device)
-        if self.ws_diff_prefill is None:
-            self.ws_diff_prefill = self._ws(xkv.workspace_bytes(xkv.OP_DIFF_PREFILL_ATTN, self.dims))
         xkv.diff_prefill_attn(self.dims, q, k, v, lam, gain, eps, self.cu, self.T, self.max_seqlen, out, lse,
                               self.ws_diff_prefill)
         return out, lse
@@ -517,10 +518,7 @@ class XkvSession:
         n = layer_end - layer_begin
         self._check_diff(lam, gain, (n, self.Hq), (n, self.d))
         out = self.out if out is None else out
-        if self.ws_diff_decode is None:
-            self.ws_diff_decode = self._ws(xkv.workspace_bytes(
-                xkv.OP_DIFF_DECODE_ATTN, self.dec_dims, n_layers=self.L,
-                max_cache_len=self.max_pages_per_seq * self.page_size, chunk_rows=self.chunk_rows))
+        if lse is None and self.diff_lse is None:
             self.diff_lse = torch.empty(self.L, self.B, self.Hq, 2, dtype=torch.float32, device=self.device)
         k_new, v_new = self._store_step(k_new, v_new, layer_begin, layer_end)
         xkv.diff_decode_attn(self.dec_dims, self.cache, layer_begin, layer_end, q, k_new, v_new, lam, gain, eps, out,

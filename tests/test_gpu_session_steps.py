@@ -167,3 +167,26 @@ def test_a_pool_resized_on_another_stream():
     r.expect(r.rows)
     r.step([True] * 4)
     r.status()
+
+
+@pytest.mark.parametrize("fmt", ["bf16", "int8", "e4m3"])
+def test_the_first_differential_step_is_captured(fmt):
+    """Calls between the capture and the first replay, and after it, are right, and the status is that of the calls."""
+    one, two = Run(fmt), Run(fmt)
+    q, k, v = (torch.randn(3, 4, n, 64, generator=one.gen).to(torch.bfloat16).to(DEV) for n in (8, 2, 2))
+    junk = [torch.full((1 << 20,), 0x5A5A5A5A, dtype=torch.int32, device=DEV) for _ in range(64)]
+    del junk                                                  # what the allocator hands out next is not zero
+    graph = torch.cuda.CUDAGraph()
+    with torch.cuda.graph(graph):
+        out = one.s.diff_decode(q, k, v, one.lam, one.gain, EPS)
+    one.status()
+    for i in range(6):
+        if i % 3 == 0:
+            got = one.s.diff_decode(q, k, v, one.lam, one.gain, EPS)
+        else:
+            graph.replay()
+            got = out
+        want = two.s.diff_decode(q, k, v, two.lam, two.gain, EPS)
+        torch.cuda.synchronize()
+        assert torch.equal(got, want) and torch.equal(one.s.diff_lse, two.s.diff_lse), i
+        one.status()
