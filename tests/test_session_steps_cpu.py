@@ -51,3 +51,14 @@ def test_a_set_that_has_not_run_is_not_captured(monkeypatch):
     with pytest.raises(RuntimeError, match="captured"):
         step(s, [0, -1, 2])
     assert s.calls[-1][0] == "fork_caches"                    # nothing of the step has begun
+
+
+def test_rows_make_a_freed_sequence_live(monkeypatch):
+    s = small_session(monkeypatch)
+    s.fork([-1, -1, 2])
+    k = torch.zeros(2, 2, 2, 64, dtype=torch.bfloat16)
+    s.append(k, k, [0, 2, 0])
+    assert s.live == [False, True, True] and all(type(x) is bool for x in s.live)
+    live = s.live = [True] * 3
+    s.append(k, k, [0, 2, 0])
+    assert s.live is live                                     # nothing to look at
