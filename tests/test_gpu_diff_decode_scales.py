@@ -128,3 +128,75 @@ def test_no_row_has_a_value(longest, scale, code, chunk):
         assert not out.float().any() and bool(torch.isfinite(sums).all())
         check(c, 4, q, lam, g, out, None)
         check_lse(c, q, sums)
+
+
+@pytest.mark.parametrize("name,rows", PLACES, ids=[p[0] for p in PLACES])
+@pytest.mark.parametrize("B,H,G,d,page,longest", [(3, 2, 4, 128, 16, 400), (2, 1, 2, 64, 32, 6000), (2, 2, 6, 128, 64, 300)])
+def test_far_rows_of_zeros_with_chunks(B, H, G, d, page, longest, name, rows):
+    """The streaming kernel, caches cut and joined."""
+    require_lib()
+    lens = np.random.default_rng(1).integers(91, longest + 1, (1, B))
+    lens.flat[0] = longest
+    c = RowCache("int8", 1, B, H, d, lens, page, seed=3)
+    small_scales(c)
+    for b in range(B):
+        plant(c, 0, b, [r % int(c.lens[0, b]) for r in rows], 1.0, 128, FAR)
+    run(c, G, queries(1, B, H * G, d, 6), 64)
+
+
+def test_far_rows_of_zeros_in_pages_that_start_on_16_bytes():
+    require_lib()
+    c = RowCache("int8", 1, 2, 2, 128, [[333, 97]], 32, seed=3)
+    small_scales(c)
+    for b in range(2):
+        plant(c, 0, b, [0, 50, 96], 1.0, 128, FAR)
+    for i in range(2):
+        x = c.pages[i]
+        room = torch.empty(x.numel() + 32, dtype=torch.uint8, device=DEV)
+        c.pages[i] = room[16:-16].view(x.shape).copy_(x)
+        assert c.pages[i].data_ptr() % 32 == 16
+    run(c, 4, queries(1, 2, 8, 128, 6))
+
+
+@pytest.mark.parametrize("chunk", [0, 64])
+@pytest.mark.parametrize("d", [64, 128])
+def test_a_far_new_row_of_zeros(d, chunk):
+    """Stored by the call, with the scale that a row of zeros gets."""
+    require_lib()
+    L, B, H, G, page = 1, 3, 2, 3, 16
+    c = RowCache("int8", L, B, H, d, [[100, 15, 320]], page, extra=1, seed=3)
+    small_scales(c)
+    q = queries(L, B, H * G, d, 6)
+    lam, gain = (t.to(DEV) for t in weights(L, H * G, d, 5))
+    kn, vn = (torch.full((L, B, H, d), x, dtype=torch.bfloat16, device=DEV) for x in (FAR, 0.0))
+    out, sums = attend(c, H * G, q, lam, gain, kn, vn, chunk=chunk, eps=0.0)
+    scale = float(np.float32(FAR) / np.float32(127))
+    for b in range(B):
+        n = int(c.lens[0, b])
+        at = c.table[0, b, n // page].long()
+        assert bool((c.scales[1][at, :, n % page] == 1.0).all()) and bool((c.pages[1][at, :, n % page] == 128).all())
+        c.values[0][at, :, n % page], c.values[1][at, :, n % page] = 127 * scale, 0.0
+    c.lens = c.lens + 1
+    c.fmt = "bf16"                     # (no absolute error of a weight)
+    check(c, H * G, q, lam, gain, out, None, eps=0.0)
+    check_lse(c, q, sums)
+
+
+@pytest.mark.parametrize("power", [-24, -14, 12, 30])
+def test_row_scales_of_any_size_with_chunks(power):
+    """V's scales far from 1, and a block of rows whose scales are far from the others', in the streaming kernel."""
+    require_lib()
+    c = RowCache("int8", 1, 3, 2, 128, [[400, 37, 1000]], 16, seed=3)
+    c.scales[1] *= 2.0 ** power
+    c.values[1] *= 2.0 ** power
+    first = c.table[0, :, 0].long()
+    c.scales[1][first] *= 2.0 ** -20
+    c.values[1][first] *= 2.0 ** -20
+    lam, gain = (t.to(DEV) for t in weights(1, 8, 128, 5))
+    q = queries(1, 3, 8, 128, 6)
+    for g in (gain, None):
+        out, sums = attend(c, 8, q, lam, g, chunk=64, eps=0.0)
+        c.fmt = "bf16"
+        check(c, 8, q, lam, g, out, None, eps=0.0)
+        c.fmt = "int8"
+        check_lse(c, q, sums)
