@@ -122,26 +122,11 @@ __device__ __forceinline__ uint32_t int8x2_to_biased_f16x2(uint32_t word) {
   asm("prmt.b32 %0, %1, 0x64646464, %2;" : "=r"(r) : "r"(word), "n"(kSelector));
   return r;
 }
-// Products of weights and 8-bit rows under a norm, where the smallest output counts: the fp16 products weight * scale of V's row have
-// a reference of their own, the largest of those that reach an output, beside the one of the denominators.  A row that has no value (all
-// its bytes 128, stored with scale 1, 2^8 of an ordinary row's; or scale 0) can have any logit and must not set it.
-//   m: reference of the denominators (largest logit), mp: of the products (largest logit + log2 scale), f = 2^(m - mp)
-// so a product is 2^(z - m) * f * scale.  mp is at least m - 60: below that nothing is left of an output beside its denominator.
-struct ProductRef {
-  float mp[2] = {-INFINITY, -INFINITY}, f[2] = {1.f, 1.f};
-  // A raise; top: over the warp.  What the outputs so far are multiplied by goes to al.
-  __device__ __forceinline__ void raise(const float (&m)[2], const float (&top)[2], float (&al)[2]) {
-#pragma unroll
-    for (int i = 0; i < 2; ++i) {
-      const float to = fmaxf(fmaxf(mp[i], top[i]), m[i] - 60.f);
-      al[i] = mp[i] == -INFINITY ? 0.f : fast_exp2(mp[i] - to);
-      f[i] = to == -INFINITY ? 1.f : fast_exp2(m[i] - to);
-      mp[i] = to;
-    }
-  }
-  // outputs and products with ones: from 2^mp to 2^m
-  __device__ __forceinline__ float back(int i, float m) const { return mp[i] == -INFINITY ? 0.f : fast_exp2(mp[i] - m); }
-};
+// The softmax's reference of 8-bit rows under a norm, where the smallest output counts: the largest logit + log2 of the row's V scale, so
+// that the largest product of a weight and its row's scale, which is rounded to fp16, is 1.  A row without a value (all its V bytes
+// 128, stored with scale 1, 2^8 of an ordinary row's; or scale 0) can have any logit; it must not set the reference, only keep it
+// within 2^90, so that its weight, which counts in the denominator alone, is a number: this is the least that a row's scale counts for.
+__device__ __forceinline__ float scale_share(float scale) { return fmaxf(__log2f(scale), -90.f); }
 // Lanes 4 r .. 4 r + 3 hold a row; whether any of them has a byte that stands for a value (x: the bytes that differ from 128).
 __device__ __forceinline__ bool row_has_value(uint32_t x) {
   return ((__ballot_sync(0xffffffffu, x != 0u) >> (threadIdx.x & 28u)) & 15u) != 0u;

@@ -661,8 +661,7 @@ decode_attn_kernel(const __grid_constant__ CUtensorMap tmap_k, const __grid_cons
       }
     };
 
-    constexpr bool kTwoRefs = Q8 && Diff;                // products with V under a norm: see ProductRef
-    [[maybe_unused]] ProductRef ref;
+    constexpr bool kScaleInRef = Q8 && Diff;             // products with V under a norm: see scale_share
     const int n_tiles = (I.w - I.z + kTileRows - 1) / kTileRows;
     // The row this call appends to (e, h) is the last row of the unit's last chunk.  Its page slot still holds
     // old bytes when the tile is copied in, so the owner of that chunk takes the row from k_new / v_new:
@@ -763,18 +762,14 @@ decode_attn_kernel(const __grid_constant__ CUtensorMap tmap_k, const __grid_cons
           }
         }
         float mx0 = fmaxf(sv[0], sv[2]), mx1 = fmaxf(sv[1], sv[3]);
-        bool grow = (mx0 > m_ref[0] + kLazy) || (mx1 > m_ref[1] + kLazy);
-        [[maybe_unused]] float ptop[2];
-        auto product_tops = [&] {
-          const float b0 = __log2f(vs0), b1 = __log2f(vs1);
-          ptop[0] = fmaxf(sv[0] + b0, sv[2] + b1), ptop[1] = fmaxf(sv[1] + b0, sv[3] + b1);
+        [[maybe_unused]] auto tops_with_scales = [&] {
+          const float b0 = scale_share(vs0), b1 = scale_share(vs1);
+          mx0 = fmaxf(sv[0] + b0, sv[2] + b1), mx1 = fmaxf(sv[1] + b0, sv[3] + b1);
         };
-        if constexpr (kTwoRefs) {
-          product_tops();
-          grow = grow || ptop[0] > ref.mp[0] + kLazy || ptop[1] > ref.mp[1] + kLazy;
-        }
+        if constexpr (kScaleInRef) tops_with_scales();
+        const bool grow = (mx0 > m_ref[0] + kLazy) || (mx1 > m_ref[1] + kLazy);
         if (__any_sync(0xffffffffu, grow)) {
-          if constexpr (kTwoRefs) {                    // a quarter of rows gid and gid + 8 a lane
+          if constexpr (kScaleInRef) {                  // a quarter of rows gid and gid + 8 a lane
             const uint8_t* vt = raw_v(s) + gid * D + tig * (D / 4);
             uint32_t x0 = 0u, x1 = 0u;
 #pragma unroll
@@ -785,12 +780,7 @@ decode_attn_kernel(const __grid_constant__ CUtensorMap tmap_k, const __grid_cons
             }
             if (!row_has_value(x0)) vs0 = 0.f;
             if (!row_has_value(x1)) vs1 = 0.f;
-            product_tops();
-#pragma unroll
-            for (int x = 4; x < 32; x <<= 1) {
-              ptop[0] = fmaxf(ptop[0], __shfl_xor_sync(0xffffffffu, ptop[0], x));
-              ptop[1] = fmaxf(ptop[1], __shfl_xor_sync(0xffffffffu, ptop[1], x));
-            }
+            tops_with_scales();
           }
 #pragma unroll
           for (int x = 4; x < 32; x <<= 1) {
@@ -798,16 +788,11 @@ decode_attn_kernel(const __grid_constant__ CUtensorMap tmap_k, const __grid_cons
             mx1 = fmaxf(mx1, __shfl_xor_sync(0xffffffffu, mx1, x));
           }
           const float n0 = fmaxf(m_ref[0], mx0), n1 = fmaxf(m_ref[1], mx1);
-          float al0 = fast_exp2(m_ref[0] - n0), al1 = fast_exp2(m_ref[1] - n1);
+          const float al0 = fast_exp2(m_ref[0] - n0), al1 = fast_exp2(m_ref[1] - n1);
           m_ref[0] = n0;
           m_ref[1] = n1;
           l_part[0] *= al0;
           l_part[1] *= al1;
-          if constexpr (kTwoRefs) {
-            float al[2];
-            ref.raise({n0, n1}, ptop, al);
-            al0 = al[0], al1 = al[1];
-          }
 #pragma unroll
           for (int mt = 0; mt < D / 16; ++mt) {
             o[mt][0] *= al0;
@@ -822,14 +807,10 @@ decode_attn_kernel(const __grid_constant__ CUtensorMap tmap_k, const __grid_cons
             p_sum[3] *= al1;
           }
         }
-        float p0 = fast_exp2(sv[0] - m_ref[0]), p1 = fast_exp2(sv[1] - m_ref[1]);
-        float p2 = fast_exp2(sv[2] - m_ref[0]), p3 = fast_exp2(sv[3] - m_ref[1]);
+        const float p0 = fast_exp2(sv[0] - m_ref[0]), p1 = fast_exp2(sv[1] - m_ref[1]);
+        const float p2 = fast_exp2(sv[2] - m_ref[0]), p3 = fast_exp2(sv[3] - m_ref[1]);
         l_part[0] += p0 + p2;
         l_part[1] += p1 + p3;
-        if constexpr (kTwoRefs) {
-          p0 *= ref.f[0], p1 *= ref.f[1];
-          p2 *= ref.f[0], p3 *= ref.f[1];
-        }
         // P^T as the B operand of O^T += V^T.P^T: transpose the two 8x8 blocks of the accumulator layout
         const uint32_t b0 = movmatrix_trans(Q8 ? pack_f16(p0 * vs0, p1 * vs0) : pack_bf16(p0, p1));
         const uint32_t b1 = movmatrix_trans(Q8 ? pack_f16(p2 * vs1, p3 * vs1) : pack_bf16(p2, p3));
@@ -875,12 +856,6 @@ decode_attn_kernel(const __grid_constant__ CUtensorMap tmap_k, const __grid_cons
         o[mt][2] -= kInt8Bias * p_sum[0];
         o[mt][3] -= kInt8Bias * p_sum[1];
       }
-    }
-    if constexpr (kTwoRefs) {
-#pragma unroll
-      for (int mt = 0; mt < D / 16; ++mt)
-#pragma unroll
-        for (int i = 0; i < 4; ++i) o[mt][i] *= ref.back(i & 1, m_ref[i & 1]);
     }
     // ---- finish the work item: denominators of the lane's two heads over all rows
 #pragma unroll

@@ -15,7 +15,7 @@
 // off the sums.  The last CTA of a cache to finish joins the chunks (in their order, so the result does not depend on who that is)
 // and sets the ticket back to zero.
 // Weights are rounded to 16 bits for their product: half a step, 2^-8 of a weight in bf16, 2^-11 of weight times row scale in fp16, and
-// below 2^-14 of the largest such product of a row that has a value 2^-25 (see ProductRef); sums, maxima and outputs are fp32.
+// below 2^-14 of the largest such product of a row that has a value 2^-25 (see scale_share); sums, maxima and outputs are fp32.
 // Measured, device time: 16 caches of 49 - 146 rows of 64 7.4 us (floor 0.1: latencies of ids, rows, barriers and the launch); 2048 caches,
 // 1.66 GB of bf16 rows 264 us = 6.3 TB/s, HBM; int8, one head a KV head, 338 MB 65 us = 5.2 TB/s, the chains
 // of latencies at a CTA's two ends (loads take 36 % of L1's cycles, instructions 47 % of the issue slots).
@@ -237,7 +237,6 @@ __global__ void __launch_bounds__(32 * W, ctas_of_an_sm(D, W)) diff_decode_rows_
     }
   }
   float m[2] = {-INFINITY, -INFINITY}, l[2] = {0.f, 0.f};     // of query rows 2 tig and 2 tig + 1; l: of this lane's rows
-  ProductRef ref;                                             // 8-bit rows: of the products with V
   float o[D / 16][4];
 #pragma unroll
   for (int x = 0; x < D / 16; ++x) o[x][0] = o[x][1] = o[x][2] = o[x][3] = 0.f;
@@ -278,15 +277,18 @@ __global__ void __launch_bounds__(32 * W, ctas_of_an_sm(D, W)) diff_decode_rows_
           }
         }
     }
-    // the warp's references are exact on its first tile and raised lazily (by 2^8) afterwards; 8-bit rows: that of the products as well
-    float top[2] = {fmaxf(z[0], z[2]), fmaxf(z[1], z[3])}, ptop[2] = {-INFINITY, -INFINITY};
-    bool grow = top[0] > m[0] + kLazy || top[1] > m[1] + kLazy;
-    if constexpr (Q8) {
-      const float b0 = __log2f(vs[0]), b1 = __log2f(vs[1]);
-      ptop[0] = fmaxf(z[0] + b0, z[2] + b1), ptop[1] = fmaxf(z[1] + b0, z[3] + b1);
-      grow = grow || ptop[0] > ref.mp[0] + kLazy || ptop[1] > ref.mp[1] + kLazy;
-    }
-    if (__any_sync(0xffffffffu, grow)) {
+    // the warp's reference is exact on its first tile and raised lazily (by 2^8) afterwards
+    float top[2];
+    auto tops = [&] {
+      if constexpr (Q8) {
+        const float b0 = scale_share(vs[0]), b1 = scale_share(vs[1]);
+        top[0] = fmaxf(z[0] + b0, z[2] + b1), top[1] = fmaxf(z[1] + b0, z[3] + b1);
+      } else {
+        top[0] = fmaxf(z[0], z[2]), top[1] = fmaxf(z[1], z[3]);
+      }
+    };
+    tops();
+    if (__any_sync(0xffffffffu, top[0] > m[0] + kLazy || top[1] > m[1] + kLazy)) {
       float al[2];
       if constexpr (Q8) {
 #pragma unroll
@@ -296,22 +298,17 @@ __global__ void __launch_bounds__(32 * W, ctas_of_an_sm(D, W)) diff_decode_rows_
           for (int j = 0; j < kPieces; ++j) x |= (v[y].x[j][0] ^ 0x80808080u) | (v[y].x[j][1] ^ 0x80808080u);
           if (!row_has_value(x)) vs[y] = 0.f;
         }
-        const float b0 = __log2f(vs[0]), b1 = __log2f(vs[1]);
-        ptop[0] = fmaxf(z[0] + b0, z[2] + b1), ptop[1] = fmaxf(z[1] + b0, z[3] + b1);
+        tops();
       }
 #pragma unroll
       for (int i = 0; i < 2; ++i) {
 #pragma unroll
-        for (int x = 4; x < 32; x <<= 1) {
-          top[i] = fmaxf(top[i], __shfl_xor_sync(0xffffffffu, top[i], x));
-          if constexpr (Q8) ptop[i] = fmaxf(ptop[i], __shfl_xor_sync(0xffffffffu, ptop[i], x));
-        }
+        for (int x = 4; x < 32; x <<= 1) top[i] = fmaxf(top[i], __shfl_xor_sync(0xffffffffu, top[i], x));
         top[i] = fmaxf(top[i], m[i]);
         al[i] = m[i] == -INFINITY ? 0.f : fast_exp2(m[i] - top[i]);
         m[i] = top[i];
         l[i] *= al[i];
       }
-      if constexpr (Q8) ref.raise(m, ptop, al);
 #pragma unroll
       for (int x = 0; x < D / 16; ++x) {
         o[x][0] *= al[0];
@@ -330,7 +327,7 @@ __global__ void __launch_bounds__(32 * W, ctas_of_an_sm(D, W)) diff_decode_rows_
     // the weights as the B operand (rounded to 16 bits, 8-bit rows: times the row's scale)
     if constexpr (Q8) {
 #pragma unroll
-      for (int i = 0; i < 4; ++i) w[i] *= ref.f[i & 1] * vs[i >> 1];
+      for (int i = 0; i < 4; ++i) w[i] *= vs[i >> 1];
     }
     const uint32_t b0 = movmatrix_trans(pack16<Q8>(w[0], w[1])), b1 = movmatrix_trans(pack16<Q8>(w[2], w[3]));
 #pragma unroll
@@ -355,7 +352,6 @@ __global__ void __launch_bounds__(32 * W, ctas_of_an_sm(D, W)) diff_decode_rows_
   for (int i = 0; i < 2; ++i)
 #pragma unroll
     for (int x = 4; x < 32; x <<= 1) l[i] += __shfl_xor_sync(0xffffffffu, l[i], x);
-  const float back[2] = {ref.back(0, m[0]), ref.back(1, m[1])};
   // accumulator row gid of block (j, i) is column 4 i + gid % 2 of piece j of lane gid / 2, row gid + 8 the one 2 further; 8-bit rows:
   // + 2 (gid % 2), and the next one
 #pragma unroll
@@ -363,7 +359,7 @@ __global__ void __launch_bounds__(32 * W, ctas_of_an_sm(D, W)) diff_decode_rows_
 #pragma unroll
     for (int i = 0; i < 4; ++i) {
       const int col = Part::column(gid >> 1, x >> 1) + 4 * (x & 1) + (Q8 ? 2 * (gid & 1) + (i >> 1) : 2 * (i >> 1) + (gid & 1));
-      s_o[warp][2 * tig + (i & 1)][Out::at(col)] = Q8 ? fmaf(-kInt8Bias, w_sum[i], o[x][i]) * back[i & 1] : o[x][i];
+      s_o[warp][2 * tig + (i & 1)][Out::at(col)] = Q8 ? fmaf(-kInt8Bias, w_sum[i], o[x][i]) : o[x][i];
     }
   if (gid == 0) {
 #pragma unroll
