@@ -212,7 +212,8 @@ xkv_status xkv_score(const xkv_dims* dims, const void* q_win, const void* k,
  * For every sequence b, query head h and position i < t_b:
  *   out[i,h,:] = softmax over the keys c <= i of scale * q[i,h,:] . k[c,g,:]  times  v[c,g,:]     (g = h / G)
  *   lse[h][i]  = natural log of the sum over c <= i of exp(scale * q[i,h,:] . k[c,g,:])
- * bf16 inputs, fp32 accumulation, the weights rounded to bf16 before they multiply v, bf16 output.
+ * bf16 inputs, fp32 accumulation, the weights rounded to bf16 before they multiply v, bf16 output. A prompt longer than
+ * max_seqlen is processed as if cut to it (no device status: xkv_score reports it).
  * The lse entries of the last W positions of a sequence are the normalisers of the observation-window rows
  * of W_attn; xkv_score_lse takes them instead of recomputing them with a pass over the keys.
  *
@@ -245,7 +246,10 @@ xkv_status xkv_prefill_attn(const xkv_dims* dims, const void* q, const void* k, 
  * workspace  dev, at least xkv_workspace_bytes(XKV_OP_DIFF_PREFILL_ATTN, ...) bytes (the status word), 256-byte aligned
  * bf16 inputs, fp32 accumulation, difference and norm, the weights rounded to bf16 before they multiply v, bf16 output. A value v
  * that is not finite also reaches rows of its own sequence up to 127 positions before it (0 * v), never another sequence's.
- * Everything else as in xkv_prefill_attn.
+ * Everything else as in xkv_prefill_attn; but its lse is not one that xkv_score_lse takes: the importance scores of this library are
+ * those of ordinary maps of the whole row, softmax(scale * q . k), which a differential head does not have. Caches that are evicted by
+ * them are read by xkv_diff_decode_attn as they are; whether the rows that they keep are the ones such a model needs is the caller's
+ * to judge (budgets and pages work the same for rows kept by any other choice).
  */
 xkv_status xkv_diff_prefill_attn(const xkv_dims* dims, const void* q, const void* k, const void* v, const float* lambda,
                                  const float* gain, float eps, const int32_t* cu_seqlens, int64_t total_tokens,
@@ -561,7 +565,9 @@ xkv_status xkv_decode_attn(const xkv_dims* dims, const xkv_cache* cache, int32_t
  * lse        dev out fp32 [Lr][B][Hq][2], may be NULL: of each map
  * workspace  dev, at least xkv_workspace_bytes(XKV_OP_DIFF_DECODE_ATTN, ...) bytes
  * Everything else (q, k_new, v_new, the append, out, chunk_rows, statuses, limits, rows of empty caches) as in xkv_decode_attn. The
- * difference, its norm and everything before them are fp32; weights are rounded as there.
+ * difference, its norm (its sum of squares included) and everything before them are fp32; weights are rounded as there, of int8 rows
+ * relative to the largest product of a weight and its row's V scale among rows that have a value, so that neither scales far from 1 nor
+ * rows of zeros cost the others bits. A cached K row with an element that is not finite makes both maps NaN, whichever half it is in.
  * Launches: with chunk_rows = 0 a bf16 or int8 cache whose pages start on 32 bytes is read by a kernel that plans nothing (one
  * launch, one more for new rows, a memset where more than 48 caches of a KV head are cut up); calls with chunk_rows and XKV_KV_E4M3
  * caches take the launches of xkv_decode_attn. The kernels add in different orders: their results agree within the

@@ -17,8 +17,9 @@
 // Weights are rounded to 16 bits for their product: half a step, 2^-8 of a weight in bf16, 2^-11 of weight times row scale in fp16, and
 // below 2^-14 of the largest such product of a row that has a value 2^-25 (see scale_share); sums, maxima and outputs are fp32.
 // Measured, device time: 16 caches of 49 - 146 rows of 64 7.4 us (floor 0.1: latencies of ids, rows, barriers and the launch); 2048 caches,
-// 1.66 GB of bf16 rows 264 us = 6.3 TB/s, HBM; int8, one head a KV head, 338 MB 65 us = 5.2 TB/s, the chains
-// of latencies at a CTA's two ends (loads take 36 % of L1's cycles, instructions 47 % of the issue slots).
+// 1.66 GB of bf16 rows 264 us = 6.3 TB/s, HBM; int8, one head a KV head, 338 MB 65 to 67 us = 5.1 TB/s, the chains
+// of latencies at a CTA's two ends (loads take 36 % of L1's cycles, instructions 47 % of the issue slots).  bf16 rows of 128 spill 48 bytes a
+// thread at their 128 registers.
 #include <algorithm>
 
 #include "common.cuh"
@@ -529,9 +530,11 @@ Cut cut(const xkv_dims& streamed, const xkv_cache& cache, int n_layers, int64_t 
 }  // namespace
 
 // Whether this kernel or the streaming one takes a call without chunk_rows.  Device time of both, us (rows of 128, G = 4 unless said):
-//   bf16: 8 caches of 2129 rows 12.2 / 28.8, 64 of 2000 20.5 / 36.4, 2048 of 120 34.9 / 35.5, of 1000 177 / 215, 4096 of 1500 472 / 575;
-//   G = 1: 2048 of 1000 173 / 180
-//   int8, the same: 11.7 / 46.8, 18.6 / 50.1, 22.6 / 41.5, 102 / 152, 260 / 403;  G = 1: 98 / 142
+//   bf16: 8 caches of 2129 rows 12.3 / 31.0, 64 of 2000 20.6 / 36.6, 2048 of 120 37.5 / 38.3, of 1000 177 / 218, 4096 of 1500 475 / 585;
+//   G = 1: 2048 of 1000 175 / 191
+//   int8, the same: 11.6 / 48.6, 18.6 / 52.1, 23.7 / 45.2, 103 / 155, 269 / 427;  G = 1: 101 / 146
+// Not so where one cache is much longer than the others in tables of up to 12 288 rows, which this kernel does not cut: 512 caches of
+// 200 - 1000 rows and one sequence of 12 000 195 / 89, int8 171 / 91.
 bool diff_decode_by_rows(const xkv_dims* streamed, const xkv_cache* c, int n_layers, int64_t max_rows) {
   if (c->kv_format == XKV_KV_E4M3 || ((reinterpret_cast<uintptr_t>(c->k_pages) | reinterpret_cast<uintptr_t>(c->v_pages)) & 31u) != 0)
     return false;                     // (a run is one load)

@@ -15,7 +15,7 @@
 // two such buffers, or one of 128 keys: the chain weights - product - logits is then in the way, 980 and 1010 us for the largest case.)
 //   warps 0-3  softmax of map 1, warps 4-7 of map 2: thread = query row = tensor-memory lane.  A row's 64 logits leave tensor memory
 //              once; the reference maximum is exact on the first tile and raised lazily (by 2^8) afterwards, which is when O_s is
-//              rescaled; P_s goes back as bf16 pairs over the tile's logits, the A operand of O_s += P_s V.  At the end of an item
+//              rescaled; P_s goes back as bf16 pairs to one of its two buffers, the A operand of O_s += P_s V.  At the end of an item
 //              each map's warps take half of the columns of both O_1 and O_2.
 //   warp 8     Q tiles (two buffers, so that the next item's logits start under this item's last products) and K tiles by TMA
 //   warps 9, 10   issue the logits of map 1 and of map 2, warps 12, 13 the outputs (a warp of its own each: what runs once a tile runs out
@@ -25,10 +25,11 @@
 // Every wait is bounded and ends when another role has given up; an expired one sets the status word and lets the CTA drain.
 //
 // Measured (device time, clock under the power limit 1.65 - 1.8 GHz): four prompts of 2399 - 4428 tokens, 32 heads of 128 over 8 KV heads 864
-// us = 840 TFLOP/s (830 to 864 from GPU to GPU); one of 32 768 tokens, 8 heads 1020 TFLOP/s; one of 487 tokens, 4 heads of 64 13.4 us.  What bounds it is the issue of
-// the softmax, at d = 64 as at 128: 1550 clocks a tile where the tensor pipe would take 896 and the exponentials 1024, two warps
-// an SM sub-partition, and some 7000 clocks at an item's end, when the tensor pipe has nothing to do (the same warps form the output;
-// four warps of their own for it left the softmax 96 registers a thread instead of 128: 1010 us).
+// us = 840 TFLOP/s (773 to 884 from GPU to GPU); one of 32 768 tokens, 8 heads 1020 TFLOP/s; one of 487 tokens, 4 heads of 64 13.4 us.  What bounds it is
+// latency in the softmax, at d = 64 as at 128 (four prompts of 4096 tokens, 32 heads: 755 and 934 us): 1550 clocks a tile where the
+// tensor pipe would take 896 and the exponentials 1024, since two warps an SM sub-partition do not cover each other's waits (issue
+// slots 42 % taken, exponentials 59 %, tensor pipe 44 %), and some 7000 clocks at an item's end, when the tensor pipe has nothing to do (the
+// same warps form the output; four warps of their own for it left the softmax 96 registers a thread instead of 128: 1010 us).
 #include <atomic>
 
 #include "ops.h"

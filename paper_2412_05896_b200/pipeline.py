@@ -245,7 +245,8 @@ class XkvSession:
                                gain: torch.Tensor | None = None, eps: float = 1e-5, out: torch.Tensor | None = None,
                                lse: torch.Tensor | None = None):
         """prefill_attention of heads that attend by the difference of two softmax maps: rows of q [q1 | q2], of k
-        [k1 | k2]; lam fp32 [Hq], gain fp32 [d] (the heads' norm) or None -> (out [T, Hq, d] bf16, lse [Hq, 2, T] fp32)."""
+        [k1 | k2]; lam fp32 [Hq], gain fp32 [d] (the heads' norm) or None -> (out [T, Hq, d] bf16, lse [Hq, 2, T] fp32).  The lse
+        is not for score_layer: there are no scores of differential heads (see diff_decode)."""
         self._check_diff(lam, gain, (self.Hq,), (self.d,))
         if out is None:
             out = torch.empty_like(q)
@@ -511,7 +512,9 @@ class XkvSession:
                     lse: torch.Tensor | None = None, layer_begin: int = 0, layer_end: int | None = None,
                     chunk_rows: int | None = None) -> torch.Tensor:
         """decode of heads that attend by the difference of two softmax maps: q rows [q1 | q2], cached K rows [k1 | k2];
-        lam fp32 [layers, Hq], gain fp32 [layers, d] (the heads' norm) or None, lse fp32 [layers, B, Hq, 2]."""
+        lam fp32 [layers, Hq], gain fp32 [layers, d] (the heads' norm) or None, lse fp32 [layers, B, Hq, 2].
+        It reads the caches as they are.  The rows that prefill keeps are chosen by scores of ordinary maps of the whole row,
+        softmax(scale * q . k), which a differential head does not have; a budget of a whole prompt keeps every row."""
         if self.head_level:
             raise ValueError("diff_decode: lam is given per head of a layer, head-level caches are read as sequences of their own")
         self.join()
@@ -559,7 +562,8 @@ class XkvSession:
         cache), sharing its pages; -1 frees it.  keep: rows of a cache that stay, [B] or [L, B], negative: all.  Host
         integers or dev int32 tensors.  A freed sequence takes no part in later steps until it goes on as another one or
         append gives it rows -- where parent is host integers: a tensor is not read here, and then every sequence takes part
-        (a freed one begins again with the next step's row).  Needs pages_on_demand; device_status("pages")."""
+        (a freed one begins again with the next step's row).  A captured step keeps the sequences that it was captured with.
+        Needs pages_on_demand; device_status("pages")."""
         if not self.pages_on_demand:
             raise ValueError("fork needs a session with pages_on_demand=True")
         live = [True] * self.B
