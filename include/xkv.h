@@ -471,8 +471,9 @@ xkv_status xkv_store_rows(const xkv_dims* dims, const xkv_cache* cache, const vo
  * workspace     dev, at least xkv_workspace_bytes(XKV_OP_FORK_CACHES, ...) bytes, 256-byte aligned
  * Table entries behind a cache's last page, and rows of a new page behind its last row, stay as they are. A cache that needs a page
  * when the list has ended keeps its whole pages only: device status XKV_ERR_CAPACITY. Page ids outside [0, n_pages) in used
- * entries are not counted, and counters that do not agree with the tables leave a page where it is: device status
- * XKV_ERR_INVALID_ARG. At most 16384 caches a layer.
+ * entries are not counted, and a page that is dropped more often than its counter says it is held goes to the list once: device
+ * status XKV_ERR_INVALID_ARG. The counters are not compared with the tables: where they are too high a page stays out of the list,
+ * where they are too low it is returned while an entry still has it. At most 16384 caches a layer.
  */
 xkv_status xkv_fork_caches(const xkv_dims* dims, const xkv_cache* cache, const int32_t* parent, const int32_t* keep,
                            int32_t keep_stride, int32_t* shares, int32_t* free_pages, int32_t n_free, int32_t* pages_used,
